@@ -260,6 +260,77 @@ int32_t layer_qkv_publish(ca_ctx* ctx, int32_t n_blocks, const int64_t* block_id
                           int32_t prompt_epoch, const void* x_dev, int64_t ldx, const void* w_qkv_dev,
                           int64_t ldw, int32_t k_in, void* q_out_dev, void* hip_stream, int32_t* slots_out);
 
+/* ---- The rest of a layer.  The paper gives none of the generator's internals; these are the operators that DiT layers in use have
+ * around the attention: norms of queries and keys, 8-bit projections, a gated feed-forward block.  Conventions as above; calls that
+ * need device memory of their own take it from the caller, aligned to 16 bytes, and keep nothing in it. */
+
+/* Queries or keys of some tokens: [token, heads, head_dim], heads and head_dim the context's, strides in elements. */
+typedef struct {
+  void* dev;
+  int64_t tok_stride, head_stride;
+} ca_heads;
+
+/* Per-head RMS norm and the rotation of rope3d_apply in one pass: of each head's head_dim values x,
+ * y = weight * x / sqrt(mean(x^2) + eps), then y rotated by its token's position.  n_tokens tokens that are consecutive in the
+ * video, from the first token of latent frame first_frame on.  q or k may be null (with the outputs and weights that belong to
+ * it); both go in one launch.  Weights: head_dim values of the context's type.  In fp32, rounded once.  An output may be its
+ * own input (then with its strides) and overlaps nothing else.  eps >= 0; a head of zeros gives zeros for eps > 0. */
+int32_t layer_qk_norm_rope(const ca_ctx* ctx, const ca_heads* q, const ca_heads* k, const void* q_weight_dev, const void* k_weight_dev,
+                           float eps, const ca_heads* q_out, const ca_heads* k_out, int64_t n_tokens, int64_t first_frame,
+                           void* hip_stream);
+
+/* Its gradients: from those of the outputs (dq_out, dk_out) those of the inputs (dq, dk; each may be its dq_out / dk_out) and of the
+ * weights (fp32, head_dim values, written, not added to; summed over tokens and heads in an order that the sizes fix).  q and
+ * k are the forward's inputs.  workspace_dev: layer_qk_norm_rope_workspace(ctx) bytes.  n_tokens == 0: zero weight gradients. */
+size_t layer_qk_norm_rope_workspace(const ca_ctx* ctx);
+int32_t layer_qk_norm_rope_backward(const ca_ctx* ctx, const ca_heads* dq_out, const ca_heads* dk_out, const ca_heads* q, const ca_heads* k,
+                                    const void* q_weight_dev, const void* k_weight_dev, float eps, const ca_heads* dq, const ca_heads* dk,
+                                    float* dq_weight_dev, float* dk_weight_dev, int64_t n_tokens, int64_t first_frame, void* workspace_dev,
+                                    size_t workspace_bytes, void* hip_stream);
+
+/* kv_cache_append_batch with each head of K normed ahead of its rotation, on its way into the pages: the pages hold
+ * the bits of layer_qk_norm_rope's keys.  Needs a pool (CA_ENOPOOL). */
+int32_t kv_cache_append_batch_norm(ca_ctx* ctx, int32_t n_blocks, const int64_t* block_ids, const int32_t* timesteps, int32_t prompt_epoch,
+                                   const void* const* k_dev, const void* const* v_dev, int64_t tok_stride, int64_t head_stride,
+                                   const void* k_weight_dev, float eps, void* hip_stream, int32_t* slots_out);
+
+/* Rows of x (CA_BF16 or CA_F32) in 8 bits with a scale each: scale = (largest magnitude) / 127, code = 127 x / (largest magnitude)
+ * rounded half to even, as exact arithmetic gives it.  A row of zeros has scale 0 and codes 0; one that holds an infinity or
+ * NaN has scale NaN and codes 0.  Codes behind k_in, up to the next multiple of 256, are written as zeros: a row of codes takes
+ * ld_codes >= that many bytes (a multiple of 16).  x: any alignment and row stride (16-byte aligned rows are read faster). */
+#define CA_I8_MAX_K (1 << 17)    /* 127 * 127 * 2^17 < 2^31: sums of products are exact */
+int32_t layer_quantize_rows_i8(const void* x_dev, int32_t dtype, int8_t* codes_dev, float* scales_dev, int64_t rows, int32_t k_in,
+                               int64_t ldx, int64_t ld_codes, void* hip_stream);
+
+/* The linear map in 8 bits: y[m][n] = (sum_k x_codes[m][k] * w_codes[n][k]) * x_scales[m] * w_scales[n], whole sums in 32 bits, scaled in
+ * fp32, rounded to bf16 once.  Codes as layer_quantize_rows_i8 leaves them (zeros behind k_in), weights with a scale for each output
+ * channel.  n_out a multiple of 8 (ldy too, in elements; ldx and ldw in bytes); m_rows and k_in <= CA_I8_MAX_K are free.  The
+ * result does not depend on the size of the call's tiles. */
+int32_t layer_linear_i8(const int8_t* x_codes_dev, const float* x_scales_dev, const int8_t* w_codes_dev, const float* w_scales_dev,
+                        void* y_dev, int64_t m_rows, int32_t n_out, int32_t k_in, int64_t ldx, int64_t ldw, int64_t ldy,
+                        void* hip_stream);
+
+/* The first half of a gated feed-forward block, both projections, activation and product in one kernel:
+ * h = act(g) * u, g = x . w_gate', u = x . w_up', in bf16 with fp32 accumulation; g and u are rounded nowhere on the way to h, h once.
+ * CA_SILU: g / (1 + exp(-g)); CA_GELU: g (1 + tanh(sqrt(2/pi) (g + 0.044715 g^3))) / 2.  With g_dev and u_dev (both or neither)
+ * the projections are written as well, in bf16, for the backward pass.  w_gate, w_up: [n_hidden, k_in]; shapes as layer_linear_bf16
+ * (n_hidden a multiple of 8, k_in of 128). */
+enum { CA_SILU = 0, CA_GELU = 1 };
+int32_t layer_gated_bf16(const void* x_dev, const void* w_gate_dev, const void* w_up_dev, void* h_dev, void* g_dev, void* u_dev,
+                         int32_t activation, int64_t m_rows, int32_t n_hidden, int32_t k_in, int64_t ldx, int64_t ldw_gate, int64_t ldw_up,
+                         int64_t ldh, int64_t ld_saved, void* hip_stream);
+
+/* Its gradients: dg = dh u act'(g), du = dh act(g) (rounded to bf16); dx = dg . w_gate + du . w_up, dw_gate = dg' . x, dw_up = du' . x, each
+ * rounded to bf16 once, written, not added to.  dx_dev, dw_gate_dev, dw_up_dev: those that are null are left out (not all).  g and u
+ * as layer_gated_bf16 wrote them.  workspace_dev: layer_gated_backward_workspace() bytes, 0 where the shape is not supported.
+ * m_rows == 0: zero weight gradients. */
+size_t layer_gated_backward_workspace(int64_t m_rows, int32_t n_hidden, int32_t k_in);
+int32_t layer_gated_backward_bf16(const void* dh_dev, const void* x_dev, const void* w_gate_dev, const void* w_up_dev, const void* g_dev,
+                                  const void* u_dev, int32_t activation, void* dx_dev, void* dw_gate_dev, void* dw_up_dev, int64_t m_rows,
+                                  int32_t n_hidden, int32_t k_in, int64_t lddh, int64_t ldx, int64_t ldw_gate, int64_t ldw_up,
+                                  int64_t ld_saved, int64_t lddx, int64_t lddw, void* workspace_dev, size_t workspace_bytes,
+                                  void* hip_stream);
+
 /* ---- Cascade scheduler: the control flow of Algorithm 1, host integers only.
  * State (b, tau, d) = primary block, timestep index of the primary block, cascade depth.  An
  * iteration forwards blocks b .. b + min(d, G-1), block b+i at timesteps[tau - i] (older blocks

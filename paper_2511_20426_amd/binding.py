@@ -26,6 +26,8 @@ CA_OK, CA_EINVAL, CA_ENOSPC, CA_ENOENT, CA_ESTATE, CA_EUNSUPPORTED, CA_ENOPOOL, 
 CA_F32, CA_BF16 = 0, 1
 CA_BIDIRECTIONAL, CA_BLOCK_CAUSAL = 0, 1
 CA_FREE, CA_NOISY, CA_CLEAN, CA_SINK = 0, 1, 2, 3
+CA_SILU, CA_GELU = 0, 1
+CA_I8_MAX_K = 1 << 17
 
 # every symbol include/cascade_attn.h declares
 EXPORTS = (
@@ -34,6 +36,8 @@ EXPORTS = (
     "rope3d_apply", "rope3d_apply_strided", "cascade_attn_forward", "cascade_attn_forward_share", "cascade_attn_forward_static", "cascade_attn_forward_rope", "ca_debug_visibility", "ca_set_kernel_variant",
     "ca_strerror", "ca_last_device_error",
     "ca_mfma_microbench", "layer_linear_bf16", "layer_qkv_publish",
+    "layer_qk_norm_rope", "layer_qk_norm_rope_workspace", "layer_qk_norm_rope_backward", "kv_cache_append_batch_norm", "layer_quantize_rows_i8",
+    "layer_linear_i8", "layer_gated_bf16", "layer_gated_backward_workspace", "layer_gated_backward_bf16",
     "ca_sched_create", "ca_sched_create_lagged", "ca_sched_destroy", "ca_sched_batch", "ca_sched_advance", "ca_sched_state",
 )
 
@@ -52,6 +56,10 @@ class ca_config(C.Structure):
 class ca_slot_info(C.Structure):
     _fields_ = [("slot", C.c_int32), ("state", C.c_int32), ("block_id", C.c_int64),
                 ("timestep", C.c_int32), ("prompt_epoch", C.c_int32)]
+
+
+class ca_heads(C.Structure):
+    _fields_ = [("dev", C.c_void_p), ("tok_stride", C.c_int64), ("head_stride", C.c_int64)]
 
 
 class ca_sched_entry(C.Structure):
@@ -135,6 +143,26 @@ def _load() -> C.CDLL:
     lib.layer_qkv_publish.restype = i32
     lib.layer_qkv_publish.argtypes = [vp, i32, C.POINTER(i64), C.POINTER(i32), i32, vp, i64, vp, i64, i32, vp, vp,
                                       C.POINTER(i32)]
+    hp, f32 = C.POINTER(ca_heads), C.c_float
+    lib.layer_qk_norm_rope.restype = i32
+    lib.layer_qk_norm_rope.argtypes = [vp, hp, hp, vp, vp, f32, hp, hp, i64, i64, vp]
+    lib.layer_qk_norm_rope_workspace.restype = C.c_size_t
+    lib.layer_qk_norm_rope_workspace.argtypes = [vp]
+    lib.layer_qk_norm_rope_backward.restype = i32
+    lib.layer_qk_norm_rope_backward.argtypes = [vp, hp, hp, hp, hp, vp, vp, f32, hp, hp, vp, vp, i64, i64, vp, C.c_size_t, vp]
+    lib.kv_cache_append_batch_norm.restype = i32
+    lib.kv_cache_append_batch_norm.argtypes = [vp, i32, C.POINTER(i64), C.POINTER(i32), i32, C.POINTER(vp), C.POINTER(vp), i64, i64, vp, f32,
+                                               vp, C.POINTER(i32)]
+    lib.layer_quantize_rows_i8.restype = i32
+    lib.layer_quantize_rows_i8.argtypes = [vp, i32, vp, vp, i64, i32, i64, i64, vp]
+    lib.layer_linear_i8.restype = i32
+    lib.layer_linear_i8.argtypes = [vp, vp, vp, vp, vp, i64, i32, i32, i64, i64, i64, vp]
+    lib.layer_gated_bf16.restype = i32
+    lib.layer_gated_bf16.argtypes = [vp] * 6 + [i32, i64, i32, i32] + [i64] * 5 + [vp]
+    lib.layer_gated_backward_workspace.restype = C.c_size_t
+    lib.layer_gated_backward_workspace.argtypes = [i64, i32, i32]
+    lib.layer_gated_backward_bf16.restype = i32
+    lib.layer_gated_backward_bf16.argtypes = [vp] * 6 + [i32] + [vp] * 3 + [i64, i32, i32] + [i64] * 7 + [vp, C.c_size_t, vp]
     lib.ca_sched_create.restype = i32
     lib.ca_sched_create.argtypes = [i64, i32, C.POINTER(i32), i32, C.POINTER(vp)]
     lib.ca_sched_create_lagged.restype = i32
@@ -353,6 +381,37 @@ class Context:
         m = n_kv.value
         return [[int(vis[i * m + r]) for r in range(m)] for i in range(n)], [int(kv[r]) for r in range(m)]
 
+    # the rest of a layer; a view of queries or keys is (address, token stride, head stride) or None
+    def kv_cache_append_batch_norm(self, block_ids: Sequence[int], timesteps: Sequence[int], prompt_epoch: int,
+                                   k_ptrs: Sequence[int], v_ptrs: Sequence[int], tok_stride: int, head_stride: int,
+                                   k_weight_ptr: int, eps: float, stream: int = 0) -> List[int]:
+        n = len(block_ids)
+        assert len(timesteps) == n and len(k_ptrs) == n and len(v_ptrs) == n
+        ids = (C.c_int64 * n)(*block_ids)
+        ts = (C.c_int32 * n)(*timesteps)
+        kp = (C.c_void_p * n)(*[index(p or 0) or None for p in k_ptrs])
+        vp = (C.c_void_p * n)(*[index(p or 0) or None for p in v_ptrs])
+        slots = (C.c_int32 * max(n, 1))()
+        _check(lib.kv_cache_append_batch_norm(self._h, n, ids, ts, prompt_epoch, kp, vp, tok_stride, head_stride,
+                                              index(k_weight_ptr or 0), eps, index(stream or 0), slots), "kv_cache_append_batch_norm")
+        return [int(slots[i]) for i in range(n)]
+
+    def layer_qk_norm_rope(self, q, k, q_weight_ptr: int, k_weight_ptr: int, eps: float, q_out, k_out, n_tokens: int,
+                           first_frame: int, stream: int = 0) -> None:
+        _check(lib.layer_qk_norm_rope(self._h, _heads(q), _heads(k), index(q_weight_ptr or 0), index(k_weight_ptr or 0), eps,
+                                      _heads(q_out), _heads(k_out), n_tokens, first_frame, index(stream or 0)), "layer_qk_norm_rope")
+
+    def layer_qk_norm_rope_workspace(self) -> int:
+        return int(lib.layer_qk_norm_rope_workspace(self._h))
+
+    def layer_qk_norm_rope_backward(self, dq_out, dk_out, q, k, q_weight_ptr: int, k_weight_ptr: int, eps: float, dq, dk,
+                                    dq_weight_ptr: int, dk_weight_ptr: int, n_tokens: int, first_frame: int, workspace_ptr: int,
+                                    workspace_bytes: int, stream: int = 0) -> None:
+        _check(lib.layer_qk_norm_rope_backward(self._h, _heads(dq_out), _heads(dk_out), _heads(q), _heads(k), index(q_weight_ptr or 0),
+                                               index(k_weight_ptr or 0), eps, _heads(dq), _heads(dk), index(dq_weight_ptr or 0),
+                                               index(dk_weight_ptr or 0), n_tokens, first_frame, index(workspace_ptr or 0),
+                                               workspace_bytes, index(stream or 0)), "layer_qk_norm_rope_backward")
+
     def set_kernel_variant(self, variant: int) -> None:
         _check(lib.ca_set_kernel_variant(self._h, variant), "ca_set_kernel_variant")
 
@@ -360,6 +419,43 @@ class Context:
 def layer_linear_bf16(x_ptr: int, w_ptr: int, y_ptr: int, m_rows: int, n_out: int, k_in: int,
                       ldx: int, ldw: int, ldy: int, stream: int = 0) -> None:
     _check(lib.layer_linear_bf16(x_ptr, w_ptr, y_ptr, m_rows, n_out, k_in, ldx, ldw, ldy, stream), "layer_linear_bf16")
+
+
+def _heads(view):
+    return None if view is None else C.byref(ca_heads(index(view[0] or 0) or None, view[1], view[2]))
+
+
+def layer_quantize_rows_i8(x_ptr: int, dtype: int, codes_ptr: int, scales_ptr: int, rows: int, k_in: int, ldx: int, ld_codes: int,
+                           stream: int = 0) -> None:
+    _check(lib.layer_quantize_rows_i8(index(x_ptr or 0), dtype, index(codes_ptr or 0), index(scales_ptr or 0), rows, k_in, ldx, ld_codes,
+                                      index(stream or 0)), "layer_quantize_rows_i8")
+
+
+def layer_linear_i8(x_codes_ptr: int, x_scales_ptr: int, w_codes_ptr: int, w_scales_ptr: int, y_ptr: int, m_rows: int, n_out: int,
+                    k_in: int, ldx: int, ldw: int, ldy: int, stream: int = 0) -> None:
+    _check(lib.layer_linear_i8(index(x_codes_ptr or 0), index(x_scales_ptr or 0), index(w_codes_ptr or 0), index(w_scales_ptr or 0),
+                               index(y_ptr or 0), m_rows, n_out, k_in, ldx, ldw, ldy, index(stream or 0)), "layer_linear_i8")
+
+
+def layer_gated_bf16(x_ptr: int, w_gate_ptr: int, w_up_ptr: int, h_ptr: int, g_ptr: int, u_ptr: int, activation: int, m_rows: int,
+                     n_hidden: int, k_in: int, ldx: int, ldw_gate: int, ldw_up: int, ldh: int, ld_saved: int, stream: int = 0) -> None:
+    _check(lib.layer_gated_bf16(index(x_ptr or 0), index(w_gate_ptr or 0), index(w_up_ptr or 0), index(h_ptr or 0), index(g_ptr or 0),
+                                index(u_ptr or 0), activation, m_rows, n_hidden, k_in, ldx, ldw_gate, ldw_up, ldh, ld_saved,
+                                index(stream or 0)), "layer_gated_bf16")
+
+
+def layer_gated_backward_workspace(m_rows: int, n_hidden: int, k_in: int) -> int:
+    return int(lib.layer_gated_backward_workspace(m_rows, n_hidden, k_in))
+
+
+def layer_gated_backward_bf16(dh_ptr: int, x_ptr: int, w_gate_ptr: int, w_up_ptr: int, g_ptr: int, u_ptr: int, activation: int,
+                              dx_ptr: int, dw_gate_ptr: int, dw_up_ptr: int, m_rows: int, n_hidden: int, k_in: int, lddh: int, ldx: int,
+                              ldw_gate: int, ldw_up: int, ld_saved: int, lddx: int, lddw: int, workspace_ptr: int, workspace_bytes: int,
+                              stream: int = 0) -> None:
+    _check(lib.layer_gated_backward_bf16(index(dh_ptr or 0), index(x_ptr or 0), index(w_gate_ptr or 0), index(w_up_ptr or 0),
+                                         index(g_ptr or 0), index(u_ptr or 0), activation, index(dx_ptr or 0), index(dw_gate_ptr or 0),
+                                         index(dw_up_ptr or 0), m_rows, n_hidden, k_in, lddh, ldx, ldw_gate, ldw_up, ld_saved, lddx, lddw,
+                                         index(workspace_ptr or 0), workspace_bytes, index(stream or 0)), "layer_gated_backward_bf16")
 
 
 def mfma_microbench(data_kind: int, trips: int, scratch_ptr: int, scratch_bytes: int, stream: int = 0):

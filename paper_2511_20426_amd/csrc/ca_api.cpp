@@ -8,29 +8,8 @@
 
 namespace {
 
-ca::RopeGeom rope_geom(const ca::CacheMeta& m) {
-  ca::RopeGeom g{};
-  const ca_config& c = m.cfg();
-  for (int i = 0; i < ca::kMaxPairs; ++i) g.freq[i] = m.rope_freq()[i];
-  g.pairs_t = c.rope_dim_t / 2;
-  g.pairs_h = c.rope_dim_h / 2;
-  g.grid_h = c.grid_h;
-  g.grid_w = c.grid_w;
-  g.heads = c.heads;
-  g.head_dim = c.head_dim;
-  return g;
-}
-
-// A [token, head, dim] view must address whole 8-element groups on 16-byte (bf16) or
-// 32-byte (fp32) boundaries: the kernels move 8 elements at a time.
-bool strides_ok(const ca_config& c, const void* p, int64_t tok_stride, int64_t head_stride) {
-  if (tok_stride < 0 || head_stride < 0) return false;
-  if (head_stride < c.head_dim && c.heads > 1) return false;
-  if (tok_stride < c.head_dim) return false;
-  if ((tok_stride % 8) || (head_stride % 8)) return false;
-  if (reinterpret_cast<uintptr_t>(p) % 16) return false;
-  return true;
-}
+using ca::rope_geom;
+using ca::strides_ok;
 
 }  // namespace
 

@@ -82,6 +82,27 @@ int32_t launch_cache_write(const RopeGeom& g, int dtype, int32_t n_blocks, const
                            const int64_t* first_frame, int32_t block_tokens, int32_t page_tokens,
                            int32_t pages_per_block, const int32_t* slot, void* pool, void* stream);
 
+// The same with each head of K normed ahead of its rotation (norm_weight: head_dim values of the storage type).
+int32_t launch_cache_write_norm(const RopeGeom& g, int dtype, int32_t n_blocks, const void* const* k,
+                                const void* const* v, int64_t tok_stride, int64_t head_stride,
+                                const int64_t* first_frame, int32_t block_tokens, int32_t page_tokens,
+                                int32_t pages_per_block, const int32_t* slot, const void* norm_weight, float norm_eps, void* pool,
+                                void* stream);
+
+// Per-head RMS norm and rotation of queries, keys or both (x null: not these) in one pass, and its gradients.
+struct NormTensors {
+  const void* x;
+  const void* w;                                  // head_dim values of the storage type
+  const void* dz;                                 // backward: gradient of the result
+  void* y;                                        // the result; backward: gradient of x
+  int64_t x_tok, x_head, dz_tok, dz_head, y_tok, y_head;
+};
+int32_t launch_norm_rope(const RopeGeom& g, int dtype, const NormTensors& q, const NormTensors& k, float eps, int64_t n_tokens,
+                         int64_t first_frame, void* stream);
+size_t norm_rope_backward_bytes(int32_t head_dim);
+int32_t launch_norm_rope_backward(const RopeGeom& g, int dtype, const NormTensors& q, const NormTensors& k, float eps, int64_t n_tokens,
+                                  int64_t first_frame, float* dq_weight, float* dk_weight, void* workspace, void* stream);
+
 struct AttnPlan {
   int32_t heads, head_dim, page_tokens, pages_per_block, block_tokens;
   int32_t n_q_blocks;                 // query blocks of this launch; query rows are n_q_blocks * block_tokens
@@ -135,6 +156,29 @@ int32_t gemm_tiles_ready();
 int32_t launch_gemm_qkv_publish(const RopeGeom& g, int32_t n_blocks, int32_t block_tokens, int32_t pages_per_block,
                                 const int32_t* slot, const int64_t* first_frame, const void* x, int64_t ldx,
                                 const void* w, int64_t ldw, int32_t K, void* q_out, void* pool, void* stream);
+// Rows of x (CA_BF16 or CA_F32) brought to 8 bits: codes [rows][ld_codes], zeros from k to the next multiple of 256.
+int32_t launch_quantize_rows(int dtype, const void* x, void* codes, float* scales, int64_t rows, int32_t k, int64_t ldx, int64_t ld_codes,
+                             void* stream);
+// Y = (X . W') * x_scales * w_scales; rows of X and W hold codes up to the next multiple of 256 of K.
+int32_t launch_gemm_i8(const void* x, const float* x_scales, const void* w, const float* w_scales, void* y, int64_t M, int32_t N, int32_t K,
+                       int64_t ldx, int64_t ldw, int64_t ldy, void* stream);
+// H = act(X Wg') * (X Wu'), with g and u (both or neither) the projections themselves as well
+int32_t launch_gemm_gated(const void* x, const void* w_gate, const void* w_up, void* h, void* g, void* u, int activation, int64_t M, int32_t F,
+                          int32_t K, int64_t ldx, int64_t ldwg, int64_t ldwu, int64_t ldh, int64_t ld_saved, void* stream);
+// act(g) = g sigmoid(g (act0 + act1 g^2))
+inline void activation_factors(int activation, float* act0, float* act1) {
+  *act0 = activation == CA_GELU ? 1.5957691216057308f : 1.f;                       // 2 sqrt(2 / pi)
+  *act1 = activation == CA_GELU ? 1.5957691216057308f * 0.044715f : 0.f;
+}
+// Where the backward pass of the gated projections keeps what it multiplies: offsets in bytes.
+struct GatedWorkspace {
+  int64_t Mp, Fp;
+  size_t rows, cols, xt, wt, bytes;
+};
+GatedWorkspace gated_workspace(int64_t M, int32_t F, int32_t K);
+int32_t launch_gated_backward(const void* dh, const void* x, const void* w_gate, const void* w_up, const void* g, const void* u, int activation,
+                              void* dx, void* dw_gate, void* dw_up, int64_t M, int32_t F, int32_t K, int64_t lddh, int64_t ldx, int64_t ldwg,
+                              int64_t ldwu, int64_t ld_saved, int64_t lddx, int64_t lddw, void* workspace, void* stream);
 // Per-device facts and one-time kernel attributes, cached for up to kMaxDevices devices (thread
 // safe: the cached values are idempotent and written with relaxed atomics).
 constexpr int kMaxDevices = 64;
@@ -145,11 +189,39 @@ struct KernelLds {
   const void* kernel;
   int bytes;
 };
-enum LdsSlot { kLdsAttn, kLdsAttnRope, kLdsGemm, kLdsGemmRows, kLdsGemmPublish, kLdsSlots };
+enum LdsSlot { kLdsAttn, kLdsAttnRope, kLdsGemm, kLdsGemmRows, kLdsGemmPublish, kLdsI8, kLdsGated, kLdsSlots };
 int32_t ensure_dynamic_lds(const KernelLds* kernels, int n, LdsSlot slot);   // slot: which set of kernels
 int32_t finish_launch(const char* what);   // launchers end with this: CA_OK, or CA_EDEVICE after recording HIP's last error
 int32_t device_failure(const char* what, int hip_error);   // records the text, clears HIP's last error, returns CA_EDEVICE
 const char* last_device_error();
+
+}  // namespace ca
+
+namespace ca {
+
+inline RopeGeom rope_geom(const CacheMeta& m) {
+  RopeGeom g{};
+  const ca_config& c = m.cfg();
+  for (int i = 0; i < kMaxPairs; ++i) g.freq[i] = m.rope_freq()[i];
+  g.pairs_t = c.rope_dim_t / 2;
+  g.pairs_h = c.rope_dim_h / 2;
+  g.grid_h = c.grid_h;
+  g.grid_w = c.grid_w;
+  g.heads = c.heads;
+  g.head_dim = c.head_dim;
+  return g;
+}
+
+// A [token, head, dim] view must address whole 8-element groups on 16-byte (bf16) or
+// 32-byte (fp32) boundaries: the kernels move 8 elements at a time.
+inline bool strides_ok(const ca_config& c, const void* p, int64_t tok_stride, int64_t head_stride) {
+  if (tok_stride < 0 || head_stride < 0) return false;
+  if (head_stride < c.head_dim && c.heads > 1) return false;
+  if (tok_stride < c.head_dim) return false;
+  if ((tok_stride % 8) || (head_stride % 8)) return false;
+  if (reinterpret_cast<uintptr_t>(p) % 16) return false;
+  return true;
+}
 
 }  // namespace ca
 

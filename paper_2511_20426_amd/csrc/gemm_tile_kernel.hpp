@@ -45,8 +45,18 @@ struct TileArgsOf {
 template <int kThreads, typename Args>
 __device__ void publish_tile(const Args& a, const uint8_t* tile, int col, int blk, int page, int m0, float2* trig, int t, int fill_t, int fill_n);
 
+// the products of a step: 16 bytes of a row of W and of X to a lane
+struct Bf16Products {
+  using Frag = bf16x8;
+  using Sums = f32x4;
+  static __device__ __forceinline__ Sums multiply(const Frag& w, const Frag& x, const Sums& c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(w, x, c, 0, 0, 0);
+  }
+};
+
 template <typename T, bool kPublish>
 __global__ __launch_bounds__(T::kThreads) void gemm_tile_kernel(typename TileArgsOf<kPublish>::type a) {
+  using Products = Bf16Products;
   constexpr int BM = T::kBm, BN = T::kBn, kWavesM = T::kWavesAlongM, kStages = T::kRing;
   extern __shared__ __attribute__((aligned(1024))) uint8_t lds[];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -79,71 +89,8 @@ __global__ __launch_bounds__(T::kThreads) void gemm_tile_kernel(typename TileArg
   }
   uint64_t base_w = reinterpret_cast<uint64_t>(a.w + int64_t(n0) * a.ldw);
   uint64_t base_x = reinterpret_cast<uint64_t>(a.x + int64_t(m0) * a.ldx);
-  const uint32_t lds0 = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(lds));
   const int n_stages = a.K / 64;
-  int issued = 0;
-  uint32_t fill = lds0;                       // ring slot the next stage goes to
-  auto issue = [&]() {
-#pragma unroll
-    for (int i = 0; i < T::kLoadsW; ++i)
-      asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
-                   :: "s"(fill + (wave * T::kLoadsW + i) * 1024), "v"(offw[i]), "s"(base_w) : "memory", "m0");
-#pragma unroll
-    for (int i = 0; i < T::kLoadsX; ++i)
-      asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
-                   :: "s"(fill + BN * 128 + (wave * T::kLoadsX + i) * 1024), "v"(offx[i]), "s"(base_x) : "memory", "m0");
-    // past the last stage the loads repeat it, into slots nothing reads any more: the wait counts stay exact
-    ++issued;
-    base_w += issued < n_stages ? 128 : 0;
-    base_x += issued < n_stages ? 128 : 0;
-    fill += T::kStageBytes;
-    fill = fill == lds0 + kStages * T::kStageBytes ? lds0 : fill;
-  };
-  const uint32_t swz = (l15 >> 1) & 7;
-  const uint32_t aw0 = uint32_t((wn * T::kTn * 16 + l15) * 128) + ((uint32_t(grp) ^ swz) << 4);
-  const uint32_t ax0 = uint32_t(BN * 128 + (wm * T::kTm * 16 + l15) * 128) + ((uint32_t(grp) ^ swz) << 4);
-
-  f32x4 acc[T::kTn][T::kTm];
-#pragma unroll
-  for (int i = 0; i < T::kTn; ++i)
-#pragma unroll
-    for (int j = 0; j < T::kTm; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-  bf16x8 fw[2][T::kTn], fx[2][T::kTm];
-  uint32_t slot = 0;
-  auto read = [&](int kk) {
-#pragma unroll
-    for (int i = 0; i < T::kTn; ++i) fw[kk][i] = *reinterpret_cast<const bf16x8*>(lds + slot + (aw0 ^ (kk << 6)) + i * 2048);
-#pragma unroll
-    for (int j = 0; j < T::kTm; ++j) fx[kk][j] = *reinterpret_cast<const bf16x8*>(lds + slot + (ax0 ^ (kk << 6)) + j * 2048);
-    __builtin_amdgcn_sched_barrier(0);        // reads stay ahead of the products they run beside
-  };
-  auto multiply = [&](int kk) {
-#pragma unroll
-    for (int i = 0; i < T::kTn; ++i)
-#pragma unroll
-      for (int j = 0; j < T::kTm; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fw[kk][i], fx[kk][j], acc[i][j], 0, 0, 0);
-  };
-#pragma unroll
-  for (int s = 0; s < kStages; ++s) issue();
-  constexpr int kFlying = (kStages - 1) * (T::kLoadsW + T::kLoadsX);
-  asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" :: "n"(kFlying) : "memory");
-  read(0);
-  // operands are read one k-step ahead of their products, across stages too: the barrier stands before a
-  // stage's second k-step
-  for (int s = 0; s < n_stages; ++s) {
-    read(1);
-    multiply(0);
-    __builtin_amdgcn_sched_barrier(0);
-    // the next stage has landed; every wave has this one in registers: its slot takes the next loads
-    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" :: "n"(kFlying - T::kLoadsW - T::kLoadsX) : "memory");
-    issue();
-    slot += T::kStageBytes;
-    slot = slot == kStages * T::kStageBytes ? 0 : slot;
-    read(0);
-    multiply(1);
-    __builtin_amdgcn_sched_barrier(0);
-  }
-  asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");     // the ring is free
+#include "gemm_tile_loop.hpp"
 
   int pitch = T::kPitch;
   if constexpr (kPublish) pitch = n0 / (a.pub.heads * 128) == 2 ? kEpiRowV : kEpiRow;

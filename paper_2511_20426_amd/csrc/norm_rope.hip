@@ -1,0 +1,251 @@
+// Per-head RMS norm of queries and keys with the 3-axis rotation in the same pass, and its gradients (gfx950).
+//
+//   y = w x r,  r = 1 / sqrt(mean(x^2) + eps),  z = R y           (R turns pair j by position * theta^(-2j/Da))
+//   dy = R' dz,  dw = sum over tokens and heads of dy x r,  dn = dy w,  dx = r (dn - x r mean(dn x r))
+//
+// Memory bound: forward reads x and writes z once, backward reads x and dz and writes dx; statistics and products are fp32, with
+// one rounding of each result to the storage type.  The gradients of the weights are summed in fp32 by each lane over the tokens
+// and heads that it meets, over a workgroup's lanes in LDS and over the workgroups by a second small launch in fp64, in an order
+// that depends on the sizes alone: no atomics, the same bits every time.
+#include <hip/hip_runtime.h>
+
+#include "ca_internal.hpp"
+
+namespace ca {
+namespace {
+
+#include "rope_device.hpp"
+#include "norm_device.hpp"
+
+constexpr int kMaxWorkgroups = 1024;              // of a backward launch: each leaves a partial sum of the weights' gradients
+
+struct NormSide {                                 // queries or keys
+  const void* x;
+  const void* w;
+  const void* dz;                                 // backward only
+  void* y;                                        // forward: z, backward: dx
+  int64_t x_tok, x_head, dz_tok, dz_head, y_tok, y_head;
+};
+
+struct NormArgs {
+  NormSide side[2];
+  int64_t n_tokens, first_frame;
+  float* partials;                                // backward: [workgroup][side][head_dim]
+  float eps;
+  int32_t rows, rows_per_group;                   // heads of all sides, and of them a workgroup's
+};
+
+// cos / sin of the lane's four pairs at token n: a lane evaluates one pair of the token's and takes its four from the others
+template <bool kFp64>
+__device__ __forceinline__ void token_angles(const RopeGeom& g, int64_t n, int64_t first_frame, int lane, int c8, float* cs, float* sn) {
+  const TokenPos p = token_pos_any(n, first_frame, g.grid_h, g.grid_w);
+  float c1, s1;
+  pair_cs<kFp64>(g, p, lane % (g.head_dim / 2), &c1, &s1);
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    cs[j] = __shfl(c1, c8 * 4 + j, 64);
+    sn[j] = __shfl(s1, c8 * 4 + j, 64);
+  }
+}
+
+// A wave takes a token: its lanes cover 64 / chunks heads at a time (1 KB of bf16), rows_per_group heads in all, kAhead loads
+// requested together.
+template <typename T>
+__global__ __launch_bounds__(256) void norm_rope_kernel(RopeGeom g, NormArgs a) {
+  constexpr int kAhead = 4;
+  const int chunks = g.head_dim / 8, head_slots = 64 / chunks;
+  const int64_t n = int64_t(blockIdx.x) * 4 + (threadIdx.x >> 6);
+  if (n >= a.n_tokens) return;
+  const int lane = threadIdx.x & 63, c8 = lane % chunks, hs = lane / chunks;
+  const int r0 = blockIdx.y * a.rows_per_group, r1 = min(r0 + a.rows_per_group, a.rows);
+  Vec8<T> w[2];
+#pragma unroll
+  for (int s = 0; s < 2; ++s)
+    if (s == 0 || a.rows > g.heads) w[s].load(static_cast<const T*>(a.side[s].w) + c8 * 8);
+  float cs[4], sn[4];
+  bool angles = false;
+  for (int r = r0 + hs; r - hs < r1; r += kAhead * head_slots) {
+    Vec8<T> e[kAhead];
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) {             // rows past the group's re-read its last one
+      const int row = min(r + i * head_slots, r1 - 1), s = row >= g.heads;
+      const NormSide& side = a.side[s];
+      e[i].load(static_cast<const T*>(side.x) + n * side.x_tok + int64_t(row - s * g.heads) * side.x_head + c8 * 8);
+    }
+    if (!angles) token_angles<sizeof(T) == 4>(g, n, a.first_frame, lane, c8, cs, sn);
+    angles = true;
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) {
+      const int row = r + i * head_slots, s = row >= g.heads;
+      const NormSide& side = a.side[s];
+      norm8(e[i], s ? w[1].v : w[0].v, chunks, a.eps);
+      rotate8(e[i], cs, sn);
+      if (row < r1) e[i].store(static_cast<T*>(side.y) + n * side.y_tok + int64_t(row - s * g.heads) * side.y_head + c8 * 8);
+    }
+  }
+}
+
+// A wave takes every so manieth token, all its rows or a group's, and keeps the sums of dy x r of its lanes.
+template <typename T>
+__global__ __launch_bounds__(256) void norm_rope_backward_kernel(RopeGeom g, NormArgs a) {
+  constexpr int kAhead = 2;
+  __shared__ float sums[4][2][2 * kMaxPairs];
+  const int chunks = g.head_dim / 8, head_slots = 64 / chunks;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c8 = lane % chunks, hs = lane / chunks;
+  const int r0 = blockIdx.y * a.rows_per_group, r1 = min(r0 + a.rows_per_group, a.rows);
+  Vec8<T> w[2];
+  float dw[2][8];
+#pragma unroll
+  for (int s = 0; s < 2; ++s) {
+    if (s == 0 || a.rows > g.heads) w[s].load(static_cast<const T*>(a.side[s].w) + c8 * 8);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) dw[s][j] = 0.f;
+  }
+  for (int64_t n = int64_t(blockIdx.x) * 4 + wave; n < a.n_tokens; n += int64_t(gridDim.x) * 4) {
+    float cs[4], sn[4];
+    bool angles = false;
+    for (int r = r0 + hs; r - hs < r1; r += kAhead * head_slots) {
+      Vec8<T> x[kAhead], d[kAhead];
+#pragma unroll
+      for (int i = 0; i < kAhead; ++i) {
+        const int row = min(r + i * head_slots, r1 - 1), s = row >= g.heads;
+        const NormSide& side = a.side[s];
+        x[i].load(static_cast<const T*>(side.x) + n * side.x_tok + int64_t(row - s * g.heads) * side.x_head + c8 * 8);
+        d[i].load(static_cast<const T*>(side.dz) + n * side.dz_tok + int64_t(row - s * g.heads) * side.dz_head + c8 * 8);
+      }
+      if (!angles) {
+        token_angles<sizeof(T) == 4>(g, n, a.first_frame, lane, c8, cs, sn);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) sn[j] = -sn[j];          // R' turns back
+        angles = true;
+      }
+#pragma unroll
+      for (int i = 0; i < kAhead; ++i) {
+        const int row = r + i * head_slots, s = row >= g.heads;
+        const bool mine = row < r1;
+        rotate8(d[i], cs, sn);
+        const float rstd = head_rstd(x[i], chunks, a.eps);
+        float dot = 0.f;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          x[i].v[j] *= rstd;
+          const float part = mine ? d[i].v[j] * x[i].v[j] : 0.f;
+          dw[0][j] += s ? 0.f : part;
+          dw[1][j] += s ? part : 0.f;
+          d[i].v[j] *= s ? w[1].v[j] : w[0].v[j];
+          dot = fmaf(d[i].v[j], x[i].v[j], dot);
+        }
+        const float mean = head_sum(dot, chunks) * (1.f / float(8 * chunks));
+#pragma unroll
+        for (int j = 0; j < 8; ++j) d[i].v[j] = rstd * fmaf(-x[i].v[j], mean, d[i].v[j]);
+        const NormSide& side = a.side[s];
+        if (mine) d[i].store(static_cast<T*>(side.y) + n * side.y_tok + int64_t(row - s * g.heads) * side.y_head + c8 * 8);
+      }
+    }
+  }
+#pragma unroll
+  for (int s = 0; s < 2; ++s)
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      float v = dw[s][j];
+      for (int d = chunks; d < 64; d *= 2) v += __shfl_xor(v, d, 64);
+      if (lane < chunks) sums[wave][s][lane * 8 + j] = v;
+    }
+  __syncthreads();
+  float* out = a.partials + (int64_t(blockIdx.y) * gridDim.x + blockIdx.x) * 2 * g.head_dim;
+  for (int i = threadIdx.x; i < 2 * g.head_dim; i += 256) {
+    const int s = i / g.head_dim, d = i - s * g.head_dim;
+    out[i] = (sums[0][s][d] + sums[1][s][d]) + (sums[2][s][d] + sums[3][s][d]);
+  }
+}
+
+// dw[side][d] from the workgroups' sums: 32 columns to a workgroup, its 32 rows of threads share the partials
+__global__ __launch_bounds__(1024) void norm_weight_grad_kernel(const float* partials, int n_partials, int head_dim, float* dw0, float* dw1) {
+  __shared__ double sums[32][33];
+  const int x = threadIdx.x & 31, y = threadIdx.x >> 5, col = blockIdx.x * 32 + x;
+  double v = 0.;
+#pragma unroll 8
+  for (int i = y; i < n_partials; i += 32) v += double(partials[int64_t(i) * 2 * head_dim + col]);
+  sums[y][x] = v;
+  __syncthreads();
+  if (y != 0) return;
+  for (int i = 1; i < 32; ++i) v += sums[i][x];
+  float* dw = col < head_dim ? dw0 : dw1;
+  if (dw) dw[col < head_dim ? col : col - head_dim] = float(v);
+}
+
+// workgroups of four waves along the tokens, and groups of rows where there are few tokens
+struct NormGrid {
+  unsigned x, y;
+  int32_t rows_per_group;
+};
+
+NormGrid norm_grid(int64_t workgroups, int rows, int head_dim, int fill) {
+  const int slots = 512 / head_dim;               // heads of a wave's load
+  int groups = 1;
+  while (workgroups * groups < fill && groups * slots < rows) groups *= 2;
+  NormGrid out;
+  out.rows_per_group = (rows + groups - 1) / groups;
+  out.x = unsigned(workgroups);
+  out.y = unsigned((rows + out.rows_per_group - 1) / out.rows_per_group);
+  return out;
+}
+
+int norm_sides(const RopeGeom& g, const NormTensors& q, const NormTensors& k, int64_t n_tokens, int64_t first_frame, float eps, NormArgs* a) {
+  int n = 0;
+  for (const NormTensors* t : {&q, &k}) {
+    if (!t->x) continue;
+    a->side[n++] = NormSide{t->x, t->w, t->dz, t->y, t->x_tok, t->x_head, t->dz_tok, t->dz_head, t->y_tok, t->y_head};
+  }
+  a->n_tokens = n_tokens;
+  a->first_frame = first_frame;
+  a->eps = eps;
+  a->rows = n * g.heads;
+  return n;
+}
+
+NormGrid backward_grid(const RopeGeom& g, int64_t n_tokens, int rows) {
+  const int64_t all = (n_tokens + 3) / 4;
+  return norm_grid(all < kMaxWorkgroups ? all : kMaxWorkgroups, rows, g.head_dim, kMaxWorkgroups / 2);
+}
+
+}  // namespace
+
+int32_t launch_norm_rope(const RopeGeom& g, int dtype, const NormTensors& q, const NormTensors& k, float eps, int64_t n_tokens,
+                         int64_t first_frame, void* stream) {
+  if (n_tokens == 0) return CA_OK;
+  NormArgs a{};
+  if (norm_sides(g, q, k, n_tokens, first_frame, eps, &a) == 0) return CA_EINVAL;
+  const int64_t gx = (n_tokens + 3) / 4;
+  if (gx > (1 << 24)) return CA_EUNSUPPORTED;      // (a launch may have 2^32 threads)
+  const NormGrid grid = norm_grid(gx, a.rows, g.head_dim, 2048);
+  a.rows_per_group = grid.rows_per_group;
+  const auto kernel = dtype == CA_BF16 ? norm_rope_kernel<uint16_t> : norm_rope_kernel<float>;
+  hipLaunchKernelGGL(kernel, dim3(grid.x, grid.y), dim3(256), 0, static_cast<hipStream_t>(stream), g, a);
+  return finish_launch("norm_rope.hip");
+}
+
+size_t norm_rope_backward_bytes(int32_t head_dim) { return size_t(kMaxWorkgroups) * 2 * head_dim * sizeof(float); }
+
+int32_t launch_norm_rope_backward(const RopeGeom& g, int dtype, const NormTensors& q, const NormTensors& k, float eps, int64_t n_tokens,
+                                  int64_t first_frame, float* dq_weight, float* dk_weight, void* workspace, void* stream) {
+  NormArgs a{};
+  const int sides = norm_sides(g, q, k, n_tokens, first_frame, eps, &a);
+  if (sides == 0) return CA_EINVAL;
+  a.partials = static_cast<float*>(workspace);
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  int n_partials = 0;
+  if (n_tokens > 0) {
+    const NormGrid grid = backward_grid(g, n_tokens, a.rows);
+    a.rows_per_group = grid.rows_per_group;
+    n_partials = int(grid.x * grid.y);
+    const auto kernel = dtype == CA_BF16 ? norm_rope_backward_kernel<uint16_t> : norm_rope_backward_kernel<float>;
+    hipLaunchKernelGGL(kernel, dim3(grid.x, grid.y), dim3(256), 0, s, g, a);
+    if (const int32_t rc = finish_launch("norm_rope.hip"); rc != CA_OK) return rc;
+  }
+  float* const dw[2] = {q.x ? dq_weight : dk_weight, sides == 2 ? dk_weight : nullptr};
+  hipLaunchKernelGGL(norm_weight_grad_kernel, dim3(unsigned(2 * g.head_dim / 32)), dim3(1024), 0, s, a.partials, n_partials, g.head_dim, dw[0], dw[1]);
+  return finish_launch("norm_rope.hip");
+}
+
+}  // namespace ca

@@ -19,6 +19,16 @@ namespace ca {
 namespace {
 
 #include "rope_device.hpp"
+#include "norm_device.hpp"
+
+// What the writes of normed keys are given beside the others' arguments.
+template <typename Args, bool kNorm>
+struct WithNorm : Args {};
+template <typename Args>
+struct WithNorm<Args, true> : Args {
+  const void* norm_weight;
+  float norm_eps;
+};
 
 // ----------------------------------------------------------------------------- generic path
 // One thread owns 4 consecutive pairs (8 elements) of one token and walks a range of heads; the 64
@@ -27,7 +37,7 @@ namespace {
 // sin / cos of one and takes its four from the others (small fp32 launches are one such evaluation long, in fp64:
 // 5.3 us with four, 3.4 with one).
 // MODE 0: y[token][head][dim] (rope3d_apply).  MODE 1: K/V pages of the fp32 pool layout
-// (row-major [token][dim] pages), V copied unrotated; grid.z picks the block.
+// (row-major [token][dim] pages), V copied unrotated; grid.z picks the block.  kNorm: each head of K is normed first.
 struct GenericBlock {
   const void* x;        // MODE 0: input; MODE 1: K
   const void* v;        // MODE 1: V
@@ -45,8 +55,8 @@ struct GenericArgs {
   int32_t page_tokens, pages_per_block, valid_tokens;
 };
 
-template <typename T, int MODE>
-__global__ __launch_bounds__(256) void rope_generic_kernel(RopeGeom g, GenericArgs a) {
+template <typename T, int MODE, bool kNorm = false>
+__global__ __launch_bounds__(256) void rope_generic_kernel(RopeGeom g, WithNorm<GenericArgs, kNorm> a) {
   const int chunks = g.head_dim / 8;              // 4, 8 or 16
   const int head_slots = 64 / chunks;             // heads a wave touches per load
   const int64_t n = int64_t(blockIdx.x) * 4 + (threadIdx.x >> 6);
@@ -77,8 +87,13 @@ __global__ __launch_bounds__(256) void rope_generic_kernel(RopeGeom g, GenericAr
     for (int j = 0; j < 8; ++j) e.v[j] = w.v[j] = 0.f;
     if (!pad) {
       e.load(x + src);
-      rotate8(e, cs, sn);
     }
+    if constexpr (kNorm) {                         // (pad tokens' zeros stay zeros)
+      Vec8<T> nw;
+      nw.load(static_cast<const T*>(a.norm_weight) + c8 * 8);
+      if (!pad) norm8(e, nw.v, chunks, a.norm_eps);
+    }
+    if (!pad) rotate8(e, cs, sn);
     if (MODE == 0) {
       e.store(static_cast<T*>(a.y) + n * a.y_tok_stride + int64_t(h) * a.y_head_stride + c8 * 8);
     } else {
@@ -128,8 +143,9 @@ struct PagedArgs {             // what the kernel body works with: the batch's e
   TrigTable tab;
 };
 
-template <int kTokens>
-__global__ __launch_bounds__(256) void cache_write_bf16_kernel(RopeGeom g, PagedBatch batch) {
+// kNorm: each head of K is normed ahead of its rotation, in the registers that it is rotated in; its sixteen lanes are neighbours.
+template <int kTokens, bool kNorm>
+__global__ __launch_bounds__(256) void cache_write_bf16_kernel(RopeGeom g, WithNorm<PagedBatch, kNorm> batch) {
   constexpr int kParts = kPage / kTokens, kRows = kTokens / 16;   // workgroups of a page; rows (K) and chunks (V) of a thread
   constexpr int kChunks = kTokens / 8, kDims = 256 / kChunks;     // V chunks a workgroup writes of a dim; dims a step covers
   PagedArgs a;
@@ -162,6 +178,8 @@ __global__ __launch_bounds__(256) void cache_write_bf16_kernel(RopeGeom g, Paged
     }
   };
   request(h0);
+  Vec8<uint16_t> nw;
+  if constexpr (kNorm) nw.load(static_cast<const uint16_t*>(batch.norm_weight) + c * 8);
 
   // cos/sin of this thread's 4 pairs at its tokens
   float cs[kRows][4], sn[kRows][4];
@@ -198,6 +216,7 @@ __global__ __launch_bounds__(256) void cache_write_bf16_kernel(RopeGeom g, Paged
       Vec8<uint16_t> e;
       e.v[0] = bf16_lo(raw.x); e.v[1] = bf16_hi(raw.x); e.v[2] = bf16_lo(raw.y); e.v[3] = bf16_hi(raw.y);
       e.v[4] = bf16_lo(raw.z); e.v[5] = bf16_hi(raw.z); e.v[6] = bf16_lo(raw.w); e.v[7] = bf16_hi(raw.w);
+      if constexpr (kNorm) norm8(e, nw.v, 16, batch.norm_eps);
       rotate8(e, cs[i], sn[i]);
       U4 kk;
       kk.x = pad ? 0u : pack_bf16(e.v[0], e.v[1]); kk.y = pad ? 0u : pack_bf16(e.v[2], e.v[3]);
@@ -287,7 +306,7 @@ int32_t launch_rope_apply(const RopeGeom& g, int dtype, const void* x, void* y, 
                           int64_t first_frame, int64_t tok_stride, int64_t head_stride,
                           int64_t y_tok_stride, int64_t y_head_stride, void* stream) {
   if (n_tokens == 0) return CA_OK;
-  GenericArgs a{};
+  WithNorm<GenericArgs, false> a{};
   a.b[0].x = x; a.b[0].first_frame = first_frame;
   a.y = y;
   a.n_tokens = n_tokens;
@@ -309,21 +328,26 @@ int32_t launch_rope_apply(const RopeGeom& g, int dtype, const void* x, void* y, 
   return finish_launch("rope_cache.hip");
 }
 
-int32_t launch_cache_write(const RopeGeom& g, int dtype, int32_t n_blocks, const void* const* k,
-                           const void* const* v, int64_t tok_stride, int64_t head_stride,
-                           const int64_t* first_frame, int32_t block_tokens, int32_t page_tokens,
-                           int32_t pages_per_block, const int32_t* slot, void* pool, void* stream) {
+namespace {
+
+template <bool kNorm>
+int32_t enqueue_cache_write(const RopeGeom& g, int dtype, int32_t n_blocks, const void* const* k,
+                            const void* const* v, int64_t tok_stride, int64_t head_stride,
+                            const int64_t* first_frame, int32_t block_tokens, int32_t page_tokens,
+                            int32_t pages_per_block, const int32_t* slot, const void* norm_weight, float norm_eps, void* pool,
+                            void* stream) {
   hipStream_t s = static_cast<hipStream_t>(stream);
   if (n_blocks < 1 || n_blocks > kMaxInflight) return CA_EINVAL;
   if (dtype == CA_BF16) {
     if (g.head_dim != 128 || page_tokens != kPage) return CA_EUNSUPPORTED;
-    PagedBatch a{};
+    WithNorm<PagedBatch, kNorm> a{};
     for (int i = 0; i < n_blocks; ++i) {
       a.b[i].k = static_cast<const uint16_t*>(k[i]);
       a.b[i].v = static_cast<const uint16_t*>(v[i]);
       a.b[i].first_frame = first_frame[i];
       a.b[i].slot = slot[i];
     }
+    if constexpr (kNorm) a.norm_weight = norm_weight, a.norm_eps = norm_eps;
     a.pool = static_cast<uint8_t*>(pool);
     a.tok_stride = tok_stride; a.head_stride = head_stride;
     a.block_tokens = block_tokens; a.pages_per_block = pages_per_block;
@@ -349,15 +373,16 @@ int32_t launch_cache_write(const RopeGeom& g, int dtype, int32_t n_blocks, const
                     (unsigned)((g.heads + a.heads_per_group - 1) / a.heads_per_group), (unsigned)n_blocks);
     size_t tab_bytes = 0;
     a.tab = trig_table_for(g, tokens, 16384, &tab_bytes);
-    const auto kernel = tokens == 32 ? cache_write_bf16_kernel<32> : (tokens == 64 ? cache_write_bf16_kernel<64> : cache_write_bf16_kernel<kPage>);
+    const auto kernel = tokens == 32 ? cache_write_bf16_kernel<32, kNorm> : (tokens == 64 ? cache_write_bf16_kernel<64, kNorm> : cache_write_bf16_kernel<kPage, kNorm>);
     hipLaunchKernelGGL(kernel, grid, dim3(256), tab_bytes, s, g, a);
   } else {
-    GenericArgs a{};
+    WithNorm<GenericArgs, kNorm> a{};
     for (int i = 0; i < n_blocks; ++i) {
       a.b[i].x = k[i]; a.b[i].v = v[i];
       a.b[i].first_frame = first_frame[i];
       a.b[i].slot = slot[i];
     }
+    if constexpr (kNorm) a.norm_weight = norm_weight, a.norm_eps = norm_eps;
     a.y = pool;
     a.n_tokens = int64_t(pages_per_block) * page_tokens;
     a.valid_tokens = block_tokens;
@@ -365,9 +390,28 @@ int32_t launch_cache_write(const RopeGeom& g, int dtype, int32_t n_blocks, const
     a.page_tokens = page_tokens; a.pages_per_block = pages_per_block;
     a.heads_per_group = g.heads;
     const dim3 grid((unsigned)((a.n_tokens + 3) / 4), 1, (unsigned)n_blocks);
-    hipLaunchKernelGGL((rope_generic_kernel<float, 1>), grid, dim3(256), 0, s, g, a);
+    hipLaunchKernelGGL((rope_generic_kernel<float, 1, kNorm>), grid, dim3(256), 0, s, g, a);
   }
   return finish_launch("rope_cache.hip");
+}
+
+}  // namespace
+
+int32_t launch_cache_write(const RopeGeom& g, int dtype, int32_t n_blocks, const void* const* k,
+                           const void* const* v, int64_t tok_stride, int64_t head_stride,
+                           const int64_t* first_frame, int32_t block_tokens, int32_t page_tokens,
+                           int32_t pages_per_block, const int32_t* slot, void* pool, void* stream) {
+  return enqueue_cache_write<false>(g, dtype, n_blocks, k, v, tok_stride, head_stride, first_frame, block_tokens, page_tokens,
+                                    pages_per_block, slot, nullptr, 0.f, pool, stream);
+}
+
+int32_t launch_cache_write_norm(const RopeGeom& g, int dtype, int32_t n_blocks, const void* const* k,
+                                const void* const* v, int64_t tok_stride, int64_t head_stride,
+                                const int64_t* first_frame, int32_t block_tokens, int32_t page_tokens,
+                                int32_t pages_per_block, const int32_t* slot, const void* norm_weight, float norm_eps, void* pool,
+                                void* stream) {
+  return enqueue_cache_write<true>(g, dtype, n_blocks, k, v, tok_stride, head_stride, first_frame, block_tokens, page_tokens,
+                                   pages_per_block, slot, norm_weight, norm_eps, pool, stream);
 }
 
 }  // namespace ca

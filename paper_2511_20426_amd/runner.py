@@ -82,10 +82,12 @@ class CascadePool:
                                         k.stride(0), k.stride(1), self._stream())
 
     def append_batch(self, block_ids: Sequence[int], timesteps: Sequence[int], epoch: int,
-                     ks: Sequence[torch.Tensor], vs: Sequence[torch.Tensor]) -> list[int]:
-        """All blocks of one cascade iteration in one launch; the tensors share their strides."""
+                     ks: Sequence[torch.Tensor], vs: Sequence[torch.Tensor], k_weight: torch.Tensor | None = None,
+                     eps: float = 1e-6) -> list[int]:
+        """All blocks of one cascade iteration in one launch; the tensors share their strides.  With k_weight [D] each head of K
+        is normed (as qk_norm_rope does) ahead of its rotation."""
         h = self.ctx._h
-        if h:
+        if h and k_weight is None:
             r = B.calls.append_batch(h.value, self._shape, block_ids, timesteps, epoch, ks, vs)
             if r.__class__ is list:
                 return r
@@ -96,6 +98,11 @@ class CascadePool:
             self._check(k); self._check(v)
             assert k.shape[0] == self.block_tokens and k.shape == v.shape
             assert k.stride() == stride and v.stride() == stride
+        if k_weight is not None:
+            self._check_weight(k_weight)
+            return self.ctx.kv_cache_append_batch_norm(list(block_ids), list(timesteps), epoch, [k.data_ptr() for k in ks],
+                                                       [v.data_ptr() for v in vs], stride[0], stride[1], k_weight.data_ptr(), eps,
+                                                       self._stream())
         return self.ctx.kv_cache_append_batch(list(block_ids), list(timesteps), epoch,
                                               [k.data_ptr() for k in ks], [v.data_ptr() for v in vs],
                                               stride[0], stride[1], self._stream())
@@ -197,6 +204,76 @@ def _qkv_publish(self, x: torch.Tensor, w_qkv: torch.Tensor, block_ids: Sequence
 CascadePool.qkv_publish = _qkv_publish
 
 
+def _check_weight(self, w: torch.Tensor) -> None:
+    assert w.is_cuda and w.dtype == self._torch_dtype and w.shape == (self.head_dim,) and (self.head_dim == 1 or w.stride(0) == 1)
+
+
+def _view(self, t: torch.Tensor, n: int):
+    """(address, token stride, head stride) of a [n, H, D] tensor; of a single token or head the stride is free."""
+    self._check(t)
+    assert t.shape[0] == n
+    s = t.stride()
+    return (t.data_ptr(), s[0] if n > 1 else self.heads * self.head_dim, s[1] if self.heads > 1 else self.head_dim)
+
+
+def _qk_norm_rope(self, q: torch.Tensor | None, k: torch.Tensor | None, q_weight: torch.Tensor | None, k_weight: torch.Tensor | None,
+                  first_frame: int, eps: float = 1e-6, q_out: torch.Tensor | None = None, k_out: torch.Tensor | None = None):
+    """Each head of q and k (either may be None) normed, y = weight * x / sqrt(mean(x^2) + eps), and rotated by its token's
+    position, in one launch: [n, H, D] with any token / head strides, consecutive tokens from latent frame `first_frame` on; weights
+    [D].  Returns (q', k'), in q_out / k_out (their own strides) or new contiguous tensors; an output may be its input."""
+    given, outs, views = [], [], []
+    n = (k if q is None else q).shape[0]
+    for x, w, out in ((q, q_weight, q_out), (k, k_weight, k_out)):
+        if x is None:
+            assert w is None and out is None
+            views += [None, None]
+            given.append(0)
+            outs.append(None)
+            continue
+        self._check_weight(w)
+        y = torch.empty(x.shape, dtype=x.dtype, device=x.device) if out is None else out
+        views += [self._view(x, n), self._view(y, n)]
+        given.append(w.data_ptr())
+        outs.append(y)
+    self.ctx.layer_qk_norm_rope(views[0], views[2], given[0], given[1], eps, views[1], views[3], n, first_frame, self._stream())
+    return outs[0], outs[1]
+
+
+def _qk_norm_rope_backward(self, dq_out: torch.Tensor | None, dk_out: torch.Tensor | None, q: torch.Tensor | None,
+                           k: torch.Tensor | None, q_weight: torch.Tensor | None, k_weight: torch.Tensor | None, first_frame: int,
+                           eps: float = 1e-6, dq: torch.Tensor | None = None, dk: torch.Tensor | None = None):
+    """Gradients of qk_norm_rope: from those of its outputs (dq_out, dk_out) and its inputs to (dq, dk, dq_weight, dk_weight), the
+    weights' in fp32.  What belongs to a q or k of None is None.  dq may be dq_out, dk dk_out."""
+    n = (k if q is None else q).shape[0]
+    views, weights, grads, dws = [], [], [], []
+    for x, w, dz, dx in ((q, q_weight, dq_out, dq), (k, k_weight, dk_out, dk)):
+        if x is None:
+            assert w is None and dz is None and dx is None
+            views.append((None, None, None))
+            weights.append(0)
+            grads.append(None)
+            dws.append(None)
+            continue
+        self._check_weight(w)
+        g = torch.empty(x.shape, dtype=x.dtype, device=x.device) if dx is None else dx
+        views.append((self._view(dz, n), self._view(x, n), self._view(g, n)))
+        weights.append(w.data_ptr())
+        grads.append(g)
+        dws.append(torch.empty(self.head_dim, dtype=torch.float32, device=x.device))
+    nbytes = self.ctx.layer_qk_norm_rope_workspace()
+    work = torch.empty(nbytes, dtype=torch.uint8, device=(k if q is None else q).device)
+    (dzq, xq, gq), (dzk, xk, gk) = views
+    self.ctx.layer_qk_norm_rope_backward(dzq, dzk, xq, xk, weights[0], weights[1], eps, gq, gk, *(0 if d is None else d.data_ptr() for d in dws),
+                                         n, first_frame, work.data_ptr(), nbytes, self._stream())
+    return grads[0], grads[1], dws[0], dws[1]
+
+
+CascadePool._check_weight = _check_weight
+CascadePool._view = _view
+CascadePool.qk_norm_rope = _qk_norm_rope
+CascadePool.qk_norm_rope_backward = _qk_norm_rope_backward
+
+
 def linear(x: torch.Tensor, w: torch.Tensor, out: torch.Tensor | None = None) -> torch.Tensor:
     """y = x @ w.T through layer_linear_bf16: x [M, K], w [N, K], y [M, N], bf16, rows may be
     strided (last dimension contiguous)."""
@@ -215,6 +292,108 @@ def linear(x: torch.Tensor, w: torch.Tensor, out: torch.Tensor | None = None) ->
     B.layer_linear_bf16(x.data_ptr(), w.data_ptr(), y.data_ptr(), xs[0], ws[0], xs[1], sx[0], sw[0], sy[0],
                         _current_stream(device))
     return y
+
+
+def _matrix(t: torch.Tensor, like: torch.Tensor, dtype, rows: int, cols: int) -> int:
+    """The row stride of a [rows, cols] matrix with unit stride along its rows; that of a single row is free."""
+    shape, s = t.shape, t.stride()
+    assert t.dtype == dtype and len(shape) == 2 and shape[0] == rows and shape[1] == cols and (s[1] == 1 or cols == 1) and _reachable(t, like)
+    return s[0] if rows > 1 else -(-cols // 16) * 16
+
+
+class QuantizedRows:
+    """Rows in 8 bits with a scale each (layer_quantize_rows_i8): codes [rows, k filled up with zeros to a multiple of 256] and
+    scales [rows]; what they stand for is codes[:, :k] * scales[:, None]."""
+
+    def __init__(self, codes: torch.Tensor, scales: torch.Tensor, k: int):
+        assert codes.dtype == torch.int8 and codes.dim() == 2 and codes.stride(1) == 1 and codes.shape[1] == -(-k // 256) * 256
+        assert scales.dtype == torch.float32 and scales.shape == (codes.shape[0],) and scales.is_contiguous() and scales.device == codes.device
+        self.codes, self.scales, self.k = codes, scales, k
+
+    @property
+    def shape(self):
+        return (self.codes.shape[0], self.k)
+
+    @classmethod
+    def from_codes(cls, codes: torch.Tensor, scales: torch.Tensor) -> "QuantizedRows":
+        """From codes [rows, k] and scales [rows] made elsewhere (a checkpoint's)."""
+        rows, k = codes.shape
+        whole = torch.zeros((rows, -(-k // 256) * 256), dtype=torch.int8, device=codes.device)
+        whole[:, :k] = codes
+        return cls(whole, scales.to(torch.float32).contiguous(), k)
+
+
+def quantize_rows(x: torch.Tensor) -> QuantizedRows:
+    """x [rows, k], bf16 or fp32, in 8 bits: a scale of largest magnitude / 127 for each row, codes rounded half to even."""
+    assert x.is_cuda and x.dim() == 2 and x.dtype in (torch.bfloat16, torch.float32)
+    rows, k = x.shape
+    ldx = _matrix(x, x, x.dtype, rows, k)
+    codes = torch.empty((rows, -(-k // 256) * 256), dtype=torch.int8, device=x.device)
+    scales = torch.empty(rows, dtype=torch.float32, device=x.device)
+    B.layer_quantize_rows_i8(x.data_ptr(), B.CA_BF16 if x.dtype == _BF16 else B.CA_F32, codes.data_ptr(), scales.data_ptr(), rows, k, ldx,
+                             codes.shape[1], _current_stream(x.device))
+    return QuantizedRows(codes, scales, k)
+
+
+def linear_i8(x: torch.Tensor | QuantizedRows, w: QuantizedRows, out: torch.Tensor | None = None) -> torch.Tensor:
+    """y = x @ w.T in 8-bit integers with a scale for each row of x (token) and of w (output channel), y [M, N] in bf16; x [M, K] in bf16
+    or fp32 is brought to 8 bits on the way."""
+    if not isinstance(x, QuantizedRows):
+        x = quantize_rows(x)
+    (m, k), n, device = x.shape, w.shape[0], x.codes.device
+    assert w.k == k and w.codes.device == device
+    y = torch.empty((m, n), dtype=_BF16, device=device) if out is None else out
+    ldy = _matrix(y, x.codes, _BF16, m, n)
+    B.layer_linear_i8(x.codes.data_ptr(), x.scales.data_ptr(), w.codes.data_ptr(), w.scales.data_ptr(), y.data_ptr(), m, n, k,
+                      x.codes.shape[1] if m <= 1 else x.codes.stride(0), w.codes.shape[1] if n <= 1 else w.codes.stride(0), ldy,
+                      _current_stream(device))
+    return y
+
+
+_ACTIVATIONS = {"silu": B.CA_SILU, "gelu": B.CA_GELU}
+
+
+def _gated(x, w_gate, w_up, activation, out, saved):
+    assert x.is_cuda and w_gate.is_cuda and w_up.is_cuda
+    (m, k), f, device = x.shape, w_gate.shape[0], x.device
+    ldx, ldg, ldu = _matrix(x, x, _BF16, m, k), _matrix(w_gate, x, _BF16, f, k), _matrix(w_up, x, _BF16, f, k)
+    h = torch.empty((m, f), dtype=_BF16, device=device) if out is None else out
+    g, u = saved if saved is not None else (None, None)
+    B.layer_gated_bf16(x.data_ptr(), w_gate.data_ptr(), w_up.data_ptr(), h.data_ptr(), 0 if g is None else g.data_ptr(),
+                       0 if u is None else u.data_ptr(), _ACTIVATIONS[activation], m, f, k, ldx, ldg, ldu, _matrix(h, x, _BF16, m, f),
+                       f, _current_stream(device))
+    return h
+
+
+def gated_linear(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, activation: str = "silu",
+                 out: torch.Tensor | None = None) -> torch.Tensor:
+    """h = act(x @ w_gate.T) * (x @ w_up.T), the first half of a gated feed-forward block, in one kernel: x [M, K], w_gate and w_up
+    [F, K], h [M, F], bf16, rows may be strided (last dimension contiguous); activation "silu" or "gelu" (its tanh form)."""
+    return _gated(x, w_gate, w_up, activation, out, None)
+
+
+def gated_linear_train(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, activation: str = "silu",
+                       out: torch.Tensor | None = None):
+    """gated_linear for training: (h, saved), saved being the two projections [M, F] that gated_linear_backward takes."""
+    saved = torch.empty((2, x.shape[0], w_gate.shape[0]), dtype=_BF16, device=x.device)
+    return _gated(x, w_gate, w_up, activation, out, saved), saved
+
+
+def gated_linear_backward(dh: torch.Tensor, x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, saved: torch.Tensor,
+                          activation: str = "silu"):
+    """(dx, dw_gate, dw_up) from the gradient dh [M, F] of gated_linear_train's h, its inputs and what it saved."""
+    assert x.is_cuda and w_gate.is_cuda and w_up.is_cuda
+    (m, k), f, device = x.shape, w_gate.shape[0], x.device
+    ldx, ldg, ldu = _matrix(x, x, _BF16, m, k), _matrix(w_gate, x, _BF16, f, k), _matrix(w_up, x, _BF16, f, k)
+    lddh = _matrix(dh, x, _BF16, m, f)
+    assert saved.shape == (2, m, f) and saved.dtype == _BF16 and saved.is_contiguous() and _reachable(saved, x)
+    dx, dw = torch.empty((m, k), dtype=_BF16, device=device), torch.empty((2, f, k), dtype=_BF16, device=device)
+    nbytes = B.layer_gated_backward_workspace(m, f, k)
+    work = torch.empty(nbytes, dtype=torch.uint8, device=device)
+    B.layer_gated_backward_bf16(dh.data_ptr(), x.data_ptr(), w_gate.data_ptr(), w_up.data_ptr(), saved[0].data_ptr(), saved[1].data_ptr(),
+                                _ACTIVATIONS[activation], dx.data_ptr(), dw[0].data_ptr(), dw[1].data_ptr(), m, f, k, lddh, ldx, ldg, ldu,
+                                f, k, k, work.data_ptr(), nbytes, _current_stream(device))
+    return dx, dw[0], dw[1]
 
 
 def attention_layer(pool: CascadePool, x: torch.Tensor, w_qkv: torch.Tensor, w_out: torch.Tensor,
