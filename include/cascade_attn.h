@@ -310,13 +310,20 @@ int32_t layer_linear_i8(const int8_t* x_codes_dev, const float* x_scales_dev, co
                         void* y_dev, int64_t m_rows, int32_t n_out, int32_t k_in, int64_t ldx, int64_t ldw, int64_t ldy,
                         void* hip_stream);
 
+/* The same from x itself (CA_BF16 or CA_F32, as layer_quantize_rows_i8 takes it; ldx in elements): the rows are brought to 8 bits on the
+ * way.  workspace_dev: layer_linear_i8_workspace() bytes (0 where the sizes are not supported). */
+size_t layer_linear_i8_workspace(int64_t m_rows, int32_t k_in);
+int32_t layer_linear_i8_values(const void* x_dev, int32_t dtype, const int8_t* w_codes_dev, const float* w_scales_dev, void* y_dev, int64_t m_rows,
+                               int32_t n_out, int32_t k_in, int64_t ldx, int64_t ldw, int64_t ldy, void* workspace_dev, size_t workspace_bytes,
+                               void* hip_stream);
+
 /* The first half of a gated feed-forward block, both projections, activation and product in one kernel:
  * h = act(g) * u, g = x . w_gate', u = x . w_up', in bf16 with fp32 accumulation; g and u are rounded nowhere on the way to h, h once.
  * CA_SILU: g / (1 + exp(-g)); CA_GELU: g (1 + tanh(sqrt(2/pi) (g + 0.044715 g^3))) / 2.  With g_dev and u_dev (both or neither)
- * the projections are written as well, in bf16, for the backward pass.  w_gate, w_up: [n_hidden, k_in]; shapes as layer_linear_bf16
+ * the projections are written as well, in fp32, for the backward pass.  w_gate, w_up: [n_hidden, k_in]; shapes as layer_linear_bf16
  * (n_hidden a multiple of 8, k_in of 128). */
 enum { CA_SILU = 0, CA_GELU = 1 };
-int32_t layer_gated_bf16(const void* x_dev, const void* w_gate_dev, const void* w_up_dev, void* h_dev, void* g_dev, void* u_dev,
+int32_t layer_gated_bf16(const void* x_dev, const void* w_gate_dev, const void* w_up_dev, void* h_dev, float* g_dev, float* u_dev,
                          int32_t activation, int64_t m_rows, int32_t n_hidden, int32_t k_in, int64_t ldx, int64_t ldw_gate, int64_t ldw_up,
                          int64_t ldh, int64_t ld_saved, void* hip_stream);
 
@@ -325,8 +332,8 @@ int32_t layer_gated_bf16(const void* x_dev, const void* w_gate_dev, const void* 
  * as layer_gated_bf16 wrote them.  workspace_dev: layer_gated_backward_workspace() bytes, 0 where the shape is not supported.
  * m_rows == 0: zero weight gradients. */
 size_t layer_gated_backward_workspace(int64_t m_rows, int32_t n_hidden, int32_t k_in);
-int32_t layer_gated_backward_bf16(const void* dh_dev, const void* x_dev, const void* w_gate_dev, const void* w_up_dev, const void* g_dev,
-                                  const void* u_dev, int32_t activation, void* dx_dev, void* dw_gate_dev, void* dw_up_dev, int64_t m_rows,
+int32_t layer_gated_backward_bf16(const void* dh_dev, const void* x_dev, const void* w_gate_dev, const void* w_up_dev, const float* g_dev,
+                                  const float* u_dev, int32_t activation, void* dx_dev, void* dw_gate_dev, void* dw_up_dev, int64_t m_rows,
                                   int32_t n_hidden, int32_t k_in, int64_t lddh, int64_t ldx, int64_t ldw_gate, int64_t ldw_up,
                                   int64_t ld_saved, int64_t lddx, int64_t lddw, void* workspace_dev, size_t workspace_bytes,
                                   void* hip_stream);

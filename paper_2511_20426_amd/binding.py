@@ -37,7 +37,7 @@ EXPORTS = (
     "ca_strerror", "ca_last_device_error",
     "ca_mfma_microbench", "layer_linear_bf16", "layer_qkv_publish",
     "layer_qk_norm_rope", "layer_qk_norm_rope_workspace", "layer_qk_norm_rope_backward", "kv_cache_append_batch_norm", "layer_quantize_rows_i8",
-    "layer_linear_i8", "layer_gated_bf16", "layer_gated_backward_workspace", "layer_gated_backward_bf16",
+    "layer_linear_i8", "layer_linear_i8_workspace", "layer_linear_i8_values", "layer_gated_bf16", "layer_gated_backward_workspace", "layer_gated_backward_bf16",
     "ca_sched_create", "ca_sched_create_lagged", "ca_sched_destroy", "ca_sched_batch", "ca_sched_advance", "ca_sched_state",
 )
 
@@ -157,6 +157,10 @@ def _load() -> C.CDLL:
     lib.layer_quantize_rows_i8.argtypes = [vp, i32, vp, vp, i64, i32, i64, i64, vp]
     lib.layer_linear_i8.restype = i32
     lib.layer_linear_i8.argtypes = [vp, vp, vp, vp, vp, i64, i32, i32, i64, i64, i64, vp]
+    lib.layer_linear_i8_workspace.restype = C.c_size_t
+    lib.layer_linear_i8_workspace.argtypes = [i64, i32]
+    lib.layer_linear_i8_values.restype = i32
+    lib.layer_linear_i8_values.argtypes = [vp, i32, vp, vp, vp, i64, i32, i32, i64, i64, i64, vp, C.c_size_t, vp]
     lib.layer_gated_bf16.restype = i32
     lib.layer_gated_bf16.argtypes = [vp] * 6 + [i32, i64, i32, i32] + [i64] * 5 + [vp]
     lib.layer_gated_backward_workspace.restype = C.c_size_t
@@ -212,6 +216,10 @@ def _load_calls():
         ext.bind(*(C.cast(f, C.c_void_p).value for f in (
             lib.kv_cache_append_batch, lib.rope3d_apply_strided, lib.cascade_attn_forward, lib.cascade_attn_forward_share,
             lib.cascade_attn_forward_rope, lib.layer_qkv_publish, lib.layer_linear_bf16)))
+        ext.bind_layer(*(C.cast(f, C.c_void_p).value for f in (
+            lib.layer_qk_norm_rope, lib.layer_qk_norm_rope_workspace, lib.layer_qk_norm_rope_backward, lib.kv_cache_append_batch_norm,
+            lib.layer_linear_i8_workspace, lib.layer_linear_i8_values, lib.layer_gated_bf16, lib.layer_gated_backward_workspace,
+            lib.layer_gated_backward_bf16)))
         return ext
     except Exception as e:
         warnings.warn(f"{path} cannot be used, calls take more host time without it: {e}", RuntimeWarning)
@@ -435,6 +443,17 @@ def layer_linear_i8(x_codes_ptr: int, x_scales_ptr: int, w_codes_ptr: int, w_sca
                     k_in: int, ldx: int, ldw: int, ldy: int, stream: int = 0) -> None:
     _check(lib.layer_linear_i8(index(x_codes_ptr or 0), index(x_scales_ptr or 0), index(w_codes_ptr or 0), index(w_scales_ptr or 0),
                                index(y_ptr or 0), m_rows, n_out, k_in, ldx, ldw, ldy, index(stream or 0)), "layer_linear_i8")
+
+
+def layer_linear_i8_workspace(m_rows: int, k_in: int) -> int:
+    return int(lib.layer_linear_i8_workspace(m_rows, k_in))
+
+
+def layer_linear_i8_values(x_ptr: int, dtype: int, w_codes_ptr: int, w_scales_ptr: int, y_ptr: int, m_rows: int, n_out: int, k_in: int,
+                           ldx: int, ldw: int, ldy: int, workspace_ptr: int, workspace_bytes: int, stream: int = 0) -> None:
+    _check(lib.layer_linear_i8_values(index(x_ptr or 0), dtype, index(w_codes_ptr or 0), index(w_scales_ptr or 0), index(y_ptr or 0), m_rows,
+                                      n_out, k_in, ldx, ldw, ldy, index(workspace_ptr or 0), workspace_bytes, index(stream or 0)),
+           "layer_linear_i8_values")
 
 
 def layer_gated_bf16(x_ptr: int, w_gate_ptr: int, w_up_ptr: int, h_ptr: int, g_ptr: int, u_ptr: int, activation: int, m_rows: int,

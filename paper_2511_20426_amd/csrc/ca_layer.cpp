@@ -139,14 +139,36 @@ int32_t layer_linear_i8(const int8_t* x_codes_dev, const float* x_scales_dev, co
   return ca::launch_gemm_i8(x_codes_dev, x_scales_dev, w_codes_dev, w_scales_dev, y_dev, m_rows, n_out, k_in, ldx, ldw, ldy, hip_stream);
 }
 
-int32_t layer_gated_bf16(const void* x_dev, const void* w_gate_dev, const void* w_up_dev, void* h_dev, void* g_dev, void* u_dev,
+size_t layer_linear_i8_workspace(int64_t m_rows, int32_t k_in) {
+  if (m_rows < 0 || m_rows > kMaxRows || k_in < 1 || k_in > CA_I8_MAX_K) return 0;
+  return size_t(m_rows) * ((size_t(k_in) + 255) / 256 * 256 + 4) + 16;
+}
+
+int32_t layer_linear_i8_values(const void* x_dev, int32_t dtype, const int8_t* w_codes_dev, const float* w_scales_dev, void* y_dev, int64_t m_rows,
+                               int32_t n_out, int32_t k_in, int64_t ldx, int64_t ldw, int64_t ldy, void* workspace_dev, size_t workspace_bytes,
+                               void* hip_stream) {
+  if (m_rows < 0 || (dtype != CA_F32 && dtype != CA_BF16)) return CA_EINVAL;
+  if (m_rows > kMaxRows || n_out < 8 || n_out % 8 != 0 || k_in < 1 || k_in > CA_I8_MAX_K) return CA_EUNSUPPORTED;
+  if (ldx < k_in || ldw < (k_in + 255) / 256 * 256 || ldy < n_out || ldw % 16 != 0 || ldy % 8 != 0) return CA_EINVAL;
+  if (ldx >= kMaxLd || ldw >= 2 * kMaxLd) return CA_EUNSUPPORTED;
+  if (!workspace_dev || !aligned16(workspace_dev) || workspace_bytes < layer_linear_i8_workspace(m_rows, k_in)) return CA_EINVAL;
+  if (m_rows == 0) return CA_OK;
+  if (!x_dev || !w_codes_dev || !w_scales_dev || !y_dev) return CA_EINVAL;
+  if (!aligned16(w_codes_dev) || !aligned16(y_dev) || !aligned16(w_scales_dev) || reinterpret_cast<uintptr_t>(x_dev) % (dtype == CA_BF16 ? 2 : 4) != 0)
+    return CA_EINVAL;
+  return ca::launch_gemm_i8_values(dtype, x_dev, ldx, w_codes_dev, w_scales_dev, y_dev, m_rows, n_out, k_in, ldw, ldy, workspace_dev, hip_stream);
+}
+
+int32_t layer_gated_bf16(const void* x_dev, const void* w_gate_dev, const void* w_up_dev, void* h_dev, float* g_dev, float* u_dev,
                          int32_t activation, int64_t m_rows, int32_t n_hidden, int32_t k_in, int64_t ldx, int64_t ldw_gate, int64_t ldw_up,
                          int64_t ldh, int64_t ld_saved, void* hip_stream) {
   if (int32_t rc = check_gated(activation, m_rows, n_hidden, k_in)) return rc;
   if ((g_dev != nullptr) != (u_dev != nullptr)) return CA_EINVAL;
   for (int64_t ld : {ldx, ldw_gate, ldw_up})
     if (int32_t rc = check_ld(ld, k_in)) return rc;
-  if (ldh < n_hidden || ldh % 8 != 0 || (g_dev && (ld_saved < n_hidden || ld_saved % 8 != 0))) return CA_EINVAL;
+  if (ldh < n_hidden || ldh % 8 != 0) return CA_EINVAL;
+  if (g_dev)
+    if (int32_t rc = check_ld(ld_saved, n_hidden)) return rc;
   if (m_rows == 0) return CA_OK;
   for (const void* p : {x_dev, w_gate_dev, w_up_dev, static_cast<const void*>(h_dev)})
     if (!p || !aligned16(p)) return CA_EINVAL;
@@ -159,8 +181,8 @@ size_t layer_gated_backward_workspace(int64_t m_rows, int32_t n_hidden, int32_t 
   return check_gated(CA_SILU, m_rows, n_hidden, k_in) ? 0 : ca::gated_workspace(m_rows, n_hidden, k_in).bytes;
 }
 
-int32_t layer_gated_backward_bf16(const void* dh_dev, const void* x_dev, const void* w_gate_dev, const void* w_up_dev, const void* g_dev,
-                                  const void* u_dev, int32_t activation, void* dx_dev, void* dw_gate_dev, void* dw_up_dev, int64_t m_rows,
+int32_t layer_gated_backward_bf16(const void* dh_dev, const void* x_dev, const void* w_gate_dev, const void* w_up_dev, const float* g_dev,
+                                  const float* u_dev, int32_t activation, void* dx_dev, void* dw_gate_dev, void* dw_up_dev, int64_t m_rows,
                                   int32_t n_hidden, int32_t k_in, int64_t lddh, int64_t ldx, int64_t ldw_gate, int64_t ldw_up,
                                   int64_t ld_saved, int64_t lddx, int64_t lddw, void* workspace_dev, size_t workspace_bytes, void* hip_stream) {
   if (int32_t rc = check_gated(activation, m_rows, n_hidden, k_in)) return rc;
@@ -172,10 +194,10 @@ int32_t layer_gated_backward_bf16(const void* dh_dev, const void* x_dev, const v
   if (at.Mp >= kMaxLd - 128 || 2 * at.Fp >= kMaxLd) return CA_EUNSUPPORTED;      // (they are row strides of products)
   if (!workspace_dev || !aligned16(workspace_dev) || workspace_bytes < at.bytes) return CA_EINVAL;
   if (m_rows > 0)
-    for (const void* p : {dh_dev, x_dev, g_dev, u_dev})
+    for (const void* p : {dh_dev, x_dev, static_cast<const void*>(g_dev), static_cast<const void*>(u_dev)})
       if (!p) return CA_EINVAL;
   if (!w_gate_dev || !w_up_dev || (!dx_dev && !dw_gate_dev && !dw_up_dev)) return CA_EINVAL;
-  for (const void* p : {dh_dev, x_dev, w_gate_dev, w_up_dev, g_dev, u_dev, static_cast<const void*>(dx_dev), static_cast<const void*>(dw_gate_dev),
+  for (const void* p : {dh_dev, x_dev, w_gate_dev, w_up_dev, static_cast<const void*>(g_dev), static_cast<const void*>(u_dev), static_cast<const void*>(dx_dev), static_cast<const void*>(dw_gate_dev),
                         static_cast<const void*>(dw_up_dev)})
     if (!aligned16(p)) return CA_EINVAL;
   return ca::launch_gated_backward(dh_dev, x_dev, w_gate_dev, w_up_dev, g_dev, u_dev, activation, m_rows > 0 ? dx_dev : nullptr, dw_gate_dev,

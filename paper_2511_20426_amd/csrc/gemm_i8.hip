@@ -11,11 +11,17 @@ namespace {
 #include "rope_device.hpp"
 #include "gemm_tiles.hpp"
 #include "gemm_tile_kernel.hpp"
+#include "quantize_device.hpp"
 #include "gemm_ops.hpp"
+#include "gemm_op_rows.hpp"
 #include "gemm_op_tiles.hpp"
 #include "gemm_few.hpp"
 
 constexpr int kFewTokens = 32;
+
+constexpr OpModel kModel[] = {{256, 256, 1, 1160, 960, 1310, 6070}, {192, 256, 1, 620, 775, 970, 5700}, {128, 256, 1, 2020, 570, 765, 3500},
+                              {256, 128, 1, 0, 725, 870, 5300},     {128, 128, 1, 0, 445, 470, 3700},   {64, 64, 2, 0, 275, 355, 2300},
+                              {64, 64, 1, 0, 165, 165, 3000}};
 
 }  // namespace
 
@@ -27,12 +33,48 @@ int32_t launch_gemm_i8(const void* x, const float* x_scales, const void* w, cons
   a.ldy = ldy;
   a.M = int32_t(M); a.N = N; a.K = (K + 255) / 256 * 256;
   a.ldx = int32_t(ldx); a.ldw = int32_t(ldw);
-  const KernelLds kernels[] = {{reinterpret_cast<const void*>(gemm_op_kernel<Tile128, I8>), Tile128::kLds},
-                               {reinterpret_cast<const void*>(gemm_op_kernel<Tile64, I8>), Tile64::kLds}};
-  if (const int32_t rc = ensure_dynamic_lds(kernels, 2, kLdsI8); rc != CA_OK) return rc;
-  if (M <= kFewTokens) return enqueue_few<I8>(a, "gemm_i8.hip", stream);
-  const int64_t tiles = ((M + 127) / 128) * ((N + 127) / 128);
-  return tiles >= 128 ? enqueue_op_tile<Tile128, I8>(a, "gemm_i8.hip", stream) : enqueue_op_tile<Tile64, I8>(a, "gemm_i8.hip", stream);
+  const KernelLds kernels[] = {{reinterpret_cast<const void*>(gemm_op_rows_kernel<8, I8>), kOpRowsLds},
+                               {reinterpret_cast<const void*>(gemm_op_rows_kernel<6, I8>), kOpRowsLds},
+                               {reinterpret_cast<const void*>(gemm_op_rows_kernel<4, I8>), kOpRowsLds},
+                               {reinterpret_cast<const void*>(gemm_op_kernel<Tile256x128, I8>), Tile256x128::kLds},
+                               {reinterpret_cast<const void*>(gemm_op_kernel<Tile128, I8>), Tile128::kLds},
+                               {reinterpret_cast<const void*>(gemm_op_kernel<Tile64, I8>), Tile64::kLds},
+                               {reinterpret_cast<const void*>(gemm_op_kernel<Tile64Wide, I8>), Tile64Wide::kLds}};
+  if (const int32_t rc = ensure_dynamic_lds(kernels, 7, kLdsI8); rc != CA_OK) return rc;
+  int n_cu = 0;
+  if (const int32_t rc = device_cu_count(&n_cu); rc != CA_OK) return rc;
+  constexpr const char* kWhat = "gemm_i8.hip";
+  if (M <= kFewTokens) return enqueue_few<I8>(a, kWhat, stream);
+  switch (pick_op(kModel, M, N, a.K / 128, n_cu)) {
+    case kOpRows256: return enqueue_op_rows<8, I8>(a, kWhat, stream);
+    case kOpRows192: return enqueue_op_rows<6, I8>(a, kWhat, stream);
+    case kOpRows128: return enqueue_op_rows<4, I8>(a, kWhat, stream);
+    case kOpTile256x128: return enqueue_op_tile<Tile256x128, I8>(a, kWhat, stream);
+    case kOpTile128: return enqueue_op_tile<Tile128, I8>(a, kWhat, stream);
+    case kOpTile64: return enqueue_op_tile<Tile64, I8>(a, kWhat, stream);
+    default: return enqueue_op_tile<Tile64Wide, I8>(a, kWhat, stream);
+  }
+}
+
+int32_t launch_gemm_i8_values(int dtype, const void* x, int64_t ldx, const void* w, const float* w_scales, void* y, int64_t M, int32_t N, int32_t K,
+                              int64_t ldw, int64_t ldy, void* workspace, void* stream) {
+  if (M == 0) return CA_OK;
+  // Up to kCodeRows tokens go in one launch, unless making the codes in every workgroup costs more than the launch that it saves.  Us with
+  // codes made in the launch / ahead, weights from memory: one token 15360 x 5120 20.3 / 20.8, 5120 x 5120 11.0 / 13.5, 4608 x 1536 8.8 /
+  // 10.8; two 22.5 / 21.2, 11.7 / 13.9, 8.8 / 10.6; four 26.5 / 22.4, 14.3 / 14.2, 8.9 / 10.6.
+  if (dtype == CA_BF16 && M <= kCodeRows && K <= kCodeK && M * ((N + 15) / 16) * K <= 6000000 && K % 8 == 0 && (reinterpret_cast<uintptr_t>(x) | uint64_t(ldx) * 2) % 16 == 0) {
+    OpArgs a{};
+    a.x = x; a.w = w; a.y = y; a.w2 = w_scales;
+    a.ldy = ldy;
+    a.M = int32_t(M); a.N = N; a.K = (K + 255) / 256 * 256; a.k_values = K;
+    a.ldx = int32_t(2 * ldx); a.ldw = int32_t(ldw);
+    hipLaunchKernelGGL((gemm_few_kernel<I8, 1, true>), dim3(unsigned((N + 15) / 16)), dim3(64 * kFewWaves), 0, static_cast<hipStream_t>(stream), a);
+    return finish_launch("gemm_i8.hip");
+  }
+  const int64_t ld = (K + 255) / 256 * 256;
+  float* const scales = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + M * ld);
+  if (const int32_t rc = launch_quantize_rows(dtype, x, workspace, scales, M, K, ldx, ld, stream); rc != CA_OK) return rc;
+  return launch_gemm_i8(workspace, scales, w, w_scales, y, M, N, K, ld, ldw, ldy, stream);
 }
 
 }  // namespace ca

@@ -50,25 +50,23 @@ __global__ __launch_bounds__(T::kThreads) void gemm_op_kernel(OpArgs a) {
 
   // ---- the results go through LDS to leave row by row.  A lane has columns 4 grp .. +3 of row l15 of a sub-tile.
   constexpr int kPitch = kCols * 2 + 16;
-  bool save = false;
   if constexpr (Op::kGated) {
     constexpr int kHalf = T::kTn / 2;
-    static_assert(3 * BM * kPitch <= T::kLds, "the result and both projections fit");
-    save = a.g != nullptr;
 #pragma unroll
     for (int i = 0; i < kHalf; ++i)
 #pragma unroll
       for (int j = 0; j < T::kTm; ++j) {
-        f32x4 h;
+        const f32x4 &g = acc[i][j], &u = acc[i + kHalf][j];
+        const int row = (wm * T::kTm + j) * 16 + l15, col = (wn * kHalf + i) * 16 + 4 * grp;
+        float h[4];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) h[e] = gated_value(acc[i][j][e], acc[i + kHalf][j][e], a.act0, a.act1);
-        uint32_t* to = reinterpret_cast<uint32_t*>(lds + ((wm * T::kTm + j) * 16 + l15) * kPitch + ((wn * kHalf + i) * 16 + 4 * grp) * 2);
-        const f32x4* of[3] = {&h, &acc[i][j], &acc[i + kHalf][j]};
-#pragma unroll
-        for (int part = 0; part < 3; ++part) {
-          if (part > 0 && !save) break;
-          to[part * (BM * kPitch / 4)] = pack_bf16((*of[part])[0], (*of[part])[1]);
-          to[part * (BM * kPitch / 4) + 1] = pack_bf16((*of[part])[2], (*of[part])[3]);
+        for (int e = 0; e < 4; ++e) h[e] = gated_value(g[e], u[e], a.act0, a.act1);
+        uint32_t* to = reinterpret_cast<uint32_t*>(lds + row * kPitch + col * 2);
+        to[0] = pack_bf16(h[0], h[1]);
+        to[1] = pack_bf16(h[2], h[3]);
+        if (a.g && m0 + row < a.M && n0 + col < a.N) {
+          *reinterpret_cast<f32x4*>(a.g + int64_t(m0 + row) * a.ld_saved + n0 + col) = g;
+          *reinterpret_cast<f32x4*>(a.u + int64_t(m0 + row) * a.ld_saved + n0 + col) = u;
         }
       }
   } else {
@@ -92,18 +90,11 @@ __global__ __launch_bounds__(T::kThreads) void gemm_op_kernel(OpArgs a) {
   __syncthreads();
   constexpr int kChunks = kCols / 8, kRows = T::kThreads / kChunks;
   const int c = tid % kChunks;
-  auto leave = [&](int part, uint16_t* y, int64_t ldy) {
 #pragma unroll 4
-    for (int row = tid / kChunks; row < BM; row += kRows) {
-      const u32x4 v = *reinterpret_cast<const u32x4*>(lds + part * BM * kPitch + row * kPitch + c * 16);
-      if (m0 + row < a.M && n0 + c * 8 < a.N)
-        __builtin_nontemporal_store(v, reinterpret_cast<u32x4*>(y + int64_t(m0 + row) * ldy + n0 + c * 8));
-    }
-  };
-  leave(0, static_cast<uint16_t*>(a.y), a.ldy);
-  if (save) {
-    leave(1, a.g, a.ld_saved);
-    leave(2, a.u, a.ld_saved);
+  for (int row = tid / kChunks; row < BM; row += kRows) {
+    const u32x4 v = *reinterpret_cast<const u32x4*>(lds + row * kPitch + c * 16);
+    if (m0 + row < a.M && n0 + c * 8 < a.N)
+      __builtin_nontemporal_store(v, reinterpret_cast<u32x4*>(static_cast<uint16_t*>(a.y) + int64_t(m0 + row) * a.ldy + n0 + c * 8));
   }
 }
 

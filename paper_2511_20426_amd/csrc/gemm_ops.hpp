@@ -10,11 +10,12 @@ struct OpArgs {
   void* y;                                        // bf16 [M][ldy]
   const void* w2;                                 // gated: the up projection's weights [N][ldw2 bytes]; 8 bits: scales of w's rows
   const float* xs;                                // 8 bits: scales of x's rows
-  uint16_t* g;                                    // gated, training: both projections, or null
-  uint16_t* u;
+  float* g;                                       // gated, training: both projections, or null
+  float* u;
   int64_t ldy, ld_saved;                          // in elements
   int32_t M, N, K, ldx, ldw, ldw2;                // K in bytes of a row: a multiple of 256
   int32_t tiles_m, tiles_n, more;                 // as in LinearArgs
+  int32_t k_values;                               // 8 bits of values that are made codes on the way: values of a row
   float act0, act1;                               // gated: act(g) = g sigmoid(g (act0 + act1 g^2))
 };
 
@@ -47,3 +48,29 @@ struct Gated {
 
 // y = sum * scale of the token * scale of the channel, in fp32; rounded to bf16 once by the caller
 __device__ __forceinline__ float scaled(int32_t sum, float xs, float ws) { return float(sum) * xs * ws; }
+
+// What one of these products may be taken by, cheapest first by a model of what was measured, in nanoseconds (`rows` rows of X and `cols`
+// of W to a tile): start + whole rounds of tiles over the CUs x (stages x full + tile) + a last round (stages x stage + tile), the stage
+// of a last round between `stage` and `full` from half of the slots on in proportion.
+struct OpModel {
+  int rows, cols, per_cu, start, stage, full, tile;
+};
+
+template <int kN>
+int pick_op(const OpModel (&models)[kN], int64_t M, int64_t w_rows, int64_t stages, int n_cu) {
+  int64_t best = INT64_MAX;
+  int at = 0;
+  for (int i = 0; i < kN; ++i) {
+    const OpModel& m = models[i];
+    const int64_t tiles = ((M + m.rows - 1) / m.rows) * ((w_rows + m.cols - 1) / m.cols), slots = int64_t(n_cu) * m.per_cu, left = tiles % slots;
+    const int64_t stage = m.stage + (2 * left > slots ? (m.full - m.stage) * (2 * left - slots) / slots : 0);
+    const int64_t cost = m.start + tiles / slots * (stages * m.full + m.tile) + (left > 0 ? stages * stage + m.tile : 0);
+    if (cost < best) {
+      best = cost;
+      at = i;
+    }
+  }
+  return at;
+}
+
+enum { kOpRows256, kOpRows192, kOpRows128, kOpTile256x128, kOpTile128, kOpTile64, kOpTile64Wide };

@@ -21,6 +21,18 @@ random operands, TFLOP/s: rows of tiles one after the other 2110, two rows forth
 2243.  For that X's fragments of a whole stage are held in registers (two sets, the next stage's is read behind the
 barrier) and W's of two rows of tiles (three sets in turn).
 
+Besides the plain product ("plain") two relatives are emitted, gemm_rows_i8_* and gemm_rows_gated_*: stages are 128 bytes of
+a row whatever they hold, so that loads, rings, barriers and slots are the same and only the matrix instruction and the way out differ.
+
+8 bits ("i8"): v_mfma_i32_16x16x64_i8, 128 k to a stage.  Sums leave multiplied with the scales of their row of X and row of W.  A
+lane's 32 scales of W stay in registers; those of X, one to a lane, are handed to the lanes that need them by ds_bpermute.  The
+next tile's are requested when a tile has left, ahead of the stages' loads behind it, so that the waits of the stages cover them.
+
+Gated ("gated"): Y = act(X Wg') * (X Wu').  Of a tile's 256 rows of W, waves 0 and 2 load 64 rows of the gate's each and waves 1 and 3
+the up projection's of the same columns, so that of a wave's 8 sub-tiles over n the first four are gate, the last four up, and a lane
+ends up with both of the same elements; a tile has 128 columns of Y.  act(g) = g / (1 + exp(-p)), p = g (act0 + act1 g^2), g held
+within 1e4 there.  With %[save] the projections leave too, in fp32, straight from the accumulators.
+
 Register map:
   a[0:32 MT - 1]   accumulators, sub-tile (ti over n, tj over m) at a[4 (MT ti + tj) ..]
   v[0:127]    X fragments: stage parity p, k-step kk, sub-tile tj at v[64 p + 32 kk + 4 tj ..]; set 1 is scratch between tiles
@@ -28,6 +40,7 @@ Register map:
   v176..v181  LDS read addresses of W: v[176 + 2 ring slot + kk];  v182..v185 of X
   v186..v193, v194..v201  lane's byte offset from the stage's global base for W / X loads 0..7
   v202..v205  address of the lane's row of Y, temporaries
+  i8: v206..v237 scales of the lane's columns: 8 of each pair of sub-tiles; v238, v239 of rows 0..63 / 64..127 of the wave, one to a lane
 """
 from __future__ import annotations
 
@@ -42,6 +55,8 @@ ADDRW, ADDRX = 176, 182  # + 2*ring slot + kk
 OFFW, OFFX = 186, 194    # +i
 YROW, VT = 202, 204      # address of the lane's row (two registers), temporaries (two)
 LAST_VGPR = 205
+SCALEW, SCALEX = 206, 238  # i8
+LAST_VGPR_I8 = 239
 
 S_BW, S_BX = 36, 38      # global bases of the W / X stage being loaded (64-bit each)
 S_WSTEP, S_XSTEP = 40, 41  # bytes from one stage to the next: 128, 0 behind the last tile
@@ -53,6 +68,9 @@ S_RET = 54               # 54,55: where out-of-line code returns to
 S_T = 56                 # 56..63 temporaries
 S_COLS = 64              # 64..67: lanes whose columns exist, of the first 64 and the others
 S_ROWS, S_NCOL = 68, 69  # rows and columns of the tile that exist
+S_P = 70                 # 70,71: base of the scales; gated: 70 the bound on g, 70..73 strides
+LAST_SGPR = 73
+MFMA = {"plain": "v_mfma_f32_16x16x32_bf16", "gated": "v_mfma_f32_16x16x32_bf16", "i8": "v_mfma_i32_16x16x64_i8"}
 
 
 def xfrag(p, kk, tj):
@@ -63,9 +81,9 @@ def wfrag(buf, i, kk):
     return 128 + 16 * (buf % 3) + 8 * i + 4 * kk
 
 
-def mfma(P, ti, tj, kk, mt):
+def mfma(P, ti, tj, kk, mt, kind="plain"):
     acc = A(4 * (mt * ti + tj), 4)
-    return f"v_mfma_f32_16x16x32_bf16 {acc}, {V(wfrag(P + ti // 2, ti % 2, kk), 4)}, {V(xfrag(P % 2, kk, tj), 4)}, {acc}"
+    return f"{MFMA[kind]} {acc}, {V(wfrag(P + ti // 2, ti % 2, kk), 4)}, {V(xfrag(P % 2, kk, tj), 4)}, {acc}"
 
 
 def read_w(stage, ti, kk):
@@ -104,13 +122,13 @@ def w_due_lines(tag, cold):
     return [f"s_sub_u32 s{S_WL}, s{S_WL}, 1", f"s_cmp_eq_u32 s{S_WL}, 0", "s_nop 0", f"s_cbranch_scc1 {go}", f"{back}:"]
 
 
-def next_tile_lines(op, mt):
+def next_tile_lines(op, mt, kind="plain"):
     """The tile whose stages are requested next: its base, less a step, and the lanes' offsets if it has another number of
     rows than the one before (rows past the end re-read the last one).  Behind the last tile its last stage is requested
     over and over, into buffers that nothing reads."""
     name = "W" if op == 0 else "X"
     base, step, t, lim, off = (S_BW, S_WSTEP, S_WT, S_WLIM, OFFW) if op == 0 else (S_BX, S_XSTEP, S_XT, S_XLIM, OFFX)
-    rows, total, stride, ld, n, first, chunk = ((256, "%[N]", "%[tile_w]", "%[ldw2]", 8, "%[roww]", "%[chunkw]") if op == 0 else
+    rows, total, stride, ld, n, first, chunk = ((128 if kind == "gated" else 256, "%[N]", "%[tile_w]", "%[ldw2]", 8, "%[roww]", "%[chunkw]") if op == 0 else
                                                 (32 * mt, "%[M]", "%[tile_x]", "%[ldx2]", mt, "%[rowx]", "%[chunkx]"))
     a = S_T
     out = [f"s_mov_b32 s{S_WL}, s{S_HALF}"] if op == 0 else []
@@ -133,23 +151,107 @@ def next_tile_lines(op, mt):
 FORMS = ("", " sc1", " nt")     # how results are written: left in L2, written through it, past the caches
 
 
-def result_lines(mt):
+def lane_lines(v):
+    """the lane's number"""
+    return [f"v_mbcnt_lo_u32_b32 {V(v)}, -1, 0", f"v_mbcnt_hi_u32_b32 {V(v)}, -1, {V(v)}"]
+
+
+def scale_lines(mt):
+    """i8: the scales of tile S_YT are requested; columns and rows past the end take the last ones'."""
+    a, t = S_T, 84
+    out = [f"v_readlane_b32 s{a}, %[list_m], s{S_YT}", f"v_readlane_b32 s{a + 1}, %[list_n], s{S_YT}"] + lane_lines(t) + ["s_nop 3",
+           # columns tn 256 + (wave / 2) 128 + 32 c + 8 grp, rows tm 32 mt + (wave % 2) 16 mt + lane
+           f"s_lshl_b32 s{a + 1}, s{a + 1}, 8", f"s_lshr_b32 s{a + 2}, %[wave], 1", f"s_lshl_b32 s{a + 2}, s{a + 2}, 7",
+           f"s_add_u32 s{a + 1}, s{a + 1}, s{a + 2}", f"s_mul_i32 s{a}, s{a}, {32 * mt}", f"s_and_b32 s{a + 2}, %[wave], 1",
+           f"s_mul_i32 s{a + 2}, s{a + 2}, {16 * mt}", f"s_add_u32 s{a}, s{a}, s{a + 2}", f"s_sub_u32 s{a + 2}, %[N], 8", f"s_sub_u32 s{a + 3}, %[M], 1",
+           f"s_mov_b32 s{S_P}, %[ws_lo]", f"s_mov_b32 s{S_P + 1}, %[ws_hi]",
+           f"v_lshrrev_b32 {V(t + 1)}, 4, {V(t)}", f"v_lshlrev_b32 {V(t + 1)}, 3, {V(t + 1)}", f"v_add_u32 {V(t + 1)}, s{a + 1}, {V(t + 1)}"]
+    for c in range(4):
+        out += [f"v_add_u32 {V(t + 2)}, {32 * c}, {V(t + 1)}", f"v_min_u32 {V(t + 2)}, s{a + 2}, {V(t + 2)}", f"v_lshlrev_b32 {V(t + 2)}, 2, {V(t + 2)}"]
+        out += [f"global_load_dwordx4 {V(SCALEW + 8 * c + 4 * i, 4)}, {V(t + 2)}, s[{S_P}:{S_P + 1}] offset:{16 * i}" for i in range(2)]
+    out += [f"s_mov_b32 s{S_P}, %[xs_lo]", f"s_mov_b32 s{S_P + 1}, %[xs_hi]", f"v_add_u32 {V(t)}, s{a}, {V(t)}"]
+    for i in range(1 if mt == 4 else 2):
+        out += [f"v_add_u32 {V(t + 2)}, {64 * i}, {V(t)}", f"v_min_u32 {V(t + 2)}, s{a + 3}, {V(t + 2)}", f"v_lshlrev_b32 {V(t + 2)}, 2, {V(t + 2)}",
+                f"global_load_dword {V(SCALEX + i)}, {V(t + 2)}, s[{S_P}:{S_P + 1}]"]
+    return out
+
+
+def handed_lines(mt):
+    """i8: the scale of row 16 tj + lane % 16 to each lane, in v[88 + tj] (a lane reads that of lane (address + offset) / 4)"""
+    t = 84
+    return (lane_lines(t) + [f"v_and_b32 {V(t)}, 15, {V(t)}", f"v_lshlrev_b32 {V(t)}, 2, {V(t)}"] +
+            [f"ds_bpermute_b32 {V(88 + tj)}, {V(t)}, {V(SCALEX + tj // 4)} offset:{64 * (tj % 4)}" for tj in range(mt)] + ["s_waitcnt lgkmcnt(0)"])
+
+
+def gate_lines(mt, tj, c, pack):
+    """gated: eight elements of h, rounded to bf16, in v[pack ..]; gate in sub-tiles 2 c, 2 c + 1 of four, up in those four on"""
+    g, u, p, q = 64, 72, 104, 120
+    out = []
+    for i in range(8):
+        out.append(f"v_accvgpr_read_b32 {V(g + i)}, {A(4 * (mt * (2 * c + i // 4) + tj) + i % 4)}")
+    for i in range(8):
+        out.append(f"v_accvgpr_read_b32 {V(u + i)}, {A(4 * (mt * (2 * c + 4 + i // 4) + tj) + i % 4)}")
+    for step in ("v_med3_f32 {p}, {g}, s%d, -s%d" % (S_P, S_P), "v_mul_f32 {q}, {p}, {p}", "v_fma_f32 {q}, {q}, %%[act1], %s" % V(95),
+                 "v_mul_f32 {p}, {p}, {q}", "v_mul_f32 {p}, 0xbfb8aa3b, {p}", "v_exp_f32 {p}, {p}", "v_add_f32 {p}, 1.0, {p}", "v_rcp_f32 {p}, {p}",
+                 "v_mul_f32 {p}, {g}, {p}", "v_mul_f32 {p}, {p}, {u}"):
+        out += [step.format(g=V(g + i), u=V(u + i), p=V(p + i), q=V(q + i)) for i in range(8)]
+    return out + [f"v_cvt_pk_bf16_f32 {V(pack + i)}, {V(p + 2 * i)}, {V(p + 2 * i + 1)}" for i in range(4)]
+
+
+def save_lines(mt):
+    """gated, training: g and u in fp32, 16 bytes of a row to a lane straight from an accumulator.  (S_T + 2, + 3: the tile's rows and
+    columns that are ahead of it; row masks for all 16 rows of a sub-tile here.)"""
+    a, t, g, u = S_T, 84, 86, 88
+    out = ["s_cmp_eq_u64 %[g], 0", "s_nop 0", "s_cbranch_scc1 SAVED_%="] + lane_lines(t)
+    out += [f"v_lshrrev_b32 {V(t + 1)}, 4, {V(t)}", f"v_lshlrev_b32 {V(t + 1)}, 3, {V(t + 1)}", f"v_and_b32 {V(t)}, 15, {V(t)}",
+            # row of the tile (wave % 2) 16 mt + lane % 16, column (wave / 2) 64 + 8 grp
+            f"s_and_b32 s{a + 4}, %[wave], 1", f"s_mul_i32 s{a + 4}, s{a + 4}, {16 * mt}", f"v_add_u32 {V(t)}, s{a + 4}, {V(t)}",
+            f"s_lshr_b32 s{a + 4}, %[wave], 1", f"s_lshl_b32 s{a + 4}, s{a + 4}, 6", f"v_add_u32 {V(t + 1)}, s{a + 4}, {V(t + 1)}"]
+    for c in range(2):
+        out += [f"s_sub_i32 s{a + 4}, s{S_NCOL}, {32 * c}", f"v_cmp_gt_i32 s[{S_COLS + 2 * c}:{S_COLS + 2 * c + 1}], s{a + 4}, {V(t + 1)}"]
+    # g + 4 ((tm 32 mt + row) ld + tn 128 + column)
+    out += [f"s_mul_i32 s{a + 4}, s{a}, {32 * mt}", f"v_add_u32 {V(90)}, s{a + 4}, {V(t)}", f"s_lshl_b32 s{a + 4}, s{a + 1}, 7",
+            f"v_add_u32 {V(t + 1)}, s{a + 4}, {V(t + 1)}", f"v_lshlrev_b32 {V(t + 1)}, 2, {V(t + 1)}",
+            f"v_mul_lo_u32 {V(g)}, {V(90)}, %[ld4]", f"v_mul_hi_u32 {V(g + 1)}, {V(90)}, %[ld4]",
+            f"v_add_co_u32 {V(g)}, vcc, {V(g)}, {V(t + 1)}", "s_nop 1", f"v_addc_co_u32 {V(g + 1)}, vcc, 0, {V(g + 1)}, vcc"]
+    for to, name in ((u, "u"), (g, "g")):
+        out += [f"v_mov_b32 {V(91)}, %[{name}_hi]", f"v_add_co_u32 {V(to)}, vcc, %[{name}_lo], {V(g)}", "s_nop 1",
+                f"v_addc_co_u32 {V(to + 1)}, vcc, {V(91)}, {V(g + 1)}, vcc"]
+    for tj in range(mt):
+        out += [f"s_sub_i32 s{a + 4}, s{S_ROWS}, {16 * tj}", f"v_cmp_gt_i32 vcc, s{a + 4}, {V(t)}", "s_nop 1"]
+        for c in range(2):
+            out.append(f"s_and_b64 exec, vcc, s[{S_COLS + 2 * c}:{S_COLS + 2 * c + 1}]")
+            for b in range(2):
+                out += [f"global_store_dwordx4 {V(to, 2)}, {A(4 * (mt * (2 * c + b + of) + tj), 4)}, off offset:{128 * c + 16 * b}"
+                        for to, of in ((g, 0), (u, 4))]
+        out.append("s_mov_b64 exec, -1")
+        if tj < mt - 1:
+            for to in (g, u):
+                out += [f"v_add_co_u32 {V(to)}, vcc, %[ld64], {V(to)}", "s_nop 1", f"v_addc_co_u32 {V(to + 1)}, vcc, 0, {V(to + 1)}, vcc"]
+    return out + ["SAVED_%=:"]
+
+
+def result_lines(mt, kind="plain"):
     """A tile's sums leave, rounded to bf16, 16 bytes of a row to a lane, in the form that %[form] has for the last tile of the
     workgroup or for the others, and start from zero again if there is a next tile.  (Between a vector instruction that writes VCC
     or a scalar register and one that reads it stand two wait states, as the compiler has it for gfx950.)"""
-    a = S_T
+    a, gated, stored = S_T, kind == "gated", 1 if kind == "gated" else 2       # stored: pieces of 64 columns of a wave
     out = ["s_nop 15", "s_nop 15",                         # the last MFMAs have written back
            f"v_readlane_b32 s{a}, %[list_m], s{S_YT}", f"v_readlane_b32 s{a + 1}, %[list_n], s{S_YT}", "s_nop 3",
            # y + tm * (rows of a tile) + tn * 512 bytes
            f"s_mul_i32 s{a + 2}, s{a}, %[tile_y_lo]", f"s_mul_hi_u32 s{a + 3}, s{a}, %[tile_y_lo]", f"s_mul_i32 s{a + 4}, s{a}, %[tile_y_hi]",
            f"s_add_u32 s{a + 3}, s{a + 3}, s{a + 4}", f"s_add_u32 s{a + 2}, s{a + 2}, %[y_lo]", f"s_addc_u32 s{a + 3}, s{a + 3}, %[y_hi]",
-           f"s_lshl_b32 s{a + 4}, s{a + 1}, 9", f"s_add_u32 s{a + 2}, s{a + 2}, s{a + 4}", f"s_addc_u32 s{a + 3}, s{a + 3}, 0",
+           f"s_lshl_b32 s{a + 4}, s{a + 1}, {8 if gated else 9}", f"s_add_u32 s{a + 2}, s{a + 2}, s{a + 4}", f"s_addc_u32 s{a + 3}, s{a + 3}, 0",
            f"v_add_co_u32 {V(YROW)}, vcc, s{a + 2}, %[ylane_lo]", f"v_mov_b32 {V(VT)}, s{a + 3}", "s_nop 0",
            f"v_addc_co_u32 {V(YROW + 1)}, vcc, {V(VT)}, %[ylane_hi], vcc",
            # what exists of the tile
            f"s_mul_i32 s{a + 4}, s{a}, {32 * mt}", f"s_sub_u32 s{S_ROWS}, %[M], s{a + 4}",
-           f"s_lshl_b32 s{a + 4}, s{a + 1}, 8", f"s_sub_u32 s{S_NCOL}, %[N], s{a + 4}"]
-    for c in range(2):
+           f"s_lshl_b32 s{a + 4}, s{a + 1}, {7 if gated else 8}", f"s_sub_u32 s{S_NCOL}, %[N], s{a + 4}"]
+    if kind == "i8":
+        out += handed_lines(mt)
+    if gated:
+        out += save_lines(mt) + [f"s_mov_b32 s{S_P}, 0x461c4000", f"v_mov_b32 {V(95)}, %[act0]"]       # 1e4
+    for c in range(stored):
         out += [f"s_sub_i32 s{a + 4}, s{S_NCOL}, {64 * c}", f"v_cmp_gt_i32 s[{S_COLS + 2 * c}:{S_COLS + 2 * c + 1}], s{a + 4}, %[col]"]
     out += [f"s_add_u32 s{S_YT}, s{S_YT}, 1", f"s_and_b32 s{a + 5}, %[form], 3", f"s_lshr_b32 s{a + 6}, %[form], 2",
             f"s_cmp_lt_u32 s{S_YT}, %[tiles]", f"s_cselect_b32 s{a + 5}, s{a + 5}, s{a + 6}"]
@@ -159,22 +261,29 @@ def result_lines(mt):
         out.append(f"FORM{k}_%=:")
         for tj in range(mt):
             pack = 96 + 16 * (tj % 2)
-            for c in range(4):
+            for c in range(2 if gated else 4):
+                if gated:
+                    out += gate_lines(mt, tj, c, pack + 4 * c)
+                    continue
                 acc = 64 + 8 * (c % 2)
                 for i in range(8):                         # sub-tiles 2 c and 2 c + 1
                     out.append(f"v_accvgpr_read_b32 {V(acc + i)}, {A(4 * (mt * (2 * c + i // 4) + tj) + i % 4)}")
+                if kind == "i8":
+                    out += [f"v_cvt_f32_i32 {V(acc + i)}, {V(acc + i)}" for i in range(8)]
+                    out += [f"v_mul_f32 {V(acc + i)}, {V(acc + i)}, {V(88 + tj)}" for i in range(8)]
+                    out += [f"v_mul_f32 {V(acc + i)}, {V(acc + i)}, {V(SCALEW + 8 * c + i)}" for i in range(8)]
                 for i in range(4):
                     out.append(f"v_cvt_pk_bf16_f32 {V(pack + 4 * c + i)}, {V(acc + 2 * i)}, {V(acc + 2 * i + 1)}")
             # whole lines: of two pairs of sub-tiles, lanes 0..7 and 8..15 of a group exchange the one they do not keep (a register
             # is read across lanes two or more instructions after it was written)
-            for c in (0, 2):
+            for c in (0, 2)[:stored]:
                 kept, other, t = pack + 4 * c, pack + 4 * c + 4, 80 + 2 * c
                 out += [f"v_mov_b32 {V(t + i)}, {V(other + i)}" for i in range(4)]
                 out += [f"v_mov_b32_dpp {V(other + i)}, {V(kept + i)} row_ror:8 row_mask:0xf bank_mask:0x3" for i in range(4)]
                 out += [f"v_mov_b32_dpp {V(kept + i)}, {V(t + i)} row_ror:8 row_mask:0xf bank_mask:0xc" for i in range(4)]
             for half in range(2):                          # rows 0..7 of the sixteen, then the others
                 out += [f"s_sub_i32 s{a + 4}, s{S_ROWS}, {16 * tj + 8 * half}", f"v_cmp_gt_i32 vcc, s{a + 4}, %[row]", "s_nop 1"]
-                for c in range(2):
+                for c in range(stored):
                     out += [f"s_and_b64 exec, vcc, s[{S_COLS + 2 * c}:{S_COLS + 2 * c + 1}]",
                             f"global_store_dwordx4 {V(YROW, 2)}, {V(pack + 8 * c + 4 * half, 4)}, off offset:{128 * c}{form}"]
                 out.append("s_mov_b64 exec, -1")
@@ -184,18 +293,20 @@ def result_lines(mt):
         if k < 2:
             out.append("s_branch LEFT_%=")
     out += ["LEFT_%=:", f"s_mov_b32 s{S_TRIPS}, s{S_HALF}", f"s_cmp_lt_u32 s{S_YT}, %[tiles]", "s_nop 0", "s_cbranch_scc1 CLEAR_%=",
-            f"s_waitcnt vmcnt({4 * mt})",                  # the last tile: every load has landed; the results need not have
+            f"s_waitcnt vmcnt({2 * stored * mt})",                  # the last tile: every load has landed; the results need not have
             "s_branch DONE_%=", "CLEAR_%=:"]
+    if kind == "i8":
+        out += scale_lines(mt)
     return (out + [f"v_accvgpr_write_b32 {A(r)}, 0" for r in range(32 * mt)] +
             ["s_nop 7", f"s_cmp_eq_u32 s{S_HALF}, 1", "s_nop 0", "s_cbranch_scc1 TILEX_%=", f"s_setpc_b64 s[{S_RET}:{S_RET + 1}]"])
 
 
-def build_stage(P, mt=8, cold=None):
+def build_stage(P, mt=8, cold=None, kind="plain"):
     """Stage P (mod PERIOD) of the steady state: 16 mt slots of (MFMA, lines issued after it)."""
     cold = [] if cold is None else cold
     slots, x_by, pair = 16 * mt, 5 * mt, 4 * mt             # pair: slots of two rows of tiles
     half = slots // 2
-    mf = [mfma(P, ti, tj, kk, mt) for ti, tj in tile_order(mt) for kk in range(2)]
+    mf = [mfma(P, ti, tj, kk, mt, kind) for ti, tj in tile_order(mt) for kk in range(2)]
     tail = [[] for _ in range(slots)]
     # in front of the barrier: this stage's last fragments are in registers, everything but the W loads issued last has landed (and the
     # results of a tile that left at the start of this stage); behind it this stage's buffers are free
@@ -244,7 +355,7 @@ def build_stage(P, mt=8, cold=None):
     return out
 
 
-def generate(mt=8):
+def generate(mt=8, kind="plain"):
     L, cold = [], []
     e = L.append
     e(f"s_mov_b32 s{S_NST}, %[n_stages]")
@@ -259,6 +370,8 @@ def generate(mt=8):
     for r in (S_WSTEP, S_XSTEP):
         e(f"s_mov_b32 s{r}, 128")
     e(f"s_mov_b32 s{S_YT}, 0")
+    if kind == "i8":                                      # (older than every load that a wait counts)
+        L.extend(scale_lines(mt))
     # the first tile, stage 0 first, then what the steady state would have requested, in its order: X of stage 1, W of 1 and 2
     for op, name in ((0, "W"), (1, "X")):
         e(f"s_branch FIRST{name}_%=")
@@ -299,7 +412,7 @@ def generate(mt=8):
     e("LOOP_%=:")
     for P in range(PERIOD):
         e(f"; ---- stage {P}")
-        for m, lines in build_stage(P, mt, cold):
+        for m, lines in build_stage(P, mt, cold, kind):
             e(m)
             L.extend(lines)
         if P % 2 == 1:
@@ -311,31 +424,37 @@ def generate(mt=8):
             cold += [f"END{P}_%=:"] + call_lines("PAIR_%=", f"ON{P}_%=", f"E{P}")
     e("s_branch LOOP_%=")
     L += cold
-    L += ["TILEW_%=:"] + next_tile_lines(0, mt) + ["TILEX_%=:"] + next_tile_lines(1, mt)
+    L += ["TILEW_%=:"] + next_tile_lines(0, mt, kind) + ["TILEX_%=:"] + next_tile_lines(1, mt, kind)
     # a tile ends, or its last two stages begin: X of those behind them is the next tile's
-    L += ["PAIR_%=:", f"s_cmp_eq_u32 s{S_TRIPS}, 1", "s_nop 0", "s_cbranch_scc1 TILEX_%="] + result_lines(mt)
+    L += ["PAIR_%=:", f"s_cmp_eq_u32 s{S_TRIPS}, 1", "s_nop 0", "s_cbranch_scc1 TILEX_%="] + result_lines(mt, kind)
     e("DONE_%=:")
     return L
 
 
+def write_clobbers(f, name, mt, last_vgpr, last_sgpr):
+    clob = [f"v{i}" for i in range(last_vgpr + 1)] + [f"a{i}" for i in range(32 * mt)] + [f"s{i}" for i in range(36, last_sgpr + 1)]
+    f.write(f"#define {name}{32 * mt} \\\n")
+    for i in range(0, len(clob), 12):
+        chunk = ", ".join(f'"{c}"' for c in clob[i:i + 12])
+        f.write("  " + chunk + (", \\\n" if i + 12 < len(clob) else "\n"))
+
+
 def main(out_path):
     by = "// Generated by gen_gemm_rows.py -- do not edit.\n"
-    clobbers = by
-    for mt in (8, 6, 4):
-        path = out_path.replace("gemm_rows_", f"gemm_rows{32 * mt}_")
-        lines = generate(mt)
-        with open(path, "w") as f:
-            f.write(by)
-            for ln in lines:
-                f.write('"' + ln + '\\n"\n')
-        print(f"{path}: {len(lines)} lines")
-        clob = [f"v{i}" for i in range(LAST_VGPR + 1)] + [f"a{i}" for i in range(32 * mt)] + [f"s{i}" for i in range(36, S_NCOL + 1)]
-        clobbers += f"#define CA_GEMM_ROWS_CLOBBERS{32 * mt} \\\n"
-        for i in range(0, len(clob), 12):
-            chunk = ", ".join(f'"{c}"' for c in clob[i:i + 12])
-            clobbers += "  " + chunk + (", \\\n" if i + 12 < len(clob) else "\n")
-    with open(out_path.replace("gemm_rows_gfx950.inc", "gemm_rows_clobbers.inc"), "w") as f:
-        f.write(clobbers)
+    for kind, tag, name, last_vgpr, last_sgpr in (("plain", "", "CA_GEMM_ROWS_CLOBBERS", LAST_VGPR, S_NCOL),
+                                                  ("i8", "_i8_", "CA_GEMM_ROWS_I8_CLOBBERS", LAST_VGPR_I8, LAST_SGPR),
+                                                  ("gated", "_gated_", "CA_GEMM_ROWS_GATED_CLOBBERS", LAST_VGPR, LAST_SGPR)):
+        with open(out_path.replace("gemm_rows_gfx950.inc", f"gemm_rows{tag.rstrip('_')}_clobbers.inc"), "w") as clobbers:
+            clobbers.write(by)
+            for mt in (8, 6, 4):
+                path = out_path.replace("gemm_rows_", f"gemm_rows{tag}{32 * mt}_")
+                lines = generate(mt, kind)
+                with open(path, "w") as f:
+                    f.write(by)
+                    for ln in lines:
+                        f.write('"' + ln + '\\n"\n')
+                print(f"{path}: {len(lines)} lines")
+                write_clobbers(clobbers, name, mt, last_vgpr, last_sgpr)
 
 
 if __name__ == "__main__":

@@ -14,6 +14,8 @@
 #include <c10/hip/HIPFunctions.h>
 #include <c10/hip/HIPStream.h>
 
+#include <initializer_list>
+
 #include "cascade_attn.h"
 
 namespace {
@@ -26,6 +28,15 @@ decltype(&cascade_attn_forward_share) share_fn = nullptr;
 decltype(&cascade_attn_forward_rope) forward_rope_fn = nullptr;
 decltype(&layer_qkv_publish) publish_fn = nullptr;
 decltype(&layer_linear_bf16) linear_fn = nullptr;
+decltype(&layer_qk_norm_rope) norm_fn = nullptr;
+decltype(&layer_qk_norm_rope_workspace) norm_workspace_fn = nullptr;
+decltype(&layer_qk_norm_rope_backward) norm_backward_fn = nullptr;
+decltype(&kv_cache_append_batch_norm) append_norm_fn = nullptr;
+decltype(&layer_linear_i8_workspace) i8_workspace_fn = nullptr;
+decltype(&layer_linear_i8_values) i8_fn = nullptr;
+decltype(&layer_gated_bf16) gated_fn = nullptr;
+decltype(&layer_gated_backward_workspace) gated_workspace_fn = nullptr;
+decltype(&layer_gated_backward_bf16) gated_backward_fn = nullptr;
 
 constexpr int kMaxBlocks = 64;                    // of a call taken here
 
@@ -115,9 +126,10 @@ struct Result {
     t = plain(o);
     return t != nullptr;
   }
-  const at::Tensor& or_empty(at::IntArrayRef sizes, const at::Tensor& like) {
+  const at::Tensor& or_empty(at::IntArrayRef sizes, const at::Tensor& like) { return or_empty(sizes, like.options()); }
+  const at::Tensor& or_empty(at::IntArrayRef sizes, const at::TensorOptions& options) {
     if (!t) {
-      made = at::empty(sizes, like.options());
+      made = at::empty(sizes, options);
       t = &made;
     }
     return *t;
@@ -164,13 +176,25 @@ PyObject* linear(PyObject* const* a, Py_ssize_t n) {
   return r.give(released([&] { return linear_fn(xp, wp, yp, m, int32_t(cols), int32_t(k), ldx, ldw, ldy, stream); }));
 }
 
-// append_batch(handle, shape, block_ids, timesteps, epoch, ks, vs) -> slots
-PyObject* append_batch(PyObject* const* a, Py_ssize_t n) {
+bool real(PyObject* o, float* v) {
+  if (!PyFloat_CheckExact(o)) return false;
+  *v = float(PyFloat_AS_DOUBLE(o));
+  return true;
+}
+
+// a norm's weight: head_dim values of the pool's type, in one piece
+bool weighs(const Pool& p, const at::Tensor* w) {
+  return w && w->is_cuda() && w->scalar_type() == p.dtype() && w->dim() == 1 && w->size(0) == p.head_dim && w->stride(0) == 1;
+}
+
+// append_batch(handle, shape, block_ids, timesteps, epoch, ks, vs) -> slots; append_batch_norm(..., k_weight, eps)
+PyObject* append(PyObject* const* a, bool norm) {
   Pool p;
   int64_t ids[kMaxBlocks];
   int32_t ts[kMaxBlocks], slots[kMaxBlocks], epoch;
-  const void *ks[kMaxBlocks], *vs[kMaxBlocks];
-  if (n != 7 || !pool_of(a[0], a[1], &p) || !whole32(a[4], &epoch)) return not_taken();
+  const void *ks[kMaxBlocks], *vs[kMaxBlocks], *weight = nullptr;
+  float eps = 0.f;
+  if (!pool_of(a[0], a[1], &p) || !whole32(a[4], &epoch)) return not_taken();
   const int blocks = all<int64_t, whole>(a[2], ids);
   PyObject **k, **v;
   if (blocks < 1 || all<int32_t, whole32>(a[3], ts) != blocks || items(a[5], &k) != blocks || items(a[6], &v) != blocks) return not_taken();
@@ -183,12 +207,199 @@ PyObject* append_batch(PyObject* const* a, Py_ssize_t n) {
     ks[i] = kt->data_ptr();
     vs[i] = vt->data_ptr();
   }
+  if (norm) {
+    const at::Tensor* w = plain(a[7]);
+    if (!weighs(p, w) || !real(a[8], &eps)) return not_taken();
+    weight = w->data_ptr();
+  }
   void* const stream = p.stream();
-  const int32_t rc = released([&] { return append_batch_fn(p.ctx, blocks, ids, ts, epoch, ks, vs, tok, head, stream, slots); });
+  const int32_t rc = released([&] {
+    return norm ? append_norm_fn(p.ctx, blocks, ids, ts, epoch, ks, vs, tok, head, weight, eps, stream, slots)
+                : append_batch_fn(p.ctx, blocks, ids, ts, epoch, ks, vs, tok, head, stream, slots);
+  });
   if (rc != CA_OK) return PyLong_FromLong(rc);
   PyObject* const out = PyList_New(blocks);
   for (int i = 0; out && i < blocks; ++i) PyList_SET_ITEM(out, i, PyLong_FromLong(slots[i]));
   return out;
+}
+PyObject* append_batch(PyObject* const* a, Py_ssize_t n) { return n == 7 ? append(a, false) : not_taken(); }
+PyObject* append_batch_norm(PyObject* const* a, Py_ssize_t n) { return n == 9 ? append(a, true) : not_taken(); }
+
+// of a single token or head the stride is free
+ca_heads view(const Pool& p, const at::Tensor& t) {
+  return ca_heads{t.data_ptr(), t.size(0) > 1 ? t.stride(0) : p.heads * p.head_dim, p.heads > 1 ? t.stride(1) : p.head_dim};
+}
+
+PyObject* tuple(std::initializer_list<PyObject*> of) {       // (takes the references)
+  PyObject* const t = PyTuple_New(Py_ssize_t(of.size()));
+  Py_ssize_t i = 0;
+  for (PyObject* o : of) {
+    if (t)
+      PyTuple_SET_ITEM(t, i++, o);
+    else
+      Py_XDECREF(o);
+  }
+  return t;
+}
+PyObject* none() { Py_RETURN_NONE; }
+
+// norm_rope(handle, shape, q, k, q_weight, k_weight, first_frame, eps, q_out, k_out) -> (q', k'); backward: norm_rope_backward(handle,
+// shape, dq_out, dk_out, q, k, q_weight, k_weight, first_frame, eps, dq, dk) -> (dq, dk, dq_weight, dk_weight).  q or k may be None.
+PyObject* norm(PyObject* const* a, bool backward) {
+  Pool p;
+  int64_t first, rows = -1;
+  float eps;
+  PyObject* const* const of = a + (backward ? 4 : 2);          // q, k, their weights, first_frame, eps, results
+  if (!pool_of(a[0], a[1], &p) || !whole(of[4], &first) || !real(of[5], &eps)) return not_taken();
+  Result r[2];
+  ca_heads x[2], y[2], dz[2];
+  const void* w[2] = {};
+  at::Tensor dw[2];
+  bool there[2];
+  const at::Tensor* like = nullptr;
+  for (int s = 0; s < 2; ++s) {
+    there[s] = of[s] != Py_None;
+    if (!there[s]) {
+      if (of[2 + s] != Py_None || of[6 + s] != Py_None || (backward && a[2 + s] != Py_None)) return not_taken();
+      continue;
+    }
+    const at::Tensor *t = plain(of[s]), *wt = plain(of[2 + s]);
+    if (!fits(p, t) || !weighs(p, wt) || !r[s].take(of[6 + s]) || (rows >= 0 && t->size(0) != rows)) return not_taken();
+    rows = t->size(0);
+    like = t;
+    const at::Tensor& out = r[s].or_empty(t->sizes(), *t);
+    if (!fits(p, &out) || out.size(0) != rows) return not_taken();
+    if (backward) {
+      const at::Tensor* d = plain(a[2 + s]);
+      if (!fits(p, d) || d->size(0) != rows) return not_taken();
+      dz[s] = view(p, *d);
+      dw[s] = at::empty({p.head_dim}, t->options().dtype(at::kFloat));
+    }
+    x[s] = view(p, *t);
+    y[s] = view(p, out);
+    w[s] = wt->data_ptr();
+  }
+  if (!like) return not_taken();
+  void* const stream = p.stream();
+  auto at_side = [&](ca_heads* v, int s) { return there[s] ? v + s : nullptr; };
+  int32_t rc;
+  if (backward) {
+    const size_t bytes = norm_workspace_fn(p.ctx);
+    const at::Tensor work = at::empty({int64_t(bytes)}, like->options().dtype(at::kByte));
+    float* const grads[] = {there[0] ? dw[0].data_ptr<float>() : nullptr, there[1] ? dw[1].data_ptr<float>() : nullptr};
+    void* const wp = work.data_ptr();
+    rc = released([&] {
+      return norm_backward_fn(p.ctx, at_side(dz, 0), at_side(dz, 1), at_side(x, 0), at_side(x, 1), w[0], w[1], eps, at_side(y, 0), at_side(y, 1),
+                              grads[0], grads[1], rows, first, wp, bytes, stream);
+    });
+  } else {
+    rc = released([&] {
+      return norm_fn(p.ctx, at_side(x, 0), at_side(x, 1), w[0], w[1], eps, at_side(y, 0), at_side(y, 1), rows, first, stream);
+    });
+  }
+  if (rc != CA_OK) return PyLong_FromLong(rc);
+  PyObject* const out[] = {there[0] ? r[0].give(CA_OK) : none(), there[1] ? r[1].give(CA_OK) : none()};
+  if (!backward) return tuple({out[0], out[1]});
+  return tuple({out[0], out[1], there[0] ? THPVariable_Wrap(dw[0]) : none(), there[1] ? THPVariable_Wrap(dw[1]) : none()});
+}
+PyObject* norm_rope(PyObject* const* a, Py_ssize_t n) { return n == 10 ? norm(a, false) : not_taken(); }
+PyObject* norm_rope_backward(PyObject* const* a, Py_ssize_t n) { return n == 12 ? norm(a, true) : not_taken(); }
+
+// a [rows, cols] matrix with unit stride along its rows in memory of the device that `like` is on, and its row stride (of a single row
+// it is free: whole steps of 16)
+bool matrix(const at::Tensor* t, at::ScalarType type, int64_t rows, int64_t cols, const at::Tensor& like, int64_t* ld) {
+  if (!t || t->scalar_type() != type || t->dim() != 2 || t->size(0) != rows || t->size(1) != cols || (cols > 1 && t->stride(1) != 1) || !beside(*t, like))
+    return false;
+  *ld = rows > 1 ? t->stride(0) : (cols + 15) / 16 * 16;
+  return true;
+}
+
+// linear_i8(x, w_codes, w_scales, k, out): of values x; codes and scales are a QuantizedRows'
+PyObject* linear_i8(PyObject* const* a, Py_ssize_t n) {
+  int32_t k;
+  Result r;
+  if (n != 5 || !whole32(a[3], &k) || k < 1 || !r.take(a[4])) return not_taken();
+  const at::Tensor *x = plain(a[0]), *w = plain(a[1]), *scales = plain(a[2]);
+  if (!x || !w || !scales || !x->is_cuda() || x->dim() != 2 || (x->scalar_type() != at::kBFloat16 && x->scalar_type() != at::kFloat) || w->dim() != 2)
+    return not_taken();
+  const int64_t m = x->size(0), cols = w->size(0);
+  int64_t ldx, ldw, ldy;
+  if (cols != int32_t(cols) || !matrix(x, x->scalar_type(), m, k, *x, &ldx) || !matrix(w, at::kChar, cols, (int64_t(k) + 255) / 256 * 256, *x, &ldw) ||
+      scales->scalar_type() != at::kFloat || scales->dim() != 1 || scales->size(0) != cols || !scales->is_contiguous() || !beside(*scales, *x))
+    return not_taken();
+  const at::Tensor& y = r.or_empty({m, cols}, x->scalar_type() == at::kFloat ? x->options().dtype(at::kBFloat16) : x->options());
+  if (!matrix(&y, at::kBFloat16, m, cols, *x, &ldy)) return not_taken();
+  const size_t bytes = i8_workspace_fn(m, k);
+  const at::Tensor work = at::empty({int64_t(bytes)}, x->options().dtype(at::kByte));
+  void* const stream = c10::hip::getCurrentHIPStream(x->device().index()).stream();
+  const int32_t dtype = x->scalar_type() == at::kFloat ? CA_F32 : CA_BF16;
+  const void* const xp = x->data_ptr();
+  const int8_t* const wp = w->data_ptr<int8_t>();
+  const float* const sp = scales->data_ptr<float>();
+  void *const yp = y.data_ptr(), *const workp = work.data_ptr();
+  return r.give(released([&] { return i8_fn(xp, dtype, wp, sp, yp, m, int32_t(cols), k, ldx, ldw, ldy, workp, bytes, stream); }));
+}
+
+struct GatedCall {
+  const at::Tensor *x, *wg, *wu;
+  int64_t m, f, k, ldx, ldg, ldu;
+  bool take(PyObject* const* a) {
+    x = plain(a[0]), wg = plain(a[1]), wu = plain(a[2]);
+    if (!x || !wg || !wu || !x->is_cuda() || x->dim() != 2 || wg->dim() != 2) return false;
+    m = x->size(0), k = x->size(1), f = wg->size(0);
+    return k == int32_t(k) && f == int32_t(f) && matrix(x, at::kBFloat16, m, k, *x, &ldx) && matrix(wg, at::kBFloat16, f, k, *x, &ldg) &&
+           matrix(wu, at::kBFloat16, f, k, *x, &ldu);
+  }
+  void* stream() const { return c10::hip::getCurrentHIPStream(x->device().index()).stream(); }
+};
+
+// gated(x, w_gate, w_up, activation, out, train) -> h, or (h, saved)
+PyObject* gated(PyObject* const* a, Py_ssize_t n) {
+  GatedCall c;
+  Result r;
+  int32_t act;
+  if (n != 6 || !c.take(a) || !whole32(a[3], &act) || !r.take(a[4])) return not_taken();
+  const bool train = a[5] == Py_True;
+  const at::Tensor& h = r.or_empty({c.m, c.f}, *c.x);
+  int64_t ldh;
+  if (!matrix(&h, at::kBFloat16, c.m, c.f, *c.x, &ldh)) return not_taken();
+  at::Tensor saved;
+  float *g = nullptr, *u = nullptr;
+  if (train) {
+    saved = at::empty({2, c.m, c.f}, c.x->options().dtype(at::kFloat));
+    g = saved.data_ptr<float>(), u = g + c.m * c.f;
+  }
+  const void *xp = c.x->data_ptr(), *gp = c.wg->data_ptr(), *up = c.wu->data_ptr();
+  void *const hp = h.data_ptr(), *const stream = c.stream();
+  const int32_t rc = released([&] {
+    return gated_fn(xp, gp, up, hp, g, u, act, c.m, int32_t(c.f), int32_t(c.k), c.ldx, c.ldg, c.ldu, ldh, c.f, stream);
+  });
+  if (!train || rc != CA_OK) return r.give(rc);
+  return tuple({r.give(rc), THPVariable_Wrap(saved)});
+}
+
+// gated_backward(x, w_gate, w_up, dh, saved, activation) -> (dx, dw_gate, dw_up)
+PyObject* gated_backward(PyObject* const* a, Py_ssize_t n) {
+  GatedCall c;
+  int32_t act;
+  int64_t lddh;
+  if (n != 6 || !c.take(a) || !whole32(a[5], &act)) return not_taken();
+  const at::Tensor *dh = plain(a[3]), *saved = plain(a[4]);
+  if (!matrix(dh, at::kBFloat16, c.m, c.f, *c.x, &lddh) || !saved || saved->scalar_type() != at::kFloat || saved->dim() != 3 || saved->size(0) != 2 ||
+      saved->size(1) != c.m || saved->size(2) != c.f || !saved->is_contiguous() || !beside(*saved, *c.x))
+    return not_taken();
+  const size_t bytes = gated_workspace_fn(c.m, int32_t(c.f), int32_t(c.k));
+  const at::Tensor dx = at::empty({c.m, c.k}, c.x->options()), dw = at::empty({2, c.f, c.k}, c.x->options()),
+                   work = at::empty({int64_t(bytes)}, c.x->options().dtype(at::kByte));
+  const float *const g = saved->data_ptr<float>(), *const u = g + c.m * c.f;
+  const void *xp = c.x->data_ptr(), *gp = c.wg->data_ptr(), *up = c.wu->data_ptr(), *dhp = dh->data_ptr();
+  void *const dxp = dx.data_ptr(), *const dwp = dw.data_ptr(), *const workp = work.data_ptr(), *const stream = c.stream();
+  const int32_t rc = released([&] {
+    return gated_backward_fn(dhp, xp, gp, up, g, u, act, dxp, dwp, static_cast<char*>(dwp) + c.f * c.k * 2, c.m, int32_t(c.f), int32_t(c.k), lddh, c.ldx,
+                             c.ldg, c.ldu, c.f, c.k, c.k, workp, bytes, stream);
+  });
+  if (rc != CA_OK) return PyLong_FromLong(rc);
+  return tuple({THPVariable_Wrap(dx), THPVariable_Wrap(dw[0]), THPVariable_Wrap(dw[1])});
 }
 
 // rope(handle, shape, x, first_frame, out)
@@ -294,9 +505,34 @@ PyObject* bind(PyObject* const* a, Py_ssize_t n) {
   Py_RETURN_NONE;
 }
 
+// bind_layer(addresses of the nine entry points of the rest of a layer in the order above)
+PyObject* bind_layer(PyObject* const* a, Py_ssize_t n) {
+  int64_t f[9];
+  if (n != 9) {
+    PyErr_SetString(PyExc_TypeError, "nine addresses");
+    return nullptr;
+  }
+  for (int i = 0; i < 9; ++i)
+    if (!whole(a[i], f + i) || f[i] == 0) {
+      PyErr_SetString(PyExc_TypeError, "an address is an int");
+      return nullptr;
+    }
+  norm_fn = reinterpret_cast<decltype(norm_fn)>(f[0]);
+  norm_workspace_fn = reinterpret_cast<decltype(norm_workspace_fn)>(f[1]);
+  norm_backward_fn = reinterpret_cast<decltype(norm_backward_fn)>(f[2]);
+  append_norm_fn = reinterpret_cast<decltype(append_norm_fn)>(f[3]);
+  i8_workspace_fn = reinterpret_cast<decltype(i8_workspace_fn)>(f[4]);
+  i8_fn = reinterpret_cast<decltype(i8_fn)>(f[5]);
+  gated_fn = reinterpret_cast<decltype(gated_fn)>(f[6]);
+  gated_workspace_fn = reinterpret_cast<decltype(gated_workspace_fn)>(f[7]);
+  gated_backward_fn = reinterpret_cast<decltype(gated_backward_fn)>(f[8]);
+  Py_RETURN_NONE;
+}
+
 #define METHOD(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(&guarded<name>)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {METHOD(linear), METHOD(append_batch), METHOD(rope), METHOD(forward), METHOD(forward_rope), METHOD(qkv_publish),
-                         METHOD(bind), {nullptr, nullptr, 0, nullptr}};
+                         METHOD(append_batch_norm), METHOD(norm_rope), METHOD(norm_rope_backward), METHOD(linear_i8), METHOD(gated),
+                         METHOD(gated_backward), METHOD(bind), METHOD(bind_layer), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_calls", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

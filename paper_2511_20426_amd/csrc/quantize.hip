@@ -1,10 +1,6 @@
 // Rows of activations or weights brought to 8 bits with a scale each: scale = largest magnitude / 127, codes = round-half-even(127 x /
 // largest).  Memory bound: x is read once (rows of up to kHeld vectors a lane stay in registers between the two passes over them)
 // and the codes written once, padded with zeros to the products' step of 256.
-//
-// Codes are those of exact arithmetic.  Of bf16 values 127 x is exact in fp32, and a quotient that is not a tie lies at least 2^-16
-// (relative) off one: the quotient by the reciprocal with one correction is off by less than 2^-23, and it is exact where the
-// quotient is representable, as ties are.  For fp32 values next to a tie the quotient is formed again in fp64.
 #include <hip/hip_runtime.h>
 
 #include "ca_internal.hpp"
@@ -13,6 +9,7 @@ namespace ca {
 namespace {
 
 #include "rope_device.hpp"
+#include "quantize_device.hpp"
 
 constexpr int kHeld = 4;                          // vectors of eight values that a lane keeps
 
@@ -41,41 +38,12 @@ __device__ __forceinline__ void load_values(const T* row, int v, int k, float* x
   }
 }
 
-__device__ __forceinline__ uint32_t magnitude(const float* x) {      // as bits: NaN above infinity above all others
-  uint32_t m = 0;
-#pragma unroll
-  for (int j = 0; j < 8; ++j) m = max(m, __float_as_uint(x[j]) & 0x7fffffffu);
-  return m;
-}
-
 struct QuantizeArgs {
   const void* x;
   int8_t* codes;
   float* scales;
   int64_t rows, ldx, ld_codes;
   int32_t k, k_padded;
-};
-
-// A row's quotients: values and largest magnitude are brought near 1 by a power of two first where 127 x or the reciprocal would
-// leave the range of fp32.
-struct RowScale {
-  float by, most, inv;                            // most: the largest magnitude after that
-  bool finite;
-  __device__ __forceinline__ explicit RowScale(uint32_t bits) {
-    const float m = __uint_as_float(bits);
-    finite = bits < 0x7f800000u;
-    by = m > 0x1p100f ? 0x1p-64f : (m < 0x1p-64f ? 0x1p80f : 1.f);
-    most = m * by;
-    inv = finite && bits != 0 ? 1.f / most : 0.f;
-  }
-  template <typename T>
-  __device__ __forceinline__ int code(float x) const {
-    const float t = x * by * 127.f;
-    float q = t * inv;
-    q = fmaf(fmaf(-q, most, t), inv, q);
-    if (sizeof(T) == 4 && fabsf(fabsf(q - truncf(q)) - 0.5f) < 1e-4f) return int(rint(double(x * by) * 127. / double(most)));
-    return int(rintf(q));
-  }
 };
 
 template <typename T, bool kVec, int kThreads>
@@ -122,7 +90,7 @@ __global__ __launch_bounds__(256) void quantize_rows_kernel(QuantizeArgs a) {
     load_values<T, kVec>(x, v, a.k, e);
     leave(v, e);
   }
-  if (t == 0) a.scales[row] = s.finite ? __uint_as_float(most) / 127.f : __uint_as_float(0x7fc00000u);
+  if (t == 0) a.scales[row] = row_scale(most);
 }
 
 template <typename T, bool kVec>

@@ -87,12 +87,13 @@ class CascadePool:
         """All blocks of one cascade iteration in one launch; the tensors share their strides.  With k_weight [D] each head of K
         is normed (as qk_norm_rope does) ahead of its rotation."""
         h = self.ctx._h
-        if h and k_weight is None:
-            r = B.calls.append_batch(h.value, self._shape, block_ids, timesteps, epoch, ks, vs)
+        if h:
+            r = (B.calls.append_batch(h.value, self._shape, block_ids, timesteps, epoch, ks, vs) if k_weight is None else
+                 B.calls.append_batch_norm(h.value, self._shape, block_ids, timesteps, epoch, ks, vs, k_weight, eps))
             if r.__class__ is list:
                 return r
             if r is not None:
-                B._check(r, "kv_cache_append_batch")
+                B._check(r, "kv_cache_append_batch" if k_weight is None else "kv_cache_append_batch_norm")
         stride = ks[0].stride()
         for k, v in zip(ks, vs):
             self._check(k); self._check(v)
@@ -221,6 +222,13 @@ def _qk_norm_rope(self, q: torch.Tensor | None, k: torch.Tensor | None, q_weight
     """Each head of q and k (either may be None) normed, y = weight * x / sqrt(mean(x^2) + eps), and rotated by its token's
     position, in one launch: [n, H, D] with any token / head strides, consecutive tokens from latent frame `first_frame` on; weights
     [D].  Returns (q', k'), in q_out / k_out (their own strides) or new contiguous tensors; an output may be its input."""
+    h = self.ctx._h
+    if h:
+        r = B.calls.norm_rope(h.value, self._shape, q, k, q_weight, k_weight, first_frame, eps, q_out, k_out)
+        if r.__class__ is int:
+            B._check(r, "layer_qk_norm_rope")
+        if r is not None:
+            return r
     given, outs, views = [], [], []
     n = (k if q is None else q).shape[0]
     for x, w, out in ((q, q_weight, q_out), (k, k_weight, k_out)):
@@ -244,6 +252,13 @@ def _qk_norm_rope_backward(self, dq_out: torch.Tensor | None, dk_out: torch.Tens
                            eps: float = 1e-6, dq: torch.Tensor | None = None, dk: torch.Tensor | None = None):
     """Gradients of qk_norm_rope: from those of its outputs (dq_out, dk_out) and its inputs to (dq, dk, dq_weight, dk_weight), the
     weights' in fp32.  What belongs to a q or k of None is None.  dq may be dq_out, dk dk_out."""
+    h = self.ctx._h
+    if h:
+        r = B.calls.norm_rope_backward(h.value, self._shape, dq_out, dk_out, q, k, q_weight, k_weight, first_frame, eps, dq, dk)
+        if r.__class__ is int:
+            B._check(r, "layer_qk_norm_rope_backward")
+        if r is not None:
+            return r
     n = (k if q is None else q).shape[0]
     views, weights, grads, dws = [], [], [], []
     for x, w, dz, dx in ((q, q_weight, dq_out, dq), (k, k_weight, dk_out, dk)):
@@ -338,15 +353,26 @@ def quantize_rows(x: torch.Tensor) -> QuantizedRows:
 def linear_i8(x: torch.Tensor | QuantizedRows, w: QuantizedRows, out: torch.Tensor | None = None) -> torch.Tensor:
     """y = x @ w.T in 8-bit integers with a scale for each row of x (token) and of w (output channel), y [M, N] in bf16; x [M, K] in bf16
     or fp32 is brought to 8 bits on the way."""
-    if not isinstance(x, QuantizedRows):
-        x = quantize_rows(x)
-    (m, k), n, device = x.shape, w.shape[0], x.codes.device
-    assert w.k == k and w.codes.device == device
+    r = B.calls.linear_i8(x, w.codes, w.scales, w.k, out)
+    if r.__class__ is int:
+        B._check(r, "layer_linear_i8_values")
+    if r is not None:
+        return r
+    n, k, device = w.shape[0], w.k, w.codes.device
+    m = x.shape[0]
     y = torch.empty((m, n), dtype=_BF16, device=device) if out is None else out
-    ldy = _matrix(y, x.codes, _BF16, m, n)
-    B.layer_linear_i8(x.codes.data_ptr(), x.scales.data_ptr(), w.codes.data_ptr(), w.scales.data_ptr(), y.data_ptr(), m, n, k,
-                      x.codes.shape[1] if m <= 1 else x.codes.stride(0), w.codes.shape[1] if n <= 1 else w.codes.stride(0), ldy,
-                      _current_stream(device))
+    ldw, ldy = w.codes.shape[1] if n <= 1 else w.codes.stride(0), _matrix(y, w.codes, _BF16, m, n)
+    if isinstance(x, QuantizedRows):
+        assert x.k == k and x.codes.device == device
+        B.layer_linear_i8(x.codes.data_ptr(), x.scales.data_ptr(), w.codes.data_ptr(), w.scales.data_ptr(), y.data_ptr(), m, n, k,
+                          x.codes.shape[1] if m <= 1 else x.codes.stride(0), ldw, ldy, _current_stream(device))
+        return y
+    assert x.is_cuda and x.device == device and x.dtype in (_BF16, torch.float32)
+    ldx = _matrix(x, w.codes, x.dtype, m, k)
+    nbytes = B.layer_linear_i8_workspace(m, k)
+    work = torch.empty(nbytes, dtype=torch.uint8, device=device)
+    B.layer_linear_i8_values(x.data_ptr(), B.CA_BF16 if x.dtype == _BF16 else B.CA_F32, w.codes.data_ptr(), w.scales.data_ptr(), y.data_ptr(), m, n,
+                             k, ldx, ldw, ldy, work.data_ptr(), nbytes, _current_stream(device))
     return y
 
 
@@ -369,24 +395,38 @@ def gated_linear(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, acti
                  out: torch.Tensor | None = None) -> torch.Tensor:
     """h = act(x @ w_gate.T) * (x @ w_up.T), the first half of a gated feed-forward block, in one kernel: x [M, K], w_gate and w_up
     [F, K], h [M, F], bf16, rows may be strided (last dimension contiguous); activation "silu" or "gelu" (its tanh form)."""
-    return _gated(x, w_gate, w_up, activation, out, None)
+    r = B.calls.gated(x, w_gate, w_up, _ACTIVATIONS[activation], out, False)
+    if r.__class__ is int:
+        B._check(r, "layer_gated_bf16")
+    return _gated(x, w_gate, w_up, activation, out, None) if r is None else r
 
 
 def gated_linear_train(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, activation: str = "silu",
                        out: torch.Tensor | None = None):
-    """gated_linear for training: (h, saved), saved being the two projections [M, F] that gated_linear_backward takes."""
-    saved = torch.empty((2, x.shape[0], w_gate.shape[0]), dtype=_BF16, device=x.device)
+    """gated_linear for training: (h, saved), saved being the two projections in fp32 [2, M, F] that gated_linear_backward
+    takes."""
+    r = B.calls.gated(x, w_gate, w_up, _ACTIVATIONS[activation], out, True)
+    if r.__class__ is int:
+        B._check(r, "layer_gated_bf16")
+    if r is not None:
+        return r
+    saved = torch.empty((2, x.shape[0], w_gate.shape[0]), dtype=torch.float32, device=x.device)
     return _gated(x, w_gate, w_up, activation, out, saved), saved
 
 
 def gated_linear_backward(dh: torch.Tensor, x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, saved: torch.Tensor,
                           activation: str = "silu"):
     """(dx, dw_gate, dw_up) from the gradient dh [M, F] of gated_linear_train's h, its inputs and what it saved."""
+    r = B.calls.gated_backward(x, w_gate, w_up, dh, saved, _ACTIVATIONS[activation])
+    if r.__class__ is int:
+        B._check(r, "layer_gated_backward_bf16")
+    if r is not None:
+        return r
     assert x.is_cuda and w_gate.is_cuda and w_up.is_cuda
     (m, k), f, device = x.shape, w_gate.shape[0], x.device
     ldx, ldg, ldu = _matrix(x, x, _BF16, m, k), _matrix(w_gate, x, _BF16, f, k), _matrix(w_up, x, _BF16, f, k)
     lddh = _matrix(dh, x, _BF16, m, f)
-    assert saved.shape == (2, m, f) and saved.dtype == _BF16 and saved.is_contiguous() and _reachable(saved, x)
+    assert saved.shape == (2, m, f) and saved.dtype == torch.float32 and saved.is_contiguous() and _reachable(saved, x)
     dx, dw = torch.empty((m, k), dtype=_BF16, device=device), torch.empty((2, f, k), dtype=_BF16, device=device)
     nbytes = B.layer_gated_backward_workspace(m, f, k)
     work = torch.empty(nbytes, dtype=torch.uint8, device=device)

@@ -261,7 +261,7 @@ def test_rows_that_are_not_finite():
     """... have scale NaN and codes 0, their neighbours keep theirs; their outputs are NaN, the others' finite."""
     from paper_2511_20426_amd.runner import linear_i8, quantize_rows
     gen = _gen(5)
-    for rows in (6, 1030):
+    for rows in (4, 6, 1030):
         x, w = _normal(gen, rows, 300), _normal(gen, 16, 300)
         x[1, 7], x[3, 299], x[rows - 1, 0] = float("inf"), float("nan"), -float("inf")
         bad = torch.zeros(rows, dtype=torch.bool, device=DEV)
@@ -279,7 +279,7 @@ def _i8_bound(ref):
     return ref.abs() * (2.0 ** -8 + 4 * 2.0 ** -24) + 1e-38
 
 
-I8 = [(1, 8, 1), (1, 776, 1000), (3, 24, 255), (16, 64, 256), (17, 40, 257), (32, 136, 5120), (33, 8, 300), (64, 128, 512), (65, 200, 90), (129, 72, 640),
+I8 = [(1, 8, 1), (1, 8, 8), (1, 776, 1000), (2, 40, 6144), (4, 72, 6144), (3, 88, 6152), (5, 136, 640), (4, 24, 1001), (3, 24, 255), (16, 64, 256), (17, 40, 257), (32, 136, 5120), (33, 8, 300), (64, 128, 512), (65, 200, 90), (129, 72, 640),
       (300, 1032, 2000), (1100, 1400, 256), (2050, 1160, 128), (2050, 2184, 1000), (4680, 1544, 384), (700, 9000, 513)]
 
 
@@ -354,7 +354,7 @@ def test_gated_linear(M, F, K, act):
     assert (h2 == y[:M, :F]).all()
     for p, t in ((g, saved[0]), (u, saved[1])):
         w = wg[:, :K] if p is g else wu
-        assert ((t.double().cpu() - p).abs() <= p.abs() * 2.0 ** -8 + 2e-6 * (x[:M, :K].double().cpu().abs() @ w.double().cpu().abs().T)).all()
+        assert ((t.double().cpu() - p).abs() <= 2e-6 * (x[:M, :K].double().cpu().abs() @ w.double().cpu().abs().T)).all()
 
 
 @pytest.mark.gpu
@@ -374,15 +374,14 @@ def test_gates_that_are_large(M, act):
 
 
 def _gated_grads(x, wg, wu, dh, act):
-    """Gradients, and how far bf16 roundings of g, u, dg and du take them (first order, a quarter more for the rest)"""
+    """Gradients, and how far bf16 roundings of dg and du take them"""
     g = (x @ wg.T).requires_grad_()
     u, e = x @ wu.T, 2.0 ** -8
     a = _act(g, act)
-    slope = torch.autograd.grad(a.sum(), g, create_graph=True)[0]
-    bend = torch.autograd.grad(slope.sum(), g)[0]
-    g, a, slope = g.detach(), a.detach(), slope.detach()
+    slope = torch.autograd.grad(a.sum(), g)[0]
+    a = a.detach()
     dg, du = dh * u * slope, dh * a
-    ddg, ddu = 1.25 * e * (2 * dg.abs() + (dh * u * bend * g).abs()), 1.25 * e * (du.abs() + (dh * slope * g).abs())
+    ddg, ddu = e * dg.abs(), e * du.abs()
     out = []
     for ref, off, size in ((dg @ wg + du @ wu, ddg @ wg.abs() + ddu @ wu.abs(), dg.abs() @ wg.abs() + du.abs() @ wu.abs()),
                            (dg.T @ x, ddg.T @ x.abs(), dg.abs().T @ x.abs()), (du.T @ x, ddu.T @ x.abs(), du.abs().T @ x.abs())):
@@ -488,6 +487,45 @@ def test_replayed_from_a_graph():
         assert all((a == b).all() for a, b in zip(held, eager)), i
 
 
+@pytest.mark.gpu
+def test_both_ways_do_the_same(monkeypatch):
+    """The calls that the extension takes and those that go through the Python code give the same bits, given results or none."""
+    from paper_2511_20426_amd import runner as R
+    pool, gen = _pool(2, 128, (4, 5)), _gen(12)
+    n, K, F = 60, 256, 136
+    qkv, dz, w = _normal(gen, n, 3, 2, 128), _normal(gen, n, 2, 2, 128), _normal(gen, 128)
+    x, wg, wu, dh = _normal(gen, n, K), _normal(gen, F, K), _normal(gen, F, K), _normal(gen, n, F)
+    wq = R.quantize_rows(_normal(gen, 64, K))
+
+    def results():
+        new = lambda t: torch.empty(t.shape, dtype=t.dtype, device=DEV)  # noqa: E731
+        q, k = new(qkv[:, 0]), new(qkv[:, 1])
+        assert pool.qk_norm_rope(qkv[:, 0], qkv[:, 1], w, w, 3, q_out=q, k_out=k)[1] is k
+        out = [q, k, *pool.qk_norm_rope(qkv[:, 0], None, w, None, 3)[:1], *pool.qk_norm_rope(None, qkv[:1, 1], None, w, 3)[1:]]
+        out += pool.qk_norm_rope_backward(dz[:, :, 0], dz[:, :, 1], qkv[:, 0], qkv[:, 1], w, w, 3)
+        dk = dz[:, :, 1].clone()
+        some = pool.qk_norm_rope_backward(None, dk, None, qkv[:, 1], None, w, 3, dk=dk)
+        assert some[0] is None and some[1] is dk and some[2] is None
+        out += [dk, some[3]]
+        assert pool.append_batch([1], [0], 0, [qkv[:, 1]], [qkv[:, 2]], k_weight=w) == [1]
+        at = pool.ctx.kv_cache_page_index(1, 0, 0) * 65536
+        out.append(pool.pool[at:at + 2 * 65536].clone())
+        y, h = torch.empty((n, 64), dtype=torch.bfloat16, device=DEV), torch.empty((n, F + 8), dtype=torch.bfloat16, device=DEV)[:, :F]
+        assert R.linear_i8(x, wq, out=y) is y
+        out += [y, R.linear_i8(x[:1], wq), R.linear_i8(x.float(), wq), R.linear_i8(R.quantize_rows(x), wq)]
+        assert R.gated_linear(x, wg, wu, out=h) is h
+        h2, saved = R.gated_linear_train(x, wg, wu, "gelu")
+        return out + [h, R.gated_linear(x[:1], wg, wu), h2, saved, *R.gated_linear_backward(dh, x, wg, wu, saved, "gelu")]
+
+    first = results()
+    monkeypatch.setattr(B, "calls", B._NoCalls())
+    second = results()
+    assert len(first) == len(second)
+    for i, (a, b) in enumerate(zip(first, second)):
+        assert a.shape == b.shape and a.dtype == b.dtype and (a == b).all(), i
+    assert (first[11] == first[14]).all()         # codes made on the way or before
+
+
 def _refused(code, call, *args):
     with pytest.raises(B.CascadeAttnError) as e:
         call(*args)
@@ -543,6 +581,14 @@ def test_refusals():
         args = list(ok)
         args[i] = bad
         _refused(code, B.layer_linear_i8, *args)
+    need = B.layer_linear_i8_workspace(5, 300)
+    assert need >= 5 * (512 + 4) and B.layer_linear_i8_workspace(5, 0) == 0 == B.layer_linear_i8_workspace(-1, 8)
+    ok = [4096, B.CA_BF16, 4096, 4096, 4096, 5, 16, 300, 300, 512, 16, 4096, need]
+    for i, bad, code in [(0, 0, E), (0, 4097, E), (1, 7, E), (2, 4104, E), (3, 4100, E), (4, 0, E), (5, -1, E), (6, 4, U), (7, 0, U), (8, 299, E), (8, 1 << 22, U), (9, 256, E),
+                         (10, 12, E), (11, 0, E), (11, 4104, E), (12, need - 1, E)]:
+        args = list(ok)
+        args[i] = bad
+        _refused(code, B.layer_linear_i8_values, *args)
     ok = [4096] * 6 + [B.CA_SILU, 5, 16, 128, 128, 128, 128, 16, 16]
     for i, bad, code in [(0, 0, E), (1, 4104, E), (2, 0, E), (3, 0, E), (4, 0, E), (5, 8, E), (6, 2, E), (7, -1, E), (7, 1 << 31, U), (8, 12, U), (9, 64, U), (9, 192, U),
                          (10, 120, E), (11, 132, E), (12, 1 << 22, U), (13, 8, E), (14, 8, E), (14, 20, E)]:
@@ -563,6 +609,7 @@ def test_refusals():
 @pytest.mark.parametrize("host", [b"bytes of the host", (C.c_char * 64)(), 16.0, np.int64(16)], ids=["bytes", "array", "float", "numpy"])
 def test_addresses_are_integers(host):
     calls = [(B.layer_quantize_rows_i8, [16, 1, 16, 16, 0, 8, 8, 256], (0, 2, 3)), (B.layer_linear_i8, [16] * 5 + [0, 8, 8, 256, 256, 8], range(5)),
+             (B.layer_linear_i8_values, [16, 1, 16, 16, 16, 0, 8, 8, 8, 256, 8, 16, 1 << 20], (0, 2, 3, 4, 11)),
              (B.layer_gated_bf16, [16] * 6 + [0, 0, 8, 128, 128, 128, 128, 8, 8], range(6)),
              (B.layer_gated_backward_bf16, [16] * 6 + [0] + [16] * 3 + [0, 8, 128, 8, 128, 128, 128, 8, 128, 128, 16, 0], (0, 1, 2, 3, 4, 5, 7, 8, 9, 20))]
     for call, args, pointers in calls:
@@ -587,7 +634,7 @@ def test_refusals_of_the_torch_calls():
     for bad in (lambda: R.quantize_rows(x.half()), lambda: R.quantize_rows(x.cpu()), lambda: R.linear_i8(x[:, :64], wq),
                 lambda: R.linear_i8(x, wq, out=torch.zeros((4, 16), device=DEV)), lambda: R.linear_i8(x, wq, out=torch.zeros((4, 8), **t)),
                 lambda: R.gated_linear(x, m, m[:8]), lambda: R.gated_linear(x.T, m, m), lambda: R.gated_linear(x, m, m.float()),
-                lambda: R.gated_linear(x, m, m, out=torch.zeros((4, 16))), lambda: R.gated_linear_backward(x, x, m, m, torch.zeros((2, 4, 16), **t))):
+                lambda: R.gated_linear(x, m, m, out=torch.zeros((4, 16))), lambda: R.gated_linear_backward(x, x, m, m, torch.zeros((2, 4, 16), device=DEV))):
         with pytest.raises(AssertionError):
             bad()
     with pytest.raises(KeyError):
