@@ -364,4 +364,4 @@ def test_kernels_do_not_spill(tmp_path, file):
     text = out.read_text()
     names = re.findall(r"\.name:\s*(\S*_kernel\S*)", text)
     spilled = [int(n) for n in re.findall(r"\.[sv]gpr_spill_count:\s*(\d+)", text)]
-    assert len(names) == 8 and len(spilled) == 2 * len(names) and not any(spilled), list(zip(names, spilled[::2], spilled[1::2]))
+    assert len(names) >= 8 and len(spilled) == 2 * len(names) and not any(spilled), list(zip(names, spilled[::2], spilled[1::2]))
