@@ -319,23 +319,24 @@ int32_t layer_linear_i8_values(const void* x_dev, int32_t dtype, const int8_t* w
 
 /* The first half of a gated feed-forward block, both projections, activation and product in one kernel:
  * h = act(g) * u, g = x . w_gate', u = x . w_up', in bf16 with fp32 accumulation; g and u are rounded nowhere on the way to h, h once.
- * CA_SILU: g / (1 + exp(-g)); CA_GELU: g (1 + tanh(sqrt(2/pi) (g + 0.044715 g^3))) / 2.  With g_dev and u_dev (both or neither)
- * the projections are written as well, in fp32, for the backward pass.  w_gate, w_up: [n_hidden, k_in]; shapes as layer_linear_bf16
- * (n_hidden a multiple of 8, k_in of 128). */
+ * CA_SILU: g / (1 + exp(-g)); CA_GELU: g (1 + tanh(sqrt(2/pi) (g + 0.044715 g^3))) / 2.  With saved_dev (layer_gated_saved_bytes(), or
+ * null) the projections are kept as well, in fp32, for the backward pass, in an order that is the library's own.  w_gate, w_up:
+ * [n_hidden, k_in]; shapes as layer_linear_bf16 (n_hidden a multiple of 8, k_in of 128). */
 enum { CA_SILU = 0, CA_GELU = 1 };
-int32_t layer_gated_bf16(const void* x_dev, const void* w_gate_dev, const void* w_up_dev, void* h_dev, float* g_dev, float* u_dev,
+int32_t layer_gated_bf16(const void* x_dev, const void* w_gate_dev, const void* w_up_dev, void* h_dev, float* saved_dev,
                          int32_t activation, int64_t m_rows, int32_t n_hidden, int32_t k_in, int64_t ldx, int64_t ldw_gate, int64_t ldw_up,
-                         int64_t ldh, int64_t ld_saved, void* hip_stream);
+                         int64_t ldh, void* hip_stream);
+size_t layer_gated_saved_bytes(int64_t m_rows, int32_t n_hidden);
 
 /* Its gradients: dg = dh u act'(g), du = dh act(g) (rounded to bf16); dx = dg . w_gate + du . w_up, dw_gate = dg' . x, dw_up = du' . x, each
- * rounded to bf16 once, written, not added to.  dx_dev, dw_gate_dev, dw_up_dev: those that are null are left out (not all).  g and u
- * as layer_gated_bf16 wrote them.  workspace_dev: layer_gated_backward_workspace() bytes, 0 where the shape is not supported.
+ * rounded to bf16 once, written, not added to.  dx_dev, dw_gate_dev, dw_up_dev: those that are null are left out (not all).
+ * saved_dev as layer_gated_bf16 wrote it.  workspace_dev: layer_gated_backward_workspace() bytes, 0 where the shape is not supported.
  * m_rows == 0: zero weight gradients. */
 size_t layer_gated_backward_workspace(int64_t m_rows, int32_t n_hidden, int32_t k_in);
-int32_t layer_gated_backward_bf16(const void* dh_dev, const void* x_dev, const void* w_gate_dev, const void* w_up_dev, const float* g_dev,
-                                  const float* u_dev, int32_t activation, void* dx_dev, void* dw_gate_dev, void* dw_up_dev, int64_t m_rows,
+int32_t layer_gated_backward_bf16(const void* dh_dev, const void* x_dev, const void* w_gate_dev, const void* w_up_dev, const float* saved_dev,
+                                  int32_t activation, void* dx_dev, void* dw_gate_dev, void* dw_up_dev, int64_t m_rows,
                                   int32_t n_hidden, int32_t k_in, int64_t lddh, int64_t ldx, int64_t ldw_gate, int64_t ldw_up,
-                                  int64_t ld_saved, int64_t lddx, int64_t lddw, void* workspace_dev, size_t workspace_bytes,
+                                  int64_t lddx, int64_t lddw, void* workspace_dev, size_t workspace_bytes,
                                   void* hip_stream);
 
 /* ---- Cascade scheduler: the control flow of Algorithm 1, host integers only.

@@ -37,7 +37,7 @@ EXPORTS = (
     "ca_strerror", "ca_last_device_error",
     "ca_mfma_microbench", "layer_linear_bf16", "layer_qkv_publish",
     "layer_qk_norm_rope", "layer_qk_norm_rope_workspace", "layer_qk_norm_rope_backward", "kv_cache_append_batch_norm", "layer_quantize_rows_i8",
-    "layer_linear_i8", "layer_linear_i8_workspace", "layer_linear_i8_values", "layer_gated_bf16", "layer_gated_backward_workspace", "layer_gated_backward_bf16",
+    "layer_linear_i8", "layer_linear_i8_workspace", "layer_linear_i8_values", "layer_gated_bf16", "layer_gated_saved_bytes", "layer_gated_backward_workspace", "layer_gated_backward_bf16",
     "ca_sched_create", "ca_sched_create_lagged", "ca_sched_destroy", "ca_sched_batch", "ca_sched_advance", "ca_sched_state",
 )
 
@@ -162,11 +162,13 @@ def _load() -> C.CDLL:
     lib.layer_linear_i8_values.restype = i32
     lib.layer_linear_i8_values.argtypes = [vp, i32, vp, vp, vp, i64, i32, i32, i64, i64, i64, vp, C.c_size_t, vp]
     lib.layer_gated_bf16.restype = i32
-    lib.layer_gated_bf16.argtypes = [vp] * 6 + [i32, i64, i32, i32] + [i64] * 5 + [vp]
+    lib.layer_gated_bf16.argtypes = [vp] * 5 + [i32, i64, i32, i32] + [i64] * 4 + [vp]
+    lib.layer_gated_saved_bytes.restype = C.c_size_t
+    lib.layer_gated_saved_bytes.argtypes = [i64, i32]
     lib.layer_gated_backward_workspace.restype = C.c_size_t
     lib.layer_gated_backward_workspace.argtypes = [i64, i32, i32]
     lib.layer_gated_backward_bf16.restype = i32
-    lib.layer_gated_backward_bf16.argtypes = [vp] * 6 + [i32] + [vp] * 3 + [i64, i32, i32] + [i64] * 7 + [vp, C.c_size_t, vp]
+    lib.layer_gated_backward_bf16.argtypes = [vp] * 5 + [i32] + [vp] * 3 + [i64, i32, i32] + [i64] * 6 + [vp, C.c_size_t, vp]
     lib.ca_sched_create.restype = i32
     lib.ca_sched_create.argtypes = [i64, i32, C.POINTER(i32), i32, C.POINTER(vp)]
     lib.ca_sched_create_lagged.restype = i32
@@ -218,7 +220,7 @@ def _load_calls():
             lib.cascade_attn_forward_rope, lib.layer_qkv_publish, lib.layer_linear_bf16)))
         ext.bind_layer(*(C.cast(f, C.c_void_p).value for f in (
             lib.layer_qk_norm_rope, lib.layer_qk_norm_rope_workspace, lib.layer_qk_norm_rope_backward, lib.kv_cache_append_batch_norm,
-            lib.layer_linear_i8_workspace, lib.layer_linear_i8_values, lib.layer_gated_bf16, lib.layer_gated_backward_workspace,
+            lib.layer_linear_i8_workspace, lib.layer_linear_i8_values, lib.layer_gated_bf16, lib.layer_gated_saved_bytes, lib.layer_gated_backward_workspace,
             lib.layer_gated_backward_bf16)))
         return ext
     except Exception as e:
@@ -456,24 +458,28 @@ def layer_linear_i8_values(x_ptr: int, dtype: int, w_codes_ptr: int, w_scales_pt
            "layer_linear_i8_values")
 
 
-def layer_gated_bf16(x_ptr: int, w_gate_ptr: int, w_up_ptr: int, h_ptr: int, g_ptr: int, u_ptr: int, activation: int, m_rows: int,
-                     n_hidden: int, k_in: int, ldx: int, ldw_gate: int, ldw_up: int, ldh: int, ld_saved: int, stream: int = 0) -> None:
-    _check(lib.layer_gated_bf16(index(x_ptr or 0), index(w_gate_ptr or 0), index(w_up_ptr or 0), index(h_ptr or 0), index(g_ptr or 0),
-                                index(u_ptr or 0), activation, m_rows, n_hidden, k_in, ldx, ldw_gate, ldw_up, ldh, ld_saved,
+def layer_gated_bf16(x_ptr: int, w_gate_ptr: int, w_up_ptr: int, h_ptr: int, saved_ptr: int, activation: int, m_rows: int,
+                     n_hidden: int, k_in: int, ldx: int, ldw_gate: int, ldw_up: int, ldh: int, stream: int = 0) -> None:
+    _check(lib.layer_gated_bf16(index(x_ptr or 0), index(w_gate_ptr or 0), index(w_up_ptr or 0), index(h_ptr or 0),
+                                index(saved_ptr or 0), activation, m_rows, n_hidden, k_in, ldx, ldw_gate, ldw_up, ldh,
                                 index(stream or 0)), "layer_gated_bf16")
+
+
+def layer_gated_saved_bytes(m_rows: int, n_hidden: int) -> int:
+    return int(lib.layer_gated_saved_bytes(m_rows, n_hidden))
 
 
 def layer_gated_backward_workspace(m_rows: int, n_hidden: int, k_in: int) -> int:
     return int(lib.layer_gated_backward_workspace(m_rows, n_hidden, k_in))
 
 
-def layer_gated_backward_bf16(dh_ptr: int, x_ptr: int, w_gate_ptr: int, w_up_ptr: int, g_ptr: int, u_ptr: int, activation: int,
+def layer_gated_backward_bf16(dh_ptr: int, x_ptr: int, w_gate_ptr: int, w_up_ptr: int, saved_ptr: int, activation: int,
                               dx_ptr: int, dw_gate_ptr: int, dw_up_ptr: int, m_rows: int, n_hidden: int, k_in: int, lddh: int, ldx: int,
-                              ldw_gate: int, ldw_up: int, ld_saved: int, lddx: int, lddw: int, workspace_ptr: int, workspace_bytes: int,
+                              ldw_gate: int, ldw_up: int, lddx: int, lddw: int, workspace_ptr: int, workspace_bytes: int,
                               stream: int = 0) -> None:
     _check(lib.layer_gated_backward_bf16(index(dh_ptr or 0), index(x_ptr or 0), index(w_gate_ptr or 0), index(w_up_ptr or 0),
-                                         index(g_ptr or 0), index(u_ptr or 0), activation, index(dx_ptr or 0), index(dw_gate_ptr or 0),
-                                         index(dw_up_ptr or 0), m_rows, n_hidden, k_in, lddh, ldx, ldw_gate, ldw_up, ld_saved, lddx, lddw,
+                                         index(saved_ptr or 0), activation, index(dx_ptr or 0), index(dw_gate_ptr or 0),
+                                         index(dw_up_ptr or 0), m_rows, n_hidden, k_in, lddh, ldx, ldw_gate, ldw_up, lddx, lddw,
                                          index(workspace_ptr or 0), workspace_bytes, index(stream or 0)), "layer_gated_backward_bf16")
 
 

@@ -165,9 +165,10 @@ int32_t launch_gemm_i8(const void* x, const float* x_scales, const void* w, cons
 // The same of values of X (CA_BF16 or CA_F32), with room in the workspace for their codes [M][K up to 256s] and scales.
 int32_t launch_gemm_i8_values(int dtype, const void* x, int64_t ldx, const void* w, const float* w_scales, void* y, int64_t M, int32_t N, int32_t K,
                               int64_t ldw, int64_t ldy, void* workspace, void* stream);
-// H = act(X Wg') * (X Wu'), with g and u (both or neither) the projections themselves in fp32 as well
-int32_t launch_gemm_gated(const void* x, const void* w_gate, const void* w_up, void* h, float* g, float* u, int activation, int64_t M, int32_t F,
-                          int32_t K, int64_t ldx, int64_t ldwg, int64_t ldwu, int64_t ldh, int64_t ld_saved, void* stream);
+// H = act(X Wg') * (X Wu'); with saved the projections themselves in fp32 as well, the gate's and the up projection's in one half each
+inline int64_t gated_saved_values(int64_t M, int32_t F) { return 2 * ((M + 15) / 16 * 16) * ((int64_t(F) + 31) / 32 * 32); }
+int32_t launch_gemm_gated(const void* x, const void* w_gate, const void* w_up, void* h, float* saved, int activation, int64_t M, int32_t F,
+                          int32_t K, int64_t ldx, int64_t ldwg, int64_t ldwu, int64_t ldh, void* stream);
 // act(g) = g sigmoid(g (act0 + act1 g^2))
 inline void activation_factors(int activation, float* act0, float* act1) {
   *act0 = activation == CA_GELU ? 1.5957691216057308f : 1.f;                       // 2 sqrt(2 / pi)
@@ -179,9 +180,9 @@ struct GatedWorkspace {
   size_t rows, cols, xt, wt, bytes;
 };
 GatedWorkspace gated_workspace(int64_t M, int32_t F, int32_t K);
-int32_t launch_gated_backward(const void* dh, const void* x, const void* w_gate, const void* w_up, const float* g, const float* u, int activation,
+int32_t launch_gated_backward(const void* dh, const void* x, const void* w_gate, const void* w_up, const float* saved, int activation,
                               void* dx, void* dw_gate, void* dw_up, int64_t M, int32_t F, int32_t K, int64_t lddh, int64_t ldx, int64_t ldwg,
-                              int64_t ldwu, int64_t ld_saved, int64_t lddx, int64_t lddw, void* workspace, void* stream);
+                              int64_t ldwu, int64_t lddx, int64_t lddw, void* workspace, void* stream);
 // Per-device facts and one-time kernel attributes, cached for up to kMaxDevices devices (thread
 // safe: the cached values are idempotent and written with relaxed atomics).
 constexpr int kMaxDevices = 64;

@@ -159,49 +159,49 @@ int32_t layer_linear_i8_values(const void* x_dev, int32_t dtype, const int8_t* w
   return ca::launch_gemm_i8_values(dtype, x_dev, ldx, w_codes_dev, w_scales_dev, y_dev, m_rows, n_out, k_in, ldw, ldy, workspace_dev, hip_stream);
 }
 
-int32_t layer_gated_bf16(const void* x_dev, const void* w_gate_dev, const void* w_up_dev, void* h_dev, float* g_dev, float* u_dev,
+int32_t layer_gated_bf16(const void* x_dev, const void* w_gate_dev, const void* w_up_dev, void* h_dev, float* saved_dev,
                          int32_t activation, int64_t m_rows, int32_t n_hidden, int32_t k_in, int64_t ldx, int64_t ldw_gate, int64_t ldw_up,
-                         int64_t ldh, int64_t ld_saved, void* hip_stream) {
+                         int64_t ldh, void* hip_stream) {
   if (int32_t rc = check_gated(activation, m_rows, n_hidden, k_in)) return rc;
-  if ((g_dev != nullptr) != (u_dev != nullptr)) return CA_EINVAL;
   for (int64_t ld : {ldx, ldw_gate, ldw_up})
     if (int32_t rc = check_ld(ld, k_in)) return rc;
   if (ldh < n_hidden || ldh % 8 != 0) return CA_EINVAL;
-  if (g_dev)
-    if (int32_t rc = check_ld(ld_saved, n_hidden)) return rc;
   if (m_rows == 0) return CA_OK;
   for (const void* p : {x_dev, w_gate_dev, w_up_dev, static_cast<const void*>(h_dev)})
     if (!p || !aligned16(p)) return CA_EINVAL;
-  if (!aligned16(g_dev) || !aligned16(u_dev)) return CA_EINVAL;
-  return ca::launch_gemm_gated(x_dev, w_gate_dev, w_up_dev, h_dev, g_dev, u_dev, activation, m_rows, n_hidden, k_in, ldx, ldw_gate, ldw_up,
-                               ldh, ld_saved, hip_stream);
+  if (!aligned16(saved_dev)) return CA_EINVAL;
+  return ca::launch_gemm_gated(x_dev, w_gate_dev, w_up_dev, h_dev, saved_dev, activation, m_rows, n_hidden, k_in, ldx, ldw_gate, ldw_up,
+                               ldh, hip_stream);
+}
+
+size_t layer_gated_saved_bytes(int64_t m_rows, int32_t n_hidden) {
+  return check_gated(CA_SILU, m_rows, n_hidden, 128) ? 0 : size_t(ca::gated_saved_values(m_rows, n_hidden)) * sizeof(float);
 }
 
 size_t layer_gated_backward_workspace(int64_t m_rows, int32_t n_hidden, int32_t k_in) {
   return check_gated(CA_SILU, m_rows, n_hidden, k_in) ? 0 : ca::gated_workspace(m_rows, n_hidden, k_in).bytes;
 }
 
-int32_t layer_gated_backward_bf16(const void* dh_dev, const void* x_dev, const void* w_gate_dev, const void* w_up_dev, const float* g_dev,
-                                  const float* u_dev, int32_t activation, void* dx_dev, void* dw_gate_dev, void* dw_up_dev, int64_t m_rows,
+int32_t layer_gated_backward_bf16(const void* dh_dev, const void* x_dev, const void* w_gate_dev, const void* w_up_dev, const float* saved_dev,
+                                  int32_t activation, void* dx_dev, void* dw_gate_dev, void* dw_up_dev, int64_t m_rows,
                                   int32_t n_hidden, int32_t k_in, int64_t lddh, int64_t ldx, int64_t ldw_gate, int64_t ldw_up,
-                                  int64_t ld_saved, int64_t lddx, int64_t lddw, void* workspace_dev, size_t workspace_bytes, void* hip_stream) {
+                                  int64_t lddx, int64_t lddw, void* workspace_dev, size_t workspace_bytes, void* hip_stream) {
   if (int32_t rc = check_gated(activation, m_rows, n_hidden, k_in)) return rc;
   for (int64_t ld : {ldx, ldw_gate, ldw_up, lddx, lddw})
     if (int32_t rc = check_ld(ld, k_in)) return rc;
-  for (int64_t ld : {lddh, ld_saved})
-    if (int32_t rc = check_ld(ld, n_hidden)) return rc;
+  if (int32_t rc = check_ld(lddh, n_hidden)) return rc;
   const ca::GatedWorkspace at = ca::gated_workspace(m_rows, n_hidden, k_in);
   if (at.Mp >= kMaxLd - 128 || 2 * at.Fp >= kMaxLd) return CA_EUNSUPPORTED;      // (they are row strides of products)
   if (!workspace_dev || !aligned16(workspace_dev) || workspace_bytes < at.bytes) return CA_EINVAL;
   if (m_rows > 0)
-    for (const void* p : {dh_dev, x_dev, static_cast<const void*>(g_dev), static_cast<const void*>(u_dev)})
+    for (const void* p : {dh_dev, x_dev, static_cast<const void*>(saved_dev)})
       if (!p) return CA_EINVAL;
   if (!w_gate_dev || !w_up_dev || (!dx_dev && !dw_gate_dev && !dw_up_dev)) return CA_EINVAL;
-  for (const void* p : {dh_dev, x_dev, w_gate_dev, w_up_dev, static_cast<const void*>(g_dev), static_cast<const void*>(u_dev), static_cast<const void*>(dx_dev), static_cast<const void*>(dw_gate_dev),
+  for (const void* p : {dh_dev, x_dev, w_gate_dev, w_up_dev, static_cast<const void*>(saved_dev), static_cast<const void*>(dx_dev), static_cast<const void*>(dw_gate_dev),
                         static_cast<const void*>(dw_up_dev)})
     if (!aligned16(p)) return CA_EINVAL;
-  return ca::launch_gated_backward(dh_dev, x_dev, w_gate_dev, w_up_dev, g_dev, u_dev, activation, m_rows > 0 ? dx_dev : nullptr, dw_gate_dev,
-                                   dw_up_dev, m_rows, n_hidden, k_in, lddh, ldx, ldw_gate, ldw_up, ld_saved, lddx, lddw, workspace_dev, hip_stream);
+  return ca::launch_gated_backward(dh_dev, x_dev, w_gate_dev, w_up_dev, saved_dev, activation, m_rows > 0 ? dx_dev : nullptr, dw_gate_dev,
+                                   dw_up_dev, m_rows, n_hidden, k_in, lddh, ldx, ldw_gate, ldw_up, lddx, lddw, workspace_dev, hip_stream);
 }
 
 }  // extern "C"

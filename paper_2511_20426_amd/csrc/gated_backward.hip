@@ -73,7 +73,7 @@ struct GatedGradArgs {
   const uint16_t* dh;
   const float *g, *u;
   uint16_t *rows, *cols;                          // [M][2 Fp] and [2 F][Mp]
-  int64_t lddh, ld_saved;
+  int64_t lddh;
   int32_t M, F, Mp, Fp;
   float act0, act1;
 };
@@ -88,20 +88,23 @@ __global__ __launch_bounds__(256) void gated_grad_kernel(GatedGradArgs a) {
     U4 dg = {0, 0, 0, 0}, du = {0, 0, 0, 0};
     if (m < a.M && f < a.F) {
       Vec8<uint16_t> dh;
-      Vec8<float> g, u;
       dh.load(a.dh + int64_t(m) * a.lddh + f);
-      g.load(a.g + int64_t(m) * a.ld_saved + f);
-      u.load(a.u + int64_t(m) * a.ld_saved + f);
-      float v[8], w[8];
+      float g[8], u[8], v[8], w[8];
+#pragma unroll
+      for (int half = 0; half < 2; ++half) {
+        const int64_t at = saved_at(m, f + 4 * half, a.F);
+        *reinterpret_cast<f32x4*>(g + 4 * half) = __builtin_nontemporal_load(reinterpret_cast<const f32x4*>(a.g + at));
+        *reinterpret_cast<f32x4*>(u + 4 * half) = __builtin_nontemporal_load(reinterpret_cast<const f32x4*>(a.u + at));
+      }
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
         // act' = s + g s (1 - s) p'(g), p = g (act0 + act1 g^2)
         float p;
-        const float s = act_sigmoid(g.v[j], a.act0, a.act1, &p);
-        const float c = __builtin_amdgcn_fmed3f(g.v[j], -1e4f, 1e4f);
+        const float s = act_sigmoid(g[j], a.act0, a.act1, &p);
+        const float c = __builtin_amdgcn_fmed3f(g[j], -1e4f, 1e4f);
         const float slope = fmaf(c * c, 3.f * a.act1, a.act0);
-        v[j] = dh.v[j] * u.v[j] * fmaf(c * s * (1.f - s), slope, s);
-        w[j] = dh.v[j] * (g.v[j] * s);
+        v[j] = dh.v[j] * u[j] * fmaf(c * s * (1.f - s), slope, s);
+        w[j] = dh.v[j] * (g[j] * s);
       }
       dg = U4{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7])};
       du = U4{pack_bf16(w[0], w[1]), pack_bf16(w[2], w[3]), pack_bf16(w[4], w[5]), pack_bf16(w[6], w[7])};
@@ -147,15 +150,14 @@ GatedWorkspace gated_workspace(int64_t M, int32_t F, int32_t K) {
   return w;
 }
 
-int32_t launch_gated_backward(const void* dh, const void* x, const void* w_gate, const void* w_up, const float* g, const float* u, int activation,
+int32_t launch_gated_backward(const void* dh, const void* x, const void* w_gate, const void* w_up, const float* saved, int activation,
                               void* dx, void* dw_gate, void* dw_up, int64_t M, int32_t F, int32_t K, int64_t lddh, int64_t ldx, int64_t ldwg,
-                              int64_t ldwu, int64_t ld_saved, int64_t lddx, int64_t lddw, void* workspace, void* stream) {
+                              int64_t ldwu, int64_t lddx, int64_t lddw, void* workspace, void* stream) {
   const GatedWorkspace at = gated_workspace(M, F, K);
   uint8_t* const ws = static_cast<uint8_t*>(workspace);
   uint16_t *const rows = reinterpret_cast<uint16_t*>(ws + at.rows), *const cols = reinterpret_cast<uint16_t*>(ws + at.cols);
   uint16_t *const xt = reinterpret_cast<uint16_t*>(ws + at.xt), *const wt = reinterpret_cast<uint16_t*>(ws + at.wt);
-  GatedGradArgs a{static_cast<const uint16_t*>(dh), g, u, rows, cols, lddh, ld_saved,
-                  int32_t(M), F, int32_t(at.Mp), int32_t(at.Fp), 0.f, 0.f};
+  GatedGradArgs a{static_cast<const uint16_t*>(dh), saved, saved + gated_saved_values(M, F) / 2, rows, cols, lddh, int32_t(M), F, int32_t(at.Mp), int32_t(at.Fp), 0.f, 0.f};
   activation_factors(activation, &a.act0, &a.act1);
   const dim3 grid(unsigned(at.Fp / kSide), unsigned(at.Mp / kSide));
   hipLaunchKernelGGL(gated_grad_kernel, grid, dim3(256), 0, static_cast<hipStream_t>(stream), a);

@@ -153,8 +153,9 @@ __global__ __launch_bounds__(64 * kFewWaves) void gemm_few_kernel(OpArgs a) {
     leave(gated_value(g[0], v[0], a.act0, a.act1), gated_value(g[1], v[1], a.act0, a.act1),
           gated_value(g[2], v[2], a.act0, a.act1), gated_value(g[3], v[3], a.act0, a.act1));
     if (a.g) {
-      *reinterpret_cast<Sums*>(a.g + int64_t(m) * a.ld_saved + n) = g;
-      *reinterpret_cast<Sums*>(a.u + int64_t(m) * a.ld_saved + n) = v;
+      const int64_t at = saved_at(m, n, a.N);
+      *reinterpret_cast<Sums*>(a.g + at) = g;
+      *reinterpret_cast<Sums*>(a.u + at) = v;
     }
   } else {
     float xs;

@@ -28,13 +28,13 @@ constexpr OpModel kModel[] = {{256, 256, 1, 1580, 985, 1240, 6120}, {192, 256, 1
 
 }  // namespace
 
-int32_t launch_gemm_gated(const void* x, const void* w_gate, const void* w_up, void* h, float* g, float* u, int activation, int64_t M, int32_t F,
-                          int32_t K, int64_t ldx, int64_t ldwg, int64_t ldwu, int64_t ldh, int64_t ld_saved, void* stream) {
+int32_t launch_gemm_gated(const void* x, const void* w_gate, const void* w_up, void* h, float* saved, int activation, int64_t M, int32_t F,
+                          int32_t K, int64_t ldx, int64_t ldwg, int64_t ldwu, int64_t ldh, void* stream) {
   if (M == 0) return CA_OK;
   OpArgs a{};
   a.x = x; a.w = w_gate; a.w2 = w_up; a.y = h;
-  a.g = g; a.u = u;
-  a.ldy = ldh; a.ld_saved = ld_saved;
+  a.g = saved; a.u = saved ? saved + gated_saved_values(M, F) / 2 : nullptr;
+  a.ldy = ldh;
   a.M = int32_t(M); a.N = F; a.K = 2 * K;
   a.ldx = int32_t(2 * ldx); a.ldw = int32_t(2 * ldwg); a.ldw2 = int32_t(2 * ldwu);
   activation_factors(activation, &a.act0, &a.act1);

@@ -57,8 +57,7 @@ __global__ __launch_bounds__(256, 1) void gemm_op_rows_kernel(OpArgs a) {
     const uint64_t g = reinterpret_cast<uint64_t>(a.g), u = reinterpret_cast<uint64_t>(a.u);
 #define CA_GEMM_GATED_OPERANDS                                                                                         \
   CA_GEMM_OP_ROWS_OPERANDS, [g] "s"(g), [g_lo] "s"(uint32_t(g)), [g_hi] "s"(uint32_t(g >> 32)), [u_lo] "s"(uint32_t(u)), \
-      [u_hi] "s"(uint32_t(u >> 32)), [ld4] "s"(uint32_t(a.ld_saved) * 4), [ld64] "s"(uint32_t(a.ld_saved) * 64),       \
-      [act0] "s"(a.act0), [act1] "s"(a.act1)
+      [u_hi] "s"(uint32_t(u >> 32)), [blocks_n] "s"((a.N + 31) / 32), [act0] "s"(a.act0), [act1] "s"(a.act1)
     if constexpr (kMt == 8) {
       asm volatile(
 #include "gemm_rows_gated_256_gfx950.inc"

@@ -65,8 +65,9 @@ __global__ __launch_bounds__(T::kThreads) void gemm_op_kernel(OpArgs a) {
         to[0] = pack_bf16(h[0], h[1]);
         to[1] = pack_bf16(h[2], h[3]);
         if (a.g && m0 + row < a.M && n0 + col < a.N) {
-          *reinterpret_cast<f32x4*>(a.g + int64_t(m0 + row) * a.ld_saved + n0 + col) = g;
-          *reinterpret_cast<f32x4*>(a.u + int64_t(m0 + row) * a.ld_saved + n0 + col) = u;
+          const int64_t at = saved_at(m0 + row, n0 + col, a.N);
+          *reinterpret_cast<f32x4*>(a.g + at) = g;
+          *reinterpret_cast<f32x4*>(a.u + at) = u;
         }
       }
   } else {

@@ -31,7 +31,7 @@ next tile's are requested when a tile has left, ahead of the stages' loads behin
 Gated ("gated"): Y = act(X Wg') * (X Wu').  Of a tile's 256 rows of W, waves 0 and 2 load 64 rows of the gate's each and waves 1 and 3
 the up projection's of the same columns, so that of a wave's 8 sub-tiles over n the first four are gate, the last four up, and a lane
 ends up with both of the same elements; a tile has 128 columns of Y.  act(g) = g / (1 + exp(-p)), p = g (act0 + act1 g^2), g held
-within 1e4 there.  With %[save] the projections leave too, in fp32, straight from the accumulators.
+within 1e4 there.  With %[g] the projections leave too (save_lines).
 
 Register map:
   a[0:32 MT - 1]   accumulators, sub-tile (ti over n, tj over m) at a[4 (MT ti + tj) ..]
@@ -68,7 +68,7 @@ S_RET = 54               # 54,55: where out-of-line code returns to
 S_T = 56                 # 56..63 temporaries
 S_COLS = 64              # 64..67: lanes whose columns exist, of the first 64 and the others
 S_ROWS, S_NCOL = 68, 69  # rows and columns of the tile that exist
-S_P = 70                 # 70,71: base of the scales; gated: 70 the bound on g, 70..73 strides
+S_P = 70                 # 70,71: base of the scales; gated: 70 the bound on g, 72,73 base of the saved up projection
 LAST_SGPR = 73
 MFMA = {"plain": "v_mfma_f32_16x16x32_bf16", "gated": "v_mfma_f32_16x16x32_bf16", "i8": "v_mfma_i32_16x16x64_i8"}
 
@@ -199,35 +199,33 @@ def gate_lines(mt, tj, c, pack):
 
 
 def save_lines(mt):
-    """gated, training: g and u in fp32, 16 bytes of a row to a lane straight from an accumulator.  (S_T + 2, + 3: the tile's rows and
-    columns that are ahead of it; row masks for all 16 rows of a sub-tile here.)"""
-    a, t, g, u = S_T, 84, 86, 88
-    out = ["s_cmp_eq_u64 %[g], 0", "s_nop 0", "s_cbranch_scc1 SAVED_%="] + lane_lines(t)
-    out += [f"v_lshrrev_b32 {V(t + 1)}, 4, {V(t)}", f"v_lshlrev_b32 {V(t + 1)}, 3, {V(t + 1)}", f"v_and_b32 {V(t)}, 15, {V(t)}",
-            # row of the tile (wave % 2) 16 mt + lane % 16, column (wave / 2) 64 + 8 grp
-            f"s_and_b32 s{a + 4}, %[wave], 1", f"s_mul_i32 s{a + 4}, s{a + 4}, {16 * mt}", f"v_add_u32 {V(t)}, s{a + 4}, {V(t)}",
-            f"s_lshr_b32 s{a + 4}, %[wave], 1", f"s_lshl_b32 s{a + 4}, s{a + 4}, 6", f"v_add_u32 {V(t + 1)}, s{a + 4}, {V(t + 1)}"]
-    for c in range(2):
-        out += [f"s_sub_i32 s{a + 4}, s{S_NCOL}, {32 * c}", f"v_cmp_gt_i32 s[{S_COLS + 2 * c}:{S_COLS + 2 * c + 1}], s{a + 4}, {V(t + 1)}"]
-    # g + 4 ((tm 32 mt + row) ld + tn 128 + column)
-    out += [f"s_mul_i32 s{a + 4}, s{a}, {32 * mt}", f"v_add_u32 {V(90)}, s{a + 4}, {V(t)}", f"s_lshl_b32 s{a + 4}, s{a + 1}, 7",
-            f"v_add_u32 {V(t + 1)}, s{a + 4}, {V(t + 1)}", f"v_lshlrev_b32 {V(t + 1)}, 2, {V(t + 1)}",
-            f"v_mul_lo_u32 {V(g)}, {V(90)}, %[ld4]", f"v_mul_hi_u32 {V(g + 1)}, {V(90)}, %[ld4]",
-            f"v_add_co_u32 {V(g)}, vcc, {V(g)}, {V(t + 1)}", "s_nop 1", f"v_addc_co_u32 {V(g + 1)}, vcc, 0, {V(g + 1)}, vcc"]
-    for to, name in ((u, "u"), (g, "g")):
-        out += [f"v_mov_b32 {V(91)}, %[{name}_hi]", f"v_add_co_u32 {V(to)}, vcc, %[{name}_lo], {V(g)}", "s_nop 1",
-                f"v_addc_co_u32 {V(to + 1)}, vcc, {V(91)}, {V(g + 1)}, vcc"]
+    """gated, training: g and u in fp32 straight from the accumulators, in blocks of 16 rows and 32 columns: a store is half a block, 1 KB in
+    one piece.  Blocks that are all behind the last row or column are left out.  (In S_T, S_T + 1: the tile's numbers.)"""
+    a, g, u, off = S_T, S_T + 2, S_P + 2, 84
+    out = ["s_cmp_eq_u64 %[g], 0", "s_nop 0", "s_cbranch_scc1 SAVED_%="] + lane_lines(off)
+    # columns left to the wave: in one or two blocks; rows left
+    out += [f"v_lshlrev_b32 {V(off)}, 4, {V(off)}", f"s_lshr_b32 s{a + 4}, %[wave], 1", f"s_lshl_b32 s{a + 5}, s{a + 4}, 6",
+            f"s_sub_i32 s{a + 5}, s{S_NCOL}, s{a + 5}", f"s_cmp_ge_i32 0, s{a + 5}", "s_nop 0", "s_cbranch_scc1 SAVED_%=",
+            f"s_cmp_ge_i32 32, s{a + 5}", f"s_cselect_b32 s{S_COLS}, 0, -1", f"s_mov_b32 s{S_COLS + 1}, s{S_COLS}",
+            f"s_and_b32 s{a + 5}, %[wave], 1", f"s_mul_i32 s{a + 6}, s{a + 5}, {16 * mt}", f"s_sub_i32 s{a + 6}, s{S_ROWS}, s{a + 6}",
+            # block ((2 tm + wave % 2) mt) blocks_n + 4 tn + 2 (wave / 2), 2 KB each
+            f"s_lshl_b32 s{a}, s{a}, 1", f"s_add_u32 s{a}, s{a}, s{a + 5}", f"s_mul_i32 s{a}, s{a}, {mt}", f"s_mul_i32 s{a}, s{a}, %[blocks_n]",
+            f"s_lshl_b32 s{a + 1}, s{a + 1}, 1", f"s_add_u32 s{a + 1}, s{a + 1}, s{a + 4}", f"s_lshl_b32 s{a + 1}, s{a + 1}, 1",
+            f"s_add_u32 s{a}, s{a}, s{a + 1}", f"s_lshl_b32 s{a + 4}, s{a}, 11", f"s_lshr_b32 s{a + 5}, s{a}, 21"]
+    for to, name in ((g, "g"), (u, "u")):
+        out += [f"s_add_u32 s{to}, %[{name}_lo], s{a + 4}", f"s_addc_u32 s{to + 1}, %[{name}_hi], s{a + 5}"]
+    out.append(f"s_lshl_b32 s{a + 4}, %[blocks_n], 11")
     for tj in range(mt):
-        out += [f"s_sub_i32 s{a + 4}, s{S_ROWS}, {16 * tj}", f"v_cmp_gt_i32 vcc, s{a + 4}, {V(t)}", "s_nop 1"]
+        out += [f"s_cmp_ge_i32 {16 * tj}, s{a + 6}", "s_nop 0", "s_cbranch_scc1 SAVED_%="]
         for c in range(2):
-            out.append(f"s_and_b64 exec, vcc, s[{S_COLS + 2 * c}:{S_COLS + 2 * c + 1}]")
+            out.append("s_mov_b64 exec, -1" if c == 0 else f"s_mov_b64 exec, s[{S_COLS}:{S_COLS + 1}]")
             for b in range(2):
-                out += [f"global_store_dwordx4 {V(to, 2)}, {A(4 * (mt * (2 * c + b + of) + tj), 4)}, off offset:{128 * c + 16 * b}"
+                out += [f"global_store_dwordx4 {V(off)}, {A(4 * (mt * (2 * c + b + of) + tj), 4)}, s[{to}:{to + 1}] offset:{2048 * c + 1024 * b} nt"
                         for to, of in ((g, 0), (u, 4))]
         out.append("s_mov_b64 exec, -1")
         if tj < mt - 1:
             for to in (g, u):
-                out += [f"v_add_co_u32 {V(to)}, vcc, %[ld64], {V(to)}", "s_nop 1", f"v_addc_co_u32 {V(to + 1)}, vcc, 0, {V(to + 1)}, vcc"]
+                out += [f"s_add_u32 s{to}, s{to}, s{a + 4}", f"s_addc_u32 s{to + 1}, s{to + 1}, 0"]
     return out + ["SAVED_%=:"]
 
 

@@ -35,6 +35,7 @@ decltype(&kv_cache_append_batch_norm) append_norm_fn = nullptr;
 decltype(&layer_linear_i8_workspace) i8_workspace_fn = nullptr;
 decltype(&layer_linear_i8_values) i8_fn = nullptr;
 decltype(&layer_gated_bf16) gated_fn = nullptr;
+decltype(&layer_gated_saved_bytes) gated_saved_fn = nullptr;
 decltype(&layer_gated_backward_workspace) gated_workspace_fn = nullptr;
 decltype(&layer_gated_backward_bf16) gated_backward_fn = nullptr;
 
@@ -364,15 +365,15 @@ PyObject* gated(PyObject* const* a, Py_ssize_t n) {
   int64_t ldh;
   if (!matrix(&h, at::kBFloat16, c.m, c.f, *c.x, &ldh)) return not_taken();
   at::Tensor saved;
-  float *g = nullptr, *u = nullptr;
+  float* kept = nullptr;
   if (train) {
-    saved = at::empty({2, c.m, c.f}, c.x->options().dtype(at::kFloat));
-    g = saved.data_ptr<float>(), u = g + c.m * c.f;
+    saved = at::empty({int64_t(gated_saved_fn(c.m, int32_t(c.f)) / 4)}, c.x->options().dtype(at::kFloat));
+    kept = saved.data_ptr<float>();
   }
   const void *xp = c.x->data_ptr(), *gp = c.wg->data_ptr(), *up = c.wu->data_ptr();
   void *const hp = h.data_ptr(), *const stream = c.stream();
   const int32_t rc = released([&] {
-    return gated_fn(xp, gp, up, hp, g, u, act, c.m, int32_t(c.f), int32_t(c.k), c.ldx, c.ldg, c.ldu, ldh, c.f, stream);
+    return gated_fn(xp, gp, up, hp, kept, act, c.m, int32_t(c.f), int32_t(c.k), c.ldx, c.ldg, c.ldu, ldh, stream);
   });
   if (!train || rc != CA_OK) return r.give(rc);
   return tuple({r.give(rc), THPVariable_Wrap(saved)});
@@ -385,18 +386,18 @@ PyObject* gated_backward(PyObject* const* a, Py_ssize_t n) {
   int64_t lddh;
   if (n != 6 || !c.take(a) || !whole32(a[5], &act)) return not_taken();
   const at::Tensor *dh = plain(a[3]), *saved = plain(a[4]);
-  if (!matrix(dh, at::kBFloat16, c.m, c.f, *c.x, &lddh) || !saved || saved->scalar_type() != at::kFloat || saved->dim() != 3 || saved->size(0) != 2 ||
-      saved->size(1) != c.m || saved->size(2) != c.f || !saved->is_contiguous() || !beside(*saved, *c.x))
+  if (!matrix(dh, at::kBFloat16, c.m, c.f, *c.x, &lddh) || !saved || saved->scalar_type() != at::kFloat || 
+      uint64_t(saved->numel()) * 4 != gated_saved_fn(c.m, int32_t(c.f)) || !saved->is_contiguous() || !beside(*saved, *c.x))
     return not_taken();
   const size_t bytes = gated_workspace_fn(c.m, int32_t(c.f), int32_t(c.k));
   const at::Tensor dx = at::empty({c.m, c.k}, c.x->options()), dw = at::empty({2, c.f, c.k}, c.x->options()),
                    work = at::empty({int64_t(bytes)}, c.x->options().dtype(at::kByte));
-  const float *const g = saved->data_ptr<float>(), *const u = g + c.m * c.f;
+  const float* const kept = saved->data_ptr<float>();
   const void *xp = c.x->data_ptr(), *gp = c.wg->data_ptr(), *up = c.wu->data_ptr(), *dhp = dh->data_ptr();
   void *const dxp = dx.data_ptr(), *const dwp = dw.data_ptr(), *const workp = work.data_ptr(), *const stream = c.stream();
   const int32_t rc = released([&] {
-    return gated_backward_fn(dhp, xp, gp, up, g, u, act, dxp, dwp, static_cast<char*>(dwp) + c.f * c.k * 2, c.m, int32_t(c.f), int32_t(c.k), lddh, c.ldx,
-                             c.ldg, c.ldu, c.f, c.k, c.k, workp, bytes, stream);
+    return gated_backward_fn(dhp, xp, gp, up, kept, act, dxp, dwp, static_cast<char*>(dwp) + c.f * c.k * 2, c.m, int32_t(c.f), int32_t(c.k), lddh, c.ldx,
+                             c.ldg, c.ldu, c.k, c.k, workp, bytes, stream);
   });
   if (rc != CA_OK) return PyLong_FromLong(rc);
   return tuple({THPVariable_Wrap(dx), THPVariable_Wrap(dw[0]), THPVariable_Wrap(dw[1])});
@@ -505,14 +506,14 @@ PyObject* bind(PyObject* const* a, Py_ssize_t n) {
   Py_RETURN_NONE;
 }
 
-// bind_layer(addresses of the nine entry points of the rest of a layer in the order above)
+// bind_layer(addresses of the ten entry points of the rest of a layer in the order above)
 PyObject* bind_layer(PyObject* const* a, Py_ssize_t n) {
-  int64_t f[9];
-  if (n != 9) {
-    PyErr_SetString(PyExc_TypeError, "nine addresses");
+  int64_t f[10];
+  if (n != 10) {
+    PyErr_SetString(PyExc_TypeError, "ten addresses");
     return nullptr;
   }
-  for (int i = 0; i < 9; ++i)
+  for (int i = 0; i < 10; ++i)
     if (!whole(a[i], f + i) || f[i] == 0) {
       PyErr_SetString(PyExc_TypeError, "an address is an int");
       return nullptr;
@@ -524,8 +525,9 @@ PyObject* bind_layer(PyObject* const* a, Py_ssize_t n) {
   i8_workspace_fn = reinterpret_cast<decltype(i8_workspace_fn)>(f[4]);
   i8_fn = reinterpret_cast<decltype(i8_fn)>(f[5]);
   gated_fn = reinterpret_cast<decltype(gated_fn)>(f[6]);
-  gated_workspace_fn = reinterpret_cast<decltype(gated_workspace_fn)>(f[7]);
-  gated_backward_fn = reinterpret_cast<decltype(gated_backward_fn)>(f[8]);
+  gated_saved_fn = reinterpret_cast<decltype(gated_saved_fn)>(f[7]);
+  gated_workspace_fn = reinterpret_cast<decltype(gated_workspace_fn)>(f[8]);
+  gated_backward_fn = reinterpret_cast<decltype(gated_backward_fn)>(f[9]);
   Py_RETURN_NONE;
 }
 

@@ -384,10 +384,8 @@ def _gated(x, w_gate, w_up, activation, out, saved):
     (m, k), f, device = x.shape, w_gate.shape[0], x.device
     ldx, ldg, ldu = _matrix(x, x, _BF16, m, k), _matrix(w_gate, x, _BF16, f, k), _matrix(w_up, x, _BF16, f, k)
     h = torch.empty((m, f), dtype=_BF16, device=device) if out is None else out
-    g, u = saved if saved is not None else (None, None)
-    B.layer_gated_bf16(x.data_ptr(), w_gate.data_ptr(), w_up.data_ptr(), h.data_ptr(), 0 if g is None else g.data_ptr(),
-                       0 if u is None else u.data_ptr(), _ACTIVATIONS[activation], m, f, k, ldx, ldg, ldu, _matrix(h, x, _BF16, m, f),
-                       f, _current_stream(device))
+    B.layer_gated_bf16(x.data_ptr(), w_gate.data_ptr(), w_up.data_ptr(), h.data_ptr(), 0 if saved is None else saved.data_ptr(),
+                       _ACTIVATIONS[activation], m, f, k, ldx, ldg, ldu, _matrix(h, x, _BF16, m, f), _current_stream(device))
     return h
 
 
@@ -403,14 +401,14 @@ def gated_linear(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, acti
 
 def gated_linear_train(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, activation: str = "silu",
                        out: torch.Tensor | None = None):
-    """gated_linear for training: (h, saved), saved being the two projections in fp32 [2, M, F] that gated_linear_backward
-    takes."""
+    """gated_linear for training: (h, saved), saved being the two projections in fp32 as gated_linear_backward takes them (in an
+    order of the library's own)."""
     r = B.calls.gated(x, w_gate, w_up, _ACTIVATIONS[activation], out, True)
     if r.__class__ is int:
         B._check(r, "layer_gated_bf16")
     if r is not None:
         return r
-    saved = torch.empty((2, x.shape[0], w_gate.shape[0]), dtype=torch.float32, device=x.device)
+    saved = torch.empty(B.layer_gated_saved_bytes(x.shape[0], w_gate.shape[0]) // 4, dtype=torch.float32, device=x.device)
     return _gated(x, w_gate, w_up, activation, out, saved), saved
 
 
@@ -426,13 +424,13 @@ def gated_linear_backward(dh: torch.Tensor, x: torch.Tensor, w_gate: torch.Tenso
     (m, k), f, device = x.shape, w_gate.shape[0], x.device
     ldx, ldg, ldu = _matrix(x, x, _BF16, m, k), _matrix(w_gate, x, _BF16, f, k), _matrix(w_up, x, _BF16, f, k)
     lddh = _matrix(dh, x, _BF16, m, f)
-    assert saved.shape == (2, m, f) and saved.dtype == torch.float32 and saved.is_contiguous() and _reachable(saved, x)
+    assert saved.dtype == torch.float32 and saved.numel() * 4 == B.layer_gated_saved_bytes(m, f) and saved.is_contiguous() and _reachable(saved, x)
     dx, dw = torch.empty((m, k), dtype=_BF16, device=device), torch.empty((2, f, k), dtype=_BF16, device=device)
     nbytes = B.layer_gated_backward_workspace(m, f, k)
     work = torch.empty(nbytes, dtype=torch.uint8, device=device)
-    B.layer_gated_backward_bf16(dh.data_ptr(), x.data_ptr(), w_gate.data_ptr(), w_up.data_ptr(), saved[0].data_ptr(), saved[1].data_ptr(),
+    B.layer_gated_backward_bf16(dh.data_ptr(), x.data_ptr(), w_gate.data_ptr(), w_up.data_ptr(), saved.data_ptr(),
                                 _ACTIVATIONS[activation], dx.data_ptr(), dw[0].data_ptr(), dw[1].data_ptr(), m, f, k, lddh, ldx, ldg, ldu,
-                                f, k, k, work.data_ptr(), nbytes, _current_stream(device))
+                                k, k, work.data_ptr(), nbytes, _current_stream(device))
     return dx, dw[0], dw[1]
 
 

@@ -37,7 +37,7 @@ class _Wave:
         self.gated = kind == "gated"
         self.cols = 128 if self.gated else 256
         self.label = {ln[:-1]: k for k, ln in enumerate(text) if ln.endswith(":")}
-        self.ldx, self.ldw, self.ldy, self.ld_saved = K + 16 * pad, K + 32 * pad + (64 if self.gated and wave & 1 else 0), 2 * (N + 24 * pad), N + 8 * pad
+        self.ldx, self.ldw, self.ldy = K + 16 * pad, K + 32 * pad + (64 if self.gated and wave & 1 else 0), 2 * (N + 24 * pad)
         self.w_at = UP_AT if self.gated and wave & 1 else W_AT
         lane = np.arange(64, dtype=np.int64)
         l15, grp, wm, wn, rows_ = lane & 15, lane >> 4, wave & 1, wave >> 1, 32 * mt
@@ -52,7 +52,7 @@ class _Wave:
                     "chunkw": ((lane & 7) ^ ((lane >> 4) & 1)) * 16, "chunkx": ((lane & 7) ^ (lane >> 4)) * 16,
                     "aw0": (wn * 128 + 8 * (l15 >> 2) + (l15 & 3)) * 128 + ((grp ^ (l15 >> 1)) << 4),
                     "ax0": (wm * 16 * mt + l15) * 128 + ((grp ^ (l15 >> 1)) << 4), "row": row, "col": col, "ylane_lo": ylane & U32, "ylane_hi": ylane >> 32,
-                    "g": g, "ld4": 4 * self.ld_saved, "ld64": 64 * self.ld_saved, "act0": _Value(), "act1": _Value()}
+                    "g": g, "blocks_n": -(-N // 32), "act0": _Value(), "act1": _Value()}
         for name, at in (("x", X_AT), ("w", self.w_at), ("y", Y_AT), ("tile_y", tile_y), ("row8", row8), ("xs", XS_AT), ("ws", WS_AT), ("g", g), ("u", u)):
             self.arg[name + "_lo"], self.arg[name + "_hi"] = at & U32, at >> 32
         self.s, self.v, self.a = {}, {}, {}
@@ -117,12 +117,16 @@ class _Wave:
                 k = self.label[a[0]]
             elif op.startswith("s_cmp_"):
                 x, y = self.val(a[0]), self.val(a[1])
+                if op.endswith("i32"):
+                    x, y = signed(x), signed(y)
                 self.scc = int({"eq": x == y, "lg": x != y, "lt": x < y, "ge": x >= y}[op.split("_")[2]])
             elif op == "s_and_b64":
                 self.exec = self.val(a[1]) & self.val(a[2])
             elif op == "s_mov_b64":
-                assert a == ["exec", "-1"]
-                self.exec = np.ones(64, bool)
+                assert a[0] == "exec"
+                bits = (1 << 64) - 1 if a[1] == "-1" else self.val(a[1])
+                assert bits in (0, (1 << 64) - 1)
+                self.exec = np.full(64, bool(bits))
             elif op.startswith("s_") and op not in ("s_nop", "s_waitcnt", "s_cbranch_scc1"):
                 x = self.val(a[1])
                 y = self.val(a[2]) if len(a) > 2 else None
@@ -182,13 +186,14 @@ class _Wave:
                 self.v[int(a[0][1:])] = _Value(xs=src.xs[(addr + imm) // 4 % 64])
                 self.flying.append(int(a[0][1:]))
             elif op == "global_store_dwordx4" and a[1].startswith("a["):      # a projection, straight from the accumulators
-                acc, row0 = int(a[1][2:].split(":")[0]), int(a[0][2:].split(":")[0])
-                addr = self.v[row0] + (self.v[row0 + 1] << 32) + imm
+                acc, addr = int(a[1][2:].split(":")[0]), self.val(a[2].split()[0]) + self.val(a[0]) + imm
+                up = int(addr[0]) >= U_AT
+                rel = addr - (U_AT if up else G_AT)
+                assert (rel[self.exec] % 16 == 0).all() and (rel[self.exec] >= 0).all()
                 for lane in np.flatnonzero(self.exec):
-                    up = int(addr[lane]) >= U_AT
-                    rel = int(addr[lane]) - (U_AT if up else G_AT)
-                    m, n = rel // 4 // self.ld_saved, rel // 4 % self.ld_saved
-                    assert rel % 16 == 0 and m < M and n + 4 <= N and (m, n, up) not in self.saved
+                    block, at = divmod(int(rel[lane]), 2048)
+                    m, n = 16 * (block // -(-N // 32)) + at % 1024 // 16 % 16, 32 * (block % -(-N // 32)) + 8 * (at % 1024 // 256) + 4 * (at // 1024)
+                    assert m < -(-M // 16) * 16 and (m, n, up) not in self.saved
                     for r in range(4):
                         assert self.a[acc + r][1] == per_tile and self.sum_at(acc + r, lane) == (m, n + r, up)
                     self.saved[m, n, up] = True
@@ -337,7 +342,8 @@ def test_loop_over_tiles(kind, save, mt, shape, tiles, pad, form):
     got = [k for w in waves for k in w.written]
     assert len(got) == len(want) and set(got) == want
     kept = [k for w in waves for k in w.saved]
-    assert len(kept) == len(set(kept)) and set(kept) == {(m, n + 4 * b, up) for m, n in want for b in range(2) for up in (False, True) if save}
+    blocks = {(m // 16, n // 32) for m, n in want} if save else set()            # whole blocks, of those that hold anything
+    assert len(kept) == len(set(kept)) and set(kept) == {(16 * i + r, 32 * j + c, up) for i, j in blocks for r in range(16) for c in range(0, 32, 4) for up in (False, True)}
     assert all(w.forms.get(t, "") == rows.FORMS[form >> 2 if t == len(tiles) - 1 else form & 3].strip() for w in waves if w.written for t in w.forms)
 
 

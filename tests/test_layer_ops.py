@@ -332,6 +332,12 @@ def _gated_reference(x, wg, wu, act):
     return a * u, g, u, off
 
 
+def _kept(saved, M, F):
+    """[2, M, F] of what training saves: blocks of 16 rows and 32 columns, of each the first four of every eight columns of all rows, then the others"""
+    t = saved.view(2, -(-M // 16), -(-F // 32), 2, 4, 16, 4).permute(0, 1, 5, 2, 4, 3, 6)
+    return t.reshape(2, -(-M // 16) * 16, -(-F // 32) * 32)[:, :M, :F]
+
+
 GATED = [(1, 8, 128), (1, 1000, 640), (2, 72, 5120), (16, 64, 256), (17, 40, 128), (32, 136, 384), (33, 8, 128), (63, 128, 256), (65, 200, 128),
          (129, 72, 640), (300, 1032, 512), (1100, 1400, 256), (2050, 1160, 128), (2050, 2184, 384), (4680, 776, 256), (700, 4504, 384)]
 
@@ -352,7 +358,8 @@ def test_gated_linear(M, F, K, act):
     assert ((got - h).abs() <= h.abs() * 2.0 ** -8 + 1.05 * off + 1e-30).all()
     h2, saved = gated_linear_train(x[:M, :K], wg[:, :K], wu, act)
     assert (h2 == y[:M, :F]).all()
-    for p, t in ((g, saved[0]), (u, saved[1])):
+    kept = _kept(saved, M, F)
+    for p, t in ((g, kept[0]), (u, kept[1])):
         w = wg[:, :K] if p is g else wu
         assert ((t.double().cpu() - p).abs() <= 2e-6 * (x[:M, :K].double().cpu().abs() @ w.double().cpu().abs().T)).all()
 
@@ -452,7 +459,8 @@ def test_offsets_that_pass_32_bits():
     h, saved = gated_linear_train(x, wg, wu)
     assert (h[-300:] == gated_linear(x[-300:], wg, wu)).all()
     few, kept = gated_linear_train(x[-300:], wg, wu)
-    assert (few == h[-300:]).all() and (saved[:, -300:] == kept).all()
+    assert (few == h[-300:]).all()
+    assert (_kept(saved, M, N)[:, -300:] == _kept(kept, 300, N)).all()
 
 
 @pytest.mark.gpu
@@ -515,7 +523,7 @@ def test_both_ways_do_the_same(monkeypatch):
         out += [y, R.linear_i8(x[:1], wq), R.linear_i8(x.float(), wq), R.linear_i8(R.quantize_rows(x), wq)]
         assert R.gated_linear(x, wg, wu, out=h) is h
         h2, saved = R.gated_linear_train(x, wg, wu, "gelu")
-        return out + [h, R.gated_linear(x[:1], wg, wu), h2, saved, *R.gated_linear_backward(dh, x, wg, wu, saved, "gelu")]
+        return out + [h, R.gated_linear(x[:1], wg, wu), h2, _kept(saved, n, F), *R.gated_linear_backward(dh, x, wg, wu, saved, "gelu")]
 
     first = results()
     monkeypatch.setattr(B, "calls", B._NoCalls())
@@ -589,29 +597,30 @@ def test_refusals():
         args = list(ok)
         args[i] = bad
         _refused(code, B.layer_linear_i8_values, *args)
-    ok = [4096] * 6 + [B.CA_SILU, 5, 16, 128, 128, 128, 128, 16, 16]
-    for i, bad, code in [(0, 0, E), (1, 4104, E), (2, 0, E), (3, 0, E), (4, 0, E), (5, 8, E), (6, 2, E), (7, -1, E), (7, 1 << 31, U), (8, 12, U), (9, 64, U), (9, 192, U),
-                         (10, 120, E), (11, 132, E), (12, 1 << 22, U), (13, 8, E), (14, 8, E), (14, 20, E)]:
+    assert B.layer_gated_saved_bytes(5, 40) == 2 * 16 * 64 * 4 and B.layer_gated_saved_bytes(5, 4) == 0
+    ok = [4096] * 5 + [B.CA_SILU, 5, 16, 128, 128, 128, 128, 16]
+    for i, bad, code in [(0, 0, E), (1, 4104, E), (2, 0, E), (3, 0, E), (4, 8, E), (5, 2, E), (6, -1, E), (6, 1 << 31, U), (7, 12, U), (8, 64, U), (8, 192, U),
+                         (9, 120, E), (10, 132, E), (11, 1 << 22, U), (12, 8, E)]:
         args = list(ok)
         args[i] = bad
         _refused(code, B.layer_gated_bf16, *args)
     need = B.layer_gated_backward_workspace(5, 16, 128)
     assert need > 0 and B.layer_gated_backward_workspace(5, 12, 128) == 0 == B.layer_gated_backward_workspace(-1, 16, 128)
-    ok = [4096] * 6 + [B.CA_GELU] + [4096] * 3 + [5, 16, 128, 16, 128, 128, 128, 16, 128, 128, 4096, need]
-    for i, bad, code in [(0, 0, E), (1, 0, E), (2, 0, E), (3, 4104, E), (4, 0, E), (5, 0, E), (6, -1, E), (7, 8, E), (10, -1, E), (10, 1 << 23, U), (11, 4, U), (12, 100, U),
-                         (13, 8, E), (14, 120, E), (17, 12, E), (18, 127, E), (19, 1 << 22, U), (20, 0, E), (20, 4104, E), (21, need - 1, E)]:
+    ok = [4096] * 5 + [B.CA_GELU] + [4096] * 3 + [5, 16, 128, 16, 128, 128, 128, 128, 128, 4096, need]
+    for i, bad, code in [(0, 0, E), (1, 0, E), (2, 0, E), (3, 4104, E), (4, 0, E), (5, -1, E), (6, 8, E), (9, -1, E), (9, 1 << 23, U), (10, 4, U), (11, 100, U),
+                         (12, 8, E), (13, 120, E), (16, 127, E), (17, 1 << 22, U), (18, 0, E), (18, 4104, E), (19, need - 1, E)]:
         args = list(ok)
         args[i] = bad
         _refused(code, B.layer_gated_backward_bf16, *args)
-    _refused(E, B.layer_gated_backward_bf16, *ok[:7], 0, 0, 0, *ok[10:])
+    _refused(E, B.layer_gated_backward_bf16, *ok[:6], 0, 0, 0, *ok[9:])
 
 
 @pytest.mark.parametrize("host", [b"bytes of the host", (C.c_char * 64)(), 16.0, np.int64(16)], ids=["bytes", "array", "float", "numpy"])
 def test_addresses_are_integers(host):
     calls = [(B.layer_quantize_rows_i8, [16, 1, 16, 16, 0, 8, 8, 256], (0, 2, 3)), (B.layer_linear_i8, [16] * 5 + [0, 8, 8, 256, 256, 8], range(5)),
              (B.layer_linear_i8_values, [16, 1, 16, 16, 16, 0, 8, 8, 8, 256, 8, 16, 1 << 20], (0, 2, 3, 4, 11)),
-             (B.layer_gated_bf16, [16] * 6 + [0, 0, 8, 128, 128, 128, 128, 8, 8], range(6)),
-             (B.layer_gated_backward_bf16, [16] * 6 + [0] + [16] * 3 + [0, 8, 128, 8, 128, 128, 128, 8, 128, 128, 16, 0], (0, 1, 2, 3, 4, 5, 7, 8, 9, 20))]
+             (B.layer_gated_bf16, [16] * 5 + [0, 0, 8, 128, 128, 128, 128, 8], range(5)),
+             (B.layer_gated_backward_bf16, [16] * 5 + [0] + [16] * 3 + [0, 8, 128, 8, 128, 128, 128, 128, 128, 16, 0], (0, 1, 2, 3, 4, 6, 7, 8, 18))]
     for call, args, pointers in calls:
         for i in pointers:
             with pytest.raises(TypeError):
