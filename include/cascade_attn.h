@@ -297,7 +297,7 @@ int32_t kv_cache_append_batch_norm(ca_ctx* ctx, int32_t n_blocks, const int64_t*
 /* Rows of x (CA_BF16 or CA_F32) in 8 bits with a scale each: scale = (largest magnitude) / 127, code = 127 x / (largest magnitude)
  * rounded half to even, as exact arithmetic gives it.  A row of zeros has scale 0 and codes 0; one that holds an infinity or
  * NaN has scale NaN and codes 0.  Codes behind k_in, up to the next multiple of 256, are written as zeros: a row of codes takes
- * ld_codes >= that many bytes (a multiple of 16).  x: any alignment and row stride (16-byte aligned rows are read faster). */
+ * ld_codes >= that many bytes (a multiple of 16).  x: any row stride, aligned as its values are. */
 #define CA_I8_MAX_K (1 << 17)    /* 127 * 127 * 2^17 < 2^31: sums of products are exact */
 int32_t layer_quantize_rows_i8(const void* x_dev, int32_t dtype, int8_t* codes_dev, float* scales_dev, int64_t rows, int32_t k_in,
                                int64_t ldx, int64_t ld_codes, void* hip_stream);

@@ -49,7 +49,8 @@ __device__ __forceinline__ void token_angles(const RopeGeom& g, int64_t n, int64
 }
 
 // A wave takes a token: its lanes cover 64 / chunks heads at a time (1 KB of bf16), rows_per_group heads in all, kAhead loads
-// requested together.
+// requested together, queries first, then keys (a loop over both picked the side for each load and weight: 23400 tokens of 40 + 40
+// heads 192 us, now 178, the rate of a copy; 4680 of 12 + 12 18.5, now 13.7).
 template <typename T>
 __global__ __launch_bounds__(256) void norm_rope_kernel(RopeGeom g, NormArgs a) {
   constexpr int kAhead = 4;
@@ -58,37 +59,38 @@ __global__ __launch_bounds__(256) void norm_rope_kernel(RopeGeom g, NormArgs a) 
   if (n >= a.n_tokens) return;
   const int lane = threadIdx.x & 63, c8 = lane % chunks, hs = lane / chunks;
   const int r0 = blockIdx.y * a.rows_per_group, r1 = min(r0 + a.rows_per_group, a.rows);
-  Vec8<T> w[2];
-#pragma unroll
-  for (int s = 0; s < 2; ++s)
-    if (s == 0 || a.rows > g.heads) w[s].load(static_cast<const T*>(a.side[s].w) + c8 * 8);
   float cs[4], sn[4];
   bool angles = false;
-  for (int r = r0 + hs; r - hs < r1; r += kAhead * head_slots) {
-    Vec8<T> e[kAhead];
 #pragma unroll
-    for (int i = 0; i < kAhead; ++i) {             // rows past the group's re-read its last one
-      const int row = min(r + i * head_slots, r1 - 1), s = row >= g.heads;
-      const NormSide& side = a.side[s];
-      e[i].load(static_cast<const T*>(side.x) + n * side.x_tok + int64_t(row - s * g.heads) * side.x_head + c8 * 8);
-    }
-    if (!angles) token_angles<sizeof(T) == 4>(g, n, a.first_frame, lane, c8, cs, sn);
-    angles = true;
+  for (int s = 0; s < 2; ++s) {
+    const int first = max(r0 - s * g.heads, 0), end = min(r1 - s * g.heads, g.heads);        // the group's heads of this side
+    if (first >= end) continue;
+    const NormSide& side = a.side[s];
+    const T* const x = static_cast<const T*>(side.x) + n * side.x_tok + c8 * 8;
+    T* const y = static_cast<T*>(side.y) + n * side.y_tok + c8 * 8;
+    Vec8<T> w;
+    w.load(static_cast<const T*>(side.w) + c8 * 8);
+    for (int h = first + hs; h - hs < end; h += kAhead * head_slots) {
+      Vec8<T> e[kAhead];
 #pragma unroll
-    for (int i = 0; i < kAhead; ++i) {
-      const int row = r + i * head_slots, s = row >= g.heads;
-      const NormSide& side = a.side[s];
-      norm8(e[i], s ? w[1].v : w[0].v, chunks, a.eps);
-      rotate8(e[i], cs, sn);
-      if (row < r1) e[i].store(static_cast<T*>(side.y) + n * side.y_tok + int64_t(row - s * g.heads) * side.y_head + c8 * 8);
+      for (int i = 0; i < kAhead; ++i) e[i].load(x + int64_t(min(h + i * head_slots, end - 1)) * side.x_head);      // past the last: that again
+      if (!angles) token_angles<sizeof(T) == 4>(g, n, a.first_frame, lane, c8, cs, sn);
+      angles = true;
+#pragma unroll
+      for (int i = 0; i < kAhead; ++i) {
+        norm8(e[i], w.v, chunks, a.eps);
+        rotate8(e[i], cs, sn);
+        if (h + i * head_slots < end) e[i].store(y + int64_t(h + i * head_slots) * side.y_head);
+      }
     }
   }
 }
 
-// A wave takes every so manieth token, all its rows or a group's, and keeps the sums of dy x r of its lanes.
+// A wave takes every so manieth token, all its rows or a group's, and keeps the sums of dy x r of its lanes.  23400 tokens of 40 + 40
+// heads 279 us (5.15 TB/s), 4680 of 12 + 12 26.8 with the second launch (picking the side for each value 298 and 31.6).
 template <typename T>
 __global__ __launch_bounds__(256) void norm_rope_backward_kernel(RopeGeom g, NormArgs a) {
-  constexpr int kAhead = 2;
+  constexpr int kAhead = 3;
   __shared__ float sums[4][2][2 * kMaxPairs];
   const int chunks = g.head_dim / 8, head_slots = 64 / chunks;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c8 = lane % chunks, hs = lane / chunks;
@@ -104,53 +106,60 @@ __global__ __launch_bounds__(256) void norm_rope_backward_kernel(RopeGeom g, Nor
   for (int64_t n = int64_t(blockIdx.x) * 4 + wave; n < a.n_tokens; n += int64_t(gridDim.x) * 4) {
     float cs[4], sn[4];
     bool angles = false;
-    for (int r = r0 + hs; r - hs < r1; r += kAhead * head_slots) {
-      Vec8<T> x[kAhead], d[kAhead];
 #pragma unroll
-      for (int i = 0; i < kAhead; ++i) {
-        const int row = min(r + i * head_slots, r1 - 1), s = row >= g.heads;
-        const NormSide& side = a.side[s];
-        x[i].load(static_cast<const T*>(side.x) + n * side.x_tok + int64_t(row - s * g.heads) * side.x_head + c8 * 8);
-        d[i].load(static_cast<const T*>(side.dz) + n * side.dz_tok + int64_t(row - s * g.heads) * side.dz_head + c8 * 8);
-      }
-      if (!angles) {
-        token_angles<sizeof(T) == 4>(g, n, a.first_frame, lane, c8, cs, sn);
+    for (int s = 0; s < 2; ++s) {
+      const int first = max(r0 - s * g.heads, 0), end = min(r1 - s * g.heads, g.heads);      // the group's heads of this side
+      if (first >= end) continue;
+      const NormSide& side = a.side[s];
+      const T* const x0 = static_cast<const T*>(side.x) + n * side.x_tok + c8 * 8;
+      const T* const dz0 = static_cast<const T*>(side.dz) + n * side.dz_tok + c8 * 8;
+      T* const y0 = static_cast<T*>(side.y) + n * side.y_tok + c8 * 8;
+      for (int h = first + hs; h - hs < end; h += kAhead * head_slots) {
+        Vec8<T> x[kAhead], d[kAhead];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) sn[j] = -sn[j];          // R' turns back
-        angles = true;
-      }
-#pragma unroll
-      for (int i = 0; i < kAhead; ++i) {
-        const int row = r + i * head_slots, s = row >= g.heads;
-        const bool mine = row < r1;
-        rotate8(d[i], cs, sn);
-        const float rstd = head_rstd(x[i], chunks, a.eps);
-        float dot = 0.f;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          x[i].v[j] *= rstd;
-          const float part = mine ? d[i].v[j] * x[i].v[j] : 0.f;
-          dw[0][j] += s ? 0.f : part;
-          dw[1][j] += s ? part : 0.f;
-          d[i].v[j] *= s ? w[1].v[j] : w[0].v[j];
-          dot = fmaf(d[i].v[j], x[i].v[j], dot);
+        for (int i = 0; i < kAhead; ++i) {         // past the last head: that one again
+          const int64_t at = min(h + i * head_slots, end - 1);
+          x[i].load(x0 + at * side.x_head);
+          d[i].load(dz0 + at * side.dz_head);
         }
-        const float mean = head_sum(dot, chunks) * (1.f / float(8 * chunks));
+        if (!angles) {
+          token_angles<sizeof(T) == 4>(g, n, a.first_frame, lane, c8, cs, sn);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) d[i].v[j] = rstd * fmaf(-x[i].v[j], mean, d[i].v[j]);
-        const NormSide& side = a.side[s];
-        if (mine) d[i].store(static_cast<T*>(side.y) + n * side.y_tok + int64_t(row - s * g.heads) * side.y_head + c8 * 8);
+          for (int j = 0; j < 4; ++j) sn[j] = -sn[j];        // R' turns back
+          angles = true;
+        }
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+          const bool mine = h + i * head_slots < end;
+          rotate8(d[i], cs, sn);
+          const float rstd = head_rstd(x[i], chunks, a.eps);
+          float dot = 0.f;
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            x[i].v[j] *= rstd;
+            dw[s][j] += mine ? d[i].v[j] * x[i].v[j] : 0.f;
+            d[i].v[j] *= w[s].v[j];
+            dot = fmaf(d[i].v[j], x[i].v[j], dot);
+          }
+          const float mean = head_sum(dot, chunks) * (1.f / float(8 * chunks));
+#pragma unroll
+          for (int j = 0; j < 8; ++j) d[i].v[j] = rstd * fmaf(-x[i].v[j], mean, d[i].v[j]);
+          if (mine) d[i].store(y0 + int64_t(h + i * head_slots) * side.y_head);
+        }
       }
     }
   }
+  for (int d = chunks; d < 64; d *= 2)             // over the heads that a wave's load covers
 #pragma unroll
-  for (int s = 0; s < 2; ++s)
+    for (int s = 0; s < 2; ++s)
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      float v = dw[s][j];
-      for (int d = chunks; d < 64; d *= 2) v += __shfl_xor(v, d, 64);
-      if (lane < chunks) sums[wave][s][lane * 8 + j] = v;
-    }
+      for (int j = 0; j < 8; ++j) dw[s][j] += __shfl_xor(dw[s][j], d, 64);
+  if (lane < chunks) {
+#pragma unroll
+    for (int s = 0; s < 2; ++s)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) sums[wave][s][lane * 8 + j] = dw[s][j];
+  }
   __syncthreads();
   float* out = a.partials + (int64_t(blockIdx.y) * gridDim.x + blockIdx.x) * 2 * g.head_dim;
   for (int i = threadIdx.x; i < 2 * g.head_dim; i += 256) {
@@ -159,19 +168,23 @@ __global__ __launch_bounds__(256) void norm_rope_backward_kernel(RopeGeom g, Nor
   }
 }
 
-// dw[side][d] from the workgroups' sums: 32 columns to a workgroup, its 32 rows of threads share the partials
+// dw[side][d] from the workgroups' sums: 16 columns to a workgroup, its 64 rows of threads share the partials
+constexpr int kGradCols = 16;
 __global__ __launch_bounds__(1024) void norm_weight_grad_kernel(const float* partials, int n_partials, int head_dim, float* dw0, float* dw1) {
-  __shared__ double sums[32][33];
-  const int x = threadIdx.x & 31, y = threadIdx.x >> 5, col = blockIdx.x * 32 + x;
+  __shared__ double sums[1024 / kGradCols][kGradCols + 1];
+  const int x = threadIdx.x % kGradCols, y = threadIdx.x / kGradCols, col = blockIdx.x * kGradCols + x;
   double v = 0.;
 #pragma unroll 8
-  for (int i = y; i < n_partials; i += 32) v += double(partials[int64_t(i) * 2 * head_dim + col]);
+  for (int i = y; i < n_partials; i += 1024 / kGradCols) v += double(partials[int64_t(i) * 2 * head_dim + col]);
   sums[y][x] = v;
   __syncthreads();
+  for (int half = 1024 / kGradCols / 2; half > 0; half /= 2) {
+    if (y < half) sums[y][x] += sums[y + half][x];
+    __syncthreads();
+  }
   if (y != 0) return;
-  for (int i = 1; i < 32; ++i) v += sums[i][x];
   float* dw = col < head_dim ? dw0 : dw1;
-  if (dw) dw[col < head_dim ? col : col - head_dim] = float(v);
+  if (dw) dw[col < head_dim ? col : col - head_dim] = float(sums[0][x]);
 }
 
 // workgroups of four waves along the tokens, and groups of rows where there are few tokens
@@ -244,7 +257,7 @@ int32_t launch_norm_rope_backward(const RopeGeom& g, int dtype, const NormTensor
     if (const int32_t rc = finish_launch("norm_rope.hip"); rc != CA_OK) return rc;
   }
   float* const dw[2] = {q.x ? dq_weight : dk_weight, sides == 2 ? dk_weight : nullptr};
-  hipLaunchKernelGGL(norm_weight_grad_kernel, dim3(unsigned(2 * g.head_dim / 32)), dim3(1024), 0, s, a.partials, n_partials, g.head_dim, dw[0], dw[1]);
+  hipLaunchKernelGGL(norm_weight_grad_kernel, dim3(unsigned(2 * g.head_dim / kGradCols)), dim3(1024), 0, s, a.partials, n_partials, g.head_dim, dw[0], dw[1]);
   return finish_launch("norm_rope.hip");
 }
 

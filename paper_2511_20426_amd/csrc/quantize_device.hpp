@@ -16,25 +16,36 @@ __device__ __forceinline__ uint32_t magnitude(const float* x) {      // as bits:
 // A row's quotients: values and largest magnitude are brought near 1 by a power of two first where 127 x or the reciprocal would
 // leave the range of fp32.
 struct RowScale {
-  float by, most, inv;                            // most: the largest magnitude after that
+  float by127, most, inv;                         // most: the largest magnitude after that
   bool finite;
   __device__ __forceinline__ explicit RowScale(uint32_t bits) {
-    const float m = __uint_as_float(bits);
+    const float m = __uint_as_float(bits), by = m > 0x1p100f ? 0x1p-64f : (m < 0x1p-64f ? 0x1p80f : 1.f);
     finite = bits < 0x7f800000u;
-    by = m > 0x1p100f ? 0x1p-64f : (m < 0x1p-64f ? 0x1p80f : 1.f);
+    by127 = 127.f * by;
     most = m * by;
     inv = finite && bits != 0 ? 1.f / most : 0.f;
   }
+  // the code of x in the low eight bits: 1.5 2^23 is added, whose last place is 1, so that the sum's rounding is the code's
   template <typename T>
-  __device__ __forceinline__ int code(float x) const {
-    const float t = x * by * 127.f;
+  __device__ __forceinline__ uint32_t code(float x) const {
+    const float t = x * by127;
     float q = t * inv;
     q = fmaf(fmaf(-q, most, t), inv, q);
-    if (sizeof(T) == 4 && fabsf(fabsf(q - truncf(q)) - 0.5f) < 1e-4f) return int(rint(double(x * by) * 127. / double(most)));
-    return int(rintf(q));
+    if (sizeof(T) == 4 && fabsf(fabsf(q - truncf(q)) - 0.5f) < 1e-4f) q = float(rint(double(x) * double(by127) / double(most)));
+    return __float_as_uint(q + 12582912.f);
+  }
+  template <typename T>
+  __device__ __forceinline__ uint2 codes(const float* x) const {
+    uint32_t out[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const uint32_t lo = __builtin_amdgcn_perm(code<T>(x[4 * i + 1]), code<T>(x[4 * i]), 0x0c0c0400);
+      const uint32_t hi = __builtin_amdgcn_perm(code<T>(x[4 * i + 3]), code<T>(x[4 * i + 2]), 0x04000c0c);
+      out[i] = finite ? lo | hi : 0;
+    }
+    return uint2{out[0], out[1]};
   }
 };
-
 
 __device__ __forceinline__ float row_scale(uint32_t most) {
   return most < 0x7f800000u ? __uint_as_float(most) / 127.f : __uint_as_float(0x7fc00000u);
@@ -42,12 +53,6 @@ __device__ __forceinline__ float row_scale(uint32_t most) {
 
 // the codes of eight bf16 values
 __device__ __forceinline__ uint2 row_codes(const RowScale& s, const U4& v) {
-  const uint32_t in[4] = {v.x, v.y, v.z, v.w};
-  uint32_t out[2] = {0, 0};
-#pragma unroll
-  for (int j = 0; j < 8; ++j) {
-    const float x = j & 1 ? bf16_hi(in[j >> 1]) : bf16_lo(in[j >> 1]);
-    if (s.finite) out[j >> 2] |= uint32_t(uint8_t(s.code<uint16_t>(x))) << (8 * (j & 3));
-  }
-  return uint2{out[0], out[1]};
+  const float x[8] = {bf16_lo(v.x), bf16_hi(v.x), bf16_lo(v.y), bf16_hi(v.y), bf16_lo(v.z), bf16_hi(v.z), bf16_lo(v.w), bf16_hi(v.w)};
+  return s.codes<uint16_t>(x);
 }
