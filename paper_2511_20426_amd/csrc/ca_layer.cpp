@@ -1,6 +1,7 @@
 // C-ABI entry points of the operators around the attention of a layer (include/cascade_attn.h): argument checks and launches.
 // Every failing call returns before touching metadata or the GPU.
 #include <cmath>
+#include <cstdint>
 
 #include "ca_internal.hpp"
 
@@ -10,6 +11,9 @@ using ca::rope_geom;
 using ca::strides_ok;
 
 bool aligned16(const void* p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
+
+// frames are 32-bit numbers in the kernels
+bool frames_fit(int64_t first_frame, int64_t n_tokens) { return first_frame <= INT32_MAX && n_tokens <= INT32_MAX - first_frame; }
 
 bool eps_ok(float eps) { return eps >= 0.f && std::isfinite(eps); }
 
@@ -51,6 +55,7 @@ int32_t layer_qk_norm_rope(const ca_ctx* ctx, const ca_heads* q, const ca_heads*
                            float eps, const ca_heads* q_out, const ca_heads* k_out, int64_t n_tokens, int64_t first_frame, void* hip_stream) {
   if (!ctx || n_tokens < 0 || first_frame < 0 || !eps_ok(eps) || (!q && !k)) return CA_EINVAL;
   if (!ctx->pool) return CA_ENOPOOL;
+  if (!frames_fit(first_frame, n_tokens)) return CA_EUNSUPPORTED;
   if (n_tokens == 0) return CA_OK;
   const ca::CacheMeta& m = ctx->meta;
   ca::NormTensors tq, tk;
@@ -68,6 +73,7 @@ int32_t layer_qk_norm_rope_backward(const ca_ctx* ctx, const ca_heads* dq_out, c
   if (!ctx || n_tokens < 0 || first_frame < 0 || !eps_ok(eps) || (!q && !k)) return CA_EINVAL;
   if ((q && !dq_weight_dev) || (k && !dk_weight_dev) || !workspace_dev || !aligned16(workspace_dev)) return CA_EINVAL;
   if (!ctx->pool) return CA_ENOPOOL;
+  if (!frames_fit(first_frame, n_tokens)) return CA_EUNSUPPORTED;
   const ca::CacheMeta& m = ctx->meta;
   if (workspace_bytes < ca::norm_rope_backward_bytes(m.cfg().head_dim)) return CA_EINVAL;
   ca::NormTensors tq{}, tk{};
@@ -97,6 +103,7 @@ int32_t kv_cache_append_batch_norm(ca_ctx* ctx, int32_t n_blocks, const int64_t*
     if (int32_t rc = next.check_append(block_ids[i], &slots[i])) return rc;
     for (int j = 0; j < i; ++j)
       if (block_ids[j] == block_ids[i]) return CA_EINVAL;
+    if (block_ids[i] > INT32_MAX / c.frames_per_block - 1) return CA_EUNSUPPORTED;
     next.commit_append(slots[i], block_ids[i], timesteps[i], prompt_epoch);
     first_frame[i] = int64_t(c.frames_per_block) * block_ids[i];
     if (!k_dev[i] || !v_dev[i] || !strides_ok(c, k_dev[i], tok_stride, head_stride) || !strides_ok(c, v_dev[i], tok_stride, head_stride))

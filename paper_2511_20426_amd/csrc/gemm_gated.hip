@@ -1,5 +1,6 @@
 // H[M,F] = act(X Wg') * (X Wu') in bf16 with fp32 accumulation: both projections of a gated feed-forward block, the activation and
-// the product in one kernel.
+// the product in one kernel.  Bound by the matrix pipe as the linear maps are: 23400 x 13824 x 5120 4287 us = 1546 TFLOP/s, the activation's
+// part of a tile of 256 x 128 is about 1 us of 102.
 #include <hip/hip_runtime.h>
 
 #include <type_traits>
@@ -18,13 +19,20 @@ namespace {
 #include "gemm_op_tiles.hpp"
 #include "gemm_few.hpp"
 
+// Up to two tiles of 16 tokens the weights' way from memory is what counts (gemm_few.hpp).  Us, few tokens' kernel / the fastest tile, weights
+// in the caches: 23 x 2384 x 2560 9.9 / 10.8, 1 x 152 x 5120 11.9 / 17.5, 31 x 1608 x 2560 10.7 / 10.8; from memory 1 x 13824 x 5120
+// 52.5 / 54.3, 8 x 8816 x 3840 31.9 / 35.5.
 constexpr int kFewTokens = 32;
 
 using Tile64Tall = TileShape<64, 64, 4, 2, 6>;     // (a wave has two sub-tiles over the columns: gate and up)
 
-constexpr OpModel kModel[] = {{256, 256, 1, 1580, 985, 1240, 6120}, {192, 256, 1, 2530, 765, 975, 4240}, {128, 256, 1, 2720, 610, 755, 2770},
-                              {256, 128, 1, 0, 745, 835, 5100},     {128, 128, 1, 0, 450, 485, 2900},   {64, 64, 2, 0, 230, 360, 1725},
-                              {64, 64, 1, 0, 165, 165, 3000}};
+// Fitted to 85 products of up to 23400 rows, 13824 columns and k 5120 (64 x 64: two a CU, then one of eight waves); the pick is 0.6 % slower than
+// the fastest of the seven in the geometric mean, 12 % at the worst.  By tile in this order, us: 23400 x 13824 x 5120 4287 / 4728 / 5793 /
+// 6276 / 8090 / 11548 / -, 4680 x 4096 x 1536 99 / 103 / 103 / 123 / 139 / 181 / -, 300 x 4096 x 1536 31.8 / 25.5 / 20.7 / 23.9 / 14.6 /
+// 16.7 / -, 3974 x 728 x 128 10.6 / 8.9 / 7.6 / 8.5 / 9.6 / 9.7 / 14.7.
+constexpr OpModel kModel[] = {{256, 256, 1, 2780, 945, 1200, 5330}, {192, 256, 1, 3110, 755, 1000, 3750}, {128, 256, 1, 3010, 580, 735, 2715},
+                              {256, 128, 1, 0, 730, 835, 5310},     {128, 128, 1, 0, 430, 480, 2925},     {64, 64, 2, 0, 225, 355, 1680},
+                              {64, 64, 1, 0, 225, 195, 1795}};
 
 }  // namespace
 

@@ -1,4 +1,6 @@
 // Y[M,N] = (X[M,K] . W[N,K]') * scale of X's row * scale of W's row, X and W in 8 bits, whole sums in 32 bits, Y in bf16.
+// Large products are bound by the matrix pipe at the clock that the chip's power leaves it: 23400 x 15360 x 5120 1276 us = 2890 TOP/s where the
+// same tiles reach 1500 TFLOP/s in bf16 (stages of 128 bytes take as long, and hold twice as many k).
 #include <hip/hip_runtime.h>
 
 #include <type_traits>
@@ -17,11 +19,18 @@ namespace {
 #include "gemm_op_tiles.hpp"
 #include "gemm_few.hpp"
 
+// Up to two tiles of 16 tokens the weights' way from memory is what counts (gemm_few.hpp).  Us, few tokens' kernel / the fastest tile, weights
+// in the caches: 23 x 2552 x 2560 6.3 / 7.1, 2 x 232 x 3840 6.3 / 8.4, 24 x 4160 x 2048 6.7 / 6.3; from memory one token 15360 x 5120
+// 16.2 / 16.9, 5120 x 5120 9.3 / 12.4.
 constexpr int kFewTokens = 32;
 
-constexpr OpModel kModel[] = {{256, 256, 1, 1160, 960, 1310, 6070}, {192, 256, 1, 620, 775, 970, 5700}, {128, 256, 1, 2020, 570, 765, 3500},
-                              {256, 128, 1, 0, 725, 870, 5300},     {128, 128, 1, 0, 445, 470, 3700},   {64, 64, 2, 0, 275, 355, 2300},
-                              {64, 64, 1, 0, 165, 165, 3000}};
+// Fitted to 86 products of up to 23400 rows, 15360 columns and k 5120 (64 x 64: two a CU, then one of eight waves); the pick is 0.5 % slower than
+// the fastest of the seven in the geometric mean, 7 % at the worst.  By tile in this order, us: 23400 x 15360 x 5120 1276 / 1280 / 1528 / 1730
+// / 1939 / 2868 / -, 4680 x 4608 x 1536 40.5 / 34.5 / 38.0 / 45.3 / 51.2 / 68.1 / -, 1560 x 1536 x 1536 20.9 / 16.9 / 13.1 / 14.2 / 9.5 /
+// 11.6 / -, 13427 x 304 x 256 9.6 / 8.2 / 7.1 / 8.1 / 9.2 / 9.3 / -, 64 x 1448 x 640 12.9 / 10.5 / 8.9 / 9.4 / 6.8 / 6.4 / 6.8.
+constexpr OpModel kModel[] = {{256, 256, 1, 1980, 960, 1270, 5400}, {192, 256, 1, 2140, 770, 1010, 4460}, {128, 256, 1, 2340, 580, 745, 3350},
+                              {256, 128, 1, 0, 705, 840, 5650},     {128, 128, 1, 0, 455, 470, 3680},     {64, 64, 2, 0, 290, 370, 1990},
+                              {64, 64, 1, 0, 255, 190, 2000}};
 
 }  // namespace
 

@@ -558,6 +558,9 @@ def test_refusals():
         args = list(ok)
         args[i] = bad
         _refused(B.CA_EINVAL, ctx.layer_qk_norm_rope, *args)
+    for n, first in ((1 << 31, 0), (4, 1 << 31), (1 << 30, (1 << 30) + 8)):
+        _refused(B.CA_EUNSUPPORTED, ctx.layer_qk_norm_rope, *ok[:7], n, first)
+    _refused(B.CA_EUNSUPPORTED, ctx.kv_cache_append_batch_norm, [1 << 40], [0], 0, [4096], [4096], 256, 128, 16, 1e-6)
     _refused(B.CA_EINVAL, ctx.layer_qk_norm_rope, None, None, 0, 0, 1e-6, None, None, 4, 0)
     _refused(B.CA_EINVAL, ctx.layer_qk_norm_rope, None, t, 0, 16, 1e-6, t, t, 4, 0)
     need = ctx.layer_qk_norm_rope_workspace()
@@ -648,3 +651,83 @@ def test_refusals_of_the_torch_calls():
             bad()
     with pytest.raises(KeyError):
         R.gated_linear(x, m, m, "relu")
+
+
+# ------------------------------------------------------------------------------------------------ a layer of them
+
+def _in_8_bits(t):
+    """what the codes of t's rows stand for"""
+    most = t.abs().amax(1, keepdim=True)
+    return torch.round(t * 127 / torch.where(most > 0, most, 1.0)) * most / 127
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("activation", ["silu", "gelu"])
+def test_layer(activation):
+    """A layer's iteration against the same in 64 bits from its own 8-bit weights: two cached blocks, two in flight, an odd grid."""
+    from paper_2511_20426_amd.layer import CascadeLayer
+    gen, heads, grid, F, D = _gen(21), 2, (5, 7), 328, 128
+    width, L = heads * D, 105
+    pool = _pool(heads, D, grid)
+    ws = [_normal(gen, *s, scale=s[1] ** -0.5) for s in ((3 * width, width), (width, width), (F, width), (F, width), (width, F))]
+    norms = [_normal(gen, D) for _ in range(2)]
+    layer = CascadeLayer.from_weights(*ws, *norms, activation=activation)
+    cached = [(_normal(gen, L, heads, D), _normal(gen, L, heads, D)) for _ in range(2)]
+    for g, (k, v) in enumerate(cached):
+        pool.append(g, 0, 0, k, v)
+        pool.ctx.kv_cache_promote(g)
+    x = _normal(gen, 2 * L, width)
+    got = layer(pool, x, [2, 3], [500, 1000], mode=B.CA_BLOCK_CAUSAL).double().cpu()
+
+    wqkv, wo, wg, wu, wd = (w.double().cpu() for w in ws)
+    linear8 = lambda t, w: _in_8_bits(t) @ _in_8_bits(w).T  # noqa: E731
+    x = x.double().cpu()
+    qkv = linear8(x, wqkv).view(2 * L, 3, heads, D)
+    ang = _angles(D, grid, 6, 2 * L)
+    q, k = (_norm_rope(qkv[:, s], n.double().cpu(), 1e-6, ang).transpose(0, 1) for s, n in zip((0, 1), norms))
+    ks = torch.cat([_rotate(k_.double().cpu(), _angles(D, grid, 3 * g, L)).transpose(0, 1) for g, (k_, _) in enumerate(cached)] + [k], 1)
+    vs = torch.cat([v_.double().cpu().transpose(0, 1) for _, v_ in cached] + [qkv[:, 2].transpose(0, 1)], 1)
+    logits = q @ ks.transpose(1, 2) / D ** 0.5
+    logits[:, :L, 3 * L:] = -torch.inf             # the first block in flight does not see the second
+    o = (torch.softmax(logits, -1) @ vs).transpose(0, 1).reshape(2 * L, width)
+    y = x + linear8(o, wo)
+    ref = y + linear8(_act(y @ wg.T, activation) * (y @ wu.T), wd)
+    # roundings to bf16 on the way (2^-8 each, at most 8 of them between x and the result) and 8-bit codes that fall on the other side of a border
+    # for them (a step is 1/127 of a row's largest value, a few in a thousand of the codes): 2 % of the norm
+    assert (got - ref).norm() <= 2e-2 * ref.norm()
+
+
+@pytest.mark.gpu
+def test_feed_forward_training():
+    """Gradients of a step against 64 bits, and that steps lead down."""
+    from paper_2511_20426_amd.layer import feed_forward_step
+    gen = _gen(22)
+    M, K, F = 200, 128, 136 * 128 // 8
+    x, wg, wu, wd = _normal(gen, M, K), _normal(gen, F, K, scale=K ** -0.5), _normal(gen, F, K, scale=K ** -0.5), _normal(gen, K, F, scale=F ** -0.5)
+    target = _normal(gen, M, K)
+    leaves = [t.double().cpu().requires_grad_() for t in (wg, wu, wd, x)]
+    loss = ((_act(leaves[3] @ leaves[0].T, "silu") * (leaves[3] @ leaves[1].T) @ leaves[2].T - target.double().cpu()) ** 2).mean()
+    refs = torch.autograd.grad(loss, leaves)
+    got, grads = feed_forward_step(x, wg, wu, wd, target)
+    assert abs(got.item() - loss.item()) <= 2e-2 * loss.item()
+    for g, r in zip(grads, refs):                  # at most five bf16 roundings on the way to each: 5 * 2^-8
+        assert (g.double().cpu() - r).norm() <= 2e-2 * r.norm()
+    losses = [feed_forward_step(x, wg, wu, wd, target, lr=2.0)[0].item() for _ in range(8)]
+    assert losses[-1] < losses[0] - 1e-3
+
+
+def test_host_code_is_clean_under_asan_and_ubsan(tmp_path):
+    import os
+    import shutil
+    import subprocess
+    cxx = shutil.which("g++")
+    if cxx is None:
+        pytest.skip("no g++")
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    csrc, exe = os.path.join(root, "paper_2511_20426_amd", "csrc"), str(tmp_path / "layer_sanitize")
+    subprocess.run([cxx, "-std=c++17", "-O1", "-g", "-fsanitize=address,undefined", "-fno-sanitize-recover=all", "-static-libasan", "-static-libubsan",
+                    "-I", os.path.join(root, "include"), "-I", csrc, os.path.join(root, "tests", "layer_sanitize_driver.cpp")] +
+                   [os.path.join(csrc, f) for f in ("ca_layer.cpp", "ca_api.cpp", "ca_meta.cpp")] + ["-o", exe], check=True, capture_output=True, text=True)
+    r = subprocess.run([exe], capture_output=True, text=True, timeout=300, env=dict(os.environ, ASAN_OPTIONS="detect_leaks=1:abort_on_error=0",
+                                                                                 UBSAN_OPTIONS="print_stacktrace=1"))
+    assert r.returncode == 0 and "layer sanitizer driver: ok" in r.stdout, r.stdout + r.stderr
