@@ -177,7 +177,7 @@ inline void activation_factors(int activation, float* act0, float* act1) {
 // Where the backward pass of the gated projections keeps what it multiplies: offsets in bytes.
 struct GatedWorkspace {
   int64_t Mp, Fp;
-  size_t rows, cols, xt, wt, bytes;
+  size_t rows, cols, xt, wt, parts, bytes;
 };
 GatedWorkspace gated_workspace(int64_t M, int32_t F, int32_t K);
 int32_t launch_gated_backward(const void* dh, const void* x, const void* w_gate, const void* w_up, const float* saved, int activation,
@@ -193,7 +193,7 @@ struct KernelLds {
   const void* kernel;
   int bytes;
 };
-enum LdsSlot { kLdsAttn, kLdsAttnRope, kLdsGemm, kLdsGemmRows, kLdsGemmPublish, kLdsI8, kLdsGated, kLdsSlots };
+enum LdsSlot { kLdsAttn, kLdsAttnRope, kLdsGemm, kLdsGemmRows, kLdsGemmPublish, kLdsI8, kLdsGated, kLdsGatedBackward, kLdsSlots };
 int32_t ensure_dynamic_lds(const KernelLds* kernels, int n, LdsSlot slot);   // slot: which set of kernels
 int32_t finish_launch(const char* what);   // launchers end with this: CA_OK, or CA_EDEVICE after recording HIP's last error
 int32_t device_failure(const char* what, int hip_error);   // records the text, clears HIP's last error, returns CA_EDEVICE

@@ -32,6 +32,18 @@ constexpr OpModel kModel[] = {{256, 256, 1, 1980, 960, 1270, 5400}, {192, 256, 1
                               {256, 128, 1, 0, 705, 840, 5650},     {128, 128, 1, 0, 455, 470, 3680},     {64, 64, 2, 0, 290, 370, 1990},
                               {64, 64, 1, 0, 255, 190, 2000}};
 
+// one call of any size readies all kernels for stream capture
+int32_t i8_ready() {
+  const KernelLds kernels[] = {{reinterpret_cast<const void*>(gemm_op_rows_kernel<8, I8>), kOpRowsLds},
+                               {reinterpret_cast<const void*>(gemm_op_rows_kernel<6, I8>), kOpRowsLds},
+                               {reinterpret_cast<const void*>(gemm_op_rows_kernel<4, I8>), kOpRowsLds},
+                               {reinterpret_cast<const void*>(gemm_op_kernel<Tile256x128, I8>), Tile256x128::kLds},
+                               {reinterpret_cast<const void*>(gemm_op_kernel<Tile128, I8>), Tile128::kLds},
+                               {reinterpret_cast<const void*>(gemm_op_kernel<Tile64, I8>), Tile64::kLds},
+                               {reinterpret_cast<const void*>(gemm_op_kernel<Tile64Wide, I8>), Tile64Wide::kLds}};
+  return ensure_dynamic_lds(kernels, 7, kLdsI8);
+}
+
 }  // namespace
 
 int32_t launch_gemm_i8(const void* x, const float* x_scales, const void* w, const float* w_scales, void* y, int64_t M, int32_t N, int32_t K,
@@ -42,14 +54,7 @@ int32_t launch_gemm_i8(const void* x, const float* x_scales, const void* w, cons
   a.ldy = ldy;
   a.M = int32_t(M); a.N = N; a.K = (K + 255) / 256 * 256;
   a.ldx = int32_t(ldx); a.ldw = int32_t(ldw);
-  const KernelLds kernels[] = {{reinterpret_cast<const void*>(gemm_op_rows_kernel<8, I8>), kOpRowsLds},
-                               {reinterpret_cast<const void*>(gemm_op_rows_kernel<6, I8>), kOpRowsLds},
-                               {reinterpret_cast<const void*>(gemm_op_rows_kernel<4, I8>), kOpRowsLds},
-                               {reinterpret_cast<const void*>(gemm_op_kernel<Tile256x128, I8>), Tile256x128::kLds},
-                               {reinterpret_cast<const void*>(gemm_op_kernel<Tile128, I8>), Tile128::kLds},
-                               {reinterpret_cast<const void*>(gemm_op_kernel<Tile64, I8>), Tile64::kLds},
-                               {reinterpret_cast<const void*>(gemm_op_kernel<Tile64Wide, I8>), Tile64Wide::kLds}};
-  if (const int32_t rc = ensure_dynamic_lds(kernels, 7, kLdsI8); rc != CA_OK) return rc;
+  if (const int32_t rc = i8_ready(); rc != CA_OK) return rc;
   int n_cu = 0;
   if (const int32_t rc = device_cu_count(&n_cu); rc != CA_OK) return rc;
   constexpr const char* kWhat = "gemm_i8.hip";
@@ -68,6 +73,7 @@ int32_t launch_gemm_i8(const void* x, const float* x_scales, const void* w, cons
 int32_t launch_gemm_i8_values(int dtype, const void* x, int64_t ldx, const void* w, const float* w_scales, void* y, int64_t M, int32_t N, int32_t K,
                               int64_t ldw, int64_t ldy, void* workspace, void* stream) {
   if (M == 0) return CA_OK;
+  if (const int32_t rc = i8_ready(); rc != CA_OK) return rc;
   // Up to kCodeRows tokens go in one launch, unless making the codes in every workgroup costs more than the launch that it saves.  Us with
   // codes made in the launch / ahead, weights from memory: one token 15360 x 5120 20.3 / 20.8, 5120 x 5120 11.0 / 13.5, 4608 x 1536 8.8 /
   // 10.8; two 22.5 / 21.2, 11.7 / 13.9, 8.8 / 10.6; four 26.5 / 22.4, 14.3 / 14.2, 8.9 / 10.6.

@@ -45,9 +45,25 @@ __global__ __launch_bounds__(T::kThreads) void gemm_op_kernel(OpArgs a) {
   }
   uint64_t base_w = reinterpret_cast<uint64_t>(wbase + int64_t(n0) * ldw);
   uint64_t base_x = reinterpret_cast<uint64_t>(static_cast<const uint8_t*>(a.x) + int64_t(m0) * a.ldx);
-  const int n_stages = a.K / 128;
+  int n_stages = a.K / 128;
+  if constexpr (Op::kPart) {                                        // grid.y: the part
+    const int begin = int(blockIdx.y) * a.k_values;
+    base_w += uint64_t(begin) * 128;
+    base_x += uint64_t(begin) * 128;
+    n_stages = min(a.k_values, n_stages - begin);
+  }
 #include "gemm_tile_loop.hpp"
 
+  if constexpr (Op::kPart) {                                        // straight from registers, 16 bytes to a lane
+#pragma unroll
+    for (int i = 0; i < T::kTn; ++i)
+#pragma unroll
+      for (int j = 0; j < T::kTm; ++j) {
+        const int row = m0 + (wm * T::kTm + j) * 16 + l15, col = n0 + (wn * T::kTn + i) * 16 + 4 * grp;
+        if (row < a.M && col < a.N) *reinterpret_cast<f32x4*>(a.g + (int64_t(blockIdx.y) * a.M + row) * a.N + col) = acc[i][j];
+      }
+    return;
+  }
   // ---- the results go through LDS to leave row by row.  A lane has columns 4 grp .. +3 of row l15 of a sub-tile.
   constexpr int kPitch = kCols * 2 + 16;
   if constexpr (Op::kGated) {
@@ -100,13 +116,13 @@ __global__ __launch_bounds__(T::kThreads) void gemm_op_kernel(OpArgs a) {
 }
 
 template <typename T, typename Op>
-int32_t enqueue_op_tile(OpArgs& a, const char* what, void* stream) {
+int32_t enqueue_op_tile(OpArgs& a, const char* what, void* stream, unsigned parts = 1) {
   constexpr int kCols = Op::kGated ? T::kBn / 2 : T::kBn;
   a.tiles_m = (a.M + T::kBm - 1) / T::kBm;
   a.tiles_n = (a.N + kCols - 1) / kCols;
   const int64_t tiles = int64_t(a.tiles_m) * a.tiles_n;
-  if ((tiles + 7) * T::kThreads >= (int64_t(1) << 32)) return CA_EUNSUPPORTED;      // a launch may have 2^32 threads
+  if ((tiles + 7) * T::kThreads * parts >= (int64_t(1) << 32)) return CA_EUNSUPPORTED;      // a launch may have 2^32 threads
   a.more = int32_t((tiles + 7) / 8);
-  hipLaunchKernelGGL((gemm_op_kernel<T, Op>), dim3(unsigned(a.more) * 8), dim3(T::kThreads), T::kLds, static_cast<hipStream_t>(stream), a);
+  hipLaunchKernelGGL((gemm_op_kernel<T, Op>), dim3(unsigned(a.more) * 8, parts), dim3(T::kThreads), T::kLds, static_cast<hipStream_t>(stream), a);
   return finish_launch(what);
 }

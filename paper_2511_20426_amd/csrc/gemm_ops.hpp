@@ -15,7 +15,7 @@ struct OpArgs {
   int64_t ldy;                                    // in elements
   int32_t M, N, K, ldx, ldw, ldw2;                // K in bytes of a row: a multiple of 256
   int32_t tiles_m, tiles_n, more;                 // as in LinearArgs
-  int32_t k_values;                               // 8 bits of values that are made codes on the way: values of a row
+  int32_t k_values;                               // 8 bits of values that are made codes on the way: values of a row; in parts: stages of one
   float act0, act1;                               // gated: act(g) = g sigmoid(g (act0 + act1 g^2))
 };
 
@@ -39,11 +39,15 @@ struct I8 {
       return __builtin_amdgcn_mfma_i32_16x16x64_i8(w, x, c, 0, 0, 0);
     }
   };
-  static constexpr bool kGated = false;
+  static constexpr bool kGated = false, kPart = false;
 };
 struct Gated {
   using Products = Bf16Products;
-  static constexpr bool kGated = true;
+  static constexpr bool kGated = true, kPart = false;
+};
+struct PlainPart {                                // sums of a part of k, in fp32, to g [part][M][N]
+  using Products = Bf16Products;
+  static constexpr bool kGated = false, kPart = true;
 };
 
 // Where four values of a projection from column n (a multiple of four) of row m on lie among the saved ones of N columns: in blocks of 16

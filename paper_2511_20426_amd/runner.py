@@ -333,8 +333,11 @@ class QuantizedRows:
     def from_codes(cls, codes: torch.Tensor, scales: torch.Tensor) -> "QuantizedRows":
         """From codes [rows, k] and scales [rows] made elsewhere (a checkpoint's)."""
         rows, k = codes.shape
-        whole = torch.zeros((rows, -(-k // 256) * 256), dtype=torch.int8, device=codes.device)
-        whole[:, :k] = codes
+        if k % 256 == 0 and codes.dtype == torch.int8 and codes.stride(1) == 1 and codes.stride(0) % 16 == 0 and codes.data_ptr() % 16 == 0:
+            whole = codes                          # as they are
+        else:
+            whole = torch.zeros((rows, -(-k // 256) * 256), dtype=torch.int8, device=codes.device)
+            whole[:, :k] = codes
         return cls(whole, scales.to(torch.float32).contiguous(), k)
 
 

@@ -396,7 +396,7 @@ def _gated_grads(x, wg, wu, dh, act):
     return out
 
 
-GRADS = [(1, 8, 128), (5, 72, 256), (64, 64, 128), (127, 136, 384), (128, 200, 128), (130, 1000, 640), (1000, 328, 256), (2345, 776, 384)]
+GRADS = [(1, 8, 128), (4, 1000, 640), (5, 72, 256), (8, 520, 128), (9, 64, 384), (16, 2056, 256), (17, 40, 128), (64, 64, 128), (127, 136, 384), (128, 200, 128), (130, 1000, 640), (1000, 328, 256), (2345, 776, 384)]
 
 
 @pytest.mark.gpu
@@ -421,6 +421,29 @@ def test_gated_backward(M, F, K, act):
         loss = lambda p: (dhd * _act(p[0] @ p[1].T, act) * (p[0] @ p[2].T)).sum()  # noqa: E731
         along = (loss(at(1)) - loss(at(-1))) / (2 * step)
         assert abs(along - (ref * move).sum()) <= 1e-6 * (ref * move).abs().sum() + 1e-6
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("M", [3, 100])
+def test_gradients_that_are_asked_for(M):
+    """Each of the three alone, and weights' gradients that do not lie one behind the other: the bits of all three together; what is not asked
+    for is not written."""
+    from paper_2511_20426_amd.runner import gated_linear_backward, gated_linear_train
+    gen, F, K = _gen(M), 72, 256
+    x, wg, wu, dh = _normal(gen, M, K), _normal(gen, F, K), _normal(gen, F, K), _normal(gen, M, F)
+    _, saved = gated_linear_train(x, wg, wu)
+    whole = gated_linear_backward(dh, x, wg, wu, saved)
+    nbytes = B.layer_gated_backward_workspace(M, F, K)
+    work = torch.empty(nbytes, dtype=torch.uint8, device=DEV)
+    for asked in ((1, 0, 0), (0, 1, 0), (0, 0, 1), (0, 1, 1), (1, 1, 1)):
+        out = [torch.full((n + 2, K + 8), 7.0, dtype=torch.bfloat16, device=DEV) for n in (M, F, F)]
+        B.layer_gated_backward_bf16(dh.data_ptr(), x.data_ptr(), wg.data_ptr(), wu.data_ptr(), saved.data_ptr(), B.CA_SILU,
+                                    *(t.data_ptr() if a else 0 for t, a in zip(out, asked)), M, F, K, F, K, K, K, K + 8, K + 8, work.data_ptr(), nbytes,
+                                    torch.cuda.current_stream().cuda_stream)
+        for t, ref, a in zip(out, whole, asked):
+            n = ref.shape[0]
+            assert (t[:n, :K] == ref).all() if a else (t[:n, :K] == 7).all()
+            assert (t[n:] == 7).all() and (t[:, K:] == 7).all()
 
 
 @pytest.mark.gpu
