@@ -304,8 +304,8 @@ int32_t layer_quantize_rows_i8(const void* x_dev, int32_t dtype, int8_t* codes_d
                                int64_t ldx, int64_t ld_codes, void* hip_stream);
 
 /* The linear map in 8 bits: y[m][n] = (sum_k x_codes[m][k] * w_codes[n][k]) * x_scales[m] * w_scales[n], whole sums in 32 bits, scaled in
- * fp32, rounded to bf16 once.  Codes as layer_quantize_rows_i8 leaves them (zeros behind k_in), weights with a scale for each output
- * channel.  n_out a multiple of 8 (ldy too, in elements; ldx and ldw in bytes); m_rows and k_in <= CA_I8_MAX_K are free.  The
+ * fp32, rounded to bf16 once.  Codes as layer_quantize_rows_i8 leaves them (-127 .. 127, zeros behind k_in), weights with a scale for each
+ * output channel.  n_out a multiple of 8 (ldy too, in elements; ldx and ldw in bytes); m_rows and k_in <= CA_I8_MAX_K are free.  The
  * result does not depend on the size of the call's tiles. */
 int32_t layer_linear_i8(const int8_t* x_codes_dev, const float* x_scales_dev, const int8_t* w_codes_dev, const float* w_scales_dev,
                         void* y_dev, int64_t m_rows, int32_t n_out, int32_t k_in, int64_t ldx, int64_t ldw, int64_t ldy,
