@@ -47,6 +47,12 @@ int32_t check_gated(int32_t activation, int64_t m_rows, int32_t n_hidden, int32_
   return CA_OK;
 }
 
+// rows and twice the columns, in whole steps, are row strides of the backward pass's products
+int32_t check_gated_backward(int64_t m_rows, int32_t n_hidden, int32_t k_in) {
+  if (int32_t rc = check_gated(CA_SILU, m_rows, n_hidden, k_in)) return rc;
+  return m_rows > kMaxLd - 256 || n_hidden > kMaxLd / 2 - 64 || k_in >= kMaxLd ? CA_EUNSUPPORTED : CA_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -186,7 +192,7 @@ size_t layer_gated_saved_bytes(int64_t m_rows, int32_t n_hidden) {
 }
 
 size_t layer_gated_backward_workspace(int64_t m_rows, int32_t n_hidden, int32_t k_in) {
-  return check_gated(CA_SILU, m_rows, n_hidden, k_in) ? 0 : ca::gated_workspace(m_rows, n_hidden, k_in).bytes;
+  return check_gated_backward(m_rows, n_hidden, k_in) ? 0 : ca::gated_workspace(m_rows, n_hidden, k_in).bytes;
 }
 
 int32_t layer_gated_backward_bf16(const void* dh_dev, const void* x_dev, const void* w_gate_dev, const void* w_up_dev, const float* saved_dev,
@@ -197,9 +203,8 @@ int32_t layer_gated_backward_bf16(const void* dh_dev, const void* x_dev, const v
   for (int64_t ld : {ldx, ldw_gate, ldw_up, lddx, lddw})
     if (int32_t rc = check_ld(ld, k_in)) return rc;
   if (int32_t rc = check_ld(lddh, n_hidden)) return rc;
-  const ca::GatedWorkspace at = ca::gated_workspace(m_rows, n_hidden, k_in);
-  if (at.Mp >= kMaxLd - 128 || 2 * at.Fp >= kMaxLd) return CA_EUNSUPPORTED;      // (they are row strides of products)
-  if (!workspace_dev || !aligned16(workspace_dev) || workspace_bytes < at.bytes) return CA_EINVAL;
+  if (int32_t rc = check_gated_backward(m_rows, n_hidden, k_in)) return rc;
+  if (!workspace_dev || !aligned16(workspace_dev) || workspace_bytes < ca::gated_workspace(m_rows, n_hidden, k_in).bytes) return CA_EINVAL;
   if (m_rows > 0)
     for (const void* p : {dh_dev, x_dev, static_cast<const void*>(saved_dev)})
       if (!p) return CA_EINVAL;

@@ -641,6 +641,17 @@ def test_refusals():
     _refused(E, B.layer_gated_backward_bf16, *ok[:6], 0, 0, 0, *ok[9:])
 
 
+def test_workspaces_of_refused_shapes():
+    """The backward pass's workspace is 0 bytes for shapes that the call refuses, those whose row strides are too long among them."""
+    most = (1 << 22) - 256
+    assert B.layer_gated_backward_workspace(most, 16, 128) > 0
+    for m, f, k in ((most + 1, 16, 128), (1 << 30, 16, 128), (5, (1 << 21) - 56, 128), (1 << 30, 2**31 - 8, 128), (5, 16, 1 << 22)):
+        assert B.layer_gated_backward_workspace(m, f, k) == 0
+        ldf, ldk = -(-f // 8) * 8, k
+        code = B.CA_EUNSUPPORTED
+        _refused(code, B.layer_gated_backward_bf16, *[4096] * 5, B.CA_SILU, *[4096] * 3, m, f, k, ldf, ldk, ldk, ldk, ldk, ldk, 4096, 1 << 62)
+
+
 @pytest.mark.parametrize("host", [b"bytes of the host", (C.c_char * 64)(), 16.0, np.int64(16)], ids=["bytes", "array", "float", "numpy"])
 def test_addresses_are_integers(host):
     calls = [(B.layer_quantize_rows_i8, [16, 1, 16, 16, 0, 8, 8, 256], (0, 2, 3)), (B.layer_linear_i8, [16] * 5 + [0, 8, 8, 256, 256, 8], range(5)),
