@@ -80,7 +80,7 @@ struct GatedGradArgs {
   float act0, act1;
 };
 
-// act and act' of a gate: act' = s + g s (1 - s) p'(g), p = g (act0 + act1 g^2)
+// act and act' of a gate: act' = s + g s (1 - s) p'(g), p = g (act0 + act1 g^2).
 __device__ __forceinline__ void activation(float g, float act0, float act1, float* act, float* slope) {
   float p;
   const float s = act_sigmoid(g, act0, act1, &p), c = __builtin_amdgcn_fmed3f(g, -1e4f, 1e4f);
@@ -354,7 +354,7 @@ int32_t launch_gated_backward(const void* dh, const void* x, const void* w_gate,
   a.t[2] = TransposeArgs{static_cast<const uint16_t*>(x), xt, ldx, at.Mp, int32_t(M), K};
   const int64_t grad = int64_t(Fp / kSide) * (Mp / kSide), of_w = dx ? int64_t(K / kSide) * (Fp / kSide) : 0;
   const int64_t of_x = dw_gate || dw_up ? int64_t(K / kSide) * (Mp / kSide) : 0;
-  if (grad + 2 * of_w + of_x > (1 << 24)) return CA_EUNSUPPORTED;      // (a launch may have 2^32 threads)
+  if (grad + 2 * of_w + of_x >= (1 << 24)) return CA_EUNSUPPORTED;      // (a launch has fewer than 2^32 threads)
   a.grad_tiles = int32_t(grad);
   a.ends[0] = int32_t(grad + of_w);
   a.ends[1] = int32_t(grad + 2 * of_w);

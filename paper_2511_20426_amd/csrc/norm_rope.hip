@@ -230,7 +230,7 @@ int32_t launch_norm_rope(const RopeGeom& g, int dtype, const NormTensors& q, con
   NormArgs a{};
   if (norm_sides(g, q, k, n_tokens, first_frame, eps, &a) == 0) return CA_EINVAL;
   const int64_t gx = (n_tokens + 3) / 4;
-  if (gx > (1 << 24)) return CA_EUNSUPPORTED;      // (a launch may have 2^32 threads)
+  if (gx >= (1 << 24)) return CA_EUNSUPPORTED;     // (a launch has fewer than 2^32 threads)
   const NormGrid grid = norm_grid(gx, a.rows, g.head_dim, 2048);
   a.rows_per_group = grid.rows_per_group;
   const auto kernel = dtype == CA_BF16 ? norm_rope_kernel<uint16_t> : norm_rope_kernel<float>;

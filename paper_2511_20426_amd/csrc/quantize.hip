@@ -89,10 +89,10 @@ int32_t enqueue_quantize(const QuantizeArgs& a, void* stream) {
   // (5.5 TB/s), 95 by waves that read most of a row twice.
   if (a.rows >= 1024 && a.k <= 8 * 64 * 4) {
     const int64_t groups = (a.rows + 3) / 4;
-    if (groups > (1 << 24)) return CA_EUNSUPPORTED;
+    if (groups >= (1 << 24)) return CA_EUNSUPPORTED;
     hipLaunchKernelGGL((quantize_rows_kernel<T, 64, 4>), dim3(unsigned(groups)), dim3(256), 0, s, a);
   } else {
-    if (a.rows > (1 << 24)) return CA_EUNSUPPORTED;       // (a launch may have 2^32 threads)
+    if (a.rows >= (1 << 24)) return CA_EUNSUPPORTED;      // (a launch has fewer than 2^32 threads)
     if (a.k <= 8 * 256 * 4)
       hipLaunchKernelGGL((quantize_rows_kernel<T, 256, 4>), dim3(unsigned(a.rows)), dim3(256), 0, s, a);
     else

@@ -652,6 +652,16 @@ def test_workspaces_of_refused_shapes():
         _refused(code, B.layer_gated_backward_bf16, *[4096] * 5, B.CA_SILU, *[4096] * 3, m, f, k, ldf, ldk, ldk, ldk, ldk, ldk, 4096, 1 << 62)
 
 
+def test_launches_that_are_too_large_are_refused():
+    """Sizes whose launch would have 2^32 threads."""
+    cfg = B.make_config(heads=2, head_dim=128, frames_per_block=3, grid_h=4, grid_w=5, rope_dims=ROPE[128], rope_theta=1e4, sink_blocks=0,
+                        window_blocks=2, max_inflight=2, page_tokens=128, dtype="bf16")
+    ctx, t = B.Context(cfg, 1 << 40, B.pool_bytes(cfg)), (4096, 256, 128)
+    _refused(B.CA_EUNSUPPORTED, ctx.layer_qk_norm_rope, t, t, 16, 16, 1e-6, t, t, 1 << 26, 0)
+    for rows, k in ((1 << 24, 4096), (1 << 26, 8)):
+        _refused(B.CA_EUNSUPPORTED, B.layer_quantize_rows_i8, 4096, B.CA_BF16, 4096, 4096, rows, k, k, -(-k // 256) * 256)
+
+
 @pytest.mark.parametrize("host", [b"bytes of the host", (C.c_char * 64)(), 16.0, np.int64(16)], ids=["bytes", "array", "float", "numpy"])
 def test_addresses_are_integers(host):
     calls = [(B.layer_quantize_rows_i8, [16, 1, 16, 16, 0, 8, 8, 256], (0, 2, 3)), (B.layer_linear_i8, [16] * 5 + [0, 8, 8, 256, 256, 8], range(5)),
