@@ -141,6 +141,8 @@ int32_t run_mfma_microbench(int data_kind, int trips, void* scratch, size_t scra
                             double* tflops, double* clock_ghz);
 int32_t launch_gemm_bf16(const void* x, const void* w, void* y, int64_t M, int32_t N, int32_t K,
                          int64_t ldx, int64_t ldw, int64_t ldy, void* stream);
+// What it costs by the model that picks its tile, in nanoseconds
+int64_t gemm_bf16_cost(int64_t M, int32_t N, int32_t K, int n_cu);
 // The same in tiles of tile_rows (256, 192 or 128) x 256, a workgroup taking several one after the other; gemm_rows_ready
 // readies its kernels for stream capture.
 int32_t launch_gemm_rows(int tile_rows, const void* x, const void* w, void* y, int32_t M, int32_t N, int32_t K,

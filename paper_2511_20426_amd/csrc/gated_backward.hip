@@ -80,12 +80,12 @@ struct GatedGradArgs {
   float act0, act1;
 };
 
-// act and act' of a gate: act' = s + g s (1 - s) p'(g), p = g (act0 + act1 g^2).
+// act and act' of a gate: act' = s + g s (1 - s) p'(g), p = g (act0 + act1 g^2).  (The bound on g for p would make a number of a NaN.)
 __device__ __forceinline__ void activation(float g, float act0, float act1, float* act, float* slope) {
   float p;
   const float s = act_sigmoid(g, act0, act1, &p), c = __builtin_amdgcn_fmed3f(g, -1e4f, 1e4f);
   *act = g * s;
-  *slope = fmaf(c * s * (1.f - s), fmaf(c * c, 3.f * act1, act0), s);
+  *slope = g == g ? fmaf(c * s * (1.f - s), fmaf(c * c, 3.f * act1, act0), s) : g;
 }
 
 __device__ __forceinline__ void gated_grad_tile(const GatedGradArgs& a, uint32_t (*tile)[kSide * kRow], int nth) {
@@ -251,18 +251,14 @@ __global__ __launch_bounds__(256) void gated_few_grad_kernel(GatedFewArgs a) {
   }
 }
 
-// dX from the sums of its parts
-__global__ __launch_bounds__(256) void gated_sum_kernel(const float* partials, int parts, int M, int K, uint16_t* dx, int64_t lddx) {
-  const int i = (blockIdx.x * 256 + threadIdx.x) * 2;
-  if (i >= M * K) return;
-  float v[2] = {0.f, 0.f};
+// A product from the sums of its parts, four columns to a thread (N is a multiple of 128)
+__global__ __launch_bounds__(256) void gated_sum_kernel(const float* partials, int parts, int M, int N, uint16_t* y, int64_t ldy) {
+  const int i = (blockIdx.x * 256 + threadIdx.x) * 4;
+  if (i >= M * N) return;
+  f32x4 v = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 8
-  for (int p = 0; p < parts; ++p) {
-    const float2 s = *reinterpret_cast<const float2*>(partials + int64_t(p) * M * K + i);
-    v[0] += s.x;
-    v[1] += s.y;
-  }
-  *reinterpret_cast<uint32_t*>(dx + int64_t(i / K) * lddx + i % K) = pack_bf16(v[0], v[1]);
+  for (int p = 0; p < parts; ++p) v += *reinterpret_cast<const f32x4*>(partials + int64_t(p) * M * N + i);
+  *reinterpret_cast<uint2*>(y + int64_t(i / N) * ldy + i % N) = uint2{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
 }
 
 constexpr int kFewGradRows = 8, kFewGradMost = 512;       // rows; columns f of a workgroup
@@ -273,9 +269,9 @@ int few_grad_each(int32_t F, int32_t K) {
   return int(each < 64 ? 64 : (each > kFewGradMost ? kFewGradMost : each));
 }
 
-int32_t sum_parts(const float* partials, int parts, int64_t M, int32_t K, void* dx, int64_t lddx, void* stream) {
-  hipLaunchKernelGGL(gated_sum_kernel, dim3(unsigned((M * K / 2 + 255) / 256)), dim3(256), 0, static_cast<hipStream_t>(stream), partials, parts, int(M), K,
-                     static_cast<uint16_t*>(dx), lddx);
+int32_t sum_parts(const float* partials, int parts, int64_t M, int32_t N, void* y, int64_t ldy, void* stream) {
+  hipLaunchKernelGGL(gated_sum_kernel, dim3(unsigned((M * N / 4 + 255) / 256)), dim3(256), 0, static_cast<hipStream_t>(stream), partials, parts, int(M), N,
+                     static_cast<uint16_t*>(y), ldy);
   return finish_launch("gated_backward.hip");
 }
 
@@ -293,13 +289,49 @@ int32_t launch_few_grad(GatedFewArgs a, void* dx, int64_t lddx, void* stream) {
   return sum_parts(a.partials, int(parts), a.M, a.K, dx, lddx, stream);
 }
 
-// Parts that dX's walk over 2 Fp is cut into, where its tiles of 64 x 64 are few and the walk is long: enough for one round of the CUs,
-// each of eight stages or more.  Us of the whole backward pass, whole / in parts: 17 x 7664 x 640 65.3 / 32.8, 32 x 4096 x 1536 48.6 / 33.7, 300 x
-// 4096 x 1536 56.9 / 49.8, 16 x 13824 x 5120 443 / 243.
-int x_parts(int64_t M, int32_t F, int32_t K) {
-  const int64_t tiles = ((M + 63) / 64) * (K / 64), stages = (int64_t(F) + 63) / 64 * 2;
-  if (tiles > 128 || stages < 32) return 1;
-  return int(std::min(256 / tiles, stages / 8));
+// How a product of M x N over `stages` of 64 is taken: whole by the linear map (parts 1), or in tiles of 64 x 64 with its walk in parts
+struct Walk {
+  int parts, stages;                              // of a part
+};
+
+// Of few tiles and a long walk the chip is filled by parts of it, whose sums a second launch adds up: the cheapest by the linear map's
+// model and, for parts, by rounds of workgroups over the CUs, the second launch and the sums' way through the caches, in nanoseconds fitted
+// to 36 products in up to 32 parts (the pick is 0.5 % behind the fastest in the geometric mean, 6 % at the worst).  Us of the backward pass of
+// dX alone, whole / in parts: 17 x 7664 x 640 59.1 / 23.7, 300 x 4096 x 1536 44.5 / 36.3, 64 x 13824 x 5120 260 / 178, 500 x 1000 x 2048 20.9 / 25.7
+// (whole); of the weights' 7776 x 128 x 640 35.8 / 24.0, 3325 x 168 x 2048 25.7 / 29.3 (whole).
+Walk walk_of(int64_t M, int32_t N, int64_t stages) {
+  constexpr int kCu = 256, kStage = 110, kTileEnd = 2900, kSecond = 7000, kValues = 156;       // kValues: of a part a nanosecond
+  Walk best{1, int(stages)};
+  if (M == 0 || M * N > (int64_t(1) << 26)) return best;
+  int64_t least = gemm_bf16_cost(M, N, int32_t(64 * stages), kCu);
+  const int64_t tiles = ((M + 63) / 64) * (N / 64);
+  for (int64_t cut = 2; cut <= 32 && cut * 4 <= stages; ++cut) {
+    const int64_t each = (stages + cut - 1) / cut, parts = (stages + each - 1) / each, rounds = (tiles * parts + kCu - 1) / kCu;
+    const int64_t cost = rounds * (each * kStage + kTileEnd) + kSecond + parts * M * N / kValues;
+    if (cost < least) {
+      least = cost;
+      best = Walk{int(parts), int(each)};
+    }
+  }
+  return best;
+}
+
+size_t walk_bytes(int64_t M, int32_t N, int64_t stages) {
+  const Walk w = walk_of(M, N, stages);
+  return w.parts > 1 ? size_t(w.parts) * M * N * 4 : 0;
+}
+
+// y[M][N] = x w', rows of k = 64 stages
+int32_t product(const uint16_t* x, const uint16_t* w, void* y, int64_t M, int32_t N, int64_t k, int64_t ldy, float* partials, void* stream) {
+  const Walk walk = walk_of(M, N, k / 64);
+  if (walk.parts == 1) return launch_gemm_bf16(x, w, y, M, N, int32_t(k), k, k, ldy, stream);
+  OpArgs a{};
+  a.x = x; a.w = w; a.g = partials;
+  a.M = int32_t(M); a.N = N; a.K = int32_t(2 * k);
+  a.ldx = a.ldw = a.K;
+  a.k_values = walk.stages;
+  const int32_t rc = enqueue_op_tile<Tile64Wide, PlainPart>(a, "gated_backward.hip", stream, unsigned(walk.parts));
+  return rc != CA_OK ? rc : sum_parts(partials, walk.parts, M, N, y, ldy, stream);
 }
 
 }  // namespace
@@ -319,8 +351,9 @@ GatedWorkspace gated_workspace(int64_t M, int32_t F, int32_t K) {
   w.xt = w.cols + whole(2 * int64_t(F) * w.Mp);
   w.wt = w.xt + whole(K * w.Mp);
   w.parts = w.wt + whole(K * 2 * w.Fp);
-  const int parts = x_parts(M, F, K);
-  w.bytes = w.parts + (parts > 1 ? whole(2 * parts * M * K) : 0);
+  size_t parts = walk_bytes(M, K, 2 * w.Fp / 64);
+  for (int64_t rows : {int64_t(F), 2 * int64_t(F)}) parts = std::max(parts, walk_bytes(rows, K, w.Mp / 64));      // dWg, dWu on their own or as one
+  w.bytes = w.parts + parts;
   return w;
 }
 
@@ -361,26 +394,15 @@ int32_t launch_gated_backward(const void* dh, const void* x, const void* w_gate,
   a.ends[2] = int32_t(grad + 2 * of_w + of_x);
   hipLaunchKernelGGL(gated_layout_kernel, dim3(unsigned(a.ends[2])), dim3(256), 0, static_cast<hipStream_t>(stream), a);
   if (const int32_t rc = finish_launch("gated_backward.hip"); rc != CA_OK) return rc;
-  if (const int parts = dx ? x_parts(M, F, K) : 0; parts > 1) {
-    OpArgs p{};
-    p.x = rows; p.w = wt; p.g = reinterpret_cast<float*>(ws + at.parts);
-    p.M = int32_t(M); p.N = K; p.K = 4 * Fp;
-    p.ldx = p.ldw = 4 * Fp;
-    p.k_values = (2 * Fp / 64 + parts - 1) / parts;
-    const unsigned n = unsigned((2 * Fp / 64 + p.k_values - 1) / p.k_values);
-    if (const int32_t rc = enqueue_op_tile<Tile64Wide, PlainPart>(p, "gated_backward.hip", stream, n); rc != CA_OK) return rc;
-    if (const int32_t rc = sum_parts(p.g, int(n), M, K, dx, lddx, stream); rc != CA_OK) return rc;
-  } else if (dx) {
-    if (const int32_t rc = launch_gemm_bf16(rows, wt, dx, M, K, 2 * Fp, 2 * at.Fp, 2 * at.Fp, lddx, stream); rc != CA_OK) return rc;
-  }
+  float* const partials = reinterpret_cast<float*>(ws + at.parts);
+  if (dx)
+    if (const int32_t rc = product(rows, wt, dx, M, K, 2 * at.Fp, lddx, partials, stream); rc != CA_OK) return rc;
   // the weights' gradients in one product where they follow one another
   const bool one = dw_gate && dw_up && static_cast<uint8_t*>(dw_up) == static_cast<uint8_t*>(dw_gate) + int64_t(F) * lddw * 2;
   for (int side = 0; side < (one ? 1 : 2); ++side) {
     void* const dw = side ? dw_up : dw_gate;
     if (!dw) continue;
-    if (const int32_t rc = launch_gemm_bf16(cols + side * int64_t(F) * at.Mp, xt, dw, int64_t(one ? 2 : 1) * F, K, Mp, at.Mp, at.Mp, lddw, stream);
-        rc != CA_OK)
-      return rc;
+    if (const int32_t rc = product(cols + side * int64_t(F) * at.Mp, xt, dw, int64_t(one ? 2 : 1) * F, K, at.Mp, lddw, partials, stream); rc != CA_OK) return rc;
   }
   return CA_OK;
 }

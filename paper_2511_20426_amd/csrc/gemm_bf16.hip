@@ -378,7 +378,7 @@ GemmTile pick_gemm_tile(const GemmArgs& a, bool publish, int n_cu, int64_t* cost
 // x 5120 2423 / 2352; the other way 8192 x 8192 x 8064 673 / 696, whole rounds of long walks.  By height, 256 / 192 / 128: 4680 x 4608 x 1536 66.0
 // / 54.1 / 60.7, 23400 x 15360 x 5120 2341 / 2461 / 2752, 4680 x 1536 x 1536 32.8 / 26.9 / 22.4.  The 256 x 128 tile stays ahead of an
 // equal cost (14040 x 1152 x 384 19.7, 192 x 256 21.2).
-int rows_tile(const GemmArgs& a, int n_cu, int64_t compiled, GemmTile by) {
+int rows_tile(const GemmArgs& a, int n_cu, int64_t compiled, GemmTile by, int64_t* cost_of) {
   static constexpr struct { int rows, start, stage, full, tile; } kRows[] = {
       {256, 2260, 960, 1325, 5100}, {192, 2280, 754, 1070, 3900}, {128, 2840, 594, 785, 2410}};
   const int64_t stages = a.K / 64, limit = by == kTile256x128 ? compiled - compiled / 14 : compiled;
@@ -393,6 +393,7 @@ int rows_tile(const GemmArgs& a, int n_cu, int64_t compiled, GemmTile by) {
       rows = m.rows;
     }
   }
+  *cost_of = rows ? best : compiled;
   return rows;
 }
 
@@ -419,12 +420,22 @@ int32_t dispatch_gemm_plain(GemmArgs& a, void* stream) {
   const GemmTile compiled = pick_gemm_tile(a, false, n_cu, &cost);
   if (const int32_t rc = gemm_tiles_ready(); rc != CA_OK) return rc;
   if (const int32_t rc = gemm_rows_ready(); rc != CA_OK) return rc;
-  if (const int rows = rows_tile(a, n_cu, cost, compiled))
+  if (const int rows = rows_tile(a, n_cu, cost, compiled, &cost))
     return launch_gemm_rows(rows, a.x, a.w, a.y, a.M, a.N, a.K, a.ldx, a.ldw, a.ldy, stream);
   return launch_gemm_tile(compiled, a.x, a.w, a.y, a.M, a.N, a.K, a.ldx, a.ldw, a.ldy, stream);
 }
 
 }  // namespace
+
+int64_t gemm_bf16_cost(int64_t M, int32_t N, int32_t K, int n_cu) {
+  GemmArgs a{};
+  a.M = int32_t(M); a.N = N; a.K = K;
+  a.block_rows = a.M;
+  int64_t cost = 0;
+  const GemmTile compiled = pick_gemm_tile(a, false, n_cu, &cost);
+  rows_tile(a, n_cu, cost, compiled, &cost);
+  return cost;
+}
 
 int32_t launch_gemm_bf16(const void* x, const void* w, void* y, int64_t M, int32_t N, int32_t K,
                          int64_t ldx, int64_t ldw, int64_t ldy, void* stream) {

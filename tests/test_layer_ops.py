@@ -447,6 +447,23 @@ def test_gradients_that_are_asked_for(M):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("M", [3, 100])
+@pytest.mark.parametrize("act", ["silu", "gelu"])
+def test_gradients_of_gates_that_are_nan(M, act):
+    """A NaN among the gate's weights is in the gradients of both weights of its column and of all rows, and in no other column's."""
+    from paper_2511_20426_amd.runner import gated_linear_backward, gated_linear_train
+    gen = _gen(21)
+    x, wg, wu, dh = _normal(gen, M, 128), _normal(gen, 16, 128), _normal(gen, 16, 128), _normal(gen, M, 16)
+    wg[5, 0] = float("nan")
+    _, saved = gated_linear_train(x, wg, wu, act)
+    dx, dwg, dwu = gated_linear_backward(dh, x, wg, wu, saved, act)
+    bad = torch.arange(16, device=DEV) == 5
+    for t in (dwg, dwu):
+        assert t[bad].isnan().all() and t[~bad].isfinite().all()
+    assert dx.isnan().all()
+
+
+@pytest.mark.gpu
 def test_gated_of_no_rows():
     from paper_2511_20426_amd.runner import gated_linear, gated_linear_backward, gated_linear_train
     x, w = torch.empty((0, 128), dtype=torch.bfloat16, device=DEV), torch.ones((16, 128), dtype=torch.bfloat16, device=DEV)
