@@ -9,6 +9,8 @@
 // that depends on the sizes alone: no atomics, the same bits every time.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
+
 #include "ca_internal.hpp"
 
 namespace ca {
@@ -17,7 +19,7 @@ namespace {
 #include "rope_device.hpp"
 #include "norm_device.hpp"
 
-constexpr int kMaxWorkgroups = 1024;              // of a backward launch: each leaves a partial sum of the weights' gradients
+constexpr int kMaxWorkgroups = 2048;              // of a backward launch: each leaves a partial sum of the weights' gradients
 
 struct NormSide {                                 // queries or keys
   const void* x;
@@ -49,11 +51,10 @@ __device__ __forceinline__ void token_angles(const RopeGeom& g, int64_t n, int64
 }
 
 // A wave takes a token: its lanes cover 64 / chunks heads at a time (1 KB of bf16), rows_per_group heads in all, kAhead loads
-// requested together, queries first, then keys (a loop over both picked the side for each load and weight: 23400 tokens of 40 + 40
+// requested together (no more than there are: 23400 tokens of 1 + 1 heads 20.1 -> 18.9 us, with gradients' 48 -> 25), queries first, then keys (a loop over both picked the side for each load and weight: 23400 tokens of 40 + 40
 // heads 192 us, now 178, the rate of a copy; 4680 of 12 + 12 18.5, now 13.7).
-template <typename T>
+template <typename T, int kAhead>
 __global__ __launch_bounds__(256) void norm_rope_kernel(RopeGeom g, NormArgs a) {
-  constexpr int kAhead = 4;
   const int chunks = g.head_dim / 8, head_slots = 64 / chunks;
   const int64_t n = int64_t(blockIdx.x) * 4 + (threadIdx.x >> 6);
   if (n >= a.n_tokens) return;
@@ -86,11 +87,10 @@ __global__ __launch_bounds__(256) void norm_rope_kernel(RopeGeom g, NormArgs a) 
   }
 }
 
-// A wave takes every so manieth token, all its rows or a group's, and keeps the sums of dy x r of its lanes.  23400 tokens of 40 + 40
-// heads 279 us (5.15 TB/s), 4680 of 12 + 12 26.8 with the second launch (picking the side for each value 298 and 31.6).
-template <typename T>
+// A wave takes every so manieth token, all its rows or a group's, and keeps the sums of dy x r of its lanes.  With the second launch 23400
+// tokens of 40 + 40 heads 262 us (5.5 TB/s), 4680 of 12 + 12 23.6.
+template <typename T, int kAhead>
 __global__ __launch_bounds__(256) void norm_rope_backward_kernel(RopeGeom g, NormArgs a) {
-  constexpr int kAhead = 3;
   __shared__ float sums[4][2][2 * kMaxPairs];
   const int chunks = g.head_dim / 8, head_slots = 64 / chunks;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c8 = lane % chunks, hs = lane / chunks;
@@ -204,6 +204,12 @@ NormGrid norm_grid(int64_t workgroups, int rows, int head_dim, int fill) {
   return out;
 }
 
+// Loads of a side's heads that a wave requests together: as many as one of its row groups has, up to `most`
+int norm_ahead(const RopeGeom& g, const NormGrid& grid, int most) {
+  const int slots = 512 / g.head_dim, heads = grid.rows_per_group < g.heads ? grid.rows_per_group : g.heads;
+  return std::min((heads + slots - 1) / slots, most);
+}
+
 int norm_sides(const RopeGeom& g, const NormTensors& q, const NormTensors& k, int64_t n_tokens, int64_t first_frame, float eps, NormArgs* a) {
   int n = 0;
   for (const NormTensors* t : {&q, &k}) {
@@ -217,9 +223,14 @@ int norm_sides(const RopeGeom& g, const NormTensors& q, const NormTensors& k, in
   return n;
 }
 
-NormGrid backward_grid(const RopeGeom& g, int64_t n_tokens, int rows) {
-  const int64_t all = (n_tokens + 3) / 4;
-  return norm_grid(all < kMaxWorkgroups ? all : kMaxWorkgroups, rows, g.head_dim, kMaxWorkgroups / 2);
+// Each workgroup of a backward launch leaves partial sums that the second launch reads: 512 of them, more where there is much to read or
+// there are many tokens (each with its angles).  Us with up to 512 / 1024 / 2048, both launches: 4680 tokens of 12 + 12 heads 23.6 / 25.5 / 24.9,
+// 12000 of 16 + 16 70.5 / 67.3 / 66.2, 23400 of 40 + 40 273 / 280 / 262, of 1 + 1 28.8 / 25.3 / 30.0; heads are dealt to groups up to
+// 256 workgroups (1000 tokens of 5 + 5 heads 10.8, up to 512 13.1).
+NormGrid backward_grid(const RopeGeom& g, int64_t n_tokens, int rows, int bytes_of_value) {
+  const int64_t all = (n_tokens + 3) / 4, read = 2 * n_tokens * rows * g.head_dim * bytes_of_value;
+  const int64_t most = read > (int64_t(128) << 20) ? kMaxWorkgroups : n_tokens > 16384 ? kMaxWorkgroups / 2 : kMaxWorkgroups / 4;
+  return norm_grid(std::min(all, most), rows, g.head_dim, 256);
 }
 
 }  // namespace
@@ -233,7 +244,11 @@ int32_t launch_norm_rope(const RopeGeom& g, int dtype, const NormTensors& q, con
   if (gx >= (1 << 24)) return CA_EUNSUPPORTED;     // (a launch has fewer than 2^32 threads)
   const NormGrid grid = norm_grid(gx, a.rows, g.head_dim, 2048);
   a.rows_per_group = grid.rows_per_group;
-  const auto kernel = dtype == CA_BF16 ? norm_rope_kernel<uint16_t> : norm_rope_kernel<float>;
+  using Kernel = void (*)(RopeGeom, NormArgs);
+  static constexpr Kernel kKernels[2][4] = {{norm_rope_kernel<float, 1>, norm_rope_kernel<float, 2>, norm_rope_kernel<float, 3>, norm_rope_kernel<float, 4>},
+                                            {norm_rope_kernel<uint16_t, 1>, norm_rope_kernel<uint16_t, 2>, norm_rope_kernel<uint16_t, 3>,
+                                             norm_rope_kernel<uint16_t, 4>}};
+  const Kernel kernel = kKernels[dtype == CA_BF16][norm_ahead(g, grid, 4) - 1];
   hipLaunchKernelGGL(kernel, dim3(grid.x, grid.y), dim3(256), 0, static_cast<hipStream_t>(stream), g, a);
   return finish_launch("norm_rope.hip");
 }
@@ -249,10 +264,14 @@ int32_t launch_norm_rope_backward(const RopeGeom& g, int dtype, const NormTensor
   hipStream_t s = static_cast<hipStream_t>(stream);
   int n_partials = 0;
   if (n_tokens > 0) {
-    const NormGrid grid = backward_grid(g, n_tokens, a.rows);
+    const NormGrid grid = backward_grid(g, n_tokens, a.rows, dtype == CA_BF16 ? 2 : 4);
     a.rows_per_group = grid.rows_per_group;
     n_partials = int(grid.x * grid.y);
-    const auto kernel = dtype == CA_BF16 ? norm_rope_backward_kernel<uint16_t> : norm_rope_backward_kernel<float>;
+    using Kernel = void (*)(RopeGeom, NormArgs);
+    static constexpr Kernel kKernels[2][3] = {
+        {norm_rope_backward_kernel<float, 1>, norm_rope_backward_kernel<float, 2>, norm_rope_backward_kernel<float, 3>},
+        {norm_rope_backward_kernel<uint16_t, 1>, norm_rope_backward_kernel<uint16_t, 2>, norm_rope_backward_kernel<uint16_t, 3>}};
+    const Kernel kernel = kKernels[dtype == CA_BF16][norm_ahead(g, grid, 3) - 1];
     hipLaunchKernelGGL(kernel, dim3(grid.x, grid.y), dim3(256), 0, s, g, a);
     if (const int32_t rc = finish_launch("norm_rope.hip"); rc != CA_OK) return rc;
   }
