@@ -4,40 +4,71 @@
 // way while one is multiplied, with X's rows from L2 (lanes of rows that do not exist ask for nothing: a row asked for by all sixteen
 // costs as much of the way from L2 as W does).  The waves' sums meet in LDS, in order.
 //
-// Of up to four tokens in bf16 the 8-bit codes are made here (kCodes): every workgroup makes them for itself, while its first pieces
-// of W are on their way, instead of a launch of its own ahead of this one.
+// The 8-bit codes of tokens in bf16 can be made here (Codes): every workgroup makes them for itself, while its first pieces of W are on
+// their way, instead of a launch of its own ahead of this one.  All threads take a token's values together, or each wave a token.
 // (Included behind quantize_device.hpp and gemm_ops.hpp.)
 #pragma once
 
 constexpr int kFewWaves = 4, kFewAhead = 4;
-constexpr int kCodeRows = 4, kCodeHeld = 3, kCodeK = 8 * 64 * kFewWaves * kCodeHeld;       // tokens and k that fit; vectors of a thread
 
-// kTiles: tiles of 16 tokens.  kCodes: a.x is bf16 [M][ldx bytes], M up to kCodeRows, K values up to kCodeK, 16-byte aligned rows.
-template <typename Op, int kTiles, bool kCodes>
+// The codes that a launch makes: of kThread tokens at a time a thread has kHeld vectors of eight values each; kWaves waves share a token.
+template <int kThread, int kHeldOf, int kWavesOf>
+struct Codes {
+  static constexpr int kRows = kThread, kHeld = kHeldOf, kWaves = kWavesOf;
+  static constexpr int kTokens = kRows * kFewWaves / kWaves, kMost = 8 * 64 * kHeld * kWaves;      // tokens, and values of each
+};
+using NoCodes = Codes<0, 0, 1>;
+using CodesLong = Codes<2, 3, kFewWaves>;         // two tokens of up to 6144, by all waves
+using CodesShort = Codes<3, 3, 1>;                // twelve of up to 1536, each by a wave
+
+// Values 8 v .. +7 of a row of k >= 8 in bf16, of any alignment: the load of eight that lie in the row, and of them, once they are
+// there, the ones meant, zeros behind the row's end.  (A branch for the row's end would wait for its loads.)
+__device__ __forceinline__ U4 load_eight(const uint16_t* row, int v, int k) {
+  struct __attribute__((packed, aligned(2))) Eight { uint32_t w[4]; };
+  const Eight e = *reinterpret_cast<const Eight*>(row + min(8 * v, k - 8));
+  return U4{e.w[0], e.w[1], e.w[2], e.w[3]};
+}
+__device__ __forceinline__ U4 eight_of(const U4& e, int v, int k) {
+  const int past = max(8 * v - (k - 8), 0);
+  uint64_t lo = e.x | uint64_t(e.y) << 32, hi = e.z | uint64_t(e.w) << 32;
+  if (k % 8 != 0) {
+    const int bits = 16 * (past & 3);
+    lo = past & 4 ? hi : lo;
+    hi = past & 4 ? 0 : hi;
+    lo = lo >> bits | (hi << 1) << (63 - bits);
+    hi >>= bits;
+  }
+  if (past >= 8) lo = hi = 0;
+  return U4{uint32_t(lo), uint32_t(lo >> 32), uint32_t(hi), uint32_t(hi >> 32)};
+}
+
+// kTiles: tiles of 16 tokens.  With codes a.x is bf16 [M][ldx bytes], a.k_values (8 or more) to a row, no more of both than Code has.
+template <typename Op, int kTiles, typename Code>
 __global__ __launch_bounds__(64 * kFewWaves) void gemm_few_kernel(OpArgs a) {
   constexpr int kSides = Op::kGated ? 2 : 1, kAhead = kFewAhead, kWaves = kFewWaves;
   using Products = typename Op::Products;
   using Frag = typename Products::Frag;
   using Sums = typename Products::Sums;
   __shared__ Sums part[kWaves][kSides][kTiles][64];
-  __shared__ __attribute__((aligned(16))) uint8_t codes[kCodes ? kCodeRows : 1][kCodes ? kCodeK + 16 : 16];
-  __shared__ uint32_t most_of[kCodeRows][kWaves];
+  constexpr bool kCodes = Code::kRows > 0;
+  __shared__ __attribute__((aligned(16))) uint8_t codes[kCodes ? Code::kTokens : 1][Code::kMost + 16];
+  __shared__ uint32_t most_of[kCodes ? Code::kTokens : 1][Code::kWaves];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l15 = lane & 15, grp = lane >> 4;
   const int n0 = blockIdx.x * 16, row = min(n0 + l15, a.N - 1);          // rows past the end re-read the last one
   const uint8_t* w[kSides];
   w[0] = static_cast<const uint8_t*>(a.w) + int64_t(row) * a.ldw + grp * 16;
   if constexpr (Op::kGated) w[1] = static_cast<const uint8_t*>(a.w2) + int64_t(row) * a.ldw2 + grp * 16;
-  U4 held[kCodes ? kCodeRows : 1][kCodeHeld];
-  const int vectors = a.k_values / 8;                                   // of a row
+  U4 held[kCodes ? Code::kRows : 1][kCodes ? Code::kHeld : 1];
+  constexpr int kEach = kWaves / Code::kWaves;                          // tokens that the workgroup takes at a time
+  auto code_row = [&](int r) { return wave / Code::kWaves + r * kEach; };
+  auto code_vector = [&](int v) { return wave % Code::kWaves * 64 + lane + v * 64 * Code::kWaves; };
   if constexpr (kCodes) {
 #pragma unroll
-    for (int r = 0; r < kCodeRows; ++r)
+    for (int r = 0; r < Code::kRows; ++r)
 #pragma unroll
-      for (int v = 0; v < kCodeHeld; ++v) {
-        const int at = int(threadIdx.x) + v * 64 * kWaves;
-        held[r][v] = U4{0, 0, 0, 0};
-        if (r < a.M && at < vectors) held[r][v] = *reinterpret_cast<const U4*>(static_cast<const uint8_t*>(a.x) + int64_t(r) * a.ldx + at * 16);
-      }
+      for (int v = 0; v < Code::kHeld; ++v)
+        if (code_row(r) < a.M)
+          held[r][v] = load_eight(reinterpret_cast<const uint16_t*>(static_cast<const uint8_t*>(a.x) + int64_t(code_row(r)) * a.ldx), code_vector(v), a.k_values);
   }
   const uint8_t* x[kTiles];
 #pragma unroll
@@ -84,30 +115,32 @@ __global__ __launch_bounds__(64 * kFewWaves) void gemm_few_kernel(OpArgs a) {
     for (int j = 0; j < kAhead; ++j) request(j, j);
   }
   if constexpr (kCodes) {
-    uint32_t most[kCodeRows] = {};
+    uint32_t most[Code::kRows] = {};
 #pragma unroll
-    for (int r = 0; r < kCodeRows; ++r) {
-      if (r >= a.M) break;
-      most[r] = 0;
+    for (int r = 0; r < Code::kRows; ++r) {
+      if (code_row(r) >= a.M) break;
 #pragma unroll
-      for (int v = 0; v < kCodeHeld; ++v)
+      for (int v = 0; v < Code::kHeld; ++v) {
+        held[r][v] = eight_of(held[r][v], code_vector(v), a.k_values);
 #pragma unroll
         for (uint32_t two : {held[r][v].x, held[r][v].y, held[r][v].z, held[r][v].w})
           most[r] = max(most[r], max(two << 16 & 0x7fff0000u, two & 0x7fff0000u));
+      }
 #pragma unroll
       for (int d = 1; d < 64; d *= 2) most[r] = max(most[r], uint32_t(__shfl_xor(int(most[r]), d, 64)));
-      if (lane == 0) most_of[r][wave] = most[r];
+      if (lane == 0) most_of[code_row(r)][wave % Code::kWaves] = most[r];
     }
-    __syncthreads();
+    if constexpr (Code::kWaves > 1) __syncthreads();
 #pragma unroll
-    for (int r = 0; r < kCodeRows; ++r) {
-      if (r >= a.M) break;
-      const RowScale of(max(max(most_of[r][0], most_of[r][1]), max(most_of[r][2], most_of[r][3])));
+    for (int r = 0; r < Code::kRows; ++r) {
+      const int row = code_row(r);
+      if (row >= a.M) break;
 #pragma unroll
-      for (int v = 0; v < kCodeHeld; ++v) {
-        const int at = int(threadIdx.x) + v * 64 * kWaves;
-        if (at < a.K / 8) *reinterpret_cast<uint2*>(codes[r] + at * 8) = row_codes(of, held[r][v]);
-      }
+      for (int w = 0; w < Code::kWaves && Code::kWaves > 1; ++w) most[r] = max(most[r], most_of[row][w]);
+      const RowScale of(most[r]);
+#pragma unroll
+      for (int v = 0; v < Code::kHeld; ++v)
+        if (code_vector(v) < a.K / 8) *reinterpret_cast<uint2*>(codes[row] + code_vector(v) * 8) = row_codes(of, held[r][v]);
     }
     __syncthreads();
   }
@@ -159,10 +192,14 @@ __global__ __launch_bounds__(64 * kFewWaves) void gemm_few_kernel(OpArgs a) {
     }
   } else {
     float xs;
-    if constexpr (kCodes)
-      xs = row_scale(max(max(most_of[m][0], most_of[m][1]), max(most_of[m][2], most_of[m][3])));
-    else
+    if constexpr (kCodes) {
+      uint32_t most = most_of[m][0];
+#pragma unroll
+      for (int w = 1; w < Code::kWaves; ++w) most = max(most, most_of[m][w]);
+      xs = row_scale(most);
+    } else {
       xs = a.xs[m];
+    }
     const float* ws = static_cast<const float*>(a.w2) + n;
     leave(scaled(sum[0][0], xs, ws[0]), scaled(sum[0][1], xs, ws[1]), scaled(sum[0][2], xs, ws[2]), scaled(sum[0][3], xs, ws[3]));
   }
@@ -173,8 +210,8 @@ int32_t enqueue_few(const OpArgs& a, const char* what, void* stream) {
   const unsigned groups = unsigned((a.N + 15) / 16);
   hipStream_t s = static_cast<hipStream_t>(stream);
   if (a.M <= 16)
-    hipLaunchKernelGGL((gemm_few_kernel<Op, 1, false>), dim3(groups), dim3(64 * kFewWaves), 0, s, a);
+    hipLaunchKernelGGL((gemm_few_kernel<Op, 1, NoCodes>), dim3(groups), dim3(64 * kFewWaves), 0, s, a);
   else
-    hipLaunchKernelGGL((gemm_few_kernel<Op, 2, false>), dim3(groups), dim3(64 * kFewWaves), 0, s, a);
+    hipLaunchKernelGGL((gemm_few_kernel<Op, 2, NoCodes>), dim3(groups), dim3(64 * kFewWaves), 0, s, a);
   return finish_launch(what);
 }

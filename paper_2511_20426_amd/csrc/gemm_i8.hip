@@ -32,6 +32,15 @@ constexpr OpModel kModel[] = {{256, 256, 1, 1980, 960, 1270, 5400}, {192, 256, 1
                               {256, 128, 1, 0, 705, 840, 5650},     {128, 128, 1, 0, 455, 470, 3680},     {64, 64, 2, 0, 290, 370, 1990},
                               {64, 64, 1, 0, 255, 190, 2000}};
 
+// Whether the codes of few tokens are made in the product's launch: they are unless making them in every workgroup costs more than the launch
+// that it saves.  Us, ahead / in the launch, weights from memory: one token 512 x 230 5.7 / 3.3, 4608 x 1536 7.5 / 5.7, 5120 x 5120 13.0 /
+// 10.1, 15360 x 5120 20.2 / 18.4; two 5120 x 5120 13.4 / 11.7, 15360 x 5120 20.6 / 21.1; three 4608 x 1537 8.5 / 9.2; four 4608 x 1536 8.0 /
+// 5.8; twelve 512 x 230 6.2 / 5.1, 4608 x 1536 8.5 / 8.0, 15360 x 64 7.2 / 8.5.
+bool codes_in_launch(int64_t M, int32_t N, int32_t K) {
+  if (K <= CodesShort::kMost) return M <= (N <= 8192 ? CodesShort::kTokens : 8);
+  return K <= CodesLong::kMost && M <= (N <= 12288 ? CodesLong::kTokens : 1);
+}
+
 // one call of any size readies all kernels for stream capture
 int32_t i8_ready() {
   const KernelLds kernels[] = {{reinterpret_cast<const void*>(gemm_op_rows_kernel<8, I8>), kOpRowsLds},
@@ -74,16 +83,14 @@ int32_t launch_gemm_i8_values(int dtype, const void* x, int64_t ldx, const void*
                               int64_t ldw, int64_t ldy, void* workspace, void* stream) {
   if (M == 0) return CA_OK;
   if (const int32_t rc = i8_ready(); rc != CA_OK) return rc;
-  // Up to kCodeRows tokens go in one launch, unless making the codes in every workgroup costs more than the launch that it saves.  Us with
-  // codes made in the launch / ahead, weights from memory: one token 15360 x 5120 20.3 / 20.8, 5120 x 5120 11.0 / 13.5, 4608 x 1536 8.8 /
-  // 10.8; two 22.5 / 21.2, 11.7 / 13.9, 8.8 / 10.6; four 26.5 / 22.4, 14.3 / 14.2, 8.9 / 10.6.
-  if (dtype == CA_BF16 && M <= kCodeRows && K <= kCodeK && M * ((N + 15) / 16) * K <= 6000000 && K % 8 == 0 && (reinterpret_cast<uintptr_t>(x) | uint64_t(ldx) * 2) % 16 == 0) {
+  const auto kernel = K <= CodesShort::kMost ? gemm_few_kernel<I8, 1, CodesShort> : gemm_few_kernel<I8, 1, CodesLong>;
+  if (dtype == CA_BF16 && K >= 8 && codes_in_launch(M, N, K)) {
     OpArgs a{};
     a.x = x; a.w = w; a.y = y; a.w2 = w_scales;
     a.ldy = ldy;
     a.M = int32_t(M); a.N = N; a.K = (K + 255) / 256 * 256; a.k_values = K;
     a.ldx = int32_t(2 * ldx); a.ldw = int32_t(ldw);
-    hipLaunchKernelGGL((gemm_few_kernel<I8, 1, true>), dim3(unsigned((N + 15) / 16)), dim3(64 * kFewWaves), 0, static_cast<hipStream_t>(stream), a);
+    hipLaunchKernelGGL(kernel, dim3(unsigned((N + 15) / 16)), dim3(64 * kFewWaves), 0, static_cast<hipStream_t>(stream), a);
     return finish_launch("gemm_i8.hip");
   }
   const int64_t ld = (K + 255) / 256 * 256;

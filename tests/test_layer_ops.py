@@ -308,6 +308,29 @@ def test_linear_i8(M, N, K):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("off,pad", [(0, 0), (1, 3), (8, 8)])
+@pytest.mark.parametrize("M,N,K", [(1, 40, 7), (1, 24, 8), (1, 512, 230), (2, 72, 9), (4, 40, 255), (5, 24, 257), (8, 8200, 65), (9, 8200, 65), (9, 136, 1001), (12, 40, 1536),
+                                   (12, 264, 1535), (13, 40, 1536), (1, 40, 1537), (2, 136, 6143), (2, 24, 6144), (1, 40, 6145), (2, 12296, 1600), (3, 24, 2000)])
+def test_few_tokens_of_any_alignment_in_8_bits(M, N, K, off, pad):
+    """The calls that make the codes on their way give the bits of those that have them made ahead; NaN and rows of zeros stay in their rows."""
+    from paper_2511_20426_amd.runner import linear_i8, quantize_rows
+    gen = _gen(M + N + K + off)
+    whole = _normal(gen, M * (K + pad) + off)
+    x = whole[off:].view(M, K + pad)[:, :K]
+    w = quantize_rows(_normal(gen, N, K))
+    if M > 2:
+        x[0] = 0
+        x[2, K - 1] = float("nan")
+    y = linear_i8(x, w)
+    ahead = linear_i8(quantize_rows(x), w)
+    bad = torch.zeros(M, dtype=torch.bool, device=DEV)
+    bad[2:3] = M > 2
+    assert (y[~bad] == ahead[~bad]).all() and y[bad].isnan().all() and ahead[bad].isnan().all()
+    if M > 2:
+        assert (y[0] == 0).all()
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("M", [1, 40])
 def test_linear_i8_at_the_longest_k(M):
     from paper_2511_20426_amd.runner import QuantizedRows, linear_i8
