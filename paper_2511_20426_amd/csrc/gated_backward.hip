@@ -9,8 +9,8 @@
 // off, 1.7e-3 of which is that of the result.  (With G and U saved in bf16 as well it was 3.1e-3: they are saved in fp32.)  dX is one
 // product over both, so that their sum is not rounded in between.
 //
-// Of up to 8 rows all of it is one pass over the weights, read once, and their gradients, written once, with nothing laid out
-// (gated_few_grad_kernel).
+// Of up to 32 rows all of it is one pass over the weights, read once, and their gradients, written once, with nothing laid out
+// (gated_few_grad_kernel, gated_some_grad_kernel).
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -155,11 +155,11 @@ __global__ __launch_bounds__(256) void gated_layout_kernel(GatedLayoutArgs a) {
     transpose_tile(a.t[2], tile[0], b - a.ends[1]);
 }
 
-// Few rows: both weights read and their gradients written once are what counts (one row of 13824 x 5120 130 us, 566 MB; of 4096 x 1536 18.6 us,
-// eight 24.2; by the products of more rows nine take 32.9, and sixteen taken here, with 256 registers, took 57.6).  A workgroup takes 128 columns of K and `each` columns f of the projections: sixteen threads eight columns of K each, and
-// sixteen such rows of threads every sixteenth f.  dG and dU of the f are formed in LDS, in fp32; of each f a thread reads its part of Wg and
-// Wu, adds to its sums of dX, and forms and writes its part of dWg and dWu from X's rows, which it keeps.  The sums of dX of a
-// workgroup's f go to the workspace; a second launch adds them up in order.
+// Up to four rows: both weights read and their gradients written once are what counts (one row of 13824 x 5120 133 us, 566 MB; four 136; of 4096 x
+// 1536 18.0 and 18.5).  A workgroup takes 128 columns of K and `each` columns f of the projections: sixteen threads eight columns of K
+// each, and sixteen such rows of threads every sixteenth f.  dG and dU of the f are formed in LDS, in fp32; of each f a thread reads its
+// part of Wg and Wu, adds to its sums of dX, and forms and writes its part of dWg and dWu from X's rows, which it keeps.  The sums of
+// dX of a workgroup's f go to the workspace; a second launch adds them up in order.
 struct GatedFewArgs {
   const uint16_t *dh, *x, *wg, *wu;
   const float *g, *u;
@@ -170,8 +170,10 @@ struct GatedFewArgs {
   float act0, act1;
 };
 
-template <int kRows>
+constexpr int kFewGradRows = 4, kSomeGradRows = 32;       // rows of the two kernels for few
+
 __global__ __launch_bounds__(256) void gated_few_grad_kernel(GatedFewArgs a) {
+  constexpr int kRows = kFewGradRows;
   extern __shared__ __attribute__((aligned(16))) float grads[];        // [f of the workgroup][dG | dU][kRows]; then the sums of dX
   const int t = threadIdx.x, k = (blockIdx.x * 16 + (t & 15)) * 8, lane_f = t >> 4;
   const int f0 = blockIdx.y * a.each, count = min(a.each, a.F - f0);
@@ -251,40 +253,195 @@ __global__ __launch_bounds__(256) void gated_few_grad_kernel(GatedFewArgs a) {
   }
 }
 
-// A product from the sums of its parts, four columns to a thread (N is a multiple of 128)
+// Eight rows of eight values (16 bytes each) become eight fragments of the matrix instruction: of each column its eight rows' values.
+__device__ __forceinline__ void columns_of(const U4 (&rows)[8], Bf16Products::Frag (&cols)[8]) {
+#pragma unroll
+  for (int c = 0; c < 8; ++c) {
+    uint32_t w[4];
+#pragma unroll
+    for (int p = 0; p < 4; ++p) {
+      const U4 &lo = rows[2 * p], &hi = rows[2 * p + 1];
+      const uint32_t a = c < 2 ? lo.x : c < 4 ? lo.y : c < 6 ? lo.z : lo.w, b = c < 2 ? hi.x : c < 4 ? hi.y : c < 6 ? hi.z : hi.w;
+      w[p] = __builtin_amdgcn_perm(b, a, c & 1 ? 0x07060302 : 0x05040100);
+    }
+    cols[c] = __builtin_bit_cast(Bf16Products::Frag, U4{w[0], w[1], w[2], w[3]});
+  }
+}
+
+// Up to 32 rows, on the matrix pipe, still one pass over the weights and their gradients with nothing laid out.  A workgroup takes 128 columns
+// of K and `each` columns f in chunks of 128, whose dG and dU it forms in LDS in bf16, by rows and by columns; each wave takes 32 of a chunk.  A
+// lane brings 16 bytes of eight rows of W, whose columns in registers are what dX's product multiplies, and keeps the columns of X that the
+// weights' gradients multiply.  Of 16 x 16 products c = 0 .. 7 row i stands for column 8 i + c of the 128, so that a lane's results are 32
+// neighbours.  The waves' sums of dX meet in LDS, the workgroups' in the workspace.  Bound by memory as the kernel above: 16 rows of 13824 x 5120
+// 156 us (240 by the products of more rows, with their layout), of 1920 x 3840 25.6 (35.6), 32 rows 165 (246) and 27.4 (39.2); eight rows by
+// the kernel above took 163 and 33, here 154 and 24.6.
+template <int kTiles>
+__global__ __launch_bounds__(256, 2) void gated_some_grad_kernel(GatedFewArgs a) {
+  using Frag = Bf16Products::Frag;
+  constexpr int kChunk = 128, kRows = 16 * kTiles, kPitch = kChunk + 8, kColPitch = 32 + 8, kSumPitch = 128 + 4;
+  constexpr int kGradBytes = 2 * 2 * (kRows * kPitch + kChunk * kColPitch), kSumBytes = 4 * 16 * kSumPitch * 4;
+  __shared__ __attribute__((aligned(16))) uint8_t lds[kGradBytes > kSumBytes ? kGradBytes : kSumBytes];
+  uint16_t* const by_row = reinterpret_cast<uint16_t*>(lds);            // [dG | dU][row][f]
+  uint16_t* const by_col = by_row + 2 * kRows * kPitch;                 // [dG | dU][f][row]
+  const int t = threadIdx.x, lane = t & 63, wave = t >> 6, l15 = lane & 15, grp = lane >> 4;
+  const int k0 = blockIdx.x * 128, f0 = blockIdx.y * a.each, count = min(a.each, a.F - f0);
+  Frag xt[8];
+  U4 w[2][8];
+  auto request = [&](int side, int chunk) {       // rows past the end re-read the last one, whose gradients there are zeros
+    const int64_t ld = side ? a.ldwu : a.ldwg;
+    const uint8_t* const from = reinterpret_cast<const uint8_t*>((side ? a.wu : a.wg) + (f0 + chunk) * ld + k0);
+#pragma unroll
+    for (int e = 0; e < 8; ++e)                   // (128 rows of 2^22 values are 2^30 bytes)
+      w[side][e] = *reinterpret_cast<const U4*>(from + uint32_t(min(32 * wave + 8 * grp + e, a.F - 1 - f0 - chunk)) * uint32_t(2 * ld) + 16u * l15);
+  };
+  {
+    U4 x[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] = 8 * grp + e < a.M ? *reinterpret_cast<const U4*>(a.x + int64_t(8 * grp + e) * a.ldx + k0 + 8 * l15) : U4{0, 0, 0, 0};
+    if (a.partials) {
+      request(0, 0);
+      request(1, 0);
+    }
+    columns_of(x, xt);
+  }
+  f32x4 dx[8][kTiles];
+#pragma unroll
+  for (int c = 0; c < 8; ++c)
+#pragma unroll
+    for (int i = 0; i < kTiles; ++i) dx[c][i] = f32x4{0.f, 0.f, 0.f, 0.f};
+  auto multiply = [&](int side, int chunk) {
+    if (a.partials) {
+      Frag wt[8];
+      columns_of(w[side], wt);
+      if (chunk + kChunk < count) request(side, chunk + kChunk);
+#pragma unroll
+      for (int i = 0; i < kTiles; ++i) {
+        const Frag d = *reinterpret_cast<const Frag*>(by_row + (side * kRows + 16 * i + l15) * kPitch + 32 * wave + 8 * grp);
+#pragma unroll
+        for (int c = 0; c < 8; ++c) dx[c][i] = Bf16Products::multiply(wt[c], d, dx[c][i]);
+      }
+    }
+    uint16_t* const dw = side ? a.dwu : a.dwg;
+    if (!dw) return;
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+      const int in = 32 * wave + 16 * half + l15;
+      __builtin_amdgcn_sched_barrier(0);          // (parts that run into each other need more registers than there are)
+      const Frag d = *reinterpret_cast<const Frag*>(by_col + (side * kChunk + in) * kColPitch + 8 * grp);
+      f32x4 o[8];
+#pragma unroll
+      for (int c = 0; c < 8; ++c) o[c] = Bf16Products::multiply(xt[c], d, f32x4{0.f, 0.f, 0.f, 0.f});
+      if (chunk + in < count) {
+        uint16_t* const to = dw + int64_t(f0 + chunk + in) * a.lddw + k0 + 32 * grp;
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+          *reinterpret_cast<U4*>(to + 8 * r) = U4{pack_bf16(o[0][r], o[1][r]), pack_bf16(o[2][r], o[3][r]), pack_bf16(o[4][r], o[5][r]), pack_bf16(o[6][r], o[7][r])};
+      }
+    }
+  };
+  for (int chunk = 0; chunk < count; chunk += kChunk) {
+    if (chunk > 0) __syncthreads();
+    for (int i = t; i < 32 * (kChunk / 4); i += 256) {
+      const int m = i % 32, f = i / 32 * 4, n = f0 + chunk + f;
+      uint2 dg = {0, 0}, du = {0, 0};
+      if (m < a.M && chunk + f < count) {
+        const int64_t at = saved_at(m, n, a.F);
+        const f32x4 g = *reinterpret_cast<const f32x4*>(a.g + at), u = *reinterpret_cast<const f32x4*>(a.u + at);
+        const uint2 dh2 = *reinterpret_cast<const uint2*>(a.dh + int64_t(m) * a.lddh + n);
+        const float dh[4] = {bf16_lo(dh2.x), bf16_hi(dh2.x), bf16_lo(dh2.y), bf16_hi(dh2.y)};
+        float v[4], s[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          float act, slope;
+          activation(g[j], a.act0, a.act1, &act, &slope);
+          v[j] = dh[j] * u[j] * slope;
+          s[j] = dh[j] * act;
+        }
+        dg = uint2{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
+        du = uint2{pack_bf16(s[0], s[1]), pack_bf16(s[2], s[3])};
+      }
+      if (m < kRows) {
+        *reinterpret_cast<uint2*>(by_row + m * kPitch + f) = dg;
+        *reinterpret_cast<uint2*>(by_row + (kRows + m) * kPitch + f) = du;
+      }
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        by_col[(f + j) * kColPitch + m] = uint16_t((j & 2 ? dg.y : dg.x) >> (j & 1 ? 16 : 0));
+        by_col[(kChunk + f + j) * kColPitch + m] = uint16_t((j & 2 ? du.y : du.x) >> (j & 1 ? 16 : 0));
+      }
+    }
+    __syncthreads();
+    multiply(0, chunk);
+    __builtin_amdgcn_sched_barrier(0);
+    multiply(1, chunk);
+  }
+  if (!a.partials) return;
+  float* const sums = reinterpret_cast<float*>(lds);                    // [wave][row of 16][128]
+#pragma unroll
+  for (int i = 0; i < kTiles; ++i) {
+    if (16 * i >= a.M) break;
+    __syncthreads();
+    float* const to = sums + (wave * 16 + l15) * kSumPitch + 32 * grp;
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      *reinterpret_cast<f32x4*>(to + 8 * r) = f32x4{dx[0][i][r], dx[1][i][r], dx[2][i][r], dx[3][i][r]};
+      *reinterpret_cast<f32x4*>(to + 8 * r + 4) = f32x4{dx[4][i][r], dx[5][i][r], dx[6][i][r], dx[7][i][r]};
+    }
+    __syncthreads();
+    for (int j = t; j < 16 * 32; j += 256) {
+      const int m = j / 32, k = j % 32 * 4;
+      f32x4 v = *reinterpret_cast<const f32x4*>(sums + m * kSumPitch + k);
+#pragma unroll
+      for (int of = 1; of < 4; ++of) v += *reinterpret_cast<const f32x4*>(sums + (of * 16 + m) * kSumPitch + k);
+      if (16 * i + m < a.M) *reinterpret_cast<f32x4*>(a.partials + (int64_t(blockIdx.y) * a.M + 16 * i + m) * a.K + k0 + k) = v;
+    }
+  }
+}
+
+// A product from the sums of its parts (N is a multiple of 128): four columns to a thread, each of a workgroup's waves has every fourth part.
 __global__ __launch_bounds__(256) void gated_sum_kernel(const float* partials, int parts, int M, int N, uint16_t* y, int64_t ldy) {
-  const int i = (blockIdx.x * 256 + threadIdx.x) * 4;
-  if (i >= M * N) return;
+  __shared__ f32x4 sums[3][64];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, i = (blockIdx.x * 64 + lane) * 4;
   f32x4 v = {0.f, 0.f, 0.f, 0.f};
+  if (i < M * N) {
 #pragma unroll 8
-  for (int p = 0; p < parts; ++p) v += *reinterpret_cast<const f32x4*>(partials + int64_t(p) * M * N + i);
+    for (int p = wave; p < parts; p += 4) v += *reinterpret_cast<const f32x4*>(partials + int64_t(p) * M * N + i);
+  }
+  if (wave > 0) sums[wave - 1][lane] = v;
+  __syncthreads();
+  if (wave > 0 || i >= M * N) return;
+#pragma unroll
+  for (int s = 0; s < 3; ++s) v += sums[s][lane];
   *reinterpret_cast<uint2*>(y + int64_t(i / N) * ldy + i % N) = uint2{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
 }
 
-constexpr int kFewGradRows = 8, kFewGradMost = 512;       // rows; columns f of a workgroup
+constexpr int kFewGradMost = 512;                 // columns f of a workgroup of gated_few_grad_kernel
 
-// columns f to a workgroup: enough workgroups to fill the chip, 64 to 512 columns
-int few_grad_each(int32_t F, int32_t K) {
-  const int64_t each = int64_t(F) * (K / 128) / 1024 / 16 * 16;
-  return int(each < 64 ? 64 : (each > kFewGradMost ? kFewGradMost : each));
+// columns f to a workgroup: enough workgroups to fill the chip, 64 to 512 columns; of more than kFewGradRows rows chunks of 128, two
+// workgroups to a CU at most
+int few_grad_each(int64_t M, int32_t F, int32_t K) {
+  if (M <= kFewGradRows) return int(std::clamp<int64_t>(int64_t(F) * (K / 128) / 1024 / 16 * 16, 64, kFewGradMost));
+  const int64_t parts = std::max(512 / (K / 128), 1);
+  return int((F + 128 * parts - 1) / (128 * parts) * 128);
 }
 
 int32_t sum_parts(const float* partials, int parts, int64_t M, int32_t N, void* y, int64_t ldy, void* stream) {
-  hipLaunchKernelGGL(gated_sum_kernel, dim3(unsigned((M * N / 4 + 255) / 256)), dim3(256), 0, static_cast<hipStream_t>(stream), partials, parts, int(M), N,
+  hipLaunchKernelGGL(gated_sum_kernel, dim3(unsigned((M * N / 4 + 63) / 64)), dim3(256), 0, static_cast<hipStream_t>(stream), partials, parts, int(M), N,
                      static_cast<uint16_t*>(y), ldy);
   return finish_launch("gated_backward.hip");
 }
 
 int32_t launch_few_grad(GatedFewArgs a, void* dx, int64_t lddx, void* stream) {
-  a.each = few_grad_each(a.F, a.K);
+  a.each = few_grad_each(a.M, a.F, a.K);
   const unsigned parts = unsigned((a.F + a.each - 1) / a.each);
   hipStream_t s = static_cast<hipStream_t>(stream);
-  auto bytes = [&](int rows) { return unsigned(std::max(a.each * 2, 4 * 128) * rows * 4); };        // up to 32 KB
   const dim3 grid(unsigned(a.K / 128), parts);
-  if (a.M <= 4)
-    hipLaunchKernelGGL(gated_few_grad_kernel<4>, grid, dim3(256), bytes(4), s, a);
+    if (a.M > 16)
+    hipLaunchKernelGGL(gated_some_grad_kernel<2>, grid, dim3(256), 0, s, a);
+  else if (a.M > kFewGradRows)
+    hipLaunchKernelGGL(gated_some_grad_kernel<1>, grid, dim3(256), 0, s, a);
   else
-    hipLaunchKernelGGL(gated_few_grad_kernel<8>, grid, dim3(256), bytes(8), s, a);
+    hipLaunchKernelGGL(gated_few_grad_kernel, grid, dim3(256), unsigned(std::max(a.each * 2, 4 * 128) * kFewGradRows * 4), s, a);      // up to 16 KB of LDS
   if (const int32_t rc = finish_launch("gated_backward.hip"); rc != CA_OK || !dx) return rc;
   return sum_parts(a.partials, int(parts), a.M, a.K, dx, lddx, stream);
 }
@@ -341,8 +498,8 @@ GatedWorkspace gated_workspace(int64_t M, int32_t F, int32_t K) {
   w.Mp = M > 0 ? (M + 127) / 128 * 128 : 128;      // (of no rows the weights' gradients are zero)
   w.Fp = (int64_t(F) + 63) / 64 * 64;
   auto whole = [](int64_t elements) { return (size_t(elements) * 2 + 255) / 256 * 256; };
-  if (M > 0 && M <= kFewGradRows) {
-    const int64_t each = few_grad_each(F, K);
+  if (M > 0 && M <= kSomeGradRows) {
+    const int64_t each = few_grad_each(M, F, K);
     w.bytes = whole(2 * ((F + each - 1) / each) * M * K);
     return w;
   }
@@ -369,7 +526,7 @@ int32_t launch_gated_backward(const void* dh, const void* x, const void* w_gate,
   if (const int32_t rc = ensure_dynamic_lds(kernel, 1, kLdsGatedBackward); rc != CA_OK) return rc;
   if (const int32_t rc = gemm_tiles_ready(); rc != CA_OK) return rc;
   if (const int32_t rc = gemm_rows_ready(); rc != CA_OK) return rc;
-  if (M > 0 && M <= kFewGradRows) {
+  if (M > 0 && M <= kSomeGradRows) {
     const GatedFewArgs a{static_cast<const uint16_t*>(dh), static_cast<const uint16_t*>(x), static_cast<const uint16_t*>(w_gate),
                          static_cast<const uint16_t*>(w_up), saved, saved_up, static_cast<uint16_t*>(dw_gate), static_cast<uint16_t*>(dw_up),
                          dx ? static_cast<float*>(workspace) : nullptr, lddh, ldx, ldwg, ldwu, lddw, int32_t(M), F, K, 0, act0, act1};

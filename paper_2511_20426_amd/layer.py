@@ -48,7 +48,7 @@ class CascadeLayer:
         """One iteration for the blocks in flight (oldest first, consecutive in the video): x [C*L, width] -> [C*L, width]."""
         L, H, D = pool.block_tokens, pool.heads, pool.head_dim
         n = len(inflight) * L
-        assert x.shape == (n, H * D)
+        assert x.shape == (n, H * D) and all(b == inflight[0] + i for i, b in enumerate(inflight))
         qkv = linear_i8(x, self.w_qkv).view(n, 3, H, D)
         blocks = [qkv[i * L:(i + 1) * L] for i in range(len(inflight))]
         pool.append_batch(inflight, timesteps, epoch, [b[:, 1] for b in blocks], [b[:, 2] for b in blocks], k_weight=self.k_norm, eps=self.eps)

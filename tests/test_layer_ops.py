@@ -487,6 +487,32 @@ def test_gradients_of_gates_that_are_nan(M, act):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("M,F,K", [(5, 8, 128), (7, 136, 128), (11, 2000, 5120), (16, 264, 1664), (20, 72, 384), (31, 4008, 640), (32, 2056, 2560), (33, 136, 256)])
+def test_gradients_of_some_rows(M, F, K):
+    """Up to 32 rows: several chunks of columns, ends inside a chunk and a wave's part, strided weights; then each of the three alone and into
+    strides, with the bits of all together, and nothing beside them written."""
+    from paper_2511_20426_amd.runner import gated_linear_backward, gated_linear_train
+    gen = _gen(M + F + K + 7)
+    x, wg, wu = _normal(gen, M, K + 24)[:, :K], _normal(gen, F, K + 8, scale=2 * K ** -0.5)[:, :K], _normal(gen, F, K, scale=K ** -0.5)
+    dh = _normal(gen, M, F + 16)[:, :F]
+    _, saved = gated_linear_train(x, wg, wu, "gelu")
+    whole = gated_linear_backward(dh, x, wg, wu, saved, "gelu")
+    for t, (ref, bound) in zip(whole, _gated_grads(*(t.double().cpu() for t in (x, wg, wu, dh)), "gelu")):
+        assert ((t.double().cpu() - ref).abs() <= bound).all()
+    nbytes = B.layer_gated_backward_workspace(M, F, K)
+    work = torch.empty(nbytes, dtype=torch.uint8, device=DEV)
+    for asked in ((1, 0, 0), (0, 1, 0), (0, 0, 1), (1, 1, 1)):
+        out = [torch.full((n + 2, K + 8), 7.0, dtype=torch.bfloat16, device=DEV) for n in (M, F, F)]
+        B.layer_gated_backward_bf16(dh.data_ptr(), x.data_ptr(), wg.data_ptr(), wu.data_ptr(), saved.data_ptr(), B.CA_GELU,
+                                    *(t.data_ptr() if a else 0 for t, a in zip(out, asked)), M, F, K, F + 16, K + 24, K + 8, K, K + 8, K + 8, work.data_ptr(),
+                                    nbytes, torch.cuda.current_stream().cuda_stream)
+        for t, ref, a in zip(out, whole, asked):
+            n = ref.shape[0]
+            assert (t[:n, :K] == ref).all() if a else (t[:n, :K] == 7).all()
+            assert (t[n:] == 7).all() and (t[:, K:] == 7).all()
+
+
+@pytest.mark.gpu
 def test_gated_of_no_rows():
     from paper_2511_20426_amd.runner import gated_linear, gated_linear_backward, gated_linear_train
     x, w = torch.empty((0, 128), dtype=torch.bfloat16, device=DEV), torch.ones((16, 128), dtype=torch.bfloat16, device=DEV)
