@@ -18,8 +18,11 @@ struct Codes {
   static constexpr int kTokens = kRows * kFewWaves / kWaves, kMost = 8 * 64 * kHeld * kWaves;      // tokens, and values of each
 };
 using NoCodes = Codes<0, 0, 1>;
-using CodesLong = Codes<2, 3, kFewWaves>;         // two tokens of up to 6144, by all waves
-using CodesShort = Codes<3, 3, 1>;                // twelve of up to 1536, each by a wave
+using CodesOne = Codes<1, 3, kFewWaves>;          // one token of up to 6144, by all waves
+using CodesTwo = Codes<2, 3, kFewWaves>;          // two
+using CodesFour = Codes<4, 3, kFewWaves>;         // four
+using CodesFourShort = Codes<1, 3, 1>;            // four of up to 1536, each by a wave
+using CodesTwelve = Codes<3, 3, 1>;               // twelve (rows that are not there are read as the last one)
 
 // Values 8 v .. +7 of a row of k >= 8 in bf16, of any alignment: the load of eight that lie in the row, and of them, once they are
 // there, the ones meant, zeros behind the row's end.  (A branch for the row's end would wait for its loads.)
@@ -53,7 +56,8 @@ __global__ __launch_bounds__(64 * kFewWaves) void gemm_few_kernel(OpArgs a) {
   constexpr bool kCodes = Code::kRows > 0;
   __shared__ __attribute__((aligned(16))) uint8_t codes[kCodes ? Code::kTokens : 1][Code::kMost + 16];
   __shared__ uint32_t most_of[kCodes ? Code::kTokens : 1][Code::kWaves];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l15 = lane & 15, grp = lane >> 4;
+  // (a scalar, so that what goes by it is branched around: an MFMA runs whatever the mask of lanes is)
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, l15 = lane & 15, grp = lane >> 4;
   const int n0 = blockIdx.x * 16, row = min(n0 + l15, a.N - 1);          // rows past the end re-read the last one
   const uint8_t* w[kSides];
   w[0] = static_cast<const uint8_t*>(a.w) + int64_t(row) * a.ldw + grp * 16;
@@ -67,8 +71,8 @@ __global__ __launch_bounds__(64 * kFewWaves) void gemm_few_kernel(OpArgs a) {
     for (int r = 0; r < Code::kRows; ++r)
 #pragma unroll
       for (int v = 0; v < Code::kHeld; ++v)
-        if (code_row(r) < a.M)
-          held[r][v] = load_eight(reinterpret_cast<const uint16_t*>(static_cast<const uint8_t*>(a.x) + int64_t(code_row(r)) * a.ldx), code_vector(v), a.k_values);
+        held[r][v] = load_eight(reinterpret_cast<const uint16_t*>(static_cast<const uint8_t*>(a.x) + int64_t(min(code_row(r), a.M - 1)) * a.ldx), code_vector(v),
+                                a.k_values);
   }
   const uint8_t* x[kTiles];
 #pragma unroll
@@ -79,7 +83,7 @@ __global__ __launch_bounds__(64 * kFewWaves) void gemm_few_kernel(OpArgs a) {
 #pragma unroll
     for (int t = 0; t < kTiles; ++t) acc[s][t] = Sums{0, 0, 0, 0};
   // piece i of the wave is number wave + i kWaves of the row's
-  const int pieces = (a.K / 128 - wave + kWaves - 1) / kWaves;
+  const int all = a.K / 128, pieces = (all - wave + kWaves - 1) / kWaves;
   Frag fw[kAhead][kSides][2], fx[kAhead][kTiles][2] = {};
   auto request = [&](int slot, int i) {
     const int64_t at = int64_t(wave + i * kWaves) * 128;
@@ -109,13 +113,9 @@ __global__ __launch_bounds__(64 * kFewWaves) void gemm_few_kernel(OpArgs a) {
 #pragma unroll
         for (int t = 0; t < kTiles; ++t) acc[s][t] = Products::multiply(fw[slot][s][kk], fx[slot][t][kk], acc[s][t]);
   };
-  const bool deep = pieces >= kAhead;
-  if (deep) {
-#pragma unroll
-    for (int j = 0; j < kAhead; ++j) request(j, j);
-  }
-  if constexpr (kCodes) {
-    uint32_t most[Code::kRows] = {};
+  auto make_codes = [&]() {
+    if constexpr (!kCodes) return;
+    uint32_t most[kCodes ? Code::kRows : 1] = {};
 #pragma unroll
     for (int r = 0; r < Code::kRows; ++r) {
       if (code_row(r) >= a.M) break;
@@ -143,9 +143,13 @@ __global__ __launch_bounds__(64 * kFewWaves) void gemm_few_kernel(OpArgs a) {
         if (code_vector(v) < a.K / 8) *reinterpret_cast<uint2*>(codes[row] + code_vector(v) * 8) = row_codes(of, held[r][v]);
     }
     __syncthreads();
-  }
-  int i = 0;
-  if (deep) {
+  };
+  // (A wait behind a branch that some loads are in is for all of them: each way has its own code.)
+  if (all / kWaves >= kAhead) {
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j) request(j, j);
+    make_codes();
+    int i = 0;
     for (; i + 2 * kAhead <= pieces; i += kAhead)
 #pragma unroll
       for (int j = 0; j < kAhead; ++j) {
@@ -153,15 +157,22 @@ __global__ __launch_bounds__(64 * kFewWaves) void gemm_few_kernel(OpArgs a) {
         request(j, i + j + kAhead);
       }
 #pragma unroll
-    for (int j = 0; j < kAhead; ++j) multiply(j, i + j);
-    i += kAhead;
+    for (int j = 0; j < kAhead; ++j) {
+      multiply(j, i + j);
+      if (i + j + kAhead < pieces) request(j, i + j + kAhead);
+    }
+#pragma unroll
+    for (int j = 0; j < kAhead - 1; ++j)
+      if (i + j + kAhead < pieces) multiply(j, i + j + kAhead);
+  } else {
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j)
+      if (j < pieces) request(j, j);
+    make_codes();
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j)
+      if (j < pieces) multiply(j, j);
   }
-#pragma unroll
-  for (int j = 0; j < kAhead - 1; ++j)
-    if (i + j < pieces) request(j, i + j);
-#pragma unroll
-  for (int j = 0; j < kAhead - 1; ++j)
-    if (i + j < pieces) multiply(j, i + j);
 #pragma unroll
   for (int s = 0; s < kSides; ++s)
 #pragma unroll

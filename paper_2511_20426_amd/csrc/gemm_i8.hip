@@ -33,12 +33,13 @@ constexpr OpModel kModel[] = {{256, 256, 1, 1980, 960, 1270, 5400}, {192, 256, 1
                               {64, 64, 1, 0, 255, 190, 2000}};
 
 // Whether the codes of few tokens are made in the product's launch: they are unless making them in every workgroup costs more than the launch
-// that it saves.  Us, ahead / in the launch, weights from memory: one token 512 x 230 5.7 / 3.3, 4608 x 1536 7.5 / 5.7, 5120 x 5120 13.0 /
-// 10.1, 15360 x 5120 20.2 / 18.4; two 5120 x 5120 13.4 / 11.7, 15360 x 5120 20.6 / 21.1; three 4608 x 1537 8.5 / 9.2; four 4608 x 1536 8.0 /
-// 5.8; twelve 512 x 230 6.2 / 5.1, 4608 x 1536 8.5 / 8.0, 15360 x 64 7.2 / 8.5.
+// that it saves.  Us, ahead / in the launch, weights from memory: one token 512 x 230 5.7 / 3.1, 4608 x 1536 7.5 / 5.3, 5120 x 5120 13.0 /
+// 8.0, 15360 x 5120 20.2 / 16.1; two 5120 x 5120 13.4 / 8.9, 15360 x 5120 20.1 / 21.1; four 4608 x 1536 8.0 / 5.7, 1536 x 5120 9.2 / 8.7; twelve
+// 512 x 230 6.2 / 4.9, 4608 x 1536 8.5 / 7.7, 15360 x 512 8.0 / 8.7.
 bool codes_in_launch(int64_t M, int32_t N, int32_t K) {
-  if (K <= CodesShort::kMost) return M <= (N <= 8192 ? CodesShort::kTokens : 8);
-  return K <= CodesLong::kMost && M <= (N <= 12288 ? CodesLong::kTokens : 1);
+  if (K <= CodesTwelve::kMost) return M <= (N <= 8192 ? CodesTwelve::kTokens : 8);
+  if (K > CodesOne::kMost) return false;
+  return M == 1 || (M == 2 && N <= 12288) || (M <= CodesFour::kTokens && M * ((N + 15) / 16) * K <= 6000000);
 }
 
 // one call of any size readies all kernels for stream capture
@@ -83,7 +84,10 @@ int32_t launch_gemm_i8_values(int dtype, const void* x, int64_t ldx, const void*
                               int64_t ldw, int64_t ldy, void* workspace, void* stream) {
   if (M == 0) return CA_OK;
   if (const int32_t rc = i8_ready(); rc != CA_OK) return rc;
-  const auto kernel = K <= CodesShort::kMost ? gemm_few_kernel<I8, 1, CodesShort> : gemm_few_kernel<I8, 1, CodesLong>;
+  const auto kernel = M == 1                         ? gemm_few_kernel<I8, 1, CodesOne>
+                      : K > CodesTwelve::kMost       ? M == 2 ? gemm_few_kernel<I8, 1, CodesTwo> : gemm_few_kernel<I8, 1, CodesFour>
+                      : M <= CodesFourShort::kTokens ? gemm_few_kernel<I8, 1, CodesFourShort>
+                                                     : gemm_few_kernel<I8, 1, CodesTwelve>;
   if (dtype == CA_BF16 && K >= 8 && codes_in_launch(M, N, K)) {
     OpArgs a{};
     a.x = x; a.w = w; a.y = y; a.w2 = w_scales;
