@@ -273,7 +273,7 @@ __device__ __forceinline__ void columns_of(const U4 (&rows)[8], Bf16Products::Fr
 // lane brings 16 bytes of eight rows of W, whose columns in registers are what dX's product multiplies, and keeps the columns of X that the
 // weights' gradients multiply.  Of 16 x 16 products c = 0 .. 7 row i stands for column 8 i + c of the 128, so that a lane's results are 32
 // neighbours.  The waves' sums of dX meet in LDS, the workgroups' in the workspace.  Bound by memory as the kernel above: 16 rows of 13824 x 5120
-// 156 us (240 by the products of more rows, with their layout), of 1920 x 3840 25.6 (35.6), 32 rows 165 (246) and 27.4 (39.2); eight rows by
+// 156 us (240 by the products of more rows, with their layout), of 1920 x 3840 25.6 (35.6), 32 rows 170 (246) and 26.9 (39.2); eight rows by
 // the kernel above took 163 and 33, here 154 and 24.6.
 template <int kTiles>
 __global__ __launch_bounds__(256, 2) void gated_some_grad_kernel(GatedFewArgs a) {
@@ -283,7 +283,7 @@ __global__ __launch_bounds__(256, 2) void gated_some_grad_kernel(GatedFewArgs a)
   __shared__ __attribute__((aligned(16))) uint8_t lds[kGradBytes > kSumBytes ? kGradBytes : kSumBytes];
   uint16_t* const by_row = reinterpret_cast<uint16_t*>(lds);            // [dG | dU][row][f]
   uint16_t* const by_col = by_row + 2 * kRows * kPitch;                 // [dG | dU][f][row]
-  const int t = threadIdx.x, lane = t & 63, wave = t >> 6, l15 = lane & 15, grp = lane >> 4;
+  const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6), l15 = lane & 15, grp = lane >> 4;
   const int k0 = blockIdx.x * 128, f0 = blockIdx.y * a.each, count = min(a.each, a.F - f0);
   Frag xt[8];
   U4 w[2][8];
@@ -313,13 +313,16 @@ __global__ __launch_bounds__(256, 2) void gated_some_grad_kernel(GatedFewArgs a)
     if (a.partials) {
       Frag wt[8];
       columns_of(w[side], wt);
-      if (chunk + kChunk < count) request(side, chunk + kChunk);
+      // (with two tiles of rows there are registers for the next only behind the products: asked for here some are spilled, and 17 rows of 456 x 1024
+      // take 11.9 us for 10.9; with one, 16 rows of 13824 x 5120 took 165 us for 156 there)
+      if (kTiles == 1 && chunk + kChunk < count) request(side, chunk + kChunk);
 #pragma unroll
       for (int i = 0; i < kTiles; ++i) {
         const Frag d = *reinterpret_cast<const Frag*>(by_row + (side * kRows + 16 * i + l15) * kPitch + 32 * wave + 8 * grp);
 #pragma unroll
         for (int c = 0; c < 8; ++c) dx[c][i] = Bf16Products::multiply(wt[c], d, dx[c][i]);
       }
+      if (kTiles > 1 && chunk + kChunk < count) request(side, chunk + kChunk);
     }
     uint16_t* const dw = side ? a.dwu : a.dwg;
     if (!dw) return;
