@@ -287,7 +287,7 @@ __global__ __launch_bounds__(256, 2) void gated_some_grad_kernel(GatedFewArgs a)
   const int k0 = blockIdx.x * 128, f0 = blockIdx.y * a.each, count = min(a.each, a.F - f0);
   Frag xt[8];
   U4 w[2][8];
-  auto request = [&](int side, int chunk) {       // rows past the end re-read the last one, whose gradients there are zeros
+  auto request = [&](int side, int chunk) {       // rows past the end re-read the last one; they become zeros (it may hold an infinity)
     const int64_t ld = side ? a.ldwu : a.ldwg;
     const uint8_t* const from = reinterpret_cast<const uint8_t*>((side ? a.wu : a.wg) + (f0 + chunk) * ld + k0);
 #pragma unroll
@@ -311,6 +311,10 @@ __global__ __launch_bounds__(256, 2) void gated_some_grad_kernel(GatedFewArgs a)
     for (int i = 0; i < kTiles; ++i) dx[c][i] = f32x4{0.f, 0.f, 0.f, 0.f};
   auto multiply = [&](int side, int chunk) {
     if (a.partials) {
+      if (chunk + kChunk > count && 32 * wave + 8 * grp >= count - chunk) {       // (F and `each` are whole eights: a lane's rows exist or do not)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) w[side][e] = U4{0, 0, 0, 0};
+      }
       Frag wt[8];
       columns_of(w[side], wt);
       // (with two tiles of rows there are registers for the next only behind the products: asked for here some are spilled, and 17 rows of 456 x 1024
