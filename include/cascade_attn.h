@@ -329,8 +329,9 @@ int32_t layer_gated_bf16(const void* x_dev, const void* w_gate_dev, const void* 
                          int64_t ldh, void* hip_stream);
 size_t layer_gated_saved_bytes(int64_t m_rows, int32_t n_hidden);
 
-/* Its gradients: dg = dh u act'(g), du = dh act(g) (rounded to bf16); dx = dg . w_gate + du . w_up, dw_gate = dg' . x, dw_up = du' . x, each
- * rounded to bf16 once, written, not added to.  dx_dev, dw_gate_dev, dw_up_dev: those that are null are left out (not all).
+/* Its gradients: dg = dh u act'(g), du = dh act(g); dx = dg . w_gate + du . w_up, dw_gate = dg' . x, dw_up = du' . x, each
+ * rounded to bf16 once, written, not added to.  On the way dg and du are fp32 values of up to 4 rows, within 2^-15 of them of 5 to 32 rows, and
+ * rounded to bf16 as the products' operands from 33 rows on.  dx_dev, dw_gate_dev, dw_up_dev: those that are null are left out (not all).
  * saved_dev as layer_gated_bf16 wrote it.  workspace_dev: layer_gated_backward_workspace() bytes, 0 where the shape is not supported.
  * m_rows == 0: zero weight gradients. */
 size_t layer_gated_backward_workspace(int64_t m_rows, int32_t n_hidden, int32_t k_in);

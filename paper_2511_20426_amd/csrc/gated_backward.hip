@@ -4,13 +4,15 @@
 //
 // The products are the framework's own linear map, which multiplies rows by rows: one launch forms dG and dU from dH and the saved
 // projections, in rows (side by side, [M][2 Fp], for dX) and transposed ([2 F][Mp], for dW), and lays out X' [K][Mp] and [Wg; Wu]' [K][2 Fp]
-// in the workspace.  Fp and Mp are F and M filled up with zeros to whole steps of the products (2 Fp and Mp are multiples of 128).  dG
-// and dU are rounded to bf16, the type that the matrix products take: with the result's own rounding gradients are 2.3e-3 of their norm
-// off, 1.7e-3 of which is that of the result.  (With G and U saved in bf16 as well it was 3.1e-3: they are saved in fp32.)  dX is one
-// product over both, so that their sum is not rounded in between.
+// in the workspace.  Fp and Mp are F and M filled up with zeros to whole steps of the products (2 Fp and Mp are multiples of 128).  There dG
+// and dU are rounded to bf16, the type that the matrix products take: with the result's own rounding gradients are 2.35e-3 of their norm
+// off, 1.66e-3 of which is that of the result.  (With G and U saved in bf16 as well it was 3.1e-3: they are saved in fp32.)  In two bf16 values
+// each, as below, the products are twice as long: 4680 x 4096 x 1536 dX 92 and dW 90 us, 177 and 169 so.  dX is one product over both, so that
+// their sum is not rounded in between.
 //
 // Of up to 32 rows all of it is one pass over the weights, read once, and their gradients, written once, with nothing laid out
-// (gated_few_grad_kernel, gated_some_grad_kernel).
+// (gated_few_grad_kernel, gated_some_grad_kernel), bound by memory: dG and dU go into the products in fp32 (up to four rows) or as two bf16 values
+// each, which stand for 16 bits and more, and gradients are 1.66e-3 of their norm off, the rounding of the result.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -268,21 +270,36 @@ __device__ __forceinline__ void columns_of(const U4 (&rows)[8], Bf16Products::Fr
   }
 }
 
+// The larger part of a value that is cut to bf16, and what that leaves over: as two operands of the matrix pipe they stand for 16 bits of the
+// value and more (the rest is rounded to bf16, half a step of 2^-7 of it).  Of a value that bf16 holds the rest is 2^-24 of it instead of zero, and
+// of an infinity an infinity, so that an infinite weight or activation meets two factors of one sign and not a zero.
+__device__ __forceinline__ float rest_of(float v) {
+  return copysignf(fmaxf(fabsf(v - __uint_as_float(__float_as_uint(v) & 0xffff0000u)), fabsf(v) * 0x1p-24f), v);
+}
+__device__ __forceinline__ uint2 cut_bf16(const float (&v)[4]) {
+  return uint2{__builtin_amdgcn_perm(__float_as_uint(v[1]), __float_as_uint(v[0]), 0x07060302), __builtin_amdgcn_perm(__float_as_uint(v[3]), __float_as_uint(v[2]), 0x07060302)};
+}
+
 // Up to 32 rows, on the matrix pipe, still one pass over the weights and their gradients with nothing laid out.  A workgroup takes 128 columns
-// of K and `each` columns f in chunks of 128, whose dG and dU it forms in LDS in bf16, by rows and by columns; each wave takes 32 of a chunk.  A
+// of K and `each` columns f in chunks of 128, whose dG and dU it forms in LDS, in two parts of bf16, by rows and by columns; each wave takes 32 of a chunk.  A
 // lane brings 16 bytes of eight rows of W, whose columns in registers are what dX's product multiplies, and keeps the columns of X that the
 // weights' gradients multiply.  Of 16 x 16 products c = 0 .. 7 row i stands for column 8 i + c of the 128, so that a lane's results are 32
 // neighbours.  The waves' sums of dX meet in LDS, the workgroups' in the workspace.  Bound by memory as the kernel above: 16 rows of 13824 x 5120
-// 156 us (240 by the products of more rows, with their layout), of 1920 x 3840 25.6 (35.6), 32 rows 170 (246) and 26.9 (39.2); eight rows by
-// the kernel above took 163 and 33, here 154 and 24.6.
+// 160 us (240 by the products of more rows, with their layout), of 1920 x 3840 26.8 (35.6), 32 rows 174 (246) and 27.8 (39.2); eight rows by
+// the kernel above took 163 and 33, here 160 and 25.9.  The parts' products and LDS are 1 us of the small ones (rounded to bf16 instead 156, 25.8,
+// 170, 27.2, 155, 24.9).
+template <int kTiles>
+constexpr int kSomeGradLds = 8 * (16 * kTiles * 136 + 128 * 40);       // 57 and 74 KB: two workgroups to a CU
+
 template <int kTiles>
 __global__ __launch_bounds__(256, 2) void gated_some_grad_kernel(GatedFewArgs a) {
   using Frag = Bf16Products::Frag;
   constexpr int kChunk = 128, kRows = 16 * kTiles, kPitch = kChunk + 8, kColPitch = 32 + 8, kSumPitch = 128 + 4;
-  constexpr int kGradBytes = 2 * 2 * (kRows * kPitch + kChunk * kColPitch), kSumBytes = 4 * 16 * kSumPitch * 4;
-  __shared__ __attribute__((aligned(16))) uint8_t lds[kGradBytes > kSumBytes ? kGradBytes : kSumBytes];
-  uint16_t* const by_row = reinterpret_cast<uint16_t*>(lds);            // [dG | dU][row][f]
-  uint16_t* const by_col = by_row + 2 * kRows * kPitch;                 // [dG | dU][f][row]
+  static_assert(kSomeGradLds<kTiles> == 2 * 2 * 2 * (kRows * kPitch + kChunk * kColPitch) && kSomeGradLds<kTiles> >= 4 * 16 * kSumPitch * 4,
+                "the sums take the gradients' place");
+  extern __shared__ __attribute__((aligned(16))) uint8_t some_lds[];
+  uint16_t* const by_row = reinterpret_cast<uint16_t*>(some_lds);            // [dG | dU][cut | rest][row][f]
+  uint16_t* const by_col = by_row + 2 * 2 * kRows * kPitch;             // [dG | dU][cut | rest][f][row]
   const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6), l15 = lane & 15, grp = lane >> 4;
   const int k0 = blockIdx.x * 128, f0 = blockIdx.y * a.each, count = min(a.each, a.F - f0);
   Frag xt[8];
@@ -321,10 +338,10 @@ __global__ __launch_bounds__(256, 2) void gated_some_grad_kernel(GatedFewArgs a)
       // take 11.9 us for 10.9; with one, 16 rows of 13824 x 5120 took 165 us for 156 there)
       if (kTiles == 1 && chunk + kChunk < count) request(side, chunk + kChunk);
 #pragma unroll
-      for (int i = 0; i < kTiles; ++i) {
-        const Frag d = *reinterpret_cast<const Frag*>(by_row + (side * kRows + 16 * i + l15) * kPitch + 32 * wave + 8 * grp);
+      for (int i = 0; i < 2 * kTiles; ++i) {
+        const Frag d = *reinterpret_cast<const Frag*>(by_row + ((2 * side + i % 2) * kRows + 16 * (i / 2) + l15) * kPitch + 32 * wave + 8 * grp);
 #pragma unroll
-        for (int c = 0; c < 8; ++c) dx[c][i] = Bf16Products::multiply(wt[c], d, dx[c][i]);
+        for (int c = 0; c < 8; ++c) dx[c][i / 2] = Bf16Products::multiply(wt[c], d, dx[c][i / 2]);
       }
       if (kTiles > 1 && chunk + kChunk < count) request(side, chunk + kChunk);
     }
@@ -334,10 +351,13 @@ __global__ __launch_bounds__(256, 2) void gated_some_grad_kernel(GatedFewArgs a)
     for (int half = 0; half < 2; ++half) {
       const int in = 32 * wave + 16 * half + l15;
       __builtin_amdgcn_sched_barrier(0);          // (parts that run into each other need more registers than there are)
-      const Frag d = *reinterpret_cast<const Frag*>(by_col + (side * kChunk + in) * kColPitch + 8 * grp);
+      const uint16_t* const from = by_col + (2 * side * kChunk + in) * kColPitch + 8 * grp;
+      const Frag cut = *reinterpret_cast<const Frag*>(from), rest = *reinterpret_cast<const Frag*>(from + kChunk * kColPitch);
       f32x4 o[8];
 #pragma unroll
-      for (int c = 0; c < 8; ++c) o[c] = Bf16Products::multiply(xt[c], d, f32x4{0.f, 0.f, 0.f, 0.f});
+      for (int c = 0; c < 8; ++c) o[c] = Bf16Products::multiply(xt[c], cut, f32x4{0.f, 0.f, 0.f, 0.f});
+#pragma unroll
+      for (int c = 0; c < 8; ++c) o[c] = Bf16Products::multiply(xt[c], rest, o[c]);
       if (chunk + in < count) {
         uint16_t* const to = dw + int64_t(f0 + chunk + in) * a.lddw + k0 + 32 * grp;
 #pragma unroll
@@ -350,31 +370,31 @@ __global__ __launch_bounds__(256, 2) void gated_some_grad_kernel(GatedFewArgs a)
     if (chunk > 0) __syncthreads();
     for (int i = t; i < 32 * (kChunk / 4); i += 256) {
       const int m = i % 32, f = i / 32 * 4, n = f0 + chunk + f;
-      uint2 dg = {0, 0}, du = {0, 0};
+      float dg[4] = {}, du[4] = {};
       if (m < a.M && chunk + f < count) {
         const int64_t at = saved_at(m, n, a.F);
         const f32x4 g = *reinterpret_cast<const f32x4*>(a.g + at), u = *reinterpret_cast<const f32x4*>(a.u + at);
         const uint2 dh2 = *reinterpret_cast<const uint2*>(a.dh + int64_t(m) * a.lddh + n);
         const float dh[4] = {bf16_lo(dh2.x), bf16_hi(dh2.x), bf16_lo(dh2.y), bf16_hi(dh2.y)};
-        float v[4], s[4];
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
           float act, slope;
           activation(g[j], a.act0, a.act1, &act, &slope);
-          v[j] = dh[j] * u[j] * slope;
-          s[j] = dh[j] * act;
+          dg[j] = dh[j] * u[j] * slope;
+          du[j] = dh[j] * act;
         }
-        dg = uint2{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
-        du = uint2{pack_bf16(s[0], s[1]), pack_bf16(s[2], s[3])};
-      }
-      if (m < kRows) {
-        *reinterpret_cast<uint2*>(by_row + m * kPitch + f) = dg;
-        *reinterpret_cast<uint2*>(by_row + (kRows + m) * kPitch + f) = du;
       }
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        by_col[(f + j) * kColPitch + m] = uint16_t((j & 2 ? dg.y : dg.x) >> (j & 1 ? 16 : 0));
-        by_col[(kChunk + f + j) * kColPitch + m] = uint16_t((j & 2 ? du.y : du.x) >> (j & 1 ? 16 : 0));
+      for (int side = 0; side < 2; ++side) {
+        const float(&d)[4] = side ? du : dg;
+        const uint2 part[2] = {cut_bf16(d), uint2{pack_bf16(rest_of(d[0]), rest_of(d[1])), pack_bf16(rest_of(d[2]), rest_of(d[3]))}};
+#pragma unroll
+        for (int p = 0; p < 2; ++p) {
+          if (m < kRows) *reinterpret_cast<uint2*>(by_row + ((2 * side + p) * kRows + m) * kPitch + f) = part[p];
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+            by_col[((2 * side + p) * kChunk + f + j) * kColPitch + m] = uint16_t((j & 2 ? part[p].y : part[p].x) >> (j & 1 ? 16 : 0));
+        }
       }
     }
     __syncthreads();
@@ -383,7 +403,7 @@ __global__ __launch_bounds__(256, 2) void gated_some_grad_kernel(GatedFewArgs a)
     multiply(1, chunk);
   }
   if (!a.partials) return;
-  float* const sums = reinterpret_cast<float*>(lds);                    // [wave][row of 16][128]
+  float* const sums = reinterpret_cast<float*>(some_lds);               // [wave][row of 16][128]
 #pragma unroll
   for (int i = 0; i < kTiles; ++i) {
     if (16 * i >= a.M) break;
@@ -443,10 +463,10 @@ int32_t launch_few_grad(GatedFewArgs a, void* dx, int64_t lddx, void* stream) {
   const unsigned parts = unsigned((a.F + a.each - 1) / a.each);
   hipStream_t s = static_cast<hipStream_t>(stream);
   const dim3 grid(unsigned(a.K / 128), parts);
-    if (a.M > 16)
-    hipLaunchKernelGGL(gated_some_grad_kernel<2>, grid, dim3(256), 0, s, a);
+  if (a.M > 16)
+    hipLaunchKernelGGL(gated_some_grad_kernel<2>, grid, dim3(256), kSomeGradLds<2>, s, a);
   else if (a.M > kFewGradRows)
-    hipLaunchKernelGGL(gated_some_grad_kernel<1>, grid, dim3(256), 0, s, a);
+    hipLaunchKernelGGL(gated_some_grad_kernel<1>, grid, dim3(256), kSomeGradLds<1>, s, a);
   else
     hipLaunchKernelGGL(gated_few_grad_kernel, grid, dim3(256), unsigned(std::max(a.each * 2, 4 * 128) * kFewGradRows * 4), s, a);      // up to 16 KB of LDS
   if (const int32_t rc = finish_launch("gated_backward.hip"); rc != CA_OK || !dx) return rc;
@@ -529,8 +549,10 @@ int32_t launch_gated_backward(const void* dh, const void* x, const void* w_gate,
   float act0, act1;
   activation_factors(activation, &act0, &act1);
   // (one call of any size readies all of them for stream capture)
-  const KernelLds kernel[] = {{reinterpret_cast<const void*>(gemm_op_kernel<Tile64Wide, PlainPart>), Tile64Wide::kLds}};
-  if (const int32_t rc = ensure_dynamic_lds(kernel, 1, kLdsGatedBackward); rc != CA_OK) return rc;
+  const KernelLds kernels[] = {{reinterpret_cast<const void*>(gemm_op_kernel<Tile64Wide, PlainPart>), Tile64Wide::kLds},
+                               {reinterpret_cast<const void*>(gated_some_grad_kernel<1>), kSomeGradLds<1>},
+                               {reinterpret_cast<const void*>(gated_some_grad_kernel<2>), kSomeGradLds<2>}};
+  if (const int32_t rc = ensure_dynamic_lds(kernels, 3, kLdsGatedBackward); rc != CA_OK) return rc;
   if (const int32_t rc = gemm_tiles_ready(); rc != CA_OK) return rc;
   if (const int32_t rc = gemm_rows_ready(); rc != CA_OK) return rc;
   if (M > 0 && M <= kSomeGradRows) {

@@ -4,7 +4,7 @@ import pytest
 import torch
 
 from paper_2511_20426_amd import binding as B
-from tests.test_layer_ops import DEV, _act, _gen, _normal
+from tests.test_layer_ops import DEV, _act, _gen, _kept, _normal
 
 
 def _given_gradients(g, u, dh, act):
@@ -33,3 +33,77 @@ def test_an_infinity_in_the_last_row_of_weights(M, F, which):
     assert (d != 0).all() and (dx[:, 5] == d.sign() * float("inf")).all()
     dx[:, 5] = 0
     assert all(t.isfinite().all() for t in (dx, dwg, dwu))
+
+
+def _given_saved(M, F, K, act, seed):
+    """inputs of a backward pass and dg, du of the projections that it is given, in 64 bits"""
+    from paper_2511_20426_amd.runner import gated_linear_train
+    gen = _gen(seed)
+    x, wg, wu, dh = _normal(gen, M, K), _normal(gen, F, K, scale=2 * K ** -0.5), _normal(gen, F, K, scale=K ** -0.5), _normal(gen, M, F)
+    _, saved = gated_linear_train(x, wg, wu, act)
+    g, u = (t.double().cpu() for t in _kept(saved, M, F))
+    return x, wg, wu, dh, saved, g, u
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("act", ["silu", "gelu"])
+@pytest.mark.parametrize("M,F,K", [(1, 8, 128), (4, 72, 256), (4, 200, 128), (5, 8, 128), (5, 64, 256), (8, 136, 128), (9, 264, 128), (16, 40, 384), (17, 8, 128),
+                                   (24, 200, 256), (32, 64, 128), (32, 392, 128)])
+def test_gradients_of_few_rows_keep_their_bits(M, F, K, act):
+    """Of up to four rows dg and du go into the products in fp32, of 5 to 32 as two bf16 values each: within 2^-15 of themselves."""
+    from paper_2511_20426_amd.runner import gated_linear_backward
+    x, wg, wu, dh, saved, g, u = _given_saved(M, F, K, act, M + F + K)
+    dg, du = _given_gradients(g, u, dh.double().cpu(), act)
+    # in fp32: some 16 roundings of 2^-24 and the exponent's (p 2^-23, |p| < 64 at these gates) of terms of the size of dh u and of du; the cut and
+    # rest of a value: the rest is below 2^-7 of it and half a step, 2^-8, off
+    cut = 2.0 ** -15 if M > 4 else 0.0
+    ddg, ddu = 2.0 ** -17 * (dh.double().cpu() * u).abs() + cut * dg.abs(), (2.0 ** -17 + cut) * du.abs()
+    xd, gd, ud = (t.double().cpu() for t in (x, wg, wu))
+    refs = ((dg @ gd + du @ ud, ddg @ gd.abs() + ddu @ ud.abs(), dg.abs() @ gd.abs() + du.abs() @ ud.abs()),
+            (dg.T @ xd, ddg.T @ xd.abs(), dg.abs().T @ xd.abs()), (du.T @ xd, ddu.T @ xd.abs(), du.abs().T @ xd.abs()))
+    for t, (ref, off, size) in zip(gated_linear_backward(dh, x, wg, wu, saved, act), refs):
+        # one rounding of the result, fp32 sums of at most 784 products (1e-5 is the linear maps' allowance for 5120)
+        assert ((t.double().cpu() - ref).abs() <= ref.abs() * 2.0 ** -8 + off + 1e-5 * size + 1e-30).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("M", [3, 8, 20, 40])
+def test_infinities_meet_gradients_that_bf16_holds(M):
+    """dg of 1/2, 2 and the like, which leave no rest: infinite weights and activations give infinities of their sign, not NaN; gradients of zero give
+    NaN with them, as the formula does."""
+    from paper_2511_20426_amd.runner import gated_linear_backward
+    F, K = 24, 128
+    dh = torch.tensor([1.0, -4.0, 0.25], device=DEV, dtype=torch.bfloat16)[torch.arange(M * F, device=DEV) % 3].view(M, F).contiguous()
+    dh[:, 7] = 0
+    half = B.layer_gated_saved_bytes(M, F) // 8
+    saved = torch.cat((torch.zeros(half, device=DEV), torch.ones(half, device=DEV)))         # g = 0, u = 1: dg = dh / 2, du = 0
+    gen = _gen(M)
+    x, wg, wu = _normal(gen, M, K), _normal(gen, F, K), _normal(gen, F, K)
+    x[1, 9], wg[3, 5], wg[4, 6], wg[7, 8] = float("inf"), float("inf"), float("-inf"), float("inf")
+    dx, dwg, dwu = (t.double().cpu() for t in gated_linear_backward(dh, x, wg, wu, saved))
+    d, inf = dh.double().cpu(), float("inf")
+    assert (dx[:, 5] == d[:, 3].sign() * inf).all() and (dx[:, 6] == d[:, 4].sign() * -inf).all() and dx[:, 8].isnan().all()
+    keep = torch.ones(F, dtype=torch.bool)
+    keep[7] = False
+    assert (dwg[keep, 9] == d[1, keep].sign() * inf).all() and dwg[7, 9].isnan() and dwu[:, 9].isnan().all()
+    for t, cols in ((dx, [5, 6, 8]), (dwg, [9]), (dwu, [9])):
+        t[:, cols] = 0
+        assert t.isfinite().all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("M", [3, 8, 20, 40])
+@pytest.mark.parametrize("value", [float("nan"), float("inf"), float("-inf")])
+def test_gradients_from_above_that_are_not_finite(M, value):
+    """... reach the rows of dX and the columns f of the weights' gradients that they belong to, and no others."""
+    from paper_2511_20426_amd.runner import gated_linear_backward
+    F, K = 136, 128
+    x, wg, wu, dh, saved, g, u = _given_saved(M, F, K, "silu", 5)
+    dh[2, 131] = value
+    dg, du = _given_gradients(g, u, dh.double().cpu(), "silu")
+    dx, dwg, dwu = (t.double().cpu() for t in gated_linear_backward(dh, x, wg, wu, saved))
+    rows, cols = torch.arange(M) == 2, torch.arange(F) == 131
+    assert dx[~rows].isfinite().all() and not dx[rows].isfinite().any()
+    for t, d in ((dwg, dg), (dwu, du)):
+        ref = d[2, 131] * x[2].double().cpu()
+        assert t[~cols].isfinite().all() and (t[cols][0].isnan() if value != value else t[cols][0] == ref).all()
