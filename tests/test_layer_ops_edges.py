@@ -4,7 +4,7 @@ import pytest
 import torch
 
 from paper_2511_20426_amd import binding as B
-from tests.test_layer_ops import DEV, _act, _gen, _kept, _normal
+from tests.test_layer_ops import DEV, _act, _gated_grads, _gen, _kept, _normal
 
 
 def _given_gradients(g, u, dh, act):
@@ -107,3 +107,52 @@ def test_gradients_from_above_that_are_not_finite(M, value):
     for t, d in ((dwg, dg), (dwu, du)):
         ref = d[2, 131] * x[2].double().cpu()
         assert t[~cols].isfinite().all() and (t[cols][0].isnan() if value != value else t[cols][0] == ref).all()
+
+
+def _parts_bytes(M, F, K):
+    """what the workspace has behind the layout: room for the sums of products that are walked in parts"""
+    up = lambda n, to: -(-n // to) * to  # noqa: E731
+    rows, cols = up(M, 128), up(F, 64)
+    return B.layer_gated_backward_workspace(M, F, K) - sum(up(2 * n, 256) for n in (M * 2 * cols, 2 * F * rows, K * rows, K * 2 * cols))
+
+
+# dX in 8, 14 and 4 parts, weights' gradients in 11 and 6 (a last part that is shorter among them), rows and columns that
+# end inside a tile (asserted, so that another model does not drop them)
+IN_PARTS = [(100, 2000, 128), (65, 4008, 256), (4000, 40, 128), (3325, 64, 256), (777, 3000, 128)]
+
+
+@pytest.mark.parametrize("M,F,K", IN_PARTS)
+def test_which_products_are_walked_in_parts(M, F, K):
+    assert _parts_bytes(M, F, K) > 0
+    assert _parts_bytes(130, 1000, 640) == 0
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("act", ["silu", "gelu"])
+@pytest.mark.parametrize("M,F,K", IN_PARTS)
+def test_gradients_by_products_in_parts(M, F, K, act):
+    """Element by element; then each of the three alone, both weights' apart (their parts take the same room, one after the other), into strides:
+    dX has the same bits, the weights' (which may be walked in other parts than as one product) the same bounds; nothing beside them is written."""
+    from paper_2511_20426_amd.runner import gated_linear_backward, gated_linear_train
+    gen = _gen(M + F + K)
+    x, wg, wu = _normal(gen, M, K + 8)[:, :K], _normal(gen, F, K + 16, scale=2 * K ** -0.5)[:, :K], _normal(gen, F, K, scale=K ** -0.5)
+    dh = _normal(gen, M, F + 8)[:, :F]
+    _, saved = gated_linear_train(x, wg, wu, act)
+    whole = gated_linear_backward(dh, x, wg, wu, saved, act)
+    refs = _gated_grads(*(t.double().cpu() for t in (x, wg, wu, dh)), act)
+    for t, (ref, bound) in zip(whole, refs):
+        assert ((t.double().cpu() - ref).abs() <= bound).all()
+    nbytes = B.layer_gated_backward_workspace(M, F, K)
+    work = torch.empty(nbytes + 4096, dtype=torch.uint8, device=DEV)
+    for asked in ((1, 0, 0), (0, 1, 0), (0, 0, 1), (0, 1, 1), (1, 1, 1)):
+        out = [torch.full((n + 2, K + 8), 7.0, dtype=torch.bfloat16, device=DEV) for n in (M, F, F)]
+        work.fill_(0x55)
+        B.layer_gated_backward_bf16(dh.data_ptr(), x.data_ptr(), wg.data_ptr(), wu.data_ptr(), saved.data_ptr(), B.CA_GELU if act == "gelu" else B.CA_SILU,
+                                    *(t.data_ptr() if a else 0 for t, a in zip(out, asked)), M, F, K, F + 8, K + 8, K + 16, K, K + 8, K + 8, work.data_ptr(),
+                                    nbytes, torch.cuda.current_stream().cuda_stream)
+        assert (work[nbytes:] == 0x55).all()
+        assert not asked[0] or (out[0][:M, :K] == whole[0]).all()
+        for t, (ref, bound), a in zip(out, refs, asked):
+            n = ref.shape[0]
+            assert ((t[:n, :K].double().cpu() - ref).abs() <= bound).all() if a else (t[:n, :K] == 7).all()
+            assert (t[n:] == 7).all() and (t[:, K:] == 7).all()
