@@ -285,13 +285,19 @@ __device__ __forceinline__ uint2 cut_bf16(const float (&v)[4]) {
 // lane brings 16 bytes of eight rows of W, whose columns in registers are what dX's product multiplies, and keeps the columns of X that the
 // weights' gradients multiply.  Of 16 x 16 products c = 0 .. 7 row i stands for column 8 i + c of the 128, so that a lane's results are 32
 // neighbours.  The waves' sums of dX meet in LDS, the workgroups' in the workspace.  Bound by memory as the kernel above: 16 rows of 13824 x 5120
-// 160 us (240 by the products of more rows, with their layout), of 1920 x 3840 26.8 (35.6), 32 rows 174 (246) and 27.8 (39.2); eight rows by
-// the kernel above took 163 and 33, here 160 and 25.9.  The parts' products and LDS are 1 us of the small ones (rounded to bf16 instead 156, 25.8,
-// 170, 27.2, 155, 24.9).
+// 160 us (240 by the products of more rows, with their layout), of 1920 x 3840 26.8 (35.6), 32 rows 170 (246) and 27.6 (39.2); eight rows by
+// the kernel above took 163 and 33, here 160 and 25.9.  The parts' products and LDS are 1 us of the small ones and 5 of the large (rounded to bf16
+// instead 156, 25.8, 165, 27.2, 155, 24.9).
 template <int kTiles>
 constexpr int kSomeGradLds = 8 * (16 * kTiles * 136 + 128 * 40);       // 57 and 74 KB: two workgroups to a CU
 
-template <int kTiles>
+// kEarly: a chunk's weights are asked for ahead of the products of the chunk before, else behind those of dX, where their registers are free.  With
+// two tiles of rows some registers are spilled for it, which pays in long walks only; us, 17 rows early / late: 456 x 1024 (one chunk) 12.7 /
+// 11.7, 8192 x 1536 (two) 39.8 / 39.0, 13824 x 2048 (four) 67.2 / 64.3, 6912 x 5120 (five) 91.7 / 93.8, 13824 x 5120 (nine) 167 / 170.  With one
+// nothing is spilled: 8 rows of 13824 x 2048 65.2 / 63.4, of 6912 x 5120 88 / 91, of 13824 x 5120 160 / 169.
+constexpr int kEarlyFrom = 5 * 128;               // columns f of a workgroup
+
+template <int kTiles, bool kEarly>
 __global__ __launch_bounds__(256, 2) void gated_some_grad_kernel(GatedFewArgs a) {
   using Frag = Bf16Products::Frag;
   constexpr int kChunk = 128, kRows = 16 * kTiles, kPitch = kChunk + 8, kColPitch = 32 + 8, kSumPitch = 128 + 4;
@@ -307,9 +313,9 @@ __global__ __launch_bounds__(256, 2) void gated_some_grad_kernel(GatedFewArgs a)
   auto request = [&](int side, int chunk) {       // rows past the end re-read the last one; they become zeros (it may hold an infinity)
     const int64_t ld = side ? a.ldwu : a.ldwg;
     const uint8_t* const from = reinterpret_cast<const uint8_t*>((side ? a.wu : a.wg) + (f0 + chunk) * ld + k0);
+    const uint32_t at = uint32_t(min(32 * wave + 8 * grp, a.F - 8 - f0 - chunk)) * uint32_t(2 * ld) + 16u * l15;      // (128 rows of 2^22 values are 2^30 bytes)
 #pragma unroll
-    for (int e = 0; e < 8; ++e)                   // (128 rows of 2^22 values are 2^30 bytes)
-      w[side][e] = *reinterpret_cast<const U4*>(from + uint32_t(min(32 * wave + 8 * grp + e, a.F - 1 - f0 - chunk)) * uint32_t(2 * ld) + 16u * l15);
+    for (int e = 0; e < 8; ++e) w[side][e] = *reinterpret_cast<const U4*>(from + 2 * e * ld + at);
   };
   {
     U4 x[8];
@@ -334,16 +340,14 @@ __global__ __launch_bounds__(256, 2) void gated_some_grad_kernel(GatedFewArgs a)
       }
       Frag wt[8];
       columns_of(w[side], wt);
-      // (with two tiles of rows there are registers for the next only behind the products: asked for here some are spilled, and 17 rows of 456 x 1024
-      // take 11.9 us for 10.9; with one, 16 rows of 13824 x 5120 took 165 us for 156 there)
-      if (kTiles == 1 && chunk + kChunk < count) request(side, chunk + kChunk);
+      if (kEarly && chunk + kChunk < count) request(side, chunk + kChunk);
 #pragma unroll
       for (int i = 0; i < 2 * kTiles; ++i) {
         const Frag d = *reinterpret_cast<const Frag*>(by_row + ((2 * side + i % 2) * kRows + 16 * (i / 2) + l15) * kPitch + 32 * wave + 8 * grp);
 #pragma unroll
         for (int c = 0; c < 8; ++c) dx[c][i / 2] = Bf16Products::multiply(wt[c], d, dx[c][i / 2]);
       }
-      if (kTiles > 1 && chunk + kChunk < count) request(side, chunk + kChunk);
+      if (!kEarly && chunk + kChunk < count) request(side, chunk + kChunk);
     }
     uint16_t* const dw = side ? a.dwu : a.dwg;
     if (!dw) return;
@@ -463,10 +467,12 @@ int32_t launch_few_grad(GatedFewArgs a, void* dx, int64_t lddx, void* stream) {
   const unsigned parts = unsigned((a.F + a.each - 1) / a.each);
   hipStream_t s = static_cast<hipStream_t>(stream);
   const dim3 grid(unsigned(a.K / 128), parts);
-  if (a.M > 16)
-    hipLaunchKernelGGL(gated_some_grad_kernel<2>, grid, dim3(256), kSomeGradLds<2>, s, a);
+  if (a.M > 16 && a.each >= kEarlyFrom)
+    hipLaunchKernelGGL((gated_some_grad_kernel<2, true>), grid, dim3(256), kSomeGradLds<2>, s, a);
+  else if (a.M > 16)
+    hipLaunchKernelGGL((gated_some_grad_kernel<2, false>), grid, dim3(256), kSomeGradLds<2>, s, a);
   else if (a.M > kFewGradRows)
-    hipLaunchKernelGGL(gated_some_grad_kernel<1>, grid, dim3(256), kSomeGradLds<1>, s, a);
+    hipLaunchKernelGGL((gated_some_grad_kernel<1, true>), grid, dim3(256), kSomeGradLds<1>, s, a);
   else
     hipLaunchKernelGGL(gated_few_grad_kernel, grid, dim3(256), unsigned(std::max(a.each * 2, 4 * 128) * kFewGradRows * 4), s, a);      // up to 16 KB of LDS
   if (const int32_t rc = finish_launch("gated_backward.hip"); rc != CA_OK || !dx) return rc;
@@ -550,9 +556,10 @@ int32_t launch_gated_backward(const void* dh, const void* x, const void* w_gate,
   activation_factors(activation, &act0, &act1);
   // (one call of any size readies all of them for stream capture)
   const KernelLds kernels[] = {{reinterpret_cast<const void*>(gemm_op_kernel<Tile64Wide, PlainPart>), Tile64Wide::kLds},
-                               {reinterpret_cast<const void*>(gated_some_grad_kernel<1>), kSomeGradLds<1>},
-                               {reinterpret_cast<const void*>(gated_some_grad_kernel<2>), kSomeGradLds<2>}};
-  if (const int32_t rc = ensure_dynamic_lds(kernels, 3, kLdsGatedBackward); rc != CA_OK) return rc;
+                               {reinterpret_cast<const void*>(gated_some_grad_kernel<1, true>), kSomeGradLds<1>},
+                               {reinterpret_cast<const void*>(gated_some_grad_kernel<2, false>), kSomeGradLds<2>},
+                               {reinterpret_cast<const void*>(gated_some_grad_kernel<2, true>), kSomeGradLds<2>}};
+  if (const int32_t rc = ensure_dynamic_lds(kernels, 4, kLdsGatedBackward); rc != CA_OK) return rc;
   if (const int32_t rc = gemm_tiles_ready(); rc != CA_OK) return rc;
   if (const int32_t rc = gemm_rows_ready(); rc != CA_OK) return rc;
   if (M > 0 && M <= kSomeGradRows) {

@@ -156,3 +156,17 @@ def test_gradients_by_products_in_parts(M, F, K, act):
             n = ref.shape[0]
             assert ((t[:n, :K].double().cpu() - ref).abs() <= bound).all() if a else (t[:n, :K] == 7).all()
             assert (t[n:] == 7).all() and (t[:, K:] == 7).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("M,F,K", [(8, 6920, 5120), (17, 6920, 5120), (32, 2568, 16384), (32, 4000, 5120)])
+def test_gradients_of_some_rows_in_long_walks(M, F, K):
+    """Workgroups of 4 to 6 chunks of columns, the last of which ends inside a chunk (references in 64 bits on the device)."""
+    from paper_2511_20426_amd.runner import gated_linear_backward, gated_linear_train
+    gen = torch.Generator(device=DEV).manual_seed(M)
+    x, wg, wu, dh = (torch.randn(*s, generator=gen, device=DEV).mul_(scale).to(torch.bfloat16)
+                     for s, scale in (((M, K), 1), ((F, K), 2 * K ** -0.5), ((F, K), K ** -0.5), ((M, F), 1)))
+    _, saved = gated_linear_train(x, wg, wu)
+    got = gated_linear_backward(dh, x, wg, wu, saved)
+    for t, (ref, bound) in zip(got, _gated_grads(*(t.double() for t in (x, wg, wu, dh)), "silu")):
+        assert ((t.double() - ref).abs() <= bound).all()
