@@ -362,6 +362,7 @@ def linear_i8(x: torch.Tensor | QuantizedRows, w: QuantizedRows, out: torch.Tens
     if r is not None:
         return r
     n, k, device = w.shape[0], w.k, w.codes.device
+    assert w.codes.is_cuda
     m = x.shape[0]
     y = torch.empty((m, n), dtype=_BF16, device=device) if out is None else out
     ldw, ldy = w.codes.shape[1] if n <= 1 else w.codes.stride(0), _matrix(y, w.codes, _BF16, m, n)

@@ -170,3 +170,16 @@ def test_gradients_of_some_rows_in_long_walks(M, F, K):
     got = gated_linear_backward(dh, x, wg, wu, saved)
     for t, (ref, bound) in zip(got, _gated_grads(*(t.double() for t in (x, wg, wu, dh)), "silu")):
         assert ((t.double() - ref).abs() <= bound).all()
+
+
+def test_codes_in_host_memory_reach_no_kernel(monkeypatch):
+    """Weights and tokens in 8 bits that both lie in host memory (a checkpoint's, not yet moved) are refused, not handed on by their addresses."""
+    from paper_2511_20426_amd import runner as R
+    monkeypatch.setattr(B, "layer_linear_i8", lambda *a: pytest.fail("a host address went to the library"))
+    monkeypatch.setattr(R, "_current_stream", lambda device: 0)
+    x, w = (R.QuantizedRows.from_codes(torch.ones((n, 300), dtype=torch.int8), torch.ones(n)) for n in (4, 16))
+    for out in (None, torch.empty((4, 16), dtype=torch.bfloat16)):
+        with pytest.raises(AssertionError):
+            R.linear_i8(x, w, out=out)
+    with pytest.raises(AssertionError):
+        R.linear_i8(torch.ones((4, 300), dtype=torch.bfloat16), w)
