@@ -273,7 +273,8 @@ typedef struct {
 /* Per-head RMS norm and the rotation of rope3d_apply in one pass: of each head's head_dim values x,
  * y = weight * x / sqrt(mean(x^2) + eps), then y rotated by its token's position.  n_tokens tokens that are consecutive in the
  * video, from the first token of latent frame first_frame on.  q or k may be null (with the outputs and weights that belong to
- * it); both go in one launch.  Weights: head_dim values of the context's type.  In fp32, rounded once.  An output may be its
+ * it); both go in one launch.  Weights: head_dim values of the context's type.  In fp32, rounded once, for x of any size that
+ * the type holds (means of squares beyond fp32's range too).  An output may be its
  * own input (then with its strides) and overlaps nothing else.  eps >= 0; a head of zeros gives zeros for eps > 0.  Frames and tokens
  * that pass 2^31 are CA_EUNSUPPORTED. */
 int32_t layer_qk_norm_rope(const ca_ctx* ctx, const ca_heads* q, const ca_heads* k, const void* q_weight_dev, const void* k_weight_dev,

@@ -18,19 +18,35 @@ __device__ __forceinline__ float head_sum(float x, int chunks) {
   return chunks == 16 ? sixteen : (chunks == 8 ? eight : x);
 }
 
-// 1 / sqrt(mean(x^2) + eps) of the head that the lane's eight values are part of
+// mean(x^2) + eps of the head that the lane's eight values are part of
 template <typename T>
-__device__ __forceinline__ float head_rstd(const Vec8<T>& x, int chunks, float eps) {
+__device__ __forceinline__ float head_mean(const Vec8<T>& x, int chunks, float eps) {
   float s = 0.f;
 #pragma unroll
   for (int j = 0; j < 8; ++j) s = fmaf(x.v[j], x.v[j], s);
-  return 1.f / sqrtf(fmaf(head_sum(s, chunks), 1.f / float(8 * chunks), eps));
+  return fmaf(head_sum(s, chunks), 1.f / float(8 * chunks), eps);
+}
+
+// 1 / sqrt(mean(x^2) + eps) of x times `by`: 1, or of a head whose squares leave fp32's range (values of 1e19, or of 1e-19 beside a small eps) a power
+// of two that brings x back into it first.  (All lanes of a head take the same way, and the sums read no others'.)
+template <typename T>
+__device__ __forceinline__ float head_rstd(Vec8<T>& x, int chunks, float eps, float* by) {
+  float mean = head_mean(x, chunks, eps);
+  *by = 1.f;
+  if (__builtin_expect(!(mean >= 0x1p-90f && mean <= 0x1p100f), 0)) {
+    *by = mean > 1.f ? 0x1p-72f : 0x1p90f;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) x.v[j] *= *by;
+    mean = head_mean(x, chunks, eps * *by * *by);
+  }
+  return 1.f / sqrtf(mean);
 }
 
 // x <- w x / sqrt(mean(x^2) + eps), in fp32
 template <typename T>
 __device__ __forceinline__ void norm8(Vec8<T>& x, const float* w, int chunks, float eps) {
-  const float r = head_rstd(x, chunks, eps);
+  float by;
+  const float r = head_rstd(x, chunks, eps, &by);
 #pragma unroll
   for (int j = 0; j < 8; ++j) x.v[j] = x.v[j] * r * w[j];
 }

@@ -87,10 +87,11 @@ __global__ __launch_bounds__(256) void norm_rope_kernel(RopeGeom g, NormArgs a) 
   }
 }
 
+// (Of one load's heads in bf16 129 registers would do; held to 128 there are four waves to a SIMD: 23400 tokens of 1 + 1 heads 25.5 us, 33.5 of three.)
 // A wave takes every so manieth token, all its rows or a group's, and keeps the sums of dy x r of its lanes.  With the second launch 23400
 // tokens of 40 + 40 heads 262 us (5.5 TB/s), 4680 of 12 + 12 23.6.
 template <typename T, int kAhead>
-__global__ __launch_bounds__(256) void norm_rope_backward_kernel(RopeGeom g, NormArgs a) {
+__global__ __launch_bounds__(256, kAhead == 1 && sizeof(T) == 2 ? 4 : 1) void norm_rope_backward_kernel(RopeGeom g, NormArgs a) {
   __shared__ float sums[4][2][2 * kMaxPairs];
   const int chunks = g.head_dim / 8, head_slots = 64 / chunks;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c8 = lane % chunks, hs = lane / chunks;
@@ -132,8 +133,8 @@ __global__ __launch_bounds__(256) void norm_rope_backward_kernel(RopeGeom g, Nor
         for (int i = 0; i < kAhead; ++i) {
           const bool mine = h + i * head_slots < end;
           rotate8(d[i], cs, sn);
-          const float rstd = head_rstd(x[i], chunks, a.eps);
-          float dot = 0.f;
+          float by, dot = 0.f;
+          const float rstd = head_rstd(x[i], chunks, a.eps, &by), out = rstd * by;
 #pragma unroll
           for (int j = 0; j < 8; ++j) {
             x[i].v[j] *= rstd;
@@ -143,7 +144,7 @@ __global__ __launch_bounds__(256) void norm_rope_backward_kernel(RopeGeom g, Nor
           }
           const float mean = head_sum(dot, chunks) * (1.f / float(8 * chunks));
 #pragma unroll
-          for (int j = 0; j < 8; ++j) d[i].v[j] = rstd * fmaf(-x[i].v[j], mean, d[i].v[j]);
+          for (int j = 0; j < 8; ++j) d[i].v[j] = out * fmaf(-x[i].v[j], mean, d[i].v[j]);
           if (mine) d[i].store(y0 + int64_t(h + i * head_slots) * side.y_head);
         }
       }

@@ -4,7 +4,7 @@ import pytest
 import torch
 
 from paper_2511_20426_amd import binding as B
-from tests.test_layer_ops import DEV, _act, _gated_grads, _gen, _kept, _normal
+from tests.test_layer_ops import DEV, HALF, WAY, _act, _angles, _gated_grads, _gen, _kept, _norm_grads, _norm_rope, _normal, _pairs, _pool
 
 
 def _given_gradients(g, u, dh, act):
@@ -183,3 +183,69 @@ def test_codes_in_host_memory_reach_no_kernel(monkeypatch):
             R.linear_i8(x, w, out=out)
     with pytest.raises(AssertionError):
         R.linear_i8(torch.ones((4, 300), dtype=torch.bfloat16), w)
+
+
+# factors of heads that lie beside each other in a wave: squares that fp32 holds, that pass its largest value, that it loses
+SIZES = [1.0, 1e18, 1e20, 1e30, 1e37, 1e-18, 1e-22, 1e-30]
+
+
+def _heads_of_all_sizes(gen, n, heads, D, t, sizes):
+    x = torch.randn(n, 3, heads, D, generator=gen, dtype=torch.float64)
+    return (x * torch.tensor(sizes, dtype=torch.float64)[torch.arange(n * 3 * heads) % len(sizes)].view(n, 3, heads, 1)).to(t).to(DEV)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("eps", [0.0, 1e-30, 1e-6])
+@pytest.mark.parametrize("dtype,D,heads", [("bf16", 128, 5), ("bf16", 128, 40), ("f32", 128, 3), ("f32", 64, 5), ("f32", 32, 11)])
+def test_norms_of_values_whose_squares_leave_the_range(dtype, D, heads, eps):
+    """Forward and on the way into the pool, over the whole range of the type."""
+    grid, n, t = (1, 3), 9, {"bf16": torch.bfloat16, "f32": torch.float32}[dtype]      # (a block of the pool)
+    pool, gen = _pool(heads, D, grid, dtype), _gen(heads)
+    qkv, w = _heads_of_all_sizes(gen, n, heads, D, t, SIZES), [_normal(gen, D, dtype=t) for _ in range(2)]
+    outs = pool.qk_norm_rope(qkv[:, 0], qkv[:, 1], w[0], w[1], 0, eps=eps)
+    ang = _angles(D, grid, 0, n)
+    for s in range(2):
+        ref = _norm_rope(qkv[:, s].double().cpu(), w[s].double().cpu(), eps, ang)
+        # (as test_norm_rope; bringing a head into the range is exact)
+        assert ((outs[s].double().cpu() - ref).abs() <= ref.abs() * HALF[t] + _pairs(ref) * 2 * WAY + 1e-30).all()
+    pool.append_batch([0], [0], 0, [qkv[:, 1]], [qkv[:, 2]], k_weight=w[1], eps=eps)
+    per = 2 * 128 * D
+    for h in range(heads):
+        at = pool.ctx.kv_cache_page_index(0, 0, h)
+        k = pool.pool[at * per * t.itemsize:(at + 1) * per * t.itemsize].view(t).view(2, 128, D)[0]
+        if dtype == "bf16":
+            c = torch.arange(16, device=DEV)[None] ^ (torch.arange(128, device=DEV)[:, None] & 15)
+            k = k.view(128, 16, 8).gather(1, c[:, :, None].expand(128, 16, 8)).view(128, D)
+        assert (k[:n] == outs[1][:, h]).all() and (k[n:] == 0).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("eps", [0.0, 1e-6])
+@pytest.mark.parametrize("dtype,D,heads,n", [("bf16", 128, 5, 9), ("bf16", 128, 40, 3), ("f32", 64, 5, 70), ("f32", 32, 11, 5)])
+def test_gradients_of_norms_whose_squares_leave_the_range(dtype, D, heads, n, eps):
+    t = {"bf16": torch.bfloat16, "f32": torch.float32}[dtype]
+    pool, gen = _pool(heads, D, (4, 5), dtype), _gen(n + 1)
+    qkv = _heads_of_all_sizes(gen, n, heads, D, t, [1.0, 1e18, 1e20, 1e25, 1e-18, 1e-22])
+    dz, w = _normal(gen, n, heads, 2, D, dtype=t), [_normal(gen, D, dtype=t) for _ in range(2)]
+    got = pool.qk_norm_rope_backward(dz[:, :, 0], dz[:, :, 1], qkv[:, 0], qkv[:, 1], w[0], w[1], 2, eps=eps)
+    ang = _angles(D, (4, 5), 2, n)
+    for s in range(2):
+        dx, dw, size, size_w = _norm_grads(dz[:, :, s].double().cpu(), qkv[:, s].double().cpu(), w[s].double().cpu(), eps, ang)
+        # (as test_norm_rope_backward)
+        assert ((got[s].double().cpu() - dx).abs() <= dx.abs() * HALF[t] + size * 3 * WAY + 1e-38).all()
+        assert ((got[2 + s].double().cpu() - dw).abs() <= size_w * (2 * WAY + 128 * 2.0 ** -24) + 1e-30).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype,D", [("bf16", 128), ("f32", 32)])
+def test_heads_that_are_not_finite(dtype, D):
+    """... stay by themselves: the heads beside them in the wave have the bits that they have without them."""
+    t = {"bf16": torch.bfloat16, "f32": torch.float32}[dtype]
+    pool, gen = _pool(9, D, (4, 5), dtype), _gen(4)
+    x, w = _normal(gen, 6, 9, D, dtype=t), _normal(gen, D, dtype=t)
+    fine = pool.qk_norm_rope(x, None, w, None, 0)[0]
+    x[1, 2, 5], x[3, 4, 7], x[5, 8, 0] = float("inf"), float("nan"), -float("inf")
+    y = pool.qk_norm_rope(x, None, w, None, 0)[0]
+    bad = torch.zeros((6, 9), dtype=torch.bool, device=DEV)
+    bad[1, 2] = bad[3, 4] = bad[5, 8] = True
+    assert (y[~bad] == fine[~bad]).all() and y[bad].isnan().any(-1).all()
