@@ -216,6 +216,8 @@ __global__ __launch_bounds__(64 * kFewWaves) void gemm_few_kernel(OpArgs a) {
   }
 }
 
+constexpr int kFewColumns = (1 << 28) - 16;       // of a result: 16 to a workgroup of 256, and a launch has fewer than 2^32 threads
+
 template <typename Op>
 int32_t enqueue_few(const OpArgs& a, const char* what, void* stream) {
   const unsigned groups = unsigned((a.N + 15) / 16);

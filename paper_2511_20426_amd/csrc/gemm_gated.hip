@@ -39,6 +39,7 @@ constexpr OpModel kModel[] = {{256, 256, 1, 2780, 945, 1200, 5330}, {192, 256, 1
 int32_t launch_gemm_gated(const void* x, const void* w_gate, const void* w_up, void* h, float* saved, int activation, int64_t M, int32_t F,
                           int32_t K, int64_t ldx, int64_t ldwg, int64_t ldwu, int64_t ldh, void* stream) {
   if (M == 0) return CA_OK;
+  if (M <= kFewTokens && F > kFewColumns) return CA_EUNSUPPORTED;
   OpArgs a{};
   a.x = x; a.w = w_gate; a.w2 = w_up; a.y = h;
   a.g = saved; a.u = saved ? saved + gated_saved_values(M, F) / 2 : nullptr;

@@ -59,6 +59,7 @@ int32_t i8_ready() {
 int32_t launch_gemm_i8(const void* x, const float* x_scales, const void* w, const float* w_scales, void* y, int64_t M, int32_t N, int32_t K,
                        int64_t ldx, int64_t ldw, int64_t ldy, void* stream) {
   if (M == 0) return CA_OK;
+  if (M <= kFewTokens && N > kFewColumns) return CA_EUNSUPPORTED;
   OpArgs a{};
   a.x = x; a.w = w; a.y = y; a.w2 = w_scales; a.xs = x_scales;
   a.ldy = ldy;
@@ -83,6 +84,7 @@ int32_t launch_gemm_i8(const void* x, const float* x_scales, const void* w, cons
 int32_t launch_gemm_i8_values(int dtype, const void* x, int64_t ldx, const void* w, const float* w_scales, void* y, int64_t M, int32_t N, int32_t K,
                               int64_t ldw, int64_t ldy, void* workspace, void* stream) {
   if (M == 0) return CA_OK;
+  if (M <= kFewTokens && N > kFewColumns) return CA_EUNSUPPORTED;
   if (const int32_t rc = i8_ready(); rc != CA_OK) return rc;
   const auto kernel = M == 1                         ? gemm_few_kernel<I8, 1, CodesOne>
                       : K > CodesTwelve::kMost       ? M == 2 ? gemm_few_kernel<I8, 1, CodesTwo> : gemm_few_kernel<I8, 1, CodesFour>

@@ -249,3 +249,15 @@ def test_heads_that_are_not_finite(dtype, D):
     bad = torch.zeros((6, 9), dtype=torch.bool, device=DEV)
     bad[1, 2] = bad[3, 4] = bad[5, 8] = True
     assert (y[~bad] == fine[~bad]).all() and y[bad].isnan().any(-1).all()
+
+
+@pytest.mark.parametrize("rows", [1, 2, 16, 32])
+def test_few_tokens_of_too_many_columns_are_refused(rows):
+    """Their launch would have 2^32 threads."""
+    n, p = (1 << 28) - 8, 4096
+    for call in (lambda: B.layer_linear_i8(p, p, p, p, p, rows, n, 200, 256, 256, n),
+                 lambda: B.layer_linear_i8_values(p, B.CA_BF16, p, p, p, rows, n, 200, 200, 256, n, p, 1 << 30),
+                 lambda: B.layer_gated_bf16(p, p, p, p, 0, B.CA_SILU, rows, n, 128, 128, 128, 128, n)):
+        with pytest.raises(B.CascadeAttnError) as e:
+            call()
+        assert e.value.code == B.CA_EUNSUPPORTED
