@@ -214,7 +214,7 @@ def save_lines(mt):
             f"s_add_u32 s{a}, s{a}, s{a + 1}", f"s_lshl_b32 s{a + 4}, s{a}, 11", f"s_lshr_b32 s{a + 5}, s{a}, 21"]
     for to, name in ((g, "g"), (u, "u")):
         out += [f"s_add_u32 s{to}, %[{name}_lo], s{a + 4}", f"s_addc_u32 s{to + 1}, %[{name}_hi], s{a + 5}"]
-    out.append(f"s_lshl_b32 s{a + 4}, %[blocks_n], 11")
+    out += [f"s_lshl_b32 s{a + 4}, %[blocks_n], 11", f"s_lshr_b32 s{a + 5}, %[blocks_n], 21"]
     for tj in range(mt):
         out += [f"s_cmp_ge_i32 {16 * tj}, s{a + 6}", "s_nop 0", "s_cbranch_scc1 SAVED_%="]
         for c in range(2):
@@ -225,7 +225,7 @@ def save_lines(mt):
         out.append("s_mov_b64 exec, -1")
         if tj < mt - 1:
             for to in (g, u):
-                out += [f"s_add_u32 s{to}, s{to}, s{a + 4}", f"s_addc_u32 s{to + 1}, s{to + 1}, 0"]
+                out += [f"s_add_u32 s{to}, s{to}, s{a + 4}", f"s_addc_u32 s{to + 1}, s{to + 1}, s{a + 5}"]
     return out + ["SAVED_%=:"]
 
 

@@ -261,3 +261,11 @@ def test_few_tokens_of_too_many_columns_are_refused(rows):
         with pytest.raises(B.CascadeAttnError) as e:
             call()
         assert e.value.code == B.CA_EUNSUPPORTED
+
+
+@pytest.mark.parametrize("mt", [4, 6])
+def test_where_the_projections_of_many_columns_lie(mt):
+    """A row of blocks of 2^32 bytes: the generated program followed over a tile of several such rows, at the last columns."""
+    from tests import test_gemm_op_rows as T
+    N = (1 << 26) + 40
+    T.test_loop_over_tiles("gated", True, mt, (32 * mt + 20, N, 256), [(0, N // 128), (1, N // 128 - 1)], 0, 10)
