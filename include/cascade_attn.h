@@ -260,8 +260,8 @@ int32_t layer_qkv_publish(ca_ctx* ctx, int32_t n_blocks, const int64_t* block_id
                           int32_t prompt_epoch, const void* x_dev, int64_t ldx, const void* w_qkv_dev,
                           int64_t ldw, int32_t k_in, void* q_out_dev, void* hip_stream, int32_t* slots_out);
 
-/* ---- The rest of a layer.  The paper gives none of the generator's internals; these are the operators that DiT layers in use have
- * around the attention: norms of queries and keys, 8-bit projections, a gated feed-forward block.  Conventions as above; calls that
+/* ---- The rest of a layer.  The paper gives none of the generator's internals; these are operators that DiT layers may have
+ * around the attention: per-head norms of queries and keys, 8-bit projections, a gated feed-forward block.  Conventions as above; calls that
  * need device memory of their own take it from the caller, aligned to 16 bytes, and keep nothing in it. */
 
 /* Queries or keys of some tokens: [token, heads, head_dim], heads and head_dim the context's, strides in elements. */

@@ -277,7 +277,8 @@ __device__ __forceinline__ float rest_of(float v) {
   return copysignf(fmaxf(fabsf(v - __uint_as_float(__float_as_uint(v) & 0xffff0000u)), fabsf(v) * 0x1p-24f), v);
 }
 __device__ __forceinline__ uint2 cut_bf16(const float (&v)[4]) {
-  return uint2{__builtin_amdgcn_perm(__float_as_uint(v[1]), __float_as_uint(v[0]), 0x07060302), __builtin_amdgcn_perm(__float_as_uint(v[3]), __float_as_uint(v[2]), 0x07060302)};
+  auto upper = [](float lo, float hi) { return uint32_t(__builtin_amdgcn_perm(__float_as_uint(hi), __float_as_uint(lo), 0x07060302)); };
+  return uint2{upper(v[0], v[1]), upper(v[2], v[3])};
 }
 
 // Up to 32 rows, on the matrix pipe, still one pass over the weights and their gradients with nothing laid out.  A workgroup takes 128 columns
@@ -449,7 +450,7 @@ __global__ __launch_bounds__(256) void gated_sum_kernel(const float* partials, i
 constexpr int kFewGradMost = 512;                 // columns f of a workgroup of gated_few_grad_kernel
 
 // columns f to a workgroup: enough workgroups to fill the chip, 64 to 512 columns; of more than kFewGradRows rows chunks of 128, two
-// workgroups to a CU at most
+// workgroups to a CU at most.  (Of an MI355X's 256 CUs, here and in walk_of: the workspace's size goes by it, which is asked for without a device.)
 int few_grad_each(int64_t M, int32_t F, int32_t K) {
   if (M <= kFewGradRows) return int(std::clamp<int64_t>(int64_t(F) * (K / 128) / 1024 / 16 * 16, 64, kFewGradMost));
   const int64_t parts = std::max(512 / (K / 128), 1);

@@ -51,8 +51,9 @@ __device__ __forceinline__ void token_angles(const RopeGeom& g, int64_t n, int64
 }
 
 // A wave takes a token: its lanes cover 64 / chunks heads at a time (1 KB of bf16), rows_per_group heads in all, kAhead loads
-// requested together (no more than there are: 23400 tokens of 1 + 1 heads 20.1 -> 18.9 us, with gradients' 48 -> 25), queries first, then keys (a loop over both picked the side for each load and weight: 23400 tokens of 40 + 40
-// heads 192 us, now 178, the rate of a copy; 4680 of 12 + 12 18.5, now 13.7).
+// requested together, no more than there are (four for one head of each: 23400 tokens of 1 + 1 heads 20.1 us for 18.9, backward 48 for 25).
+// Queries first, then keys: a loop over both picked the side for each load and weight (23400 tokens of 40 + 40 heads 192 us, now 178, the
+// rate of a copy; 4680 of 12 + 12 18.5, now 13.4).
 template <typename T, int kAhead>
 __global__ __launch_bounds__(256) void norm_rope_kernel(RopeGeom g, NormArgs a) {
   const int chunks = g.head_dim / 8, head_slots = 64 / chunks;
@@ -88,8 +89,8 @@ __global__ __launch_bounds__(256) void norm_rope_kernel(RopeGeom g, NormArgs a) 
 }
 
 // (Of one load's heads in bf16 129 registers would do; held to 128 there are four waves to a SIMD: 23400 tokens of 1 + 1 heads 25.5 us, 33.5 of three.)
-// A wave takes every so manieth token, all its rows or a group's, and keeps the sums of dy x r of its lanes.  With the second launch 23400
-// tokens of 40 + 40 heads 262 us (5.5 TB/s), 4680 of 12 + 12 23.6.
+// A wave takes the tokens that lie a launch's waves apart, of each all heads or a group's, and keeps the sums of dy x r of its lanes.  With the
+// second launch 23400 tokens of 40 + 40 heads 262 us (5.5 TB/s), 4680 of 12 + 12 24.4.
 template <typename T, int kAhead>
 __global__ __launch_bounds__(256, kAhead == 1 && sizeof(T) == 2 ? 4 : 1) void norm_rope_backward_kernel(RopeGeom g, NormArgs a) {
   __shared__ float sums[4][2][2 * kMaxPairs];

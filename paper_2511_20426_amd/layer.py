@@ -4,7 +4,8 @@
 
 The projections into and out of the attention and out of the feed-forward block are held and multiplied in 8 bits (linear_i8), gate and up
 projection are one kernel in bf16 (gated_linear), queries and keys are normed per head on the way to their rotation, the keys on the way into
-the shared pool.  Norms of the layer's input, modulation by the timestep and cross-attention are the caller's.
+the shared pool.  Norms of the layer's input, modulation by the timestep and cross-attention are the caller's.  (Sizes are Wan's; its published
+layers norm queries and keys over the whole width and have a plain gelu feed-forward half.)
 
 Run as a program it times such a layer in the steady state of a cascade, or a training step of the feed-forward half:
 
@@ -61,7 +62,8 @@ class CascadeLayer:
 
 def feed_forward_step(x, w_gate, w_up, w_down, target, activation: str = "silu", lr: float = 0.0):
     """One step of training the feed-forward half towards target [M, N] (mean squared error), all in bf16: (loss, gradients of w_gate, w_up,
-    w_down and x); with lr the weights are updated in place."""
+    w_down and x); with lr the weights are updated in place.  (w_down, dy and h are transposed by torch's copies for the linear map, which multiplies
+    rows by rows.)"""
     h, saved = gated_linear_train(x, w_gate, w_up, activation)
     y = linear(h, w_down)
     off = y.float() - target.float()

@@ -1,7 +1,8 @@
 """Torch plumbing around the C ABI: device memory for the pool and the current HIP stream.
 
 No arithmetic of the method happens here; every tensor handed to the library is passed as a
-raw device address.
+raw device address.  Results carry no autograd history, whatever the arguments require: where there is a
+backward pass (qk_norm_rope_backward, gated_linear_backward) the caller calls it.
 """
 from __future__ import annotations
 
