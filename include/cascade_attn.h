@@ -342,6 +342,28 @@ int32_t layer_gated_backward_bf16(const void* dh_dev, const void* x_dev, const v
                                   int64_t lddx, int64_t lddw, void* workspace_dev, size_t workspace_bytes,
                                   void* hip_stream);
 
+/* ---- Operators that a layer is adapted with: the norm of its input with the modulation of the block in flight, low-rank adapters beside its
+ * projections, the step of the optimizer.  The paper gives none of them.  Conventions as above. */
+
+/* Layer norm of rows x [rows][width] of type dtype (CA_F32 or CA_BF16): y = weight * (x - mean) / sqrt(mean((x - mean)^2) + eps) + bias, in fp32,
+ * rounded once.  weight, bias: [groups][width] of weight_dtype (fp32, or bf16 with rows in bf16), rows ldw apart, either or both null (ones,
+ * zeros); rows are dealt to the groups in equal runs, rows / groups consecutive ones to each (CA_EINVAL if they do not come out even): with the
+ * rows of a block in flight as a group that is its timestep's modulation.  x and y: any row strides >= width, aligned as their values are
+ * (faster: width a multiple of 8, rows and weights on 16 bytes); y may be x, with its stride, and overlaps nothing else.  Statistics hold for values of
+ * any size that the type has.  A row that holds an infinity or NaN is NaN; one of equal values gives the bias for eps > 0, NaN for eps == 0.
+ * width <= CA_LAYER_NORM_MAX_WIDTH, rows <= 2^30, groups <= 2^20 (CA_EUNSUPPORTED). */
+#define CA_LAYER_NORM_MAX_WIDTH 32768
+int32_t layer_norm(const void* x_dev, int32_t dtype, const void* weight_dev, const void* bias_dev, int32_t weight_dtype, float eps, void* y_dev,
+                   int64_t rows, int32_t width, int64_t groups, int64_t ldx, int64_t ldw, int64_t ldy, void* hip_stream);
+
+/* Its gradients, from that of y: dx (may be dy, with its stride), dweight and dbias (fp32, [groups][width] packed, written, not added to; either or
+ * both null: not asked for), summed over a group's rows in an order that the sizes fix.  weight as in the forward pass (null: ones).
+ * workspace_dev: layer_norm_backward_workspace() bytes (may be 0; not needed without weight gradients).  rows == 0: zero weight gradients. */
+size_t layer_norm_backward_workspace(int64_t rows, int32_t width, int64_t groups);
+int32_t layer_norm_backward(const void* dy_dev, const void* x_dev, int32_t dtype, const void* weight_dev, int32_t weight_dtype, float eps, void* dx_dev,
+                            float* dweight_dev, float* dbias_dev, int64_t rows, int32_t width, int64_t groups, int64_t lddy, int64_t ldx, int64_t ldw,
+                            int64_t lddx, void* workspace_dev, size_t workspace_bytes, void* hip_stream);
+
 /* ---- Cascade scheduler: the control flow of Algorithm 1, host integers only.
  * State (b, tau, d) = primary block, timestep index of the primary block, cascade depth.  An
  * iteration forwards blocks b .. b + min(d, G-1), block b+i at timesteps[tau - i] (older blocks

@@ -38,6 +38,7 @@ EXPORTS = (
     "ca_mfma_microbench", "layer_linear_bf16", "layer_qkv_publish",
     "layer_qk_norm_rope", "layer_qk_norm_rope_workspace", "layer_qk_norm_rope_backward", "kv_cache_append_batch_norm", "layer_quantize_rows_i8",
     "layer_linear_i8", "layer_linear_i8_workspace", "layer_linear_i8_values", "layer_gated_bf16", "layer_gated_saved_bytes", "layer_gated_backward_workspace", "layer_gated_backward_bf16",
+    "layer_norm", "layer_norm_backward_workspace", "layer_norm_backward",
     "ca_sched_create", "ca_sched_create_lagged", "ca_sched_destroy", "ca_sched_batch", "ca_sched_advance", "ca_sched_state",
 )
 
@@ -169,6 +170,12 @@ def _load() -> C.CDLL:
     lib.layer_gated_backward_workspace.argtypes = [i64, i32, i32]
     lib.layer_gated_backward_bf16.restype = i32
     lib.layer_gated_backward_bf16.argtypes = [vp] * 5 + [i32] + [vp] * 3 + [i64, i32, i32] + [i64] * 6 + [vp, C.c_size_t, vp]
+    lib.layer_norm.restype = i32
+    lib.layer_norm.argtypes = [vp, i32, vp, vp, i32, f32, vp, i64, i32] + [i64] * 4 + [vp]
+    lib.layer_norm_backward_workspace.restype = C.c_size_t
+    lib.layer_norm_backward_workspace.argtypes = [i64, i32, i64]
+    lib.layer_norm_backward.restype = i32
+    lib.layer_norm_backward.argtypes = [vp, vp, i32, vp, i32, f32, vp, vp, vp, i64, i32] + [i64] * 5 + [vp, C.c_size_t, vp]
     lib.ca_sched_create.restype = i32
     lib.ca_sched_create.argtypes = [i64, i32, C.POINTER(i32), i32, C.POINTER(vp)]
     lib.ca_sched_create_lagged.restype = i32
@@ -481,6 +488,24 @@ def layer_gated_backward_bf16(dh_ptr: int, x_ptr: int, w_gate_ptr: int, w_up_ptr
                                          index(saved_ptr or 0), activation, index(dx_ptr or 0), index(dw_gate_ptr or 0),
                                          index(dw_up_ptr or 0), m_rows, n_hidden, k_in, lddh, ldx, ldw_gate, ldw_up, lddx, lddw,
                                          index(workspace_ptr or 0), workspace_bytes, index(stream or 0)), "layer_gated_backward_bf16")
+
+
+def layer_norm(x_ptr: int, dtype: int, weight_ptr: int, bias_ptr: int, weight_dtype: int, eps: float, y_ptr: int, rows: int, width: int, groups: int,
+               ldx: int, ldw: int, ldy: int, stream: int = 0) -> None:
+    _check(lib.layer_norm(index(x_ptr or 0), dtype, index(weight_ptr or 0), index(bias_ptr or 0), weight_dtype, eps, index(y_ptr or 0), rows, width, groups,
+                          ldx, ldw, ldy, index(stream or 0)), "layer_norm")
+
+
+def layer_norm_backward_workspace(rows: int, width: int, groups: int) -> int:
+    return int(lib.layer_norm_backward_workspace(rows, width, groups))
+
+
+def layer_norm_backward(dy_ptr: int, x_ptr: int, dtype: int, weight_ptr: int, weight_dtype: int, eps: float, dx_ptr: int, dweight_ptr: int, dbias_ptr: int,
+                        rows: int, width: int, groups: int, lddy: int, ldx: int, ldw: int, lddx: int, workspace_ptr: int, workspace_bytes: int,
+                        stream: int = 0) -> None:
+    _check(lib.layer_norm_backward(index(dy_ptr or 0), index(x_ptr or 0), dtype, index(weight_ptr or 0), weight_dtype, eps, index(dx_ptr or 0),
+                                   index(dweight_ptr or 0), index(dbias_ptr or 0), rows, width, groups, lddy, ldx, ldw, lddx, index(workspace_ptr or 0),
+                                   workspace_bytes, index(stream or 0)), "layer_norm_backward")
 
 
 def mfma_microbench(data_kind: int, trips: int, scratch_ptr: int, scratch_bytes: int, stream: int = 0):

@@ -185,6 +185,18 @@ GatedWorkspace gated_workspace(int64_t M, int32_t F, int32_t K);
 int32_t launch_gated_backward(const void* dh, const void* x, const void* w_gate, const void* w_up, const float* saved, int activation,
                               void* dx, void* dw_gate, void* dw_up, int64_t M, int32_t F, int32_t K, int64_t lddh, int64_t ldx, int64_t ldwg,
                               int64_t ldwu, int64_t lddx, int64_t lddw, void* workspace, void* stream);
+// Layer norm of rows and its gradients; groups of equally many consecutive rows have weights and biases of their own (null: none).
+struct RowNorm {
+  const void* x;
+  const void* w;
+  const void* b;
+  int64_t rows, groups, ldx, ldy, ldw;
+  int32_t width, dtype, w_dtype;
+  float eps;
+};
+int32_t launch_layer_norm(const RowNorm& n, const void* y, void* stream);
+size_t layer_norm_backward_bytes(int64_t rows, int32_t width, int64_t groups);
+int32_t launch_layer_norm_backward(const RowNorm& n, const void* dy, int64_t lddy, void* dx, float* dw, float* db, void* workspace, void* stream);
 // Per-device facts and one-time kernel attributes, cached for up to kMaxDevices devices (thread
 // safe: the cached values are idempotent and written with relaxed atomics).
 constexpr int kMaxDevices = 64;

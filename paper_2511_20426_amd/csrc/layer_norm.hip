@@ -1,0 +1,453 @@
+// Layer norm of rows, with weights and biases of the group of rows (the block in flight) that a row belongs to, and its gradients (gfx950).
+//
+//   y = w n + b,  n = (x - mean) r,  r = 1 / sqrt(mean((x - mean)^2) + eps)
+//   dn = dy w,  dx = r (dn - mean(dn) - n mean(dn n)),  dw = sum over a group's rows of dy n,  db = of dy
+//
+// Memory bound: forward reads x and writes y once, backward reads x and dy and writes dx.  A row stays in registers (as it is stored), of 64
+// threads up to a width of 2048, of 256 up to 8192, of 1024 up to 32768; a workgroup goes from row to row of a group, so that the weights are
+// loaded once and the sums of the weights' gradients stay in registers too.  Statistics are fp32 in two steps: the mean, then squares and
+// sum of what is left, whose mean corrects the first one, so that rows far from zero lose nothing.  The gradients of the weights are summed by
+// a thread over its rows, over a workgroup's waves in LDS and over the workgroups by a second launch in fp64, in an order that the sizes fix.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+
+#include "ca_internal.hpp"
+
+namespace ca {
+namespace {
+
+#include "rope_device.hpp"
+#include "norm_device.hpp"
+
+struct RowNormArgs {
+  const void* x;
+  const void* dy;                                 // backward
+  const void* w;                                  // null: ones, zeros
+  const void* b;
+  void* y;                                        // forward: y, backward: dx
+  float* dw;                                      // backward: [group][width] or a workgroup's part [workgroup][2][width]; null: not asked for
+  float* db;
+  int64_t ldx, lddy, ldy, ldw;
+  int32_t width, groups, group_rows, per_group;   // workgroups of a group
+  float eps;
+};
+
+// Eight values of a row as they are stored
+template <typename T> struct Piece;
+template <> struct Piece<uint16_t> {
+  U4 p;
+  __device__ __forceinline__ float operator[](int j) const {
+    const uint32_t two = j < 2 ? p.x : j < 4 ? p.y : j < 6 ? p.z : p.w;
+    return j % 2 ? bf16_hi(two) : bf16_lo(two);
+  }
+  __device__ __forceinline__ void load(const uint16_t* at) { p = load_once(at); }
+  __device__ __forceinline__ void load_some(const uint16_t* at, int stride, int left) {        // value j at j * stride, zero from `left` on
+    uint32_t v[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = j * stride < left ? at[j * stride] : 0;
+    p = U4{v[0] | v[1] << 16, v[2] | v[3] << 16, v[4] | v[5] << 16, v[6] | v[7] << 16};
+  }
+  __device__ __forceinline__ void clear() { p = U4{0, 0, 0, 0}; }
+};
+template <> struct Piece<float> {
+  float v[8];
+  __device__ __forceinline__ float operator[](int j) const { return v[j]; }
+  __device__ __forceinline__ void load(const float* at) {
+    const U4 a = load_once(at), b = load_once(at + 4);
+    v[0] = __uint_as_float(a.x); v[1] = __uint_as_float(a.y); v[2] = __uint_as_float(a.z); v[3] = __uint_as_float(a.w);
+    v[4] = __uint_as_float(b.x); v[5] = __uint_as_float(b.y); v[6] = __uint_as_float(b.z); v[7] = __uint_as_float(b.w);
+  }
+  __device__ __forceinline__ void load_some(const float* at, int stride, int left) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = j * stride < left ? at[j * stride] : 0.f;
+  }
+  __device__ __forceinline__ void clear() {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = 0.f;
+  }
+};
+__device__ __forceinline__ void put8(uint16_t* at, const float* v) {
+  store_once(at, U4{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7])});
+}
+__device__ __forceinline__ void put8(float* at, const float* v) {
+  store_once(at, U4{__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])});
+  store_once(at + 4, U4{__float_as_uint(v[4]), __float_as_uint(v[5]), __float_as_uint(v[6]), __float_as_uint(v[7])});
+}
+__device__ __forceinline__ void put1(uint16_t* at, float v) { *at = uint16_t(pack_bf16(v, v)); }
+__device__ __forceinline__ void put1(float* at, float v) { *at = v; }
+__device__ __forceinline__ float get1(const uint16_t* at) { return __uint_as_float(uint32_t(*at) << 16); }
+__device__ __forceinline__ float get1(const float* at) { return *at; }
+
+// kWaves to a row, kPieces of eight values to a thread.  Whole rows (kWhole: a multiple of 8 values, everything aligned to 16 bytes): piece i of
+// thread t has the values from 8 (64 kWaves i + t) on; otherwise values 64 kWaves (8 i + j) + t.
+template <int kWaves, int kPieces, bool kWhole>
+struct RowShape {
+  static constexpr int kThreads = 64 * kWaves, kRows = kWaves == 1 ? 4 : 1;          // rows that a workgroup has at a time
+  static __device__ __forceinline__ int at(int t, int i) { return kWhole ? 8 * (kThreads * i + t) : kThreads * 8 * i + t; }
+  static constexpr int kStep = kWhole ? 1 : kThreads;                                // from one value of a piece to the next
+};
+
+template <typename Shape, bool kWhole, typename T>
+__device__ __forceinline__ void load_piece(Piece<T>& p, const T* row, int at, int width) {
+  if (kWhole) {
+    if (at < width) p.load(row + at); else p.clear();
+  } else {
+    p.load_some(row + at, Shape::kStep, width - at);
+  }
+}
+
+// The sums of two numbers over the threads of a row, in all of them, each adding the same pairs in the same order.  (Several waves: `room` is
+// kWaves places of LDS that the call after the next may use again: whoever writes them then has passed a barrier that all came to behind reading.)
+template <int kWaves>
+__device__ __forceinline__ void row_sum(float& a, float& b, float2* room) {
+  a = head_sum(a, 16);
+  b = head_sum(b, 16);
+#pragma unroll
+  for (int d = 16; d < 64; d *= 2) {
+    a += __shfl_xor(a, d, 64);
+    b += __shfl_xor(b, d, 64);
+  }
+  if constexpr (kWaves > 1) {
+    if ((threadIdx.x & 63) == 0) room[threadIdx.x >> 6] = make_float2(a, b);
+    __syncthreads();
+    a = b = 0.f;
+#pragma unroll
+    for (int i = 0; i < kWaves; ++i) {
+      const float2 v = room[i];
+      a += v.x;
+      b += v.y;
+    }
+  }
+}
+
+// Of a row: what is left of its values is (x pre - mean) post, and r.  pre and post are 1, or powers of two that bring rows whose squares leave
+// fp32's range back into it (values of 1e19, or differences of 1e-15 beside an eps as small): r is then that of the scaled ones.
+struct RowStats {
+  float mean, r, pre, post;
+  __device__ __forceinline__ float left(float x) const { return (x * pre - mean) * post; }
+};
+
+template <typename Shape, int kWaves, int kPieces, bool kWhole, typename T>
+__device__ __forceinline__ float row_variance(const Piece<T> (&x)[kPieces], int t, int width, float per, RowStats& s, float2* room) {
+  float sum = 0.f, none = 0.f;
+#pragma unroll
+  for (int i = 0; i < kPieces; ++i)
+#pragma unroll
+    for (int j = 0; j < 8; ++j) sum += x[i][j] * s.pre;              // values past the end are zeros
+  row_sum<kWaves>(sum, none, room);
+  s.mean = sum * per;
+  float off = 0.f, squares = 0.f;
+#pragma unroll
+  for (int i = 0; i < kPieces; ++i)
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const float d = Shape::at(t, i) + j * Shape::kStep < width ? s.left(x[i][j]) : 0.f;
+      off += d;
+      squares = fmaf(d, d, squares);
+    }
+  row_sum<kWaves>(off, squares, room + kWaves);
+  off *= per;
+  s.mean += off / s.post;
+  return fmaxf(fmaf(-off, off, squares * per), 0.f) + (squares - squares);           // (fmaxf would take a zero for a NaN)
+}
+
+template <typename Shape, int kWaves, int kPieces, bool kWhole, typename T>
+__device__ __forceinline__ RowStats row_stats(const Piece<T> (&x)[kPieces], int t, int width, float per, float eps, float2* room) {
+  RowStats s{0.f, 0.f, 1.f, 1.f};
+  float var = row_variance<Shape, kWaves, kPieces, kWhole>(x, t, width, per, s, room) + eps;
+  if (__builtin_expect(!(var >= 0x1p-90f && var <= 0x1p100f), 0)) {                  // (the same in all threads of the row)
+    if (var < 1.f) s.post = 0x1p90f; else s.pre = 0x1p-72f;
+    const float by = s.pre * s.post;
+    var = row_variance<Shape, kWaves, kPieces, kWhole>(x, t, width, per, s, room) + eps * by * by;
+  }
+  s.r = 1.f / sqrtf(var);
+  return s;
+}
+
+// the weights (or biases) of a thread's values
+template <typename Shape, bool kWhole, int kPieces, typename W>
+__device__ __forceinline__ void load_weights(float (&to)[kPieces][8], const W* w, int t, int width, float otherwise) {
+#pragma unroll
+  for (int i = 0; i < kPieces; ++i)
+#pragma unroll
+    for (int j = 0; j < 8; ++j) to[i][j] = otherwise;
+  if (!w) return;
+#pragma unroll
+  for (int i = 0; i < kPieces; ++i) {
+    const int at = Shape::at(t, i);
+    if (kWhole) {
+      if (at < width) {
+        Vec8<W> v;
+        v.load(w + at);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) to[i][j] = v.v[j];
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        if (at + j * Shape::kStep < width) to[i][j] = get1(w + at + j * Shape::kStep);
+    }
+  }
+}
+
+template <typename Shape, bool kWhole, typename T>
+__device__ __forceinline__ void store_piece(T* row, int at, int width, const float* v) {
+  if (kWhole) {
+    if (at < width) put8(row + at, v);
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      if (at + j * Shape::kStep < width) put1(row + at + j * Shape::kStep, v[j]);
+  }
+}
+
+template <typename T, typename W, int kWaves, int kPieces, bool kWhole>
+__global__ __launch_bounds__(kWaves == 1 ? 256 : 64 * kWaves) void layer_norm_kernel(RowNormArgs a) {
+  using Shape = RowShape<kWaves, kPieces, kWhole>;
+  __shared__ float2 room[2 * kWaves];
+  const int t = threadIdx.x % Shape::kThreads;
+  const int group = blockIdx.x / unsigned(a.per_group), nth = blockIdx.x - group * a.per_group;
+  const int64_t first = int64_t(group) * a.group_rows;
+  const float per = 1.f / float(a.width);
+  float w[kPieces][8], b[kPieces][8];
+  load_weights<Shape, kWhole>(w, a.w ? static_cast<const W*>(a.w) + group * a.ldw : nullptr, t, a.width, 1.f);
+  load_weights<Shape, kWhole>(b, a.b ? static_cast<const W*>(a.b) + group * a.ldw : nullptr, t, a.width, 0.f);
+  for (int64_t n = int64_t(nth) * Shape::kRows + threadIdx.x / Shape::kThreads; n < a.group_rows; n += int64_t(a.per_group) * Shape::kRows) {
+    const T* const row = static_cast<const T*>(a.x) + (first + n) * a.ldx;
+    Piece<T> x[kPieces];
+#pragma unroll
+    for (int i = 0; i < kPieces; ++i) load_piece<Shape, kWhole>(x[i], row, Shape::at(t, i), a.width);
+    const RowStats s = row_stats<Shape, kWaves, kPieces, kWhole>(x, t, a.width, per, a.eps, room);
+    T* const out = static_cast<T*>(a.y) + (first + n) * a.ldy;
+#pragma unroll
+    for (int i = 0; i < kPieces; ++i) {
+      float v[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[j] = fmaf(s.left(x[i][j]) * s.r, w[i][j], b[i][j]);
+      store_piece<Shape, kWhole>(out, Shape::at(t, i), a.width, v);
+    }
+  }
+}
+
+template <typename T, typename W, int kWaves, int kPieces, bool kWhole>
+__global__ __launch_bounds__(kWaves == 1 ? 256 : 64 * kWaves) void layer_norm_backward_kernel(RowNormArgs a) {
+  using Shape = RowShape<kWaves, kPieces, kWhole>;
+  __shared__ float2 room[3 * kWaves];
+  __shared__ float sums[kWaves == 1 ? 2 : 1][kWaves == 1 ? 512 * kPieces : 1];
+  const int t = threadIdx.x % Shape::kThreads;
+  const int group = blockIdx.x / unsigned(a.per_group), nth = blockIdx.x - group * a.per_group;
+  const int64_t first = int64_t(group) * a.group_rows;
+  const float per = 1.f / float(a.width);
+  float w[kPieces][8], dw[kPieces][8], db[kPieces][8];
+  load_weights<Shape, kWhole>(w, a.w ? static_cast<const W*>(a.w) + group * a.ldw : nullptr, t, a.width, 1.f);
+#pragma unroll
+  for (int i = 0; i < kPieces; ++i)
+#pragma unroll
+    for (int j = 0; j < 8; ++j) dw[i][j] = db[i][j] = 0.f;
+  for (int64_t n = int64_t(nth) * Shape::kRows + threadIdx.x / Shape::kThreads; n < a.group_rows; n += int64_t(a.per_group) * Shape::kRows) {
+    const T* const row = static_cast<const T*>(a.x) + (first + n) * a.ldx;
+    const T* const drow = static_cast<const T*>(a.dy) + (first + n) * a.lddy;
+    Piece<T> x[kPieces], d[kPieces];
+#pragma unroll
+    for (int i = 0; i < kPieces; ++i) load_piece<Shape, kWhole>(x[i], row, Shape::at(t, i), a.width);
+#pragma unroll
+    for (int i = 0; i < kPieces; ++i) load_piece<Shape, kWhole>(d[i], drow, Shape::at(t, i), a.width);
+    const RowStats s = row_stats<Shape, kWaves, kPieces, kWhole>(x, t, a.width, per, a.eps, room);
+    float sum = 0.f, dot = 0.f;
+#pragma unroll
+    for (int i = 0; i < kPieces; ++i)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {                                 // dy is zero past the end, and n finite where the row is
+        const float dy = d[i][j], normed = s.left(x[i][j]) * s.r, dn = dy * w[i][j];
+        if (kWhole || Shape::at(t, i) + j * Shape::kStep < a.width) {
+          sum += dn;
+          dot = fmaf(dn, normed, dot);
+          dw[i][j] = fmaf(dy, normed, dw[i][j]);
+          db[i][j] += dy;
+        }
+      }
+    row_sum<kWaves>(sum, dot, room + 2 * kWaves);
+    sum *= per;
+    dot *= per;
+    const float out_by = s.r * s.pre * s.post;
+    T* const out = static_cast<T*>(a.y) + (first + n) * a.ldy;
+#pragma unroll
+    for (int i = 0; i < kPieces; ++i) {
+      float v[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const float normed = s.left(x[i][j]) * s.r;
+        v[j] = out_by * (fmaf(d[i][j], w[i][j], -sum) - normed * dot);
+      }
+      store_piece<Shape, kWhole>(out, Shape::at(t, i), a.width, v);
+    }
+  }
+  if (!a.dw && !a.db) return;
+  // one workgroup to a group: the gradients themselves; several: a part of them
+  const int64_t part = a.per_group > 1 ? int64_t(blockIdx.x) * 2 * a.width : int64_t(group) * a.width;
+  float* const to[2] = {a.dw ? a.dw + part : nullptr, a.db ? a.db + part : nullptr};
+  if constexpr (kWaves == 1) {                                      // the four waves' sums, one behind the other
+    for (int wave = 0; wave < 4; ++wave) {
+      if (int(threadIdx.x >> 6) == wave) {
+#pragma unroll
+        for (int i = 0; i < kPieces; ++i)
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            const int at = (i * 8 + j) * 64 + t;                    // (a place of its own to each, of whatever column)
+            sums[0][at] = (wave ? sums[0][at] : 0.f) + dw[i][j];
+            sums[1][at] = (wave ? sums[1][at] : 0.f) + db[i][j];
+          }
+      }
+      __syncthreads();
+    }
+    for (int k = threadIdx.x; k < 512 * kPieces; k += 256) {
+      const int lane = k % 64, i = k / 512, j = k / 64 % 8, col = Shape::at(lane, i) + j * Shape::kStep;
+      if (col >= a.width) continue;
+      if (to[0]) to[0][col] = sums[0][k];
+      if (to[1]) to[1][col] = sums[1][k];
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < kPieces; ++i)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const int col = Shape::at(t, i) + j * Shape::kStep;
+        if (col >= a.width) continue;
+        if (to[0]) to[0][col] = dw[i][j];
+        if (to[1]) to[1][col] = db[i][j];
+      }
+  }
+}
+
+// dw and db [group][width] from the workgroups' parts [group][n][2][width]: 16 columns of one of them to a workgroup, its 16 rows of threads
+// share the parts
+constexpr int kSumCols = 16, kSumRows = 16;
+__global__ __launch_bounds__(kSumCols * kSumRows) void layer_norm_sum_kernel(const float* parts, int n, int width, int columns, float* dw, float* db) {
+  __shared__ double sums[kSumRows][kSumCols + 1];
+  const int x = threadIdx.x % kSumCols, y = threadIdx.x / kSumCols;
+  const int group = blockIdx.x / unsigned(columns), col = (blockIdx.x - group * columns) * kSumCols + x;
+  float* const to = blockIdx.y ? db : dw;
+  if (!to) return;
+  const float* const from = parts + (int64_t(group) * n * 2 + blockIdx.y) * width + col;
+  double v = 0.;
+  if (col < width) {
+#pragma unroll 8
+    for (int i = y; i < n; i += kSumRows) v += double(from[int64_t(i) * 2 * width]);
+  }
+  sums[y][x] = v;
+  __syncthreads();
+  for (int half = kSumRows / 2; half > 0; half /= 2) {
+    if (y < half) sums[y][x] += sums[y + half][x];
+    __syncthreads();
+  }
+  if (y == 0 && col < width) to[int64_t(group) * width + col] = float(sums[0][x]);
+}
+
+__global__ __launch_bounds__(256) void layer_norm_zero_kernel(float* dw, float* db, int64_t n) {
+  for (int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x; i < n; i += int64_t(gridDim.x) * 256) {
+    if (dw) dw[i] = 0.f;
+    if (db) db[i] = 0.f;
+  }
+}
+
+using RowKernel = void (*)(RowNormArgs);
+
+template <bool kBackward, typename T, typename W, int kWaves, int kPieces>
+RowKernel row_kernel_of(bool whole) {
+  if constexpr (kBackward)
+    return whole ? layer_norm_backward_kernel<T, W, kWaves, kPieces, true> : layer_norm_backward_kernel<T, W, kWaves, kPieces, false>;
+  else
+    return whole ? layer_norm_kernel<T, W, kWaves, kPieces, true> : layer_norm_kernel<T, W, kWaves, kPieces, false>;
+}
+
+// Threads of a row
+int row_waves(int width) { return width <= 2048 ? 1 : width <= 8192 ? 4 : 16; }
+
+template <bool kBackward, typename T, typename W>
+RowKernel pick_row_kernel(int width, bool whole) {
+  switch (const int waves = row_waves(width); waves * 8 + (width + 512 * waves - 1) / (512 * waves)) {
+    case 8 + 1: return row_kernel_of<kBackward, T, W, 1, 1>(whole);
+    case 8 + 2: return row_kernel_of<kBackward, T, W, 1, 2>(whole);
+    case 8 + 3: return row_kernel_of<kBackward, T, W, 1, 3>(whole);
+    case 8 + 4: return row_kernel_of<kBackward, T, W, 1, 4>(whole);
+    case 32 + 2: return row_kernel_of<kBackward, T, W, 4, 2>(whole);
+    case 32 + 3: return row_kernel_of<kBackward, T, W, 4, 3>(whole);
+    case 32 + 4: return row_kernel_of<kBackward, T, W, 4, 4>(whole);
+    case 128 + 2: return row_kernel_of<kBackward, T, W, 16, 2>(whole);
+    case 128 + 3: return row_kernel_of<kBackward, T, W, 16, 3>(whole);
+    default: return row_kernel_of<kBackward, T, W, 16, 4>(whole);
+  }
+}
+
+template <bool kBackward>
+RowKernel pick_row_kernel(int dtype, int w_dtype, int width, bool whole) {
+  if (dtype == CA_F32) return pick_row_kernel<kBackward, float, float>(width, whole);
+  if (w_dtype == CA_F32) return pick_row_kernel<kBackward, uint16_t, float>(width, whole);
+  return pick_row_kernel<kBackward, uint16_t, uint16_t>(width, whole);
+}
+
+// Workgroups of a group: enough to fill the chip, no more than there are rows for
+int per_group(int64_t group_rows, int64_t groups, int width, int all) {
+  const int64_t rows = row_waves(width) == 1 ? 4 : 1, most = (group_rows + rows - 1) / rows;
+  return int(std::max<int64_t>(1, std::min(most, (all + groups - 1) / groups)));
+}
+constexpr int kForwardGroups = 2048, kBackwardGroups = 512;
+
+bool aligned(const void* p, int64_t ld, int64_t rows, int bytes_of_value) {
+  return reinterpret_cast<uintptr_t>(p) % 16 == 0 && (rows <= 1 || ld * bytes_of_value % 16 == 0);
+}
+
+}  // namespace
+
+int32_t launch_layer_norm(const RowNorm& n, const void* y, void* stream) {
+  if (n.rows == 0) return CA_OK;
+  const int size = n.dtype == CA_F32 ? 4 : 2, w_size = n.w_dtype == CA_F32 ? 4 : 2;
+  RowNormArgs a{};
+  a.x = n.x; a.w = n.w; a.b = n.b; a.y = const_cast<void*>(y);
+  a.ldx = n.ldx; a.ldy = n.ldy; a.ldw = n.ldw;
+  a.width = n.width; a.groups = int32_t(n.groups); a.group_rows = int32_t(n.rows / n.groups); a.eps = n.eps;
+  a.per_group = per_group(a.group_rows, n.groups, n.width, kForwardGroups);
+  const bool whole = n.width % 8 == 0 && aligned(n.x, n.ldx, n.rows, size) && aligned(y, n.ldy, n.rows, size) && aligned(n.w, n.ldw, n.groups, w_size) &&
+                     aligned(n.b, n.ldw, n.groups, w_size);
+  const int waves = row_waves(n.width);
+  hipLaunchKernelGGL(pick_row_kernel<false>(n.dtype, n.w_dtype, n.width, whole), dim3(unsigned(n.groups * a.per_group)), dim3(waves == 1 ? 256 : 64 * waves), 0,
+                     static_cast<hipStream_t>(stream), a);
+  return finish_launch("layer_norm.hip");
+}
+
+size_t layer_norm_backward_bytes(int64_t rows, int32_t width, int64_t groups) {
+  const int parts = rows > 0 ? per_group(rows / groups, groups, width, kBackwardGroups) : 1;
+  return parts > 1 ? size_t(groups) * parts * 2 * width * sizeof(float) : 0;
+}
+
+int32_t launch_layer_norm_backward(const RowNorm& n, const void* dy, int64_t lddy, void* dx, float* dw, float* db, void* workspace, void* stream) {
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  const int64_t all = n.groups * n.width;
+  if (n.rows == 0) {                               // of no rows the weights' gradients are zero
+    if (!dw && !db) return CA_OK;
+    hipLaunchKernelGGL(layer_norm_zero_kernel, dim3(unsigned(std::min<int64_t>((all + 255) / 256, 4096))), dim3(256), 0, s, dw, db, all);
+    return finish_launch("layer_norm.hip");
+  }
+  const int size = n.dtype == CA_F32 ? 4 : 2, w_size = n.w_dtype == CA_F32 ? 4 : 2;
+  RowNormArgs a{};
+  a.x = n.x; a.dy = dy; a.w = n.w; a.y = dx;
+  a.ldx = n.ldx; a.lddy = lddy; a.ldy = n.ldy; a.ldw = n.ldw;
+  a.width = n.width; a.groups = int32_t(n.groups); a.group_rows = int32_t(n.rows / n.groups); a.eps = n.eps;
+  a.per_group = per_group(a.group_rows, n.groups, n.width, kBackwardGroups);
+  float* const parts = static_cast<float*>(workspace);
+  const bool split = a.per_group > 1;
+  if (dw) a.dw = split ? parts : dw;
+  if (db) a.db = split ? parts + n.width : db;
+  const bool whole = n.width % 8 == 0 && aligned(n.x, n.ldx, n.rows, size) && aligned(dy, lddy, n.rows, size) && aligned(dx, n.ldy, n.rows, size) &&
+                     aligned(n.w, n.ldw, n.groups, w_size);
+  const int waves = row_waves(n.width);
+  hipLaunchKernelGGL(pick_row_kernel<true>(n.dtype, n.w_dtype, n.width, whole), dim3(unsigned(n.groups * a.per_group)), dim3(waves == 1 ? 256 : 64 * waves), 0, s, a);
+  if (const int32_t rc = finish_launch("layer_norm.hip"); rc != CA_OK) return rc;
+  if (!split || (!dw && !db)) return CA_OK;
+  const int columns = (n.width + kSumCols - 1) / kSumCols;
+  hipLaunchKernelGGL(layer_norm_sum_kernel, dim3(unsigned(n.groups * columns), 2), dim3(kSumCols * kSumRows), 0, s, parts, a.per_group, n.width, columns, dw, db);
+  return finish_launch("layer_norm.hip");
+}
+
+}  // namespace ca

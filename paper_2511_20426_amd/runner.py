@@ -6,6 +6,7 @@ backward pass (qk_norm_rope_backward, gated_linear_backward) the caller calls it
 """
 from __future__ import annotations
 
+import contextlib
 from typing import Sequence
 
 import torch
@@ -437,6 +438,73 @@ def gated_linear_backward(dh: torch.Tensor, x: torch.Tensor, w_gate: torch.Tenso
                                 _ACTIVATIONS[activation], dx.data_ptr(), dw[0].data_ptr(), dw[1].data_ptr(), m, f, k, lddh, ldx, ldg, ldu,
                                 k, k, work.data_ptr(), nbytes, _current_stream(device))
     return dx, dw[0], dw[1]
+
+
+_TYPES = {torch.float32: B.CA_F32, torch.bfloat16: B.CA_BF16}
+
+
+def _on_device(device: torch.device):
+    """Launches go to the current device: the tensors' own, where that is another."""
+    return contextlib.nullcontext() if device.index == torch.cuda.current_device() else torch.cuda.device(device)
+
+
+def _rows(t: torch.Tensor, like: torch.Tensor, dtype, rows: int, cols: int) -> int:
+    """The row stride of a [rows, cols] matrix of any alignment with unit stride along its rows; that of a single row is free."""
+    assert t.dtype == dtype and t.shape == (rows, cols) and (t.stride(1) == 1 or cols == 1) and _reachable(t, like)
+    return t.stride(0) if rows > 1 else cols
+
+
+def _norm_weights(x, weight, bias):
+    """(type, groups, row stride) of a norm's weights: [width], or [groups, width] for as many equal runs of rows."""
+    given = [t for t in (weight, bias) if t is not None]
+    if not given:
+        return B.CA_F32, 1, x.shape[1]
+    w = given[0]
+    assert w.dtype in (torch.float32, x.dtype) and w.dim() in (1, 2) and w.shape[-1] == x.shape[1] and (w.stride(-1) == 1 or w.shape[-1] == 1)
+    assert all(t.dtype == w.dtype and t.shape == w.shape and t.stride() == w.stride() and _reachable(t, x) for t in given)
+    groups = w.shape[0] if w.dim() == 2 else 1
+    assert groups >= 1 and x.shape[0] % groups == 0, "rows are dealt to the weights in equal runs"
+    return _TYPES[w.dtype], groups, w.stride(0) if groups > 1 else x.shape[1]
+
+
+def _address(t: torch.Tensor | None) -> int:
+    return 0 if t is None else t.data_ptr()
+
+
+def layer_norm(x: torch.Tensor, weight: torch.Tensor | None = None, bias: torch.Tensor | None = None, eps: float = 1e-6,
+               out: torch.Tensor | None = None) -> torch.Tensor:
+    """y = weight * (x - mean) / sqrt(mean((x - mean)^2) + eps) + bias of each row: x [M, W] in bf16 or fp32, rows may be strided; weight and bias (either
+    or both may be None) [W], or [G, W] for G equal runs of consecutive rows, as the blocks in flight are (modulation by the timestep: 1 + scale
+    and shift), of x's type or fp32, with the same strides.  out may be x."""
+    assert x.is_cuda and x.dtype in _TYPES and x.dim() == 2
+    m, width = x.shape
+    w_type, groups, ldw = _norm_weights(x, weight, bias)
+    ldx = _rows(x, x, x.dtype, m, width)
+    y = torch.empty((m, width), dtype=x.dtype, device=x.device) if out is None else out
+    ldy = _rows(y, x, x.dtype, m, width)
+    with _on_device(x.device):
+        B.layer_norm(x.data_ptr(), _TYPES[x.dtype], _address(weight), _address(bias), w_type, eps, y.data_ptr(), m, width, groups, ldx, ldw, ldy,
+                     _current_stream(x.device))
+    return y
+
+
+def layer_norm_backward(dy: torch.Tensor, x: torch.Tensor, weight: torch.Tensor | None = None, bias: torch.Tensor | None = None, eps: float = 1e-6,
+                        dx: torch.Tensor | None = None):
+    """Gradients of layer_norm: (dx, dweight, dbias) from that of its result and its arguments, the weights' in fp32 and of the weights' shapes (None for
+    those that are None).  dx may be dy."""
+    assert x.is_cuda and x.dtype in _TYPES and x.dim() == 2
+    m, width = x.shape
+    w_type, groups, ldw = _norm_weights(x, weight, bias)
+    ldx, lddy = _rows(x, x, x.dtype, m, width), _rows(dy, x, x.dtype, m, width)
+    g = torch.empty((m, width), dtype=x.dtype, device=x.device) if dx is None else dx
+    lddx = _rows(g, x, x.dtype, m, width)
+    dw, db = (None if t is None else torch.empty(t.shape, dtype=torch.float32, device=x.device) for t in (weight, bias))
+    nbytes = B.layer_norm_backward_workspace(m, width, groups)
+    work = torch.empty(nbytes, dtype=torch.uint8, device=x.device)
+    with _on_device(x.device):
+        B.layer_norm_backward(dy.data_ptr(), x.data_ptr(), _TYPES[x.dtype], _address(weight), w_type, eps, g.data_ptr(), _address(dw), _address(db), m,
+                              width, groups, lddy, ldx, ldw, lddx, work.data_ptr(), nbytes, _current_stream(x.device))
+    return g, dw, db
 
 
 def attention_layer(pool: CascadePool, x: torch.Tensor, w_qkv: torch.Tensor, w_out: torch.Tensor,
