@@ -364,6 +364,38 @@ int32_t layer_norm_backward(const void* dy_dev, const void* x_dev, int32_t dtype
                             float* dweight_dev, float* dbias_dev, int64_t rows, int32_t width, int64_t groups, int64_t lddy, int64_t ldx, int64_t ldw,
                             int64_t lddx, void* workspace_dev, size_t workspace_bytes, void* hip_stream);
 
+/* One AdamW step of many tensors: with g = grad_scale * grad and t the steps of a tensor up to and with this one,
+ * m = beta1 m + (1 - beta1) g, v = beta2 v + (1 - beta2) g^2, param = (1 - lr weight_decay) param - lr / (1 - beta1^t) m / (sqrt(v / (1 - beta2^t)) + eps),
+ * in fp32, the parameter rounded to its type once.  Of a tensor without a gradient (null) nothing changes.
+ *   param, grad   n values each, packed, fp32 or bf16, aligned as their values are; copy (or null; fp32 parameters only): gets the new ones in bf16
+ *   m, v          state_bits 32: fp32, n values.  8: codes (int8, uint8) of n values, up to the next multiple of 256, all zero at first, with a scale for
+ *                 every 256 in m_scale and v_scale: m = sign(c) scale (c / 127)^2, v = scale (c / 255)^4, the scale the largest magnitude, codes
+ *                 rounded to the nearest (of v > 0 at least 1), m and v being computed in 64 bits; the parameter moves by m and v as they are
+ *                 before they become codes.  Aligned to 16 bytes.  A gradient that is not finite (or whose square passes fp32) makes all values
+ *                 that share its scale infinite or NaN.
+ *   step          four numbers on the device, aligned to 16 bytes: steps done (0 at first; the call adds one, so that a recorded call counts on in every
+ *                 replay), and room that the call uses
+ * Tensors, copies, states and steps overlap nothing else of the call.  lr, weight_decay and the like are taken when the call is made: a recorded one keeps
+ * them.  0 <= beta < 1, eps > 0 (CA_EINVAL); n <= CA_ADAMW_MAX_VALUES.  Two launches for every 40 tensors. */
+#define CA_ADAMW_MAX_VALUES ((int64_t)1 << 40)
+typedef struct {
+  void* param;
+  const void* grad;
+  void* copy;
+  void* m;
+  void* v;
+  float* m_scale;
+  float* v_scale;
+  int32_t* step;
+  int64_t n;
+  int32_t param_dtype, grad_dtype;
+} ca_adamw_tensor;
+int32_t layer_adamw(const ca_adamw_tensor* tensors, int32_t n_tensors, int32_t state_bits, double lr, double beta1, double beta2, double eps,
+                    double weight_decay, double grad_scale, void* hip_stream);
+/* What states in 8 bits stand for, in fp32: n values, a multiple of 256 (codes and results aligned to 16 bytes). */
+int32_t layer_adamw_values(const void* m_codes_dev, const void* v_codes_dev, const float* m_scales_dev, const float* v_scales_dev, float* m_dev,
+                           float* v_dev, int64_t n, void* hip_stream);
+
 /* ---- Cascade scheduler: the control flow of Algorithm 1, host integers only.
  * State (b, tau, d) = primary block, timestep index of the primary block, cascade depth.  An
  * iteration forwards blocks b .. b + min(d, G-1), block b+i at timesteps[tau - i] (older blocks

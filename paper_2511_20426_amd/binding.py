@@ -38,7 +38,7 @@ EXPORTS = (
     "ca_mfma_microbench", "layer_linear_bf16", "layer_qkv_publish",
     "layer_qk_norm_rope", "layer_qk_norm_rope_workspace", "layer_qk_norm_rope_backward", "kv_cache_append_batch_norm", "layer_quantize_rows_i8",
     "layer_linear_i8", "layer_linear_i8_workspace", "layer_linear_i8_values", "layer_gated_bf16", "layer_gated_saved_bytes", "layer_gated_backward_workspace", "layer_gated_backward_bf16",
-    "layer_norm", "layer_norm_backward_workspace", "layer_norm_backward",
+    "layer_norm", "layer_norm_backward_workspace", "layer_norm_backward", "layer_adamw", "layer_adamw_values",
     "ca_sched_create", "ca_sched_create_lagged", "ca_sched_destroy", "ca_sched_batch", "ca_sched_advance", "ca_sched_state",
 )
 
@@ -72,6 +72,11 @@ class CascadeAttnError(RuntimeError):
         detail = lib.ca_last_device_error().decode() if code == CA_EDEVICE else ""
         super().__init__(f"{what}: {strerror(code)} ({code}) {detail}")
         self.code = code
+
+
+class ca_adamw_tensor(C.Structure):
+    _fields_ = [(name, C.c_void_p) for name in ("param", "grad", "copy", "m", "v", "m_scale", "v_scale", "step")] + [
+        ("n", C.c_int64), ("param_dtype", C.c_int32), ("grad_dtype", C.c_int32)]
 
 
 def _build(what: str) -> None:
@@ -176,6 +181,11 @@ def _load() -> C.CDLL:
     lib.layer_norm_backward_workspace.argtypes = [i64, i32, i64]
     lib.layer_norm_backward.restype = i32
     lib.layer_norm_backward.argtypes = [vp, vp, i32, vp, i32, f32, vp, vp, vp, i64, i32] + [i64] * 5 + [vp, C.c_size_t, vp]
+    f64 = C.c_double
+    lib.layer_adamw.restype = i32
+    lib.layer_adamw.argtypes = [C.POINTER(ca_adamw_tensor), i32, i32] + [f64] * 6 + [vp]
+    lib.layer_adamw_values.restype = i32
+    lib.layer_adamw_values.argtypes = [vp] * 6 + [i64, vp]
     lib.ca_sched_create.restype = i32
     lib.ca_sched_create.argtypes = [i64, i32, C.POINTER(i32), i32, C.POINTER(vp)]
     lib.ca_sched_create_lagged.restype = i32
@@ -506,6 +516,17 @@ def layer_norm_backward(dy_ptr: int, x_ptr: int, dtype: int, weight_ptr: int, we
     _check(lib.layer_norm_backward(index(dy_ptr or 0), index(x_ptr or 0), dtype, index(weight_ptr or 0), weight_dtype, eps, index(dx_ptr or 0),
                                    index(dweight_ptr or 0), index(dbias_ptr or 0), rows, width, groups, lddy, ldx, ldw, lddx, index(workspace_ptr or 0),
                                    workspace_bytes, index(stream or 0)), "layer_norm_backward")
+
+
+def layer_adamw(tensors, n_tensors: int, state_bits: int, lr: float, beta1: float, beta2: float, eps: float, weight_decay: float, grad_scale: float,
+                stream: int = 0) -> None:
+    """tensors: an array of ca_adamw_tensor"""
+    _check(lib.layer_adamw(tensors, n_tensors, state_bits, lr, beta1, beta2, eps, weight_decay, grad_scale, index(stream or 0)), "layer_adamw")
+
+
+def layer_adamw_values(m_codes_ptr: int, v_codes_ptr: int, m_scales_ptr: int, v_scales_ptr: int, m_ptr: int, v_ptr: int, n: int, stream: int = 0) -> None:
+    _check(lib.layer_adamw_values(index(m_codes_ptr or 0), index(v_codes_ptr or 0), index(m_scales_ptr or 0), index(v_scales_ptr or 0), index(m_ptr or 0),
+                                  index(v_ptr or 0), n, index(stream or 0)), "layer_adamw_values")
 
 
 def mfma_microbench(data_kind: int, trips: int, scratch_ptr: int, scratch_bytes: int, stream: int = 0):

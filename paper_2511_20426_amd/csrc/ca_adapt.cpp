@@ -23,6 +23,19 @@ int32_t check_row_norm(const ca::RowNorm& n) {
   return (n.w || n.b) && n.groups > 1 && n.ldw < n.width ? CA_EINVAL : CA_OK;
 }
 
+// of the state's two buffers: codes and fp32 values are moved in pieces of up to 16 bytes
+int32_t check_adamw(const ca_adamw_tensor& t, int32_t state_bits) {
+  if (t.n < 0 || !dtype_ok(t.param_dtype) || !dtype_ok(t.grad_dtype)) return CA_EINVAL;
+  if (t.n > CA_ADAMW_MAX_VALUES) return CA_EUNSUPPORTED;
+  if (t.n == 0 || !t.grad) return CA_OK;
+  if (!t.param || !t.m || !t.v || !t.step) return CA_EINVAL;
+  if (!aligned(t.param, size_of(t.param_dtype)) || !aligned(t.grad, size_of(t.grad_dtype)) || !aligned(t.copy, 2) || !aligned(t.m, 16) || !aligned(t.v, 16) ||
+      !aligned(t.step, 16))
+    return CA_EINVAL;
+  if (t.copy && t.param_dtype != CA_F32) return CA_EINVAL;
+  return state_bits == 8 && (!t.m_scale || !t.v_scale || !aligned(t.m_scale, 4) || !aligned(t.v_scale, 4)) ? CA_EINVAL : CA_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -53,6 +66,26 @@ int32_t layer_norm_backward(const void* dy_dev, const void* x_dev, int32_t dtype
     if (need > 0 && (!workspace_dev || !aligned(workspace_dev, 16) || workspace_bytes < need)) return CA_EINVAL;
   }
   return ca::launch_layer_norm_backward(n, dy_dev, lddy, dx_dev, dweight_dev, dbias_dev, workspace_dev, hip_stream);
+}
+
+int32_t layer_adamw(const ca_adamw_tensor* tensors, int32_t n_tensors, int32_t state_bits, double lr, double beta1, double beta2, double eps,
+                    double weight_decay, double grad_scale, void* hip_stream) {
+  if (n_tensors < 0 || (n_tensors > 0 && !tensors) || (state_bits != 8 && state_bits != 32)) return CA_EINVAL;
+  if (!(lr >= 0.) || !(weight_decay >= 0.) || !(beta1 >= 0. && beta1 < 1.) || !(beta2 >= 0. && beta2 < 1.) || !(float(eps) > 0.f)) return CA_EINVAL;
+  if (!std::isfinite(float(lr)) || !std::isfinite(lr * weight_decay) || !std::isfinite(float(eps)) || !std::isfinite(float(grad_scale))) return CA_EINVAL;
+  for (int32_t i = 0; i < n_tensors; ++i)
+    if (int32_t rc = check_adamw(tensors[i], state_bits)) return rc;
+  return ca::launch_adamw(tensors, n_tensors, state_bits, lr, beta1, beta2, eps, weight_decay, grad_scale, hip_stream);
+}
+
+int32_t layer_adamw_values(const void* m_codes_dev, const void* v_codes_dev, const float* m_scales_dev, const float* v_scales_dev, float* m_dev,
+                           float* v_dev, int64_t n, void* hip_stream) {
+  if (n < 0 || n % 256 != 0) return CA_EINVAL;
+  if (n == 0) return CA_OK;
+  for (const void* p : {m_codes_dev, v_codes_dev, static_cast<const void*>(m_dev), static_cast<const void*>(v_dev)})
+    if (!p || !aligned(p, 16)) return CA_EINVAL;
+  if (!m_scales_dev || !v_scales_dev || !aligned(m_scales_dev, 4) || !aligned(v_scales_dev, 4)) return CA_EINVAL;
+  return ca::launch_adamw_values(m_codes_dev, v_codes_dev, m_scales_dev, v_scales_dev, m_dev, v_dev, n, hip_stream);
 }
 
 }  // extern "C"

@@ -1,0 +1,90 @@
+"""The optimizer of a layer's weights and adapters: AdamW over many tensors in one call (layer_adamw), states in 32 bits or in 8."""
+from __future__ import annotations
+
+import ctypes as C
+from typing import Sequence
+
+import torch
+
+from . import binding as B
+from .runner import _TYPES, _current_stream, _on_device
+
+_BLOCK = 256                                     # values to a scale; the states of a tensor begin at a multiple
+
+
+class AdamW:
+    """m = b1 m + (1 - b1) g, v = b2 v + (1 - b2) g^2, p = (1 - lr wd) p - lr / (1 - b1^t) m / (sqrt(v / (1 - b2^t)) + eps).
+
+    params: tensors of one device, packed, bf16 or fp32, that share no memory; they are updated in place.  copies: None, or for each of them None or a
+    bf16 tensor that gets the new values as well (for a master in fp32).  state_bits 8: m and v as codes with a scale for every 256 values (cascade_attn.h says
+    which).  lr, betas, eps and weight_decay are plain attributes that each step reads; a step that is captured into a graph keeps those it was
+    captured with, while the number of steps goes on in every replay, for it is kept on the device: steps[i] of tensor i."""
+
+    def __init__(self, params: Sequence[torch.Tensor], lr: float = 1e-3, betas: tuple[float, float] = (0.9, 0.999), eps: float = 1e-8,
+                 weight_decay: float = 1e-2, state_bits: int = 32, copies: Sequence[torch.Tensor | None] | None = None):
+        self.params, self.copies = list(params), [None] * len(params) if copies is None else list(copies)
+        self.lr, self.betas, self.eps, self.weight_decay, self.state_bits = lr, betas, eps, weight_decay, state_bits
+        assert state_bits in (8, 32) and self.params and len(self.copies) == len(self.params)
+        self.device = device = self.params[0].device
+        assert all(p.is_cuda and p.device == device and p.dtype in _TYPES and p.is_contiguous() for p in self.params)
+        assert all(c is None or (c.device == device and c.dtype == torch.bfloat16 and c.is_contiguous() and c.shape == p.shape and p.dtype == torch.float32)
+                   for p, c in zip(self.params, self.copies))
+        spans = sorted((t.data_ptr(), t.data_ptr() + t.numel() * t.element_size()) for t in self.params + self.copies if t is not None and t.numel())
+        assert all(a[1] <= b[0] for a, b in zip(spans, spans[1:])), "tensors share memory"
+        sizes = [p.numel() for p in self.params]
+        self.offsets = [0]                       # where the states of tensor i begin among all; and how many places there are
+        for n in sizes:
+            self.offsets.append(self.offsets[-1] + -(-n // _BLOCK) * _BLOCK)
+        room = self.offsets[-1]
+
+        def zeros(n, dtype):
+            return torch.zeros(n, dtype=dtype, device=device)
+
+        m_type, v_type = (torch.float32, torch.float32) if state_bits == 32 else (torch.int8, torch.uint8)
+        self.m, self.v = zeros(room, m_type), zeros(room, v_type)
+        self.m_scale, self.v_scale = (None, None) if state_bits == 32 else (zeros(room // _BLOCK, torch.float32), zeros(room // _BLOCK, torch.float32))
+        self._steps = zeros((len(sizes), 4), torch.int32)
+        self.steps = self._steps[:, 0]
+        self._tensors = (B.ca_adamw_tensor * len(sizes))()
+        size = self.m.element_size()
+        for i, (t, p, c, at) in enumerate(zip(self._tensors, self.params, self.copies, self.offsets)):
+            t.param, t.copy, t.n, t.param_dtype = p.data_ptr(), 0 if c is None else c.data_ptr(), sizes[i], _TYPES[p.dtype]
+            t.m, t.v, t.step = self.m.data_ptr() + at * size, self.v.data_ptr() + at * size, self._steps.data_ptr() + 16 * i
+            if state_bits == 8:
+                t.m_scale, t.v_scale = self.m_scale.data_ptr() + at // _BLOCK * 4, self.v_scale.data_ptr() + at // _BLOCK * 4
+
+    def step(self, grads: Sequence[torch.Tensor | None], grad_scale: float = 1.0) -> None:
+        """One step by the gradients, each of its parameter's shape, packed, bf16 or fp32, or None: that tensor and its state stay as they are.
+        grad_scale: what they are multiplied with first."""
+        assert len(grads) == len(self.params)
+        for t, p, g in zip(self._tensors, self.params, grads):
+            if g is None:
+                t.grad = None
+                continue
+            assert g.device == self.device and g.dtype in _TYPES and g.shape == p.shape and g.is_contiguous()
+            t.grad, t.grad_dtype = g.data_ptr(), _TYPES[g.dtype]
+        with _on_device(self.device):
+            B.layer_adamw(self._tensors, len(self._tensors), self.state_bits, self.lr, *self.betas, self.eps, self.weight_decay, grad_scale,
+                          _current_stream(self.device))
+
+    def state_values(self) -> tuple[torch.Tensor, torch.Tensor]:
+        """m and v of all tensors in fp32, those of tensor i from offsets[i] on: the states themselves, or what their codes stand for."""
+        if self.state_bits == 32:
+            return self.m, self.v
+        m, v = (torch.empty(self.m.shape, dtype=torch.float32, device=self.device) for _ in range(2))
+        with _on_device(self.device):
+            B.layer_adamw_values(self.m.data_ptr(), self.v.data_ptr(), self.m_scale.data_ptr(), self.v_scale.data_ptr(), m.data_ptr(), v.data_ptr(),
+                                 m.numel(), _current_stream(self.device))
+        return m, v
+
+    def load_state(self, m: torch.Tensor, v: torch.Tensor, step: int | Sequence[int], m_scale: torch.Tensor | None = None,
+                   v_scale: torch.Tensor | None = None) -> None:
+        """States as m, v, m_scale and v_scale hold them (a checkpoint's), and how many steps are behind them: of all tensors, or of each."""
+        for mine, given in ((self.m, m), (self.v, v), (self.m_scale, m_scale), (self.v_scale, v_scale)):
+            assert (mine is None) == (given is None)
+            if mine is not None:
+                assert given.dtype == mine.dtype and given.shape == mine.shape
+                mine.copy_(given)
+        steps = torch.as_tensor(step, dtype=torch.int32)
+        assert steps.shape in ((), self.steps.shape) and bool((steps >= 0).all())
+        self.steps.copy_(steps)
