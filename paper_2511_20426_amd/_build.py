@@ -14,7 +14,7 @@ LIB = os.environ.get("CASCADE_ATTN_LIB") or os.path.join(PKG, "libcascade_attn.s
 
 SOURCES = ["ca_meta.cpp", "ca_api.cpp", "ca_sched.cpp", "rope_cache.hip", "attn_f32.hip", "attn_bf16.hip", "mfma_peak.hip", "gemm_bf16.hip", "gemm_rows.hip", "gemm_tiles.hip",
            "ca_layer.cpp", "norm_rope.hip", "quantize.hip", "gemm_i8.hip", "gemm_gated.hip", "gated_backward.hip",
-           "ca_adapt.cpp", "layer_norm.hip", "adamw.hip"]
+           "ca_adapt.cpp", "layer_norm.hip", "adamw.hip", "gemm_adapted.hip"]
 
 # packed fp32 instructions are kept off for all device code
 DEVICE_FLAGS = ["-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"]

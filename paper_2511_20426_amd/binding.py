@@ -39,6 +39,7 @@ EXPORTS = (
     "layer_qk_norm_rope", "layer_qk_norm_rope_workspace", "layer_qk_norm_rope_backward", "kv_cache_append_batch_norm", "layer_quantize_rows_i8",
     "layer_linear_i8", "layer_linear_i8_workspace", "layer_linear_i8_values", "layer_gated_bf16", "layer_gated_saved_bytes", "layer_gated_backward_workspace", "layer_gated_backward_bf16",
     "layer_norm", "layer_norm_backward_workspace", "layer_norm_backward", "layer_adamw", "layer_adamw_values",
+    "layer_linear_adapted_bf16", "layer_linear_adapted_backward_workspace", "layer_linear_adapted_backward_bf16",
     "ca_sched_create", "ca_sched_create_lagged", "ca_sched_destroy", "ca_sched_batch", "ca_sched_advance", "ca_sched_state",
 )
 
@@ -181,6 +182,12 @@ def _load() -> C.CDLL:
     lib.layer_norm_backward_workspace.argtypes = [i64, i32, i64]
     lib.layer_norm_backward.restype = i32
     lib.layer_norm_backward.argtypes = [vp, vp, i32, vp, i32, f32, vp, vp, vp, i64, i32] + [i64] * 5 + [vp, C.c_size_t, vp]
+    lib.layer_linear_adapted_bf16.restype = i32
+    lib.layer_linear_adapted_bf16.argtypes = [vp] * 8 + [i64] + [i32] * 4 + [i64] * 3 + [vp]
+    lib.layer_linear_adapted_backward_workspace.restype = C.c_size_t
+    lib.layer_linear_adapted_backward_workspace.argtypes = [i64] + [i32] * 4
+    lib.layer_linear_adapted_backward_bf16.restype = i32
+    lib.layer_linear_adapted_backward_bf16.argtypes = [vp] * 11 + [i64] + [i32] * 5 + [i64] * 4 + [vp, C.c_size_t, vp]
     f64 = C.c_double
     lib.layer_adamw.restype = i32
     lib.layer_adamw.argtypes = [C.POINTER(ca_adamw_tensor), i32, i32] + [f64] * 6 + [vp]
@@ -516,6 +523,26 @@ def layer_norm_backward(dy_ptr: int, x_ptr: int, dtype: int, weight_ptr: int, we
     _check(lib.layer_norm_backward(index(dy_ptr or 0), index(x_ptr or 0), dtype, index(weight_ptr or 0), weight_dtype, eps, index(dx_ptr or 0),
                                    index(dweight_ptr or 0), index(dbias_ptr or 0), rows, width, groups, lddy, ldx, ldw, lddx, index(workspace_ptr or 0),
                                    workspace_bytes, index(stream or 0)), "layer_norm_backward")
+
+
+def layer_linear_adapted_bf16(x_ptr: int, w_ptr: int, down_ptr: int, up_ptr: int, scales_ptr: int, index_ptr: int, low_ptr: int, y_ptr: int, m_rows: int,
+                              n_out: int, k_in: int, adapters: int, rank: int, ldx: int, ldw: int, ldy: int, stream: int = 0) -> None:
+    _check(lib.layer_linear_adapted_bf16(*(index(p or 0) for p in (x_ptr, w_ptr, down_ptr, up_ptr, scales_ptr, index_ptr, low_ptr, y_ptr)), m_rows, n_out,
+                                         k_in, adapters, rank, ldx, ldw, ldy, index(stream or 0)), "layer_linear_adapted_bf16")
+
+
+def layer_linear_adapted_backward_workspace(m_rows: int, n_out: int, k_in: int, adapters: int, rank: int) -> int:
+    return int(lib.layer_linear_adapted_backward_workspace(m_rows, n_out, k_in, adapters, rank))
+
+
+def layer_linear_adapted_backward_bf16(dy_ptr: int, x_ptr: int, w_t_ptr: int, down_ptr: int, up_ptr: int, scales_ptr: int, index_ptr: int, low_ptr: int,
+                                       dx_ptr: int, d_down_ptr: int, d_up_ptr: int, m_rows: int, n_out: int, k_in: int, adapters: int, rank: int,
+                                       rank_used: int, lddy: int, ldx: int, ldw_t: int, lddx: int, workspace_ptr: int, workspace_bytes: int,
+                                       stream: int = 0) -> None:
+    _check(lib.layer_linear_adapted_backward_bf16(*(index(p or 0) for p in (dy_ptr, x_ptr, w_t_ptr, down_ptr, up_ptr, scales_ptr, index_ptr, low_ptr, dx_ptr,
+                                                                            d_down_ptr, d_up_ptr)), m_rows, n_out, k_in, adapters, rank, rank_used, lddy, ldx,
+                                                  ldw_t, lddx, index(workspace_ptr or 0), workspace_bytes, index(stream or 0)),
+           "layer_linear_adapted_backward_bf16")
 
 
 def layer_adamw(tensors, n_tensors: int, state_bits: int, lr: float, beta1: float, beta2: float, eps: float, weight_decay: float, grad_scale: float,

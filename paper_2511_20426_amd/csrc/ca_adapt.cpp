@@ -23,6 +23,28 @@ int32_t check_row_norm(const ca::RowNorm& n) {
   return (n.w || n.b) && n.groups > 1 && n.ldw < n.width ? CA_EINVAL : CA_OK;
 }
 
+constexpr int64_t kMaxAdaptedRows = int64_t(1) << 30, kMaxLd = int64_t(1) << 22;
+constexpr int32_t kMaxColumns = 1 << 20;
+
+int32_t check_ld(int64_t ld, int64_t cols) {
+  if (ld < cols || ld % 8 != 0) return CA_EINVAL;
+  return ld >= kMaxLd ? CA_EUNSUPPORTED : CA_OK;
+}
+
+int32_t check_adapted(int64_t m_rows, int32_t n_out, int32_t k_in, int32_t adapters, int32_t rank) {
+  if (m_rows < 0 || adapters < 1) return CA_EINVAL;
+  if (m_rows > kMaxAdaptedRows || n_out < 8 || n_out % 8 != 0 || n_out > kMaxColumns || k_in < 128 || k_in % 128 != 0 || k_in > kMaxColumns ||
+      adapters > CA_MAX_ADAPTERS || (rank != 32 && rank != 64 && rank != 128))
+    return CA_EUNSUPPORTED;
+  return CA_OK;
+}
+
+// the products of the backward pass sum over the columns of Y too
+int32_t check_adapted_backward(int64_t m_rows, int32_t n_out, int32_t k_in, int32_t adapters, int32_t rank) {
+  if (int32_t rc = check_adapted(m_rows, n_out, k_in, adapters, rank)) return rc;
+  return n_out % 128 != 0 ? CA_EUNSUPPORTED : CA_OK;
+}
+
 // of the state's two buffers: codes and fp32 values are moved in pieces of up to 16 bytes
 int32_t check_adamw(const ca_adamw_tensor& t, int32_t state_bits) {
   if (t.n < 0 || !dtype_ok(t.param_dtype) || !dtype_ok(t.grad_dtype)) return CA_EINVAL;
@@ -66,6 +88,50 @@ int32_t layer_norm_backward(const void* dy_dev, const void* x_dev, int32_t dtype
     if (need > 0 && (!workspace_dev || !aligned(workspace_dev, 16) || workspace_bytes < need)) return CA_EINVAL;
   }
   return ca::launch_layer_norm_backward(n, dy_dev, lddy, dx_dev, dweight_dev, dbias_dev, workspace_dev, hip_stream);
+}
+
+int32_t layer_linear_adapted_bf16(const void* x_dev, const void* w_dev, const void* down_dev, const void* up_dev, const float* scales_dev,
+                                  const int32_t* index_dev, void* low_dev, void* y_dev, int64_t m_rows, int32_t n_out, int32_t k_in, int32_t adapters,
+                                  int32_t rank, int64_t ldx, int64_t ldw, int64_t ldy, void* hip_stream) {
+  if (int32_t rc = check_adapted(m_rows, n_out, k_in, adapters, rank)) return rc;
+  for (int64_t ld : {ldx, ldw})
+    if (int32_t rc = check_ld(ld, k_in)) return rc;
+  if (ldy < n_out || ldy % 8 != 0) return CA_EINVAL;
+  if (m_rows == 0) return CA_OK;
+  for (const void* p : {x_dev, w_dev, down_dev, up_dev, static_cast<const void*>(low_dev), static_cast<const void*>(y_dev)})
+    if (!p || !aligned(p, 16)) return CA_EINVAL;
+  if (!scales_dev || !index_dev || !aligned(scales_dev, 4) || !aligned(index_dev, 4)) return CA_EINVAL;
+  const ca::AdaptedLinear p{x_dev, w_dev, down_dev, up_dev, scales_dev, index_dev, m_rows, ldx, ldw, ldy, n_out, k_in, adapters, rank};
+  return ca::launch_gemm_adapted(p, y_dev, low_dev, hip_stream);
+}
+
+size_t layer_linear_adapted_backward_workspace(int64_t m_rows, int32_t n_out, int32_t k_in, int32_t adapters, int32_t rank) {
+  return check_adapted_backward(m_rows, n_out, k_in, adapters, rank) ? 0 : ca::adapted_backward_bytes(m_rows, n_out, k_in, adapters, rank);
+}
+
+int32_t layer_linear_adapted_backward_bf16(const void* dy_dev, const void* x_dev, const void* w_t_dev, const void* down_dev, const void* up_dev,
+                                           const float* scales_dev, const int32_t* index_dev, const void* low_dev, void* dx_dev, void* d_down_dev,
+                                           void* d_up_dev, int64_t m_rows, int32_t n_out, int32_t k_in, int32_t adapters, int32_t rank, int32_t rank_used,
+                                           int64_t lddy, int64_t ldx, int64_t ldw_t, int64_t lddx, void* workspace_dev, size_t workspace_bytes,
+                                           void* hip_stream) {
+  if (int32_t rc = check_adapted_backward(m_rows, n_out, k_in, adapters, rank)) return rc;
+  if (rank_used < 1 || rank_used > rank || (!dx_dev && !d_down_dev && !d_up_dev)) return CA_EINVAL;
+  if (int32_t rc = check_ld(lddy, n_out)) return rc;
+  if (d_down_dev)
+    if (int32_t rc = check_ld(ldx, k_in)) return rc;
+  if (dx_dev) {
+    if (int32_t rc = check_ld(ldw_t, n_out)) return rc;
+    if (lddx < k_in || lddx % 8 != 0) return CA_EINVAL;
+  }
+  if (!workspace_dev || !aligned(workspace_dev, 16) || workspace_bytes < ca::adapted_backward_bytes(m_rows, n_out, k_in, adapters, rank)) return CA_EINVAL;
+  if (!aligned(d_down_dev, 2) || !aligned(d_up_dev, 2) || !aligned(dx_dev, 16)) return CA_EINVAL;
+  if (m_rows > 0) {
+    for (const void* p : {dy_dev, up_dev, dx_dev ? w_t_dev : dy_dev, dx_dev ? down_dev : dy_dev, d_down_dev ? x_dev : dy_dev, d_up_dev ? low_dev : dy_dev})
+      if (!p || !aligned(p, 16)) return CA_EINVAL;
+    if (!scales_dev || !index_dev || !aligned(scales_dev, 4) || !aligned(index_dev, 4)) return CA_EINVAL;
+  }
+  const ca::AdaptedLinear p{x_dev, w_t_dev, down_dev, up_dev, scales_dev, index_dev, m_rows, ldx, ldw_t, lddx, n_out, k_in, adapters, rank};
+  return ca::launch_adapted_backward(p, dy_dev, lddy, low_dev, rank_used, m_rows > 0 ? dx_dev : nullptr, d_down_dev, d_up_dev, workspace_dev, hip_stream);
 }
 
 int32_t layer_adamw(const ca_adamw_tensor* tensors, int32_t n_tensors, int32_t state_bits, double lr, double beta1, double beta2, double eps,

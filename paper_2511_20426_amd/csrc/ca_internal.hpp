@@ -201,6 +201,23 @@ int32_t launch_layer_norm_backward(const RowNorm& n, const void* dy, int64_t ldd
 int32_t launch_adamw(const ca_adamw_tensor* tensors, int32_t n_tensors, int32_t state_bits, double lr, double beta1, double beta2, double eps,
                      double weight_decay, double grad_scale, void* stream);
 int32_t launch_adamw_values(const void* m, const void* v, const float* m_scale, const float* v_scale, float* m_out, float* v_out, int64_t n, void* stream);
+// Y = X W' + (s_g X A_g') B_g' with g = index of the row (down: A [adapters][rank][K], up: B [adapters][N][rank]; rank 32, 64 or 128), low [M][rank] gets
+// s_g X A_g'.  Backward (w: the weights transposed [K][N], ldy: the row stride of dX): the gradients of X and of the adapters' first rank_used; those
+// that are null are left out.
+struct AdaptedLinear {
+  const void* x;
+  const void* w;
+  const void* down;
+  const void* up;
+  const float* scales;
+  const int32_t* index;
+  int64_t M, ldx, ldw, ldy;
+  int32_t N, K, adapters, rank;
+};
+int32_t launch_gemm_adapted(const AdaptedLinear& p, void* y, void* low, void* stream);
+size_t adapted_backward_bytes(int64_t M, int32_t N, int32_t K, int32_t adapters, int32_t rank);
+int32_t launch_adapted_backward(const AdaptedLinear& p, const void* dy, int64_t lddy, const void* low, int32_t rank_used, void* dx, void* d_down, void* d_up,
+                                void* workspace, void* stream);
 // Per-device facts and one-time kernel attributes, cached for up to kMaxDevices devices (thread
 // safe: the cached values are idempotent and written with relaxed atomics).
 constexpr int kMaxDevices = 64;
@@ -211,7 +228,7 @@ struct KernelLds {
   const void* kernel;
   int bytes;
 };
-enum LdsSlot { kLdsAttn, kLdsAttnRope, kLdsGemm, kLdsGemmRows, kLdsGemmPublish, kLdsI8, kLdsGated, kLdsGatedBackward, kLdsSlots };
+enum LdsSlot { kLdsAttn, kLdsAttnRope, kLdsGemm, kLdsGemmRows, kLdsGemmPublish, kLdsI8, kLdsGated, kLdsGatedBackward, kLdsAdapted, kLdsSlots };
 int32_t ensure_dynamic_lds(const KernelLds* kernels, int n, LdsSlot slot);   // slot: which set of kernels
 int32_t finish_launch(const char* what);   // launchers end with this: CA_OK, or CA_EDEVICE after recording HIP's last error
 int32_t device_failure(const char* what, int hip_error);   // records the text, clears HIP's last error, returns CA_EDEVICE

@@ -1,0 +1,620 @@
+// A projection with low-rank adapters of many requests at once: Y[m] = X[m] W' + (s_g X[m] A_g') B_g', g = index[m], in bf16 with fp32
+// accumulation; rows whose index is no adapter's have the projection alone (gfx950).  And the gradients: dX = dY W + (s_g dY B_g) A_g is the same with
+// the transposed matrices, dA_g = (s_g dY B_g)' X and dB_g = dY' (s_g X A_g') are sums over the rows that have the adapter.
+//
+// Two launches.  The first makes the few values T[m] = s_g X[m] A_g' (the rank: 32, 64 or 128 of them), rounded to bf16 as operands of the second,
+// which multiplies X and W as the plain linear map does and adds T's products with the rows of B to the same sums before they are rounded, so that
+// neither product is written or rounded by itself.  (T's rounding, 2^-9 of each of its values, is 2^-9 / sqrt(3 rank) of the adapter's part of a sum of
+// random signs.)  An adapter's products go to sums of their own and are added for the rows that have it, so that no value of one request's adapter, not
+// even an infinity, touches another's rows.  What adapters a tile's rows have is found in the tile: any order and number works, runs of rows cost least.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <climits>
+
+#include "ca_internal.hpp"
+
+namespace ca {
+namespace {
+
+#include "rope_device.hpp"
+#include "gemm_tiles.hpp"
+#include "gemm_tile_kernel.hpp"
+#include "gemm_ops.hpp"
+
+using Frag = Bf16Products::Frag;
+using Sums = Bf16Products::Sums;
+
+struct AdaptedArgs {
+  const uint16_t* x;
+  const uint16_t* w;
+  uint16_t* y;
+  const uint16_t* t;                              // [M][rank]
+  const uint16_t* up;                             // [adapters][N][rank]
+  const int32_t* index;
+  int64_t ldy;
+  int32_t M, N, K, ldx, ldw, adapters;            // row strides in elements
+  int32_t tiles_m, tiles_n, more;                 // as in LinearArgs
+};
+
+struct LowArgs {
+  const uint16_t* x;
+  const uint16_t* down;                           // [adapters][rank][K]
+  const float* scales;
+  const int32_t* index;
+  uint16_t* t;                                    // [M][rank]
+  int32_t M, K, ldx, adapters, rank;
+};
+
+__device__ __forceinline__ Frag frag_at(const uint16_t* p) { return *reinterpret_cast<const Frag*>(p); }
+
+// the adapter of a row, -1 for none (whatever the index says that is no adapter's number)
+__device__ __forceinline__ int adapter_of(const int32_t* index, int row, int rows, int adapters) {
+  const int g = row < rows ? index[row] : -1;
+  return g >= 0 && g < adapters ? g : -1;
+}
+
+template <int kCtrl>
+__device__ __forceinline__ int dpp_min(int x) {
+  return min(x, __builtin_amdgcn_update_dpp(0, x, kCtrl, 0xf, 0xf, true));
+}
+// The lowest adapter above `after` that sixteen neighbouring lanes' rows have (every sixteen lanes have the same rows); INT_MAX: none
+template <int kRows>
+__device__ __forceinline__ int next_adapter(const int (&mine)[kRows], int after) {
+  int g = INT_MAX;
+#pragma unroll
+  for (int j = 0; j < kRows; ++j) g = mine[j] > after ? min(g, mine[j]) : g;
+  g = dpp_min<0xb1>(g);                          // quad_perm [1, 0, 3, 2]
+  g = dpp_min<0x4e>(g);                          // quad_perm [2, 3, 0, 1]
+  g = dpp_min<0x141>(g);                         // row_half_mirror
+  g = dpp_min<0x140>(g);                         // row_mirror
+  return __builtin_amdgcn_readfirstlane(g);
+}
+
+// ------------------------------------------------------------------------------------------------ T
+
+// A workgroup takes 16 kTm rows and 16 kTn values of each; its waves share K in pieces of 128 bytes of a row, which go straight from memory (X) and L2
+// (A) to the registers that the MFMA multiplies from, kAhead pieces on their way; their sums meet in LDS, in order.  Bound by X's way from memory: 23400 x
+// 5120 of rank 32 in 64 rows to a workgroup; fewer rows have fewer of them to a workgroup, few rows eight waves to share K.
+template <int kTm, int kTn, int kWaves, int kAhead>
+__global__ __launch_bounds__(64 * kWaves) void adapted_low_kernel(LowArgs a) {
+  __shared__ Sums part[kWaves][kTm][64];
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, l15 = lane & 15, grp = lane >> 4;
+  const int m0 = blockIdx.x * 16 * kTm, r0 = blockIdx.y * 16 * kTn;
+  int mine[kTm];
+  const uint16_t* x[kTm];
+#pragma unroll
+  for (int j = 0; j < kTm; ++j) {
+    const int row = m0 + 16 * j + l15;
+    mine[j] = adapter_of(a.index, row, a.M, a.adapters);
+    x[j] = a.x + int64_t(min(row, a.M - 1)) * a.ldx + grp * 8;
+    if (row < a.M && mine[j] < 0 && wave == 0) {                    // none: zeros
+#pragma unroll
+      for (int i = 0; i < kTn; ++i) *reinterpret_cast<uint2*>(a.t + int64_t(row) * a.rank + r0 + 16 * i + 4 * grp) = make_uint2(0, 0);
+    }
+  }
+  // piece i of the wave is number wave + i kWaves of the row's
+  const int pieces = (a.K / 64 - wave + kWaves - 1) / kWaves;
+  for (int g = next_adapter<kTm>(mine, -1); g != INT_MAX; g = next_adapter<kTm>(mine, g)) {
+    const uint16_t* const down = a.down + (int64_t(g) * a.rank + r0 + l15) * a.K + grp * 8;
+    Sums acc[kTn][kTm];
+#pragma unroll
+    for (int i = 0; i < kTn; ++i)
+#pragma unroll
+      for (int j = 0; j < kTm; ++j) acc[i][j] = Sums{0, 0, 0, 0};
+    Frag fa[kAhead][kTn][2], fx[kAhead][kTm][2];
+    auto request = [&](int slot, int i) {
+      const int64_t at = int64_t(wave + i * kWaves) * 64;
+#pragma unroll
+      for (int kk = 0; kk < 2; ++kk) {
+#pragma unroll
+        for (int j = 0; j < kTm; ++j) fx[slot][j][kk] = frag_at(x[j] + at + kk * 32);
+#pragma unroll
+        for (int n = 0; n < kTn; ++n) fa[slot][n][kk] = frag_at(down + int64_t(16 * n) * a.K + at + kk * 32);
+      }
+    };
+#pragma unroll
+    for (int s = 0; s < kAhead; ++s)
+      if (s < pieces) request(s, s);
+    for (int i = 0; i < pieces; i += kAhead) {
+#pragma unroll
+      for (int s = 0; s < kAhead; ++s) {
+        if (i + s >= pieces) break;
+#pragma unroll
+        for (int kk = 0; kk < 2; ++kk)
+#pragma unroll
+          for (int n = 0; n < kTn; ++n)
+#pragma unroll
+            for (int j = 0; j < kTm; ++j) acc[n][j] = Bf16Products::multiply(fa[s][n][kk], fx[s][j][kk], acc[n][j]);
+        if (i + s + kAhead < pieces) request(s, i + s + kAhead);
+      }
+    }
+    const float scale = a.scales[g];
+#pragma unroll
+    for (int n = 0; n < kTn; ++n) {
+#pragma unroll
+      for (int j = 0; j < kTm; ++j) part[wave][j][lane] = acc[n][j];
+      __syncthreads();
+#pragma unroll
+      for (int j = 0; j < kTm; ++j) {
+        if (wave != j % kWaves) continue;
+        Sums sum = part[0][j][lane];
+#pragma unroll
+        for (int v = 1; v < kWaves; ++v) sum += part[v][j][lane];
+        // the lane has values 4 grp .. +3 of sixteen of row l15
+        if (mine[j] == g)
+          *reinterpret_cast<uint2*>(a.t + int64_t(m0 + 16 * j + l15) * a.rank + r0 + 16 * n + 4 * grp) =
+              make_uint2(pack_bf16(sum[0] * scale, sum[1] * scale), pack_bf16(sum[2] * scale, sum[3] * scale));
+      }
+      __syncthreads();
+    }
+  }
+}
+
+// ------------------------------------------------------------------------------------------------ Y
+
+// The adapters' part of a wave's kTn x kTm sub-tiles is added to acc: W's rows (columns of Y) n0 + 16 i + l15, X's rows m0 + 16 j + l15.
+template <int kTn, int kTm, int kSteps>
+__device__ __forceinline__ void add_adapters(Sums (&acc)[kTn][kTm], const AdaptedArgs& a, int m0, int n0, int l15, int grp) {
+  constexpr int kRank = 32 * kSteps;
+  int mine[kTm];
+#pragma unroll
+  for (int j = 0; j < kTm; ++j) mine[j] = adapter_of(a.index, m0 + 16 * j + l15, a.M, a.adapters);
+  int g = next_adapter<kTm>(mine, -1);
+  if (g == INT_MAX) return;
+  Frag ft[kTm][kSteps];
+#pragma unroll
+  for (int j = 0; j < kTm; ++j)
+#pragma unroll
+    for (int kk = 0; kk < kSteps; ++kk) ft[j][kk] = frag_at(a.t + int64_t(min(m0 + 16 * j + l15, a.M - 1)) * kRank + kk * 32 + grp * 8);
+  for (; g != INT_MAX; g = next_adapter<kTm>(mine, g)) {
+#pragma unroll
+    for (int i = 0; i < kTn; ++i) {
+      const uint16_t* const up = a.up + (int64_t(g) * a.N + min(n0 + 16 * i + l15, a.N - 1)) * kRank + grp * 8;
+      Frag fu[kSteps];
+#pragma unroll
+      for (int kk = 0; kk < kSteps; ++kk) fu[kk] = frag_at(up + kk * 32);
+#pragma unroll
+      for (int j = 0; j < kTm; ++j) {
+        Sums sum{0, 0, 0, 0};
+#pragma unroll
+        for (int kk = 0; kk < kSteps; ++kk) sum = Bf16Products::multiply(fu[kk], ft[j][kk], sum);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[i][j][e] = mine[j] == g ? acc[i][j][e] + sum[e] : acc[i][j][e];
+      }
+    }
+  }
+}
+
+template <typename T, int kSteps>
+__global__ __launch_bounds__(T::kThreads) void gemm_adapted_kernel(AdaptedArgs a) {
+  using Products = Bf16Products;
+  constexpr int BM = T::kBm, BN = T::kBn, kWavesM = T::kWavesAlongM, kStages = T::kRing;
+  extern __shared__ __attribute__((aligned(1024))) uint8_t lds[];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int l15 = lane & 15, grp = lane >> 4;
+  const int wm = wave % kWavesM, wn = wave / kWavesM;
+  const int nth = int(blockIdx.x & 7) * a.more + int(blockIdx.x >> 3);          // XCD x takes a contiguous range of the tiles
+  if (nth >= a.tiles_m * a.tiles_n) return;
+  int tm, tn;
+  tile_at(a.tiles_m, a.tiles_n, nth, &tm, &tn);
+  const int m0 = tm * BM, n0 = tn * BN;
+  // load i of a wave brings 8 rows of 128 bytes, chunks swizzled by the row; rows past the end re-read the last one
+  uint32_t offw[T::kLoadsW], offx[T::kLoadsX];
+#pragma unroll
+  for (int i = 0; i < T::kLoadsW; ++i) {
+    const int row = (wave * T::kLoadsW + i) * 8 + (lane >> 3), c = (lane & 7) ^ ((row >> 1) & 7);
+    offw[i] = uint32_t(min(n0 + row, a.N - 1) - n0) * uint32_t(a.ldw) * 2 + c * 16;
+  }
+#pragma unroll
+  for (int i = 0; i < T::kLoadsX; ++i) {
+    const int row = (wave * T::kLoadsX + i) * 8 + (lane >> 3), c = (lane & 7) ^ ((row >> 1) & 7);
+    offx[i] = uint32_t(min(m0 + row, a.M - 1) - m0) * uint32_t(a.ldx) * 2 + c * 16;
+  }
+  uint64_t base_w = reinterpret_cast<uint64_t>(a.w + int64_t(n0) * a.ldw);
+  uint64_t base_x = reinterpret_cast<uint64_t>(a.x + int64_t(m0) * a.ldx);
+  const int n_stages = a.K / 64;
+#include "gemm_tile_loop.hpp"
+
+  add_adapters<T::kTn, T::kTm, kSteps>(acc, a, m0 + wm * T::kTm * 16, n0 + wn * T::kTn * 16, l15, grp);
+#pragma unroll
+  for (int i = 0; i < T::kTn; ++i)
+#pragma unroll
+    for (int j = 0; j < T::kTm; ++j) {
+      uint32_t* to = reinterpret_cast<uint32_t*>(lds + ((wm * T::kTm + j) * 16 + l15) * T::kPitch + ((wn * T::kTn + i) * 16 + 4 * grp) * 2);
+      to[0] = pack_bf16(acc[i][j][0], acc[i][j][1]);
+      to[1] = pack_bf16(acc[i][j][2], acc[i][j][3]);
+    }
+  __syncthreads();
+  constexpr int kChunks = BN / 8, kRows = T::kThreads / kChunks;
+  const int c = tid % kChunks;
+#pragma unroll 4
+  for (int row = tid / kChunks; row < BM; row += kRows) {
+    const u32x4 v = *reinterpret_cast<const u32x4*>(lds + row * T::kPitch + c * 16);
+    if (m0 + row < a.M && n0 + c * 8 < a.N) __builtin_nontemporal_store(v, reinterpret_cast<u32x4*>(a.y + int64_t(m0 + row) * a.ldy + n0 + c * 8));
+  }
+}
+
+// Few rows (single tokens when serving): the weights' way from memory is all there is.  As gemm_few_kernel: a workgroup takes 16 columns, its four waves
+// share K in pieces of 128 bytes of 16 rows of W, kAhead on their way straight to the registers that the MFMA multiplies from, with X's rows from L2; of an
+// adapter each wave takes one step of 32 of its rank.
+template <int kTiles>
+__global__ __launch_bounds__(256) void adapted_few_kernel(AdaptedArgs a, int rank) {
+  constexpr int kWaves = 4, kAhead = 4;
+  __shared__ Sums part[kWaves][kTiles][64];
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, l15 = lane & 15, grp = lane >> 4;
+  const int n0 = blockIdx.x * 16, col = min(n0 + l15, a.N - 1);
+  const uint16_t* const w = a.w + int64_t(col) * a.ldw + grp * 8;
+  const uint16_t* x[kTiles];
+#pragma unroll
+  for (int t = 0; t < kTiles; ++t) x[t] = a.x + int64_t(min(16 * t + l15, a.M - 1)) * a.ldx + grp * 8;
+  Sums acc[kTiles];
+#pragma unroll
+  for (int t = 0; t < kTiles; ++t) acc[t] = Sums{0, 0, 0, 0};
+  const int pieces = (a.K / 64 - wave + kWaves - 1) / kWaves;
+  Frag fw[kAhead][2], fx[kAhead][kTiles][2] = {};
+  auto request = [&](int slot, int i) {
+    const int64_t at = int64_t(wave + i * kWaves) * 64;
+#pragma unroll
+    for (int kk = 0; kk < 2; ++kk) fw[slot][kk] = frag_at(w + at + kk * 32);
+#pragma unroll
+    for (int t = 0; t < kTiles; ++t)
+      if (16 * t + l15 < a.M) {                                     // lanes of rows that do not exist ask for nothing
+#pragma unroll
+        for (int kk = 0; kk < 2; ++kk) fx[slot][t][kk] = frag_at(x[t] + at + kk * 32);
+      }
+  };
+#pragma unroll
+  for (int s = 0; s < kAhead; ++s)
+    if (s < pieces) request(s, s);
+  // the adapters' rows while the first pieces are on their way
+  int mine[kTiles];
+#pragma unroll
+  for (int t = 0; t < kTiles; ++t) mine[t] = adapter_of(a.index, 16 * t + l15, a.M, a.adapters);
+  Frag ft[kTiles] = {};
+  const int at = 32 * wave + grp * 8;
+  if (32 * wave < rank) {
+#pragma unroll
+    for (int t = 0; t < kTiles; ++t) ft[t] = frag_at(a.t + int64_t(min(16 * t + l15, a.M - 1)) * rank + at);
+    for (int g = next_adapter<kTiles>(mine, -1); g != INT_MAX; g = next_adapter<kTiles>(mine, g)) {
+      const Frag fu = frag_at(a.up + (int64_t(g) * a.N + col) * rank + at);
+#pragma unroll
+      for (int t = 0; t < kTiles; ++t) {
+        const Sums sum = Bf16Products::multiply(fu, ft[t], Sums{0, 0, 0, 0});
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[t][e] = mine[t] == g ? acc[t][e] + sum[e] : acc[t][e];
+      }
+    }
+  }
+  for (int i = 0; i < pieces; i += kAhead) {
+#pragma unroll
+    for (int s = 0; s < kAhead; ++s) {
+      if (i + s >= pieces) break;
+#pragma unroll
+      for (int kk = 0; kk < 2; ++kk)
+#pragma unroll
+        for (int t = 0; t < kTiles; ++t) acc[t] = Bf16Products::multiply(fw[s][kk], fx[s][t][kk], acc[t]);
+      if (i + s + kAhead < pieces) request(s, i + s + kAhead);
+    }
+  }
+#pragma unroll
+  for (int t = 0; t < kTiles; ++t) part[wave][t][lane] = acc[t];
+  __syncthreads();
+  const int t = wave;                                               // a wave takes a tile of 16 rows
+  if (t >= kTiles) return;
+  const Sums sum = (part[0][t][lane] + part[1][t][lane]) + (part[2][t][lane] + part[3][t][lane]);
+  const int row = 16 * t + l15, n = n0 + 4 * grp;
+  if (row < a.M && n < a.N)
+    *reinterpret_cast<uint2*>(a.y + int64_t(row) * a.ldy + n) = make_uint2(pack_bf16(sum[0], sum[1]), pack_bf16(sum[2], sum[3]));
+}
+
+// ------------------------------------------------------------------------------------------------ the adapters' gradients
+
+struct SumArgs {
+  const uint16_t* low;                            // [M][rank]
+  const uint16_t* wide;                           // [M][ld]
+  const int32_t* index;
+  float* parts;                                   // [split][adapters][rank][C]
+  int32_t* there;                                 // [split][adapters]: whether the split has rows of the adapter
+  int32_t M, C, ld, adapters, split_rows;
+};
+constexpr int kSumCols = 128, kSumStep = 32, kMostAdapters = 4096;
+
+// parts[g][r][c] = sum over a split's rows that have adapter g of low[m][r] wide[m][c].  A workgroup takes 128 columns, 32 rows at a time through LDS, from
+// where the lanes collect 8 rows of a column each, as the matrix instruction takes them (rows in steps of 4 bytes more than whole lines lie in other
+// banks); the next rows are on their way meanwhile.  Rows of other adapters are zeros on both sides.
+template <int kTn>
+__global__ __launch_bounds__(256) void adapted_sum_kernel(SumArgs a) {
+  constexpr int kRank = 16 * kTn, kPitchW = kSumCols * 2 + 4, kPitchL = kRank * 2 + 4, kLoadsL = (kRank / 8 * kSumStep + 255) / 256;
+  __shared__ __attribute__((aligned(16))) uint8_t wide[kSumStep * kPitchW];
+  __shared__ __attribute__((aligned(16))) uint8_t low[kSumStep * kPitchL];
+  __shared__ uint8_t there[kMostAdapters];
+  __shared__ int lowest[4];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, l15 = lane & 15, grp = lane >> 4;
+  const int c0 = blockIdx.x * kSumCols, split = blockIdx.y;
+  const int begin = split * a.split_rows, end = min(begin + a.split_rows, a.M);
+  for (int g = tid; g < a.adapters; g += 256) there[g] = 0;
+  for (int after = -1;;) {
+    int g = INT_MAX;
+    for (int m = begin + tid; m < end; m += 256) {
+      const int of = adapter_of(a.index, m, a.M, a.adapters);
+      g = of > after ? min(g, of) : g;
+    }
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) g = min(g, __shfl_xor(g, d, 64));
+    __syncthreads();                                                // (the last adapter's have been read)
+    if (lane == 0) lowest[wave] = g;
+    __syncthreads();
+    g = min(min(lowest[0], lowest[1]), min(lowest[2], lowest[3]));
+    if (g == INT_MAX) break;
+    after = g;
+    if (tid == 0) there[g] = 1;
+    Sums acc[2][kTn];
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int n = 0; n < kTn; ++n) acc[i][n] = Sums{0, 0, 0, 0};
+    // rows from m on, of the first 32 that hold any of the adapter's; which of them, in `rows`
+    uint32_t rows = 0;
+    auto find = [&](int m) {
+      for (; m < end; m += kSumStep) {
+        const int of = lane < kSumStep && m + lane < end ? a.index[m + lane] : -1;
+        rows = uint32_t(__ballot(of == g));
+        if (rows) break;
+      }
+      return m;
+    };
+    U4 held_w[2], held_l[kLoadsL];
+    auto request = [&](int m) {
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const int at = tid + 256 * i, row = at / 16, col = c0 + at % 16 * 8;
+        held_w[i] = U4{0, 0, 0, 0};
+        if ((rows >> row & 1) && col < a.C) held_w[i] = *reinterpret_cast<const U4*>(a.wide + int64_t(m + row) * a.ld + col);
+      }
+#pragma unroll
+      for (int i = 0; i < kLoadsL; ++i) {
+        const int at = tid + 256 * i, row = at / (kRank / 8);
+        held_l[i] = U4{0, 0, 0, 0};
+        if (row < kSumStep && (rows >> row & 1)) held_l[i] = *reinterpret_cast<const U4*>(a.low + int64_t(m + row) * kRank + at % (kRank / 8) * 8);
+      }
+    };
+    int m = find(begin);
+    request(m);                                                     // (there is one)
+    while (m < end) {
+      __syncthreads();
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const int at = tid + 256 * i;
+        uint32_t* const to = reinterpret_cast<uint32_t*>(wide + at / 16 * kPitchW + at % 16 * 16);
+        to[0] = held_w[i].x; to[1] = held_w[i].y; to[2] = held_w[i].z; to[3] = held_w[i].w;
+      }
+#pragma unroll
+      for (int i = 0; i < kLoadsL; ++i) {
+        const int at = tid + 256 * i, row = at / (kRank / 8);
+        if (row >= kSumStep) continue;
+        uint32_t* const to = reinterpret_cast<uint32_t*>(low + row * kPitchL + at % (kRank / 8) * 16);
+        to[0] = held_l[i].x; to[1] = held_l[i].y; to[2] = held_l[i].z; to[3] = held_l[i].w;
+      }
+      __syncthreads();
+      m = find(m + kSumStep);
+      if (m < end) request(m);
+      auto column = [&](const uint8_t* from, int pitch) {           // rows 8 grp .. +7 of a column
+        uint32_t v[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = *reinterpret_cast<const uint16_t*>(from + (8 * grp + e) * pitch);
+        const u32x4 two = {v[0] | v[1] << 16, v[2] | v[3] << 16, v[4] | v[5] << 16, v[6] | v[7] << 16};
+        return __builtin_bit_cast(Frag, two);
+      };
+      Frag fw[2];
+#pragma unroll
+      for (int i = 0; i < 2; ++i) fw[i] = column(wide + (wave * 32 + i * 16 + l15) * 2, kPitchW);
+#pragma unroll
+      for (int n = 0; n < kTn; ++n) {
+        const Frag fl = column(low + (n * 16 + l15) * 2, kPitchL);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) acc[i][n] = Bf16Products::multiply(fw[i], fl, acc[i][n]);
+      }
+    }
+    // the lane has columns 4 grp .. +3 of sixteen of row r = l15
+    float* const out = a.parts + (int64_t(split) * a.adapters + g) * kRank * a.C;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int col = c0 + wave * 32 + i * 16 + 4 * grp;
+      if (col >= a.C) continue;
+#pragma unroll
+      for (int n = 0; n < kTn; ++n) *reinterpret_cast<Sums*>(out + int64_t(n * 16 + l15) * a.C + col) = acc[i][n];
+    }
+  }
+  if (blockIdx.x == 0)
+    for (int g = tid; g < a.adapters; g += 256) a.there[split * a.adapters + g] = there[g];
+}
+
+// out [adapters][R][C], or transposed [adapters][C][R], from the splits' parts
+template <bool kTransposed>
+__global__ __launch_bounds__(256) void adapted_join_kernel(const float* parts, const int32_t* there, int splits, int adapters, int rank, int R, int C, uint16_t* out) {
+  const int64_t all = int64_t(adapters) * R * C;
+  for (int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x; i < all; i += int64_t(gridDim.x) * 256) {
+    const int c = int(i % C), r = int(i / C % R), g = int(i / C / R);
+    float sum = 0.f;
+    for (int s = 0; s < splits; ++s)
+      if (there[s * adapters + g]) sum += parts[((int64_t(s) * adapters + g) * rank + r) * C + c];
+    out[kTransposed ? (int64_t(g) * C + c) * R + r : i] = uint16_t(pack_bf16(sum, sum));
+  }
+}
+
+// [rows][cols] of each adapter to [cols][rows]
+__global__ __launch_bounds__(256) void adapted_transpose_kernel(const uint16_t* from, uint16_t* to, int rows, int cols) {
+  __shared__ uint16_t tile[32][33];
+  const int64_t at = int64_t(blockIdx.z) * rows * cols;
+  const int r0 = blockIdx.y * 32, c0 = blockIdx.x * 32, x = threadIdx.x & 31, y = threadIdx.x >> 5;
+  for (int i = y; i < 32; i += 8)
+    if (r0 + i < rows && c0 + x < cols) tile[i][x] = from[at + int64_t(r0 + i) * cols + c0 + x];
+  __syncthreads();
+  for (int i = y; i < 32; i += 8)
+    if (c0 + i < cols && r0 + x < rows) to[at + int64_t(c0 + i) * rows + r0 + x] = tile[x][i];
+}
+
+// ------------------------------------------------------------------------------------------------ launches
+
+constexpr int kFewRows = 32;
+constexpr const char* kWhat = "gemm_adapted.hip";
+
+// the compiled tiles' part of the 8-bit linear map's model: their stages take as long
+constexpr OpModel kModel[] = {{256, 128, 1, 0, 705, 840, 5650}, {128, 128, 1, 0, 455, 470, 3680}, {64, 64, 2, 0, 290, 370, 1990}, {64, 64, 1, 0, 255, 190, 2000}};
+
+template <typename T>
+const void* tile_kernel_address(int steps) {
+  return reinterpret_cast<const void*>(steps == 1 ? gemm_adapted_kernel<T, 1> : steps == 2 ? gemm_adapted_kernel<T, 2> : gemm_adapted_kernel<T, 4>);
+}
+
+// one call of any size readies all kernels for stream capture
+int32_t adapted_ready() {
+  KernelLds kernels[12];
+  for (int i = 0; i < 3; ++i) {
+    const int steps = 1 << i;
+    kernels[4 * i] = {tile_kernel_address<Tile256x128>(steps), Tile256x128::kLds};
+    kernels[4 * i + 1] = {tile_kernel_address<Tile128>(steps), Tile128::kLds};
+    kernels[4 * i + 2] = {tile_kernel_address<Tile64>(steps), Tile64::kLds};
+    kernels[4 * i + 3] = {tile_kernel_address<Tile64Wide>(steps), Tile64Wide::kLds};
+  }
+  return ensure_dynamic_lds(kernels, 12, kLdsAdapted);
+}
+
+template <typename T>
+int32_t enqueue_adapted(AdaptedArgs& a, int rank, void* stream) {
+  a.tiles_m = (a.M + T::kBm - 1) / T::kBm;
+  a.tiles_n = (a.N + T::kBn - 1) / T::kBn;
+  const int64_t tiles = int64_t(a.tiles_m) * a.tiles_n;
+  if ((tiles + 7) * T::kThreads >= (int64_t(1) << 32)) return CA_EUNSUPPORTED;
+  a.more = int32_t((tiles + 7) / 8);
+  const auto kernel = rank == 32 ? gemm_adapted_kernel<T, 1> : rank == 64 ? gemm_adapted_kernel<T, 2> : gemm_adapted_kernel<T, 4>;
+  hipLaunchKernelGGL(kernel, dim3(unsigned(a.more) * 8), dim3(T::kThreads), T::kLds, static_cast<hipStream_t>(stream), a);
+  return finish_launch(kWhat);
+}
+
+template <int kTm, int kTn, int kWaves, int kAhead>
+int32_t enqueue_low(const LowArgs& a, void* stream) {
+  hipLaunchKernelGGL((adapted_low_kernel<kTm, kTn, kWaves, kAhead>), dim3(unsigned((a.M + 16 * kTm - 1) / (16 * kTm)), unsigned(a.rank / (16 * kTn))),
+                     dim3(64 * kWaves), 0, static_cast<hipStream_t>(stream), a);
+  return finish_launch(kWhat);
+}
+
+// T = s (X A'): few rows: 16 values to a workgroup, eight waves; up to 8192 rows 16 to a workgroup, above 64
+int32_t launch_low(const LowArgs& a, void* stream) {
+  if (a.M <= kFewRows) return enqueue_low<1, 1, 8, 4>(a, stream);
+  const bool many = a.M > 8192;
+  if (a.rank == 32) return many ? enqueue_low<4, 2, 4, 2>(a, stream) : enqueue_low<1, 2, 4, 4>(a, stream);
+  if (a.rank == 64) return many ? enqueue_low<4, 4, 4, 2>(a, stream) : enqueue_low<1, 4, 4, 2>(a, stream);
+  return many ? enqueue_low<4, 8, 4, 1>(a, stream) : enqueue_low<1, 8, 4, 2>(a, stream);
+}
+
+int32_t launch_adapted_gemm(AdaptedArgs& a, int rank, void* stream) {
+  if (const int32_t rc = adapted_ready(); rc != CA_OK) return rc;
+  if (a.M <= kFewRows) {
+    const int64_t groups = (int64_t(a.N) + 15) / 16;
+    if (groups * 256 >= (int64_t(1) << 32)) return CA_EUNSUPPORTED;
+    hipLaunchKernelGGL(a.M <= 16 ? adapted_few_kernel<1> : adapted_few_kernel<2>, dim3(unsigned(groups)), dim3(256), 0, static_cast<hipStream_t>(stream), a, rank);
+    return finish_launch(kWhat);
+  }
+  int n_cu = 0;
+  if (const int32_t rc = device_cu_count(&n_cu); rc != CA_OK) return rc;
+  switch (pick_op(kModel, a.M, a.N, a.K / 64, n_cu)) {
+    case 0: return enqueue_adapted<Tile256x128>(a, rank, stream);
+    case 1: return enqueue_adapted<Tile128>(a, rank, stream);
+    case 2: return enqueue_adapted<Tile64>(a, rank, stream);
+    default: return enqueue_adapted<Tile64Wide>(a, rank, stream);
+  }
+}
+
+// Splits of the rows of a sum over C columns: enough workgroups to fill the chip, 64 rows or more to each, no more room than 256 MB
+int sum_splits(int64_t M, int32_t C, int32_t adapters, int32_t rank) {
+  const int64_t tiles = (int64_t(C) + kSumCols - 1) / kSumCols, one = int64_t(adapters) * rank * C * 4;
+  return int(std::max<int64_t>(1, std::min({(1024 + tiles - 1) / tiles, (M + 63) / 64, (int64_t(256) << 20) / one})));
+}
+
+size_t up16(size_t n) { return (n + 15) / 16 * 16; }
+
+struct AdaptedRoom {                              // of the backward pass, in bytes
+  size_t low, down_t, up_t, there, parts, bytes;
+};
+AdaptedRoom adapted_room(int64_t M, int32_t N, int32_t K, int32_t adapters, int32_t rank) {
+  AdaptedRoom r{};
+  r.down_t = up16(size_t(M) * rank * 2);
+  r.up_t = r.down_t + up16(size_t(adapters) * rank * K * 2);
+  r.there = r.up_t + up16(size_t(adapters) * rank * N * 2);
+  const int sk = sum_splits(M, K, adapters, rank), sn = sum_splits(M, N, adapters, rank);
+  r.parts = r.there + up16(size_t(adapters) * std::max(sk, sn) * 4);
+  r.bytes = r.parts + std::max(size_t(sk) * K, size_t(sn) * N) * adapters * rank * 4;
+  return r;
+}
+
+// out = sum over the rows of each adapter of low' wide
+int32_t launch_adapter_sum(const uint16_t* low, const void* wide, int64_t ld, const int32_t* index, int32_t M, int32_t C, int32_t adapters, int32_t rank,
+                           int32_t rank_used, bool transposed, void* out, int32_t* there, float* parts, void* stream) {
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  int splits = 0;
+  if (M > 0) {
+    const int most = sum_splits(M, C, adapters, rank);
+    SumArgs a{low, static_cast<const uint16_t*>(wide), index, parts, there, M, C, int32_t(ld), adapters, 0};
+    a.split_rows = int32_t((int64_t(M) + most - 1) / most);
+    splits = (M + a.split_rows - 1) / a.split_rows;
+    const auto kernel = rank == 32 ? adapted_sum_kernel<2> : rank == 64 ? adapted_sum_kernel<4> : adapted_sum_kernel<8>;
+    hipLaunchKernelGGL(kernel, dim3(unsigned((C + kSumCols - 1) / kSumCols), unsigned(splits)), dim3(256), 0, s, a);
+    if (const int32_t rc = finish_launch(kWhat); rc != CA_OK) return rc;
+  }
+  const int64_t all = int64_t(adapters) * rank_used * C;
+  hipLaunchKernelGGL(transposed ? adapted_join_kernel<true> : adapted_join_kernel<false>, dim3(unsigned(std::min<int64_t>((all + 255) / 256, 16384))), dim3(256), 0, s,
+                     parts, there, splits, adapters, rank, rank_used, C, static_cast<uint16_t*>(out));
+  return finish_launch(kWhat);
+}
+
+int32_t launch_transpose(const void* from, void* to, int rows, int cols, int adapters, void* stream) {
+  hipLaunchKernelGGL(adapted_transpose_kernel, dim3(unsigned((cols + 31) / 32), unsigned((rows + 31) / 32), unsigned(adapters)), dim3(256), 0,
+                     static_cast<hipStream_t>(stream), static_cast<const uint16_t*>(from), static_cast<uint16_t*>(to), rows, cols);
+  return finish_launch(kWhat);
+}
+
+}  // namespace
+
+int32_t launch_gemm_adapted(const AdaptedLinear& p, void* y, void* low, void* stream) {
+  if (p.M == 0) return CA_OK;
+  LowArgs l{static_cast<const uint16_t*>(p.x), static_cast<const uint16_t*>(p.down), p.scales, p.index, static_cast<uint16_t*>(low), int32_t(p.M), p.K,
+            int32_t(p.ldx), p.adapters, p.rank};
+  if (const int32_t rc = launch_low(l, stream); rc != CA_OK) return rc;
+  AdaptedArgs a{static_cast<const uint16_t*>(p.x), static_cast<const uint16_t*>(p.w), static_cast<uint16_t*>(y), static_cast<const uint16_t*>(low),
+                static_cast<const uint16_t*>(p.up), p.index, p.ldy, int32_t(p.M), p.N, p.K, int32_t(p.ldx), int32_t(p.ldw), p.adapters, 0, 0, 0};
+  return launch_adapted_gemm(a, p.rank, stream);
+}
+
+size_t adapted_backward_bytes(int64_t M, int32_t N, int32_t K, int32_t adapters, int32_t rank) { return adapted_room(M, N, K, adapters, rank).bytes; }
+
+int32_t launch_adapted_backward(const AdaptedLinear& p, const void* dy, int64_t lddy, const void* low, int32_t rank_used, void* dx, void* d_down, void* d_up,
+                                void* workspace, void* stream) {
+  const AdaptedRoom r = adapted_room(p.M, p.N, p.K, p.adapters, p.rank);
+  uint8_t* const room = static_cast<uint8_t*>(workspace);
+  uint16_t* const low_dy = reinterpret_cast<uint16_t*>(room);
+  int32_t* const there = reinterpret_cast<int32_t*>(room + r.there);
+  float* const parts = reinterpret_cast<float*>(room + r.parts);
+  const int32_t M = int32_t(p.M);
+  if (M > 0 && (dx || d_down)) {                   // s dY B
+    if (const int32_t rc = launch_transpose(p.up, room + r.up_t, p.N, p.rank, p.adapters, stream); rc != CA_OK) return rc;
+    const LowArgs l{static_cast<const uint16_t*>(dy), reinterpret_cast<const uint16_t*>(room + r.up_t), p.scales, p.index, low_dy, M, p.N, int32_t(lddy), p.adapters,
+                    p.rank};
+    if (const int32_t rc = launch_low(l, stream); rc != CA_OK) return rc;
+  }
+  if (M > 0 && dx) {
+    if (const int32_t rc = launch_transpose(p.down, room + r.down_t, p.rank, p.K, p.adapters, stream); rc != CA_OK) return rc;
+    AdaptedArgs a{static_cast<const uint16_t*>(dy), static_cast<const uint16_t*>(p.w), static_cast<uint16_t*>(dx), low_dy,
+                  reinterpret_cast<const uint16_t*>(room + r.down_t), p.index, p.ldy, M, p.K, p.N, int32_t(lddy), int32_t(p.ldw), p.adapters, 0, 0, 0};
+    if (const int32_t rc = launch_adapted_gemm(a, p.rank, stream); rc != CA_OK) return rc;
+  }
+  if (d_down)
+    if (const int32_t rc = launch_adapter_sum(low_dy, p.x, p.ldx, p.index, M, p.K, p.adapters, p.rank, rank_used, false, d_down, there, parts, stream); rc != CA_OK)
+      return rc;
+  if (d_up)
+    return launch_adapter_sum(static_cast<const uint16_t*>(low), dy, lddy, p.index, M, p.N, p.adapters, p.rank, rank_used, true, d_up, there, parts, stream);
+  return CA_OK;
+}
+
+}  // namespace ca

@@ -507,6 +507,77 @@ def layer_norm_backward(dy: torch.Tensor, x: torch.Tensor, weight: torch.Tensor 
     return g, dw, db
 
 
+class Adapters:
+    """Low-rank adapters of a projection of k values to n as linear_adapted takes them, of many requests side by side: down [G, rank, k] and up [G, n, rank] in
+    bf16, rank filled up with zeros to 32, 64 or 128, and a scale each [G] in fp32.  Adapter g adds scales[g] * (x @ down[g].T) @ up[g].T."""
+
+    def __init__(self, down: torch.Tensor, up: torch.Tensor, scales: torch.Tensor, rank: int):
+        g, room, _ = down.shape
+        assert room in (32, 64, 128) and up.dim() == 3 and up.shape[0] == g and up.shape[2] == room and 1 <= rank <= room and g >= 1
+        assert down.dtype == up.dtype == _BF16 and down.is_contiguous() and up.is_contiguous() and down.device == up.device == scales.device
+        assert scales.shape == (g,) and scales.dtype == torch.float32 and scales.is_contiguous()
+        self.down, self.up, self.scales, self.rank = down, up, scales, rank
+
+    @classmethod
+    def from_weights(cls, down: torch.Tensor, up: torch.Tensor, scales: torch.Tensor | None = None) -> "Adapters":
+        """From down [G, r, k] and up [G, n, r], r up to 128; scales: None for ones.  bf16 weights of a rank of 32, 64 or 128 are taken as they are, so
+        that training may go on in them."""
+        g, r, k = down.shape
+        assert up.dim() == 3 and up.shape[0] == g and up.shape[2] == r and 1 <= r <= 128
+        room = 32 if r <= 32 else 64 if r <= 64 else 128
+        scales = torch.ones(g, dtype=torch.float32, device=down.device) if scales is None else scales.to(torch.float32).contiguous()
+        if r != room:
+            whole = torch.zeros((g, room, k), dtype=_BF16, device=down.device), torch.zeros((g, up.shape[1], room), dtype=_BF16, device=down.device)
+            whole[0][:, :r], whole[1][:, :, :r] = down, up
+            down, up = whole
+        return cls(down.to(_BF16).contiguous(), up.to(_BF16).contiguous(), scales, r)
+
+
+def linear_adapted_train(x: torch.Tensor, w: torch.Tensor, adapters: Adapters, index: torch.Tensor, out: torch.Tensor | None = None):
+    """linear_adapted for training: (y, saved), saved being what linear_adapted_backward takes (scales[g] * x @ down[g].T in bf16)."""
+    assert x.is_cuda and x.dim() == 2 and w.dim() == 2
+    (m, k), n, device = x.shape, w.shape[0], x.device
+    g, rank, _ = adapters.down.shape
+    assert adapters.down.device == device and adapters.down.shape[2] == k and adapters.up.shape[1] == n
+    assert index.dtype == torch.int32 and index.shape == (m,) and index.is_contiguous() and _reachable(index, x)
+    ldx, ldw = _matrix(x, x, _BF16, m, k), _matrix(w, x, _BF16, n, k)
+    low = torch.empty((m, rank), dtype=_BF16, device=device)
+    y = torch.empty((m, n), dtype=_BF16, device=device) if out is None else out
+    ldy = _matrix(y, x, _BF16, m, n)
+    with _on_device(device):
+        B.layer_linear_adapted_bf16(x.data_ptr(), w.data_ptr(), adapters.down.data_ptr(), adapters.up.data_ptr(), adapters.scales.data_ptr(), index.data_ptr(),
+                                    low.data_ptr(), y.data_ptr(), m, n, k, g, rank, ldx, ldw, ldy, _current_stream(device))
+    return y, low
+
+
+def linear_adapted(x: torch.Tensor, w: torch.Tensor, adapters: Adapters, index: torch.Tensor, out: torch.Tensor | None = None) -> torch.Tensor:
+    """y = x @ w.T as linear has it, and beside it the adapter of each row: + scales[g] * (x @ down[g].T) @ up[g].T, g = index[row], a number of an adapter or
+    any other (-1) for none; index [M] in int32 on the device.  x [M, K], w [N, K], y [M, N], bf16, rows may be strided (last dimension contiguous)."""
+    return linear_adapted_train(x, w, adapters, index, out)[0]
+
+
+def linear_adapted_backward(dy: torch.Tensor, x: torch.Tensor, w_t: torch.Tensor | None, adapters: Adapters, index: torch.Tensor, saved: torch.Tensor):
+    """(dx, d_down, d_up) from the gradient dy [M, N] of linear_adapted_train's y, its arguments and what it saved; the weights are frozen, and w_t [K, N] is they
+    transposed, laid out once (None: dx is not asked for).  d_down [G, r, K] and d_up [G, N, r] in bf16, r the adapters' own rank."""
+    assert x.is_cuda and x.dim() == 2 and dy.dim() == 2
+    (m, k), n, device = x.shape, dy.shape[1], x.device
+    g, rank, _ = adapters.down.shape
+    assert adapters.down.device == device and adapters.down.shape[2] == k and adapters.up.shape[1] == n
+    assert index.dtype == torch.int32 and index.shape == (m,) and index.is_contiguous() and _reachable(index, x)
+    assert saved.dtype == _BF16 and saved.shape == (m, rank) and saved.is_contiguous() and _reachable(saved, x)
+    lddy, ldx = _matrix(dy, x, _BF16, m, n), _matrix(x, x, _BF16, m, k)
+    ldw = n if w_t is None else _matrix(w_t, x, _BF16, k, n)
+    dx = None if w_t is None else torch.empty((m, k), dtype=_BF16, device=device)
+    d_down, d_up = torch.empty((g, adapters.rank, k), dtype=_BF16, device=device), torch.empty((g, n, adapters.rank), dtype=_BF16, device=device)
+    nbytes = B.layer_linear_adapted_backward_workspace(m, n, k, g, rank)
+    work = torch.empty(nbytes, dtype=torch.uint8, device=device)
+    with _on_device(device):
+        B.layer_linear_adapted_backward_bf16(dy.data_ptr(), x.data_ptr(), _address(w_t), adapters.down.data_ptr(), adapters.up.data_ptr(),
+                                             adapters.scales.data_ptr(), index.data_ptr(), saved.data_ptr(), _address(dx), d_down.data_ptr(), d_up.data_ptr(),
+                                             m, n, k, g, rank, adapters.rank, lddy, ldx, ldw, k, work.data_ptr(), nbytes, _current_stream(device))
+    return dx, d_down, d_up
+
+
 def attention_layer(pool: CascadePool, x: torch.Tensor, w_qkv: torch.Tensor, w_out: torch.Tensor,
                     inflight: Sequence[int], timesteps: Sequence[int], epoch: int, mode: int,
                     rotate_q_in_kernel: bool = True, publish_in_projection: bool = False) -> torch.Tensor:
