@@ -400,7 +400,7 @@ int32_t layer_linear_adapted_backward_bf16(const void* dy_dev, const void* x_dev
  *   step          four numbers on the device, aligned to 16 bytes: steps done (0 at first; the call adds one, so that a recorded call counts on in every
  *                 replay), and room that the call uses
  * Tensors, copies, states and steps overlap nothing else of the call.  lr, weight_decay and the like are taken when the call is made: a recorded one keeps
- * them.  0 <= beta < 1, eps > 0 (CA_EINVAL); n <= CA_ADAMW_MAX_VALUES.  Two launches for every 40 tensors. */
+ * them.  0 <= beta < 1, eps >= 2^-126 (CA_EINVAL); n <= CA_ADAMW_MAX_VALUES.  Two launches for every 40 tensors. */
 #define CA_ADAMW_MAX_VALUES ((int64_t)1 << 40)
 typedef struct {
   void* param;

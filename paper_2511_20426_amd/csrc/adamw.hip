@@ -47,12 +47,15 @@ struct AdamArgs {
 };
 static_assert(sizeof(AdamArgs) <= 4096, "a launch's arguments");
 
-// Eight values of any alignment that their type allows
+typedef __attribute__((ext_vector_type(8))) float F8;
+
+// Eight values of any alignment that their type allows; zeros from `left` on
 struct __attribute__((packed, aligned(4))) Packed4 { uint32_t w[4]; };
 struct __attribute__((packed, aligned(2))) Packed2 { uint32_t w[4]; };
 
-__device__ __forceinline__ void load8(const void* from, int64_t at, int left, bool half, float (&to)[8]) {
-  if (half) {
+template <bool kHalf>
+__device__ __forceinline__ void load8(const void* from, int64_t at, int left, F8& to) {
+  if constexpr (kHalf) {
     const uint16_t* const p = static_cast<const uint16_t*>(from) + at;
     if (left >= 8) {
       const Packed2 a = *reinterpret_cast<const Packed2*>(p);
@@ -75,7 +78,7 @@ __device__ __forceinline__ void load8(const void* from, int64_t at, int left, bo
   }
 }
 
-__device__ __forceinline__ void store8_half(uint16_t* p, int left, const float (&v)[8]) {
+__device__ __forceinline__ void store8_half(uint16_t* p, int left, const F8& v) {
   if (left >= 8) {
     *reinterpret_cast<Packed2*>(p) = Packed2{{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7])}};
   } else {
@@ -84,7 +87,7 @@ __device__ __forceinline__ void store8_half(uint16_t* p, int left, const float (
       if (j < left) p[j] = uint16_t(pack_bf16(v[j], v[j]));
   }
 }
-__device__ __forceinline__ void store8(float* p, int left, const float (&v)[8]) {
+__device__ __forceinline__ void store8(float* p, int left, const F8& v) {
   if (left >= 8) {
     *reinterpret_cast<Packed4*>(p) = Packed4{{__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])}};
     *reinterpret_cast<Packed4*>(p + 4) = Packed4{{__float_as_uint(v[4]), __float_as_uint(v[5]), __float_as_uint(v[6]), __float_as_uint(v[7])}};
@@ -108,23 +111,61 @@ __device__ __forceinline__ uint32_t block_max(uint32_t x) {
   return max(x, uint32_t(__shfl_xor(int(x), 16, 64)));
 }
 
-__device__ __forceinline__ double m_of(int c, double a) { return a * (double(c * abs(c)) * (1. / (127. * 127.))); }
-__device__ __forceinline__ double v_of(int c, double a) {
+// What codes stand for beside a scale, without what belongs to all codes: m = m_size / 127^2 a, v = v_size / 255^4 a
+constexpr double kPerM = 1. / (127. * 127.), kPerV = 1. / (255. * 255. * 255. * 255.);
+__device__ __forceinline__ double m_size(int c) { return double(c * abs(c)); }
+__device__ __forceinline__ double v_size(int c) {
   const double square = double(c * c);
-  return a * (square * square * (1. / (255. * 255. * 255. * 255.)));
+  return square * square;
 }
 
-// The code of a magnitude x beside the scale a > 0: round(127 sqrt(x / a)); x / a is in `part`
-__device__ __forceinline__ int m_code(double x, double a, float part) {
-  const int c = min(int(127.f * __builtin_amdgcn_sqrtf(part)), 127);                 // one too few at most, next to a whole number
-  const double b = double((2 * c + 1) * (2 * c + 1));
-  return min(c + int(x * (4. * 127. * 127.) >= a * b), 127);
+// Codes of eight magnitudes x (xf: in fp32) beside the scale a: round(kMost (|x| / a)^(1/2)), of the second moment the (1/4).  An estimate in fp32 is off
+// by less than 1e-4 (kMost times five roundings); where one of the eight lies as near to a border between two codes as that (a wave in five), or the
+// scale is no ordinary number, the border is compared with in 64 bits.
+template <bool kSecond>
+__device__ __forceinline__ void codes8(const double (&x)[8], const F8& xf, float a, int (&code)[8]) {
+  constexpr float kMost = kSecond ? 255.f : 127.f;
+  const float part = __builtin_amdgcn_rcpf(a);
+  bool near = !(a >= 0x1p-100f && a <= 0x1p100f);
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    float t = __builtin_amdgcn_sqrtf(fabsf(xf[j]) * part);
+    if (kSecond) t = __builtin_amdgcn_sqrtf(t);
+    t *= kMost;
+    const float whole = rintf(t);
+    near |= fabsf(t - whole) > 0.4999f;
+    code[j] = int(whole);
+    if (kSecond) code[j] = max(code[j], min(__double2hiint(x[j]), 1));                // (a double above zero has bits in its upper half, from 2^-1042 on)
+  }
+  if (__any(near)) {
+    const double scale = double(a), per = 1. / scale;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      float t = __builtin_amdgcn_sqrtf(float(fabs(x[j]) * per));
+      if (kSecond) t = __builtin_amdgcn_sqrtf(t);
+      int c = min(int(t * kMost), int(kMost));                     // the code or one below
+      double b = double((2 * c + 1) * (2 * c + 1)), of = fabs(x[j]) * (4. * kMost * kMost);
+      if (kSecond) b *= b, of *= 4. * kMost * kMost;
+      c = min(c + int(of >= scale * b), int(kMost));
+      if (kSecond) c = x[j] > 0. ? max(c, 1) : 0;
+      // of a block of zeros all are zeros; one that holds an infinity or NaN is not a number: its largest code times such a scale
+      code[j] = a == 0.f ? 0 : a <= 0x1.fffffep127f ? c : int(kMost);
+    }
+  }
 }
-// round(255 (x / a)^(1/4)), at least 1 for x > 0
-__device__ __forceinline__ int v_code(double x, double a, float part) {
-  const int c = min(int(255.f * __builtin_amdgcn_sqrtf(__builtin_amdgcn_sqrtf(part))), 255);
-  const double b = double((2 * c + 1) * (2 * c + 1));
-  return x > 0. ? max(1, min(c + int(x * (510. * 510. * 510. * 510.) >= a * (b * b)), 255)) : 0;
+
+// The root of a number of fp32 to a rounding or so; those below the normal ones, which the instruction takes for zeros, only where they matter: beside an
+// eps of 2^-30 and more a root of 2^-63 does not
+template <bool kSmall>
+__device__ __forceinline__ float root(float x) {
+  const bool small = kSmall && x < 0x1p-96f;
+  return __builtin_amdgcn_sqrtf(small ? x * 0x1p64f : x) * (small ? 0x1p-32f : 1.f);
+}
+
+template <bool kSmall>
+__device__ __forceinline__ void move8(F8& p, const F8& m, const F8& v, float keep, float rate, float by, float eps) {
+#pragma unroll
+  for (int j = 0; j < 8; ++j) p[j] = fmaf(keep, p[j], -rate * (m[j] * __builtin_amdgcn_rcpf(fmaf(root<kSmall>(v[j]), by, eps))));
 }
 
 __device__ __forceinline__ double power(double x, int n) {
@@ -145,25 +186,20 @@ __global__ __launch_bounds__(64) void adamw_count_kernel(AdamArgs a) {
   step[2] = __float_as_int(float(1. / sqrt(1. - power(a.beta2, now))));
 }
 
-template <int kBits>
-__global__ __launch_bounds__(64 * kWaves) void adamw_kernel(AdamArgs a) {
-  int i = 0;
-  while (i + 1 < a.tensors && int(blockIdx.x) >= a.of[i + 1].first) ++i;
-  const AdamTensor t = a.of[i];
-  const int64_t units = (t.n + kUnit - 1) / kUnit, begin = int64_t(int(blockIdx.x) - t.first) * a.units;
-  const int64_t end = begin + a.units < units ? begin + a.units : units;
+// units begin + wave, + kWaves .. below end
+template <int kBits, bool kHalfP, bool kHalfG>
+__device__ __forceinline__ void step_units(const AdamArgs& a, const AdamTensor t, int64_t begin, int64_t end) {
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
   const float rate = __int_as_float(t.step[1]), by = __int_as_float(t.step[2]);
-  const bool half_p = t.types & 1, half_g = t.types & 2;
   for (int64_t u = begin + wave; u < end; u += kWaves) {
     const int64_t at = u * kUnit + lane * 8;
     const int left = int(t.n - at < 8 ? t.n - at : 8);                              // (zero and less behind the end)
-    float p[8], g[8], m[8], v[8];
-    load8(t.g, at, left, half_g, g);
+    F8 p, g, m, v;
+    load8<kHalfG>(t.g, at, left, g);
     if constexpr (kBits == 32) {
-      load8(t.m, at, left, false, m);
-      load8(t.v, at, left, false, v);
-      load8(t.p, at, left, half_p, p);
+      load8<false>(t.m, at, left, m);
+      load8<false>(t.v, at, left, v);
+      load8<kHalfP>(t.p, at, left, p);
       const float scale = float(a.grad_scale), b1 = float(a.beta1), b2 = float(a.beta2), c1 = float(1. - a.beta1), c2 = float(1. - a.beta2);
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
@@ -179,17 +215,18 @@ __global__ __launch_bounds__(64 * kWaves) void adamw_kernel(AdamArgs a) {
       const bool there = block * 256 < t.n;
       const uint2 cm = there ? *reinterpret_cast<const uint2*>(static_cast<const uint8_t*>(t.m) + at) : make_uint2(0, 0);
       const uint2 cv = there ? *reinterpret_cast<const uint2*>(static_cast<const uint8_t*>(t.v) + at) : make_uint2(0, 0);
-      const double am = there ? double(t.m_scale[block]) : 0., av = there ? double(t.v_scale[block]) : 0.;
-      load8(t.p, at, left, half_p, p);
-      double dm[8], dv[8];
+      const float am = there ? t.m_scale[block] : 0.f, av = there ? t.v_scale[block] : 0.f;
+      load8<kHalfP>(t.p, at, left, p);
       uint32_t most_m = 0, most_v = 0;
+      const double keep_m = a.beta1 * kPerM * double(am), keep_v = a.beta2 * kPerV * double(av);
+      const double add_m = (1. - a.beta1) * a.grad_scale, add_v = (1. - a.beta2) * a.grad_scale * a.grad_scale;
+      double dm[8], dv[8];
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
         const int old_m = int(int8_t((j < 4 ? cm.x : cm.y) >> (8 * (j % 4)))), old_v = int((j < 4 ? cv.x : cv.y) >> (8 * (j % 4)) & 255);
-        const double scaled = double(g[j]) * a.grad_scale;
-        dm[j] = fma(a.beta1, m_of(old_m, am), (1. - a.beta1) * scaled);
-        dv[j] = fma(a.beta2, v_of(old_v, av), (1. - a.beta2) * (scaled * scaled));
-        if (j >= left) dm[j] = dv[j] = 0.;
+        const double grad = double(g[j]);                           // (behind the end gradients and codes are zeros)
+        dm[j] = fma(keep_m, m_size(old_m), add_m * grad);
+        dv[j] = fma(keep_v, v_size(old_v), add_v * (grad * grad));
         m[j] = float(dm[j]);
         v[j] = float(dv[j]);
         most_m = max(most_m, __float_as_uint(m[j]) & 0x7fffffffu);                   // (a NaN is more than any number so)
@@ -197,19 +234,14 @@ __global__ __launch_bounds__(64 * kWaves) void adamw_kernel(AdamArgs a) {
       }
       most_m = block_max(most_m);
       most_v = block_max(most_v);
-      const double new_m = double(__uint_as_float(most_m)), new_v = double(__uint_as_float(most_v));
-      const double per_m = 1. / new_m, per_v = 1. / new_v;
+      int new_m[8], new_v[8];
+      codes8<false>(dm, m, __uint_as_float(most_m), new_m);
+      codes8<true>(dv, v, __uint_as_float(most_v), new_v);
       uint32_t codes_m[2] = {0, 0}, codes_v[2] = {0, 0};
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        const double size = fabs(dm[j]);
-        int c = m_code(size, new_m, float(size * per_m)), d = v_code(dv[j], new_v, float(dv[j] * per_v));
-        // of a block of zeros all are zeros; one that holds an infinity or NaN is not a number: its largest code times such a scale
-        c = most_m == 0 ? 0 : most_m >= 0x7f800000u ? 127 : c;
-        d = most_v == 0 ? 0 : most_v >= 0x7f800000u ? 255 : d;
-        c = dm[j] < 0. ? -c : c;
-        codes_m[j / 4] |= uint32_t(c & 255) << (8 * (j % 4));
-        codes_v[j / 4] |= uint32_t(d) << (8 * (j % 4));
+        codes_m[j / 4] |= uint32_t((__double2hiint(dm[j]) < 0 ? -new_m[j] : new_m[j]) & 255) << (8 * (j % 4));
+        codes_v[j / 4] |= uint32_t(new_v[j]) << (8 * (j % 4));
       }
       if (there) {
         *reinterpret_cast<uint2*>(static_cast<uint8_t*>(t.m) + at) = make_uint2(codes_m[0], codes_m[1]);
@@ -220,34 +252,48 @@ __global__ __launch_bounds__(64 * kWaves) void adamw_kernel(AdamArgs a) {
         }
       }
     }
-#pragma unroll
-    for (int j = 0; j < 8; ++j) p[j] = fmaf(a.keep, p[j], -rate * (m[j] / fmaf(sqrtf(v[j]), by, a.eps)));
-    if (half_p) store8_half(static_cast<uint16_t*>(t.p) + at, left, p); else store8(static_cast<float*>(t.p) + at, left, p);
+    if (a.eps >= 0x1p-30f) move8<false>(p, m, v, a.keep, rate, by, a.eps); else move8<true>(p, m, v, a.keep, rate, by, a.eps);
+    if constexpr (kHalfP) store8_half(static_cast<uint16_t*>(t.p) + at, left, p); else store8(static_cast<float*>(t.p) + at, left, p);
     if (t.copy) store8_half(t.copy + at, left, p);
   }
 }
 
-// What states in 8 bits stand for
-__global__ __launch_bounds__(256) void adamw_values_kernel(const int8_t* m, const uint8_t* v, const float* m_scale, const float* v_scale, float* m_out,
-                                                           float* v_out, int64_t n) {
-  for (int64_t at = (int64_t(blockIdx.x) * 256 + threadIdx.x) * 8; at < n; at += int64_t(gridDim.x) * 2048) {
-    const uint2 cm = *reinterpret_cast<const uint2*>(m + at), cv = *reinterpret_cast<const uint2*>(v + at);
-    const double am = double(m_scale[at >> 8]), av = double(v_scale[at >> 8]);
-    uint32_t to[2][8];
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      to[0][j] = __float_as_uint(float(m_of(int(int8_t((j < 4 ? cm.x : cm.y) >> (8 * (j % 4)))), am)));
-      to[1][j] = __float_as_uint(float(v_of(int((j < 4 ? cv.x : cv.y) >> (8 * (j % 4)) & 255), av)));
-    }
-    store_once(m_out + at, U4{to[0][0], to[0][1], to[0][2], to[0][3]});
-    store_once(m_out + at + 4, U4{to[0][4], to[0][5], to[0][6], to[0][7]});
-    store_once(v_out + at, U4{to[1][0], to[1][1], to[1][2], to[1][3]});
-    store_once(v_out + at + 4, U4{to[1][4], to[1][5], to[1][6], to[1][7]});
+template <int kBits>
+__global__ __launch_bounds__(64 * kWaves) void adamw_kernel(AdamArgs a) {
+  int i = 0;
+  while (i + 1 < a.tensors && int(blockIdx.x) >= a.of[i + 1].first) ++i;
+  const AdamTensor t = a.of[i];
+  const int64_t units = (t.n + kUnit - 1) / kUnit, begin = int64_t(int(blockIdx.x) - t.first) * a.units;
+  const int64_t end = begin + a.units < units ? begin + a.units : units;
+  switch (t.types) {
+    case 0: return step_units<kBits, false, false>(a, t, begin, end);
+    case 1: return step_units<kBits, true, false>(a, t, begin, end);
+    case 2: return step_units<kBits, false, true>(a, t, begin, end);
+    default: return step_units<kBits, true, true>(a, t, begin, end);
   }
 }
 
-// Units of a workgroup: one to a wave until the launch has several thousand workgroups
-constexpr int64_t kWorkgroups = 4096;
+// What states in 8 bits stand for.  Four values to a lane, whole lines to a store: eight to a lane, stores of every other 16 bytes, took 530 us for
+// 3 x 13824 x 5120 values.
+__global__ __launch_bounds__(256) void adamw_values_kernel(const int8_t* m, const uint8_t* v, const float* m_scale, const float* v_scale, float* m_out,
+                                                           float* v_out, int64_t n) {
+  for (int64_t at = (int64_t(blockIdx.x) * 256 + threadIdx.x) * 4; at < n; at += int64_t(gridDim.x) * 1024) {
+    const uint32_t cm = *reinterpret_cast<const uint32_t*>(m + at), cv = *reinterpret_cast<const uint32_t*>(v + at);
+    const double am = double(m_scale[at >> 8]) * kPerM, av = double(v_scale[at >> 8]) * kPerV;
+    uint32_t to[2][4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      to[0][j] = __float_as_uint(float(m_size(int(int8_t(cm >> (8 * j)))) * am));
+      to[1][j] = __float_as_uint(float(v_size(int(cv >> (8 * j) & 255)) * av));
+    }
+    store_once(m_out + at, U4{to[0][0], to[0][1], to[0][2], to[0][3]});
+    store_once(v_out + at, U4{to[1][0], to[1][1], to[1][2], to[1][3]});
+  }
+}
+
+// Workgroups of a launch, from which on each of their waves takes several units.  Us for 3 x 13824 x 5120 values with 4096 / 16384 / 65536 of them (where
+// the last round of them is a small part): 32 bits 1003 / 955 / 900, 8 bits 562 / 547 / 571.
+constexpr int64_t kWorkgroups32 = 65536, kWorkgroups8 = 16384;
 
 }  // namespace
 
@@ -269,7 +315,7 @@ int32_t launch_adamw(const ca_adamw_tensor* tensors, int32_t n_tensors, int32_t 
     }
     from = to;
     if (a.tensors == 0) continue;
-    a.units = int32_t(std::max<int64_t>(1, units / (kWaves * kWorkgroups))) * kWaves;
+    a.units = int32_t(std::max<int64_t>(1, units / (kWaves * (state_bits == 8 ? kWorkgroups8 : kWorkgroups32)))) * kWaves;
     int32_t workgroups = 0;
     for (int i = 0; i < a.tensors; ++i) {
       a.of[i].first = workgroups;
@@ -285,7 +331,7 @@ int32_t launch_adamw(const ca_adamw_tensor* tensors, int32_t n_tensors, int32_t 
 
 int32_t launch_adamw_values(const void* m, const void* v, const float* m_scale, const float* v_scale, float* m_out, float* v_out, int64_t n, void* stream) {
   if (n == 0) return CA_OK;
-  const int64_t all = (n + 2047) / 2048;
+  const int64_t all = (n + 1023) / 1024;
   hipLaunchKernelGGL(adamw_values_kernel, dim3(unsigned(std::min<int64_t>(all, 16384))), dim3(256), 0, static_cast<hipStream_t>(stream),
                      static_cast<const int8_t*>(m), static_cast<const uint8_t*>(v), m_scale, v_scale, m_out, v_out, n);
   return finish_launch("adamw.hip");

@@ -137,7 +137,7 @@ int32_t layer_linear_adapted_backward_bf16(const void* dy_dev, const void* x_dev
 int32_t layer_adamw(const ca_adamw_tensor* tensors, int32_t n_tensors, int32_t state_bits, double lr, double beta1, double beta2, double eps,
                     double weight_decay, double grad_scale, void* hip_stream) {
   if (n_tensors < 0 || (n_tensors > 0 && !tensors) || (state_bits != 8 && state_bits != 32)) return CA_EINVAL;
-  if (!(lr >= 0.) || !(weight_decay >= 0.) || !(beta1 >= 0. && beta1 < 1.) || !(beta2 >= 0. && beta2 < 1.) || !(float(eps) > 0.f)) return CA_EINVAL;
+  if (!(lr >= 0.) || !(weight_decay >= 0.) || !(beta1 >= 0. && beta1 < 1.) || !(beta2 >= 0. && beta2 < 1.) || !(float(eps) >= 0x1p-126f)) return CA_EINVAL;
   if (!std::isfinite(float(lr)) || !std::isfinite(lr * weight_decay) || !std::isfinite(float(eps)) || !std::isfinite(float(grad_scale))) return CA_EINVAL;
   for (int32_t i = 0; i < n_tensors; ++i)
     if (int32_t rc = check_adamw(tensors[i], state_bits)) return rc;
