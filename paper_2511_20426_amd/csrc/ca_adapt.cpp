@@ -23,7 +23,7 @@ int32_t check_row_norm(const ca::RowNorm& n) {
   return (n.w || n.b) && n.groups > 1 && n.ldw < n.width ? CA_EINVAL : CA_OK;
 }
 
-constexpr int64_t kMaxAdaptedRows = int64_t(1) << 30, kMaxLd = int64_t(1) << 22;
+constexpr int64_t kMaxAdaptedRows = int64_t(1) << 27, kMaxLd = int64_t(1) << 22;
 constexpr int32_t kMaxColumns = 1 << 20;
 
 int32_t check_ld(int64_t ld, int64_t cols) {
@@ -42,7 +42,8 @@ int32_t check_adapted(int64_t m_rows, int32_t n_out, int32_t k_in, int32_t adapt
 // the products of the backward pass sum over the columns of Y too
 int32_t check_adapted_backward(int64_t m_rows, int32_t n_out, int32_t k_in, int32_t adapters, int32_t rank) {
   if (int32_t rc = check_adapted(m_rows, n_out, k_in, adapters, rank)) return rc;
-  return n_out % 128 != 0 ? CA_EUNSUPPORTED : CA_OK;
+  const int64_t largest = int64_t(adapters) * rank * (n_out > k_in ? n_out : k_in);           // a launch may have 2^32 threads
+  return n_out % 128 != 0 || largest > (int64_t(1) << 30) ? CA_EUNSUPPORTED : CA_OK;
 }
 
 // of the state's two buffers: codes and fp32 values are moved in pieces of up to 16 bytes

@@ -75,28 +75,34 @@ __device__ __forceinline__ int next_adapter(const int (&mine)[kRows], int after)
 
 // A workgroup takes 16 kTm rows and 16 kTn values of each; its waves share K in pieces of 128 bytes of a row, which go straight from memory (X) and L2
 // (A) to the registers that the MFMA multiplies from, kAhead pieces on their way; their sums meet in LDS, in order.  Bound by X's way from memory: 23400 x
-// 5120 of rank 32 in 64 rows to a workgroup; fewer rows have fewer of them to a workgroup, few rows eight waves to share K.
+// 5120 of rank 32 72 us, 3.4 TB/s of it; fewer rows have fewer of them to a workgroup (launch_low).
 template <int kTm, int kTn, int kWaves, int kAhead>
 __global__ __launch_bounds__(64 * kWaves) void adapted_low_kernel(LowArgs a) {
   __shared__ Sums part[kWaves][kTm][64];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, l15 = lane & 15, grp = lane >> 4;
   const int m0 = blockIdx.x * 16 * kTm, r0 = blockIdx.y * 16 * kTn;
   int mine[kTm];
-  const uint16_t* x[kTm];
+  // (offsets of 32 bits from an address that all lanes share: 63 rows of up to 2^23 bytes)
+  const uint8_t* const x = reinterpret_cast<const uint8_t*>(a.x + int64_t(m0) * a.ldx);
+  uint32_t xat[kTm], aat[kTn];
+#pragma unroll
+  for (int n = 0; n < kTn; ++n) aat[n] = uint32_t(16 * n + l15) * uint32_t(a.K) * 2 + grp * 16 + wave * 128;
 #pragma unroll
   for (int j = 0; j < kTm; ++j) {
     const int row = m0 + 16 * j + l15;
     mine[j] = adapter_of(a.index, row, a.M, a.adapters);
-    x[j] = a.x + int64_t(min(row, a.M - 1)) * a.ldx + grp * 8;
-    if (row < a.M && mine[j] < 0 && wave == 0) {                    // none: zeros
+    xat[j] = uint32_t(min(row, a.M - 1) - m0) * uint32_t(a.ldx) * 2 + grp * 16 + wave * 128;
+    if (row < a.M && mine[j] < 0 && wave == 0 && blockIdx.z == 0) {                    // none: zeros
 #pragma unroll
       for (int i = 0; i < kTn; ++i) *reinterpret_cast<uint2*>(a.t + int64_t(row) * a.rank + r0 + 16 * i + 4 * grp) = make_uint2(0, 0);
     }
   }
   // piece i of the wave is number wave + i kWaves of the row's
   const int pieces = (a.K / 64 - wave + kWaves - 1) / kWaves;
+  int nth = 0;                                                      // of the rows' adapters; workgroups of another z have others
   for (int g = next_adapter<kTm>(mine, -1); g != INT_MAX; g = next_adapter<kTm>(mine, g)) {
-    const uint16_t* const down = a.down + (int64_t(g) * a.rank + r0 + l15) * a.K + grp * 8;
+    if (nth++ % gridDim.z != blockIdx.z) continue;
+    const uint8_t* const down = reinterpret_cast<const uint8_t*>(a.down + (int64_t(g) * a.rank + r0) * a.K);
     Sums acc[kTn][kTm];
 #pragma unroll
     for (int i = 0; i < kTn; ++i)
@@ -104,30 +110,37 @@ __global__ __launch_bounds__(64 * kWaves) void adapted_low_kernel(LowArgs a) {
       for (int j = 0; j < kTm; ++j) acc[i][j] = Sums{0, 0, 0, 0};
     Frag fa[kAhead][kTn][2], fx[kAhead][kTm][2];
     auto request = [&](int slot, int i) {
-      const int64_t at = int64_t(wave + i * kWaves) * 64;
+      const uint32_t at = uint32_t(i) * (kWaves * 128);
 #pragma unroll
       for (int kk = 0; kk < 2; ++kk) {
 #pragma unroll
-        for (int j = 0; j < kTm; ++j) fx[slot][j][kk] = frag_at(x[j] + at + kk * 32);
+        for (int j = 0; j < kTm; ++j) fx[slot][j][kk] = *reinterpret_cast<const Frag*>(x + at + kk * 64 + xat[j]);
 #pragma unroll
-        for (int n = 0; n < kTn; ++n) fa[slot][n][kk] = frag_at(down + int64_t(16 * n) * a.K + at + kk * 32);
+        for (int n = 0; n < kTn; ++n) fa[slot][n][kk] = *reinterpret_cast<const Frag*>(down + at + kk * 64 + aat[n]);
       }
     };
+    auto multiply = [&](int slot) {
 #pragma unroll
-    for (int s = 0; s < kAhead; ++s)
-      if (s < pieces) request(s, s);
-    for (int i = 0; i < pieces; i += kAhead) {
+      for (int kk = 0; kk < 2; ++kk)
 #pragma unroll
-      for (int s = 0; s < kAhead; ++s) {
-        if (i + s >= pieces) break;
+        for (int n = 0; n < kTn; ++n)
 #pragma unroll
-        for (int kk = 0; kk < 2; ++kk)
+          for (int j = 0; j < kTm; ++j) acc[n][j] = Bf16Products::multiply(fa[slot][n][kk], fx[slot][j][kk], acc[n][j]);
+    };
+    if (pieces > 0) {                                               // (pieces past the wave's last are that again, and not multiplied)
 #pragma unroll
-          for (int n = 0; n < kTn; ++n)
+      for (int s = 0; s < kAhead; ++s) request(s, min(s, pieces - 1));
+      int i = 0;
+      for (; i + kAhead < pieces; i += kAhead) {
 #pragma unroll
-            for (int j = 0; j < kTm; ++j) acc[n][j] = Bf16Products::multiply(fa[s][n][kk], fx[s][j][kk], acc[n][j]);
-        if (i + s + kAhead < pieces) request(s, i + s + kAhead);
+        for (int s = 0; s < kAhead; ++s) {
+          multiply(s);
+          request(s, min(i + s + kAhead, pieces - 1));
+        }
       }
+#pragma unroll
+      for (int s = 0; s < kAhead; ++s)
+        if (i + s < pieces) multiply(s);
     }
     const float scale = a.scales[g];
 #pragma unroll
@@ -244,29 +257,33 @@ __global__ __launch_bounds__(256) void adapted_few_kernel(AdaptedArgs a, int ran
   __shared__ Sums part[kWaves][kTiles][64];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, l15 = lane & 15, grp = lane >> 4;
   const int n0 = blockIdx.x * 16, col = min(n0 + l15, a.N - 1);
-  const uint16_t* const w = a.w + int64_t(col) * a.ldw + grp * 8;
-  const uint16_t* x[kTiles];
+  // (offsets of 32 bits from addresses that all lanes share: 31 rows of up to 2^23 bytes)
+  const uint8_t* const w = reinterpret_cast<const uint8_t*>(a.w + int64_t(n0) * a.ldw);
+  const uint8_t* const x = reinterpret_cast<const uint8_t*>(a.x);
+  const uint32_t wat = uint32_t(col - n0) * uint32_t(a.ldw) * 2 + grp * 16 + wave * 128;
+  uint32_t xat[kTiles];
 #pragma unroll
-  for (int t = 0; t < kTiles; ++t) x[t] = a.x + int64_t(min(16 * t + l15, a.M - 1)) * a.ldx + grp * 8;
+  for (int t = 0; t < kTiles; ++t) xat[t] = uint32_t(min(16 * t + l15, a.M - 1)) * uint32_t(a.ldx) * 2 + grp * 16 + wave * 128;
   Sums acc[kTiles];
 #pragma unroll
   for (int t = 0; t < kTiles; ++t) acc[t] = Sums{0, 0, 0, 0};
-  const int pieces = (a.K / 64 - wave + kWaves - 1) / kWaves;
+  const int pieces = (a.K / 64 - wave + kWaves - 1) / kWaves;       // (of k 128 two waves have none)
   Frag fw[kAhead][2], fx[kAhead][kTiles][2] = {};
   auto request = [&](int slot, int i) {
-    const int64_t at = int64_t(wave + i * kWaves) * 64;
+    const uint32_t at = uint32_t(i) * (kWaves * 128);
 #pragma unroll
-    for (int kk = 0; kk < 2; ++kk) fw[slot][kk] = frag_at(w + at + kk * 32);
+    for (int kk = 0; kk < 2; ++kk) fw[slot][kk] = *reinterpret_cast<const Frag*>(w + at + kk * 64 + wat);
 #pragma unroll
     for (int t = 0; t < kTiles; ++t)
       if (16 * t + l15 < a.M) {                                     // lanes of rows that do not exist ask for nothing
 #pragma unroll
-        for (int kk = 0; kk < 2; ++kk) fx[slot][t][kk] = frag_at(x[t] + at + kk * 32);
+        for (int kk = 0; kk < 2; ++kk) fx[slot][t][kk] = *reinterpret_cast<const Frag*>(x + at + kk * 64 + xat[t]);
       }
   };
+  if (pieces > 0) {                                                 // (pieces past the wave's last are that again, and not multiplied)
 #pragma unroll
-  for (int s = 0; s < kAhead; ++s)
-    if (s < pieces) request(s, s);
+    for (int s = 0; s < kAhead; ++s) request(s, min(s, pieces - 1));
+  }
   // the adapters' rows while the first pieces are on their way
   int mine[kTiles];
 #pragma unroll
@@ -286,17 +303,23 @@ __global__ __launch_bounds__(256) void adapted_few_kernel(AdaptedArgs a, int ran
       }
     }
   }
-  for (int i = 0; i < pieces; i += kAhead) {
+  auto multiply = [&](int slot) {
+#pragma unroll
+    for (int kk = 0; kk < 2; ++kk)
+#pragma unroll
+      for (int t = 0; t < kTiles; ++t) acc[t] = Bf16Products::multiply(fw[slot][kk], fx[slot][t][kk], acc[t]);
+  };
+  int i = 0;
+  for (; i + kAhead < pieces; i += kAhead) {
 #pragma unroll
     for (int s = 0; s < kAhead; ++s) {
-      if (i + s >= pieces) break;
-#pragma unroll
-      for (int kk = 0; kk < 2; ++kk)
-#pragma unroll
-        for (int t = 0; t < kTiles; ++t) acc[t] = Bf16Products::multiply(fw[s][kk], fx[s][t][kk], acc[t]);
-      if (i + s + kAhead < pieces) request(s, i + s + kAhead);
+      multiply(s);
+      request(s, min(i + s + kAhead, pieces - 1));
     }
   }
+#pragma unroll
+  for (int s = 0; s < kAhead; ++s)
+    if (i + s < pieces) multiply(s);
 #pragma unroll
   for (int t = 0; t < kTiles; ++t) part[wave][t][lane] = acc[t];
   __syncthreads();
@@ -430,29 +453,56 @@ __global__ __launch_bounds__(256) void adapted_sum_kernel(SumArgs a) {
     for (int g = tid; g < a.adapters; g += 256) a.there[split * a.adapters + g] = there[g];
 }
 
-// out [adapters][R][C], or transposed [adapters][C][R], from the splits' parts
+// out [adapters][R][C], or transposed [adapters][C][R], from the splits' parts: a workgroup takes 256 columns of a row (C is a multiple of 8), four to a
+// lane, and its four waves share the splits
 template <bool kTransposed>
 __global__ __launch_bounds__(256) void adapted_join_kernel(const float* parts, const int32_t* there, int splits, int adapters, int rank, int R, int C, uint16_t* out) {
-  const int64_t all = int64_t(adapters) * R * C;
-  for (int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x; i < all; i += int64_t(gridDim.x) * 256) {
-    const int c = int(i % C), r = int(i / C % R), g = int(i / C / R);
-    float sum = 0.f;
-    for (int s = 0; s < splits; ++s)
-      if (there[s * adapters + g]) sum += parts[((int64_t(s) * adapters + g) * rank + r) * C + c];
-    out[kTransposed ? (int64_t(g) * C + c) * R + r : i] = uint16_t(pack_bf16(sum, sum));
+  __shared__ Sums sums[4][64];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = blockIdx.x * 256 + 4 * lane, r = blockIdx.y, g = blockIdx.z;
+  Sums sum{0, 0, 0, 0};
+  if (c < C) {
+    const float* const from = parts + (int64_t(g) * rank + r) * C + c;
+    const int64_t step = int64_t(adapters) * rank * C;
+#pragma unroll 4
+    for (int s = wave; s < splits; s += 4) {                        // (a part that is not there holds anything)
+      const Sums one = *reinterpret_cast<const Sums*>(from + s * step);
+      const bool adds = there[s * adapters + g] != 0;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) sum[e] = adds ? sum[e] + one[e] : sum[e];
+    }
+  }
+  sums[wave][lane] = sum;
+  __syncthreads();
+  if (wave != 0 || c >= C) return;
+  sum = (sums[0][lane] + sums[1][lane]) + (sums[2][lane] + sums[3][lane]);
+  const uint2 two = make_uint2(pack_bf16(sum[0], sum[1]), pack_bf16(sum[2], sum[3]));
+  if constexpr (kTransposed) {
+    uint16_t* const to = out + (int64_t(g) * C + c) * R + r;
+    to[0] = uint16_t(two.x), to[R] = uint16_t(two.x >> 16), to[2 * R] = uint16_t(two.y), to[3 * R] = uint16_t(two.y >> 16);
+  } else {
+    uint16_t* const to = out + (int64_t(g) * R + r) * C + c;       // (whose alignment is the caller's)
+    to[0] = uint16_t(two.x), to[1] = uint16_t(two.x >> 16), to[2] = uint16_t(two.y), to[3] = uint16_t(two.y >> 16);
   }
 }
 
-// [rows][cols] of each adapter to [cols][rows]
-__global__ __launch_bounds__(256) void adapted_transpose_kernel(const uint16_t* from, uint16_t* to, int rows, int cols) {
-  __shared__ uint16_t tile[32][33];
-  const int64_t at = int64_t(blockIdx.z) * rows * cols;
-  const int r0 = blockIdx.y * 32, c0 = blockIdx.x * 32, x = threadIdx.x & 31, y = threadIdx.x >> 5;
-  for (int i = y; i < 32; i += 8)
-    if (r0 + i < rows && c0 + x < cols) tile[i][x] = from[at + int64_t(r0 + i) * cols + c0 + x];
+// [rows][cols] of each adapter to [cols][rows], of up to two of them
+struct Transposed {
+  const uint16_t* from;
+  uint16_t* to;
+  int32_t rows, cols, tiles;                      // tiles of 64 x 32 of an adapter
+};
+__global__ __launch_bounds__(256) void adapted_transpose_kernel(Transposed one, Transposed two) {
+  __shared__ uint16_t tile[64][33];
+  const bool second = int(blockIdx.x) >= one.tiles;
+  const Transposed t = second ? two : one;
+  const int nth = blockIdx.x - (second ? one.tiles : 0), across = (t.cols + 31) / 32;
+  const int64_t at = int64_t(blockIdx.y) * t.rows * t.cols;
+  const int r0 = nth / across * 64, c0 = nth % across * 32;
+  for (int i = threadIdx.x >> 5, x = threadIdx.x & 31; i < 64; i += 8)
+    if (r0 + i < t.rows && c0 + x < t.cols) tile[i][x] = t.from[at + int64_t(r0 + i) * t.cols + c0 + x];
   __syncthreads();
-  for (int i = y; i < 32; i += 8)
-    if (c0 + i < cols && r0 + x < rows) to[at + int64_t(c0 + i) * rows + r0 + x] = tile[x][i];
+  for (int i = threadIdx.x >> 6, x = threadIdx.x & 63; i < 32; i += 4)
+    if (c0 + i < t.cols && r0 + x < t.rows) t.to[at + int64_t(c0 + i) * t.rows + r0 + x] = tile[x][i];
 }
 
 // ------------------------------------------------------------------------------------------------ launches
@@ -495,18 +545,21 @@ int32_t enqueue_adapted(AdaptedArgs& a, int rank, void* stream) {
 
 template <int kTm, int kTn, int kWaves, int kAhead>
 int32_t enqueue_low(const LowArgs& a, void* stream) {
-  hipLaunchKernelGGL((adapted_low_kernel<kTm, kTn, kWaves, kAhead>), dim3(unsigned((a.M + 16 * kTm - 1) / (16 * kTm)), unsigned(a.rank / (16 * kTn))),
-                     dim3(64 * kWaves), 0, static_cast<hipStream_t>(stream), a);
+  // few rows' adapters are dealt to several workgroups: 257 rows of six in any order, of rank 5 and k 1024 21 us by one of them
+  const unsigned x = unsigned((a.M + 16 * kTm - 1) / (16 * kTm)), y = unsigned(a.rank / (16 * kTn));
+  const unsigned z = std::max(1u, std::min({unsigned(a.adapters), 8u, 512u / (x * y)}));
+  hipLaunchKernelGGL((adapted_low_kernel<kTm, kTn, kWaves, kAhead>), dim3(x, y, z), dim3(64 * kWaves), 0, static_cast<hipStream_t>(stream), a);
   return finish_launch(kWhat);
 }
 
-// T = s (X A'): few rows: 16 values to a workgroup, eight waves; up to 8192 rows 16 to a workgroup, above 64
+// T = s (X A').  Few rows take small workgroups, to be many; many rows 32 or 64 at a time, for A's way from L2.  Us for k 5120 by 16 rows and values /
+// by 32 rows and 32 values: 1000 rows of rank 32 11.4 / 19.9, 23400 111 / 72; k 1536, 4680 rows 13.0 / 7.8; 23400 rows of rank 64 by 32 rows and 64
+// values in four waves / in eight 106 / 87 (4680 x 1536 11.0 / 13.9); of rank 128 by 32 x 128 / 64 x 64 140 / 152 (4680 x 1536 17.1 / 14.9).
 int32_t launch_low(const LowArgs& a, void* stream) {
-  if (a.M <= kFewRows) return enqueue_low<1, 1, 8, 4>(a, stream);
-  const bool many = a.M > 8192;
-  if (a.rank == 32) return many ? enqueue_low<4, 2, 4, 2>(a, stream) : enqueue_low<1, 2, 4, 4>(a, stream);
-  if (a.rank == 64) return many ? enqueue_low<4, 4, 4, 2>(a, stream) : enqueue_low<1, 4, 4, 2>(a, stream);
-  return many ? enqueue_low<4, 8, 4, 1>(a, stream) : enqueue_low<1, 8, 4, 2>(a, stream);
+  if (a.M <= 2048) return a.M <= 512 || a.rank == 32 ? enqueue_low<1, 1, 4, 4>(a, stream) : enqueue_low<1, 2, 8, 4>(a, stream);
+  if (a.rank == 32) return enqueue_low<2, 2, 4, 2>(a, stream);
+  if (a.rank == 64) return a.M > 8192 ? enqueue_low<2, 4, 8, 2>(a, stream) : enqueue_low<2, 4, 4, 2>(a, stream);
+  return enqueue_low<4, 4, 4, 2>(a, stream);
 }
 
 int32_t launch_adapted_gemm(AdaptedArgs& a, int rank, void* stream) {
@@ -527,10 +580,10 @@ int32_t launch_adapted_gemm(AdaptedArgs& a, int rank, void* stream) {
   }
 }
 
-// Splits of the rows of a sum over C columns: enough workgroups to fill the chip, 64 rows or more to each, no more room than 256 MB
+// Splits of the rows of a sum over C columns: enough workgroups to fill the chip, 128 rows or more to each, no more room than 256 MB
 int sum_splits(int64_t M, int32_t C, int32_t adapters, int32_t rank) {
   const int64_t tiles = (int64_t(C) + kSumCols - 1) / kSumCols, one = int64_t(adapters) * rank * C * 4;
-  return int(std::max<int64_t>(1, std::min({(1024 + tiles - 1) / tiles, (M + 63) / 64, (int64_t(256) << 20) / one})));
+  return int(std::max<int64_t>(1, std::min({(768 + tiles - 1) / tiles, (M + 127) / 128, (int64_t(256) << 20) / one})));
 }
 
 size_t up16(size_t n) { return (n + 15) / 16 * 16; }
@@ -563,16 +616,13 @@ int32_t launch_adapter_sum(const uint16_t* low, const void* wide, int64_t ld, co
     hipLaunchKernelGGL(kernel, dim3(unsigned((C + kSumCols - 1) / kSumCols), unsigned(splits)), dim3(256), 0, s, a);
     if (const int32_t rc = finish_launch(kWhat); rc != CA_OK) return rc;
   }
-  const int64_t all = int64_t(adapters) * rank_used * C;
-  hipLaunchKernelGGL(transposed ? adapted_join_kernel<true> : adapted_join_kernel<false>, dim3(unsigned(std::min<int64_t>((all + 255) / 256, 16384))), dim3(256), 0, s,
-                     parts, there, splits, adapters, rank, rank_used, C, static_cast<uint16_t*>(out));
+  hipLaunchKernelGGL(transposed ? adapted_join_kernel<true> : adapted_join_kernel<false>, dim3(unsigned((C + 255) / 256), unsigned(rank_used), unsigned(adapters)),
+                     dim3(256), 0, s, parts, there, splits, adapters, rank, rank_used, C, static_cast<uint16_t*>(out));
   return finish_launch(kWhat);
 }
 
-int32_t launch_transpose(const void* from, void* to, int rows, int cols, int adapters, void* stream) {
-  hipLaunchKernelGGL(adapted_transpose_kernel, dim3(unsigned((cols + 31) / 32), unsigned((rows + 31) / 32), unsigned(adapters)), dim3(256), 0,
-                     static_cast<hipStream_t>(stream), static_cast<const uint16_t*>(from), static_cast<uint16_t*>(to), rows, cols);
-  return finish_launch(kWhat);
+Transposed transposed(const void* from, void* to, int rows, int cols) {
+  return Transposed{static_cast<const uint16_t*>(from), static_cast<uint16_t*>(to), rows, cols, (rows + 63) / 64 * ((cols + 31) / 32)};
 }
 
 }  // namespace
@@ -598,13 +648,14 @@ int32_t launch_adapted_backward(const AdaptedLinear& p, const void* dy, int64_t 
   float* const parts = reinterpret_cast<float*>(room + r.parts);
   const int32_t M = int32_t(p.M);
   if (M > 0 && (dx || d_down)) {                   // s dY B
-    if (const int32_t rc = launch_transpose(p.up, room + r.up_t, p.N, p.rank, p.adapters, stream); rc != CA_OK) return rc;
+    const Transposed up = transposed(p.up, room + r.up_t, p.N, p.rank), down = dx ? transposed(p.down, room + r.down_t, p.rank, p.K) : Transposed{};
+    hipLaunchKernelGGL(adapted_transpose_kernel, dim3(unsigned(up.tiles + down.tiles), unsigned(p.adapters)), dim3(256), 0, static_cast<hipStream_t>(stream), up, down);
+    if (const int32_t rc = finish_launch(kWhat); rc != CA_OK) return rc;
     const LowArgs l{static_cast<const uint16_t*>(dy), reinterpret_cast<const uint16_t*>(room + r.up_t), p.scales, p.index, low_dy, M, p.N, int32_t(lddy), p.adapters,
                     p.rank};
     if (const int32_t rc = launch_low(l, stream); rc != CA_OK) return rc;
   }
   if (M > 0 && dx) {
-    if (const int32_t rc = launch_transpose(p.down, room + r.down_t, p.rank, p.K, p.adapters, stream); rc != CA_OK) return rc;
     AdaptedArgs a{static_cast<const uint16_t*>(dy), static_cast<const uint16_t*>(p.w), static_cast<uint16_t*>(dx), low_dy,
                   reinterpret_cast<const uint16_t*>(room + r.down_t), p.index, p.ldy, M, p.K, p.N, int32_t(lddy), int32_t(p.ldw), p.adapters, 0, 0, 0};
     if (const int32_t rc = launch_adapted_gemm(a, p.rank, stream); rc != CA_OK) return rc;

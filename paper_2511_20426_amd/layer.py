@@ -4,13 +4,19 @@
 
 The projections into and out of the attention and out of the feed-forward block are held and multiplied in 8 bits (linear_i8), gate and up
 projection are one kernel in bf16 (gated_linear), queries and keys are normed per head on the way to their rotation, the keys on the way into
-the shared pool.  Norms of the layer's input, modulation by the timestep and cross-attention are the caller's.  (Sizes are Wan's; its published
-layers norm queries and keys over the whole width and have a plain gelu feed-forward half.)
+the shared pool.  With a modulation each half has its input normed and modulated by the timestep of its block (layer_norm), and its result gated:
+
+    y = x + gate1 * W_out attention(.. weight1 * norm(x) + bias1 ..)        z = y + gate2 * W_down (.. weight2 * norm(y) + bias2 ..)
+
+Cross-attention is the caller's.  (Sizes are Wan's; its published layers norm queries and keys over the whole width and have a plain gelu
+feed-forward half.)
 
 Run as a program it times such a layer in the steady state of a cascade, or a training step of the feed-forward half:
 
     python -m paper_2511_20426_amd.layer                  # Wan-1.3B shape, five blocks in flight over six cached ones
     python -m paper_2511_20426_amd.layer --train          # gated projections and the one behind them, forward, backward, update
+    python -m paper_2511_20426_amd.layer --train --adamw 8   # the same by AdamW, states in 8 bits (or 32)
+    python -m paper_2511_20426_amd.layer --adapt          # low-rank adapters of the QKV projection behind a norm: forward, backward, AdamW
 """
 from __future__ import annotations
 
@@ -22,7 +28,9 @@ from typing import Sequence
 import torch
 
 from . import binding as B
-from .runner import CascadePool, QuantizedRows, gated_linear, gated_linear_backward, gated_linear_train, linear, linear_i8, quantize_rows
+from .optim import AdamW
+from .runner import (Adapters, CascadePool, QuantizedRows, gated_linear, gated_linear_backward, gated_linear_train, layer_norm, layer_norm_backward, linear,
+                     linear_adapted_backward, linear_adapted_train, linear_i8, quantize_rows)
 
 
 @dataclass
@@ -45,24 +53,34 @@ class CascadeLayer:
         return cls(quantize_rows(w_qkv), quantize_rows(w_out), quantize_rows(w_down), w_gate, w_up, q_norm, k_norm, **more)
 
     def __call__(self, pool: CascadePool, x: torch.Tensor, inflight: Sequence[int], timesteps: Sequence[int], epoch: int = 0,
-                 mode: int = B.CA_BIDIRECTIONAL) -> torch.Tensor:
-        """One iteration for the blocks in flight (oldest first, consecutive in the video): x [C*L, width] -> [C*L, width]."""
+                 mode: int = B.CA_BIDIRECTIONAL, modulation: torch.Tensor | None = None) -> torch.Tensor:
+        """One iteration for the blocks in flight (oldest first, consecutive in the video): x [C*L, width] -> [C*L, width].  modulation (fp32 or bf16): [C, 6,
+        width], of each block weight, bias and gate of the attention's half, then those of the feed-forward half; None: no norms, gates of one."""
         L, H, D = pool.block_tokens, pool.heads, pool.head_dim
         n = len(inflight) * L
         assert x.shape == (n, H * D) and all(b == inflight[0] + i for i, b in enumerate(inflight))
-        qkv = linear_i8(x, self.w_qkv).view(n, 3, H, D)
+        assert modulation is None or modulation.shape == (len(inflight), 6, H * D)
+
+        def normed(t, half):
+            return t if modulation is None else layer_norm(t, modulation[:, 3 * half], modulation[:, 3 * half + 1], eps=self.eps)
+
+        def added(t, result, half):
+            return t + result if modulation is None else torch.addcmul(t.view(len(inflight), L, -1), result.view(len(inflight), L, -1),
+                                                                       modulation[:, 3 * half + 2, None].to(t.dtype)).view_as(t)
+
+        qkv = linear_i8(normed(x, 0), self.w_qkv).view(n, 3, H, D)
         blocks = [qkv[i * L:(i + 1) * L] for i in range(len(inflight))]
         pool.append_batch(inflight, timesteps, epoch, [b[:, 1] for b in blocks], [b[:, 2] for b in blocks], k_weight=self.k_norm, eps=self.eps)
         q, _ = pool.qk_norm_rope(qkv[:, 0], None, self.q_norm, None, pool.frames_per_block * inflight[0], eps=self.eps)
         o = pool.forward(q, inflight, mode)
-        x = x + linear_i8(o.view(n, H * D), self.w_out)
-        h = gated_linear(x, self.w_gate, self.w_up, self.activation)
-        return x + linear_i8(h, self.w_down)
+        x = added(x, linear_i8(o.view(n, H * D), self.w_out), 0)
+        h = gated_linear(normed(x, 1), self.w_gate, self.w_up, self.activation)
+        return added(x, linear_i8(h, self.w_down), 1)
 
 
-def feed_forward_step(x, w_gate, w_up, w_down, target, activation: str = "silu", lr: float = 0.0):
+def feed_forward_step(x, w_gate, w_up, w_down, target, activation: str = "silu", lr: float = 0.0, optimizer: AdamW | None = None):
     """One step of training the feed-forward half towards target [M, N] (mean squared error), all in bf16: (loss, gradients of w_gate, w_up,
-    w_down and x); with lr the weights are updated in place.  (w_down, dy and h are transposed by torch's copies for the linear map, which multiplies
+    w_down and x); with an optimizer of the three weights it takes a step, with lr the weights go down their gradients.  (w_down, dy and h are transposed by torch's copies for the linear map, which multiplies
     rows by rows.)"""
     h, saved = gated_linear_train(x, w_gate, w_up, activation)
     y = linear(h, w_down)
@@ -74,10 +92,27 @@ def feed_forward_step(x, w_gate, w_up, w_down, target, activation: str = "silu",
     dyt[:, :dy.shape[0]], ht[:, :h.shape[0]] = dy.t(), h.t()
     dw_down = linear(dyt, ht)
     dx, dw_gate, dw_up = gated_linear_backward(dh, x, w_gate, w_up, saved, activation)
-    if lr:
+    if optimizer is not None:
+        optimizer.step((dw_gate, dw_up, dw_down))
+    elif lr:
         for w, d in ((w_gate, dw_gate), (w_up, dw_up), (w_down, dw_down)):
             w.add_(d, alpha=-lr)
     return off.square().mean(), (dw_gate, dw_up, dw_down, dx)
+
+
+def adapter_step(x, norm_weight, norm_bias, w, w_t, adapters: Adapters, index, target, optimizer: AdamW | None = None, eps: float = 1e-6):
+    """One step of training low-rank adapters of a frozen projection w [N, K] (w_t [K, N]: it transposed, laid out once) and the norm ahead of it towards
+    target [M, N] (mean squared error): y = adapted(norm(x)), each row of x [M, K] with the adapter that index says.  (loss, gradients of the adapters'
+    down and up, of the norm's weight and bias and of x); an optimizer of those four parameters takes a step."""
+    h = layer_norm(x, norm_weight, norm_bias, eps=eps)
+    y, saved = linear_adapted_train(h, w, adapters, index)
+    off = y.float() - target.float()
+    dy = (off * (2.0 / off.numel())).to(torch.bfloat16)
+    dh, d_down, d_up = linear_adapted_backward(dy, h, w_t, adapters, index, saved)
+    dx, dweight, dbias = layer_norm_backward(dh, x, norm_weight, norm_bias, eps=eps, dx=dh)
+    if optimizer is not None:
+        optimizer.step((d_down, d_up, dweight, dbias))
+    return off.square().mean(), (d_down, d_up, dweight, dbias, dx)
 
 
 def _timed(f, steps):
@@ -101,6 +136,10 @@ def main() -> None:
     p.add_argument("--hidden", type=int, help="columns of the feed-forward block (8/3 of the width)")
     p.add_argument("--steps", type=int, default=10)
     p.add_argument("--train", action="store_true")
+    p.add_argument("--adamw", type=int, choices=(8, 32), help="--train: AdamW with states of so many bits in place of plain descent")
+    p.add_argument("--adapt", action="store_true")
+    p.add_argument("--adapters", type=int, default=1, help="--adapt: how many, in equal runs of the tokens")
+    p.add_argument("--rank", type=int, default=32, choices=(32, 64, 128))
     a = p.parse_args()
     dev, width = "cuda:0", a.heads * 128
     hidden = a.hidden or -(-width * 8 // 3 // 128) * 128
@@ -114,9 +153,22 @@ def main() -> None:
     if a.train:
         x, target = normal(L, width), normal(L, width)
         losses = []
-        ms = _timed(lambda: losses.append(feed_forward_step(x, w_gate, w_up, w_down, target, lr=64.0)[0]), a.steps)
+        optimizer = AdamW((w_gate, w_up, w_down), lr=1e-3, state_bits=a.adamw) if a.adamw else None
+        ms = _timed(lambda: losses.append(feed_forward_step(x, w_gate, w_up, w_down, target, lr=64.0, optimizer=optimizer)[0]), a.steps)
         print(json.dumps({"metric": "feed_forward_training_step_ms", "value": ms, "rows": L, "width": width, "hidden": hidden,
                           "loss_first": losses[0].item(), "loss_last": losses[-1].item(), "data": "synthetic"}))
+        return
+    if a.adapt:
+        w = normal(3 * width, width, scale=width ** -0.5)
+        down, up = normal(a.adapters, a.rank, width, scale=width ** -0.5), torch.zeros((a.adapters, 3 * width, a.rank), dtype=torch.bfloat16, device=dev)
+        adapters, weight, bias = Adapters.from_weights(down, up), torch.ones(width, device=dev), torch.zeros(width, device=dev)
+        # masters in fp32; the adapters' own weights are their copies
+        optimizer = AdamW((down.float(), up.float(), weight, bias), lr=1e-3, copies=(adapters.down, adapters.up, None, None))
+        x, target, index = normal(L, width), normal(L, 3 * width), (torch.arange(L, device=dev) * a.adapters // L).to(torch.int32)
+        losses, w_t = [], w.t().contiguous()
+        ms = _timed(lambda: losses.append(adapter_step(x, weight, bias, w, w_t, adapters, index, target, optimizer)[0]), a.steps)
+        print(json.dumps({"metric": "adapter_training_step_ms", "value": ms, "rows": L, "width": width, "n_out": 3 * width, "adapters": a.adapters,
+                          "rank": a.rank, "loss_first": losses[0].item(), "loss_last": losses[-1].item(), "data": "synthetic"}))
         return
     pool = CascadePool(heads=a.heads, head_dim=128, frames_per_block=3, grid_h=a.grid[0], grid_w=a.grid[1], rope_dims=(44, 42, 42), rope_theta=10000.0,
                        sink_blocks=0, window_blocks=a.cached, max_inflight=a.inflight, page_tokens=128, dtype="bf16", device=dev)

@@ -2,7 +2,7 @@
 
 No arithmetic of the method happens here; every tensor handed to the library is passed as a
 raw device address.  Results carry no autograd history, whatever the arguments require: where there is a
-backward pass (qk_norm_rope_backward, gated_linear_backward) the caller calls it.
+backward pass (qk_norm_rope_backward, gated_linear_backward, layer_norm_backward, linear_adapted_backward) the caller calls it.
 """
 from __future__ import annotations
 
@@ -580,7 +580,8 @@ def linear_adapted_backward(dy: torch.Tensor, x: torch.Tensor, w_t: torch.Tensor
 
 def attention_layer(pool: CascadePool, x: torch.Tensor, w_qkv: torch.Tensor, w_out: torch.Tensor,
                     inflight: Sequence[int], timesteps: Sequence[int], epoch: int, mode: int,
-                    rotate_q_in_kernel: bool = True, publish_in_projection: bool = False) -> torch.Tensor:
+                    rotate_q_in_kernel: bool = True, publish_in_projection: bool = False, qkv_adapters: Adapters | None = None,
+                    out_adapters: Adapters | None = None, adapter_index: torch.Tensor | None = None) -> torch.Tensor:
     """One self-attention layer around the shared pool, for the blocks in flight (oldest first,
     consecutive in the video): QKV projection, K/V of every block published to the cache, Q
     rotated, cascaded attention, output projection.  x [C*L, width], w_qkv [3*width, width] with
@@ -589,15 +590,21 @@ def attention_layer(pool: CascadePool, x: torch.Tensor, w_qkv: torch.Tensor, w_o
     queries go to the attention kernel as they are (it rotates them while loading), or, with
     rotate_q_in_kernel=False, through rope3d_apply into a contiguous tensor first.  With
     publish_in_projection the first two steps are one launch (layer_qkv_publish): K/V go from the
-    projection's epilogue straight into pool pages; three launches per layer in all."""
+    projection's epilogue straight into pool pages; three launches per layer in all.
+    qkv_adapters, out_adapters: low-rank adapters beside the projections (linear_adapted), adapter_index [C*L] saying which of them
+    each token has; not with publish_in_projection, whose kernel has none."""
     L, H, D = pool.block_tokens, pool.heads, pool.head_dim
     n = len(inflight) * L
     assert x.shape == (n, H * D) and w_qkv.shape == (3 * H * D, H * D) and w_out.shape == (H * D, H * D)
+    def projected(t, w, adapters):
+        return linear(t, w) if adapters is None else linear_adapted(t, w, adapters, adapter_index)
+
     if publish_in_projection:
+        assert qkv_adapters is None, "the publishing projection has no adapters"
         q = pool.qkv_publish(x, w_qkv, inflight, timesteps, epoch)
         o = pool.forward_rope(q, inflight, mode)
-        return linear(o.view(n, H * D), w_out)
-    qkv = linear(x, w_qkv).view(n, 3, H, D)
+        return projected(o.view(n, H * D), w_out, out_adapters)
+    qkv = projected(x, w_qkv, qkv_adapters).view(n, 3, H, D)
     blocks = [qkv[i * L:(i + 1) * L] for i in range(len(inflight))]
     pool.append_batch(inflight, timesteps, epoch, [b[:, 1] for b in blocks], [b[:, 2] for b in blocks])
     if rotate_q_in_kernel:
@@ -605,4 +612,4 @@ def attention_layer(pool: CascadePool, x: torch.Tensor, w_qkv: torch.Tensor, w_o
     else:
         q_rot = pool.rope(qkv[:, 0], pool.frames_per_block * inflight[0])     # strided view -> contiguous
         o = pool.forward(q_rot, inflight, mode)
-    return linear(o.view(n, H * D), w_out)
+    return projected(o.view(n, H * D), w_out, out_adapters)

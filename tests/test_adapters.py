@@ -273,7 +273,7 @@ def test_arguments_refused():
     good = dict(x=p, w=p, down=p, up=p, scales=p, index=p, low=p, y=p, m=40, n=136, k=256, adapters=3, rank=32, ldx=256, ldw=256, ldy=136)
     for change, code in ((dict(m=-1), B.CA_EINVAL), (dict(adapters=0), B.CA_EINVAL), (dict(adapters=4097), B.CA_EUNSUPPORTED), (dict(rank=16), B.CA_EUNSUPPORTED),
                          (dict(rank=96), B.CA_EUNSUPPORTED), (dict(n=4), B.CA_EUNSUPPORTED), (dict(n=132), B.CA_EUNSUPPORTED), (dict(k=192), B.CA_EUNSUPPORTED),
-                         (dict(n=2 ** 20 + 8, ldy=2 ** 20 + 8), B.CA_EUNSUPPORTED), (dict(m=2 ** 30 + 1), B.CA_EUNSUPPORTED), (dict(ldx=248), B.CA_EINVAL),
+                         (dict(n=2 ** 20 + 8, ldy=2 ** 20 + 8), B.CA_EUNSUPPORTED), (dict(m=2 ** 27 + 1), B.CA_EUNSUPPORTED), (dict(ldx=248), B.CA_EINVAL),
                          (dict(ldw=260), B.CA_EINVAL), (dict(ldx=2 ** 22), B.CA_EUNSUPPORTED), (dict(ldy=128), B.CA_EINVAL), (dict(ldy=140), B.CA_EINVAL),
                          (dict(scales=0), B.CA_EINVAL), (dict(index=0), B.CA_EINVAL), (dict(index=p + 2), B.CA_EINVAL), (dict(scales=p + 1), B.CA_EINVAL)) + tuple(
                              (dict([(name, at)]), B.CA_EINVAL) for name in ("x", "w", "down", "up", "low", "y") for at in (0, p + 8)):
@@ -282,6 +282,7 @@ def test_arguments_refused():
         assert e.value.code == code, change
     B.layer_linear_adapted_bf16(*{**good, "m": 0, "x": 0, "y": 0}.values())
     assert B.layer_linear_adapted_backward_workspace(40, 136, 256, 3, 32) == 0 and B.layer_linear_adapted_backward_workspace(40, 256, 256, 3, 33) == 0
+    assert B.layer_linear_adapted_backward_workspace(40, 256, 2 ** 20, 64, 32) == 0
     need = B.layer_linear_adapted_backward_workspace(40, 256, 384, 3, 32)
     assert need > 0
     back = dict(dy=p, x=p, w_t=p, down=p, up=p, scales=p, index=p, low=p, dx=p, d_down=p, d_up=p, m=40, n=256, k=384, adapters=3, rank=32, used=5, lddy=256, ldx=384,
