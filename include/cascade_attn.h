@@ -399,8 +399,9 @@ int32_t layer_linear_adapted_backward_bf16(const void* dy_dev, const void* x_dev
  *                 that share its scale infinite or NaN.
  *   step          four numbers on the device, aligned to 16 bytes: steps done (0 at first; the call adds one, so that a recorded call counts on in every
  *                 replay), and room that the call uses
- * Tensors, copies, states and steps overlap nothing else of the call.  lr, weight_decay and the like are taken when the call is made: a recorded one keeps
- * them.  0 <= beta < 1, eps >= 2^-126 (CA_EINVAL); n <= CA_ADAMW_MAX_VALUES.  Two launches for every 40 tensors. */
+ * tensors_dev: the same array in device memory, aligned to 16 bytes, which the caller made once and keeps as long as calls (or graphs of them) go by it;
+ * its gradients are not read, they are those of `tensors`.  Tensors, copies, states and steps overlap nothing else of the call.  lr, weight_decay and the like are taken when the call is made: a recorded one keeps
+ * them.  0 <= beta < 1, eps >= 2^-126 (CA_EINVAL); n <= CA_ADAMW_MAX_VALUES.  Two launches for every 300 tensors. */
 #define CA_ADAMW_MAX_VALUES ((int64_t)1 << 40)
 typedef struct {
   void* param;
@@ -414,8 +415,8 @@ typedef struct {
   int64_t n;
   int32_t param_dtype, grad_dtype;
 } ca_adamw_tensor;
-int32_t layer_adamw(const ca_adamw_tensor* tensors, int32_t n_tensors, int32_t state_bits, double lr, double beta1, double beta2, double eps,
-                    double weight_decay, double grad_scale, void* hip_stream);
+int32_t layer_adamw(const ca_adamw_tensor* tensors, const ca_adamw_tensor* tensors_dev, int32_t n_tensors, int32_t state_bits, double lr, double beta1,
+                    double beta2, double eps, double weight_decay, double grad_scale, void* hip_stream);
 /* What states in 8 bits stand for, in fp32: n values, a multiple of 256 (codes and results aligned to 16 bytes). */
 int32_t layer_adamw_values(const void* m_codes_dev, const void* v_codes_dev, const float* m_scales_dev, const float* v_scales_dev, float* m_dev,
                            float* v_dev, int64_t n, void* hip_stream);

@@ -190,7 +190,7 @@ def _load() -> C.CDLL:
     lib.layer_linear_adapted_backward_bf16.argtypes = [vp] * 11 + [i64] + [i32] * 5 + [i64] * 4 + [vp, C.c_size_t, vp]
     f64 = C.c_double
     lib.layer_adamw.restype = i32
-    lib.layer_adamw.argtypes = [C.POINTER(ca_adamw_tensor), i32, i32] + [f64] * 6 + [vp]
+    lib.layer_adamw.argtypes = [C.POINTER(ca_adamw_tensor), vp, i32, i32] + [f64] * 6 + [vp]
     lib.layer_adamw_values.restype = i32
     lib.layer_adamw_values.argtypes = [vp] * 6 + [i64, vp]
     lib.ca_sched_create.restype = i32
@@ -246,6 +246,9 @@ def _load_calls():
             lib.layer_qk_norm_rope, lib.layer_qk_norm_rope_workspace, lib.layer_qk_norm_rope_backward, lib.kv_cache_append_batch_norm,
             lib.layer_linear_i8_workspace, lib.layer_linear_i8_values, lib.layer_gated_bf16, lib.layer_gated_saved_bytes, lib.layer_gated_backward_workspace,
             lib.layer_gated_backward_bf16)))
+        ext.bind_adapt(*(C.cast(f, C.c_void_p).value for f in (
+            lib.layer_norm, lib.layer_norm_backward_workspace, lib.layer_norm_backward, lib.layer_linear_adapted_bf16,
+            lib.layer_linear_adapted_backward_workspace, lib.layer_linear_adapted_backward_bf16, lib.layer_adamw)))
         return ext
     except Exception as e:
         warnings.warn(f"{path} cannot be used, calls take more host time without it: {e}", RuntimeWarning)
@@ -545,10 +548,10 @@ def layer_linear_adapted_backward_bf16(dy_ptr: int, x_ptr: int, w_t_ptr: int, do
            "layer_linear_adapted_backward_bf16")
 
 
-def layer_adamw(tensors, n_tensors: int, state_bits: int, lr: float, beta1: float, beta2: float, eps: float, weight_decay: float, grad_scale: float,
-                stream: int = 0) -> None:
-    """tensors: an array of ca_adamw_tensor"""
-    _check(lib.layer_adamw(tensors, n_tensors, state_bits, lr, beta1, beta2, eps, weight_decay, grad_scale, index(stream or 0)), "layer_adamw")
+def layer_adamw(tensors, tensors_dev_ptr: int, n_tensors: int, state_bits: int, lr: float, beta1: float, beta2: float, eps: float, weight_decay: float,
+                grad_scale: float, stream: int = 0) -> None:
+    """tensors: an array of ca_adamw_tensor, and where it lies on the device"""
+    _check(lib.layer_adamw(tensors, index(tensors_dev_ptr or 0), n_tensors, state_bits, lr, beta1, beta2, eps, weight_decay, grad_scale, index(stream or 0)), "layer_adamw")
 
 
 def layer_adamw_values(m_codes_ptr: int, v_codes_ptr: int, m_scales_ptr: int, v_scales_ptr: int, m_ptr: int, v_ptr: int, n: int, stream: int = 0) -> None:

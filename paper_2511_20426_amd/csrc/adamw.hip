@@ -9,8 +9,9 @@
 // that the codes are those of exact arithmetic: an estimate in fp32 says between which two codes a value lies, a comparison with the border in 64 bits
 // says which of them it is.
 //
-// A wave takes 512 values at a time, 8 to a lane, 32 lanes to a block.  What tensors there are comes with the launch (40 to one), so that nothing
-// has to be copied ahead of it.  How many steps a tensor has behind it is counted on the device, by a small launch ahead that leaves what the step needs of
+// A wave takes 512 values at a time, 8 to a lane, 32 lanes to a block.  Where the parameters and their states are lies in a table on the device, which the
+// caller keeps; the gradients' addresses come with the launch, 300 to one (with all addresses in the launch it were 40: 120 tensors of 49152 values in
+// fp32 three launches of 17 us and three more that count).  How many steps a tensor has behind it is counted on the device, by a small launch ahead that leaves what the step needs of
 // it, so that a captured step goes on counting in every replay.  (Counted by the workgroup of a tensor that ends last, by a ticket, it was one
 // launch, but each ticket took 40 ns: 3 x 4096 x 1536 values, 4608 workgroups, 289 us.)
 #include <hip/hip_runtime.h>
@@ -24,26 +25,18 @@ namespace {
 
 #include "rope_device.hpp"
 
-constexpr int kMostTensors = 40 /* at most a wave */, kUnit = 512, kWaves = 4;
+constexpr int kMostTensors = 300, kUnit = 512, kWaves = 4;
 
-struct AdamTensor {
-  void* p;
-  const void* g;
-  uint16_t* copy;
-  void* m;
-  void* v;
-  float* m_scale;
-  float* v_scale;
-  int32_t* step;                                  // [0] steps done; [1], [2] lr / (1 - b1^t) and 1 / sqrt(1 - b2^t) in fp32
-  int64_t n;
-  int32_t first, types;                           // workgroup of the launch; bit 0: parameters in bf16, bit 1: gradients
-};
+// a tensor as a workgroup sees it: of the table, whose values all lanes share, so that they come by scalar loads
+typedef const __attribute__((address_space(4))) ca_adamw_tensor* AdamTable;
 
 struct AdamArgs {
+  const ca_adamw_tensor* table;                   // step: [0] steps done; [1], [2] lr / (1 - b1^t) and 1 / sqrt(1 - b2^t) in fp32
   double beta1, beta2, grad_scale;
   float lr, keep, eps;                            // keep: 1 - lr wd
   int32_t tensors, units;                         // units of a workgroup
-  AdamTensor of[kMostTensors];
+  uint64_t grads[kMostTensors];                   // and 1 where they are bf16; 0: the tensor is left out
+  int32_t first[kMostTensors];                    // workgroup of the launch; of a tensor that is left out that of the next one
 };
 static_assert(sizeof(AdamArgs) <= 4096, "a launch's arguments");
 
@@ -177,14 +170,27 @@ __device__ __forceinline__ double power(double x, int n) {
   return r;
 }
 
-__global__ __launch_bounds__(64) void adamw_count_kernel(AdamArgs a) {
-  if (int(threadIdx.x) >= a.tensors) return;
-  int32_t* const step = a.of[threadIdx.x].step;
+__global__ __launch_bounds__(kMostTensors) void adamw_count_kernel(AdamArgs a) {
+  const int i = threadIdx.x;
+  if (i >= a.tensors || a.grads[i] == 0) return;
+  int32_t* const step = a.table[i].step;
   const int now = step[0] + 1;
   step[0] = now;
   step[1] = __float_as_int(float(double(a.lr) / (1. - power(a.beta1, now))));
   step[2] = __float_as_int(float(1. / sqrt(1. - power(a.beta2, now))));
 }
+
+struct AdamTensor {
+  void* p;
+  const void* g;
+  uint16_t* copy;
+  void* m;
+  void* v;
+  float* m_scale;
+  float* v_scale;
+  const int32_t* step;
+  int64_t n;
+};
 
 // units begin + wave, + kWaves .. below end
 template <int kBits, bool kHalfP, bool kHalfG>
@@ -260,12 +266,18 @@ __device__ __forceinline__ void step_units(const AdamArgs& a, const AdamTensor t
 
 template <int kBits>
 __global__ __launch_bounds__(64 * kWaves) void adamw_kernel(AdamArgs a) {
-  int i = 0;
-  while (i + 1 < a.tensors && int(blockIdx.x) >= a.of[i + 1].first) ++i;
-  const AdamTensor t = a.of[i];
-  const int64_t units = (t.n + kUnit - 1) / kUnit, begin = int64_t(int(blockIdx.x) - t.first) * a.units;
+  int i = 0, behind = a.tensors;                  // the last tensor that begins at this workgroup or before
+  while (behind - i > 1) {
+    const int mid = (i + behind) >> 1;
+    if (a.first[mid] <= int(blockIdx.x)) i = mid; else behind = mid;
+  }
+  const AdamTable of = reinterpret_cast<AdamTable>(reinterpret_cast<uintptr_t>(a.table)) + i;
+  const uint64_t grad = a.grads[i];
+  const AdamTensor t{of->param, reinterpret_cast<const void*>(grad & ~uint64_t(1)), static_cast<uint16_t*>(of->copy), of->m, of->v, of->m_scale, of->v_scale,
+                     of->step, of->n};
+  const int64_t units = (t.n + kUnit - 1) / kUnit, begin = int64_t(int(blockIdx.x) - a.first[i]) * a.units;
   const int64_t end = begin + a.units < units ? begin + a.units : units;
-  switch (t.types) {
+  switch ((of->param_dtype == CA_BF16 ? 1 : 0) | (grad & 1 ? 2 : 0)) {
     case 0: return step_units<kBits, false, false>(a, t, begin, end);
     case 1: return step_units<kBits, true, false>(a, t, begin, end);
     case 2: return step_units<kBits, false, true>(a, t, begin, end);
@@ -297,31 +309,28 @@ constexpr int64_t kWorkgroups32 = 65536, kWorkgroups8 = 16384;
 
 }  // namespace
 
-int32_t launch_adamw(const ca_adamw_tensor* tensors, int32_t n_tensors, int32_t state_bits, double lr, double beta1, double beta2, double eps,
-                     double weight_decay, double grad_scale, void* stream) {
-  AdamArgs a{};
+int32_t launch_adamw(const ca_adamw_tensor* tensors, const ca_adamw_tensor* tensors_dev, int32_t n_tensors, int32_t state_bits, double lr, double beta1,
+                     double beta2, double eps, double weight_decay, double grad_scale, void* stream) {
+  AdamArgs a;
   a.beta1 = beta1; a.beta2 = beta2; a.grad_scale = grad_scale;
   a.lr = float(lr); a.keep = float(1. - lr * weight_decay); a.eps = float(eps);
-  for (int32_t from = 0; from < n_tensors;) {
-    int64_t units = 0;
-    int32_t to = from;
-    a.tensors = 0;
-    for (; to < n_tensors && a.tensors < kMostTensors; ++to) {
-      const ca_adamw_tensor& t = tensors[to];
-      if (t.n == 0 || !t.grad) continue;
-      a.of[a.tensors++] = AdamTensor{t.param, t.grad, static_cast<uint16_t*>(t.copy), t.m, t.v, t.m_scale, t.v_scale, t.step, t.n, 0,
-                                     (t.param_dtype == CA_BF16 ? 1 : 0) | (t.grad_dtype == CA_BF16 ? 2 : 0)};
-      units += (t.n + kUnit - 1) / kUnit;
-    }
-    from = to;
-    if (a.tensors == 0) continue;
-    a.units = int32_t(std::max<int64_t>(1, units / (kWaves * (state_bits == 8 ? kWorkgroups8 : kWorkgroups32)))) * kWaves;
-    int32_t workgroups = 0;
+  const int64_t most = kWaves * (state_bits == 8 ? kWorkgroups8 : kWorkgroups32);
+  for (int32_t from = 0; from < n_tensors; from += kMostTensors) {
+    a.table = tensors_dev + from;
+    a.tensors = std::min(n_tensors - from, kMostTensors);
+    int64_t units = 0, workgroups = 0;
+    for (int i = 0; i < a.tensors; ++i)
+      if (const ca_adamw_tensor& t = tensors[from + i]; t.grad) units += (t.n + kUnit - 1) / kUnit;
+    a.units = int32_t(std::max<int64_t>(1, units / most)) * kWaves;
     for (int i = 0; i < a.tensors; ++i) {
-      a.of[i].first = workgroups;
-      workgroups += int32_t(((a.of[i].n + kUnit - 1) / kUnit + a.units - 1) / a.units);
+      const ca_adamw_tensor& t = tensors[from + i];
+      const bool there = t.grad && t.n > 0;
+      a.grads[i] = there ? uint64_t(reinterpret_cast<uintptr_t>(t.grad)) | (t.grad_dtype == CA_BF16 ? 1 : 0) : 0;
+      a.first[i] = int32_t(workgroups);
+      if (there) workgroups += ((t.n + kUnit - 1) / kUnit + a.units - 1) / a.units;
     }
-    hipLaunchKernelGGL(adamw_count_kernel, dim3(1), dim3(64), 0, static_cast<hipStream_t>(stream), a);
+    if (workgroups == 0) continue;
+    hipLaunchKernelGGL(adamw_count_kernel, dim3(1), dim3(kMostTensors), 0, static_cast<hipStream_t>(stream), a);
     if (const int32_t rc = finish_launch("adamw.hip"); rc != CA_OK) return rc;
     hipLaunchKernelGGL(state_bits == 8 ? adamw_kernel<8> : adamw_kernel<32>, dim3(unsigned(workgroups)), dim3(64 * kWaves), 0, static_cast<hipStream_t>(stream), a);
     if (const int32_t rc = finish_launch("adamw.hip"); rc != CA_OK) return rc;

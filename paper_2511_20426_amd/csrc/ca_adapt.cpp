@@ -135,14 +135,14 @@ int32_t layer_linear_adapted_backward_bf16(const void* dy_dev, const void* x_dev
   return ca::launch_adapted_backward(p, dy_dev, lddy, low_dev, rank_used, m_rows > 0 ? dx_dev : nullptr, d_down_dev, d_up_dev, workspace_dev, hip_stream);
 }
 
-int32_t layer_adamw(const ca_adamw_tensor* tensors, int32_t n_tensors, int32_t state_bits, double lr, double beta1, double beta2, double eps,
-                    double weight_decay, double grad_scale, void* hip_stream) {
-  if (n_tensors < 0 || (n_tensors > 0 && !tensors) || (state_bits != 8 && state_bits != 32)) return CA_EINVAL;
+int32_t layer_adamw(const ca_adamw_tensor* tensors, const ca_adamw_tensor* tensors_dev, int32_t n_tensors, int32_t state_bits, double lr, double beta1,
+                    double beta2, double eps, double weight_decay, double grad_scale, void* hip_stream) {
+  if (n_tensors < 0 || (n_tensors > 0 && (!tensors || !tensors_dev)) || !aligned(tensors_dev, 16) || (state_bits != 8 && state_bits != 32)) return CA_EINVAL;
   if (!(lr >= 0.) || !(weight_decay >= 0.) || !(beta1 >= 0. && beta1 < 1.) || !(beta2 >= 0. && beta2 < 1.) || !(float(eps) >= 0x1p-126f)) return CA_EINVAL;
   if (!std::isfinite(float(lr)) || !std::isfinite(lr * weight_decay) || !std::isfinite(float(eps)) || !std::isfinite(float(grad_scale))) return CA_EINVAL;
   for (int32_t i = 0; i < n_tensors; ++i)
     if (int32_t rc = check_adamw(tensors[i], state_bits)) return rc;
-  return ca::launch_adamw(tensors, n_tensors, state_bits, lr, beta1, beta2, eps, weight_decay, grad_scale, hip_stream);
+  return ca::launch_adamw(tensors, tensors_dev, n_tensors, state_bits, lr, beta1, beta2, eps, weight_decay, grad_scale, hip_stream);
 }
 
 int32_t layer_adamw_values(const void* m_codes_dev, const void* v_codes_dev, const float* m_scales_dev, const float* v_scales_dev, float* m_dev,

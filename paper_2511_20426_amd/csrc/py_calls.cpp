@@ -39,6 +39,14 @@ decltype(&layer_gated_saved_bytes) gated_saved_fn = nullptr;
 decltype(&layer_gated_backward_workspace) gated_workspace_fn = nullptr;
 decltype(&layer_gated_backward_bf16) gated_backward_fn = nullptr;
 
+decltype(&layer_norm) row_norm_fn = nullptr;
+decltype(&layer_norm_backward_workspace) row_norm_workspace_fn = nullptr;
+decltype(&layer_norm_backward) row_norm_backward_fn = nullptr;
+decltype(&layer_linear_adapted_bf16) adapted_fn = nullptr;
+decltype(&layer_linear_adapted_backward_workspace) adapted_workspace_fn = nullptr;
+decltype(&layer_linear_adapted_backward_bf16) adapted_backward_fn = nullptr;
+decltype(&layer_adamw) adamw_fn = nullptr;
+
 constexpr int kMaxBlocks = 64;                    // of a call taken here
 
 PyObject* not_taken() { Py_RETURN_NONE; }
@@ -403,6 +411,200 @@ PyObject* gated_backward(PyObject* const* a, Py_ssize_t n) {
   return tuple({THPVariable_Wrap(dx), THPVariable_Wrap(dw[0]), THPVariable_Wrap(dw[1])});
 }
 
+// a [rows, cols] matrix of any alignment and row stride
+bool rows_of(const at::Tensor* t, at::ScalarType type, int64_t rows, int64_t cols, const at::Tensor& like, int64_t* ld) {
+  if (!t || t->scalar_type() != type || t->dim() != 2 || t->size(0) != rows || t->size(1) != cols || (cols > 1 && t->stride(1) != 1) || !beside(*t, like))
+    return false;
+  *ld = rows > 1 ? t->stride(0) : cols;
+  return true;
+}
+bool stored(const at::Tensor& t, int32_t* dtype) {
+  *dtype = t.scalar_type() == at::kFloat ? CA_F32 : CA_BF16;
+  return t.scalar_type() == at::kFloat || t.scalar_type() == at::kBFloat16;
+}
+// launches go to the current device: other ones are left to the Python code
+bool here(const at::Tensor& t) { return t.is_cuda() && t.device().index() == c10::hip::current_device(); }
+
+struct RowNormCall {                              // x, weight, bias
+  const at::Tensor *x, *w[2] = {nullptr, nullptr};
+  int64_t rows, width, groups = 1, ldx, ldw;
+  int32_t dtype, w_dtype = CA_F32;
+  bool take(PyObject* const* a) {
+    x = plain(a[0]);
+    if (!x || x->dim() != 2 || !here(*x) || !stored(*x, &dtype)) return false;
+    rows = x->size(0), width = ldw = x->size(1);
+    if (width != int32_t(width) || width < 1 || !rows_of(x, x->scalar_type(), rows, width, *x, &ldx)) return false;
+    const at::Tensor* like = nullptr;
+    for (int i = 0; i < 2; ++i) {
+      if (a[1 + i] == Py_None) continue;
+      const at::Tensor* t = w[i] = plain(a[1 + i]);
+      if (!t || !beside(*t, *x) || !stored(*t, &w_dtype) || (t->scalar_type() != at::kFloat && t->scalar_type() != x->scalar_type()) || t->dim() < 1 ||
+          t->dim() > 2 || t->size(-1) != width || (width > 1 && t->stride(-1) != 1) ||
+          (like && (t->scalar_type() != like->scalar_type() || t->sizes() != like->sizes() || t->strides() != like->strides())))
+        return false;
+      like = t;
+      groups = t->dim() == 2 ? t->size(0) : 1;
+      ldw = groups > 1 ? t->stride(0) : width;
+    }
+    return groups >= 1 && rows % groups == 0;
+  }
+  const void* weight(int i) const { return w[i] ? w[i]->data_ptr() : nullptr; }
+  void* stream() const { return c10::hip::getCurrentHIPStream(x->device().index()).stream(); }
+};
+
+// layer_norm(x, weight, bias, eps, out)
+PyObject* layer_norm_(PyObject* const* a, Py_ssize_t n) {
+  RowNormCall c;
+  Result r;
+  float eps;
+  int64_t ldy;
+  if (n != 5 || !c.take(a) || !real(a[3], &eps) || !r.take(a[4])) return not_taken();
+  const at::Tensor& y = r.or_empty({c.rows, c.width}, *c.x);
+  if (!rows_of(&y, c.x->scalar_type(), c.rows, c.width, *c.x, &ldy)) return not_taken();
+  const void *const xp = c.x->data_ptr(), *const wp = c.weight(0), *const bp = c.weight(1);
+  void *const yp = y.data_ptr(), *const stream = c.stream();
+  return r.give(released([&] { return row_norm_fn(xp, c.dtype, wp, bp, c.w_dtype, eps, yp, c.rows, int32_t(c.width), c.groups, c.ldx, c.ldw, ldy, stream); }));
+}
+
+// layer_norm_backward(x, weight, bias, dy, eps, dx) -> (dx, dweight, dbias)
+PyObject* layer_norm_backward_(PyObject* const* a, Py_ssize_t n) {
+  RowNormCall c;
+  Result r;
+  float eps;
+  int64_t lddy, lddx;
+  if (n != 6 || !c.take(a) || !real(a[4], &eps) || !r.take(a[5])) return not_taken();
+  const at::Tensor* dy = plain(a[3]);
+  if (!rows_of(dy, c.x->scalar_type(), c.rows, c.width, *c.x, &lddy)) return not_taken();
+  const at::Tensor& dx = r.or_empty({c.rows, c.width}, *c.x);
+  if (!rows_of(&dx, c.x->scalar_type(), c.rows, c.width, *c.x, &lddx)) return not_taken();
+  const auto single = c.x->options().dtype(at::kFloat);
+  at::Tensor grads[2], work;
+  float* to[2] = {nullptr, nullptr};
+  for (int i = 0; i < 2; ++i)
+    if (c.w[i]) {
+      grads[i] = at::empty(c.w[i]->sizes(), single);
+      to[i] = grads[i].data_ptr<float>();
+    }
+  const size_t bytes = row_norm_workspace_fn(c.rows, int32_t(c.width), c.groups);
+  work = at::empty({int64_t(bytes)}, c.x->options().dtype(at::kByte));
+  const void *const xp = c.x->data_ptr(), *const wp = c.weight(0), *const dyp = dy->data_ptr();
+  void *const dxp = dx.data_ptr(), *const workp = work.data_ptr(), *const stream = c.stream();
+  const int32_t rc = released([&] {
+    return row_norm_backward_fn(dyp, xp, c.dtype, wp, c.w_dtype, eps, dxp, to[0], to[1], c.rows, int32_t(c.width), c.groups, lddy, c.ldx, c.ldw, lddx, workp, bytes,
+                                stream);
+  });
+  if (rc != CA_OK) return PyLong_FromLong(rc);
+  return tuple({r.give(rc), c.w[0] ? THPVariable_Wrap(grads[0]) : none(), c.w[1] ? THPVariable_Wrap(grads[1]) : none()});
+}
+
+struct AdaptedCall {                              // x, down, up, scales, index
+  const at::Tensor *x, *down, *up, *scales, *index;
+  int64_t m, n, k, adapters, rank, ldx;
+  bool take(PyObject* const* a) {
+    const at::Tensor** const to[] = {&x, &down, &up, &scales, &index};
+    for (int i = 0; i < 5; ++i)
+      if (!(*to[i] = plain(a[i]))) return false;
+    if (!here(*x) || x->dim() != 2 || down->dim() != 3 || up->dim() != 3) return false;
+    m = x->size(0), k = x->size(1), n = up->size(1), adapters = down->size(0), rank = down->size(1);
+    for (const at::Tensor* t : {down, up, scales, index})
+      if (!beside(*t, *x) || !t->is_contiguous()) return false;
+    return n == int32_t(n) && k == int32_t(k) && adapters == int32_t(adapters) && rank == int32_t(rank) && matrix(x, at::kBFloat16, m, k, *x, &ldx) &&
+           down->scalar_type() == at::kBFloat16 && up->scalar_type() == at::kBFloat16 && down->size(2) == k && up->size(0) == adapters && up->size(2) == rank &&
+           scales->scalar_type() == at::kFloat && scales->dim() == 1 && scales->size(0) == adapters && index->scalar_type() == at::kInt && index->dim() == 1 &&
+           index->size(0) == m;
+  }
+  void* stream() const { return c10::hip::getCurrentHIPStream(x->device().index()).stream(); }
+};
+
+// linear_adapted(x, down, up, scales, index, w, out) -> (y, low)
+PyObject* linear_adapted(PyObject* const* a, Py_ssize_t n) {
+  AdaptedCall c;
+  Result r;
+  int64_t ldw, ldy;
+  if (n != 7 || !c.take(a) || !r.take(a[6])) return not_taken();
+  const at::Tensor* w = plain(a[5]);
+  if (!matrix(w, at::kBFloat16, c.n, c.k, *c.x, &ldw)) return not_taken();
+  const at::Tensor& y = r.or_empty({c.m, c.n}, *c.x);
+  if (!matrix(&y, at::kBFloat16, c.m, c.n, *c.x, &ldy)) return not_taken();
+  const at::Tensor low = at::empty({c.m, c.rank}, c.x->options());
+  const void *const xp = c.x->data_ptr(), *const wp = w->data_ptr(), *const dp = c.down->data_ptr(), *const up = c.up->data_ptr();
+  const float* const sp = c.scales->data_ptr<float>();
+  const int32_t* const ip = c.index->data_ptr<int32_t>();
+  void *const lp = low.data_ptr(), *const yp = y.data_ptr(), *const stream = c.stream();
+  const int32_t rc = released([&] {
+    return adapted_fn(xp, wp, dp, up, sp, ip, lp, yp, c.m, int32_t(c.n), int32_t(c.k), int32_t(c.adapters), int32_t(c.rank), c.ldx, ldw, ldy, stream);
+  });
+  return rc != CA_OK ? PyLong_FromLong(rc) : tuple({r.give(rc), THPVariable_Wrap(low)});
+}
+
+// linear_adapted_backward(x, down, up, scales, index, dy, w_t, saved, rank) -> (dx, d_down, d_up)
+PyObject* linear_adapted_backward(PyObject* const* a, Py_ssize_t n) {
+  AdaptedCall c;
+  int64_t lddy, ldw, used;
+  if (n != 9 || !c.take(a) || !whole(a[8], &used) || used < 1 || used > c.rank) return not_taken();
+  const at::Tensor *dy = plain(a[5]), *w = a[6] == Py_None ? nullptr : plain(a[6]), *saved = plain(a[7]);
+  ldw = c.n;
+  if (!matrix(dy, at::kBFloat16, c.m, c.n, *c.x, &lddy) || (a[6] != Py_None && !matrix(w, at::kBFloat16, c.k, c.n, *c.x, &ldw)) || !saved ||
+      saved->scalar_type() != at::kBFloat16 || saved->dim() != 2 || saved->size(0) != c.m || saved->size(1) != c.rank || !saved->is_contiguous() ||
+      !beside(*saved, *c.x))
+    return not_taken();
+  const size_t bytes = adapted_workspace_fn(c.m, int32_t(c.n), int32_t(c.k), int32_t(c.adapters), int32_t(c.rank));
+  at::Tensor dx;
+  if (w) dx = at::empty({c.m, c.k}, c.x->options());
+  const at::Tensor d_down = at::empty({c.adapters, used, c.k}, c.x->options()), d_up = at::empty({c.adapters, c.n, used}, c.x->options()),
+                   work = at::empty({int64_t(bytes)}, c.x->options().dtype(at::kByte));
+  const void *const xp = c.x->data_ptr(), *const wp = w ? w->data_ptr() : nullptr, *const dp = c.down->data_ptr(), *const up = c.up->data_ptr(),
+             *const dyp = dy->data_ptr(), *const lp = saved->data_ptr();
+  const float* const sp = c.scales->data_ptr<float>();
+  const int32_t* const ip = c.index->data_ptr<int32_t>();
+  void *const dxp = w ? dx.data_ptr() : nullptr, *const ddp = d_down.data_ptr(), *const dup = d_up.data_ptr(), *const workp = work.data_ptr(), *const stream = c.stream();
+  const int32_t rc = released([&] {
+    return adapted_backward_fn(dyp, xp, wp, dp, up, sp, ip, lp, dxp, ddp, dup, c.m, int32_t(c.n), int32_t(c.k), int32_t(c.adapters), int32_t(c.rank), int32_t(used),
+                               lddy, c.ldx, ldw, c.k, workp, bytes, stream);
+  });
+  if (rc != CA_OK) return PyLong_FromLong(rc);
+  return tuple({w ? THPVariable_Wrap(dx) : none(), THPVariable_Wrap(d_down), THPVariable_Wrap(d_up)});
+}
+
+// adamw(address of the tensors, their table on the device, params, grads, state_bits, lr, (beta1, beta2), eps, weight_decay, grad_scale)
+PyObject* adamw(PyObject* const* a, Py_ssize_t n) {
+  int64_t at_host;
+  int32_t bits;
+  double v[4], betas[2];
+  if (n != 10 || !whole(a[0], &at_host) || at_host == 0 || !whole32(a[4], &bits) || !PyTuple_CheckExact(a[6]) || PyTuple_GET_SIZE(a[6]) != 2) return not_taken();
+  PyObject* const numbers[] = {a[5], a[7], a[8], a[9]};
+  for (int i = 0; i < 4; ++i) {
+    if (!PyFloat_CheckExact(numbers[i])) return not_taken();
+    v[i] = PyFloat_AS_DOUBLE(numbers[i]);
+  }
+  for (int i = 0; i < 2; ++i) {
+    PyObject* const o = PyTuple_GET_ITEM(a[6], i);
+    if (!PyFloat_CheckExact(o)) return not_taken();
+    betas[i] = PyFloat_AS_DOUBLE(o);
+  }
+  const at::Tensor* table = plain(a[1]);
+  if (!table || !here(*table) || !PyList_CheckExact(a[2]) || (!PyList_CheckExact(a[3]) && !PyTuple_CheckExact(a[3]))) return not_taken();
+  const Py_ssize_t count = PyList_GET_SIZE(a[2]);
+  if (PySequence_Fast_GET_SIZE(a[3]) != count || size_t(table->numel()) != size_t(count) * sizeof(ca_adamw_tensor)) return not_taken();
+  ca_adamw_tensor* const tensors = reinterpret_cast<ca_adamw_tensor*>(at_host);
+  PyObject** const grads = PySequence_Fast_ITEMS(a[3]);
+  for (Py_ssize_t i = 0; i < count; ++i) {
+    const at::Tensor* p = plain(PyList_GET_ITEM(a[2], i));
+    if (!p || p->data_ptr() != tensors[i].param) return not_taken();
+    if (grads[i] == Py_None) {
+      tensors[i].grad = nullptr;
+      continue;
+    }
+    const at::Tensor* g = plain(grads[i]);
+    if (!g || !beside(*g, *p) || g->sizes() != p->sizes() || !g->is_contiguous() || !stored(*g, &tensors[i].grad_dtype)) return not_taken();
+    tensors[i].grad = g->data_ptr();
+  }
+  const ca_adamw_tensor* const on_device = static_cast<const ca_adamw_tensor*>(table->data_ptr());
+  void* const stream = c10::hip::getCurrentHIPStream(table->device().index()).stream();
+  // (the lock is held: the tensors are the optimizer's, and another thread's call would write them)
+  return PyLong_FromLong(adamw_fn(tensors, on_device, int32_t(count), bits, v[0], betas[0], betas[1], v[1], v[2], v[3], stream));
+}
+
 // rope(handle, shape, x, first_frame, out)
 PyObject* rope(PyObject* const* a, Py_ssize_t n) {
   Pool p;
@@ -531,10 +733,35 @@ PyObject* bind_layer(PyObject* const* a, Py_ssize_t n) {
   Py_RETURN_NONE;
 }
 
+// bind_adapt(addresses of the seven entry points of the operators that a layer is adapted with in the order above)
+PyObject* bind_adapt(PyObject* const* a, Py_ssize_t n) {
+  int64_t f[7];
+  if (n != 7) {
+    PyErr_SetString(PyExc_TypeError, "seven addresses");
+    return nullptr;
+  }
+  for (int i = 0; i < 7; ++i)
+    if (!whole(a[i], f + i) || f[i] == 0) {
+      PyErr_SetString(PyExc_TypeError, "an address is an int");
+      return nullptr;
+    }
+  row_norm_fn = reinterpret_cast<decltype(row_norm_fn)>(f[0]);
+  row_norm_workspace_fn = reinterpret_cast<decltype(row_norm_workspace_fn)>(f[1]);
+  row_norm_backward_fn = reinterpret_cast<decltype(row_norm_backward_fn)>(f[2]);
+  adapted_fn = reinterpret_cast<decltype(adapted_fn)>(f[3]);
+  adapted_workspace_fn = reinterpret_cast<decltype(adapted_workspace_fn)>(f[4]);
+  adapted_backward_fn = reinterpret_cast<decltype(adapted_backward_fn)>(f[5]);
+  adamw_fn = reinterpret_cast<decltype(adamw_fn)>(f[6]);
+  Py_RETURN_NONE;
+}
+
 #define METHOD(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(&guarded<name>)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {METHOD(linear), METHOD(append_batch), METHOD(rope), METHOD(forward), METHOD(forward_rope), METHOD(qkv_publish),
                          METHOD(append_batch_norm), METHOD(norm_rope), METHOD(norm_rope_backward), METHOD(linear_i8), METHOD(gated),
-                         METHOD(gated_backward), METHOD(bind), METHOD(bind_layer), {nullptr, nullptr, 0, nullptr}};
+                         METHOD(gated_backward), METHOD(linear_adapted), METHOD(linear_adapted_backward), METHOD(adamw),
+                         {"layer_norm", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(&guarded<layer_norm_>)), METH_FASTCALL, nullptr},
+                         {"layer_norm_backward", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(&guarded<layer_norm_backward_>)), METH_FASTCALL, nullptr},
+                         METHOD(bind), METHOD(bind_layer), METHOD(bind_adapt), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_calls", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -52,20 +52,27 @@ class AdamW:
             t.m, t.v, t.step = self.m.data_ptr() + at * size, self.v.data_ptr() + at * size, self._steps.data_ptr() + 16 * i
             if state_bits == 8:
                 t.m_scale, t.v_scale = self.m_scale.data_ptr() + at // _BLOCK * 4, self.v_scale.data_ptr() + at // _BLOCK * 4
+        self._table = torch.frombuffer(bytearray(bytes(self._tensors)), dtype=torch.uint8).to(device)
+        self._host = C.addressof(self._tensors)
 
     def step(self, grads: Sequence[torch.Tensor | None], grad_scale: float = 1.0) -> None:
         """One step by the gradients, each of its parameter's shape, packed, bf16 or fp32, or None: that tensor and its state stay as they are.
         grad_scale: what they are multiplied with first."""
+        r = B.calls.adamw(self._host, self._table, self.params, grads, self.state_bits, self.lr, self.betas, self.eps, self.weight_decay, grad_scale)
+        if r is not None:
+            B._check(r, "layer_adamw")
+            return
         assert len(grads) == len(self.params)
         for t, p, g in zip(self._tensors, self.params, grads):
+            assert p.data_ptr() == (t.param or 0), "a parameter has moved"
             if g is None:
                 t.grad = None
                 continue
             assert g.device == self.device and g.dtype in _TYPES and g.shape == p.shape and g.is_contiguous()
             t.grad, t.grad_dtype = g.data_ptr(), _TYPES[g.dtype]
         with _on_device(self.device):
-            B.layer_adamw(self._tensors, len(self._tensors), self.state_bits, self.lr, *self.betas, self.eps, self.weight_decay, grad_scale,
-                          _current_stream(self.device))
+            B.layer_adamw(self._tensors, self._table.data_ptr(), len(self._tensors), self.state_bits, self.lr, *self.betas, self.eps, self.weight_decay,
+                          grad_scale, _current_stream(self.device))
 
     def state_values(self) -> tuple[torch.Tensor, torch.Tensor]:
         """m and v of all tensors in fp32, those of tensor i from offsets[i] on: the states themselves, or what their codes stand for."""

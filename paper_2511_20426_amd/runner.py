@@ -476,6 +476,11 @@ def layer_norm(x: torch.Tensor, weight: torch.Tensor | None = None, bias: torch.
     """y = weight * (x - mean) / sqrt(mean((x - mean)^2) + eps) + bias of each row: x [M, W] in bf16 or fp32, rows may be strided; weight and bias (either
     or both may be None) [W], or [G, W] for G equal runs of consecutive rows, as the blocks in flight are (modulation by the timestep: 1 + scale
     and shift), of x's type or fp32, with the same strides.  out may be x."""
+    r = B.calls.layer_norm(x, weight, bias, eps, out)
+    if r.__class__ is int:
+        B._check(r, "layer_norm")
+    if r is not None:
+        return r
     assert x.is_cuda and x.dtype in _TYPES and x.dim() == 2
     m, width = x.shape
     w_type, groups, ldw = _norm_weights(x, weight, bias)
@@ -492,6 +497,11 @@ def layer_norm_backward(dy: torch.Tensor, x: torch.Tensor, weight: torch.Tensor 
                         dx: torch.Tensor | None = None):
     """Gradients of layer_norm: (dx, dweight, dbias) from that of its result and its arguments, the weights' in fp32 and of the weights' shapes (None for
     those that are None).  dx may be dy."""
+    r = B.calls.layer_norm_backward(x, weight, bias, dy, eps, dx)
+    if r.__class__ is int:
+        B._check(r, "layer_norm_backward")
+    if r is not None:
+        return r
     assert x.is_cuda and x.dtype in _TYPES and x.dim() == 2
     m, width = x.shape
     w_type, groups, ldw = _norm_weights(x, weight, bias)
@@ -535,6 +545,11 @@ class Adapters:
 
 def linear_adapted_train(x: torch.Tensor, w: torch.Tensor, adapters: Adapters, index: torch.Tensor, out: torch.Tensor | None = None):
     """linear_adapted for training: (y, saved), saved being what linear_adapted_backward takes (scales[g] * x @ down[g].T in bf16)."""
+    r = B.calls.linear_adapted(x, adapters.down, adapters.up, adapters.scales, index, w, out)
+    if r.__class__ is int:
+        B._check(r, "layer_linear_adapted_bf16")
+    if r is not None:
+        return r
     assert x.is_cuda and x.dim() == 2 and w.dim() == 2
     (m, k), n, device = x.shape, w.shape[0], x.device
     g, rank, _ = adapters.down.shape
@@ -559,6 +574,11 @@ def linear_adapted(x: torch.Tensor, w: torch.Tensor, adapters: Adapters, index: 
 def linear_adapted_backward(dy: torch.Tensor, x: torch.Tensor, w_t: torch.Tensor | None, adapters: Adapters, index: torch.Tensor, saved: torch.Tensor):
     """(dx, d_down, d_up) from the gradient dy [M, N] of linear_adapted_train's y, its arguments and what it saved; the weights are frozen, and w_t [K, N] is they
     transposed, laid out once (None: dx is not asked for).  d_down [G, r, K] and d_up [G, N, r] in bf16, r the adapters' own rank."""
+    r = B.calls.linear_adapted_backward(x, adapters.down, adapters.up, adapters.scales, index, dy, w_t, saved, adapters.rank)
+    if r.__class__ is int:
+        B._check(r, "layer_linear_adapted_backward_bf16")
+    if r is not None:
+        return r
     assert x.is_cuda and x.dim() == 2 and dy.dim() == 2
     (m, k), n, device = x.shape, dy.shape[1], x.device
     g, rank, _ = adapters.down.shape
