@@ -234,7 +234,7 @@ template <typename T, typename W, int kWaves, int kPieces, bool kWhole>
 __global__ __launch_bounds__(kWaves == 1 ? 256 : 64 * kWaves) void layer_norm_backward_kernel(RowNormArgs a) {
   using Shape = RowShape<kWaves, kPieces, kWhole>;
   __shared__ float2 room[3 * kWaves];
-  __shared__ float sums[kWaves == 1 ? 2 : 1][kWaves == 1 ? 512 * kPieces : 1];
+  __shared__ float sums[kWaves == 1 ? 2 : 1][kWaves == 1 ? 2 : 1][kWaves == 1 ? 512 * kPieces : 1];
   const int t = threadIdx.x % Shape::kThreads;
   const int group = blockIdx.x / unsigned(a.per_group), nth = blockIdx.x - group * a.per_group;
   const int64_t first = int64_t(group) * a.group_rows;
@@ -245,14 +245,26 @@ __global__ __launch_bounds__(kWaves == 1 ? 256 : 64 * kWaves) void layer_norm_ba
   for (int i = 0; i < kPieces; ++i)
 #pragma unroll
     for (int j = 0; j < 8; ++j) dw[i][j] = db[i][j] = 0.f;
-  for (int64_t n = int64_t(nth) * Shape::kRows + threadIdx.x / Shape::kThreads; n < a.group_rows; n += int64_t(a.per_group) * Shape::kRows) {
+  // A wave asks for its next row ahead of the work on one (4680 x 1536 22.3 -> 19.1 us with 256 workgroups); rows of several waves are not: the registers
+  // cost them a workgroup of four on a CU (23400 x 5120 185 us, 222 so)
+  constexpr bool kNext = kWaves == 1;
+  Piece<T> next_x[kPieces], next_d[kPieces];
+  auto request = [&](int64_t n) {
     const T* const row = static_cast<const T*>(a.x) + (first + n) * a.ldx;
     const T* const drow = static_cast<const T*>(a.dy) + (first + n) * a.lddy;
+#pragma unroll
+    for (int i = 0; i < kPieces; ++i) load_piece<Shape, kWhole>(next_x[i], row, Shape::at(t, i), a.width);
+#pragma unroll
+    for (int i = 0; i < kPieces; ++i) load_piece<Shape, kWhole>(next_d[i], drow, Shape::at(t, i), a.width);
+  };
+  const int64_t begin = int64_t(nth) * Shape::kRows + threadIdx.x / Shape::kThreads, step = int64_t(a.per_group) * Shape::kRows;
+  if (kNext && begin < a.group_rows) request(begin);
+  for (int64_t n = begin; n < a.group_rows; n += step) {
+    if (!kNext) request(n);
     Piece<T> x[kPieces], d[kPieces];
 #pragma unroll
-    for (int i = 0; i < kPieces; ++i) load_piece<Shape, kWhole>(x[i], row, Shape::at(t, i), a.width);
-#pragma unroll
-    for (int i = 0; i < kPieces; ++i) load_piece<Shape, kWhole>(d[i], drow, Shape::at(t, i), a.width);
+    for (int i = 0; i < kPieces; ++i) x[i] = next_x[i], d[i] = next_d[i];
+    if (kNext && n + step < a.group_rows) request(n + step);
     const RowStats s = row_stats<Shape, kWaves, kPieces, kWhole>(x, t, a.width, per, a.eps, room);
     float sum = 0.f, dot = 0.f;
 #pragma unroll
@@ -287,25 +299,37 @@ __global__ __launch_bounds__(kWaves == 1 ? 256 : 64 * kWaves) void layer_norm_ba
   // one workgroup to a group: the gradients themselves; several: a part of them
   const int64_t part = a.per_group > 1 ? int64_t(blockIdx.x) * 2 * a.width : int64_t(group) * a.width;
   float* const to[2] = {a.dw ? a.dw + part : nullptr, a.db ? a.db + part : nullptr};
-  if constexpr (kWaves == 1) {                                      // the four waves' sums, one behind the other
-    for (int wave = 0; wave < 4; ++wave) {
-      if (int(threadIdx.x >> 6) == wave) {
+  if constexpr (kWaves == 1) {                                      // four waves' sums: those of two go to the other two, then one's to the other
+    const int wave = threadIdx.x >> 6;
+#pragma unroll
+    for (int half = 2; half > 0; half /= 2) {
+      if (wave >= half && wave < 2 * half) {
 #pragma unroll
         for (int i = 0; i < kPieces; ++i)
 #pragma unroll
-          for (int j = 0; j < 8; ++j) {
-            const int at = (i * 8 + j) * 64 + t;                    // (a place of its own to each, of whatever column)
-            sums[0][at] = (wave ? sums[0][at] : 0.f) + dw[i][j];
-            sums[1][at] = (wave ? sums[1][at] : 0.f) + db[i][j];
-          }
+          for (int j = 0; j < 8; ++j) sums[wave - half][0][(i * 8 + j) * 64 + t] = dw[i][j], sums[wave - half][1][(i * 8 + j) * 64 + t] = db[i][j];
+      }
+      __syncthreads();
+      if (wave < half) {
+#pragma unroll
+        for (int i = 0; i < kPieces; ++i)
+#pragma unroll
+          for (int j = 0; j < 8; ++j) dw[i][j] += sums[wave][0][(i * 8 + j) * 64 + t], db[i][j] += sums[wave][1][(i * 8 + j) * 64 + t];
       }
       __syncthreads();
     }
-    for (int k = threadIdx.x; k < 512 * kPieces; k += 256) {
+    if (wave == 0) {
+#pragma unroll
+      for (int i = 0; i < kPieces; ++i)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) sums[0][0][(i * 8 + j) * 64 + t] = dw[i][j], sums[0][1][(i * 8 + j) * 64 + t] = db[i][j];
+    }
+    __syncthreads();
+    for (int k = threadIdx.x; k < 512 * kPieces; k += 256) {        // (a place of its own to each, of whatever column)
       const int lane = k % 64, i = k / 512, j = k / 64 % 8, col = Shape::at(lane, i) + j * Shape::kStep;
       if (col >= a.width) continue;
-      if (to[0]) to[0][col] = sums[0][k];
-      if (to[1]) to[1][col] = sums[1][k];
+      if (to[0]) to[0][col] = sums[0][0][k];
+      if (to[1]) to[1][col] = sums[0][1][k];
     }
   } else {
 #pragma unroll
@@ -320,9 +344,9 @@ __global__ __launch_bounds__(kWaves == 1 ? 256 : 64 * kWaves) void layer_norm_ba
   }
 }
 
-// dw and db [group][width] from the workgroups' parts [group][n][2][width]: 16 columns of one of them to a workgroup, its 16 rows of threads
+// dw and db [group][width] from the workgroups' parts [group][n][2][width]: 32 columns (a line) of one of them to a workgroup, its 32 rows of threads
 // share the parts
-constexpr int kSumCols = 16, kSumRows = 16;
+constexpr int kSumCols = 32, kSumRows = 32;
 __global__ __launch_bounds__(kSumCols * kSumRows) void layer_norm_sum_kernel(const float* parts, int n, int width, int columns, float* dw, float* db) {
   __shared__ double sums[kSumRows][kSumCols + 1];
   const int x = threadIdx.x % kSumCols, y = threadIdx.x / kSumCols;
@@ -392,7 +416,11 @@ int per_group(int64_t group_rows, int64_t groups, int width, int all) {
   const int64_t rows = row_waves(width) == 1 ? 4 : 1, most = (group_rows + rows - 1) / rows;
   return int(std::max<int64_t>(1, std::min(most, (all + groups - 1) / groups)));
 }
-constexpr int kForwardGroups = 2048, kBackwardGroups = 512;
+constexpr int kForwardGroups = 2048;
+// ... of a backward launch, each of which leaves its part of the weights' gradients for the second launch to read.  Us of both with 256 / 512 / 1024 in
+// bf16: 4680 x 1536 17.8 / 18.8 / 32, 23400 x 1536 51 / 44.5 / 55, rows of several waves 4680 x 5120 63 / 52 / 69, 23400 x 5120 in five groups
+// 274 / 185 / 188 (3.9 TB/s: each row waits for three sums over its waves).
+int backward_groups(int64_t rows, int width) { return row_waves(width) == 1 && rows * width <= (int64_t(1) << 24) ? 256 : 512; }
 
 bool aligned(const void* p, int64_t ld, int64_t rows, int bytes_of_value) {
   return reinterpret_cast<uintptr_t>(p) % 16 == 0 && (rows <= 1 || ld * bytes_of_value % 16 == 0);
@@ -417,7 +445,7 @@ int32_t launch_layer_norm(const RowNorm& n, const void* y, void* stream) {
 }
 
 size_t layer_norm_backward_bytes(int64_t rows, int32_t width, int64_t groups) {
-  const int parts = rows > 0 ? per_group(rows / groups, groups, width, kBackwardGroups) : 1;
+  const int parts = rows > 0 ? per_group(rows / groups, groups, width, backward_groups(rows, width)) : 1;
   return parts > 1 ? size_t(groups) * parts * 2 * width * sizeof(float) : 0;
 }
 
@@ -434,7 +462,7 @@ int32_t launch_layer_norm_backward(const RowNorm& n, const void* dy, int64_t ldd
   a.x = n.x; a.dy = dy; a.w = n.w; a.y = dx;
   a.ldx = n.ldx; a.lddy = lddy; a.ldy = n.ldy; a.ldw = n.ldw;
   a.width = n.width; a.groups = int32_t(n.groups); a.group_rows = int32_t(n.rows / n.groups); a.eps = n.eps;
-  a.per_group = per_group(a.group_rows, n.groups, n.width, kBackwardGroups);
+  a.per_group = per_group(a.group_rows, n.groups, n.width, backward_groups(n.rows, n.width));
   float* const parts = static_cast<float*>(workspace);
   const bool split = a.per_group > 1;
   if (dw) a.dw = split ? parts : dw;
