@@ -21,6 +21,7 @@ namespace {
 #include "gemm_tiles.hpp"
 #include "gemm_tile_kernel.hpp"
 #include "gemm_ops.hpp"
+#include "gemm_rows_adapted_clobbers.inc"
 
 using Frag = Bf16Products::Frag;
 using Sums = Bf16Products::Sums;
@@ -245,6 +246,72 @@ __global__ __launch_bounds__(T::kThreads) void gemm_adapted_kernel(AdaptedArgs a
   for (int row = tid / kChunks; row < BM; row += kRows) {
     const u32x4 v = *reinterpret_cast<const u32x4*>(lds + row * T::kPitch + c * 16);
     if (m0 + row < a.M && n0 + c * 8 < a.N) __builtin_nontemporal_store(v, reinterpret_cast<u32x4*>(a.y + int64_t(m0 + row) * a.ldy + n0 + c * 8));
+  }
+}
+
+// Tiles of 256 columns of W: the kernel around the assembly that gen_gemm_rows.py emits for it, which documents the pipeline, the register map and how
+// the adapters join a tile's sums before they leave.  The dealing of tiles and the lanes' parts in loads and reads are those of gemm_rows.hip.
+constexpr int kRowsLds = 160 * 1024;              // 3 stages of W, 2 of X
+constexpr int kFormThrough = 1, kFormPast = 2;    // results written through L2, past the caches; 0: left in L2
+constexpr int kList = 64;                         // tiles of a workgroup: one to a lane
+
+struct AdaptedRowsArgs {
+  AdaptedArgs a;
+  int32_t rank;
+};
+
+template <int kMt>
+__global__ __launch_bounds__(256, 1) void gemm_adapted_rows_kernel(AdaptedRowsArgs args) {
+  constexpr int kTileRows = 32 * kMt, kWaveRows = 16 * kMt, kTileCols = 256;
+  extern __shared__ __attribute__((aligned(1024))) uint8_t lds[];
+  const AdaptedArgs& a = args.a;
+  const int tid = threadIdx.x, lane = tid & 63, l15 = lane & 15, grp = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int wm = wave & 1, wn = wave >> 1;
+  // ---- this workgroup's tiles, one to a lane
+  const int xcd = int(blockIdx.x & 7), j = int(blockIdx.x >> 3) & 31, first = int(blockIdx.x >> 8) * kList;
+  const int total = a.tiles_m * a.tiles_n, full = total >> 8, left = total & 255, share = last_round_share(left);
+  const int mine = full + (j < share && xcd * share + j < left ? 1 : 0);
+  const int tiles = min(mine - first, kList);
+  if (tiles <= 0) return;
+  const int r = min(first + lane, mine - 1);
+  int list_m, list_n;
+  tile_at(a.tiles_m, a.tiles_n, r < full ? r * 256 + xcd * 32 + j : full * 256 + xcd * share + j, &list_m, &list_n);
+
+  const int roww = wave * 64 + (lane >> 3), rowx = wave * 8 * kMt + (lane >> 3);
+  const int chunkw = ((lane & 7) ^ ((lane >> 4) & 1)) * 16, chunkx = ((lane & 7) ^ (lane >> 4)) * 16;
+  const int aw0 = (wn * 128 + 8 * (l15 >> 2) + (l15 & 3)) * 128 + ((grp ^ (l15 >> 1)) << 4);
+  const int ax0 = (wm * kWaveRows + l15) * 128 + ((grp ^ (l15 >> 1)) << 4);
+  const int row = wm * kWaveRows + (l15 & 7), col = wn * 128 + 32 * (l15 >> 3) + 8 * grp;
+  const uint64_t ylane = uint64_t(row) * uint64_t(a.ldy) * 2 + uint64_t(col) * 2;
+  const uint64_t x = reinterpret_cast<uint64_t>(a.x), w = reinterpret_cast<uint64_t>(a.w), y = reinterpret_cast<uint64_t>(a.y);
+  const uint64_t tile_y = uint64_t(a.ldy) * 2 * kTileRows, row8 = uint64_t(a.ldy) * 2 * 8;
+  const uint64_t low = reinterpret_cast<uint64_t>(a.t), up = reinterpret_cast<uint64_t>(a.up), index = reinterpret_cast<uint64_t>(a.index);
+  const uint32_t ldw2 = uint32_t(a.ldw) * 2, ldx2 = uint32_t(a.ldx) * 2;        // below 2^23
+  const uint32_t lds0 = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(lds));
+#define CA_GEMM_ADAPTED_OPERANDS                                                                                       \
+  [x_lo] "s"(uint32_t(x)), [x_hi] "s"(uint32_t(x >> 32)), [w_lo] "s"(uint32_t(w)), [w_hi] "s"(uint32_t(w >> 32)),      \
+      [y_lo] "s"(uint32_t(y)), [y_hi] "s"(uint32_t(y >> 32)), [tile_x] "s"(ldx2 * kTileRows),                          \
+      [tile_w] "s"(ldw2 * kTileCols), [tile_y_lo] "s"(uint32_t(tile_y)), [tile_y_hi] "s"(uint32_t(tile_y >> 32)),      \
+      [row8_lo] "s"(uint32_t(row8)), [row8_hi] "s"(uint32_t(row8 >> 32)), [ldw2] "s"(ldw2), [ldx2] "s"(ldx2),          \
+      [M] "s"(a.M), [N] "s"(a.N), [n_stages] "s"(a.K / 64), [tiles] "s"(tiles), [form] "s"(a.more), [wave] "s"(wave),  \
+      [lds0] "s"(lds0), [low_lo] "s"(uint32_t(low)), [low_hi] "s"(uint32_t(low >> 32)), [up_lo] "s"(uint32_t(up)),     \
+      [up_hi] "s"(uint32_t(up >> 32)), [index] "s"(index), [rank2] "s"(args.rank * 2), [adapters] "s"(a.adapters),     \
+      [list_m] "v"(list_m), [list_n] "v"(list_n), [roww] "v"(roww), [rowx] "v"(rowx), [chunkw] "v"(chunkw),            \
+      [chunkx] "v"(chunkx), [aw0] "v"(aw0), [ax0] "v"(ax0), [row] "v"(row), [col] "v"(col),                            \
+      [ylane_lo] "v"(uint32_t(ylane)), [ylane_hi] "v"(uint32_t(ylane >> 32))
+  if constexpr (kMt == 8) {
+    asm volatile(
+#include "gemm_rows_adapted_256_gfx950.inc"
+        :: CA_GEMM_ADAPTED_OPERANDS : "memory", "vcc", "scc", "m0", CA_GEMM_ROWS_ADAPTED_CLOBBERS256);
+  } else if constexpr (kMt == 6) {
+    asm volatile(
+#include "gemm_rows_adapted_192_gfx950.inc"
+        :: CA_GEMM_ADAPTED_OPERANDS : "memory", "vcc", "scc", "m0", CA_GEMM_ROWS_ADAPTED_CLOBBERS192);
+  } else {
+    asm volatile(
+#include "gemm_rows_adapted_128_gfx950.inc"
+        :: CA_GEMM_ADAPTED_OPERANDS : "memory", "vcc", "scc", "m0", CA_GEMM_ROWS_ADAPTED_CLOBBERS128);
   }
 }
 
@@ -510,8 +577,7 @@ __global__ __launch_bounds__(256) void adapted_transpose_kernel(Transposed one, 
 constexpr int kFewRows = 32;
 constexpr const char* kWhat = "gemm_adapted.hip";
 
-// the compiled tiles' part of the 8-bit linear map's model: their stages take as long
-constexpr OpModel kModel[] = {{256, 128, 1, 0, 705, 840, 5650}, {128, 128, 1, 0, 455, 470, 3680}, {64, 64, 2, 0, 290, 370, 1990}, {64, 64, 1, 0, 255, 190, 2000}};
+constexpr OpModel kModel[] = {{256, 256, 1, 2260, 960, 1325, 8000}, {192, 256, 1, 2280, 754, 1070, 6500}, {128, 256, 1, 2840, 594, 785, 4500}, {256, 128, 1, 0, 705, 840, 5650}, {128, 128, 1, 0, 455, 470, 3680}, {64, 64, 2, 0, 290, 370, 1990}, {64, 64, 1, 0, 255, 190, 2000}};
 
 template <typename T>
 const void* tile_kernel_address(int steps) {
@@ -520,7 +586,10 @@ const void* tile_kernel_address(int steps) {
 
 // one call of any size readies all kernels for stream capture
 int32_t adapted_ready() {
-  KernelLds kernels[12];
+  KernelLds kernels[15] = {};
+  kernels[12] = {reinterpret_cast<const void*>(gemm_adapted_rows_kernel<8>), kRowsLds};
+  kernels[13] = {reinterpret_cast<const void*>(gemm_adapted_rows_kernel<6>), kRowsLds};
+  kernels[14] = {reinterpret_cast<const void*>(gemm_adapted_rows_kernel<4>), kRowsLds};
   for (int i = 0; i < 3; ++i) {
     const int steps = 1 << i;
     kernels[4 * i] = {tile_kernel_address<Tile256x128>(steps), Tile256x128::kLds};
@@ -528,7 +597,7 @@ int32_t adapted_ready() {
     kernels[4 * i + 2] = {tile_kernel_address<Tile64>(steps), Tile64::kLds};
     kernels[4 * i + 3] = {tile_kernel_address<Tile64Wide>(steps), Tile64Wide::kLds};
   }
-  return ensure_dynamic_lds(kernels, 12, kLdsAdapted);
+  return ensure_dynamic_lds(kernels, 15, kLdsAdapted);
 }
 
 template <typename T>
@@ -540,6 +609,20 @@ int32_t enqueue_adapted(AdaptedArgs& a, int rank, void* stream) {
   a.more = int32_t((tiles + 7) / 8);
   const auto kernel = rank == 32 ? gemm_adapted_kernel<T, 1> : rank == 64 ? gemm_adapted_kernel<T, 2> : gemm_adapted_kernel<T, 4>;
   hipLaunchKernelGGL(kernel, dim3(unsigned(a.more) * 8), dim3(T::kThreads), T::kLds, static_cast<hipStream_t>(stream), a);
+  return finish_launch(kWhat);
+}
+
+template <int kMt>
+int32_t enqueue_adapted_rows(AdaptedArgs& a, int rank, void* stream) {
+  a.tiles_m = (a.M + 32 * kMt - 1) / (32 * kMt);
+  a.tiles_n = (a.N + 255) / 256;
+  const int64_t total = int64_t(a.tiles_m) * a.tiles_n, rounds = (total + 255) / 256;
+  if (total >= (int64_t(1) << 30)) return CA_EUNSUPPORTED;
+  const unsigned workgroups = total < 256 ? 8 * unsigned(last_round_share(int(total))) : 256 * unsigned((rounds + kList - 1) / kList);
+  // how results leave: as enqueue_gemm_rows says
+  const bool whole_lines = a.ldy % 64 == 0 && reinterpret_cast<uintptr_t>(a.y) % 128 == 0;
+  a.more = whole_lines ? kFormPast | kFormThrough << 2 : (rounds <= 1 ? kFormThrough << 2 : 0);
+  hipLaunchKernelGGL((gemm_adapted_rows_kernel<kMt>), dim3(workgroups), dim3(256), kRowsLds, static_cast<hipStream_t>(stream), AdaptedRowsArgs{a, rank});
   return finish_launch(kWhat);
 }
 
@@ -573,9 +656,12 @@ int32_t launch_adapted_gemm(AdaptedArgs& a, int rank, void* stream) {
   int n_cu = 0;
   if (const int32_t rc = device_cu_count(&n_cu); rc != CA_OK) return rc;
   switch (pick_op(kModel, a.M, a.N, a.K / 64, n_cu)) {
-    case 0: return enqueue_adapted<Tile256x128>(a, rank, stream);
-    case 1: return enqueue_adapted<Tile128>(a, rank, stream);
-    case 2: return enqueue_adapted<Tile64>(a, rank, stream);
+    case kOpRows256: return enqueue_adapted_rows<8>(a, rank, stream);
+    case kOpRows192: return enqueue_adapted_rows<6>(a, rank, stream);
+    case kOpRows128: return enqueue_adapted_rows<4>(a, rank, stream);
+    case kOpTile256x128: return enqueue_adapted<Tile256x128>(a, rank, stream);
+    case kOpTile128: return enqueue_adapted<Tile128>(a, rank, stream);
+    case kOpTile64: return enqueue_adapted<Tile64>(a, rank, stream);
     default: return enqueue_adapted<Tile64Wide>(a, rank, stream);
   }
 }

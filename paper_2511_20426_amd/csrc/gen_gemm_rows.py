@@ -33,6 +33,8 @@ the up projection's of the same columns, so that of a wave's 8 sub-tiles over n 
 ends up with both of the same elements; a tile has 128 columns of Y.  act(g) = g / (1 + exp(-p)), p = g (act0 + act1 g^2), g held
 within 1e4 there.  With %[g] the projections leave too (save_lines).
 
+Adapted ("adapted"): the plain product, to whose sums the low-rank adapters' part is added before a tile leaves (adapter_lines).
+
 Register map:
   a[0:32 MT - 1]   accumulators, sub-tile (ti over n, tj over m) at a[4 (MT ti + tj) ..]
   v[0:127]    X fragments: stage parity p, k-step kk, sub-tile tj at v[64 p + 32 kk + 4 tj ..]; set 1 is scratch between tiles
@@ -41,6 +43,7 @@ Register map:
   v186..v193, v194..v201  lane's byte offset from the stage's global base for W / X loads 0..7
   v202..v205  address of the lane's row of Y, temporaries
   i8: v206..v237 scales of the lane's columns: 8 of each pair of sub-tiles; v238, v239 of rows 0..63 / 64..127 of the wave, one to a lane
+  adapted, between tiles: v64..v95 fragments of the adapter, v96..v127 of T, v206..v213 the adapters of the lane's rows, v214..v224 temporaries
 """
 from __future__ import annotations
 
@@ -70,7 +73,15 @@ S_COLS = 64              # 64..67: lanes whose columns exist, of the first 64 an
 S_ROWS, S_NCOL = 68, 69  # rows and columns of the tile that exist
 S_P = 70                 # 70,71: base of the scales; gated: 70 the bound on g, 72,73 base of the saved up projection
 LAST_SGPR = 73
-MFMA = {"plain": "v_mfma_f32_16x16x32_bf16", "gated": "v_mfma_f32_16x16x32_bf16", "i8": "v_mfma_i32_16x16x64_i8"}
+# adapted
+ADAPTER, LOW, INDEX = 64, 96, 206             # fragments of the adapter and of T, the adapters of the lane's rows
+AL, AGRP, AROW, AT, AMAX, ASUM = 214, 215, 216, 217, 218, 220     # lane % 16, 16 bytes x lane group, row of the adapter, temporary, 2^31 - 1, sums (four, and one)
+LAST_VGPR_ADAPTED = 224
+S_G, S_PREV, S_LOADED, S_KK = 74, 75, 76, 77  # adapter at hand, the one before, the one whose fragments there are; byte of the rank
+S_UP, S_LOW, S_MINE = 78, 80, 82              # bases of the adapter and of T, lanes whose row has the adapter (64-bit each)
+S_N0, S_M0, S_LIM, S_X, S_BACK = 84, 85, 86, 87, 88     # first column and row of the wave, its last row, temporary, return address (88, 89)
+LAST_SGPR_ADAPTED = 89
+MFMA = {"adapted": "v_mfma_f32_16x16x32_bf16", "plain": "v_mfma_f32_16x16x32_bf16", "gated": "v_mfma_f32_16x16x32_bf16", "i8": "v_mfma_i32_16x16x64_i8"}
 
 
 def xfrag(p, kk, tj):
@@ -229,14 +240,83 @@ def save_lines(mt):
     return out + ["SAVED_%=:"]
 
 
+def adapter_lines(mt):
+    """adapted: of each sub-tile of 16 rows, and each adapter that they have, the product of its rows of B with the rows of T joins the sums: at
+    once where all sixteen have it, otherwise by way of sums of their own, added in the lanes whose row has it, so that an adapter touches no
+    other rows.  The rank is taken 32 at a time.  (In S_T, S_T + 1: the tile's numbers.)"""
+    a = S_T
+    out = ["s_mul_i32 s%d, s%d, %d" % (S_M0, a, 32 * mt), f"s_and_b32 s{S_X}, %[wave], 1", f"s_mul_i32 s{S_X}, s{S_X}, {16 * mt}",
+           f"s_add_u32 s{S_M0}, s{S_M0}, s{S_X}", f"s_cmp_ge_u32 s{S_M0}, %[M]", "s_nop 0", "s_cbranch_scc1 ADAPTED_%=",      # no rows
+           f"s_lshl_b32 s{S_N0}, s{a + 1}, 8", f"s_lshr_b32 s{S_X}, %[wave], 1", f"s_lshl_b32 s{S_X}, s{S_X}, 7", f"s_add_u32 s{S_N0}, s{S_N0}, s{S_X}",
+           f"s_sub_u32 s{S_LIM}, %[M], s{S_M0}", f"s_sub_u32 s{S_LIM}, s{S_LIM}, 1"] + lane_lines(AL) + [
+           f"v_lshrrev_b32 {V(AGRP)}, 4, {V(AL)}", f"v_lshlrev_b32 {V(AGRP)}, 4, {V(AGRP)}", f"v_and_b32 {V(AL)}, 15, {V(AL)}",
+           # rows of B as W's: 32 c + 8 (lane / 4) + 4 b + lane % 4
+           f"v_lshrrev_b32 {V(AROW)}, 2, {V(AL)}", f"v_lshlrev_b32 {V(AROW)}, 3, {V(AROW)}", f"v_and_b32 {V(AT)}, 3, {V(AL)}",
+           f"v_add_u32 {V(AROW)}, {V(AT)}, {V(AROW)}", f"v_add_u32 {V(AROW)}, s{S_N0}, {V(AROW)}", f"v_bfrev_b32 {V(AMAX)}, -2",
+           # T's base; the wave's rows of the index
+           f"s_mul_i32 s{S_LOW}, s{S_M0}, %[rank2]", f"s_mul_hi_u32 s{S_LOW + 1}, s{S_M0}, %[rank2]", f"s_add_u32 s{S_LOW}, s{S_LOW}, %[low_lo]",
+           f"s_addc_u32 s{S_LOW + 1}, s{S_LOW + 1}, %[low_hi]"]
+    for tj in range(mt):
+        out += [f"v_add_u32 {V(AT)}, {16 * tj}, {V(AL)}", f"v_min_u32 {V(AT)}, s{S_LIM}, {V(AT)}", f"v_add_u32 {V(AT)}, s{S_M0}, {V(AT)}",
+                f"v_lshlrev_b32 {V(AT)}, 2, {V(AT)}", f"global_load_dword {V(INDEX + tj)}, {V(AT)}, %[index]"]
+    out.append("s_waitcnt vmcnt(0)")
+    for tj in range(mt):                                   # -1 behind the last row, and for what is no adapter's number
+        out += [f"v_add_u32 {V(AT)}, {16 * tj}, {V(AL)}", f"v_cmp_ge_u32 vcc, s{S_LIM}, {V(AT)}", "s_nop 1",
+                f"v_cndmask_b32 {V(INDEX + tj)}, -1, {V(INDEX + tj)}, vcc", f"v_cmp_gt_u32 vcc, %[adapters], {V(INDEX + tj)}", "s_nop 1",
+                f"v_cndmask_b32 {V(INDEX + tj)}, -1, {V(INDEX + tj)}, vcc"]
+    out += [f"s_mov_b32 s{S_KK}, 0", "RANK_%=:"]
+    for tj in range(mt):
+        out += [f"v_add_u32 {V(AT)}, {16 * tj}, {V(AL)}", f"v_min_u32 {V(AT)}, s{S_LIM}, {V(AT)}", f"v_mul_u32_u24 {V(AT)}, %[rank2], {V(AT)}",
+                f"v_add_u32 {V(AT)}, {V(AGRP)}, {V(AT)}", f"v_add_u32 {V(AT)}, s{S_KK}, {V(AT)}",
+                f"global_load_dwordx4 {V(LOW + 4 * tj, 4)}, {V(AT)}, s[{S_LOW}:{S_LOW + 1}]"]
+    out.append(f"s_mov_b32 s{S_LOADED}, -1")
+    for tj in range(mt):
+        out += [f"s_mov_b32 s{S_PREV}, -1", f"ADAPTER{tj}_%=:",
+                # the lowest adapter above the one before
+                f"v_cmp_lt_i32 vcc, s{S_PREV}, {V(INDEX + tj)}", "s_nop 1", f"v_cndmask_b32 {V(AT)}, {V(AMAX)}, {V(INDEX + tj)}, vcc"]
+        for how in ("quad_perm:[1,0,3,2]", "quad_perm:[2,3,0,1]", "row_half_mirror", "row_mirror"):
+            out += ["s_nop 1", f"v_min_i32_dpp {V(AT)}, {V(AT)}, {V(AT)} {how} row_mask:0xf bank_mask:0xf"]
+        out += ["s_nop 3", f"v_readfirstlane_b32 s{S_G}, {V(AT)}", "s_nop 3", f"s_cmp_eq_u32 s{S_G}, 0x7fffffff", "s_nop 0", f"s_cbranch_scc1 ROWS{tj}_%=",
+                f"s_cmp_eq_u32 s{S_G}, s{S_LOADED}", "s_nop 0", f"s_cbranch_scc1 LOADED{tj}_%=",
+                f"s_getpc_b64 s[{S_BACK}:{S_BACK + 1}]", f"PCA{tj}_%=:", f"s_add_u32 s{S_BACK}, s{S_BACK}, LOADED{tj}_%=-PCA{tj}_%=",
+                f"s_addc_u32 s{S_BACK + 1}, s{S_BACK + 1}, 0", "s_branch LOADADAPTER_%=",
+                f"LOADED{tj}_%=:", "s_waitcnt vmcnt(0)", f"v_cmp_eq_u32 s[{S_MINE}:{S_MINE + 1}], s{S_G}, {V(INDEX + tj)}", "s_nop 3",
+                f"s_cmp_eq_u64 s[{S_MINE}:{S_MINE + 1}], -1", "s_nop 0", f"s_cbranch_scc1 ALL{tj}_%="]
+        for ti in range(8):
+            acc = 4 * (mt * ti + tj)
+            out += [f"{MFMA['adapted']} {V(ASUM, 4)}, {V(ADAPTER + 4 * ti, 4)}, {V(LOW + 4 * tj, 4)}, 0", "s_nop 15", "s_nop 7"]
+            for r in range(4):
+                out += [f"v_accvgpr_read_b32 {V(ASUM + 4)}, {A(acc + r)}", f"v_add_f32 {V(ASUM + r)}, {V(ASUM + 4)}, {V(ASUM + r)}",
+                        f"v_cndmask_b32_e64 {V(ASUM + r)}, {V(ASUM + 4)}, {V(ASUM + r)}, s[{S_MINE}:{S_MINE + 1}]", f"v_accvgpr_write_b32 {A(acc + r)}, {V(ASUM + r)}"]
+        out += [f"s_mov_b32 s{S_PREV}, s{S_G}", f"s_branch ADAPTER{tj}_%=", f"ALL{tj}_%=:"]
+        for ti in range(8):
+            acc = A(4 * (mt * ti + tj), 4)
+            out.append(f"{MFMA['adapted']} {acc}, {V(ADAPTER + 4 * ti, 4)}, {V(LOW + 4 * tj, 4)}, {acc}")
+        out.append(f"ROWS{tj}_%=:")
+    return out + ["s_nop 15", "s_nop 15", f"s_add_u32 s{S_KK}, s{S_KK}, 64", f"s_cmp_lt_u32 s{S_KK}, %[rank2]", "s_nop 0", "s_cbranch_scc1 RANK_%=", "ADAPTED_%=:"]
+
+
+def load_adapter_lines():
+    """adapted, out of line: the fragments of adapter S_G for the wave's eight sub-tiles over n (rows past the end re-read the last one)"""
+    out = ["LOADADAPTER_%=:", f"s_mul_i32 s{S_X}, s{S_G}, %[N]", f"s_mul_i32 s{S_UP}, s{S_X}, %[rank2]", f"s_mul_hi_u32 s{S_UP + 1}, s{S_X}, %[rank2]",
+           f"s_add_u32 s{S_UP}, s{S_UP}, %[up_lo]", f"s_addc_u32 s{S_UP + 1}, s{S_UP + 1}, %[up_hi]", f"s_sub_u32 s{S_X}, %[N], 1"]
+    for ti in range(8):
+        out += [f"v_add_u32 {V(AT)}, {32 * (ti // 2) + 4 * (ti % 2)}, {V(AROW)}", f"v_min_u32 {V(AT)}, s{S_X}, {V(AT)}",
+                f"v_mul_u32_u24 {V(AT)}, %[rank2], {V(AT)}", f"v_add_u32 {V(AT)}, {V(AGRP)}, {V(AT)}", f"v_add_u32 {V(AT)}, s{S_KK}, {V(AT)}",
+                f"global_load_dwordx4 {V(ADAPTER + 4 * ti, 4)}, {V(AT)}, s[{S_UP}:{S_UP + 1}]"]
+    return out + [f"s_mov_b32 s{S_LOADED}, s{S_G}", f"s_setpc_b64 s[{S_BACK}:{S_BACK + 1}]"]
+
+
 def result_lines(mt, kind="plain"):
     """A tile's sums leave, rounded to bf16, 16 bytes of a row to a lane, in the form that %[form] has for the last tile of the
     workgroup or for the others, and start from zero again if there is a next tile.  (Between a vector instruction that writes VCC
     or a scalar register and one that reads it stand two wait states, as the compiler has it for gfx950.)"""
     a, gated, stored = S_T, kind == "gated", 1 if kind == "gated" else 2       # stored: pieces of 64 columns of a wave
     out = ["s_nop 15", "s_nop 15",                         # the last MFMAs have written back
-           f"v_readlane_b32 s{a}, %[list_m], s{S_YT}", f"v_readlane_b32 s{a + 1}, %[list_n], s{S_YT}", "s_nop 3",
-           # y + tm * (rows of a tile) + tn * 512 bytes
+           f"v_readlane_b32 s{a}, %[list_m], s{S_YT}", f"v_readlane_b32 s{a + 1}, %[list_n], s{S_YT}", "s_nop 3"]
+    if kind == "adapted":
+        out += adapter_lines(mt)
+    out += [# y + tm * (rows of a tile) + tn * 512 bytes
            f"s_mul_i32 s{a + 2}, s{a}, %[tile_y_lo]", f"s_mul_hi_u32 s{a + 3}, s{a}, %[tile_y_lo]", f"s_mul_i32 s{a + 4}, s{a}, %[tile_y_hi]",
            f"s_add_u32 s{a + 3}, s{a + 3}, s{a + 4}", f"s_add_u32 s{a + 2}, s{a + 2}, %[y_lo]", f"s_addc_u32 s{a + 3}, s{a + 3}, %[y_hi]",
            f"s_lshl_b32 s{a + 4}, s{a + 1}, {8 if gated else 9}", f"s_add_u32 s{a + 2}, s{a + 2}, s{a + 4}", f"s_addc_u32 s{a + 3}, s{a + 3}, 0",
@@ -425,6 +505,8 @@ def generate(mt=8, kind="plain"):
     L += ["TILEW_%=:"] + next_tile_lines(0, mt, kind) + ["TILEX_%=:"] + next_tile_lines(1, mt, kind)
     # a tile ends, or its last two stages begin: X of those behind them is the next tile's
     L += ["PAIR_%=:", f"s_cmp_eq_u32 s{S_TRIPS}, 1", "s_nop 0", "s_cbranch_scc1 TILEX_%="] + result_lines(mt, kind)
+    if kind == "adapted":
+        L += load_adapter_lines()
     e("DONE_%=:")
     return L
 
@@ -441,7 +523,8 @@ def main(out_path):
     by = "// Generated by gen_gemm_rows.py -- do not edit.\n"
     for kind, tag, name, last_vgpr, last_sgpr in (("plain", "", "CA_GEMM_ROWS_CLOBBERS", LAST_VGPR, S_NCOL),
                                                   ("i8", "_i8_", "CA_GEMM_ROWS_I8_CLOBBERS", LAST_VGPR_I8, LAST_SGPR),
-                                                  ("gated", "_gated_", "CA_GEMM_ROWS_GATED_CLOBBERS", LAST_VGPR, LAST_SGPR)):
+                                                  ("gated", "_gated_", "CA_GEMM_ROWS_GATED_CLOBBERS", LAST_VGPR, LAST_SGPR),
+                                                  ("adapted", "_adapted_", "CA_GEMM_ROWS_ADAPTED_CLOBBERS", LAST_VGPR_ADAPTED, LAST_SGPR_ADAPTED)):
         with open(out_path.replace("gemm_rows_gfx950.inc", f"gemm_rows{tag.rstrip('_')}_clobbers.inc"), "w") as clobbers:
             clobbers.write(by)
             for mt in (8, 6, 4):
