@@ -201,8 +201,8 @@ int32_t launch_layer_norm_backward(const RowNorm& n, const void* dy, int64_t ldd
 int32_t launch_adamw(const ca_adamw_tensor* tensors, const ca_adamw_tensor* tensors_dev, int32_t n_tensors, int32_t state_bits, double lr, double beta1,
                      double beta2, double eps, double weight_decay, double grad_scale, void* stream);
 int32_t launch_adamw_values(const void* m, const void* v, const float* m_scale, const float* v_scale, float* m_out, float* v_out, int64_t n, void* stream);
-// Y = X W' + (s_g X A_g') B_g' with g = index of the row (down: A [adapters][rank][K], up: B [adapters][N][rank]; rank 32, 64 or 128), low [M][rank] gets
-// s_g X A_g'.  Backward (w: the weights transposed [K][N], ldy: the row stride of dX): the gradients of X and of the adapters' first rank_used; those
+// Y = X W' + (s_g X A_g') B_g' with g = index of the row (down: A [adapters][rank][K], up: B [adapters][N][rank]; rank 32, 64 or 128), low [2][M][rank] gets
+// s_g X A_g' and what its rounding left.  Backward (w: the weights transposed [K][N], ldy: the row stride of dX): the gradients of X and of the adapters' first rank_used; those
 // that are null are left out.
 struct AdaptedLinear {
   const void* x;

@@ -4,8 +4,9 @@
 //
 // Two launches.  The first makes the few values T[m] = s_g X[m] A_g' (the rank: 32, 64 or 128 of them), rounded to bf16 as operands of the second,
 // which multiplies X and W as the plain linear map does and adds T's products with the rows of B to the same sums before they are rounded, so that
-// neither product is written or rounded by itself.  (T's rounding, 2^-9 of each of its values, is 2^-9 / sqrt(3 rank) of the adapter's part of a sum of
-// random signs.)  An adapter's products go to sums of their own and are added for the rows that have it, so that no value of one request's adapter, not
+// neither product is written or rounded by itself.  (T's rounding, up to 2^-8 of each of its values, is 2^-8 / sqrt(3) of the adapter's part of a sum of random
+// signs, which is a small part of it.  The adapters' gradients are sums of nothing else, so that what the rounding left, in bf16 too, is kept beside T for
+// them: with T alone they were 2.35e-3 of their norm off, 1.66e-3 with both, which is their own rounding.)  An adapter's products go to sums of their own and are added for the rows that have it, so that no value of one request's adapter, not
 // even an infinity, touches another's rows.  What adapters a tile's rows have is found in the tile: any order and number works, runs of rows cost least.
 #include <hip/hip_runtime.h>
 
@@ -43,7 +44,7 @@ struct LowArgs {
   const uint16_t* down;                           // [adapters][rank][K]
   const float* scales;
   const int32_t* index;
-  uint16_t* t;                                    // [M][rank]
+  uint16_t* t;                                    // [2][M][rank]: T, and what its rounding to bf16 left
   int32_t M, K, ldx, adapters, rank;
 };
 
@@ -74,6 +75,9 @@ __device__ __forceinline__ int next_adapter(const int (&mine)[kRows], int after)
 
 // ------------------------------------------------------------------------------------------------ T
 
+// what a rounding left of x; nothing of an infinity or NaN, which it keeps
+__device__ __forceinline__ float left_of(float x, float rounded) { return fabsf(rounded) <= 0x1.fffffep127f ? x - rounded : 0.f; }
+
 // A workgroup takes 16 kTm rows and 16 kTn values of each; its waves share K in pieces of 128 bytes of a row, which go straight from memory (X) and L2
 // (A) to the registers that the MFMA multiplies from, kAhead pieces on their way; their sums meet in LDS, in order.  Bound by X's way from memory: 23400 x
 // 5120 of rank 32 72 us, 3.4 TB/s of it; fewer rows have fewer of them to a workgroup (launch_low).
@@ -95,7 +99,9 @@ __global__ __launch_bounds__(64 * kWaves) void adapted_low_kernel(LowArgs a) {
     xat[j] = uint32_t(min(row, a.M - 1) - m0) * uint32_t(a.ldx) * 2 + grp * 16 + wave * 128;
     if (row < a.M && mine[j] < 0 && wave == 0 && blockIdx.z == 0) {                    // none: zeros
 #pragma unroll
-      for (int i = 0; i < kTn; ++i) *reinterpret_cast<uint2*>(a.t + int64_t(row) * a.rank + r0 + 16 * i + 4 * grp) = make_uint2(0, 0);
+      for (int i = 0; i < kTn; ++i)
+#pragma unroll
+        for (int p = 0; p < 2; ++p) *reinterpret_cast<uint2*>(a.t + (int64_t(p) * a.M + row) * a.rank + r0 + 16 * i + 4 * grp) = make_uint2(0, 0);
     }
   }
   // piece i of the wave is number wave + i kWaves of the row's
@@ -156,9 +162,14 @@ __global__ __launch_bounds__(64 * kWaves) void adapted_low_kernel(LowArgs a) {
 #pragma unroll
         for (int v = 1; v < kWaves; ++v) sum += part[v][j][lane];
         // the lane has values 4 grp .. +3 of sixteen of row l15
-        if (mine[j] == g)
-          *reinterpret_cast<uint2*>(a.t + int64_t(m0 + 16 * j + l15) * a.rank + r0 + 16 * n + 4 * grp) =
-              make_uint2(pack_bf16(sum[0] * scale, sum[1] * scale), pack_bf16(sum[2] * scale, sum[3] * scale));
+        if (mine[j] == g) {
+          uint16_t* const to = a.t + int64_t(m0 + 16 * j + l15) * a.rank + r0 + 16 * n + 4 * grp;
+          sum *= scale;
+          const uint2 t = make_uint2(pack_bf16(sum[0], sum[1]), pack_bf16(sum[2], sum[3]));
+          *reinterpret_cast<uint2*>(to) = t;
+          *reinterpret_cast<uint2*>(to + int64_t(a.M) * a.rank) = make_uint2(pack_bf16(left_of(sum[0], bf16_lo(t.x)), left_of(sum[1], bf16_hi(t.x))),
+                                                                             pack_bf16(left_of(sum[2], bf16_lo(t.y)), left_of(sum[3], bf16_hi(t.y))));
+        }
       }
       __syncthreads();
     }
@@ -401,7 +412,7 @@ __global__ __launch_bounds__(256) void adapted_few_kernel(AdaptedArgs a, int ran
 // ------------------------------------------------------------------------------------------------ the adapters' gradients
 
 struct SumArgs {
-  const uint16_t* low;                            // [M][rank]
+  const uint16_t* low;                            // [2][M][rank]: their sum is meant
   const uint16_t* wide;                           // [M][ld]
   const int32_t* index;
   float* parts;                                   // [split][adapters][rank][C]
@@ -415,7 +426,7 @@ constexpr int kSumCols = 128, kSumStep = 32, kMostAdapters = 4096;
 // banks); the next rows are on their way meanwhile.  Rows of other adapters are zeros on both sides.
 template <int kTn>
 __global__ __launch_bounds__(256) void adapted_sum_kernel(SumArgs a) {
-  constexpr int kRank = 16 * kTn, kPitchW = kSumCols * 2 + 4, kPitchL = kRank * 2 + 4, kLoadsL = (kRank / 8 * kSumStep + 255) / 256;
+  constexpr int kRank = 16 * kTn, kPitchW = kSumCols * 2 + 4, kPitchL = kRank * 4 + 4, kChunksL = kRank / 4, kLoadsL = kChunksL * kSumStep / 256;
   __shared__ __attribute__((aligned(16))) uint8_t wide[kSumStep * kPitchW];
   __shared__ __attribute__((aligned(16))) uint8_t low[kSumStep * kPitchL];
   __shared__ uint8_t there[kMostAdapters];
@@ -464,9 +475,10 @@ __global__ __launch_bounds__(256) void adapted_sum_kernel(SumArgs a) {
       }
 #pragma unroll
       for (int i = 0; i < kLoadsL; ++i) {
-        const int at = tid + 256 * i, row = at / (kRank / 8);
+        const int at = tid + 256 * i, row = at / kChunksL, of = at % kChunksL;        // the two of a row side by side
         held_l[i] = U4{0, 0, 0, 0};
-        if (row < kSumStep && (rows >> row & 1)) held_l[i] = *reinterpret_cast<const U4*>(a.low + int64_t(m + row) * kRank + at % (kRank / 8) * 8);
+        if (rows >> row & 1)
+          held_l[i] = *reinterpret_cast<const U4*>(a.low + (int64_t(of >= kChunksL / 2) * a.M + m + row) * kRank + of % (kChunksL / 2) * 8);
       }
     };
     int m = find(begin);
@@ -481,9 +493,8 @@ __global__ __launch_bounds__(256) void adapted_sum_kernel(SumArgs a) {
       }
 #pragma unroll
       for (int i = 0; i < kLoadsL; ++i) {
-        const int at = tid + 256 * i, row = at / (kRank / 8);
-        if (row >= kSumStep) continue;
-        uint32_t* const to = reinterpret_cast<uint32_t*>(low + row * kPitchL + at % (kRank / 8) * 16);
+        const int at = tid + 256 * i;
+        uint32_t* const to = reinterpret_cast<uint32_t*>(low + at / kChunksL * kPitchL + at % kChunksL * 16);
         to[0] = held_l[i].x; to[1] = held_l[i].y; to[2] = held_l[i].z; to[3] = held_l[i].w;
       }
       __syncthreads();
@@ -500,10 +511,10 @@ __global__ __launch_bounds__(256) void adapted_sum_kernel(SumArgs a) {
 #pragma unroll
       for (int i = 0; i < 2; ++i) fw[i] = column(wide + (wave * 32 + i * 16 + l15) * 2, kPitchW);
 #pragma unroll
-      for (int n = 0; n < kTn; ++n) {
+      for (int n = 0; n < 2 * kTn; ++n) {
         const Frag fl = column(low + (n * 16 + l15) * 2, kPitchL);
 #pragma unroll
-        for (int i = 0; i < 2; ++i) acc[i][n] = Bf16Products::multiply(fw[i], fl, acc[i][n]);
+        for (int i = 0; i < 2; ++i) acc[i][n % kTn] = Bf16Products::multiply(fw[i], fl, acc[i][n % kTn]);
       }
     }
     // the lane has columns 4 grp .. +3 of sixteen of row r = l15
@@ -635,7 +646,7 @@ int32_t enqueue_low(const LowArgs& a, void* stream) {
   return finish_launch(kWhat);
 }
 
-// T = s (X A').  Few rows take small workgroups, to be many; many rows 32 or 64 at a time, for A's way from L2.  Us for k 5120 by 16 rows and values /
+// T = s (X A') and what is left of it.  Few rows take small workgroups, to be many; many rows 32 or 64 at a time, for A's way from L2.  Us for k 5120 by 16 rows and values /
 // by 32 rows and 32 values: 1000 rows of rank 32 11.4 / 19.9, 23400 111 / 72; k 1536, 4680 rows 13.0 / 7.8; 23400 rows of rank 64 by 32 rows and 64
 // values in four waves / in eight 106 / 87 (4680 x 1536 11.0 / 13.9); of rank 128 by 32 x 128 / 64 x 64 140 / 152 (4680 x 1536 17.1 / 14.9).
 int32_t launch_low(const LowArgs& a, void* stream) {
@@ -679,7 +690,7 @@ struct AdaptedRoom {                              // of the backward pass, in by
 };
 AdaptedRoom adapted_room(int64_t M, int32_t N, int32_t K, int32_t adapters, int32_t rank) {
   AdaptedRoom r{};
-  r.down_t = up16(size_t(M) * rank * 2);
+  r.down_t = up16(size_t(M) * rank * 4);
   r.up_t = r.down_t + up16(size_t(adapters) * rank * K * 2);
   r.there = r.up_t + up16(size_t(adapters) * rank * N * 2);
   const int sk = sum_splits(M, K, adapters, rank), sn = sum_splits(M, N, adapters, rank);

@@ -526,7 +526,7 @@ PyObject* linear_adapted(PyObject* const* a, Py_ssize_t n) {
   if (!matrix(w, at::kBFloat16, c.n, c.k, *c.x, &ldw)) return not_taken();
   const at::Tensor& y = r.or_empty({c.m, c.n}, *c.x);
   if (!matrix(&y, at::kBFloat16, c.m, c.n, *c.x, &ldy)) return not_taken();
-  const at::Tensor low = at::empty({c.m, c.rank}, c.x->options());
+  const at::Tensor low = at::empty({2, c.m, c.rank}, c.x->options());
   const void *const xp = c.x->data_ptr(), *const wp = w->data_ptr(), *const dp = c.down->data_ptr(), *const up = c.up->data_ptr();
   const float* const sp = c.scales->data_ptr<float>();
   const int32_t* const ip = c.index->data_ptr<int32_t>();
@@ -545,7 +545,7 @@ PyObject* linear_adapted_backward(PyObject* const* a, Py_ssize_t n) {
   const at::Tensor *dy = plain(a[5]), *w = a[6] == Py_None ? nullptr : plain(a[6]), *saved = plain(a[7]);
   ldw = c.n;
   if (!matrix(dy, at::kBFloat16, c.m, c.n, *c.x, &lddy) || (a[6] != Py_None && !matrix(w, at::kBFloat16, c.k, c.n, *c.x, &ldw)) || !saved ||
-      saved->scalar_type() != at::kBFloat16 || saved->dim() != 2 || saved->size(0) != c.m || saved->size(1) != c.rank || !saved->is_contiguous() ||
+      saved->scalar_type() != at::kBFloat16 || saved->dim() != 3 || saved->size(0) != 2 || saved->size(1) != c.m || saved->size(2) != c.rank || !saved->is_contiguous() ||
       !beside(*saved, *c.x))
     return not_taken();
   const size_t bytes = adapted_workspace_fn(c.m, int32_t(c.n), int32_t(c.k), int32_t(c.adapters), int32_t(c.rank));

@@ -544,7 +544,8 @@ class Adapters:
 
 
 def linear_adapted_train(x: torch.Tensor, w: torch.Tensor, adapters: Adapters, index: torch.Tensor, out: torch.Tensor | None = None):
-    """linear_adapted for training: (y, saved), saved being what linear_adapted_backward takes (scales[g] * x @ down[g].T in bf16)."""
+    """linear_adapted for training: (y, saved), saved being what linear_adapted_backward takes (scales[g] * x @ down[g].T
+    in bf16, and what the rounding left of it)."""
     r = B.calls.linear_adapted(x, adapters.down, adapters.up, adapters.scales, index, w, out)
     if r.__class__ is int:
         B._check(r, "layer_linear_adapted_bf16")
@@ -556,7 +557,7 @@ def linear_adapted_train(x: torch.Tensor, w: torch.Tensor, adapters: Adapters, i
     assert adapters.down.device == device and adapters.down.shape[2] == k and adapters.up.shape[1] == n
     assert index.dtype == torch.int32 and index.shape == (m,) and index.is_contiguous() and _reachable(index, x)
     ldx, ldw = _matrix(x, x, _BF16, m, k), _matrix(w, x, _BF16, n, k)
-    low = torch.empty((m, rank), dtype=_BF16, device=device)
+    low = torch.empty((2, m, rank), dtype=_BF16, device=device)
     y = torch.empty((m, n), dtype=_BF16, device=device) if out is None else out
     ldy = _matrix(y, x, _BF16, m, n)
     with _on_device(device):
@@ -584,7 +585,7 @@ def linear_adapted_backward(dy: torch.Tensor, x: torch.Tensor, w_t: torch.Tensor
     g, rank, _ = adapters.down.shape
     assert adapters.down.device == device and adapters.down.shape[2] == k and adapters.up.shape[1] == n
     assert index.dtype == torch.int32 and index.shape == (m,) and index.is_contiguous() and _reachable(index, x)
-    assert saved.dtype == _BF16 and saved.shape == (m, rank) and saved.is_contiguous() and _reachable(saved, x)
+    assert saved.dtype == _BF16 and saved.shape == (2, m, rank) and saved.is_contiguous() and _reachable(saved, x)
     lddy, ldx = _matrix(dy, x, _BF16, m, n), _matrix(x, x, _BF16, m, k)
     ldw = n if w_t is None else _matrix(w_t, x, _BF16, k, n)
     dx = None if w_t is None else torch.empty((m, k), dtype=_BF16, device=device)

@@ -74,9 +74,11 @@ def test_forward(m, n, k, g, r, how):
     ref, t, off = _adapted(x, w, down, up, scales, index)
     _close(y, ref, off)
     way = 1.01 * (k + 2) * 2.0 ** -24 * 1.5 * (x.double().cpu().abs() @ down.double().cpu().abs().amax(0).T)
-    _close(saved[:, :r], t, way)
+    _close(saved[0, :, :r], t, way)
+    # ... and what the rounding left: a half step of a half step is between their sum and T
+    assert ((saved[:, :, :r].double().cpu().sum(0) - t).abs() <= 1.01 * HALF * HALF * t.abs() + 1.01 * way).all()
     none = (index.cpu() < 0) | (index.cpu() >= g)
-    assert (saved[:, r:] == 0).all() and (saved.cpu()[none] == 0).all()
+    assert (saved[:, :, r:] == 0).all() and (saved.cpu()[:, none] == 0).all()
     assert torch.equal(linear_adapted(x, w, adapters, index), y)
 
 
@@ -101,9 +103,9 @@ def test_gradients(m, n, k, g, r, how):
     xd, dyd = x.double().cpu(), dy.double().cpu()
     for a in range(g):
         of = index.cpu() == a
-        # the operand of the rank is rounded to bf16, behind a sum in fp32; the sum over the rows, in fp32 too, is joined from up to 64 parts
+        # the operand of the rank is rounded to bf16 twice, behind a sum in fp32; the sum over the rows, in fp32 too, is joined from up to 64 parts
         for low, wide, mine, of_sum in ((u, xd, got[1][a], k), (t, dyd, got[2][a].t(), n)):
-            _close(mine, low[of].T @ wide[of], ((HALF + (of.sum() + 70) * 2.0 ** -24) * low[of].abs() + 2.0 ** -24 * 4096 * low[of].abs().mean()).T @ wide[of].abs()
+            _close(mine, low[of].T @ wide[of], ((HALF * HALF + (2 * of.sum() + 70) * 2.0 ** -24) * low[of].abs() + 2.0 ** -24 * 4096 * low[of].abs().mean()).T @ wide[of].abs()
                    if of.any() else torch.zeros(mine.shape, dtype=torch.float64))
     none, d_down, d_up = linear_adapted_backward(dy, x, None, adapters, index, saved)
     assert none is None and torch.equal(d_down, got[1]) and torch.equal(d_up, got[2])
@@ -152,7 +154,7 @@ def test_no_request_touches_another(m):
         other = index != 2
         other[2] = False
         y2, saved2 = linear_adapted_train(x2, w, poisoned, index)
-        assert torch.equal(y2[other], y[other]) and torch.equal(saved2[other], saved[other]) and not y2[2].isfinite().any()
+        assert torch.equal(y2[other], y[other]) and torch.equal(saved2[:, other], saved[:, other]) and not y2[2].isfinite().any()
         dx, d_down, d_up = linear_adapted_backward(dy2, x2, w_t, poisoned, index, saved2)
         keep = [0, 1, 3]
         assert torch.equal(dx[other], grads[0][other]) and torch.equal(d_down[keep], grads[1][keep]) and torch.equal(d_up[keep], grads[2][keep])
@@ -255,7 +257,7 @@ def test_arguments_refused_on_device():
                 lambda: linear_adapted(x.float(), w, a, index), lambda: linear_adapted(x, w[:248], a, index), lambda: linear_adapted(x[:, :64], w[:, :64], a, index),
                 lambda: linear_adapted(x, w, a, index, out=y.float()), lambda: linear_adapted(x, w.t(), a, index), lambda: linear_adapted(x, w, a, index[::2]),
                 lambda: Adapters.from_weights(_normal(_gen(0), 1, 129, 128), _normal(_gen(0), 1, 8, 129)), lambda: Adapters.from_weights(down, up[:1]),
-                lambda: linear_adapted_backward(dy, x, w, a, index, saved), lambda: linear_adapted_backward(dy, x, w_t, a, index, saved[:, :16]),
+                lambda: linear_adapted_backward(dy, x, w, a, index, saved), lambda: linear_adapted_backward(dy, x, w_t, a, index, saved[:, :, :16]),
                 lambda: linear_adapted_backward(dy[:, :128], x, w_t, a, index, saved)):
         with pytest.raises(AssertionError):
             bad()
