@@ -370,11 +370,13 @@ int32_t layer_norm_backward(const void* dy_dev, const void* x_dev, int32_t dtype
  * adapters and more) y is x . w'.  Any order of adapters is right; runs of rows with the same one cost least.  A row's results depend on its own adapter
  * alone, whatever values others hold.  down: [adapters][rank][k_in], up: [adapters][n_out][rank], packed; rank 32, 64 or 128: rows and columns
  * behind an adapter's own rank are zeros.  scales: fp32.  Shapes, strides and alignment as layer_linear_bf16; adapters <= CA_MAX_ADAPTERS, columns up to
- * 2^20, rows up to 2^27. */
+ * 2^20, rows up to 2^27.  workspace_dev: layer_linear_adapted_workspace() bytes (0 for more than a few rows). */
 #define CA_MAX_ADAPTERS 4096
+size_t layer_linear_adapted_workspace(int64_t m_rows, int32_t rank);
 int32_t layer_linear_adapted_bf16(const void* x_dev, const void* w_dev, const void* down_dev, const void* up_dev, const float* scales_dev,
                                   const int32_t* index_dev, void* low_dev, void* y_dev, int64_t m_rows, int32_t n_out, int32_t k_in, int32_t adapters,
-                                  int32_t rank, int64_t ldx, int64_t ldw, int64_t ldy, void* hip_stream);
+                                  int32_t rank, int64_t ldx, int64_t ldw, int64_t ldy, void* workspace_dev, size_t workspace_bytes,
+                                  void* hip_stream);
 
 /* Its gradients for frozen weights, from that of y: dx [m_rows][k_in], d_down [adapters][rank_used][k_in], d_up [adapters][n_out][rank_used] (packed; of
  * an adapter without rows zeros), each rounded to bf16 once, written, not added to; those that are null are left out (not all).  w_t_dev: the weights

@@ -39,7 +39,7 @@ EXPORTS = (
     "layer_qk_norm_rope", "layer_qk_norm_rope_workspace", "layer_qk_norm_rope_backward", "kv_cache_append_batch_norm", "layer_quantize_rows_i8",
     "layer_linear_i8", "layer_linear_i8_workspace", "layer_linear_i8_values", "layer_gated_bf16", "layer_gated_saved_bytes", "layer_gated_backward_workspace", "layer_gated_backward_bf16",
     "layer_norm", "layer_norm_backward_workspace", "layer_norm_backward", "layer_adamw", "layer_adamw_values",
-    "layer_linear_adapted_bf16", "layer_linear_adapted_backward_workspace", "layer_linear_adapted_backward_bf16",
+    "layer_linear_adapted_workspace", "layer_linear_adapted_bf16", "layer_linear_adapted_backward_workspace", "layer_linear_adapted_backward_bf16",
     "ca_sched_create", "ca_sched_create_lagged", "ca_sched_destroy", "ca_sched_batch", "ca_sched_advance", "ca_sched_state",
 )
 
@@ -183,7 +183,9 @@ def _load() -> C.CDLL:
     lib.layer_norm_backward.restype = i32
     lib.layer_norm_backward.argtypes = [vp, vp, i32, vp, i32, f32, vp, vp, vp, i64, i32] + [i64] * 5 + [vp, C.c_size_t, vp]
     lib.layer_linear_adapted_bf16.restype = i32
-    lib.layer_linear_adapted_bf16.argtypes = [vp] * 8 + [i64] + [i32] * 4 + [i64] * 3 + [vp]
+    lib.layer_linear_adapted_bf16.argtypes = [vp] * 8 + [i64] + [i32] * 4 + [i64] * 3 + [vp, C.c_size_t, vp]
+    lib.layer_linear_adapted_workspace.restype = C.c_size_t
+    lib.layer_linear_adapted_workspace.argtypes = [i64, i32]
     lib.layer_linear_adapted_backward_workspace.restype = C.c_size_t
     lib.layer_linear_adapted_backward_workspace.argtypes = [i64] + [i32] * 4
     lib.layer_linear_adapted_backward_bf16.restype = i32
@@ -247,8 +249,8 @@ def _load_calls():
             lib.layer_linear_i8_workspace, lib.layer_linear_i8_values, lib.layer_gated_bf16, lib.layer_gated_saved_bytes, lib.layer_gated_backward_workspace,
             lib.layer_gated_backward_bf16)))
         ext.bind_adapt(*(C.cast(f, C.c_void_p).value for f in (
-            lib.layer_norm, lib.layer_norm_backward_workspace, lib.layer_norm_backward, lib.layer_linear_adapted_bf16,
-            lib.layer_linear_adapted_backward_workspace, lib.layer_linear_adapted_backward_bf16, lib.layer_adamw)))
+            lib.layer_norm, lib.layer_norm_backward_workspace, lib.layer_norm_backward, lib.layer_linear_adapted_workspace,
+            lib.layer_linear_adapted_bf16, lib.layer_linear_adapted_backward_workspace, lib.layer_linear_adapted_backward_bf16, lib.layer_adamw)))
         return ext
     except Exception as e:
         warnings.warn(f"{path} cannot be used, calls take more host time without it: {e}", RuntimeWarning)
@@ -528,10 +530,16 @@ def layer_norm_backward(dy_ptr: int, x_ptr: int, dtype: int, weight_ptr: int, we
                                    workspace_bytes, index(stream or 0)), "layer_norm_backward")
 
 
+def layer_linear_adapted_workspace(m_rows: int, rank: int) -> int:
+    return int(lib.layer_linear_adapted_workspace(m_rows, rank))
+
+
 def layer_linear_adapted_bf16(x_ptr: int, w_ptr: int, down_ptr: int, up_ptr: int, scales_ptr: int, index_ptr: int, low_ptr: int, y_ptr: int, m_rows: int,
-                              n_out: int, k_in: int, adapters: int, rank: int, ldx: int, ldw: int, ldy: int, stream: int = 0) -> None:
+                              n_out: int, k_in: int, adapters: int, rank: int, ldx: int, ldw: int, ldy: int, workspace_ptr: int, workspace_bytes: int,
+                              stream: int = 0) -> None:
     _check(lib.layer_linear_adapted_bf16(*(index(p or 0) for p in (x_ptr, w_ptr, down_ptr, up_ptr, scales_ptr, index_ptr, low_ptr, y_ptr)), m_rows, n_out,
-                                         k_in, adapters, rank, ldx, ldw, ldy, index(stream or 0)), "layer_linear_adapted_bf16")
+                                         k_in, adapters, rank, ldx, ldw, ldy, index(workspace_ptr or 0), workspace_bytes, index(stream or 0)),
+           "layer_linear_adapted_bf16")
 
 
 def layer_linear_adapted_backward_workspace(m_rows: int, n_out: int, k_in: int, adapters: int, rank: int) -> int:

@@ -91,9 +91,13 @@ int32_t layer_norm_backward(const void* dy_dev, const void* x_dev, int32_t dtype
   return ca::launch_layer_norm_backward(n, dy_dev, lddy, dx_dev, dweight_dev, dbias_dev, workspace_dev, hip_stream);
 }
 
+size_t layer_linear_adapted_workspace(int64_t m_rows, int32_t rank) {
+  return m_rows < 0 || m_rows > kMaxAdaptedRows || (rank != 32 && rank != 64 && rank != 128) ? 0 : ca::adapted_bytes(m_rows, rank);
+}
+
 int32_t layer_linear_adapted_bf16(const void* x_dev, const void* w_dev, const void* down_dev, const void* up_dev, const float* scales_dev,
                                   const int32_t* index_dev, void* low_dev, void* y_dev, int64_t m_rows, int32_t n_out, int32_t k_in, int32_t adapters,
-                                  int32_t rank, int64_t ldx, int64_t ldw, int64_t ldy, void* hip_stream) {
+                                  int32_t rank, int64_t ldx, int64_t ldw, int64_t ldy, void* workspace_dev, size_t workspace_bytes, void* hip_stream) {
   if (int32_t rc = check_adapted(m_rows, n_out, k_in, adapters, rank)) return rc;
   for (int64_t ld : {ldx, ldw})
     if (int32_t rc = check_ld(ld, k_in)) return rc;
@@ -102,8 +106,10 @@ int32_t layer_linear_adapted_bf16(const void* x_dev, const void* w_dev, const vo
   for (const void* p : {x_dev, w_dev, down_dev, up_dev, static_cast<const void*>(low_dev), static_cast<const void*>(y_dev)})
     if (!p || !aligned(p, 16)) return CA_EINVAL;
   if (!scales_dev || !index_dev || !aligned(scales_dev, 4) || !aligned(index_dev, 4)) return CA_EINVAL;
+  const size_t need = ca::adapted_bytes(m_rows, rank);
+  if (need > 0 && (!workspace_dev || !aligned(workspace_dev, 16) || workspace_bytes < need)) return CA_EINVAL;
   const ca::AdaptedLinear p{x_dev, w_dev, down_dev, up_dev, scales_dev, index_dev, m_rows, ldx, ldw, ldy, n_out, k_in, adapters, rank};
-  return ca::launch_gemm_adapted(p, y_dev, low_dev, hip_stream);
+  return ca::launch_gemm_adapted(p, y_dev, low_dev, workspace_dev, hip_stream);
 }
 
 size_t layer_linear_adapted_backward_workspace(int64_t m_rows, int32_t n_out, int32_t k_in, int32_t adapters, int32_t rank) {

@@ -214,7 +214,8 @@ struct AdaptedLinear {
   int64_t M, ldx, ldw, ldy;
   int32_t N, K, adapters, rank;
 };
-int32_t launch_gemm_adapted(const AdaptedLinear& p, void* y, void* low, void* stream);
+size_t adapted_bytes(int64_t M, int32_t rank);
+int32_t launch_gemm_adapted(const AdaptedLinear& p, void* y, void* low, void* workspace, void* stream);
 size_t adapted_backward_bytes(int64_t M, int32_t N, int32_t K, int32_t adapters, int32_t rank);
 int32_t launch_adapted_backward(const AdaptedLinear& p, const void* dy, int64_t lddy, const void* low, int32_t rank_used, void* dx, void* d_down, void* d_up,
                                 void* workspace, void* stream);

@@ -48,6 +48,17 @@ struct LowArgs {
   int32_t M, K, ldx, adapters, rank;
 };
 
+// few rows: T comes in parts of k
+constexpr int kFewRows = 32, kMostParts = 8;
+struct FewArgs {
+  AdaptedArgs a;
+  const float* parts;                             // [parts][M][rank]: X A' of a part of k
+  const float* scales;
+  uint16_t* t;                                    // [2][M][rank]
+  int32_t rank, n_parts;
+};
+__host__ __device__ constexpr int few_parts(int K) { return K >= 64 * 8 * kMostParts ? kMostParts : K >= 1024 ? K / 512 : 1; }
+
 __device__ __forceinline__ Frag frag_at(const uint16_t* p) { return *reinterpret_cast<const Frag*>(p); }
 
 // the adapter of a row, -1 for none (whatever the index says that is no adapter's number)
@@ -173,6 +184,50 @@ __global__ __launch_bounds__(64 * kWaves) void adapted_low_kernel(LowArgs a) {
       }
       __syncthreads();
     }
+  }
+}
+
+// The same of few rows (one tile of 16, or two) in parts of k, a workgroup each, in fp32 and without the scale: a CU brings A's rows at some 45 GB/s, so that
+// one of them took 7.6 us for 16 values of one row of k 5120.  The kernel that multiplies with B adds the parts.
+__global__ __launch_bounds__(256) void adapted_low_parts_kernel(LowArgs a, float* parts, int n_parts) {
+  constexpr int kWaves = 4, kAhead = 2;
+  __shared__ Sums part[kWaves][64];
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, l15 = lane & 15, grp = lane >> 4;
+  const int r0 = blockIdx.x * 16, of = blockIdx.y % n_parts, m0 = blockIdx.y / n_parts * 16, row = m0 + l15;
+  const int mine[1] = {adapter_of(a.index, row, a.M, a.adapters)};
+  float* const out = parts + (int64_t(of) * a.M + row) * a.rank + r0 + 4 * grp;
+  if (row < a.M && mine[0] < 0 && wave == 0 && blockIdx.z == 0) *reinterpret_cast<Sums*>(out) = Sums{0, 0, 0, 0};
+  // pieces of 128 bytes of the part: number begin + wave + i kWaves of the row's
+  const int all = a.K / 64, begin = all * of / n_parts, end = all * (of + 1) / n_parts, pieces = (end - begin - wave + kWaves - 1) / kWaves;
+  const uint8_t* const x = reinterpret_cast<const uint8_t*>(a.x + int64_t(m0) * a.ldx);
+  const uint32_t xat = uint32_t(min(row, a.M - 1) - m0) * uint32_t(a.ldx) * 2 + grp * 16 + (begin + wave) * 128;
+  const uint32_t aat = uint32_t(l15) * uint32_t(a.K) * 2 + grp * 16 + (begin + wave) * 128;
+  int nth = 0;                                                      // of the rows' adapters; workgroups of another z have others
+  for (int g = next_adapter<1>(mine, -1); g != INT_MAX; g = next_adapter<1>(mine, g)) {
+    if (nth++ % gridDim.z != blockIdx.z) continue;
+    const uint8_t* const down = reinterpret_cast<const uint8_t*>(a.down + (int64_t(g) * a.rank + r0) * a.K);
+    Sums acc{0, 0, 0, 0};
+    for (int i = 0; i < pieces; i += kAhead) {
+      Frag fa[kAhead][2], fx[kAhead][2];
+#pragma unroll
+      for (int s = 0; s < kAhead; ++s)
+#pragma unroll
+        for (int kk = 0; kk < 2; ++kk) {                            // (a piece past the wave's last is that again, and not multiplied)
+          const uint32_t at = uint32_t(min(i + s, pieces - 1)) * (kWaves * 128) + kk * 64;
+          fa[s][kk] = *reinterpret_cast<const Frag*>(down + at + aat);
+          fx[s][kk] = *reinterpret_cast<const Frag*>(x + at + xat);
+        }
+#pragma unroll
+      for (int s = 0; s < kAhead; ++s)
+        if (i + s < pieces) {
+#pragma unroll
+          for (int kk = 0; kk < 2; ++kk) acc = Bf16Products::multiply(fa[s][kk], fx[s][kk], acc);
+        }
+    }
+    part[wave][lane] = acc;
+    __syncthreads();
+    if (wave == 0 && mine[0] == g) *reinterpret_cast<Sums*>(out) = (part[0][lane] + part[1][lane]) + (part[2][lane] + part[3][lane]);
+    __syncthreads();
   }
 }
 
@@ -330,8 +385,10 @@ __global__ __launch_bounds__(256, 1) void gemm_adapted_rows_kernel(AdaptedRowsAr
 // share K in pieces of 128 bytes of 16 rows of W, kAhead on their way straight to the registers that the MFMA multiplies from, with X's rows from L2; of an
 // adapter each wave takes one step of 32 of its rank.
 template <int kTiles>
-__global__ __launch_bounds__(256) void adapted_few_kernel(AdaptedArgs a, int rank) {
+__global__ __launch_bounds__(256) void adapted_few_kernel(FewArgs args) {
   constexpr int kWaves = 4, kAhead = 4;
+  const AdaptedArgs& a = args.a;
+  const int rank = args.rank;
   __shared__ Sums part[kWaves][kTiles][64];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, l15 = lane & 15, grp = lane >> 4;
   const int n0 = blockIdx.x * 16, col = min(n0 + l15, a.N - 1);
@@ -370,7 +427,34 @@ __global__ __launch_bounds__(256) void adapted_few_kernel(AdaptedArgs a, int ran
   const int at = 32 * wave + grp * 8;
   if (32 * wave < rank) {
 #pragma unroll
-    for (int t = 0; t < kTiles; ++t) ft[t] = frag_at(a.t + int64_t(min(16 * t + l15, a.M - 1)) * rank + at);
+    for (int t = 0; t < kTiles; ++t) {                              // T from its parts, in order; the first workgroup leaves it for the way back
+      const int row = 16 * t + l15;
+      if (row >= a.M) continue;
+      const float* const from = args.parts + int64_t(row) * rank + at;
+      const int64_t step = int64_t(a.M) * rank;
+      Sums sum[2] = {*reinterpret_cast<const Sums*>(from), *reinterpret_cast<const Sums*>(from + 4)};
+#pragma unroll
+      for (int p = 1; p < kMostParts; ++p) {
+        if (p >= args.n_parts) break;
+        sum[0] += *reinterpret_cast<const Sums*>(from + p * step);
+        sum[1] += *reinterpret_cast<const Sums*>(from + p * step + 4);
+      }
+      const float scale = mine[t] < 0 ? 0.f : args.scales[mine[t]];
+      uint32_t low[4], left[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float v0 = mine[t] < 0 ? 0.f : sum[e / 2][e % 2 * 2] * scale, v1 = mine[t] < 0 ? 0.f : sum[e / 2][e % 2 * 2 + 1] * scale;
+        low[e] = pack_bf16(v0, v1);
+        left[e] = pack_bf16(left_of(v0, bf16_lo(low[e])), left_of(v1, bf16_hi(low[e])));
+      }
+      const u32x4 packed = {low[0], low[1], low[2], low[3]};
+      ft[t] = __builtin_bit_cast(Frag, packed);
+      if (blockIdx.x == 0) {
+        uint16_t* const to = args.t + int64_t(row) * rank + at;
+        *reinterpret_cast<u32x4*>(to) = packed;
+        *reinterpret_cast<u32x4*>(to + step) = u32x4{left[0], left[1], left[2], left[3]};
+      }
+    }
     for (int g = next_adapter<kTiles>(mine, -1); g != INT_MAX; g = next_adapter<kTiles>(mine, g)) {
       const Frag fu = frag_at(a.up + (int64_t(g) * a.N + col) * rank + at);
 #pragma unroll
@@ -585,7 +669,6 @@ __global__ __launch_bounds__(256) void adapted_transpose_kernel(Transposed one, 
 
 // ------------------------------------------------------------------------------------------------ launches
 
-constexpr int kFewRows = 32;
 constexpr const char* kWhat = "gemm_adapted.hip";
 
 constexpr OpModel kModel[] = {{256, 256, 1, 2260, 960, 1325, 8000}, {192, 256, 1, 2280, 754, 1070, 6500}, {128, 256, 1, 2840, 594, 785, 4500}, {256, 128, 1, 0, 705, 840, 5650}, {128, 128, 1, 0, 455, 470, 3680}, {64, 64, 2, 0, 290, 370, 1990}, {64, 64, 1, 0, 255, 190, 2000}};
@@ -656,14 +739,23 @@ int32_t launch_low(const LowArgs& a, void* stream) {
   return enqueue_low<4, 4, 4, 2>(a, stream);
 }
 
-int32_t launch_adapted_gemm(AdaptedArgs& a, int rank, void* stream) {
+// X A' and what is multiplied with it: for few rows T in parts (room: few_bytes), otherwise ahead
+int32_t launch_low_and_gemm(const LowArgs& l, AdaptedArgs& a, void* room, void* stream) {
   if (const int32_t rc = adapted_ready(); rc != CA_OK) return rc;
   if (a.M <= kFewRows) {
     const int64_t groups = (int64_t(a.N) + 15) / 16;
     if (groups * 256 >= (int64_t(1) << 32)) return CA_EUNSUPPORTED;
-    hipLaunchKernelGGL(a.M <= 16 ? adapted_few_kernel<1> : adapted_few_kernel<2>, dim3(unsigned(groups)), dim3(256), 0, static_cast<hipStream_t>(stream), a, rank);
+    const int n_parts = few_parts(a.K), tiles = (a.M + 15) / 16;
+    float* const parts = static_cast<float*>(room);
+    hipLaunchKernelGGL(adapted_low_parts_kernel, dim3(unsigned(l.rank / 16), unsigned(n_parts * tiles), unsigned(std::min(l.adapters, std::min(a.M, 8)))), dim3(256), 0,
+                       static_cast<hipStream_t>(stream), l, parts, n_parts);
+    if (const int32_t rc = finish_launch(kWhat); rc != CA_OK) return rc;
+    hipLaunchKernelGGL(a.M <= 16 ? adapted_few_kernel<1> : adapted_few_kernel<2>, dim3(unsigned(groups)), dim3(256), 0, static_cast<hipStream_t>(stream),
+                       FewArgs{a, parts, l.scales, l.t, l.rank, n_parts});
     return finish_launch(kWhat);
   }
+  if (const int32_t rc = launch_low(l, stream); rc != CA_OK) return rc;
+  const int rank = l.rank;
   int n_cu = 0;
   if (const int32_t rc = device_cu_count(&n_cu); rc != CA_OK) return rc;
   switch (pick_op(kModel, a.M, a.N, a.K / 64, n_cu)) {
@@ -685,12 +777,15 @@ int sum_splits(int64_t M, int32_t C, int32_t adapters, int32_t rank) {
 
 size_t up16(size_t n) { return (n + 15) / 16 * 16; }
 
+size_t few_bytes(int64_t M, int32_t rank) { return M <= kFewRows ? size_t(kMostParts) * M * rank * 4 : 0; }
+
 struct AdaptedRoom {                              // of the backward pass, in bytes
-  size_t low, down_t, up_t, there, parts, bytes;
+  size_t few, down_t, up_t, there, parts, bytes;
 };
 AdaptedRoom adapted_room(int64_t M, int32_t N, int32_t K, int32_t adapters, int32_t rank) {
   AdaptedRoom r{};
-  r.down_t = up16(size_t(M) * rank * 4);
+  r.few = up16(size_t(M) * rank * 4);
+  r.down_t = r.few + up16(few_bytes(M, rank));
   r.up_t = r.down_t + up16(size_t(adapters) * rank * K * 2);
   r.there = r.up_t + up16(size_t(adapters) * rank * N * 2);
   const int sk = sum_splits(M, K, adapters, rank), sn = sum_splits(M, N, adapters, rank);
@@ -724,14 +819,15 @@ Transposed transposed(const void* from, void* to, int rows, int cols) {
 
 }  // namespace
 
-int32_t launch_gemm_adapted(const AdaptedLinear& p, void* y, void* low, void* stream) {
+size_t adapted_bytes(int64_t M, int32_t rank) { return few_bytes(M, rank); }
+
+int32_t launch_gemm_adapted(const AdaptedLinear& p, void* y, void* low, void* workspace, void* stream) {
   if (p.M == 0) return CA_OK;
-  LowArgs l{static_cast<const uint16_t*>(p.x), static_cast<const uint16_t*>(p.down), p.scales, p.index, static_cast<uint16_t*>(low), int32_t(p.M), p.K,
-            int32_t(p.ldx), p.adapters, p.rank};
-  if (const int32_t rc = launch_low(l, stream); rc != CA_OK) return rc;
+  const LowArgs l{static_cast<const uint16_t*>(p.x), static_cast<const uint16_t*>(p.down), p.scales, p.index, static_cast<uint16_t*>(low), int32_t(p.M), p.K,
+                  int32_t(p.ldx), p.adapters, p.rank};
   AdaptedArgs a{static_cast<const uint16_t*>(p.x), static_cast<const uint16_t*>(p.w), static_cast<uint16_t*>(y), static_cast<const uint16_t*>(low),
                 static_cast<const uint16_t*>(p.up), p.index, p.ldy, int32_t(p.M), p.N, p.K, int32_t(p.ldx), int32_t(p.ldw), p.adapters, 0, 0, 0};
-  return launch_adapted_gemm(a, p.rank, stream);
+  return launch_low_and_gemm(l, a, workspace, stream);
 }
 
 size_t adapted_backward_bytes(int64_t M, int32_t N, int32_t K, int32_t adapters, int32_t rank) { return adapted_room(M, N, K, adapters, rank).bytes; }
@@ -750,12 +846,9 @@ int32_t launch_adapted_backward(const AdaptedLinear& p, const void* dy, int64_t 
     if (const int32_t rc = finish_launch(kWhat); rc != CA_OK) return rc;
     const LowArgs l{static_cast<const uint16_t*>(dy), reinterpret_cast<const uint16_t*>(room + r.up_t), p.scales, p.index, low_dy, M, p.N, int32_t(lddy), p.adapters,
                     p.rank};
-    if (const int32_t rc = launch_low(l, stream); rc != CA_OK) return rc;
-  }
-  if (M > 0 && dx) {
     AdaptedArgs a{static_cast<const uint16_t*>(dy), static_cast<const uint16_t*>(p.w), static_cast<uint16_t*>(dx), low_dy,
                   reinterpret_cast<const uint16_t*>(room + r.down_t), p.index, p.ldy, M, p.K, p.N, int32_t(lddy), int32_t(p.ldw), p.adapters, 0, 0, 0};
-    if (const int32_t rc = launch_adapted_gemm(a, p.rank, stream); rc != CA_OK) return rc;
+    if (const int32_t rc = dx ? launch_low_and_gemm(l, a, room + r.few, stream) : launch_low(l, stream); rc != CA_OK) return rc;
   }
   if (d_down)
     if (const int32_t rc = launch_adapter_sum(low_dy, p.x, p.ldx, p.index, M, p.K, p.adapters, p.rank, rank_used, false, d_down, there, parts, stream); rc != CA_OK)

@@ -42,6 +42,7 @@ decltype(&layer_gated_backward_bf16) gated_backward_fn = nullptr;
 decltype(&layer_norm) row_norm_fn = nullptr;
 decltype(&layer_norm_backward_workspace) row_norm_workspace_fn = nullptr;
 decltype(&layer_norm_backward) row_norm_backward_fn = nullptr;
+decltype(&layer_linear_adapted_workspace) adapted_room_fn = nullptr;
 decltype(&layer_linear_adapted_bf16) adapted_fn = nullptr;
 decltype(&layer_linear_adapted_backward_workspace) adapted_workspace_fn = nullptr;
 decltype(&layer_linear_adapted_backward_bf16) adapted_backward_fn = nullptr;
@@ -527,12 +528,17 @@ PyObject* linear_adapted(PyObject* const* a, Py_ssize_t n) {
   const at::Tensor& y = r.or_empty({c.m, c.n}, *c.x);
   if (!matrix(&y, at::kBFloat16, c.m, c.n, *c.x, &ldy)) return not_taken();
   const at::Tensor low = at::empty({2, c.m, c.rank}, c.x->options());
+  const size_t bytes = adapted_room_fn(c.m, int32_t(c.rank));
+  at::Tensor work;
+  if (bytes > 0) work = at::empty({int64_t(bytes)}, c.x->options().dtype(at::kByte));
+  void* const workp = bytes > 0 ? work.data_ptr() : nullptr;
   const void *const xp = c.x->data_ptr(), *const wp = w->data_ptr(), *const dp = c.down->data_ptr(), *const up = c.up->data_ptr();
   const float* const sp = c.scales->data_ptr<float>();
   const int32_t* const ip = c.index->data_ptr<int32_t>();
   void *const lp = low.data_ptr(), *const yp = y.data_ptr(), *const stream = c.stream();
   const int32_t rc = released([&] {
-    return adapted_fn(xp, wp, dp, up, sp, ip, lp, yp, c.m, int32_t(c.n), int32_t(c.k), int32_t(c.adapters), int32_t(c.rank), c.ldx, ldw, ldy, stream);
+    return adapted_fn(xp, wp, dp, up, sp, ip, lp, yp, c.m, int32_t(c.n), int32_t(c.k), int32_t(c.adapters), int32_t(c.rank), c.ldx, ldw, ldy, workp, bytes,
+                      stream);
   });
   return rc != CA_OK ? PyLong_FromLong(rc) : tuple({r.give(rc), THPVariable_Wrap(low)});
 }
@@ -733,14 +739,14 @@ PyObject* bind_layer(PyObject* const* a, Py_ssize_t n) {
   Py_RETURN_NONE;
 }
 
-// bind_adapt(addresses of the seven entry points of the operators that a layer is adapted with in the order above)
+// bind_adapt(addresses of the eight entry points of the operators that a layer is adapted with in the order above)
 PyObject* bind_adapt(PyObject* const* a, Py_ssize_t n) {
-  int64_t f[7];
-  if (n != 7) {
-    PyErr_SetString(PyExc_TypeError, "seven addresses");
+  int64_t f[8];
+  if (n != 8) {
+    PyErr_SetString(PyExc_TypeError, "eight addresses");
     return nullptr;
   }
-  for (int i = 0; i < 7; ++i)
+  for (int i = 0; i < 8; ++i)
     if (!whole(a[i], f + i) || f[i] == 0) {
       PyErr_SetString(PyExc_TypeError, "an address is an int");
       return nullptr;
@@ -748,10 +754,11 @@ PyObject* bind_adapt(PyObject* const* a, Py_ssize_t n) {
   row_norm_fn = reinterpret_cast<decltype(row_norm_fn)>(f[0]);
   row_norm_workspace_fn = reinterpret_cast<decltype(row_norm_workspace_fn)>(f[1]);
   row_norm_backward_fn = reinterpret_cast<decltype(row_norm_backward_fn)>(f[2]);
-  adapted_fn = reinterpret_cast<decltype(adapted_fn)>(f[3]);
-  adapted_workspace_fn = reinterpret_cast<decltype(adapted_workspace_fn)>(f[4]);
-  adapted_backward_fn = reinterpret_cast<decltype(adapted_backward_fn)>(f[5]);
-  adamw_fn = reinterpret_cast<decltype(adamw_fn)>(f[6]);
+  adapted_room_fn = reinterpret_cast<decltype(adapted_room_fn)>(f[3]);
+  adapted_fn = reinterpret_cast<decltype(adapted_fn)>(f[4]);
+  adapted_workspace_fn = reinterpret_cast<decltype(adapted_workspace_fn)>(f[5]);
+  adapted_backward_fn = reinterpret_cast<decltype(adapted_backward_fn)>(f[6]);
+  adamw_fn = reinterpret_cast<decltype(adamw_fn)>(f[7]);
   Py_RETURN_NONE;
 }
 

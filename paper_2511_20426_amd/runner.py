@@ -560,9 +560,11 @@ def linear_adapted_train(x: torch.Tensor, w: torch.Tensor, adapters: Adapters, i
     low = torch.empty((2, m, rank), dtype=_BF16, device=device)
     y = torch.empty((m, n), dtype=_BF16, device=device) if out is None else out
     ldy = _matrix(y, x, _BF16, m, n)
+    nbytes = B.layer_linear_adapted_workspace(m, rank)
+    work = torch.empty(nbytes, dtype=torch.uint8, device=device)
     with _on_device(device):
         B.layer_linear_adapted_bf16(x.data_ptr(), w.data_ptr(), adapters.down.data_ptr(), adapters.up.data_ptr(), adapters.scales.data_ptr(), index.data_ptr(),
-                                    low.data_ptr(), y.data_ptr(), m, n, k, g, rank, ldx, ldw, ldy, _current_stream(device))
+                                    low.data_ptr(), y.data_ptr(), m, n, k, g, rank, ldx, ldw, ldy, work.data_ptr(), nbytes, _current_stream(device))
     return y, low
 
 
