@@ -1,6 +1,8 @@
 """The operators that a layer is adapted with, as they are used together: a modulated layer, an attention layer with adapters, the training of adapters
 and the norm ahead of them by AdamW, of the feed-forward half by AdamW, and their commands."""
 import json
+import os
+import shutil
 import subprocess
 import sys
 
@@ -177,3 +179,17 @@ def test_commands(args, metric):
     assert r.returncode == 0, r.stderr[-2000:]
     said = json.loads(r.stdout.strip().splitlines()[-1])
     assert said["metric"] == metric and said["value"] > 0 and said["loss_last"] == said["loss_last"]
+
+
+def test_host_code_is_clean_under_asan_and_ubsan(tmp_path):
+    cxx = shutil.which("g++")
+    if cxx is None:
+        pytest.skip("no g++")
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    csrc, exe = os.path.join(root, "paper_2511_20426_amd", "csrc"), str(tmp_path / "adapt_sanitize")
+    subprocess.run([cxx, "-std=c++17", "-O1", "-g", "-fsanitize=address,undefined", "-fno-sanitize-recover=all", "-static-libasan", "-static-libubsan",
+                    "-I", os.path.join(root, "include"), "-I", csrc, os.path.join(root, "tests", "adapt_sanitize_driver.cpp"),
+                    os.path.join(csrc, "ca_adapt.cpp"), "-o", exe], check=True, capture_output=True, text=True)
+    r = subprocess.run([exe], capture_output=True, text=True, timeout=300, env=dict(os.environ, ASAN_OPTIONS="detect_leaks=1:abort_on_error=0",
+                                                                                 UBSAN_OPTIONS="print_stacktrace=1"))
+    assert r.returncode == 0 and "adapt sanitizer driver: ok" in r.stdout, r.stdout + r.stderr
