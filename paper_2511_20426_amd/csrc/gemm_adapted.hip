@@ -519,6 +519,7 @@ __global__ __launch_bounds__(256) void adapted_sum_kernel(SumArgs a) {
   const int c0 = blockIdx.x * kSumCols, split = blockIdx.y;
   const int begin = split * a.split_rows, end = min(begin + a.split_rows, a.M);
   for (int g = tid; g < a.adapters; g += 256) there[g] = 0;
+  int nth = 0;                                                      // of the split's adapters
   for (int after = -1;;) {
     int g = INT_MAX;
     for (int m = begin + tid; m < end; m += 256) {
@@ -534,6 +535,7 @@ __global__ __launch_bounds__(256) void adapted_sum_kernel(SumArgs a) {
     if (g == INT_MAX) break;
     after = g;
     if (tid == 0) there[g] = 1;
+    if (nth++ % gridDim.z != blockIdx.z) continue;                  // another workgroup's
     Sums acc[2][kTn];
 #pragma unroll
     for (int i = 0; i < 2; ++i)
@@ -611,13 +613,12 @@ __global__ __launch_bounds__(256) void adapted_sum_kernel(SumArgs a) {
       for (int n = 0; n < kTn; ++n) *reinterpret_cast<Sums*>(out + int64_t(n * 16 + l15) * a.C + col) = acc[i][n];
     }
   }
-  if (blockIdx.x == 0)
+  if (blockIdx.x == 0 && blockIdx.z == 0)
     for (int g = tid; g < a.adapters; g += 256) a.there[split * a.adapters + g] = there[g];
 }
 
-// out [adapters][R][C], or transposed [adapters][C][R], from the splits' parts: a workgroup takes 256 columns of a row (C is a multiple of 8), four to a
-// lane, and its four waves share the splits
-template <bool kTransposed>
+// out [adapters][R][C] from the splits' parts: a workgroup takes 256 columns of a row (C is a multiple of 8), four to a lane, and its four waves share
+// the splits
 __global__ __launch_bounds__(256) void adapted_join_kernel(const float* parts, const int32_t* there, int splits, int adapters, int rank, int R, int C, uint16_t* out) {
   __shared__ Sums sums[4][64];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = blockIdx.x * 256 + 4 * lane, r = blockIdx.y, g = blockIdx.z;
@@ -638,13 +639,35 @@ __global__ __launch_bounds__(256) void adapted_join_kernel(const float* parts, c
   if (wave != 0 || c >= C) return;
   sum = (sums[0][lane] + sums[1][lane]) + (sums[2][lane] + sums[3][lane]);
   const uint2 two = make_uint2(pack_bf16(sum[0], sum[1]), pack_bf16(sum[2], sum[3]));
-  if constexpr (kTransposed) {
-    uint16_t* const to = out + (int64_t(g) * C + c) * R + r;
-    to[0] = uint16_t(two.x), to[R] = uint16_t(two.x >> 16), to[2 * R] = uint16_t(two.y), to[3 * R] = uint16_t(two.y >> 16);
-  } else {
-    uint16_t* const to = out + (int64_t(g) * R + r) * C + c;       // (whose alignment is the caller's)
-    to[0] = uint16_t(two.x), to[1] = uint16_t(two.x >> 16), to[2] = uint16_t(two.y), to[3] = uint16_t(two.y >> 16);
+  uint16_t* const to = out + (int64_t(g) * R + r) * C + c;         // (whose alignment is the caller's)
+  to[0] = uint16_t(two.x), to[1] = uint16_t(two.x >> 16), to[2] = uint16_t(two.y), to[3] = uint16_t(two.y >> 16);
+}
+
+// Transposed, out [adapters][C][R]: 32 columns and 32 rows of the rank to a workgroup, turned in LDS
+__global__ __launch_bounds__(256) void adapted_join_transposed_kernel(const float* parts, const int32_t* there, int splits, int adapters, int rank, int R, int C,
+                                                                      uint16_t* out) {
+  __shared__ float sums[32][33];
+  const int x = threadIdx.x & 31, y = threadIdx.x >> 5, c0 = blockIdx.x * 32, r0 = blockIdx.y * 32, g = blockIdx.z;
+  float sum[4] = {0.f, 0.f, 0.f, 0.f};
+  if (c0 + x < C) {
+    const float* const from = parts + (int64_t(g) * rank + r0 + y) * C + c0 + x;      // (the rank has whole steps of 32 rows)
+    const int64_t step = int64_t(adapters) * rank * C;
+#pragma unroll 4
+    for (int s = 0; s < splits; ++s) {
+      const bool adds = there[s * adapters + g] != 0;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float one = from[s * step + int64_t(8 * i) * C];
+        sum[i] = adds ? sum[i] + one : sum[i];
+      }
+    }
   }
+#pragma unroll
+  for (int i = 0; i < 4; ++i) sums[y + 8 * i][x] = sum[i];
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    if (c0 + y + 8 * i < C && r0 + x < R) out[(int64_t(g) * C + c0 + y + 8 * i) * R + r0 + x] = uint16_t(pack_bf16(sums[x][y + 8 * i], 0.f));
 }
 
 // [rows][cols] of each adapter to [cols][rows], of up to two of them
@@ -805,11 +828,19 @@ int32_t launch_adapter_sum(const uint16_t* low, const void* wide, int64_t ld, co
     a.split_rows = int32_t((int64_t(M) + most - 1) / most);
     splits = (M + a.split_rows - 1) / a.split_rows;
     const auto kernel = rank == 32 ? adapted_sum_kernel<2> : rank == 64 ? adapted_sum_kernel<4> : adapted_sum_kernel<8>;
-    hipLaunchKernelGGL(kernel, dim3(unsigned((C + kSumCols - 1) / kSumCols), unsigned(splits)), dim3(256), 0, s, a);
+    // few rows' adapters are dealt to several workgroups: 37 rows of eight, of rank 128 and 4608 columns 44 us by one of them
+    const unsigned tiles = unsigned((C + kSumCols - 1) / kSumCols);
+    const unsigned z = std::max(1u, std::min({unsigned(adapters), 8u, 1024u / (tiles * unsigned(splits))}));
+    hipLaunchKernelGGL(kernel, dim3(tiles, unsigned(splits), z), dim3(256), 0, s, a);
     if (const int32_t rc = finish_launch(kWhat); rc != CA_OK) return rc;
   }
-  hipLaunchKernelGGL(transposed ? adapted_join_kernel<true> : adapted_join_kernel<false>, dim3(unsigned((C + 255) / 256), unsigned(rank_used), unsigned(adapters)),
-                     dim3(256), 0, s, parts, there, splits, adapters, rank, rank_used, C, static_cast<uint16_t*>(out));
+  uint16_t* const to = static_cast<uint16_t*>(out);
+  if (transposed)
+    hipLaunchKernelGGL(adapted_join_transposed_kernel, dim3(unsigned((C + 31) / 32), unsigned((rank_used + 31) / 32), unsigned(adapters)), dim3(256), 0, s, parts, there,
+                       splits, adapters, rank, rank_used, C, to);
+  else
+    hipLaunchKernelGGL(adapted_join_kernel, dim3(unsigned((C + 255) / 256), unsigned(rank_used), unsigned(adapters)), dim3(256), 0, s, parts, there, splits, adapters,
+                       rank, rank_used, C, to);
   return finish_launch(kWhat);
 }
 

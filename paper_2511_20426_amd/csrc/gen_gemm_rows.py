@@ -43,7 +43,7 @@ Register map:
   v186..v193, v194..v201  lane's byte offset from the stage's global base for W / X loads 0..7
   v202..v205  address of the lane's row of Y, temporaries
   i8: v206..v237 scales of the lane's columns: 8 of each pair of sub-tiles; v238, v239 of rows 0..63 / 64..127 of the wave, one to a lane
-  adapted, between tiles: v64..v95 fragments of the adapter, v96..v127 of T, v206..v213 the adapters of the lane's rows, v214..v224 temporaries
+  adapted, between tiles: v64..v95 fragments of the adapter, v96..v127 of T, v206..v213 the adapters of the lane's rows, v214..v235 temporaries
 """
 from __future__ import annotations
 
@@ -75,12 +75,12 @@ S_P = 70                 # 70,71: base of the scales; gated: 70 the bound on g, 
 LAST_SGPR = 73
 # adapted
 ADAPTER, LOW, INDEX = 64, 96, 206             # fragments of the adapter and of T, the adapters of the lane's rows
-AL, AGRP, AROW, AT, AMAX, ASUM = 214, 215, 216, 217, 218, 220     # lane % 16, 16 bytes x lane group, row of the adapter, temporary, 2^31 - 1, sums (four, and one)
-LAST_VGPR_ADAPTED = 224
-S_G, S_PREV, S_LOADED, S_KK = 74, 75, 76, 77  # adapter at hand, the one before, the one whose fragments there are; byte of the rank
+AL, AGRP, AROW, AT, AMAX, AOLD, ASUM = 214, 215, 216, 217, 218, 219, 220      # lane % 16, 16 bytes x lane group, row of the adapter, temporary, 2^31 - 1, ...
+LAST_VGPR_ADAPTED = 235                       # ... a sum as it was, sums of an adapter (four sub-tiles)
+S_G, S_PREV, S_KK = 74, 75, 77                # adapter at hand, the one before; byte of the rank
 S_UP, S_LOW, S_MINE = 78, 80, 82              # bases of the adapter and of T, lanes whose row has the adapter (64-bit each)
-S_N0, S_M0, S_LIM, S_X, S_BACK = 84, 85, 86, 87, 88     # first column and row of the wave, its last row, temporary, return address (88, 89)
-LAST_SGPR_ADAPTED = 89
+S_N0, S_M0, S_LIM, S_X = 84, 85, 86, 87       # first column and row of the wave, its last row, temporary
+LAST_SGPR_ADAPTED = 87
 MFMA = {"adapted": "v_mfma_f32_16x16x32_bf16", "plain": "v_mfma_f32_16x16x32_bf16", "gated": "v_mfma_f32_16x16x32_bf16", "i8": "v_mfma_i32_16x16x64_i8"}
 
 
@@ -241,9 +241,9 @@ def save_lines(mt):
 
 
 def adapter_lines(mt):
-    """adapted: of each sub-tile of 16 rows, and each adapter that they have, the product of its rows of B with the rows of T joins the sums: at
-    once where all sixteen have it, otherwise by way of sums of their own, added in the lanes whose row has it, so that an adapter touches no
-    other rows.  The rank is taken 32 at a time.  (In S_T, S_T + 1: the tile's numbers.)"""
+    """adapted: of each adapter that the wave's rows have, and each sub-tile of 16 rows that has it, the product of its rows of B with the rows of T joins
+    the sums: at once where all sixteen have it, otherwise by way of sums of their own, added in the lanes whose row has it, so that an adapter
+    touches no other rows.  The rank is taken 32 at a time.  (In S_T, S_T + 1: the tile's numbers.)"""
     a = S_T
     out = ["s_mul_i32 s%d, s%d, %d" % (S_M0, a, 32 * mt), f"s_and_b32 s{S_X}, %[wave], 1", f"s_mul_i32 s{S_X}, s{S_X}, {16 * mt}",
            f"s_add_u32 s{S_M0}, s{S_M0}, s{S_X}", f"s_cmp_ge_u32 s{S_M0}, %[M]", "s_nop 0", "s_cbranch_scc1 ADAPTED_%=",      # no rows
@@ -269,42 +269,44 @@ def adapter_lines(mt):
         out += [f"v_add_u32 {V(AT)}, {16 * tj}, {V(AL)}", f"v_min_u32 {V(AT)}, s{S_LIM}, {V(AT)}", f"v_mul_u32_u24 {V(AT)}, %[rank2], {V(AT)}",
                 f"v_add_u32 {V(AT)}, {V(AGRP)}, {V(AT)}", f"v_add_u32 {V(AT)}, s{S_KK}, {V(AT)}",
                 f"global_load_dwordx4 {V(LOW + 4 * tj, 4)}, {V(AT)}, s[{S_LOW}:{S_LOW + 1}]"]
-    out.append(f"s_mov_b32 s{S_LOADED}, -1")
+    # the lowest adapter above the one before
+    out += [f"s_mov_b32 s{S_PREV}, -1", "ADAPTER_%=:"]
     for tj in range(mt):
-        out += [f"s_mov_b32 s{S_PREV}, -1", f"ADAPTER{tj}_%=:",
-                # the lowest adapter above the one before
-                f"v_cmp_lt_i32 vcc, s{S_PREV}, {V(INDEX + tj)}", "s_nop 1", f"v_cndmask_b32 {V(AT)}, {V(AMAX)}, {V(INDEX + tj)}, vcc"]
-        for how in ("quad_perm:[1,0,3,2]", "quad_perm:[2,3,0,1]", "row_half_mirror", "row_mirror"):
-            out += ["s_nop 1", f"v_min_i32_dpp {V(AT)}, {V(AT)}, {V(AT)} {how} row_mask:0xf bank_mask:0xf"]
-        out += ["s_nop 3", f"v_readfirstlane_b32 s{S_G}, {V(AT)}", "s_nop 3", f"s_cmp_eq_u32 s{S_G}, 0x7fffffff", "s_nop 0", f"s_cbranch_scc1 ROWS{tj}_%=",
-                f"s_cmp_eq_u32 s{S_G}, s{S_LOADED}", "s_nop 0", f"s_cbranch_scc1 LOADED{tj}_%=",
-                f"s_getpc_b64 s[{S_BACK}:{S_BACK + 1}]", f"PCA{tj}_%=:", f"s_add_u32 s{S_BACK}, s{S_BACK}, LOADED{tj}_%=-PCA{tj}_%=",
-                f"s_addc_u32 s{S_BACK + 1}, s{S_BACK + 1}, 0", "s_branch LOADADAPTER_%=",
-                f"LOADED{tj}_%=:", "s_waitcnt vmcnt(0)", f"v_cmp_eq_u32 s[{S_MINE}:{S_MINE + 1}], s{S_G}, {V(INDEX + tj)}", "s_nop 3",
-                f"s_cmp_eq_u64 s[{S_MINE}:{S_MINE + 1}], -1", "s_nop 0", f"s_cbranch_scc1 ALL{tj}_%="]
-        for ti in range(8):
-            acc = 4 * (mt * ti + tj)
-            out += [f"{MFMA['adapted']} {V(ASUM, 4)}, {V(ADAPTER + 4 * ti, 4)}, {V(LOW + 4 * tj, 4)}, 0", "s_nop 15", "s_nop 7"]
-            for r in range(4):
-                out += [f"v_accvgpr_read_b32 {V(ASUM + 4)}, {A(acc + r)}", f"v_add_f32 {V(ASUM + r)}, {V(ASUM + 4)}, {V(ASUM + r)}",
-                        f"v_cndmask_b32_e64 {V(ASUM + r)}, {V(ASUM + 4)}, {V(ASUM + r)}, s[{S_MINE}:{S_MINE + 1}]", f"v_accvgpr_write_b32 {A(acc + r)}, {V(ASUM + r)}"]
-        out += [f"s_mov_b32 s{S_PREV}, s{S_G}", f"s_branch ADAPTER{tj}_%=", f"ALL{tj}_%=:"]
-        for ti in range(8):
-            acc = A(4 * (mt * ti + tj), 4)
-            out.append(f"{MFMA['adapted']} {acc}, {V(ADAPTER + 4 * ti, 4)}, {V(LOW + 4 * tj, 4)}, {acc}")
-        out.append(f"ROWS{tj}_%=:")
-    return out + ["s_nop 15", "s_nop 15", f"s_add_u32 s{S_KK}, s{S_KK}, 64", f"s_cmp_lt_u32 s{S_KK}, %[rank2]", "s_nop 0", "s_cbranch_scc1 RANK_%=", "ADAPTED_%=:"]
-
-
-def load_adapter_lines():
-    """adapted, out of line: the fragments of adapter S_G for the wave's eight sub-tiles over n (rows past the end re-read the last one)"""
-    out = ["LOADADAPTER_%=:", f"s_mul_i32 s{S_X}, s{S_G}, %[N]", f"s_mul_i32 s{S_UP}, s{S_X}, %[rank2]", f"s_mul_hi_u32 s{S_UP + 1}, s{S_X}, %[rank2]",
-           f"s_add_u32 s{S_UP}, s{S_UP}, %[up_lo]", f"s_addc_u32 s{S_UP + 1}, s{S_UP + 1}, %[up_hi]", f"s_sub_u32 s{S_X}, %[N], 1"]
+        to = AT if tj == 0 else ASUM
+        out += [f"v_cmp_lt_i32 vcc, s{S_PREV}, {V(INDEX + tj)}", "s_nop 1", f"v_cndmask_b32 {V(to)}, {V(AMAX)}, {V(INDEX + tj)}, vcc"]
+        if tj:
+            out.append(f"v_min_i32 {V(AT)}, {V(AT)}, {V(to)}")
+    for how in ("quad_perm:[1,0,3,2]", "quad_perm:[2,3,0,1]", "row_half_mirror", "row_mirror"):
+        out += ["s_nop 1", f"v_min_i32_dpp {V(AT)}, {V(AT)}, {V(AT)} {how} row_mask:0xf bank_mask:0xf"]
+    out += ["s_nop 3", f"v_readfirstlane_b32 s{S_G}, {V(AT)}", "s_nop 3", f"s_cmp_eq_u32 s{S_G}, 0x7fffffff", "s_nop 0", "s_cbranch_scc1 NEXTRANK_%=",
+            # its fragments for the wave's eight sub-tiles over n (rows past the end re-read the last one)
+            f"s_mul_i32 s{S_X}, s{S_G}, %[N]", f"s_mul_i32 s{S_UP}, s{S_X}, %[rank2]", f"s_mul_hi_u32 s{S_UP + 1}, s{S_X}, %[rank2]",
+            f"s_add_u32 s{S_UP}, s{S_UP}, %[up_lo]", f"s_addc_u32 s{S_UP + 1}, s{S_UP + 1}, %[up_hi]", f"s_sub_u32 s{S_X}, %[N], 1"]
     for ti in range(8):
         out += [f"v_add_u32 {V(AT)}, {32 * (ti // 2) + 4 * (ti % 2)}, {V(AROW)}", f"v_min_u32 {V(AT)}, s{S_X}, {V(AT)}",
                 f"v_mul_u32_u24 {V(AT)}, %[rank2], {V(AT)}", f"v_add_u32 {V(AT)}, {V(AGRP)}, {V(AT)}", f"v_add_u32 {V(AT)}, s{S_KK}, {V(AT)}",
                 f"global_load_dwordx4 {V(ADAPTER + 4 * ti, 4)}, {V(AT)}, s[{S_UP}:{S_UP + 1}]"]
-    return out + [f"s_mov_b32 s{S_LOADED}, s{S_G}", f"s_setpc_b64 s[{S_BACK}:{S_BACK + 1}]"]
+    out.append("s_waitcnt vmcnt(0)")
+    for tj in range(mt):
+        mine = f"s[{S_MINE}:{S_MINE + 1}]"
+        out += [f"v_cmp_eq_u32 {mine}, s{S_G}, {V(INDEX + tj)}", "s_nop 3", f"s_cmp_eq_u64 {mine}, 0", "s_nop 0", f"s_cbranch_scc1 ROWS{tj}_%=",
+                f"s_cmp_eq_u64 {mine}, -1", "s_nop 0", f"s_cbranch_scc1 ALL{tj}_%="]
+        for first in (0, 4):
+            for i in range(4):
+                out.append(f"{MFMA['adapted']} {V(ASUM + 4 * i, 4)}, {V(ADAPTER + 4 * (first + i), 4)}, {V(LOW + 4 * tj, 4)}, 0")
+            out += ["s_nop 15", "s_nop 7"]
+            for i in range(4):
+                for r in range(4):
+                    acc, v = A(4 * (mt * (first + i) + tj) + r), ASUM + 4 * i + r
+                    out += [f"v_accvgpr_read_b32 {V(AOLD)}, {acc}", f"v_add_f32 {V(v)}, {V(AOLD)}, {V(v)}",
+                            f"v_cndmask_b32_e64 {V(v)}, {V(AOLD)}, {V(v)}, {mine}", f"v_accvgpr_write_b32 {acc}, {V(v)}"]
+        out += [f"s_branch ROWS{tj}_%=", f"ALL{tj}_%=:"]
+        for ti in range(8):
+            acc = A(4 * (mt * ti + tj), 4)
+            out.append(f"{MFMA['adapted']} {acc}, {V(ADAPTER + 4 * ti, 4)}, {V(LOW + 4 * tj, 4)}, {acc}")
+        out.append(f"ROWS{tj}_%=:")
+    return out + [f"s_mov_b32 s{S_PREV}, s{S_G}", "s_nop 15", "s_branch ADAPTER_%=", "NEXTRANK_%=:", "s_nop 15", "s_nop 15", f"s_add_u32 s{S_KK}, s{S_KK}, 64",
+                  f"s_cmp_lt_u32 s{S_KK}, %[rank2]", "s_nop 0", "s_cbranch_scc1 RANK_%=", "ADAPTED_%=:"]
 
 
 def result_lines(mt, kind="plain"):
@@ -505,8 +507,6 @@ def generate(mt=8, kind="plain"):
     L += ["TILEW_%=:"] + next_tile_lines(0, mt, kind) + ["TILEX_%=:"] + next_tile_lines(1, mt, kind)
     # a tile ends, or its last two stages begin: X of those behind them is the next tile's
     L += ["PAIR_%=:", f"s_cmp_eq_u32 s{S_TRIPS}, 1", "s_nop 0", "s_cbranch_scc1 TILEX_%="] + result_lines(mt, kind)
-    if kind == "adapted":
-        L += load_adapter_lines()
     e("DONE_%=:")
     return L
 
