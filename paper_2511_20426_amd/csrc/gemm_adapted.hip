@@ -505,14 +505,16 @@ struct SumArgs {
 };
 constexpr int kSumCols = 128, kSumStep = 32, kMostAdapters = 4096;
 
-// parts[g][r][c] = sum over a split's rows that have adapter g of low[m][r] wide[m][c].  A workgroup takes 128 columns, 32 rows at a time through LDS, from
-// where the lanes collect 8 rows of a column each, as the matrix instruction takes them (rows in steps of 4 bytes more than whole lines lie in other
-// banks); the next rows are on their way meanwhile.  Rows of other adapters are zeros on both sides.
+// parts[g][r][c] = sum over a split's rows that have adapter g of low[m][r] wide[m][c].  A workgroup takes 128 columns, 32 rows at a time through LDS, where
+// two rows share a dword, so that a lane collects the 8 rows of a column that the matrix instruction takes by four reads (pairs of rows in steps of four
+// dwords more than whole lines lie in other banks; by eight reads of 16 bits 4680 rows of 4608 columns took 17 us); the next rows are on their way
+// meanwhile.  Rows of other adapters are zeros on both sides.
 template <int kTn>
 __global__ __launch_bounds__(256) void adapted_sum_kernel(SumArgs a) {
-  constexpr int kRank = 16 * kTn, kPitchW = kSumCols * 2 + 4, kPitchL = kRank * 4 + 4, kChunksL = kRank / 4, kLoadsL = kChunksL * kSumStep / 256;
-  __shared__ __attribute__((aligned(16))) uint8_t wide[kSumStep * kPitchW];
-  __shared__ __attribute__((aligned(16))) uint8_t low[kSumStep * kPitchL];
+  constexpr int kRank = 16 * kTn, kPairs = kSumStep / 2, kPitchW = kSumCols + 4, kPitchL = 2 * kRank + 4;
+  constexpr int kChunksL = kRank / 4, kLoadsL = (kChunksL * kPairs + 255) / 256;     // eight values of a pair of rows, both parts of T side by side
+  __shared__ __attribute__((aligned(16))) uint32_t wide[kPairs * kPitchW];
+  __shared__ __attribute__((aligned(16))) uint32_t low[kPairs * kPitchL];
   __shared__ uint8_t there[kMostAdapters];
   __shared__ int lowest[4];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, l15 = lane & 15, grp = lane >> 4;
@@ -541,64 +543,68 @@ __global__ __launch_bounds__(256) void adapted_sum_kernel(SumArgs a) {
     for (int i = 0; i < 2; ++i)
 #pragma unroll
       for (int n = 0; n < kTn; ++n) acc[i][n] = Sums{0, 0, 0, 0};
-    // rows from m on, of the first 32 that hold any of the adapter's; which of them, in `rows`
+    // rows from m on, of the first 32 that hold any of the adapter's; which of them, in `rows`.  The adapters of the 32 rows behind them are asked for with
+    // them: waited for where they are needed, each step took an index' way from memory more.
     uint32_t rows = 0;
+    int ahead = -1, ahead_at = -1;
+    auto adapters_at = [&](int m) { return lane < kSumStep && m + lane < end ? a.index[m + lane] : -1; };
     auto find = [&](int m) {
       for (; m < end; m += kSumStep) {
-        const int of = lane < kSumStep && m + lane < end ? a.index[m + lane] : -1;
-        rows = uint32_t(__ballot(of == g));
+        rows = uint32_t(__ballot((m == ahead_at ? ahead : adapters_at(m)) == g));
         if (rows) break;
       }
+      ahead_at = m + kSumStep;
+      ahead = adapters_at(ahead_at);
       return m;
     };
-    U4 held_w[2], held_l[kLoadsL];
+    U4 held_w[2], held_l[kLoadsL][2];
     auto request = [&](int m) {
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const int at = tid + 256 * i, row = at / 16, col = c0 + at % 16 * 8;
-        held_w[i] = U4{0, 0, 0, 0};
-        if ((rows >> row & 1) && col < a.C) held_w[i] = *reinterpret_cast<const U4*>(a.wide + int64_t(m + row) * a.ld + col);
+      for (int p = 0; p < 2; ++p) {
+        const int row = tid / 16 * 2 + p, col = c0 + tid % 16 * 8;
+        held_w[p] = U4{0, 0, 0, 0};
+        if ((rows >> row & 1) && col < a.C) held_w[p] = *reinterpret_cast<const U4*>(a.wide + int64_t(m + row) * a.ld + col);
       }
 #pragma unroll
-      for (int i = 0; i < kLoadsL; ++i) {
-        const int at = tid + 256 * i, row = at / kChunksL, of = at % kChunksL;        // the two of a row side by side
-        held_l[i] = U4{0, 0, 0, 0};
-        if (rows >> row & 1)
-          held_l[i] = *reinterpret_cast<const U4*>(a.low + (int64_t(of >= kChunksL / 2) * a.M + m + row) * kRank + of % (kChunksL / 2) * 8);
-      }
+      for (int i = 0; i < kLoadsL; ++i)
+#pragma unroll
+        for (int p = 0; p < 2; ++p) {
+          const int at = tid + 256 * i, row = at / kChunksL * 2 + p, of = at % kChunksL;
+          held_l[i][p] = U4{0, 0, 0, 0};
+          if (row < kSumStep && (rows >> row & 1))
+            held_l[i][p] = *reinterpret_cast<const U4*>(a.low + (int64_t(of >= kChunksL / 2) * a.M + m + row) * kRank + of % (kChunksL / 2) * 8);
+        }
+    };
+    auto put = [](uint32_t* to, const U4& x, const U4& y) {         // dword c: value c of the one row and of the other
+      const uint32_t a[4] = {x.x, x.y, x.z, x.w}, b[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+        *reinterpret_cast<u32x4*>(to + 4 * h) = u32x4{(a[2 * h] & 0xffffu) | b[2 * h] << 16, a[2 * h] >> 16 | (b[2 * h] & 0xffff0000u),
+                                                      (a[2 * h + 1] & 0xffffu) | b[2 * h + 1] << 16, a[2 * h + 1] >> 16 | (b[2 * h + 1] & 0xffff0000u)};
     };
     int m = find(begin);
     request(m);                                                     // (there is one)
     while (m < end) {
       __syncthreads();
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const int at = tid + 256 * i;
-        uint32_t* const to = reinterpret_cast<uint32_t*>(wide + at / 16 * kPitchW + at % 16 * 16);
-        to[0] = held_w[i].x; to[1] = held_w[i].y; to[2] = held_w[i].z; to[3] = held_w[i].w;
-      }
+      put(wide + tid / 16 * kPitchW + tid % 16 * 8, held_w[0], held_w[1]);
 #pragma unroll
       for (int i = 0; i < kLoadsL; ++i) {
         const int at = tid + 256 * i;
-        uint32_t* const to = reinterpret_cast<uint32_t*>(low + at / kChunksL * kPitchL + at % kChunksL * 16);
-        to[0] = held_l[i].x; to[1] = held_l[i].y; to[2] = held_l[i].z; to[3] = held_l[i].w;
+        if (at < kChunksL * kPairs) put(low + at / kChunksL * kPitchL + at % kChunksL * 8, held_l[i][0], held_l[i][1]);
       }
       __syncthreads();
       m = find(m + kSumStep);
       if (m < end) request(m);
-      auto column = [&](const uint8_t* from, int pitch) {           // rows 8 grp .. +7 of a column
-        uint32_t v[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = *reinterpret_cast<const uint16_t*>(from + (8 * grp + e) * pitch);
-        const u32x4 two = {v[0] | v[1] << 16, v[2] | v[3] << 16, v[4] | v[5] << 16, v[6] | v[7] << 16};
-        return __builtin_bit_cast(Frag, two);
+      auto column = [&](const uint32_t* from, int pitch) {          // rows 8 grp .. +7 of a column
+        const u32x4 v = {from[4 * grp * pitch], from[(4 * grp + 1) * pitch], from[(4 * grp + 2) * pitch], from[(4 * grp + 3) * pitch]};
+        return __builtin_bit_cast(Frag, v);
       };
       Frag fw[2];
 #pragma unroll
-      for (int i = 0; i < 2; ++i) fw[i] = column(wide + (wave * 32 + i * 16 + l15) * 2, kPitchW);
+      for (int i = 0; i < 2; ++i) fw[i] = column(wide + wave * 32 + i * 16 + l15, kPitchW);
 #pragma unroll
       for (int n = 0; n < 2 * kTn; ++n) {
-        const Frag fl = column(low + (n * 16 + l15) * 2, kPitchL);
+        const Frag fl = column(low + n * 16 + l15, kPitchL);
 #pragma unroll
         for (int i = 0; i < 2; ++i) acc[i][n % kTn] = Bf16Products::multiply(fw[i], fl, acc[i][n % kTn]);
       }
@@ -643,31 +649,24 @@ __global__ __launch_bounds__(256) void adapted_join_kernel(const float* parts, c
   to[0] = uint16_t(two.x), to[1] = uint16_t(two.x >> 16), to[2] = uint16_t(two.y), to[3] = uint16_t(two.y >> 16);
 }
 
-// Transposed, out [adapters][C][R]: 32 columns and 32 rows of the rank to a workgroup, turned in LDS
-__global__ __launch_bounds__(256) void adapted_join_transposed_kernel(const float* parts, const int32_t* there, int splits, int adapters, int rank, int R, int C,
-                                                                      uint16_t* out) {
+// Transposed, out [adapters][C][R]: 32 columns and 32 rows of the rank to a workgroup, one of each to a thread, turned in LDS
+__global__ __launch_bounds__(1024) void adapted_join_transposed_kernel(const float* parts, const int32_t* there, int splits, int adapters, int rank, int R, int C,
+                                                                       uint16_t* out) {
   __shared__ float sums[32][33];
   const int x = threadIdx.x & 31, y = threadIdx.x >> 5, c0 = blockIdx.x * 32, r0 = blockIdx.y * 32, g = blockIdx.z;
-  float sum[4] = {0.f, 0.f, 0.f, 0.f};
+  float sum = 0.f;
   if (c0 + x < C) {
     const float* const from = parts + (int64_t(g) * rank + r0 + y) * C + c0 + x;      // (the rank has whole steps of 32 rows)
     const int64_t step = int64_t(adapters) * rank * C;
-#pragma unroll 4
+#pragma unroll 8
     for (int s = 0; s < splits; ++s) {
-      const bool adds = there[s * adapters + g] != 0;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const float one = from[s * step + int64_t(8 * i) * C];
-        sum[i] = adds ? sum[i] + one : sum[i];
-      }
+      const float one = from[s * step];
+      sum = there[s * adapters + g] != 0 ? sum + one : sum;
     }
   }
-#pragma unroll
-  for (int i = 0; i < 4; ++i) sums[y + 8 * i][x] = sum[i];
+  sums[y][x] = sum;
   __syncthreads();
-#pragma unroll
-  for (int i = 0; i < 4; ++i)
-    if (c0 + y + 8 * i < C && r0 + x < R) out[(int64_t(g) * C + c0 + y + 8 * i) * R + r0 + x] = uint16_t(pack_bf16(sums[x][y + 8 * i], 0.f));
+  if (c0 + y < C && r0 + x < R) out[(int64_t(g) * C + c0 + y) * R + r0 + x] = uint16_t(pack_bf16(sums[x][y], 0.f));
 }
 
 // [rows][cols] of each adapter to [cols][rows], of up to two of them
@@ -836,7 +835,7 @@ int32_t launch_adapter_sum(const uint16_t* low, const void* wide, int64_t ld, co
   }
   uint16_t* const to = static_cast<uint16_t*>(out);
   if (transposed)
-    hipLaunchKernelGGL(adapted_join_transposed_kernel, dim3(unsigned((C + 31) / 32), unsigned((rank_used + 31) / 32), unsigned(adapters)), dim3(256), 0, s, parts, there,
+    hipLaunchKernelGGL(adapted_join_transposed_kernel, dim3(unsigned((C + 31) / 32), unsigned((rank_used + 31) / 32), unsigned(adapters)), dim3(1024), 0, s, parts, there,
                        splits, adapters, rank, rank_used, C, to);
   else
     hipLaunchKernelGGL(adapted_join_kernel, dim3(unsigned((C + 255) / 256), unsigned(rank_used), unsigned(adapters)), dim3(256), 0, s, parts, there, splits, adapters,
