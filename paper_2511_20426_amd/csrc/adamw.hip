@@ -2,7 +2,8 @@
 //
 //   m = b1 m + (1 - b1) g,  v = b2 v + (1 - b2) g^2,  p = (1 - lr wd) p - lr / (1 - b1^t) m / (sqrt(v / (1 - b2^t)) + eps)
 //
-// Memory bound: each value is read and written once where it lies.  States in 8 bits are codes with a scale a (fp32) for every 256 values of a
+// Memory bound: each value is read and written once where it lies (3 x 13824 x 5120 values in bf16: states in 32 bits 900 us, 5.2 TB/s, the rate of a
+// copy; in 8 bits 550, 3.9 TB/s, where some 70 instructions a value share the time with the memory).  States in 8 bits are codes with a scale a (fp32) for every 256 values of a
 // tensor: m = sign(c) a (c / 127)^2, v = a (c / 255)^4.  The square and the fourth power give small magnitudes finer steps: a code is off by at most half
 // of one, 1 / c of m and 2 / c of v, where equal steps would leave nothing of what is 250 times smaller than the block's largest; and a v above zero
 // keeps a code above zero, so that no step divides by eps alone.  With states in 8 bits m and v are computed in 64 bits, at the rate of fp32 here, so

@@ -8,6 +8,9 @@
 // signs, which is a small part of it.  The adapters' gradients are sums of nothing else, so that what the rounding left, in bf16 too, is kept beside T for
 // them: with T alone they were 2.35e-3 of their norm off, 1.66e-3 with both, which is their own rounding.)  An adapter's products go to sums of their own and are added for the rows that have it, so that no value of one request's adapter, not
 // even an infinity, touches another's rows.  What adapters a tile's rows have is found in the tile: any order and number works, runs of rows cost least.
+// Bound as the plain product by the matrix pipe (23400 x 15360 x 5120 of five adapters of rank 32, in runs, T 78 us and the product 2480, where the plain one
+// takes 2430), of few rows by the weights' way from memory; rows in any order of eight adapters cost twice to three times as much (23400 x 1536 x 1536 287 us
+// for 127 in runs and 84 without).
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
