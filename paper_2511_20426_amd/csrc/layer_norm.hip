@@ -4,11 +4,11 @@
 //   dn = dy w,  dx = r (dn - mean(dn) - n mean(dn n)),  dw = sum over a group's rows of dy n,  db = of dy
 //
 // Memory bound: forward reads x and writes y once, backward reads x and dy and writes dx.  A row stays in registers (as it is stored), of 64
-// threads up to a width of 2048, of 256 up to 8192, of 1024 up to 32768; a workgroup goes from row to row of a group, so that the weights are
-// loaded once and the sums of the weights' gradients stay in registers too (23400 x 5120 in five groups forward 92.5 us, 5.2 TB/s, the rate of a
-// copy; backward with the weights' gradients 186, 3.9 TB/s; 4680 x 1536 7.9 and 17.8).  Statistics are fp32 in two steps: the mean, then squares and
-// sum of what is left, whose mean corrects the first one, so that rows far from zero lose nothing.  The gradients of the weights are summed by
-// a thread over its rows, over a workgroup's waves in LDS and over the workgroups by a second launch in fp64, in an order that the sizes fix.
+// threads up to a width of 2560, of 256 up to 12288, of 1024 up to 32768; a workgroup goes from row to row of a group, so that the weights are
+// loaded once and the sums of the weights' gradients stay in registers too (bf16, 23400 x 5120 in five groups forward 82 us, 5.8 TB/s, some of it from
+// the last cache; backward with the weights' gradients 140, 5.1 TB/s, the rate of a copy; 4680 x 1536 7.6 and 17.6).  Statistics are fp32 in two steps: the
+// mean, then squares and sum of what is left, whose mean corrects the first one, so that rows far from zero lose nothing.  The gradients of the weights are
+// summed by a thread over its rows, over a workgroup's waves in LDS and over the workgroups by a second launch in fp64, in an order that the sizes fix.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -235,7 +235,7 @@ template <typename T, typename W, int kWaves, int kPieces, bool kWhole>
 __global__ __launch_bounds__(kWaves == 1 ? 256 : 64 * kWaves) void layer_norm_backward_kernel(RowNormArgs a) {
   using Shape = RowShape<kWaves, kPieces, kWhole>;
   __shared__ float2 room[3 * kWaves];
-  __shared__ float sums[kWaves == 1 ? 2 : 1][kWaves == 1 ? 2 : 1][kWaves == 1 ? 512 * kPieces : 1];
+  __shared__ float sums[kWaves == 1 ? 2 : 1][kWaves == 1 ? 512 * kPieces : 1];
   const int t = threadIdx.x % Shape::kThreads;
   const int group = blockIdx.x / unsigned(a.per_group), nth = blockIdx.x - group * a.per_group;
   const int64_t first = int64_t(group) * a.group_rows;
@@ -247,7 +247,7 @@ __global__ __launch_bounds__(kWaves == 1 ? 256 : 64 * kWaves) void layer_norm_ba
 #pragma unroll
     for (int j = 0; j < 8; ++j) dw[i][j] = db[i][j] = 0.f;
   // A wave asks for its next row ahead of the work on one (4680 x 1536 22.3 -> 19.1 us with 256 workgroups); rows of several waves are not: the registers
-  // cost them a workgroup of four on a CU (23400 x 5120 185 us, 222 so)
+  // cost them a workgroup on a CU (23400 x 5120 185 us with 512 of them, 222 so)
   constexpr bool kNext = kWaves == 1;
   Piece<T> next_x[kPieces], next_d[kPieces];
   auto request = [&](int64_t n) {
@@ -302,36 +302,41 @@ __global__ __launch_bounds__(kWaves == 1 ? 256 : 64 * kWaves) void layer_norm_ba
   float* const to[2] = {a.dw ? a.dw + part : nullptr, a.db ? a.db + part : nullptr};
   if constexpr (kWaves == 1) {                                      // four waves' sums: those of two go to the other two, then one's to the other
     const int wave = threadIdx.x >> 6;
+    auto place = [&](int i, int j) { return (i * 8 + j) * 64 + t; };                // (of its own to each, of whatever column)
+    auto join = [&](float (&mine)[kPieces][8], float* out) {                        // (all four waves have the same `out`)
+      if (!out) return;
 #pragma unroll
-    for (int half = 2; half > 0; half /= 2) {
-      if (wave >= half && wave < 2 * half) {
+      for (int half = 2; half > 0; half /= 2) {
+        if (wave >= half && wave < 2 * half) {
+#pragma unroll
+          for (int i = 0; i < kPieces; ++i)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) sums[wave - half][place(i, j)] = mine[i][j];
+        }
+        __syncthreads();
+        if (wave < half) {
+#pragma unroll
+          for (int i = 0; i < kPieces; ++i)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) mine[i][j] += sums[wave][place(i, j)];
+        }
+        __syncthreads();
+      }
+      if (wave == 0) {
 #pragma unroll
         for (int i = 0; i < kPieces; ++i)
 #pragma unroll
-          for (int j = 0; j < 8; ++j) sums[wave - half][0][(i * 8 + j) * 64 + t] = dw[i][j], sums[wave - half][1][(i * 8 + j) * 64 + t] = db[i][j];
+          for (int j = 0; j < 8; ++j) sums[0][place(i, j)] = mine[i][j];
       }
       __syncthreads();
-      if (wave < half) {
-#pragma unroll
-        for (int i = 0; i < kPieces; ++i)
-#pragma unroll
-          for (int j = 0; j < 8; ++j) dw[i][j] += sums[wave][0][(i * 8 + j) * 64 + t], db[i][j] += sums[wave][1][(i * 8 + j) * 64 + t];
+      for (int k = threadIdx.x; k < 512 * kPieces; k += 256) {
+        const int lane = k % 64, i = k / 512, j = k / 64 % 8, col = Shape::at(lane, i) + j * Shape::kStep;
+        if (col < a.width) out[col] = sums[0][k];
       }
       __syncthreads();
-    }
-    if (wave == 0) {
-#pragma unroll
-      for (int i = 0; i < kPieces; ++i)
-#pragma unroll
-        for (int j = 0; j < 8; ++j) sums[0][0][(i * 8 + j) * 64 + t] = dw[i][j], sums[0][1][(i * 8 + j) * 64 + t] = db[i][j];
-    }
-    __syncthreads();
-    for (int k = threadIdx.x; k < 512 * kPieces; k += 256) {        // (a place of its own to each, of whatever column)
-      const int lane = k % 64, i = k / 512, j = k / 64 % 8, col = Shape::at(lane, i) + j * Shape::kStep;
-      if (col >= a.width) continue;
-      if (to[0]) to[0][col] = sums[0][0][k];
-      if (to[1]) to[1][col] = sums[0][1][k];
-    }
+    };
+    join(dw, to[0]);
+    join(db, to[1]);
   } else {
 #pragma unroll
     for (int i = 0; i < kPieces; ++i)
@@ -386,8 +391,10 @@ RowKernel row_kernel_of(bool whole) {
     return whole ? layer_norm_kernel<T, W, kWaves, kPieces, true> : layer_norm_kernel<T, W, kWaves, kPieces, false>;
 }
 
-// Threads of a row
-int row_waves(int width) { return width <= 2048 ? 1 : width <= 8192 ? 4 : 16; }
+// Waves of a row.  Few wait for each other's sums less, many hold a row in fewer registers.  Us forward / backward, 23400 rows in bf16 by one wave and by four:
+// 2560 42.8 / 71 and 49.8 / 115, 3584 59 / 105 and 62 / 124 but 4680 rows 16.6 / 32.4 and 14.9 / 39.6, 4096 90 / 124 and 69 / 130 (in fp32 3584 136 / 200 and
+// 149 / 173); by four and by sixteen: 8192 129 / 200 and 149 / 327, 12288 203 / 401 and 270 / 431, 16384 359 / 590 and 305 / 493.  (Two: 5120 98 forward.)
+int row_waves(int width) { return width <= 2560 ? 1 : width <= 12288 ? 4 : 16; }
 
 template <bool kBackward, typename T, typename W>
 RowKernel pick_row_kernel(int width, bool whole) {
@@ -396,9 +403,12 @@ RowKernel pick_row_kernel(int width, bool whole) {
     case 8 + 2: return row_kernel_of<kBackward, T, W, 1, 2>(whole);
     case 8 + 3: return row_kernel_of<kBackward, T, W, 1, 3>(whole);
     case 8 + 4: return row_kernel_of<kBackward, T, W, 1, 4>(whole);
+    case 8 + 5: return row_kernel_of<kBackward, T, W, 1, 5>(whole);
     case 32 + 2: return row_kernel_of<kBackward, T, W, 4, 2>(whole);
     case 32 + 3: return row_kernel_of<kBackward, T, W, 4, 3>(whole);
     case 32 + 4: return row_kernel_of<kBackward, T, W, 4, 4>(whole);
+    case 32 + 5: return row_kernel_of<kBackward, T, W, 4, 5>(whole);
+    case 32 + 6: return row_kernel_of<kBackward, T, W, 4, 6>(whole);
     case 128 + 2: return row_kernel_of<kBackward, T, W, 16, 2>(whole);
     case 128 + 3: return row_kernel_of<kBackward, T, W, 16, 3>(whole);
     default: return row_kernel_of<kBackward, T, W, 16, 4>(whole);
@@ -412,16 +422,24 @@ RowKernel pick_row_kernel(int dtype, int w_dtype, int width, bool whole) {
   return pick_row_kernel<kBackward, uint16_t, uint16_t>(width, whole);
 }
 
-// Workgroups of a group: enough to fill the chip, no more than there are rows for
+// Workgroups of a group: enough to fill the chip, no more than there are rows for.  (`all` is not passed: 515 of them where 512 are on the chip at a time
+// cost a second round, 23400 x 5120 in five groups backward 179 us and 160 with 510, 12288 587 and 431.)
 int per_group(int64_t group_rows, int64_t groups, int width, int all) {
   const int64_t rows = row_waves(width) == 1 ? 4 : 1, most = (group_rows + rows - 1) / rows;
-  return int(std::max<int64_t>(1, std::min(most, (all + groups - 1) / groups)));
+  return int(std::max<int64_t>(1, std::min(most, all / groups)));
 }
+// (forward, 512 / 1024 / 2048 / 4096, us in bf16: 23400 x 1024 20.6 / 17.5 / 17.5 / 17.6, 23400 x 5120 100 / 81 / 83 / 83, 4680 x 5120 22.7 / 18.5 / 20.2 /
+// 21.8, 23400 x 8192 128 / 169 / 128 / 130)
 constexpr int kForwardGroups = 2048;
-// ... of a backward launch, each of which leaves its part of the weights' gradients for the second launch to read.  Us of both with 256 / 512 / 1024 in
-// bf16: 4680 x 1536 17.8 / 18.8 / 32, 23400 x 1536 51 / 44.5 / 55, rows of several waves 4680 x 5120 63 / 52 / 69, 23400 x 5120 in five groups
-// 274 / 185 / 188 (3.9 TB/s: each row waits for three sums over its waves).
-int backward_groups(int64_t rows, int width) { return row_waves(width) == 1 && rows * width <= (int64_t(1) << 24) ? 256 : 512; }
+// Of a backward launch as many as are on the chip at a time, each of which leaves its part of the weights' gradients for the second launch to read, so
+// that few rows are dealt to fewer.  Us of both with 256 / 512 / 768 in bf16: 1500 x 1536 12.5 / 13.2 / 13.1, 4680 x 1536 17.9 / 17.8 / 23.6, 23400 x 1536
+// 48 / 40 / 48, 23400 x 2560 64 / 72 / 79; 1500 x 5120 30 / 33 / 40, 4680 x 5120 62 / 50 / 53, 23400 x 5120 240 / 156 / 136, 23400 x 8192 292 / 199 / 231,
+// 23400 x 12288 401 / 419 / 438; in fp32 23400 x 1536 74 / 84 / 86, 23400 x 5120 343 / 243 / 282.
+int backward_groups(int64_t rows, int width, int dtype) {
+  const int waves = row_waves(width), pieces = (width + 512 * waves - 1) / (512 * waves);
+  const int resident = pieces > 4 || waves == 16 ? 1 : waves == 1 ? (dtype == CA_BF16 && pieces <= 3 ? 2 : 1) : dtype == CA_BF16 && pieces <= 3 ? 3 : 2;
+  return 256 * int(std::min<int64_t>(resident, std::max<int64_t>(1, rows / 2048)));
+}
 
 bool aligned(const void* p, int64_t ld, int64_t rows, int bytes_of_value) {
   return reinterpret_cast<uintptr_t>(p) % 16 == 0 && (rows <= 1 || ld * bytes_of_value % 16 == 0);
@@ -446,7 +464,7 @@ int32_t launch_layer_norm(const RowNorm& n, const void* y, void* stream) {
 }
 
 size_t layer_norm_backward_bytes(int64_t rows, int32_t width, int64_t groups) {
-  const int parts = rows > 0 ? per_group(rows / groups, groups, width, backward_groups(rows, width)) : 1;
+  const int parts = rows > 0 ? per_group(rows / groups, groups, width, backward_groups(rows, width, CA_BF16)) : 1;
   return parts > 1 ? size_t(groups) * parts * 2 * width * sizeof(float) : 0;
 }
 
@@ -463,7 +481,7 @@ int32_t launch_layer_norm_backward(const RowNorm& n, const void* dy, int64_t ldd
   a.x = n.x; a.dy = dy; a.w = n.w; a.y = dx;
   a.ldx = n.ldx; a.lddy = lddy; a.ldy = n.ldy; a.ldw = n.ldw;
   a.width = n.width; a.groups = int32_t(n.groups); a.group_rows = int32_t(n.rows / n.groups); a.eps = n.eps;
-  a.per_group = per_group(a.group_rows, n.groups, n.width, backward_groups(n.rows, n.width));
+  a.per_group = per_group(a.group_rows, n.groups, n.width, backward_groups(n.rows, n.width, n.dtype));
   float* const parts = static_cast<float*>(workspace);
   const bool split = a.per_group > 1;
   if (dw) a.dw = split ? parts : dw;

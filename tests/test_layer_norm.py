@@ -7,8 +7,8 @@ from paper_2511_20426_amd import binding as B
 HALF = {torch.bfloat16: 2.0 ** -8, torch.float32: 2.0 ** -24}        # a rounding, relative: half a step
 DEV = "cuda:0"
 T = {"bf16": torch.bfloat16, "f32": torch.float32}
-# A thread adds 8 values of up to four pieces, six exchanges join a wave and up to 16 additions its row: a chain of at most 32 + 6 + 16 fp32
-# roundings of the sum of magnitudes, in the mean and in the squares (of which the root halves the error); products, root and quotient
+# A thread adds 8 values of up to six pieces, six exchanges join a wave and up to 16 additions its row: a chain of at most 48 + 6 + 4 fp32
+# roundings (four waves of six pieces; sixteen have up to four: 32 + 6 + 16) of the sum of magnitudes, in the mean and in the squares (of which the root halves the error); products, root and quotient
 # are some ten more.
 WAY = 72 * 2.0 ** -24
 
@@ -38,7 +38,11 @@ def _by_row(t, rows, width):
 # rows, width, groups, type, the weights' type: single values and rows, odd widths, the borders of a wave's, four waves' and sixteen waves' rows
 NORMS = [(1, 1, 1, "bf16", "f32"), (3, 5, 1, "f32", "f32"), (1, 5120, 1, "bf16", "bf16"), (9, 8, 3, "bf16", "f32"), (433, 129, 1, "f32", "f32"),
          (6, 2048, 3, "bf16", "f32"), (7, 2047, 7, "bf16", "bf16"), (10, 2056, 5, "f32", "f32"), (5, 8192, 1, "bf16", "f32"), (4, 8193, 2, "bf16", "f32"),
-         (3, 32768, 1, "f32", "f32"), (2, 30001, 1, "bf16", "bf16"), (1205, 1536, 5, "bf16", "f32"), (600, 4096, 2, "bf16", "f32"), (70, 520, 1, "bf16", "bf16")]
+         (3, 32768, 1, "f32", "f32"), (2, 30001, 1, "bf16", "bf16"), (1205, 1536, 5, "bf16", "f32"), (600, 4096, 2, "bf16", "f32"), (70, 520, 1, "bf16", "bf16"),
+         (12, 2560, 3, "bf16", "f32"), (7, 2561, 1, "f32", "f32"), (9, 2553, 1, "f32", "f32"), (6, 10240, 2, "bf16", "bf16"), (5, 10233, 1, "f32", "f32"),
+         (5, 12288, 1, "bf16", "f32"), (6, 12281, 1, "f32", "f32"), (4, 12289, 2, "bf16", "bf16"), (5, 16384, 1, "f32", "f32"),
+         # as many rows as are dealt to two and three workgroups on a CU, and groups that they do not come out even for
+         (4705, 264, 5, "bf16", "f32"), (6150, 2568, 3, "bf16", "bf16"), (4100, 2568, 1, "f32", "f32"), (1030, 8, 515, "bf16", "f32")]
 
 
 def _case(rows, width, groups, dtype, w_dtype):
@@ -91,7 +95,7 @@ def test_gradients(rows, width, groups, dtype, w_dtype):
     ref, bound, dwr, dwo = _grads(dy.double().cpu(), x.double().cpu(), _by_row(weight, rows, width), 1e-6)
     assert dx.dtype == x.dtype and ((dx.double().cpu() - ref).abs() <= HALF[dx.dtype] * 1.01 * ref.abs() + bound + 1e-37).all()
     assert dw.shape == weight.shape and db.shape == bias.shape and dw.dtype == db.dtype == torch.float32
-    # a thread's rows (at most 600 here), four waves' and one rounding
+    # a thread's rows (at most the group's), four waves' and one rounding
     CHAIN = (rows // groups + 6) * 2.0 ** -24
     each = lambda t: t.reshape(groups, -1, width).sum(1)             # noqa: E731
     dyd = dy.double().cpu()
