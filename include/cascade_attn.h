@@ -370,7 +370,7 @@ int32_t layer_norm_backward(const void* dy_dev, const void* x_dev, int32_t dtype
  * adapters and more) y is x . w'.  Any order of adapters is right; runs of rows with the same one cost least.  A row's results depend on its own adapter
  * alone, whatever values others hold.  down: [adapters][rank][k_in], up: [adapters][n_out][rank], packed; rank 32, 64 or 128: rows and columns
  * behind an adapter's own rank are zeros.  scales: fp32.  Shapes, strides and alignment as layer_linear_bf16; adapters <= CA_MAX_ADAPTERS, columns up to
- * 2^20, rows up to 2^27.  workspace_dev: layer_linear_adapted_workspace() bytes (0 for more than a few rows). */
+ * 2^20, rows up to 2^27.  workspace_dev: layer_linear_adapted_workspace() bytes (0 for more than 512 rows). */
 #define CA_MAX_ADAPTERS 4096
 size_t layer_linear_adapted_workspace(int64_t m_rows, int32_t rank);
 int32_t layer_linear_adapted_bf16(const void* x_dev, const void* w_dev, const void* down_dev, const void* up_dev, const float* scales_dev,

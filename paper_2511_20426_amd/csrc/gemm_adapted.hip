@@ -4,13 +4,14 @@
 //
 // Two launches.  The first makes the few values T[m] = s_g X[m] A_g' (the rank: 32, 64 or 128 of them), rounded to bf16 as operands of the second,
 // which multiplies X and W as the plain linear map does and adds T's products with the rows of B to the same sums before they are rounded, so that
-// neither product is written or rounded by itself.  (T's rounding, up to 2^-8 of each of its values, is 2^-8 / sqrt(3) of the adapter's part of a sum of random
-// signs, which is a small part of it.  The adapters' gradients are sums of nothing else, so that what the rounding left, in bf16 too, is kept beside T for
-// them: with T alone they were 2.35e-3 of their norm off, 1.66e-3 with both, which is their own rounding.)  An adapter's products go to sums of their own and are added for the rows that have it, so that no value of one request's adapter, not
-// even an infinity, touches another's rows.  What adapters a tile's rows have is found in the tile: any order and number works, runs of rows cost least.
-// Bound as the plain product by the matrix pipe (23400 x 15360 x 5120 of five adapters of rank 32, in runs, T 78 us and the product 2480, where the plain one
-// takes 2430), of few rows by the weights' way from memory; rows in any order of eight adapters cost twice to three times as much (23400 x 1536 x 1536 287 us
-// for 127 in runs and 84 without).
+// neither product is written or rounded by itself.  (T's rounding, up to 2^-8 of each of its values, is 2^-8 / sqrt(3) of the adapter's part of a sum of
+// random signs, which is a small part of it.  The adapters' gradients are sums of nothing else, so that what the rounding left, in bf16 too, is kept beside T
+// for them: with T alone they were 2.35e-3 of their norm off, 1.66e-3 with both, which is their own rounding.)  An adapter's products go to sums of their
+// own and are added for the rows that have it, so that no value of one request's adapter, not even an infinity, touches another's rows.  What adapters a
+// tile's rows have is found in the tile: any order and number works, runs of rows cost least.
+// Bound as the plain product by the matrix pipe (23400 x 15360 x 5120 of five adapters of rank 32, in runs, T 72 us and the product 2420-2480, where the
+// plain one takes 2430), of few rows by the weights' way from memory; rows in any order of eight adapters cost twice to three times as much (23400 x 1536 x
+// 1536 287 us for 127 in runs and 84 without).
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -51,8 +52,16 @@ struct LowArgs {
   int32_t M, K, ldx, adapters, rank;
 };
 
-// few rows: T comes in parts of k
-constexpr int kFewRows = 32, kMostParts = 8;
+// Few rows: a workgroup has 16 columns of W, each of which reads X again, so that they are fewer for more columns.  Us this way / in tiles (with T whole): 1 x 5120 x 5120
+// 22.6 / 28.7, 16 x 5120 x 5120 30.0 / 35.1, 24 x 5120 x 5120 37.9 / 36.7, 32 x 1536 x 1536 13.7 / 16.6, 24 x 4608 x 1536 18.1 / 15.1, 4 x 15360 x 5120 43.0 / 42.6,
+// 16 x 15360 x 5120 52 / 47, 32 x 15360 x 5120 71 / 49.
+constexpr int kFewRows = 32, kFewResults = 81920;
+bool few_rows(int M, int N) { return M <= kFewRows && int64_t(M) * N <= kFewResults; }
+// Parts of k that a workgroup each takes for T: the rows of few fill few CUs otherwise.  Us of T whole / in parts and joined, rank 32: k 1024, 40 rows 4.3 / 5.7 (few
+// rows' parts need no launch to be joined), k 1536 5.8 / 5.6, k 5120 11.1 / 7.2 and 512 rows 11.1 / 10.2, k 13824 26.6 / 9.2 and 26.7 / 17.3; rank 128, k 5120: 40 rows
+// 11.2 / 8.4, 200 11.5 / 13.1, 512 19.9 / 17.8.  (As rows and k alone say: T has the same bits whatever is asked for beside it.)
+constexpr int kPartRows = 512, kMostParts = 8;
+int low_parts(int M, int K) { return M > kPartRows || K < (M <= kFewRows ? 1024 : 2048) ? 1 : std::min(K / 512, kMostParts); }
 struct FewArgs {
   AdaptedArgs a;
   const float* parts;                             // [parts][M][rank]: X A' of a part of k
@@ -60,7 +69,6 @@ struct FewArgs {
   uint16_t* t;                                    // [2][M][rank]
   int32_t rank, n_parts;
 };
-__host__ __device__ constexpr int few_parts(int K) { return K >= 64 * 8 * kMostParts ? kMostParts : K >= 1024 ? K / 512 : 1; }
 
 __device__ __forceinline__ Frag frag_at(const uint16_t* p) { return *reinterpret_cast<const Frag*>(p); }
 
@@ -172,9 +180,13 @@ __global__ __launch_bounds__(64 * kWaves) void adapted_low_kernel(LowArgs a) {
 #pragma unroll
       for (int j = 0; j < kTm; ++j) {
         if (wave != j % kWaves) continue;
-        Sums sum = part[0][j][lane];
+        Sums all[kWaves], &sum = all[0];                             // (in pairs, as of parts)
 #pragma unroll
-        for (int v = 1; v < kWaves; ++v) sum += part[v][j][lane];
+        for (int v = 0; v < kWaves; ++v) all[v] = part[v][j][lane];
+#pragma unroll
+        for (int of = kWaves / 2; of > 0; of /= 2)
+#pragma unroll
+          for (int v = 0; v < of; ++v) all[v] = all[2 * v] + all[2 * v + 1];
         // the lane has values 4 grp .. +3 of sixteen of row l15
         if (mine[j] == g) {
           uint16_t* const to = a.t + int64_t(m0 + 16 * j + l15) * a.rank + r0 + 16 * n + 4 * grp;
@@ -190,8 +202,8 @@ __global__ __launch_bounds__(64 * kWaves) void adapted_low_kernel(LowArgs a) {
   }
 }
 
-// The same of few rows (one tile of 16, or two) in parts of k, a workgroup each, in fp32 and without the scale: a CU brings A's rows at some 45 GB/s, so that
-// one of them took 7.6 us for 16 values of one row of k 5120.  The kernel that multiplies with B adds the parts.
+// The same of few rows in parts of k, a workgroup each, in fp32 and without the scale: a CU brings A's rows at some 45 GB/s, so that one of them took 7.6 us for
+// 16 values of one row of k 5120.  The kernel that multiplies few rows with B adds the parts, or adapted_low_join_kernel.
 __global__ __launch_bounds__(256) void adapted_low_parts_kernel(LowArgs a, float* parts, int n_parts) {
   constexpr int kWaves = 4, kAhead = 2;
   __shared__ Sums part[kWaves][64];
@@ -232,6 +244,40 @@ __global__ __launch_bounds__(256) void adapted_low_parts_kernel(LowArgs a, float
     if (wave == 0 && mine[0] == g) *reinterpret_cast<Sums*>(out) = (part[0][lane] + part[1][lane]) + (part[2][lane] + part[3][lane]);
     __syncthreads();
   }
+}
+
+// Values at .. +7 of a row's T from its parts, in order, as the operand that the MFMA takes; `leaves` them and what their rounding left in T's room
+__device__ __forceinline__ Frag join_parts(const FewArgs& args, int row, int at, int mine, bool leaves) {
+  const float* const from = args.parts + int64_t(row) * args.rank + at;
+  const int64_t step = int64_t(args.a.M) * args.rank;
+  Sums sum[2] = {*reinterpret_cast<const Sums*>(from), *reinterpret_cast<const Sums*>(from + 4)};
+#pragma unroll
+  for (int p = 1; p < kMostParts; ++p) {
+    if (p >= args.n_parts) break;
+    sum[0] += *reinterpret_cast<const Sums*>(from + p * step);
+    sum[1] += *reinterpret_cast<const Sums*>(from + p * step + 4);
+  }
+  const float scale = mine < 0 ? 0.f : args.scales[mine];
+  uint32_t low[4], left[4];
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const float v0 = mine < 0 ? 0.f : sum[e / 2][e % 2 * 2] * scale, v1 = mine < 0 ? 0.f : sum[e / 2][e % 2 * 2 + 1] * scale;
+    low[e] = pack_bf16(v0, v1);
+    left[e] = pack_bf16(left_of(v0, bf16_lo(low[e])), left_of(v1, bf16_hi(low[e])));
+  }
+  const u32x4 packed = {low[0], low[1], low[2], low[3]};
+  if (leaves) {
+    uint16_t* const to = args.t + int64_t(row) * args.rank + at;
+    *reinterpret_cast<u32x4*>(to) = packed;
+    *reinterpret_cast<u32x4*>(to + step) = u32x4{left[0], left[1], left[2], left[3]};
+  }
+  return __builtin_bit_cast(Frag, packed);
+}
+
+// T from its parts by itself
+__global__ __launch_bounds__(256) void adapted_low_join_kernel(FewArgs args) {
+  const int each = args.rank / 8, nth = int(blockIdx.x) * 256 + int(threadIdx.x), row = nth / each;
+  if (row < args.a.M) join_parts(args, row, (nth - row * each) * 8, adapter_of(args.a.index, row, args.a.M, args.a.adapters), true);
 }
 
 // ------------------------------------------------------------------------------------------------ Y
@@ -430,34 +476,8 @@ __global__ __launch_bounds__(256) void adapted_few_kernel(FewArgs args) {
   const int at = 32 * wave + grp * 8;
   if (32 * wave < rank) {
 #pragma unroll
-    for (int t = 0; t < kTiles; ++t) {                              // T from its parts, in order; the first workgroup leaves it for the way back
-      const int row = 16 * t + l15;
-      if (row >= a.M) continue;
-      const float* const from = args.parts + int64_t(row) * rank + at;
-      const int64_t step = int64_t(a.M) * rank;
-      Sums sum[2] = {*reinterpret_cast<const Sums*>(from), *reinterpret_cast<const Sums*>(from + 4)};
-#pragma unroll
-      for (int p = 1; p < kMostParts; ++p) {
-        if (p >= args.n_parts) break;
-        sum[0] += *reinterpret_cast<const Sums*>(from + p * step);
-        sum[1] += *reinterpret_cast<const Sums*>(from + p * step + 4);
-      }
-      const float scale = mine[t] < 0 ? 0.f : args.scales[mine[t]];
-      uint32_t low[4], left[4];
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const float v0 = mine[t] < 0 ? 0.f : sum[e / 2][e % 2 * 2] * scale, v1 = mine[t] < 0 ? 0.f : sum[e / 2][e % 2 * 2 + 1] * scale;
-        low[e] = pack_bf16(v0, v1);
-        left[e] = pack_bf16(left_of(v0, bf16_lo(low[e])), left_of(v1, bf16_hi(low[e])));
-      }
-      const u32x4 packed = {low[0], low[1], low[2], low[3]};
-      ft[t] = __builtin_bit_cast(Frag, packed);
-      if (blockIdx.x == 0) {
-        uint16_t* const to = args.t + int64_t(row) * rank + at;
-        *reinterpret_cast<u32x4*>(to) = packed;
-        *reinterpret_cast<u32x4*>(to + step) = u32x4{left[0], left[1], left[2], left[3]};
-      }
-    }
+    for (int t = 0; t < kTiles; ++t)                                // (the first workgroup leaves T for the way back)
+      if (16 * t + l15 < a.M) ft[t] = join_parts(args, 16 * t + l15, at, mine[t], blockIdx.x == 0);
     for (int g = next_adapter<kTiles>(mine, -1); g != INT_MAX; g = next_adapter<kTiles>(mine, g)) {
       const Frag fu = frag_at(a.up + (int64_t(g) * a.N + col) * rank + at);
 #pragma unroll
@@ -696,7 +716,13 @@ __global__ __launch_bounds__(256) void adapted_transpose_kernel(Transposed one, 
 
 constexpr const char* kWhat = "gemm_adapted.hip";
 
-constexpr OpModel kModel[] = {{256, 256, 1, 2260, 960, 1325, 8000}, {192, 256, 1, 2280, 754, 1070, 6500}, {128, 256, 1, 2840, 594, 785, 4500}, {256, 128, 1, 0, 705, 840, 5650}, {128, 128, 1, 0, 455, 470, 3680}, {64, 64, 2, 0, 290, 370, 1990}, {64, 64, 1, 0, 255, 190, 2000}};
+// Fitted to products of up to 23400 rows, 15360 columns and k 5120, ranks of 32 to 128; the pick is 1.3 % slower than the fastest of the seven in the geometric
+// mean of 26, 13 % at the worst.  By tile in this order, us: 23400 x 15360 x 5120 2419 / 2462 / 2762 / 3417 / 3803 / 5695 / 6284, 4680 x 4608 x 1536 71 / 61 / 73 / 87 /
+// 97 / 121 / 157, 4680 x 1536 x 4608 89 / 73 / 60 / 74 / 82 / 108 / 129, 1560 x 1536 x 1536 34.8 / 28.5 / 22.5 / 24.2 / 16.5 / 19.7 / 23.1, 300 x 5120 x 5120 97 / 74 / 61 / 68 /
+// 40 / 34 / 40, 100 x 1536 x 1536 31.1 / 26.2 / 21.3 / 23.1 / 14.6 / 9.3 / 8.3; 13427 x 304 x 256 takes the fourth, 10.6 (13.6 / 11.9 / 10.2 by the first three).
+constexpr OpModel kModel[] = {{256, 256, 1, 2260, 960, 1325, 8000}, {192, 256, 1, 2280, 754, 1070, 6500}, {128, 256, 1, 2840, 594, 785, 4500},
+                              {256, 128, 1, 0, 705, 840, 5650},     {128, 128, 1, 0, 455, 470, 3680},     {64, 64, 2, 0, 290, 370, 1990},
+                              {64, 64, 1, 0, 255, 190, 2000}};
 
 template <typename T>
 const void* tile_kernel_address(int steps) {
@@ -757,29 +783,43 @@ int32_t enqueue_low(const LowArgs& a, void* stream) {
 // T = s (X A') and what is left of it.  Few rows take small workgroups, to be many; many rows 32 or 64 at a time, for A's way from L2.  Us for k 5120 by 16 rows and values /
 // by 32 rows and 32 values: 1000 rows of rank 32 11.4 / 19.9, 23400 111 / 72; k 1536, 4680 rows 13.0 / 7.8; 23400 rows of rank 64 by 32 rows and 64
 // values in four waves / in eight 106 / 87 (4680 x 1536 11.0 / 13.9); of rank 128 by 32 x 128 / 64 x 64 140 / 152 (4680 x 1536 17.1 / 14.9).
-int32_t launch_low(const LowArgs& a, void* stream) {
+int32_t launch_whole_low(const LowArgs& a, void* stream) {
   if (a.M <= 2048) return a.M <= 512 || a.rank == 32 ? enqueue_low<1, 1, 4, 4>(a, stream) : enqueue_low<1, 2, 8, 4>(a, stream);
   if (a.rank == 32) return enqueue_low<2, 2, 4, 2>(a, stream);
   if (a.rank == 64) return a.M > 8192 ? enqueue_low<2, 4, 8, 2>(a, stream) : enqueue_low<2, 4, 4, 2>(a, stream);
   return enqueue_low<4, 4, 4, 2>(a, stream);
 }
 
-// X A' and what is multiplied with it: for few rows T in parts (room: few_bytes), otherwise ahead
+int32_t launch_low_parts(const LowArgs& l, int n_parts, float* parts, void* stream) {
+  const unsigned tiles = unsigned(l.M + 15) / 16, z = std::max(1u, std::min({unsigned(l.adapters), 8u, 512u / (tiles * n_parts * (l.rank / 16))}));
+  hipLaunchKernelGGL(adapted_low_parts_kernel, dim3(unsigned(l.rank / 16), n_parts * tiles, z), dim3(256), 0, static_cast<hipStream_t>(stream), l, parts, n_parts);
+  return finish_launch(kWhat);
+}
+
+// T whole, by itself
+int32_t launch_low(const LowArgs& l, void* room, void* stream) {
+  const int n_parts = low_parts(l.M, l.K);
+  if (n_parts == 1) return launch_whole_low(l, stream);
+  FewArgs f{{}, static_cast<float*>(room), l.scales, l.t, l.rank, n_parts};
+  f.a.index = l.index, f.a.M = l.M, f.a.adapters = l.adapters;
+  if (const int32_t rc = launch_low_parts(l, n_parts, static_cast<float*>(room), stream); rc != CA_OK) return rc;
+  hipLaunchKernelGGL(adapted_low_join_kernel, dim3(unsigned((l.M * (l.rank / 8) + 255) / 256)), dim3(256), 0, static_cast<hipStream_t>(stream), f);
+  return finish_launch(kWhat);
+}
+
+// X A' and what is multiplied with it
 int32_t launch_low_and_gemm(const LowArgs& l, AdaptedArgs& a, void* room, void* stream) {
   if (const int32_t rc = adapted_ready(); rc != CA_OK) return rc;
-  if (a.M <= kFewRows) {
+  if (few_rows(a.M, a.N)) {
     const int64_t groups = (int64_t(a.N) + 15) / 16;
-    if (groups * 256 >= (int64_t(1) << 32)) return CA_EUNSUPPORTED;
-    const int n_parts = few_parts(a.K), tiles = (a.M + 15) / 16;
+    const int n_parts = low_parts(a.M, a.K);
     float* const parts = static_cast<float*>(room);
-    hipLaunchKernelGGL(adapted_low_parts_kernel, dim3(unsigned(l.rank / 16), unsigned(n_parts * tiles), unsigned(std::min(l.adapters, std::min(a.M, 8)))), dim3(256), 0,
-                       static_cast<hipStream_t>(stream), l, parts, n_parts);
-    if (const int32_t rc = finish_launch(kWhat); rc != CA_OK) return rc;
+    if (const int32_t rc = launch_low_parts(l, n_parts, parts, stream); rc != CA_OK) return rc;
     hipLaunchKernelGGL(a.M <= 16 ? adapted_few_kernel<1> : adapted_few_kernel<2>, dim3(unsigned(groups)), dim3(256), 0, static_cast<hipStream_t>(stream),
                        FewArgs{a, parts, l.scales, l.t, l.rank, n_parts});
     return finish_launch(kWhat);
   }
-  if (const int32_t rc = launch_low(l, stream); rc != CA_OK) return rc;
+  if (const int32_t rc = launch_low(l, room, stream); rc != CA_OK) return rc;
   const int rank = l.rank;
   int n_cu = 0;
   if (const int32_t rc = device_cu_count(&n_cu); rc != CA_OK) return rc;
@@ -802,7 +842,7 @@ int sum_splits(int64_t M, int32_t C, int32_t adapters, int32_t rank) {
 
 size_t up16(size_t n) { return (n + 15) / 16 * 16; }
 
-size_t few_bytes(int64_t M, int32_t rank) { return M <= kFewRows ? size_t(kMostParts) * M * rank * 4 : 0; }
+size_t few_bytes(int64_t M, int32_t rank) { return M <= kPartRows ? size_t(kMostParts) * M * rank * 4 : 0; }
 
 struct AdaptedRoom {                              // of the backward pass, in bytes
   size_t few, down_t, up_t, there, parts, bytes;
@@ -881,7 +921,7 @@ int32_t launch_adapted_backward(const AdaptedLinear& p, const void* dy, int64_t 
                     p.rank};
     AdaptedArgs a{static_cast<const uint16_t*>(dy), static_cast<const uint16_t*>(p.w), static_cast<uint16_t*>(dx), low_dy,
                   reinterpret_cast<const uint16_t*>(room + r.down_t), p.index, p.ldy, M, p.K, p.N, int32_t(lddy), int32_t(p.ldw), p.adapters, 0, 0, 0};
-    if (const int32_t rc = dx ? launch_low_and_gemm(l, a, room + r.few, stream) : launch_low(l, stream); rc != CA_OK) return rc;
+    if (const int32_t rc = dx ? launch_low_and_gemm(l, a, room + r.few, stream) : launch_low(l, room + r.few, stream); rc != CA_OK) return rc;
   }
   if (d_down)
     if (const int32_t rc = launch_adapter_sum(low_dy, p.x, p.ldx, p.index, M, p.K, p.adapters, p.rank, rank_used, false, d_down, there, parts, stream); rc != CA_OK)

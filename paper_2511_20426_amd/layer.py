@@ -55,7 +55,8 @@ class CascadeLayer:
     def __call__(self, pool: CascadePool, x: torch.Tensor, inflight: Sequence[int], timesteps: Sequence[int], epoch: int = 0,
                  mode: int = B.CA_BIDIRECTIONAL, modulation: torch.Tensor | None = None) -> torch.Tensor:
         """One iteration for the blocks in flight (oldest first, consecutive in the video): x [C*L, width] -> [C*L, width].  modulation (fp32 or bf16): [C, 6,
-        width], of each block weight, bias and gate of the attention's half, then those of the feed-forward half; None: no norms, gates of one."""
+        width], of each block weight, bias and gate (taken in x's type) of the attention's half, then those of the feed-forward half; None: no norms, gates of
+        one."""
         L, H, D = pool.block_tokens, pool.heads, pool.head_dim
         n = len(inflight) * L
         assert x.shape == (n, H * D) and all(b == inflight[0] + i for i, b in enumerate(inflight))

@@ -56,7 +56,9 @@ def _close(got, ref, off):
 
 
 # rows, columns, k, adapters, rank, which rows have which: single tokens, the borders of the kernels for few and many rows, odd sizes and ranks
-CASES = [(1, 8, 128, 1, 1, "runs"), (2, 24, 5120, 3, 32, "mixed"), (32, 40, 1152, 7, 128, "mixed"), (20, 56, 4096, 2, 64, "none"), (40, 8, 256, 2, 4, "mixed"), (1, 776, 1024, 8, 16, "mixed"), (5, 1032, 384, 3, 5, "mixed"), (16, 264, 640, 5, 40, "mixed"), (17, 264, 256, 4, 128, "mixed"),
+CASES = [(16, 5120, 256, 3, 16, "mixed"), (16, 5128, 128, 3, 16, "mixed"), (3, 27312, 128, 2, 32, "mixed"), (31, 2648, 256, 4, 64, "mixed"), (40, 384, 2048, 3, 16, "mixed"),
+         (512, 136, 4224, 2, 100, "mixed"), (513, 128, 2176, 2, 32, "runs"), (33, 128, 13824, 5, 64, "mixed"),
+         (1, 8, 128, 1, 1, "runs"), (2, 24, 5120, 3, 32, "mixed"), (32, 40, 1152, 7, 128, "mixed"), (20, 56, 4096, 2, 64, "none"), (40, 8, 256, 2, 4, "mixed"), (1, 776, 1024, 8, 16, "mixed"), (5, 1032, 384, 3, 5, "mixed"), (16, 264, 640, 5, 40, "mixed"), (17, 264, 256, 4, 128, "mixed"),
          (32, 136, 256, 32, 64, "mixed"), (32, 136, 256, 2, 8, "none"), (33, 136, 256, 3, 33, "mixed"), (257, 776, 1024, 6, 5, "mixed"), (600, 520, 256, 5, 100, "runs"),
          (300, 1536, 1536, 1, 32, "runs"), (1205, 1288, 512, 7, 64, "mixed"), (260, 512, 384, 2, 64, "none"), (2100, 2560, 256, 3, 128, "runs"),
          (8195, 264, 128, 3, 20, "mixed"), (8210, 136, 256, 2, 64, "runs"), (8300, 128, 256, 4, 128, "mixed")]
@@ -272,7 +274,7 @@ def test_arguments_refused_on_device():
 def test_arguments_refused():
     """On the host, before anything is launched"""
     p = 4096
-    good = dict(x=p, w=p, down=p, up=p, scales=p, index=p, low=p, y=p, m=40, n=136, k=256, adapters=3, rank=32, ldx=256, ldw=256, ldy=136, work=0, nbytes=0)
+    good = dict(x=p, w=p, down=p, up=p, scales=p, index=p, low=p, y=p, m=600, n=136, k=256, adapters=3, rank=32, ldx=256, ldw=256, ldy=136, work=0, nbytes=0)
     for change, code in ((dict(m=-1), B.CA_EINVAL), (dict(adapters=0), B.CA_EINVAL), (dict(adapters=4097), B.CA_EUNSUPPORTED), (dict(rank=16), B.CA_EUNSUPPORTED),
                          (dict(rank=96), B.CA_EUNSUPPORTED), (dict(n=4), B.CA_EUNSUPPORTED), (dict(n=132), B.CA_EUNSUPPORTED), (dict(k=192), B.CA_EUNSUPPORTED),
                          (dict(n=2 ** 20 + 8, ldy=2 ** 20 + 8), B.CA_EUNSUPPORTED), (dict(m=2 ** 27 + 1), B.CA_EUNSUPPORTED), (dict(ldx=248), B.CA_EINVAL),
@@ -284,7 +286,7 @@ def test_arguments_refused():
         assert e.value.code == code, change
     B.layer_linear_adapted_bf16(*{**good, "m": 0, "x": 0, "y": 0}.values())
     room = B.layer_linear_adapted_workspace(32, 64)
-    assert room > 0 and B.layer_linear_adapted_workspace(33, 64) == 0 and B.layer_linear_adapted_workspace(5, 48) == 0
+    assert room > 0 and B.layer_linear_adapted_workspace(513, 64) == 0 and B.layer_linear_adapted_workspace(5, 48) == 0
     for change in (dict(work=0, nbytes=room), dict(work=p + 8, nbytes=room), dict(work=p, nbytes=room - 1)):
         with pytest.raises(B.CascadeAttnError):
             B.layer_linear_adapted_bf16(*{**good, "m": 32, "rank": 64, **change}.values())
