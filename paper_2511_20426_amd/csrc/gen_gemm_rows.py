@@ -264,6 +264,10 @@ def adapter_lines(mt):
         out += [f"v_add_u32 {V(AT)}, {16 * tj}, {V(AL)}", f"v_cmp_ge_u32 vcc, s{S_LIM}, {V(AT)}", "s_nop 1",
                 f"v_cndmask_b32 {V(INDEX + tj)}, -1, {V(INDEX + tj)}, vcc", f"v_cmp_gt_u32 vcc, %[adapters], {V(INDEX + tj)}", "s_nop 1",
                 f"v_cndmask_b32 {V(INDEX + tj)}, -1, {V(INDEX + tj)}, vcc"]
+    # (rows without an adapter ask for nothing: no load may be on its way behind the end)
+    out.append(f"v_and_b32 {V(AT)}, {V(INDEX)}, {V(INDEX + 1)}")
+    out += [f"v_and_b32 {V(AT)}, {V(AT)}, {V(INDEX + tj)}" for tj in range(2, mt)]
+    out += [f"v_cmp_gt_u32 vcc, -1, {V(AT)}", "s_nop 3", "s_cmp_eq_u64 vcc, 0", "s_nop 0", "s_cbranch_scc1 ADAPTED_%="]
     out += [f"s_mov_b32 s{S_KK}, 0", "RANK_%=:"]
     for tj in range(mt):
         out += [f"v_add_u32 {V(AT)}, {16 * tj}, {V(AL)}", f"v_min_u32 {V(AT)}, s{S_LIM}, {V(AT)}", f"v_mul_u32_u24 {V(AT)}, %[rank2], {V(AT)}",

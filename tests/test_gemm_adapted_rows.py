@@ -56,6 +56,7 @@ class _Wave:
     def run(self):
         signed = lambda x: np.where(np.asarray(x) & 0x80000000, np.asarray(x, dtype=np.int64) - (1 << 32), x)      # noqa: E731
         k, scc, steps, flying = 0, 0, 0, set()
+        self.flying = flying                                         # fragments asked for and not waited for
         lane = np.arange(64)
         while k < len(self.text):
             ln = self.text[k]
@@ -68,7 +69,7 @@ class _Wave:
             if op in ("s_nop",):
                 continue
             if op == "s_waitcnt":
-                flying = set()
+                flying.clear()
             elif op == "s_branch" or (op == "s_cbranch_scc1" and scc):
                 k = self.label[a[0]]
             elif op == "s_cbranch_scc1":
@@ -209,6 +210,20 @@ def test_adapters_join_the_sums(mt, wave, M, N, rank, adapters, tile, how):
     assert all(64 <= n < 128 or rows.INDEX <= n <= rows.LAST_VGPR_ADAPTED for kind, n in w.wrote)
     if how == "one" and 32 * mt * tile[0] + (wave & 1) * 16 * mt < M:
         assert w.loads == 8 * rank // 32                             # an adapter that all rows have is loaded once
+
+
+@pytest.mark.parametrize("mt", [8, 6, 4])
+@pytest.mark.parametrize("rank", [32, 128])
+@pytest.mark.parametrize("of", [set(), {0}, {70}, {0, 200}, {299}])
+def test_no_load_is_left_on_its_way(mt, rank, of):
+    """Whatever rows have an adapter, none included: a fragment that arrives behind the end would overwrite what the tile's results are in by then"""
+    text = [ln.replace("_%=", "") for ln in rows.adapter_lines(mt)]
+    index = np.array([1 if m in of else -1 for m in range(300)])
+    for wave in range(4):
+        for tile in range(-(-300 // (32 * mt))):
+            w = _Wave(mt, wave, text, 300, 256, rank, 2, (tile, 0), index, np.zeros((300, rank)), np.zeros((2, 256, rank)), 3)
+            w.run()
+            assert not w.flying, (wave, tile)
 
 
 @pytest.mark.parametrize("mt", [8, 6, 4])
