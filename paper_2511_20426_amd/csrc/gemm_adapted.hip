@@ -9,7 +9,7 @@
 // for them: with T alone they were 2.35e-3 of their norm off, 1.66e-3 with both, which is their own rounding.)  An adapter's products go to sums of their
 // own and are added for the rows that have it, so that no value of one request's adapter, not even an infinity, touches another's rows.  What adapters a
 // tile's rows have is found in the tile: any order and number works, runs of rows cost least.
-// Bound as the plain product by the matrix pipe (23400 x 15360 x 5120 of five adapters of rank 32, in runs, T 72 us and the product 2420-2480, where the
+// Bound as the plain product by the matrix pipe (23400 x 15360 x 5120 of five adapters of rank 32, in runs, T 59 us and the product 2400-2480, where the
 // plain one takes 2430), of few rows by the weights' way from memory; rows in any order of eight adapters cost twice to three times as much (23400 x 1536 x
 // 1536 287 us for 127 in runs and 84 without).
 #include <hip/hip_runtime.h>
@@ -101,10 +101,11 @@ __device__ __forceinline__ int next_adapter(const int (&mine)[kRows], int after)
 __device__ __forceinline__ float left_of(float x, float rounded) { return fabsf(rounded) <= 0x1.fffffep127f ? x - rounded : 0.f; }
 
 // A workgroup takes 16 kTm rows and 16 kTn values of each; its waves share K in pieces of 128 bytes of a row, which go straight from memory (X) and L2
-// (A) to the registers that the MFMA multiplies from, kAhead pieces on their way; their sums meet in LDS, in order.  Bound by X's way from memory: 23400 x
-// 5120 of rank 32 72 us, 3.4 TB/s of it; fewer rows have fewer of them to a workgroup (launch_low).
-template <int kTm, int kTn, int kWaves, int kAhead>
-__global__ __launch_bounds__(64 * kWaves) void adapted_low_kernel(LowArgs a) {
+// (A) to the registers that the MFMA multiplies from, kAhead pieces on their way; their sums meet in LDS, in order.  Bound by what a CU brings in, X's rows
+// and A's, some 35-40 GB/s whatever is on its way: 23400 x 5120 of rank 32 58 us, 4.1 TB/s of X.
+template <int kTm, int kTn, int kAhead>
+__global__ __launch_bounds__(256) void adapted_low_kernel(LowArgs a) {
+  constexpr int kWaves = 4;
   __shared__ Sums part[kWaves][kTm][64];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, l15 = lane & 15, grp = lane >> 4;
   const int m0 = blockIdx.x * 16 * kTm, r0 = blockIdx.y * 16 * kTn;
@@ -729,9 +730,11 @@ const void* tile_kernel_address(int steps) {
   return reinterpret_cast<const void*>(steps == 1 ? gemm_adapted_kernel<T, 1> : steps == 2 ? gemm_adapted_kernel<T, 2> : gemm_adapted_kernel<T, 4>);
 }
 
+constexpr int kAlone = 80 * 1024;                 // LDS that a workgroup of T asks for beside its sums', to be alone on its CU (launch_whole_low)
+
 // one call of any size readies all kernels for stream capture
 int32_t adapted_ready() {
-  KernelLds kernels[15] = {};
+  KernelLds kernels[22] = {};
   kernels[12] = {reinterpret_cast<const void*>(gemm_adapted_rows_kernel<8>), kRowsLds};
   kernels[13] = {reinterpret_cast<const void*>(gemm_adapted_rows_kernel<6>), kRowsLds};
   kernels[14] = {reinterpret_cast<const void*>(gemm_adapted_rows_kernel<4>), kRowsLds};
@@ -742,7 +745,12 @@ int32_t adapted_ready() {
     kernels[4 * i + 2] = {tile_kernel_address<Tile64>(steps), Tile64::kLds};
     kernels[4 * i + 3] = {tile_kernel_address<Tile64Wide>(steps), Tile64Wide::kLds};
   }
-  return ensure_dynamic_lds(kernels, 15, kLdsAdapted);
+  const void* const low[] = {reinterpret_cast<const void*>(adapted_low_kernel<1, 1, 4>), reinterpret_cast<const void*>(adapted_low_kernel<1, 2, 2>),
+                             reinterpret_cast<const void*>(adapted_low_kernel<2, 2, 2>), reinterpret_cast<const void*>(adapted_low_kernel<4, 2, 2>),
+                             reinterpret_cast<const void*>(adapted_low_kernel<2, 4, 2>), reinterpret_cast<const void*>(adapted_low_kernel<4, 4, 2>),
+                             reinterpret_cast<const void*>(adapted_low_kernel<4, 8, 1>)};
+  for (int i = 0; i < 7; ++i) kernels[15 + i] = {low[i], kAlone};
+  return ensure_dynamic_lds(kernels, 22, kLdsAdapted);
 }
 
 template <typename T>
@@ -771,23 +779,37 @@ int32_t enqueue_adapted_rows(AdaptedArgs& a, int rank, void* stream) {
   return finish_launch(kWhat);
 }
 
-template <int kTm, int kTn, int kWaves, int kAhead>
-int32_t enqueue_low(const LowArgs& a, void* stream) {
+// T = s (X A') and what is left of it, whole.  The shape costs least whose rounds of a workgroup on each of 256 CUs bring in the fewest rows of X and A (and
+// begin, as much again as 1000 values of k).  Workgroups that fit in one round ask for more LDS than half a CU has, so that no two share one: without, two sat
+// on some CUs while others had none (of 220).  Us so / without / as the shape of 32 rows and 32 values (the one for all sizes) is without:
+//   rank 32   1560 x 5120 12.9 / 19.9 / 20.1   3120 x 5120 16.5 / 28.6 / 20.4   7020 x 5120 22.6 / 36.9 / 36.9   12000 x 5120 30.7 / 55 / 38.0   23400 x 5120 - / 58 / 71
+//   rank 64   2340 x 5120 21.1 / 37.3 / 37.3   7020 x 5120 31.9 / 54.5 / 55     12000 x 5120 40 / 40 / 73        23400 x 5120 - / 78 / 122
+//   rank 128  3120 x 5120 31.2 / 55.3          7020 x 5120 46.3 / 46.6          12000 x 5120 61.5 / 61.7         23400 x 5120 - / 126 (64 rows and values 151)
+//   rank 32, k 512: 700 4.2, 4680 4.7, 23400 9.6 (10.2 by 32 rows and values)
+struct LowShape {
+  int rows, values;
+  int32_t (*launch)(const LowArgs& a, unsigned x, unsigned y, void* stream);
+};
+template <int kTm, int kTn, int kAhead>
+int32_t enqueue_low(const LowArgs& a, unsigned x, unsigned y, void* stream) {
   // few rows' adapters are dealt to several workgroups: 257 rows of six in any order, of rank 5 and k 1024 21 us by one of them
-  const unsigned x = unsigned((a.M + 16 * kTm - 1) / (16 * kTm)), y = unsigned(a.rank / (16 * kTn));
   const unsigned z = std::max(1u, std::min({unsigned(a.adapters), 8u, 512u / (x * y)}));
-  hipLaunchKernelGGL((adapted_low_kernel<kTm, kTn, kWaves, kAhead>), dim3(x, y, z), dim3(64 * kWaves), 0, static_cast<hipStream_t>(stream), a);
+  hipLaunchKernelGGL((adapted_low_kernel<kTm, kTn, kAhead>), dim3(x, y, z), dim3(256), x * y <= 256 ? kAlone : 0, static_cast<hipStream_t>(stream), a);
   return finish_launch(kWhat);
 }
+constexpr LowShape kLowShapes[] = {{16, 16, enqueue_low<1, 1, 4>}, {16, 32, enqueue_low<1, 2, 2>}, {32, 32, enqueue_low<2, 2, 2>}, {64, 32, enqueue_low<4, 2, 2>},
+                                   {32, 64, enqueue_low<2, 4, 2>}, {64, 64, enqueue_low<4, 4, 2>}, {64, 128, enqueue_low<4, 8, 1>}};
 
-// T = s (X A') and what is left of it.  Few rows take small workgroups, to be many; many rows 32 or 64 at a time, for A's way from L2.  Us for k 5120 by 16 rows and values /
-// by 32 rows and 32 values: 1000 rows of rank 32 11.4 / 19.9, 23400 111 / 72; k 1536, 4680 rows 13.0 / 7.8; 23400 rows of rank 64 by 32 rows and 64
-// values in four waves / in eight 106 / 87 (4680 x 1536 11.0 / 13.9); of rank 128 by 32 x 128 / 64 x 64 140 / 152 (4680 x 1536 17.1 / 14.9).
 int32_t launch_whole_low(const LowArgs& a, void* stream) {
-  if (a.M <= 2048) return a.M <= 512 || a.rank == 32 ? enqueue_low<1, 1, 4, 4>(a, stream) : enqueue_low<1, 2, 8, 4>(a, stream);
-  if (a.rank == 32) return enqueue_low<2, 2, 4, 2>(a, stream);
-  if (a.rank == 64) return a.M > 8192 ? enqueue_low<2, 4, 8, 2>(a, stream) : enqueue_low<2, 4, 4, 2>(a, stream);
-  return enqueue_low<4, 4, 4, 2>(a, stream);
+  if (const int32_t rc = adapted_ready(); rc != CA_OK) return rc;
+  const LowShape* best = nullptr;
+  int64_t least = 0;
+  for (const LowShape& s : kLowShapes) {
+    if (s.values > a.rank) continue;
+    const int64_t all = (int64_t(a.M) + s.rows - 1) / s.rows * (a.rank / s.values), cost = (all + 255) / 256 * (1000 + int64_t(a.K) * (s.rows + s.values) / 16);
+    if (!best || cost < least) best = &s, least = cost;
+  }
+  return best->launch(a, unsigned((a.M + best->rows - 1) / best->rows), unsigned(a.rank / best->values), stream);
 }
 
 int32_t launch_low_parts(const LowArgs& l, int n_parts, float* parts, void* stream) {
