@@ -9,7 +9,7 @@
 // for them: with T alone they were 2.35e-3 of their norm off, 1.66e-3 with both, which is their own rounding.)  An adapter's products go to sums of their
 // own and are added for the rows that have it, so that no value of one request's adapter, not even an infinity, touches another's rows.  What adapters a
 // tile's rows have is found in the tile: any order and number works, runs of rows cost least.
-// Bound as the plain product by the matrix pipe (23400 x 15360 x 5120 of five adapters of rank 32, in runs, T 59 us and the product 2400-2480, where the
+// Bound as the plain product by the matrix pipe (23400 x 15360 x 5120 of five adapters of rank 32, in runs, T 72 us and the product 2400-2480, where the
 // plain one takes 2430), of few rows by the weights' way from memory; rows in any order of eight adapters cost twice to three times as much (23400 x 1536 x
 // 1536 287 us for 127 in runs and 84 without).
 #include <hip/hip_runtime.h>
@@ -102,7 +102,7 @@ __device__ __forceinline__ float left_of(float x, float rounded) { return fabsf(
 
 // A workgroup takes 16 kTm rows and 16 kTn values of each; its waves share K in pieces of 128 bytes of a row, which go straight from memory (X) and L2
 // (A) to the registers that the MFMA multiplies from, kAhead pieces on their way; their sums meet in LDS, in order.  Bound by what a CU brings in, X's rows
-// and A's, some 35-40 GB/s whatever is on its way: 23400 x 5120 of rank 32 58 us, 4.1 TB/s of X.
+// and A's, some 35-40 GB/s whatever is on its way: 23400 x 5120 of rank 32 71 us, 3.4 TB/s of X.
 template <int kTm, int kTn, int kAhead>
 __global__ __launch_bounds__(256) void adapted_low_kernel(LowArgs a) {
   constexpr int kWaves = 4;
@@ -780,12 +780,13 @@ int32_t enqueue_adapted_rows(AdaptedArgs& a, int rank, void* stream) {
 }
 
 // T = s (X A') and what is left of it, whole.  The shape costs least whose rounds of a workgroup on each of 256 CUs bring in the fewest rows of X and A (and
-// begin, as much again as 1000 values of k).  Workgroups that fit in one round ask for more LDS than half a CU has, so that no two share one: without, two sat
-// on some CUs while others had none (of 220).  Us so / without / as the shape of 32 rows and 32 values (the one for all sizes) is without:
-//   rank 32   1560 x 5120 12.9 / 19.9 / 20.1   3120 x 5120 16.5 / 28.6 / 20.4   7020 x 5120 22.6 / 36.9 / 36.9   12000 x 5120 30.7 / 55 / 38.0   23400 x 5120 - / 58 / 71
-//   rank 64   2340 x 5120 21.1 / 37.3 / 37.3   7020 x 5120 31.9 / 54.5 / 55     12000 x 5120 40 / 40 / 73        23400 x 5120 - / 78 / 122
-//   rank 128  3120 x 5120 31.2 / 55.3          7020 x 5120 46.3 / 46.6          12000 x 5120 61.5 / 61.7         23400 x 5120 - / 126 (64 rows and values 151)
-//   rank 32, k 512: 700 4.2, 4680 4.7, 23400 9.6 (10.2 by 32 rows and values)
+// begin, as much again as 1000 values of k); several rounds cost 1.2 of them more, for their ends.  A workgroup asks for more LDS than half a CU has, so that
+// no two share one: without, two sat on some CUs while others had none (of 220).  Us so / without / as 32 rows and 32 values (once the shape for all sizes) without:
+//   rank 32   1560 x 5120 12.9 / 19.9 / 20.1   3120 x 5120 16.5 / 28.6 / 20.4   7020 x 5120 22.6 / 36.9 / 36.9   12000 x 5120 30.7 / 55 / 38.0
+//   rank 64   2340 x 5120 21.1 / 37.3 / 37.3   7020 x 5120 31.9 / 54.5 / 55     rank 128  3120 x 5120 31.2 / 55.3
+// Several rounds behind a product of the same sizes, X from memory, by (rows, values): 23400 x 5120 of rank 32 (32, 32) 71 / 84-90, (64, 32) 96 / 97; of rank 64 (32, 64)
+// 99 / 119, (64, 64) 127 / 126; of rank 128 (64, 64) 164 / 165, (64, 128) 195 / 196; 46800 x 5120 of rank 32 145 / 148 and 129 / 148, of rank 64 201 / 197 and 153 / 153, of
+// rank 128 294 / 295 and 241 / 243.
 struct LowShape {
   int rows, values;
   int32_t (*launch)(const LowArgs& a, unsigned x, unsigned y, void* stream);
@@ -794,7 +795,7 @@ template <int kTm, int kTn, int kAhead>
 int32_t enqueue_low(const LowArgs& a, unsigned x, unsigned y, void* stream) {
   // few rows' adapters are dealt to several workgroups: 257 rows of six in any order, of rank 5 and k 1024 21 us by one of them
   const unsigned z = std::max(1u, std::min({unsigned(a.adapters), 8u, 512u / (x * y)}));
-  hipLaunchKernelGGL((adapted_low_kernel<kTm, kTn, kAhead>), dim3(x, y, z), dim3(256), x * y <= 256 ? kAlone : 0, static_cast<hipStream_t>(stream), a);
+  hipLaunchKernelGGL((adapted_low_kernel<kTm, kTn, kAhead>), dim3(x, y, z), dim3(256), kAlone, static_cast<hipStream_t>(stream), a);
   return finish_launch(kWhat);
 }
 constexpr LowShape kLowShapes[] = {{16, 16, enqueue_low<1, 1, 4>}, {16, 32, enqueue_low<1, 2, 2>}, {32, 32, enqueue_low<2, 2, 2>}, {64, 32, enqueue_low<4, 2, 2>},
@@ -806,7 +807,8 @@ int32_t launch_whole_low(const LowArgs& a, void* stream) {
   int64_t least = 0;
   for (const LowShape& s : kLowShapes) {
     if (s.values > a.rank) continue;
-    const int64_t all = (int64_t(a.M) + s.rows - 1) / s.rows * (a.rank / s.values), cost = (all + 255) / 256 * (1000 + int64_t(a.K) * (s.rows + s.values) / 16);
+    const int64_t all = (int64_t(a.M) + s.rows - 1) / s.rows * (a.rank / s.values), rounds = (all + 255) / 256;
+    const int64_t cost = (10 * rounds + (rounds > 1 ? 12 : 0)) * (1000 + int64_t(a.K) * (s.rows + s.values) / 16);
     if (!best || cost < least) best = &s, least = cost;
   }
   return best->launch(a, unsigned((a.M + best->rows - 1) / best->rows), unsigned(a.rank / best->values), stream);
